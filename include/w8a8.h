@@ -441,6 +441,133 @@ w8a8_status w8a8_stream_gemm_plan(int int8_weights, int M, int N, int K, int sms
  * sms < 2; W8A8_ERR_SHAPE where the GEMM does not take the shape (K or N not a multiple of 16). */
 w8a8_status w8a8_tc_gemm_plan(int mode, int M, int N, int K, int kind, int split_ok, int sms, int* out);
 
+/* ======================================================================================
+ * Operators of a serving step (no counterpart in the paper, whose timings decode one uniform
+ * batch): sequences of different lengths in one call, their keys and values in pages that a
+ * caller hands out as they grow, rotary positions beyond the decoder's two tables, and a sampled
+ * next token.  w8a8_decoder_step_paged runs them together.
+ * ====================================================================================== */
+enum { W8A8_TYPE_BF16 = 0, W8A8_TYPE_F16 = 1, W8A8_TYPE_F32 = 2 };
+
+/* ------------------------------------------------------------------------ rotary positions
+ * Frequencies (radians a position) of the rotary_dim / 2 pairs, f_i = base^(-2 i / rotary_dim), scaled
+ * for contexts longer than the ones a model was trained on (original_len, n = original_len f / 2 pi
+ * the turns a pair makes over it):
+ *   NONE        f
+ *   LINEAR      f / factor
+ *   WAVELENGTH  f (m + (1 - m) / factor), m = clamp((n - low) / (high - low), 0, 1)
+ *   PARTS       f ((1 - r) + r / factor), r = clamp((i - a) / max(b - a, 0.001), 0, 1) between the pair indices
+ *               a = max(0, floor(at(high))) and b = min(rotary_dim - 1, ceil(at(low))) of
+ *               at(x) = rotary_dim ln(original_len / (2 pi x)) / (2 ln base)
+ * attn_factor multiplies cos and sin; 0 stands for 1, and for 0.1 ln(factor) + 1 under PARTS. */
+enum { W8A8_ROPE_NONE = 0, W8A8_ROPE_LINEAR = 1, W8A8_ROPE_WAVELENGTH = 2, W8A8_ROPE_PARTS = 3 };
+typedef struct {
+  int32_t rotary_dim; /* rotated dims of a head: a multiple of 16, at most 256 */
+  int32_t scaling;
+  double base;        /* > 1 */
+  double factor, low, high, attn_factor;
+  int32_t original_len;
+} w8a8_rope_cfg;
+
+/* Host only: turns[i] (HOST array, rotary_dim / 2 values) = f_i / (2 pi) as a fraction of 2^64, so that the
+ * angle of any 32-bit position is one wrapping 64-bit product, reduced without error; *scale = the factor on
+ * cos and sin.  W8A8_ERR_SHAPE for a rotary_dim that is not a multiple of 16 in [16, 256], W8A8_ERR_INVALID_ARG
+ * for a null pointer or parameters outside their domain (base <= 1, factor <= 0, high <= low where they are used,
+ * original_len <= 0 where it is). */
+w8a8_status w8a8_rope_frequencies(const w8a8_rope_cfg* cfg, uint64_t* turns, float* scale);
+
+typedef struct {
+  int32_t rotary_dim;
+  int32_t interleaved;   /* 0: dims (i, i + rotary_dim / 2) make pair i; 1: dims (2 i, 2 i + 1) */
+  float scale;           /* on cos and sin */
+  const uint64_t* turns; /* device [rotary_dim / 2], from w8a8_rope_frequencies */
+} w8a8_rope_table;
+
+/* y = x with every head's first rotary_dim dims rotated by its row's position, the others copied:
+ *   (a, b) -> (a c - b s, b c + a s) with c, s = scale cos, scale sin of 2 pi frac(position turns / 2^64)
+ * in fp32, rounded once to the type (bf16 or fp16).  x and y [T, heads, dim] with strides in elements
+ * (multiples of 8); dim a multiple of 16 in [rotary_dim, 256].  y may be x itself (the same pointer and strides); any other overlap,
+ * of the two or of y's own rows, is not allowed.  positions [T] int32, any value. */
+w8a8_status w8a8_rope(const w8a8_rope_table* rope, int dtype, const uint16_t* x, int64_t x_row, int64_t x_head, int T,
+                      int heads, int dim, const int32_t* positions, uint16_t* y, int64_t y_row, int64_t y_head,
+                      void* stream);
+
+/* -------------------------------------------------------------------------- paged cache
+ * Keys and values in pages of page_size slots: k and v [n_pages, page_size, n_kv, head_dim] with common strides
+ * in elements (multiples of 8, dims contiguous), so that either order of slots and heads, or both tensors
+ * in one, can be described.  page_size 16, 32, 64, 128 or 256; head_dim 64, 128 or 256. */
+typedef struct {
+  int32_t dtype; /* W8A8_TYPE_BF16 or W8A8_TYPE_F16 */
+  int32_t n_pages, page_size, n_kv, head_dim;
+  int64_t page_stride, slot_stride, head_stride;
+  uint16_t *k, *v;
+} w8a8_paged_cache;
+
+/* A ragged batch.  Sequence s owns rows [row_start[s], row_start[s + 1]) of the call's n_rows new tokens and, with
+ * them, kv_len[s] keys: its rows sit at the last positions, row i of n at kv_len[s] - n + i.  Position p lies in
+ * slot p % page_size of page pages[s, p / page_size].  All three arrays are DEVICE memory and may be written by
+ * earlier work on the stream; the host needs bounds only.  Checked on the device: rows outside
+ * [row_start[0], row_start[n_seqs]) belong to no sequence, and their outputs are left as they were; a page id outside
+ * [0, n_pages) (or past max_pages) holds no keys and takes none; a row at a negative position has no keys. */
+typedef struct {
+  int32_t n_seqs, n_rows;
+  int32_t max_new;   /* the most rows any sequence has, at least 1 (a longer one costs time only) */
+  int32_t max_pages; /* columns of pages */
+  const int32_t* row_start; /* [n_seqs + 1], not decreasing, within [0, n_rows] */
+  const int32_t* kv_len;    /* [n_seqs] */
+  const int32_t* pages;     /* [n_seqs, max_pages] */
+} w8a8_paged_batch;
+
+/* The rows of a q/k/v projection into their places: q heads to q_out, k heads to the cache, both after RMSNorm over the
+ * head (x / sqrt(mean x^2 + eps) * norm, where the fp32 [head_dim] weights are given) and rotation by the row's
+ * position, rounded once; v heads to the cache as they are.  q [n_rows, n_q, head_dim], k and v
+ * [n_rows, n_kv, head_dim], heads contiguous, row strides in elements (multiples of 8); q_out [n_rows, n_q, head_dim]
+ * with its row stride, q itself allowed.  Everything has the cache's type.  Rows that share a slot (a page id twice in
+ * one batch) leave either one's values there. */
+w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache* cache, const w8a8_paged_batch* batch,
+                             const uint16_t* q, int64_t q_row, int n_q, const uint16_t* k, int64_t k_row,
+                             const uint16_t* v, int64_t v_row, const float* q_norm, const float* k_norm, float eps,
+                             uint16_t* q_out, int64_t q_out_row, void* stream);
+
+/* Attention of every row over its sequence's cached keys (its own included: append first):
+ *   o = sum_j softmax_j(scale q . k_j) v_j over the keys j of its sequence with p - window < j <= p (window 0: all
+ *   j <= p), p the row's position; query head h reads key/value head h / (n_q / n_kv).
+ * A row without keys gets zeros.  A key outside a row's range, and slots that hold none, never reach it, whatever
+ * their values; keys within it propagate NaN and infinities as the formula does.  Scores, softmax and sums
+ * in fp32; a weight (at most e^5.5) is rounded once to the type before it meets v, and the sum that divides the
+ * output is that of the rounded weights; the output is rounded once.  Deterministic.
+ * q and o [n_rows, n_q, head_dim] of the cache's type, strides in elements (multiples of 8); n_q a multiple of n_kv,
+ * at most 128 query heads per key/value head; o overlaps no input. */
+w8a8_status w8a8_paged_attention_workspace_size(const w8a8_paged_cache* cache, int n_q, size_t* bytes);
+w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged_batch* batch, const uint16_t* q,
+                                 int64_t q_row, int64_t q_head, int n_q, float scale, int window, uint16_t* o,
+                                 int64_t o_row, int64_t o_head, void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------ sampling
+ * One token a row from logits [M, V] (fp32, bf16 or fp16; row stride in elements) and one uniform number u in
+ * [0, 1) a row.  Weights w_i = e^((l_i - max l) / temperature), in multiples of 2^-42 and accurate to about 2^-31 of each; NaN and -inf weigh
+ * nothing.  Tokens in descending order of logits, the lower index first among equals:
+ *   top_k  keeps the first top_k (all where top_k <= 0);
+ *   top_p  keeps the shortest prefix of those whose weight reaches top_p of theirs, at least one token (all where
+ *          top_p >= 1 or NaN);
+ *   min_p  keeps those with w_i >= min_p (all where min_p <= 0 or NaN).  The first token is always kept.
+ * The token is the first i, in index order, at which the kept weights sum to more than u times their total; u
+ * outside [0, 1) is taken as its nearest end, NaN as 0.  Sums are exact (64-bit integers), so a result
+ * depends on nothing but the row.  temperature <= 0 or NaN takes the largest logit (the lowest index among
+ * equals); +inf logits share the weight among themselves; a row of NaN and -inf alone gives token -1 and
+ * probability 0.
+ * Per-row parameters: device [M], each pointer nullable (temperature 1, the filters off). */
+#define W8A8_MAX_SAMPLE_VOCAB 1048576
+typedef struct {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+} w8a8_sampling;
+/* tokens [M] int32; probs [M] fp32 (nullable): the token's share of the kept weight. */
+w8a8_status w8a8_sample(int dtype, const void* logits, int64_t row_stride, int M, int V, const w8a8_sampling* sampling,
+                        const float* u, int32_t* tokens, float* probs, void* stream);
+
 /* Negative log-likelihood of targets under softmax(logits) per row (LM Head section's
  * perplexity): nll[i] = logsumexp(logits[i, :]) - logits[i, targets[i]], fp32. */
 w8a8_status w8a8_token_nll(const float* logits, const int32_t* targets, int M, int V, float* nll, void* stream);

@@ -113,7 +113,33 @@ class LayerAllocReportC(ctypes.Structure):
                 ("n_order", ctypes.c_int32), ("n_accepted", ctypes.c_int32)]
 
 
+class RopeCfgC(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("attn_factor", ctypes.c_double), ("original_len", ctypes.c_int32)]
+
+
+class RopeTableC(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float), ("turns", _vp)]
+
+
+class PagedCacheC(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("k", _vp), ("v", _vp)]
+
+
+class PagedBatchC(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("row_start", _vp), ("kv_len", _vp), ("pages", _vp)]
+
+
+class SamplingC(ctypes.Structure):
+    _fields_ = [("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp)]
+
+
 _fp = ctypes.POINTER(ctypes.c_float)
+_i64 = ctypes.c_int64
 
 # name -> (restype, argtypes)
 SIGNATURES = {
@@ -163,6 +189,14 @@ SIGNATURES = {
     "w8a8_stream_gemm_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_int32)]),
     "w8a8_tc_gemm_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_int32)]),
     "w8a8_model_set_trace": (_i32, [_vp, ctypes.POINTER(TraceC)]),
+    "w8a8_rope_frequencies": (_i32, [ctypes.POINTER(RopeCfgC), ctypes.POINTER(ctypes.c_uint64), _fp]),
+    "w8a8_rope": (_i32, [ctypes.POINTER(RopeTableC), _i32, _vp, _i64, _i64, _i32, _i32, _i32, _vp, _vp, _i64, _i64, _vp]),
+    "w8a8_rope_append": (_i32, [ctypes.POINTER(RopeTableC), ctypes.POINTER(PagedCacheC), ctypes.POINTER(PagedBatchC), _vp,
+                                _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]),
+    "w8a8_paged_attention_workspace_size": (_i32, [ctypes.POINTER(PagedCacheC), _i32, ctypes.POINTER(_sz)]),
+    "w8a8_paged_attention": (_i32, [ctypes.POINTER(PagedCacheC), ctypes.POINTER(PagedBatchC), _vp, _i64, _i64, _i32, _f32,
+                                    _i32, _vp, _i64, _i64, _vp, _sz, _vp]),
+    "w8a8_sample": (_i32, [_i32, _vp, _i64, _i32, _i32, ctypes.POINTER(SamplingC), _vp, _vp, _vp, _vp]),
     "w8a8_token_nll": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp]),
     "w8a8_choose_mask": (_i32, [_fp, _fp, _fp, ctypes.POINTER(ctypes.c_int32), _i32, _f32, _f32]),
     "w8a8_allocate_mask": (_i32, [_vp, ctypes.POINTER(AllocOptsC), ctypes.POINTER(AllocReportC), _vp]),
@@ -521,6 +555,218 @@ def lm_head(hd: HeadWeights, precision: int, X: torch.Tensor, want_logits: bool 
             logits: Optional[torch.Tensor] = None, top1: Optional[torch.Tensor] = None,
             ws: Optional[Workspace] = None, stream=None):
     return (_CALLS or _calls()).lm_head(hd, precision, X, want_logits, logits, top1, ws, stream)
+
+
+# --------------------------------------------------------------------- a serving step's operators
+ROPE_SCALINGS = {"none": 0, "linear": 1, "wavelength": 2, "parts": 3}
+TYPE_CODES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _need(cond, msg):
+    if not cond:
+        raise ValueError(msg)
+
+
+def _on(dev, *tensors):
+    for t in tensors:
+        _need(t is None or t.device == dev, f"all tensors must be on {dev}")
+
+
+def _ints(t, name):
+    _need(t.dtype == torch.int32 and t.is_contiguous(), f"{name} must be a contiguous int32 tensor")
+
+
+def _device_of(t):
+    """The tensor's device, which has to be the current one (the library launches there)."""
+    assert t.is_cuda, "tensors must be CUDA tensors"
+    _need(t.device.index == torch.cuda.current_device(), f"the tensors' device {t.device} is not the current one")
+    return t.device
+
+
+@dataclass
+class RopeConfig:
+    """Rotary frequencies (w8a8_rope_cfg); attn_factor 0: the scaling's own."""
+    rotary_dim: int
+    base: float = 10000.0
+    interleaved: bool = False
+    scaling: str = "none"
+    factor: float = 1.0
+    low: float = 1.0
+    high: float = 4.0
+    original_len: int = 0
+    attn_factor: float = 0.0
+
+
+@dataclass
+class RopeTable:
+    rotary_dim: int
+    interleaved: bool
+    scale: float
+    turns: torch.Tensor  # int64 bits of the turns a position makes, as fractions of 2^64
+
+    def c(self) -> RopeTableC:
+        return RopeTableC(self.rotary_dim, int(self.interleaved), self.scale, self.turns.data_ptr())
+
+
+def rope_frequencies(cfg: RopeConfig):
+    """(turns, scale) of w8a8_rope_frequencies: a host int64 tensor of fractions of 2^64, and the factor on cos and sin."""
+    _need(cfg.scaling in ROPE_SCALINGS, f"scaling must be one of {sorted(ROPE_SCALINGS)}")
+    c = RopeCfgC(cfg.rotary_dim, ROPE_SCALINGS[cfg.scaling], cfg.base, cfg.factor, cfg.low, cfg.high, cfg.attn_factor,
+                 cfg.original_len)
+    turns, scale = (ctypes.c_uint64 * 128)(), ctypes.c_float()
+    _check("w8a8_rope_frequencies", lib().w8a8_rope_frequencies(ctypes.byref(c), turns, ctypes.byref(scale)))
+    n = cfg.rotary_dim // 2
+    return torch.tensor([x - (1 << 64) if x >> 63 else x for x in turns[:n]], dtype=torch.int64), scale.value
+
+
+def rope_table(cfg: RopeConfig, device=None) -> RopeTable:
+    """The rotation's constants on the device: built once, used by every call."""
+    turns, scale = rope_frequencies(cfg)
+    return RopeTable(cfg.rotary_dim, bool(cfg.interleaved), scale, turns.to(device or torch.device("cuda")))
+
+
+def rope(table: RopeTable, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None,
+         stream=None) -> torch.Tensor:
+    """x [T, heads, dim] (bf16 or fp16) rotated at positions [T] int32; out=x rotates in place."""
+    dev = _device_of(x)
+    _need(x.dim() == 3 and x.stride(2) == 1 and positions.shape == x.shape[:1], "x [T, heads, dim], positions [T]")
+    _ints(positions, "positions")
+    y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=dev)
+    _need(y.shape == x.shape and y.dtype == x.dtype and y.stride(2) == 1, "out must have x's shape and type")
+    _on(dev, positions, y, table.turns)
+    rc = table.c()
+    _check("w8a8_rope", lib().w8a8_rope(ctypes.byref(rc), TYPE_CODES.get(x.dtype, -1), _p(x), x.stride(0), x.stride(1),
+                                        x.shape[0], x.shape[1], x.shape[2], _p(positions), _p(y), y.stride(0), y.stride(1),
+                                        _stream(stream)))
+    return y
+
+
+@dataclass
+class PagedCache:
+    """Keys and values in pages: k and v [n_pages, page_size, n_kv, head_dim], equal strides, dims contiguous (a
+    head-major pool is passed as its transposed view)."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    def c(self) -> PagedCacheC:
+        k, v = self.k, self.v
+        _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(3) == 1,
+              "k and v [n_pages, page_size, n_kv, head_dim] of equal shape, strides and type, dims contiguous")
+        n, page, heads, dim = k.shape
+        # the stride of an extent of one says nothing: any that the library takes
+        st = [s if e > 1 else max(-(-s // 8) * 8, dim) for s, e in zip(k.stride(), k.shape)]
+        return PagedCacheC(TYPE_CODES.get(k.dtype, -1), n, page, heads, dim, st[0], st[1], st[2], k.data_ptr(), v.data_ptr())
+
+
+@dataclass
+class PagedBatch:
+    """A ragged batch (w8a8_paged_batch): device int32 tensors row_start [n_seqs + 1], kv_len [n_seqs], pages
+    [n_seqs, max_pages], and max_new, the most rows any sequence has."""
+    row_start: torch.Tensor
+    kv_len: torch.Tensor
+    pages: torch.Tensor
+    max_new: int = 1
+
+    def c(self, rows: int) -> PagedBatchC:
+        n = self.kv_len.shape[0]
+        _need(self.row_start.shape == (n + 1,) and self.pages.dim() == 2 and self.pages.shape[0] == n,
+              "row_start [n_seqs + 1], kv_len [n_seqs], pages [n_seqs, max_pages]")
+        for name in ("row_start", "kv_len", "pages"):
+            _ints(getattr(self, name), name)
+        return PagedBatchC(n, rows, self.max_new, self.pages.shape[1], self.row_start.data_ptr(), self.kv_len.data_ptr(),
+                           self.pages.data_ptr())
+
+
+def _rows_of(t, heads, dim, name):
+    """Row stride of [rows, heads, dim] with contiguous heads."""
+    _need(t.dim() == 3 and t.shape[1:] == (heads, dim) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim),
+          f"{name} must be [rows, {heads}, {dim}] with contiguous heads")
+    return t.stride(0) if t.shape[0] > 1 else -(-t.stride(0) // 8) * 8
+
+
+def rope_append(table: RopeTable, cache: PagedCache, batch: PagedBatch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rotated (and, with the norms, RMS-normalised) q heads, returned; k heads likewise and v heads into the
+    cache's pages.  q [rows, n_q, dim], k and v [rows, n_kv, dim]: views of one projection are fine; q_out=q is too."""
+    dev = _device_of(q)
+    cc = cache.c()
+    rows, n_q, dim = q.shape
+    _need(dim == cc.head_dim and k.shape[0] == rows and v.shape[0] == rows, "q, k and v need the cache's head_dim and equal rows")
+    qs, ks, vs = _rows_of(q, n_q, dim, "q"), _rows_of(k, cc.n_kv, dim, "k"), _rows_of(v, cc.n_kv, dim, "v")
+    y = q_out if q_out is not None else torch.empty(q.shape, dtype=q.dtype, device=dev)
+    _need(y.shape == q.shape, "q_out must have q's shape")
+    _need(all(t.dtype == cache.k.dtype for t in (q, k, v, y)), "q, k, v and q_out must have the cache's type")
+    for w in (q_norm, k_norm):
+        _need(w is None or (w.dtype == torch.float32 and w.shape == (dim,) and w.is_contiguous()), "norms must be fp32 [dim]")
+    _on(dev, k, v, y, q_norm, k_norm, cache.k, cache.v, batch.row_start, batch.kv_len, batch.pages, table.turns)
+    rc, bc = table.c(), batch.c(rows)
+    _check("w8a8_rope_append", lib().w8a8_rope_append(
+        ctypes.byref(rc), ctypes.byref(cc), ctypes.byref(bc), _p(q), qs, n_q, _p(k), ks, _p(v), vs, _p(q_norm), _p(k_norm),
+        float(eps), _p(y), _rows_of(y, n_q, dim, "q_out"), _stream(stream)))
+    return y
+
+
+_STREAM_WS = {}
+
+
+def stream_workspace(nbytes: int, dev: torch.device, stream=None) -> torch.Tensor:
+    """Zeroed scratch of calls without a workspace of their own: one per stream, so that calls on different
+    streams do not share one; while a stream is captured, a new one that lives as long as the graph's memory."""
+    s = stream if stream is not None else torch.cuda.current_stream(dev)
+    with torch.cuda.stream(s):
+        if torch.cuda.is_current_stream_capturing():
+            return torch.zeros(nbytes, dtype=torch.uint8, device=dev)
+        key = (dev.index, s.cuda_stream)
+        if key not in _STREAM_WS:
+            _STREAM_WS[key] = Workspace(dev)
+        return _STREAM_WS[key].get(nbytes)
+
+
+def paged_attention(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: Optional[float] = None, window: int = 0,
+                    out: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """Attention of every row over its sequence's cached keys, its own included (append first).  scale defaults to
+    1 / sqrt(head_dim); window 0 sees all earlier keys.  Rows of no sequence: left as they were in `out`."""
+    dev = _device_of(q)
+    cc = cache.c()
+    _need(q.dim() == 3 and q.shape[2] == cc.head_dim and q.stride(2) == 1, "q must be [rows, n_q, head_dim]")
+    rows, n_q, dim = q.shape
+    y = out if out is not None else torch.empty(q.shape, dtype=q.dtype, device=dev)
+    _need(y.shape == q.shape and y.stride(2) == 1 and q.dtype == cache.k.dtype and y.dtype == q.dtype,
+          "q and out must have the cache's type and equal shapes")
+    _on(dev, y, cache.k, cache.v, batch.row_start, batch.kv_len, batch.pages)
+    bc = batch.c(rows)
+    need = _size("w8a8_paged_attention_workspace_size", ctypes.byref(cc), n_q)
+    buf = ws.get(need) if ws is not None else stream_workspace(need, dev, stream)
+
+    def strides(t):  # the stride of an extent of one says nothing: any that the library takes
+        return [s if e > 1 else max(-(-s // 8) * 8, dim) for s, e in zip(t.stride()[:2], t.shape)]
+    _check("w8a8_paged_attention", lib().w8a8_paged_attention(
+        ctypes.byref(cc), ctypes.byref(bc), _p(q), *strides(q), n_q, float(scale if scale is not None else dim ** -0.5),
+        int(window), _p(y), *strides(y), _p(buf), buf.numel(), _stream(stream)))
+    return y
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           want_probs: bool = False, tokens: Optional[torch.Tensor] = None, stream=None):
+    """One token a row of logits [M, V] (fp32, bf16, fp16) from uniform numbers u [M] fp32; per-row parameters [M]
+    (temperature, top_p, min_p fp32, top_k int32; None: 1 and off).  Returns tokens int32 [M], or (tokens, their
+    probabilities among the kept ones) with want_probs."""
+    dev = _device_of(logits)
+    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1) and u.shape == logits.shape[:1],
+          "logits [M, V] with contiguous rows, u [M]")
+    M, V = logits.shape
+    for t, kind in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
+                    (min_p, torch.float32), (tokens, torch.int32)):
+        _need(t is None or (t.dtype == kind and t.shape == (M,) and t.is_contiguous()), f"a {kind} tensor [{M}] expected")
+    _on(dev, u, temperature, top_k, top_p, min_p, tokens)
+    out = tokens if tokens is not None else torch.empty(M, dtype=torch.int32, device=dev)
+    probs = torch.empty(M, dtype=torch.float32, device=dev) if want_probs else None
+    sp = SamplingC(*(None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)))
+    _check("w8a8_sample", lib().w8a8_sample(TYPE_CODES.get(logits.dtype, -1), _p(logits), logits.stride(0), M, V,
+                                            ctypes.byref(sp), _p(u), _p(out), _p(probs), _stream(stream)))
+    return (out, probs) if want_probs else out
 
 
 # ------------------------------------------------------------------------------- decoder
