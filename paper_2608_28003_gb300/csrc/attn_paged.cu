@@ -1,99 +1,24 @@
-// Attention of a ragged batch over a paged cache.
+// Attention of a ragged batch over a paged cache: checks and choice of the kernel.
+#include <algorithm>
 #include <cmath>
 
-#include "attn_common.cuh"
+#include "attn_paged.cuh"
 #include "ops.cuh"
 #include "paged.cuh"
 
 namespace w8a8 {
 
-namespace {
-
-// One row's attention by one warp, key by key in the order of the formula: NaN and infinities travel as they do
-// in it, and nothing outside the row's range is read.  Lane l scores key j0 + l, then holds dims l, l + 32, ...
-template <bool kBf16, int kDim>
-__device__ __noinline__ void attend_row(const PagedCache& c, const PagedBatch& b, const AttnCall& a, int s, int pos,
-                                        int64_t row, int head, int lane) {
-  const uint16_t* q = a.q + row * a.q_row + head * a.q_head;
-  const int kvh = head / (a.n_q / c.n_kv);
-  const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-  float m = -INFINITY, l = 0.0f, acc[kDim / 32];
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < kDim / 32; ++i) acc[i] = 0.0f;
-  for (int j0 = lo; j0 <= pos; j0 += 32) {
-    const int j = j0 + lane;
-    const int64_t at = j <= pos ? key_offset(b, c, s, j, kvh) : -1;
-    float sc = -INFINITY;
-    if (at >= 0) {
-      float d = 0.0f;
-      for (int i = 0; i < kDim / 8; ++i) {
-        const uint4 kw = *reinterpret_cast<const uint4*>(c.k + at + 8 * i), qw = *reinterpret_cast<const uint4*>(q + 8 * i);
-        const uint32_t ka[4] = {kw.x, kw.y, kw.z, kw.w}, qa[4] = {qw.x, qw.y, qw.z, qw.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 x = unpack2<kBf16>(ka[e]), y = unpack2<kBf16>(qa[e]);
-          d = fmaf(x.x, y.x, d);
-          d = fmaf(x.y, y.y, d);
-        }
-      }
-      sc = d * a.scale;
-    }
-    const uint32_t there = __ballot_sync(0xffffffffu, at >= 0);
-    if (!there) continue;
-    any = true;
-    const float m_new = fmaxf(m, warp_max_f(sc));
-    const float ref = m_new == -INFINITY ? 0.0f : m_new;
-    const float corr = m == -INFINITY ? 0.0f : expf(m - ref);
-    const float p = at >= 0 ? expf(sc - ref) : 0.0f;
-    l = l * corr + warp_sum_f(p);
-#pragma unroll
-    for (int i = 0; i < kDim / 32; ++i) acc[i] *= corr;
-    for (int u = 0; u < 32; ++u) {
-      if (!((there >> u) & 1u)) continue;
-      const float pu = __shfl_sync(0xffffffffu, p, u);
-      const int64_t au = __shfl_sync(0xffffffffu, (long long)at, u);
-#pragma unroll
-      for (int i = 0; i < kDim / 32; ++i) {
-        const float2 v = unpack2<kBf16>((uint32_t)c.v[au + lane + 32 * i]);
-        acc[i] = fmaf(pu, v.x, acc[i]);
-      }
-    }
-    m = m_new;
-  }
-  uint16_t* o = a.o + row * a.o_row + head * a.o_head;
-#pragma unroll
-  for (int i = 0; i < kDim / 32; ++i) o[lane + 32 * i] = (uint16_t)pack2<kBf16>(any ? acc[i] / l : 0.0f, 0.0f);
+size_t paged_attention_ws(int dim, int, int, int sms) {
+  return W8A8_WS_RESERVED + std::max(attn_tokens_ws(dim, sms), attn_chunks_ws(dim, sms));
 }
 
-template <bool kBf16, int kDim>
-__global__ void __launch_bounds__(128) attn_rows_kernel(PagedCache c, PagedBatch b, AttnCall a) {
-  pdl_wait();
-  pdl_trigger();
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  const int row = (int)(w / a.n_q), head = (int)(w % a.n_q);
-  if (row >= b.n_rows) return;
-  const int s = seq_of_row(b, row);
-  const SeqShape q = seq_shape(b, s, c.page_shift);
-  if (row < q.row0 || row >= q.row0 + q.rows) return;
-  attend_row<kBf16, kDim>(c, b, a, s, q.pos0 + row - q.row0, row, head, threadIdx.x & 31);
-}
-
-}  // namespace
-
-size_t paged_attention_ws(int, int, int, int) { return W8A8_WS_RESERVED; }
-
-w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void*, int,
+// Up to 16 rows a sequence and key/value head go to the kernel for tokens, more to the one for chunks; a longer sequence in
+// the batch is right in either.
+w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)pb.n_rows * a.n_q + 3) / 4));
-  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, st, pc, pb, a); };
-  W8A8_CUDA(a.bf16 ? (a.dim == 256   ? go(attn_rows_kernel<true, 256>)
-                      : a.dim == 128 ? go(attn_rows_kernel<true, 128>)
-                                     : go(attn_rows_kernel<true, 64>))
-                   : (a.dim == 256   ? go(attn_rows_kernel<false, 256>)
-                      : a.dim == 128 ? go(attn_rows_kernel<false, 128>)
-                                     : go(attn_rows_kernel<false, 64>)));
-  return W8A8_OK;
+  const int group = a.n_q / pc.n_kv;
+  return (long long)a.max_new * group <= 16 ? launch_attn_tokens(pc, pb, a, ws, sms, st)
+                                            : launch_attn_chunks(pc, pb, a, ws, sms, st);
 }
 
 namespace {
@@ -132,6 +57,7 @@ extern "C" w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const
   W8A8_CHECK_ARG(window >= 0 && std::isfinite(scale) && scale > 0.0f, W8A8_ERR_INVALID_ARG, "%s: window %d, scale %g", who,
                  window, (double)scale);
   if (pb.n_seqs == 0 || pb.n_rows == 0) return W8A8_OK;
+  if (window >= (1 << 30)) window = 0;  // beyond every position
   W8A8_CHECK_ARG(q && o, W8A8_ERR_INVALID_ARG, "%s: null pointer", who);
   W8A8_CHECK_ARG(aligned16(q) && aligned16(o), W8A8_ERR_ALIGN, "%s: q and o must be 16-byte aligned", who);
   const int64_t big = 1ll << 38, str[4] = {q_row, q_head, o_row, o_head};

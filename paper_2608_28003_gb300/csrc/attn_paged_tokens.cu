@@ -1,0 +1,476 @@
+// Attention over a paged cache for single tokens and a few drafted ones: items of up to 16 rows (tokens times the query heads of a
+// group).
+//
+// The cache is read once and little is computed with it, so HBM bounds the kernel; everything is arranged to keep copies in
+// flight.  One CTA per SM walks its stretch of the line of key tiles (attn_paged.cuh).  A loader warp copies K and V tiles,
+// page by page, into a ring of 192 KB by TMA (64 KB a stage at head dims 256 and 128); kWarps consumer warps take 16
+// keys of a tile each, on their own from scores to output: no barrier inside the loop but the ring's.  The products
+// are mma.sync m16n8k16 (16 rows are one operand's height: tcgen05's 128 would be mostly padding, and at the rate HBM
+// feeds an SM this takes a third of the legacy tensor rate); K is read by ldmatrix, V by its transposing form, and a
+// score fragment is the next product's operand as it is.  A warp keeps its own reference, sum and output; they
+// are joined in shared memory when the item ends.
+#include "attn_paged.cuh"
+#include "ops.cuh"
+#include "tmap.cuh"
+
+namespace w8a8 {
+
+namespace {
+
+constexpr int kRows = 16;
+
+template <int kDim>
+struct Cfg {
+  static constexpr int kWarps = kDim == 256 ? 4 : 8;          // consumers
+  static constexpr int kBk = 16 * kWarps, kBkShift = kDim == 256 ? 6 : 7;
+  static constexpr int kChunks = kDim / 64;                   // 128-byte columns of a tile
+  static constexpr int kSub = kBk * 128, kTile = kChunks * kSub, kStage = 2 * kTile;
+  static constexpr int kStages = 196608 / kStage;             // 3, 3, 6
+  static constexpr int kJoin = kWarps / 2 * kRows * kDim * 4; // outputs of half of the warps
+  static constexpr int kSmem = kStages * kStage + kJoin + 1024;
+  static constexpr int kThreads = 32 * (kWarps + 1);
+  // a partial: [8 dims of 4 lanes.. as fragments: dim / 8][32 lanes][4] outputs, then m and l of the 16 rows
+  static constexpr int kPart = kRows * kDim + 2 * kRows;
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+template <bool kBf16>
+__device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (kBf16)
+    mma_bf16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
+  else
+    mma_f16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
+}
+
+template <bool kBf16, int kDim>
+__global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
+    attn_tokens_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, PagedCache c,
+                       PagedBatch b, AttnCall a, int tt, float* __restrict__ part, unsigned int* __restrict__ counters,
+                       unsigned int* __restrict__ err) {
+  using C = Cfg<kDim>;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ uint64_t bars[2 * C::kStages];
+  __shared__ LineStart ls;
+  __shared__ long long scan[C::kThreads / 32];
+  __shared__ uint32_t held[C::kStages];                    // 16-key groups of a stage's tile that lie in a page
+  __shared__ float s_m[C::kWarps][kRows], s_l[C::kWarps][kRows];
+  __shared__ uint32_t s_last, s_bad;
+  const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
+  float4* join = reinterpret_cast<float4*>(smem_raw + (ring - raw) + C::kStages * C::kStage);
+  const uint32_t bar0 = smem_u32(bars);
+  auto full = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+  auto empty = [&](int i) { return bar0 + 8u * (uint32_t)(C::kStages + i); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(full(i), 1);
+      mbar_init(empty(i), C::kWarps);
+    }
+    fence_mbar_init();
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
+    s_bad = 0;
+  }
+  pdl_wait();
+  pdl_trigger();
+  find_start<C::kThreads>(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift, &ls, scan);
+  if (ls.begin >= ls.end) return;
+  Walk w;
+  w.start(ls, b, c.page_shift, a.window, tt, C::kBkShift, lane);
+  int g = 0;  // tiles of this CTA so far
+  bool ok = true;
+
+  if (warp == C::kWarps) {
+    // -------------------------------------------------------------------------- loader
+    const int box = min(kBoxSlots, 1 << c.page_shift), boxes = C::kBk / box;  // per tile and column
+    const int n_ops = 2 * C::kChunks * boxes;
+    for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift)) {
+      const int lo = w.lo(a.window, tt), hi = w.hi(tt);
+      for (int i = 0; i < w.cnt; ++i, ++g) {
+        const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << C::kBkShift;
+        // the pages of the tile's 16-key groups (all boxes begin at multiples of 16)
+        int page = -1;
+        if (lane < C::kBk / 16) {
+          const int p = tile0 + 16 * lane, col = p >> c.page_shift;
+          if (p <= hi && (p | (box - 1)) >= lo && col < b.max_pages) page = b.pages[(int64_t)w.s * b.max_pages + col];
+          if (page < 0 || page >= c.n_pages) page = -1;
+        }
+        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+        if (g >= C::kStages && !mbar_wait_warp(empty(st), (uint32_t)(g / C::kStages - 1) & 1u, kWaitBudgetCycles)) {
+          ok = false;
+          break;
+        }
+        if (lane == 0) {
+          held[st] = there;
+          mbar_arrive_expect_tx(full(st), C::kStage);
+        }
+        __syncwarp();
+        const uint32_t dst = ring + (uint32_t)(st * C::kStage);
+        for (int o0 = 0; o0 < n_ops; o0 += 32) {
+          const int o = o0 + lane, bx = o % boxes, ch = o / boxes % C::kChunks, kv = o / boxes / C::kChunks;
+          const int pg = __shfl_sync(0xffffffffu, page, bx * (box / 16) & 31);
+          if (o < n_ops) {
+            const int slot = (tile0 + bx * box) & ((1 << c.page_shift) - 1);
+            // a page that holds nothing: a coordinate outside the tensor, which fills zeros
+            tma_load_4d(dst + (uint32_t)(kv * C::kTile + ch * C::kSub + bx * box * 128), kv ? &tmV : &tmK, 64 * ch, slot, w.h,
+                        pg < 0 ? c.n_pages : pg, full(st));
+          }
+        }
+      }
+    }
+    // the last copies land before the CTA may end
+    if (!ok && lane == 0) atomicOr(err, DEVERR_PRODUCER_WAIT);
+    for (int k = max(0, g - C::kStages); k < g; ++k)
+      if (!mbar_wait_warp(full(k % C::kStages), (uint32_t)(k / C::kStages) & 1u, kWaitBudgetCycles) && lane == 0)
+        atomicOr(err, DEVERR_DRAIN_WAIT);
+    return;
+  }
+
+  // -------------------------------------------------------------------------- consumers
+  constexpr int kBar = 1, kConsumers = 32 * C::kWarps;
+  const int group = a.n_q / c.n_kv;
+  const float sc = a.scale * kLog2e;
+  const int r0 = lane >> 2, quad = lane & 3;  // this lane's fragment rows r0, r0 + 8 and columns 2 quad, 2 quad + 1
+  for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift)) {
+    const int tok0 = w.t * tt, n_tok = min(w.q.rows - tok0, tt), rows = n_tok * group;
+    const int lo = w.lo(a.window, tt), hi = w.hi(tt);
+    // where every row of the item sees everything: between the last row's first key and the first row's position
+    const int all_lo = a.window > 0 ? max(0, hi - a.window + 1) : 0, all_hi = w.q.pos0 + tok0;
+    uint32_t qf[kDim / 16][4];
+    int pos[2], from[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + 8 * i;
+      const bool live = r < rows;
+      const int tok = live ? tok0 + r / group : tok0;
+      pos[i] = w.q.pos0 + tok;
+      from[i] = a.window > 0 ? pos[i] - a.window + 1 : 0;
+      const uint16_t* qp =
+          a.q + (int64_t)(w.q.row0 + tok) * a.q_row + (int64_t)(w.h * group + (live ? r % group : 0)) * a.q_head + 2 * quad;
+#pragma unroll
+      for (int k = 0; k < kDim / 16; ++k) {
+        qf[k][i] = live ? *reinterpret_cast<const uint32_t*>(qp + 16 * k) : 0u;
+        qf[k][2 + i] = live ? *reinterpret_cast<const uint32_t*>(qp + 16 * k + 8) : 0u;
+      }
+    }
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, acc[kDim / 8][4];
+#pragma unroll
+    for (int i = 0; i < kDim / 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+
+    for (int i = 0; i < w.cnt; ++i, ++g) {
+      const int st = g % C::kStages, j0 = ((w.first + w.k0 + i) << C::kBkShift) + 16 * warp;
+      if (ok && !mbar_wait_warp(full(st), (uint32_t)(g / C::kStages) & 1u, kWaitBudgetCycles)) ok = false;
+      if (!ok) continue;
+      if (((held[st] >> warp) & 1u) && j0 <= hi && j0 + 15 >= lo) {
+        const uint32_t kt = ring + (uint32_t)(st * C::kStage), vt = kt + C::kTile;
+        float s[2][2][4] = {};  // [keys 0-7, 8-15][even, odd k steps]
+        {
+          const int row = 16 * warp + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
+#pragma unroll
+          for (int k = 0; k < kDim / 16; ++k) {
+            uint32_t kb[4];
+            const int col = 2 * (k & 3) + half;
+            ldsm4(kt + (uint32_t)((k >> 2) * C::kSub + row * 128 + ((col ^ (row & 7)) << 4)), kb);
+            mma16<kBf16>(s[0][k & 1], qf[k], kb[0], kb[1]);
+            mma16<kBf16>(s[1][k & 1], qf[k], kb[2], kb[3]);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][0][e] += s[n][1][e];
+        if (j0 < all_lo || j0 + 15 > all_hi) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int j = j0 + 8 * n + 2 * quad + (e & 1);
+              if (j > pos[e >> 1] || j < from[e >> 1]) s[n][0][e] = -INFINITY;
+            }
+        }
+        float up[2], ref[2];
+        bool grown = false;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float top = fmaxf(fmaxf(s[0][0][2 * r], s[0][0][2 * r + 1]), fmaxf(s[1][0][2 * r], s[1][0][2 * r + 1]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * sc;
+          up[r] = 1.0f;
+          if (top > m[r] + kGrowth) {  // m = -inf: any visible key
+            up[r] = m[r] == -INFINITY ? 0.0f : ex2(m[r] - top);
+            m[r] = top;
+            grown = true;
+          }
+          ref[r] = m[r] == -INFINITY ? 0.0f : m[r];
+        }
+        if (__any_sync(0xffffffffu, grown)) {
+          l[0] *= up[0];
+          l[1] *= up[1];
+#pragma unroll
+          for (int d = 0; d < kDim / 8; ++d) {
+            acc[d][0] *= up[0];
+            acc[d][1] *= up[0];
+            acc[d][2] *= up[1];
+            acc[d][3] *= up[1];
+          }
+        }
+        uint32_t p[4];  // the weights as the second product's left operand: rows r0 / r0 + 8, keys 0-7 then 8-15
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            p[2 * n + r] = pack2<kBf16>(ex2(fmaf(s[n][0][2 * r], sc, -ref[r])), ex2(fmaf(s[n][0][2 * r + 1], sc, -ref[r])));
+            const float2 as_used = unpack2<kBf16>(p[2 * n + r]);
+            l[r] += as_used.x + as_used.y;
+          }
+        // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero
+        uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
+        const bool cut = j0 < lo || j0 + 15 > hi;
+        if (cut) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const int j = j0 + 8 * n + 2 * quad;
+            keep[n] = (j >= lo && j <= hi ? 0xffffu : 0u) | (j + 1 >= lo && j + 1 <= hi ? 0xffff0000u : 0u);
+          }
+        }
+        const int key = 16 * warp + (((lane >> 3) & 1) << 3) + (lane & 7);
+#pragma unroll
+        for (int d = 0; d < kDim / 16; ++d) {
+          uint32_t vb[4];
+          const int col = 2 * (d & 3) + (lane >> 4);
+          ldsm4t(vt + (uint32_t)((d >> 2) * C::kSub + key * 128 + ((col ^ (key & 7)) << 4)), vb);
+          if (cut) {
+            vb[0] &= keep[0];
+            vb[1] &= keep[1];
+            vb[2] &= keep[0];
+            vb[3] &= keep[1];
+          }
+          mma16<kBf16>(acc[2 * d], p, vb[0], vb[1]);
+          mma16<kBf16>(acc[2 * d + 1], p, vb[2], vb[3]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(empty(st));
+    }
+    if (!ok && lane == 0) atomicOr(err, DEVERR_CONSUMER_WAIT);
+
+    // ---- the warps' outputs of the item, on a common reference
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+      l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+      if (quad == 0) {
+        s_m[warp][r0 + 8 * r] = m[r];
+        s_l[warp][r0 + 8 * r] = l[r];
+      }
+    }
+    named_bar_sync(kBar, kConsumers);
+    float M[2], L[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      M[r] = -INFINITY;
+      L[r] = 0.0f;
+      for (int i = 0; i < C::kWarps; ++i) M[r] = fmaxf(M[r], s_m[i][r0 + 8 * r]);
+      for (int i = 0; i < C::kWarps; ++i) {
+        const float mi = s_m[i][r0 + 8 * r];
+        L[r] += s_l[i][r0 + 8 * r] * (mi == -INFINITY ? 0.0f : ex2(mi - M[r]));
+      }
+      const float f = m[r] == -INFINITY ? 0.0f : ex2(m[r] - M[r]);
+#pragma unroll
+      for (int d = 0; d < kDim / 8; ++d) {
+        acc[d][2 * r] *= f;
+        acc[d][2 * r + 1] *= f;
+      }
+    }
+#pragma unroll 1
+    for (int half = C::kWarps / 2; half > 0; half >>= 1) {
+      if (warp >= half && warp < 2 * half) {
+        float4* to = join + (warp - half) * (kRows * kDim / 4) + lane;
+#pragma unroll
+        for (int d = 0; d < kDim / 8; ++d) to[32 * d] = make_float4(acc[d][0], acc[d][1], acc[d][2], acc[d][3]);
+      }
+      named_bar_sync(kBar, kConsumers);
+      if (warp < half) {
+        const float4* add = join + warp * (kRows * kDim / 4) + lane;
+#pragma unroll
+        for (int d = 0; d < kDim / 8; ++d) {
+          const float4 x = add[32 * d];
+          acc[d][0] += x.x;
+          acc[d][1] += x.y;
+          acc[d][2] += x.z;
+          acc[d][3] += x.w;
+        }
+      }
+      named_bar_sync(kBar, kConsumers);
+    }
+
+    auto out_at = [&](int r) {
+      return a.o + (int64_t)(w.q.row0 + tok0 + r / group) * a.o_row + (int64_t)(w.h * group + r % group) * a.o_head;
+    };
+    auto exactly = [&](uint32_t bad) {  // rows whose result is not finite, or without weight, by one warp
+      for (; bad; bad &= bad - 1) {
+        const int r = __ffs(bad) - 1, tok = tok0 + r / group;
+        attend_row<kBf16, kDim>(c, b, a, w.s, w.q.pos0 + tok, w.q.row0 + tok, w.h * group + r % group, lane);
+      }
+    };
+    if (w.whole()) {
+      if (warp == 0) {
+        uint32_t bad = 0;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int row = r0 + 8 * r;
+          const float inv = 1.0f / L[r];
+          float nan = 0.0f;
+          uint16_t* o = out_at(min(row, rows - 1)) + 2 * quad;
+#pragma unroll
+          for (int d = 0; d < kDim / 8; ++d) {
+            const float x = acc[d][2 * r] * inv, y = acc[d][2 * r + 1] * inv;
+            nan = fmaf(x, 0.0f, fmaf(y, 0.0f, nan));
+            if (row < rows) *reinterpret_cast<uint32_t*>(o + 8 * d) = pack2<kBf16>(x, y);
+          }
+          const uint32_t hit = __ballot_sync(0xffffffffu, row < rows && (nan != 0.0f || !(L[r] > 0.0f)));
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if ((hit >> (4 * i)) & 0xfu) bad |= 1u << (i + 8 * r);
+        }
+        __syncwarp();
+        if (bad) exactly(bad);
+      }
+      continue;
+    }
+    // ---- a piece: into the workspace, joined by the last one to arrive
+    const Pieces ps = pieces_of(w, ls);
+    if (warp == 0) {
+      float* to = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
+#pragma unroll
+      for (int d = 0; d < kDim / 8; ++d) {
+        if (r0 < rows) __stcg(reinterpret_cast<float2*>(to + (size_t)(d * 32 + lane) * 2), make_float2(acc[d][0], acc[d][1]));
+        if (r0 + 8 < rows)
+          __stcg(reinterpret_cast<float2*>(to + 8 * kDim + (size_t)(d * 32 + lane) * 2), make_float2(acc[d][2], acc[d][3]));
+      }
+      if (quad == 0)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          __stcg(to + kRows * kDim + r0 + 8 * r, M[r]);
+          __stcg(to + kRows * kDim + kRows + r0 + 8 * r, L[r]);
+        }
+      __threadfence();
+      __syncwarp();
+      if (lane == 0) {
+        const unsigned int before = atomicAdd(counters + ps.first, 1u);
+        s_last = before + 1 == (unsigned int)ps.count;
+        if (s_last) counters[ps.first] = 0;
+        __threadfence();
+      }
+    }
+    named_bar_sync(kBar, kConsumers);
+    if (s_last) {
+      constexpr int kPer = kDim / 8 / C::kWarps;  // this warp's groups of 8 dims
+      auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
+      float Mj[2] = {-INFINITY, -INFINITY}, Lj[2] = {0.0f, 0.0f}, y[kPer][4];
+#pragma unroll
+      for (int d = 0; d < kPer; ++d) y[d][0] = y[d][1] = y[d][2] = y[d][3] = 0.0f;
+      for (int i = 0; i < ps.count; ++i)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) Mj[r] = fmaxf(Mj[r], __ldcg(slot(i) + kRows * kDim + r0 + 8 * r));
+#pragma unroll 2
+      for (int i = 0; i < ps.count; ++i) {
+        const float* from_piece = slot(i);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          if (r0 + 8 * r >= rows) continue;
+          const float mi = __ldcg(from_piece + kRows * kDim + r0 + 8 * r);
+          const float f = mi == -INFINITY ? 0.0f : ex2(mi - Mj[r]);
+          Lj[r] = fmaf(__ldcg(from_piece + kRows * kDim + kRows + r0 + 8 * r), f, Lj[r]);
+#pragma unroll
+          for (int d = 0; d < kPer; ++d) {
+            const float2 x =
+                __ldcg(reinterpret_cast<const float2*>(from_piece + 8 * kDim * r + (size_t)((warp * kPer + d) * 32 + lane) * 2));
+            y[d][2 * r] = fmaf(x.x, f, y[d][2 * r]);
+            y[d][2 * r + 1] = fmaf(x.y, f, y[d][2 * r + 1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int row = r0 + 8 * r;
+        const float inv = 1.0f / Lj[r];
+        float nan = 0.0f;
+        uint16_t* o = out_at(min(row, rows - 1)) + 2 * quad + 8 * warp * kPer;
+#pragma unroll
+        for (int d = 0; d < kPer; ++d) {
+          const float x = y[d][2 * r] * inv, z = y[d][2 * r + 1] * inv;
+          nan = fmaf(x, 0.0f, fmaf(z, 0.0f, nan));
+          if (row < rows) *reinterpret_cast<uint32_t*>(o + 8 * d) = pack2<kBf16>(x, z);
+        }
+        if (row < rows && (nan != 0.0f || !(Lj[r] > 0.0f))) atomicOr(&s_bad, 1u << row);
+      }
+      named_bar_sync(kBar, kConsumers);
+      if (warp == 0) {
+        const uint32_t bad = s_bad;
+        __syncwarp();
+        if (lane == 0) s_bad = 0;
+        if (bad) exactly(bad);
+      }
+    }
+    named_bar_sync(kBar, kConsumers);  // s_last, s_bad and the statistics are free again
+  }
+}
+
+template <bool kBf16, int kDim>
+w8a8_status launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedCache& pc, const PagedBatch& pb, const AttnCall& a,
+                   void* ws, int sms, cudaStream_t st) {
+  using C = Cfg<kDim>;
+  static bool attr_set[64] = {};
+  int dev = 0;
+  W8A8_CUDA(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+    W8A8_CUDA(cudaFuncSetAttribute(attn_tokens_kernel<kBf16, kDim>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    attr_set[dev] = true;
+  }
+  const int tt = kRows / (a.n_q / pc.n_kv);
+  char* base = static_cast<char*>(ws);
+  W8A8_CUDA(launch_pdl(attn_tokens_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tk, tv, pc,
+                       pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
+                       reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
+  return W8A8_OK;
+}
+
+}  // namespace
+
+size_t attn_tokens_ws(int dim, int sms) { return (size_t)2 * sms * (kRows * dim + 2 * kRows) * sizeof(float); }
+
+w8a8_status make_kv_maps(const PagedCache& pc, int dim, CUtensorMap* tk, CUtensorMap* tv) {
+  const int page = 1 << pc.page_shift;
+  const uint64_t dims[4] = {(uint64_t)dim, (uint64_t)page, (uint64_t)pc.n_kv, (uint64_t)pc.n_pages};
+  const uint64_t strides[3] = {(uint64_t)pc.slot_stride * 2, (uint64_t)pc.head_stride * 2, (uint64_t)pc.page_stride * 2};
+  const uint32_t box[4] = {64, (uint32_t)(page < kBoxSlots ? page : kBoxSlots), 1, 1};
+  W8A8_TRY(make_tmap_16(tk, pc.k, 4, dims, strides, box));
+  return make_tmap_16(tv, pc.v, 4, dims, strides, box);
+}
+
+w8a8_status launch_attn_tokens(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
+                               cudaStream_t st) {
+  CUtensorMap tk, tv;
+  W8A8_TRY(make_kv_maps(pc, a.dim, &tk, &tv));
+  if (a.bf16)
+    return a.dim == 256   ? launch<true, 256>(tk, tv, pc, pb, a, ws, sms, st)
+           : a.dim == 128 ? launch<true, 128>(tk, tv, pc, pb, a, ws, sms, st)
+                          : launch<true, 64>(tk, tv, pc, pb, a, ws, sms, st);
+  return a.dim == 256   ? launch<false, 256>(tk, tv, pc, pb, a, ws, sms, st)
+         : a.dim == 128 ? launch<false, 128>(tk, tv, pc, pb, a, ws, sms, st)
+                        : launch<false, 64>(tk, tv, pc, pb, a, ws, sms, st);
+}
+
+}  // namespace w8a8

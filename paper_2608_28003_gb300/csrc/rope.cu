@@ -234,8 +234,10 @@ w8a8_status check_paged(const char* who, const w8a8_paged_cache* c, const w8a8_p
   while (shift < 8 && (1 << shift) < c->page_size) ++shift;
   W8A8_CHECK_ARG((1 << shift) == c->page_size, W8A8_ERR_SHAPE, "%s: page_size %d must be 16, 32, 64, 128 or 256", who,
                  c->page_size);
-  W8A8_CHECK_ARG((long long)b->max_pages << shift <= 0x7fffff00ll && (long long)c->n_kv * c->head_dim <= 65536,
-                 W8A8_ERR_SHAPE, "%s: more than 2^31 positions a sequence, or n_kv * head_dim above 65536", who);
+  W8A8_CHECK_ARG((long long)b->max_pages << shift <= (1ll << 30) && b->n_rows <= (1 << 28) && b->n_seqs <= (1 << 28) &&
+                     (long long)c->n_kv * c->head_dim <= 65536,
+                 W8A8_ERR_SHAPE, "%s: more than 2^30 positions a sequence, 2^28 rows or sequences, or n_kv * head_dim above 65536",
+                 who);
   const int64_t str[3] = {c->page_stride, c->slot_stride, c->head_stride};
   for (int64_t s : str)
     W8A8_CHECK_ARG(s >= c->head_dim && s % 8 == 0 && s <= (1ll << 38), W8A8_ERR_SHAPE,

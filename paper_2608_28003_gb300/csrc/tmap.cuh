@@ -15,4 +15,9 @@ namespace w8a8 {
 w8a8_status make_tmap_2d(CUtensorMap* map, const void* base, int elem_bytes, uint64_t inner, uint64_t rows,
                          uint64_t pitch_bytes, uint32_t box_inner, uint32_t box_rows, int swizzle_bytes = 128);
 
+// A tensor of 3 to 5 dimensions of 16-bit elements, innermost first (contiguous; the other dimensions' strides in
+// bytes, multiples of 16); boxes of 64 elements (128 bytes) of the innermost one, 128-byte swizzle, zeros outside.
+w8a8_status make_tmap_16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                         const uint32_t* box);
+
 }  // namespace w8a8
