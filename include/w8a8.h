@@ -545,8 +545,8 @@ w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged
 
 /* ------------------------------------------------------------------------------ sampling
  * One token a row from logits [M, V] (fp32, bf16 or fp16; row stride in elements) and one uniform number u in
- * [0, 1) a row.  Weights w_i = e^((l_i - max l) / temperature), in multiples of 2^-42 and accurate to about 2^-31 of each; NaN and -inf weigh
- * nothing.  Tokens in descending order of logits, the lower index first among equals:
+ * [0, 1) a row.  Weights w_i = e^((l_i - max l) / temperature), in multiples of 2^-43 and accurate to 2^-27 of each;
+ * NaN and -inf weigh nothing.  Tokens in descending order of logits, the lower index first among equals:
  *   top_k  keeps the first top_k (all where top_k <= 0);
  *   top_p  keeps the shortest prefix of those whose weight reaches top_p of theirs, at least one token (all where
  *          top_p >= 1 or NaN);
@@ -557,7 +557,7 @@ w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged
  * equals); +inf logits share the weight among themselves; a row of NaN and -inf alone gives token -1 and
  * probability 0.
  * Per-row parameters: device [M], each pointer nullable (temperature 1, the filters off). */
-#define W8A8_MAX_SAMPLE_VOCAB 1048576
+#define W8A8_MAX_SAMPLE_VOCAB 786432
 typedef struct {
   const float* temperature;
   const int32_t* top_k;

@@ -239,7 +239,7 @@ def _calls():
             raise RuntimeError("paper_2608_28003_gb300/_calls.so is not built: run "
                                "paper_2608_28003_gb300.build.build()") from e
         mod.init({name: ctypes.cast(getattr(L, name), _vp).value for name in SIGNATURES}, _check, default_workspace,
-                 _DEFAULT_WS, Workspace)
+                 _DEFAULT_WS, Workspace, stream_workspace, _STREAM_WS)
         _CALLS = mod
     return _CALLS
 
@@ -567,20 +567,8 @@ def _need(cond, msg):
         raise ValueError(msg)
 
 
-def _on(dev, *tensors):
-    for t in tensors:
-        _need(t is None or t.device == dev, f"all tensors must be on {dev}")
-
-
 def _ints(t, name):
     _need(t.dtype == torch.int32 and t.is_contiguous(), f"{name} must be a contiguous int32 tensor")
-
-
-def _device_of(t):
-    """The tensor's device, which has to be the current one (the library launches there)."""
-    assert t.is_cuda, "tensors must be CUDA tensors"
-    _need(t.device.index == torch.cuda.current_device(), f"the tensors' device {t.device} is not the current one")
-    return t.device
 
 
 @dataclass
@@ -628,17 +616,7 @@ def rope_table(cfg: RopeConfig, device=None) -> RopeTable:
 def rope(table: RopeTable, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None,
          stream=None) -> torch.Tensor:
     """x [T, heads, dim] (bf16 or fp16) rotated at positions [T] int32; out=x rotates in place."""
-    dev = _device_of(x)
-    _need(x.dim() == 3 and x.stride(2) == 1 and positions.shape == x.shape[:1], "x [T, heads, dim], positions [T]")
-    _ints(positions, "positions")
-    y = out if out is not None else torch.empty(x.shape, dtype=x.dtype, device=dev)
-    _need(y.shape == x.shape and y.dtype == x.dtype and y.stride(2) == 1, "out must have x's shape and type")
-    _on(dev, positions, y, table.turns)
-    rc = table.c()
-    _check("w8a8_rope", lib().w8a8_rope(ctypes.byref(rc), TYPE_CODES.get(x.dtype, -1), _p(x), x.stride(0), x.stride(1),
-                                        x.shape[0], x.shape[1], x.shape[2], _p(positions), _p(y), y.stride(0), y.stride(1),
-                                        _stream(stream)))
-    return y
+    return (_CALLS or _calls()).rope(table, x, positions, out, stream)
 
 
 @dataclass
@@ -677,34 +655,12 @@ class PagedBatch:
                            self.pages.data_ptr())
 
 
-def _rows_of(t, heads, dim, name):
-    """Row stride of [rows, heads, dim] with contiguous heads."""
-    _need(t.dim() == 3 and t.shape[1:] == (heads, dim) and t.stride(2) == 1 and (heads == 1 or t.stride(1) == dim),
-          f"{name} must be [rows, {heads}, {dim}] with contiguous heads")
-    return t.stride(0) if t.shape[0] > 1 else -(-t.stride(0) // 8) * 8
-
-
 def rope_append(table: RopeTable, cache: PagedCache, batch: PagedBatch, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                 q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
                 q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Rotated (and, with the norms, RMS-normalised) q heads, returned; k heads likewise and v heads into the
     cache's pages.  q [rows, n_q, dim], k and v [rows, n_kv, dim]: views of one projection are fine; q_out=q is too."""
-    dev = _device_of(q)
-    cc = cache.c()
-    rows, n_q, dim = q.shape
-    _need(dim == cc.head_dim and k.shape[0] == rows and v.shape[0] == rows, "q, k and v need the cache's head_dim and equal rows")
-    qs, ks, vs = _rows_of(q, n_q, dim, "q"), _rows_of(k, cc.n_kv, dim, "k"), _rows_of(v, cc.n_kv, dim, "v")
-    y = q_out if q_out is not None else torch.empty(q.shape, dtype=q.dtype, device=dev)
-    _need(y.shape == q.shape, "q_out must have q's shape")
-    _need(all(t.dtype == cache.k.dtype for t in (q, k, v, y)), "q, k, v and q_out must have the cache's type")
-    for w in (q_norm, k_norm):
-        _need(w is None or (w.dtype == torch.float32 and w.shape == (dim,) and w.is_contiguous()), "norms must be fp32 [dim]")
-    _on(dev, k, v, y, q_norm, k_norm, cache.k, cache.v, batch.row_start, batch.kv_len, batch.pages, table.turns)
-    rc, bc = table.c(), batch.c(rows)
-    _check("w8a8_rope_append", lib().w8a8_rope_append(
-        ctypes.byref(rc), ctypes.byref(cc), ctypes.byref(bc), _p(q), qs, n_q, _p(k), ks, _p(v), vs, _p(q_norm), _p(k_norm),
-        float(eps), _p(y), _rows_of(y, n_q, dim, "q_out"), _stream(stream)))
-    return y
+    return (_CALLS or _calls()).rope_append(table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out, stream)
 
 
 _STREAM_WS = {}
@@ -726,25 +682,9 @@ def stream_workspace(nbytes: int, dev: torch.device, stream=None) -> torch.Tenso
 def paged_attention(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: Optional[float] = None, window: int = 0,
                     out: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
     """Attention of every row over its sequence's cached keys, its own included (append first).  scale defaults to
-    1 / sqrt(head_dim); window 0 sees all earlier keys.  Rows of no sequence: left as they were in `out`."""
-    dev = _device_of(q)
-    cc = cache.c()
-    _need(q.dim() == 3 and q.shape[2] == cc.head_dim and q.stride(2) == 1, "q must be [rows, n_q, head_dim]")
-    rows, n_q, dim = q.shape
-    y = out if out is not None else torch.empty(q.shape, dtype=q.dtype, device=dev)
-    _need(y.shape == q.shape and y.stride(2) == 1 and q.dtype == cache.k.dtype and y.dtype == q.dtype,
-          "q and out must have the cache's type and equal shapes")
-    _on(dev, y, cache.k, cache.v, batch.row_start, batch.kv_len, batch.pages)
-    bc = batch.c(rows)
-    need = _size("w8a8_paged_attention_workspace_size", ctypes.byref(cc), n_q)
-    buf = ws.get(need) if ws is not None else stream_workspace(need, dev, stream)
-
-    def strides(t):  # the stride of an extent of one says nothing: any that the library takes
-        return [s if e > 1 else max(-(-s // 8) * 8, dim) for s, e in zip(t.stride()[:2], t.shape)]
-    _check("w8a8_paged_attention", lib().w8a8_paged_attention(
-        ctypes.byref(cc), ctypes.byref(bc), _p(q), *strides(q), n_q, float(scale if scale is not None else dim ** -0.5),
-        int(window), _p(y), *strides(y), _p(buf), buf.numel(), _stream(stream)))
-    return y
+    1 / sqrt(head_dim); window 0 sees all earlier keys.  Rows of no sequence: left as they were in `out`.  Without
+    `ws`, scratch of the stream's own (stream_workspace)."""
+    return (_CALLS or _calls()).paged_attention(cache, batch, q, scale, window, out, ws, stream)
 
 
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
@@ -753,20 +693,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     """One token a row of logits [M, V] (fp32, bf16, fp16) from uniform numbers u [M] fp32; per-row parameters [M]
     (temperature, top_p, min_p fp32, top_k int32; None: 1 and off).  Returns tokens int32 [M], or (tokens, their
     probabilities among the kept ones) with want_probs."""
-    dev = _device_of(logits)
-    _need(logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1) and u.shape == logits.shape[:1],
-          "logits [M, V] with contiguous rows, u [M]")
-    M, V = logits.shape
-    for t, kind in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
-                    (min_p, torch.float32), (tokens, torch.int32)):
-        _need(t is None or (t.dtype == kind and t.shape == (M,) and t.is_contiguous()), f"a {kind} tensor [{M}] expected")
-    _on(dev, u, temperature, top_k, top_p, min_p, tokens)
-    out = tokens if tokens is not None else torch.empty(M, dtype=torch.int32, device=dev)
-    probs = torch.empty(M, dtype=torch.float32, device=dev) if want_probs else None
-    sp = SamplingC(*(None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)))
-    _check("w8a8_sample", lib().w8a8_sample(TYPE_CODES.get(logits.dtype, -1), _p(logits), logits.stride(0), M, V,
-                                            ctypes.byref(sp), _p(u), _p(out), _p(probs), _stream(stream)))
-    return (out, probs) if want_probs else out
+    return (_CALLS or _calls()).sample(logits, u, temperature, top_k, top_p, min_p, want_probs, tokens, stream)
 
 
 # ------------------------------------------------------------------------------- decoder

@@ -12,6 +12,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <cmath>
 #include <cstring>
 
 #include "../../include/w8a8.h"
@@ -29,14 +30,21 @@ struct Api {
   decltype(&w8a8_fp8_linear) fp8_linear;
   decltype(&w8a8_fp8_ffn_block) fp8_ffn;
   decltype(&w8a8_lm_head) head;
+  decltype(&w8a8_rope) rope;
+  decltype(&w8a8_rope_append) append;
+  decltype(&w8a8_paged_attention_workspace_size) paged_ws;
+  decltype(&w8a8_paged_attention) paged;
+  decltype(&w8a8_sample) sample;
 } g_api;
 
 // Python objects used by every call (owned by the module for the process's life).
+PyObject *g_f16, *g_capturing, *g_stream_ws, *g_stream_table;
 PyObject *g_empty, *g_bf16, *g_f32, *g_i32, *g_raw_stream, *g_device, *g_check, *g_default_ws, *g_ws_table, *g_ws_type;
 // interned names
 PyObject *s_data_ptr, *s_shape, *s_is_cuda, *s_is_contiguous, *s_numel, *s_device, *s_wq, *s_s_w, *s_inv_delta, *s_wq_f16,
     *s_buf, *s_get, *s_cuda_stream, *s_hidden, *s_inter, *s_vocab, *s_gate_up, *s_down, *s_gate_up_bf16, *s_down_bf16,
-    *s_q, *s_bf16;
+    *s_q, *s_bf16, *s_stride, *s_dtype, *s_get_device, *s_rotary_dim, *s_interleaved, *s_scale, *s_turns, *s_k, *s_v, *s_row_start,
+    *s_kv_len, *s_pages, *s_max_new;
 PyObject* g_kw_empty;  // ("dtype", "device")
 
 // An owned reference.
@@ -412,9 +420,309 @@ PyObject* py_lm_head(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyTuple_Pack(2, lg.p, tp.p);
 }
 
-// (addresses: dict name -> int, check, default_workspace, workspace table, Workspace)
+// ------------------------------------------------------------------ a serving step's operators
+// These take strided views and several types, so each tensor's extents, strides, type and device are read and checked.
+constexpr int kMaxDims = 4;
+struct Tensor {
+  PyObject* o = nullptr;
+  void* ptr = nullptr;
+  int dims = 0;
+  long long size[kMaxDims] = {}, stride[kMaxDims] = {};
+  int type = -1;  // W8A8_TYPE_*, 3 for int32, 4 for int64
+  bool given() const { return o != nullptr; }
+  bool contiguous() const {
+    long long s = 1;
+    for (int i = dims - 1; i >= 0; --i) {
+      if (size[i] != 1 && stride[i] != s) return size[0] == 0;
+      s *= size[i];
+    }
+    return true;
+  }
+};
+constexpr int kInt32 = 3, kInt64 = 4;
+PyObject* g_i64;
+
+bool need(bool ok, const char* msg) {
+  if (!ok && !PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, msg);
+  return ok;
+}
+bool tuple_of(PyObject* t, int* n, long long* out) {  // takes the reference
+  Ref r(t);
+  if (!r || !PyTuple_Check(r.p)) return need(false, "a tensor expected");
+  const Py_ssize_t k = PyTuple_GET_SIZE(r.p);
+  if (!need(k <= kMaxDims, "a tensor of too many dimensions")) return false;
+  *n = (int)k;
+  for (Py_ssize_t i = 0; i < k; ++i) {
+    out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(r.p, i));
+    if (out[i] == -1 && PyErr_Occurred()) return false;
+  }
+  return true;
+}
+// dev: the device every tensor of the call has to be on; -1 takes the first tensor's, which has to be the current one.
+bool tensor(PyObject* o, long long* dev, Tensor* t) {
+  *t = Tensor();
+  if (o == Py_None) return true;
+  t->o = o;
+  long long d;
+  if (!as_int(call0(o, s_get_device), &d)) return false;
+  if (d < 0) {
+    PyErr_SetString(PyExc_AssertionError, "tensors must be CUDA tensors");
+    return false;
+  }
+  if (*dev < 0) {
+    long long cur;
+    if (!as_int(PyObject_CallNoArgs(g_device), &cur) || !need(cur == d, "the tensors' device is not the current one"))
+      return false;
+    *dev = d;
+  }
+  int n;
+  if (!need(d == *dev, "all tensors must be on one device") || !tuple_of(PyObject_GetAttr(o, s_shape), &t->dims, t->size) ||
+      !tuple_of(call0(o, s_stride), &n, t->stride) || !ptr_of(o, &t->ptr))
+    return false;
+  Ref dt(PyObject_GetAttr(o, s_dtype));
+  if (!dt) return false;
+  t->type = dt.p == g_bf16  ? W8A8_TYPE_BF16
+            : dt.p == g_f16 ? W8A8_TYPE_F16
+            : dt.p == g_f32 ? W8A8_TYPE_F32
+            : dt.p == g_i32 ? kInt32
+            : dt.p == g_i64 ? kInt64
+                            : -1;
+  return true;
+}
+bool tensor_attr(PyObject* o, PyObject* name, long long* dev, Tensor* t, Ref* keep) {
+  keep->p = PyObject_GetAttr(o, name);
+  return keep->p && tensor(keep->p, dev, t);
+}
+bool vector(const Tensor& t, long long n, int type, const char* msg) {
+  return !t.given() || need(t.dims == 1 && t.size[0] == n && t.type == type && (t.stride[0] == 1 || n <= 1), msg);
+}
+bool same_shape(const Tensor& a, const Tensor& b) {
+  if (a.dims != b.dims) return false;
+  for (int i = 0; i < a.dims; ++i)
+    if (a.size[i] != b.size[i]) return false;
+  return true;
+}
+// The stride of an extent of one (or none) says nothing: any that the library takes.
+long long stride_or(const Tensor& t, int i, long long least) {
+  if (t.size[i] > 1) return t.stride[i];
+  const long long s = (t.stride[i] + 7) / 8 * 8;
+  return s > least ? s : least;
+}
+// torch.empty(like's shape, dtype, device) where out is None; a new reference either way
+bool output(PyObject* out, PyObject* like, PyObject* dtype, Ref* y) {
+  if (out != Py_None) {
+    y->p = Py_NewRef(out);
+    return true;
+  }
+  Ref shape(PyObject_GetAttr(like, s_shape)), dev(PyObject_GetAttr(like, s_device));
+  Ref dt(dtype ? Py_NewRef(dtype) : PyObject_GetAttr(like, s_dtype));
+  if (!shape || !dev || !dt) return false;
+  PyObject* args[3] = {shape.p, dt.p, dev.p};
+  y->p = PyObject_Vectorcall(g_empty, args, 1, g_kw_empty);
+  return y->p != nullptr;
+}
+bool rope_of(PyObject* o, long long* dev, w8a8_rope_table* r, Ref* keep) {
+  Tensor turns;
+  Ref sc(PyObject_GetAttr(o, s_scale)), in(PyObject_GetAttr(o, s_interleaved));
+  if (!sc || !in || !int_attr(o, s_rotary_dim, &r->rotary_dim) || !tensor_attr(o, s_turns, dev, &turns, keep)) return false;
+  r->scale = (float)PyFloat_AsDouble(sc.p);
+  r->interleaved = PyObject_IsTrue(in.p);
+  r->turns = static_cast<const uint64_t*>(turns.ptr);
+  if (PyErr_Occurred()) return false;
+  return need(turns.type == kInt64 && turns.dims == 1 && turns.size[0] == r->rotary_dim / 2 && turns.contiguous(),
+              "the rope table's turns must be int64 [rotary_dim / 2]");
+}
+struct Paged {
+  w8a8_paged_cache c;
+  w8a8_paged_batch b;
+  Ref k, v, start, len, pages;
+};
+bool paged_of(PyObject* cache, PyObject* batch, long long rows, long long* dev, Paged* p) {
+  Tensor k, v, start, len, pages;
+  if (!tensor_attr(cache, s_k, dev, &k, &p->k) || !tensor_attr(cache, s_v, dev, &v, &p->v) ||
+      !tensor_attr(batch, s_row_start, dev, &start, &p->start) || !tensor_attr(batch, s_kv_len, dev, &len, &p->len) ||
+      !tensor_attr(batch, s_pages, dev, &pages, &p->pages) || !int_attr(batch, s_max_new, &p->b.max_new))
+    return false;
+  bool same = k.dims == 4 && same_shape(k, v) && k.type == v.type && k.stride[3] == 1;
+  for (int i = 0; same && i < 4; ++i) same = k.stride[i] == v.stride[i];
+  if (!need(same, "k and v [n_pages, page_size, n_kv, head_dim] of equal shape, strides and type, dims contiguous") ||
+      !need(len.dims == 1 && start.dims == 1 && start.size[0] == len.size[0] + 1 && pages.dims == 2 && pages.size[0] == len.size[0],
+            "row_start [n_seqs + 1], kv_len [n_seqs], pages [n_seqs, max_pages]") ||
+      !need(start.type == kInt32 && len.type == kInt32 && pages.type == kInt32 && start.contiguous() && len.contiguous() &&
+                pages.contiguous(),
+            "row_start, kv_len and pages must be contiguous int32 tensors"))
+    return false;
+  p->c = w8a8_paged_cache{k.type, (int32_t)k.size[0], (int32_t)k.size[1], (int32_t)k.size[2], (int32_t)k.size[3],
+                          stride_or(k, 0, k.size[3]), stride_or(k, 1, k.size[3]), stride_or(k, 2, k.size[3]),
+                          static_cast<uint16_t*>(k.ptr), static_cast<uint16_t*>(v.ptr)};
+  p->b.n_seqs = (int32_t)len.size[0];
+  p->b.n_rows = (int32_t)rows;
+  p->b.max_pages = (int32_t)pages.size[1];
+  p->b.row_start = static_cast<const int32_t*>(start.ptr);
+  p->b.kv_len = static_cast<const int32_t*>(len.ptr);
+  p->b.pages = static_cast<const int32_t*>(pages.ptr);
+  return true;
+}
+// [rows, heads, dim] with contiguous heads
+bool head_rows(const Tensor& t, long long rows, long long heads, long long dim, int type) {
+  return need(t.dims == 3 && t.size[0] == rows && t.size[1] == heads && t.size[2] == dim && t.type == type && t.stride[2] == 1 &&
+                  (heads == 1 || t.stride[1] == dim),
+              "q, k, v and q_out must be [rows, heads, head_dim] of the cache's type, with equal rows and contiguous heads");
+}
+
+// (table, x, positions, out, stream) -> y
+PyObject* py_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 5, "rope")) return nullptr;
+  long long dev = -1;
+  w8a8_rope_table r;
+  Ref turns, y;
+  Tensor x, pos, out;
+  void* st;
+  if (!tensor(a[1], &dev, &x) || !need(x.given() && x.dims == 3 && x.stride[2] == 1, "x must be [T, heads, dim], dims contiguous") ||
+      !tensor(a[2], &dev, &pos) || !need(pos.given(), "positions [T] expected") ||
+      !vector(pos, x.size[0], kInt32, "positions must be a contiguous int32 tensor [T]") || !rope_of(a[0], &dev, &r, &turns) ||
+      !output(a[3], a[1], nullptr, &y) || !tensor(y.p, &dev, &out) ||
+      !need(same_shape(x, out) && x.type == out.type && out.stride[2] == 1, "out must have x's shape and type") ||
+      !stream_of(a[4], &st))
+    return nullptr;
+  const long long least = (x.size[2] + 7) / 8 * 8;
+  if (!check("w8a8_rope", unlocked([&] {
+               return g_api.rope(&r, x.type, static_cast<uint16_t*>(x.ptr), stride_or(x, 0, least), stride_or(x, 1, least),
+                                 (int)x.size[0], (int)x.size[1], (int)x.size[2], static_cast<int32_t*>(pos.ptr),
+                                 static_cast<uint16_t*>(out.ptr), stride_or(out, 0, least), stride_or(out, 1, least), st);
+             })))
+    return nullptr;
+  return y.give();
+}
+
+// (table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out, stream) -> q_out
+PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 11, "rope_append")) return nullptr;
+  long long dev = -1;
+  w8a8_rope_table r;
+  Paged p;
+  Ref turns, y;
+  Tensor q, k, v, qn, kn, out;
+  void* st;
+  if (!tensor(a[3], &dev, &q) || !need(q.given() && q.dims == 3, "q must be [rows, n_q, head_dim]") ||
+      !paged_of(a[1], a[2], q.size[0], &dev, &p) || !rope_of(a[0], &dev, &r, &turns) || !tensor(a[4], &dev, &k) ||
+      !tensor(a[5], &dev, &v) || !need(k.given() && v.given(), "k and v expected") || !tensor(a[6], &dev, &qn) ||
+      !tensor(a[7], &dev, &kn))
+    return nullptr;
+  const double eps = PyFloat_AsDouble(a[8]);
+  if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+  const long long rows = q.size[0], n_q = q.size[1], dim = p.c.head_dim;
+  if (!head_rows(q, rows, n_q, dim, p.c.dtype) || !head_rows(k, rows, p.c.n_kv, dim, p.c.dtype) ||
+      !head_rows(v, rows, p.c.n_kv, dim, p.c.dtype) || !vector(qn, dim, W8A8_TYPE_F32, "norms must be fp32 [head_dim]") ||
+      !vector(kn, dim, W8A8_TYPE_F32, "norms must be fp32 [head_dim]") || !output(a[9], a[3], nullptr, &y) ||
+      !tensor(y.p, &dev, &out) || !head_rows(out, rows, n_q, dim, p.c.dtype) || !stream_of(a[10], &st))
+    return nullptr;
+  if (!check("w8a8_rope_append", unlocked([&] {
+               return g_api.append(&r, &p.c, &p.b, static_cast<uint16_t*>(q.ptr), stride_or(q, 0, 0), (int)n_q,
+                                   static_cast<uint16_t*>(k.ptr), stride_or(k, 0, 0), static_cast<uint16_t*>(v.ptr),
+                                   stride_or(v, 0, 0), static_cast<float*>(qn.ptr), static_cast<float*>(kn.ptr), (float)eps,
+                                   static_cast<uint16_t*>(out.ptr), stride_or(out, 0, 0), st);
+             })))
+    return nullptr;
+  return y.give();
+}
+
+// Scratch of a call without a workspace: the current stream's (looked up here while it exists and is large enough and
+// nothing is being captured), else what the binding's stream_workspace gives.
+bool stream_workspace(PyObject* like, PyObject* stream, long long dev, void* st, size_t need_bytes, Buf* b) {
+  long long have = -1;
+  if (stream == Py_None) {
+    Ref cap(PyObject_CallNoArgs(g_capturing));
+    if (!cap) return false;
+    if (cap.p == Py_False) {
+      Ref key(Py_BuildValue("(LK)", dev, (unsigned long long)reinterpret_cast<uintptr_t>(st)));
+      if (!key) return false;
+      PyObject* ws = PyDict_GetItemWithError(g_stream_table, key.p);
+      if (!ws && PyErr_Occurred()) return false;
+      if (ws) {
+        b->t.p = PyObject_GetAttr(ws, s_buf);
+        if (!b->t || !as_int(call0(b->t.p, s_numel), &have)) return false;
+      }
+    }
+  }
+  if (have < 0 || (size_t)have < need_bytes) {
+    Py_CLEAR(b->t.p);
+    Ref d(PyObject_GetAttr(like, s_device)), n(PyLong_FromSize_t(need_bytes));
+    if (!d || !n) return false;
+    b->t.p = PyObject_CallFunctionObjArgs(g_stream_ws, n.p, d.p, stream, nullptr);
+    if (!b->t || !as_int(call0(b->t.p, s_numel), &have)) return false;
+  }
+  b->bytes = (size_t)have;
+  return ptr_of(b->t.p, &b->ptr);
+}
+
+// (cache, batch, q, scale, window, out, ws, stream) -> out
+PyObject* py_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 8, "paged_attention")) return nullptr;
+  long long dev = -1, window;
+  Paged p;
+  Ref y;
+  Tensor q, out;
+  void* st;
+  if (!tensor(a[2], &dev, &q) || !need(q.given() && q.dims == 3 && q.stride[2] == 1, "q must be [rows, n_q, head_dim]") ||
+      !paged_of(a[0], a[1], q.size[0], &dev, &p) || !output(a[5], a[2], nullptr, &y) || !tensor(y.p, &dev, &out) ||
+      !need(q.size[2] == p.c.head_dim && same_shape(q, out) && out.stride[2] == 1 && q.type == p.c.dtype && out.type == q.type,
+            "q and out must be [rows, n_q, head_dim] of the cache's type") ||
+      !as_int(PyNumber_Long(a[4]), &window) || !stream_of(a[7], &st))
+    return nullptr;
+  double scale = a[3] == Py_None ? 1.0 / std::sqrt((double)q.size[2]) : PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred() || !need(window >= -2147483647LL && window <= 2147483647LL, "window out of range")) return nullptr;
+  const int n_q = (int)q.size[1];
+  const long long dim = q.size[2];
+  size_t bytes = 0;
+  Buf b;
+  if (!check("w8a8_paged_attention_workspace_size", g_api.paged_ws(&p.c, n_q, &bytes)) ||
+      !(a[6] == Py_None ? stream_workspace(a[2], a[7], dev, st, bytes, &b) : workspace(a[6], bytes, &b)))
+    return nullptr;
+  if (!check("w8a8_paged_attention", unlocked([&] {
+               return g_api.paged(&p.c, &p.b, static_cast<uint16_t*>(q.ptr), stride_or(q, 0, dim), stride_or(q, 1, dim), n_q,
+                                  (float)scale, (int)window, static_cast<uint16_t*>(out.ptr), stride_or(out, 0, dim),
+                                  stride_or(out, 1, dim), b.ptr, b.bytes, st);
+             })))
+    return nullptr;
+  return y.give();
+}
+
+// (logits, u, temperature, top_k, top_p, min_p, want_probs, tokens, stream) -> tokens or (tokens, probs)
+PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 9, "sample")) return nullptr;
+  long long dev = -1;
+  Tensor x, u, temp, k, p, mp, tok, prob;
+  Ref y, z;
+  void* st;
+  const int want = PyObject_IsTrue(a[6]);
+  if (want < 0 || !tensor(a[0], &dev, &x) ||
+      !need(x.given() && x.dims == 2 && (x.stride[1] == 1 || x.size[1] <= 1), "logits must be [M, V] with contiguous rows") ||
+      !tensor(a[1], &dev, &u) || !need(u.given(), "u [M] expected") || !tensor(a[2], &dev, &temp) || !tensor(a[3], &dev, &k) ||
+      !tensor(a[4], &dev, &p) || !tensor(a[5], &dev, &mp))
+    return nullptr;
+  const long long M = x.size[0], V = x.size[1];
+  if (!vector(u, M, W8A8_TYPE_F32, "u must be fp32 [M]") || !vector(temp, M, W8A8_TYPE_F32, "temperature must be fp32 [M]") ||
+      !vector(k, M, kInt32, "top_k must be int32 [M]") || !vector(p, M, W8A8_TYPE_F32, "top_p must be fp32 [M]") ||
+      !vector(mp, M, W8A8_TYPE_F32, "min_p must be fp32 [M]") || !need(V <= 0x7fffffffLL, "V out of range") ||
+      !output(a[7], a[1], g_i32, &y) || !tensor(y.p, &dev, &tok) || !vector(tok, M, kInt32, "tokens must be int32 [M]"))
+    return nullptr;
+  if (want && (!output(Py_None, a[1], nullptr, &z) || !tensor(z.p, &dev, &prob))) return nullptr;
+  if (!stream_of(a[8], &st)) return nullptr;
+  const w8a8_sampling sp{static_cast<float*>(temp.ptr), static_cast<int32_t*>(k.ptr), static_cast<float*>(p.ptr),
+                         static_cast<float*>(mp.ptr)};
+  if (!check("w8a8_sample", unlocked([&] {
+               return g_api.sample(x.type < 0 || x.type > 2 ? -1 : x.type, x.ptr, M > 1 ? x.stride[0] : 0, (int)M, (int)V, &sp,
+                                   static_cast<float*>(u.ptr), static_cast<int32_t*>(tok.ptr), static_cast<float*>(prob.ptr), st);
+             })))
+    return nullptr;
+  if (!want) return y.give();
+  return PyTuple_Pack(2, y.p, z.p);
+}
+
+// (addresses: dict name -> int, check, default_workspace, workspace table, Workspace, stream_workspace, its table)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!nargs_are(n, 5, "init")) return nullptr;
+  if (!nargs_are(n, 7, "init")) return nullptr;
   auto address = [&](const char* name, void* slot) {
     PyObject* v = PyDict_GetItemString(a[0], name);
     const unsigned long long p = v ? PyLong_AsUnsignedLongLong(v) : 0ull;
@@ -431,7 +739,10 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !address("w8a8_ffn_workspace_size", &g_api.ffn_ws) || !address("w8a8_lm_head_workspace_size", &g_api.head_ws) ||
       !address("w8a8_linear", &g_api.linear) || !address("w8a8_linear_bf16", &g_api.bf16) ||
       !address("w8a8_ffn_block", &g_api.ffn) || !address("w8a8_fp8_linear", &g_api.fp8_linear) ||
-      !address("w8a8_fp8_ffn_block", &g_api.fp8_ffn) || !address("w8a8_lm_head", &g_api.head))
+      !address("w8a8_fp8_ffn_block", &g_api.fp8_ffn) || !address("w8a8_lm_head", &g_api.head) ||
+      !address("w8a8_rope", &g_api.rope) || !address("w8a8_rope_append", &g_api.append) ||
+      !address("w8a8_paged_attention_workspace_size", &g_api.paged_ws) ||
+      !address("w8a8_paged_attention", &g_api.paged) || !address("w8a8_sample", &g_api.sample))
     return nullptr;
   Ref torch(PyImport_ImportModule("torch")), c(PyImport_ImportModule("torch._C"));
   if (!torch || !c) return nullptr;
@@ -443,6 +754,9 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
                {&g_bf16, torch.p, "bfloat16"},
                {&g_f32, torch.p, "float32"},
                {&g_i32, torch.p, "int32"},
+               {&g_i64, torch.p, "int64"},
+               {&g_f16, torch.p, "float16"},
+               {&g_capturing, c.p, "_cuda_isCurrentStreamCapturing"},
                {&g_raw_stream, c.p, "_cuda_getCurrentRawStream"},
                {&g_device, c.p, "_cuda_getDevice"}};
   for (auto& it : items)
@@ -451,6 +765,8 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g_default_ws = Py_NewRef(a[2]);
   g_ws_table = Py_NewRef(a[3]);
   g_ws_type = Py_NewRef(a[4]);
+  g_stream_ws = Py_NewRef(a[5]);
+  g_stream_table = Py_NewRef(a[6]);
   struct {
     PyObject** to;
     const char* name;
@@ -459,7 +775,10 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
                {&s_s_w, "s_w"}, {&s_inv_delta, "inv_delta"}, {&s_wq_f16, "wq_f16"}, {&s_buf, "buf"}, {&s_get, "get"},
                {&s_cuda_stream, "cuda_stream"}, {&s_hidden, "hidden"}, {&s_inter, "inter"}, {&s_vocab, "vocab"},
                {&s_gate_up, "gate_up"}, {&s_down, "down"}, {&s_gate_up_bf16, "gate_up_bf16"},
-               {&s_down_bf16, "down_bf16"}, {&s_q, "q"}, {&s_bf16, "bf16"}};
+               {&s_down_bf16, "down_bf16"}, {&s_q, "q"}, {&s_bf16, "bf16"},
+               {&s_stride, "stride"}, {&s_dtype, "dtype"}, {&s_get_device, "get_device"}, {&s_rotary_dim, "rotary_dim"},
+               {&s_interleaved, "interleaved"}, {&s_scale, "scale"}, {&s_turns, "turns"}, {&s_k, "k"}, {&s_v, "v"},
+               {&s_row_start, "row_start"}, {&s_kv_len, "kv_len"}, {&s_pages, "pages"}, {&s_max_new, "max_new"}};
   for (auto& it : names)
     if (!(*it.to = PyUnicode_InternFromString(it.name))) return nullptr;
   if (!(g_kw_empty = Py_BuildValue("(ss)", "dtype", "device"))) return nullptr;
@@ -474,6 +793,10 @@ PyMethodDef g_methods[] = {{"init", FAST(py_init), "Set the library's addresses 
                            {"fp8_linear", FAST(py_fp8_linear), "w8a8_fp8_linear"},
                            {"fp8_ffn_block", FAST(py_fp8_ffn_block), "w8a8_fp8_ffn_block"},
                            {"lm_head", FAST(py_lm_head), "w8a8_lm_head"},
+                           {"rope", FAST(py_rope), "w8a8_rope"},
+                           {"rope_append", FAST(py_rope_append), "w8a8_rope_append"},
+                           {"paged_attention", FAST(py_paged_attention), "w8a8_paged_attention"},
+                           {"sample", FAST(py_sample), "w8a8_sample"},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", "Compute calls of the binding.", -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};
