@@ -557,7 +557,7 @@ w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged
  * equals); +inf logits share the weight among themselves; a row of NaN and -inf alone gives token -1 and
  * probability 0.
  * Per-row parameters: device [M], each pointer nullable (temperature 1, the filters off). */
-#define W8A8_MAX_SAMPLE_VOCAB 786432
+#define W8A8_MAX_SAMPLE_VOCAB 1048576
 typedef struct {
   const float* temperature;
   const int32_t* top_k;

@@ -1,21 +1,25 @@
 // Sampling of one token a row by temperature, top-k, top-p and min-p, from a given uniform number.
 //
 // The mathematics.  Weights are e^((l - max) / T) as multiples of 2^-43 in 64-bit integers, so that sums of up to
-// 2^20 of them are exact and depend on no order: every comparison that decides a token is one of integers.  An fp32
+// 2^20 of them are exact and depend on no order: every comparison that decides a token is one of integers.  A plain fp32
 // exponential would not do: a flat row of 262144 logits has steps of 2^-18 in the sum, and weights off by 2^-24
-// or, far from the maximum, by 2^-19 would move the token in a noticeable share of draws.  So logits become 32-bit fixed-point
-// numbers over the range that has any weight (exact for all but those near zero), their distance D to the maximum is
-// multiplied by log2(e) / T in 64 bits, and 2^-y comes from a table of 128 values and a cubic, all in integers: about 2^-28 of the
-// weight at worst, and 23 instructions.
+// or, far from the maximum, by 2^-19 would move the token in a noticeable share of draws.  So the exponent is kept with its
+// rounding errors (two-term difference and product) and 2^y comes from a table of 128 values and a cubic whose small part alone is
+// rounded in fp32: 2^-29 of the weight, in about 25 instructions (two logits at a time in packed fp32; the same
+// in 32-bit integer products took three times as long).
 //
-// The work.  A cluster of up to 16 CTAs holds a row in shared memory (one read of HBM) and goes over it there: the maximum;
-// then, where a filter needs it, a histogram of counts and weights over 2048 bins of D, whose crossing bin bounds the cut.
-// If at most kSmall tokens lie above the bin's end, one CTA sorts them and finds the cut; else the bin is divided again, by the
-// order of its floats, until one value is left, whose equals are cut by index.  The last pass sums the kept weights and finds
-// the token in index order.  A row of 262144 in fp32 is 64 KB a CTA, two CTAs an SM.
+// The work.  A cluster of up to 16 CTAs takes a row: the maximum; then, where a filter needs it, a histogram with a bin per 1/64
+// of the exponent: counts, and for a cut by weight the exact sums of the bins' weights, as two 16-bit digits of the 30-bit
+// significands (a bin's weights share their exponent), so that three 32-bit additions to shared memory take a logit (a 64-bit
+// one costs more than the three).  The crossing bin holds the cut: its tokens, up to kSmall, are collected and
+// sorted by one CTA; more (flat or tied rows) are divided by the order of their floats until one value is left, whose
+// equals are cut by index.  The last pass sums the kept weights and finds the token in index order.  Slices of up to 64 KB
+// (few rows) stay in shared memory between the passes; longer ones are read again from L2.
 #include <cmath>
+#include <type_traits>
 
 #include "ops.cuh"
+#include "paged.cuh"
 
 namespace w8a8 {
 
@@ -25,60 +29,96 @@ typedef unsigned long long u64;
 
 constexpr int kT = 512, kWarps = kT / 32;
 constexpr int kFrac = 43;     // weights are multiples of 2^-43 of the largest
-constexpr int kBins = 2048, kSmall = 1024;
+constexpr int kBins = 3072;    // one per 1/64 of the exponent, 44.5 of which weigh anything
+constexpr int kFine = 2048;    // and of the divisions of a crowded range
+constexpr int kMostSlice = 65536;  // 16-bit digits of that many weights add up in 32 bits
+constexpr int kSmall = 1024;
 constexpr int kMaxCluster = 16;
 constexpr int kUnit = 4 * 32 * kWarps;      // a CTA's slice is a multiple: 128 logits a warp and step
-constexpr int kMaxSlice = 24 * kUnit;       // 192 KB of shared memory
-static_assert(kMaxSlice * kMaxCluster >= W8A8_MAX_SAMPLE_VOCAB, "a cluster holds the largest row");
+constexpr int kHeldSlice = 8 * kUnit;       // slices up to 64 KB stay in shared memory (up to 48 two CTAs fit an SM)
 
 // ------------------------------------------------------------------------------------ weights
 struct RowScale {
-  float low;         // logits below weigh nothing
-  float scale;       // 2^(31 - e): logits as 32-bit integers
-  int top;           // the maximum's
-  u64 c;             // log2(e) / T per unit of them, times 2^(64 + shift)
-  int shift;         // 0 .. 31
+  float mx, low;     // the maximum; logits below `low` weigh nothing
+  float c_hi, c_lo;  // log2(e) / T in two terms
 };
+constexpr float kRound = 98304.0f;  // 1.5 2^16 (bits 0x47c00000): added to p, rounds it to multiples of 1 / 128
+// the exponent of l - mx rounded to steps of 1 / 128, and kRound: falls with l; and -128 times it
+__device__ __forceinline__ float rounded(const RowScale& r, float l) {
+  return __fadd_rn(__fmul_rn(l - r.mx, r.c_hi), kRound);
+}
+__device__ __forceinline__ int steps_of(const RowScale& r, float l) {
+  return __float_as_int(kRound) - __float_as_int(rounded(r, l));
+}
 __device__ __forceinline__ RowScale row_scale(float mx, float least, float temperature) {
   RowScale r;
-  const double c = 1.4426950408889634074 / (double)fmaxf(temperature, 1e-30f);
-  r.low = mx == INFINITY ? INFINITY : fmaxf(__double2float_rd((double)mx - (kFrac + 1) / c), least);
-  const float a = fmaxf(fabsf(mx), fabsf(r.low));
-  int e = a == INFINITY ? 31 : max(ilogbf(fmaxf(a, 1e-37f)) + 1, -95);
-  r.scale = scalbnf(1.0f, 31 - e);
-  r.top = __float2int_rn(mx * r.scale);
-  int k;
-  const double m = frexp(ldexp(c, e - 31), &k);
-  r.c = (u64)(m * 18446744073709551616.0);
-  if (k > 0) {  // one unit is more than the whole range: only the maximum weighs
-    r.c = ~0ull;
-    k = 0;
-  }
-  if (k < -31) {
-    r.c = -31 - k > 63 ? 0ull : r.c >> (-31 - k);
-    k = -31;
-  }
-  if (mx == INFINITY) r.c = 0;
-  r.shift = -k;
+  const float t = fminf(fmaxf(temperature, 1e-30f), 1e30f);
+  constexpr double log2e = 1.4426950408889634074;
+  constexpr float k_hi = (float)log2e, k_lo = (float)(log2e - (double)k_hi);
+  r.mx = mx;
+  r.c_hi = k_hi / t;
+  r.c_lo = (fmaf(-r.c_hi, t, k_hi) + k_lo) / t;
+  r.low = fmaxf(fmaxf(mx - (kFrac + 1.5f) / r.c_hi, least), mx - 3e38f);
   return r;
 }
-// Distance to the maximum in the row's units (l >= low).
-__device__ __forceinline__ uint32_t distance(const RowScale& r, float l) {
-  return (uint32_t)r.top - (uint32_t)__float2int_rn(l * r.scale);
+// `table`: 2^(j / 128) as a float, and 2^(29 + j / 128) as an integer less the bits of kMagic.
+struct Entry {
+  float t;
+  uint32_t i;
+};
+constexpr float kMagic = 12582912.0f;  // 1.5 2^23
+// Of two logits: v, 2^29 to 2^30, and i, so that e^((l - mx) / T) = v 2^(-29 - n), n = (kRoundBits + 127 - i) >> 7; for l >= low.
+// nz: f2_neg_zero.
+constexpr uint32_t kRoundBits = 0x47c00000u;
+__device__ __forceinline__ void parts_of(const RowScale& r, const Entry* table, f32x2 nz, float l0, float l1, uint32_t& v0,
+                                         uint32_t& v1, uint32_t& i0, uint32_t& i1) {
+  const f32x2 minus1 = f2_both(0xbf800000u), l = f2_pack(l0, l1), nm = f2_pack(-r.mx, -r.mx);
+  const f32x2 ch = f2_pack(r.c_hi, r.c_hi), cl = f2_pack(r.c_lo, r.c_lo);
+  const f32x2 d = f2_add(l, nm), bb = f2_fma(l, minus1, d);                                 // d + lost = l - mx
+  const f32x2 lost = f2_add(f2_fma(f2_fma(bb, minus1, d), minus1, l), f2_fma(bb, minus1, nm));
+  const f32x2 np = f2_mul(d, f2_pack(-r.c_hi, -r.c_hi), nz);                                // -p
+  const f32x2 e = f2_fma(lost, ch, f2_fma(d, cl, f2_fma(d, ch, np)));                       // p + e = y
+  const f32x2 round = f2_pack(kRound, kRound), s = f2_fma(np, minus1, round);               // multiples of 1 / 128 of p
+  const f32x2 g = f2_add(f2_fma(np, minus1, f2_fma(s, minus1, round)), e);                  // what they leave of y
+  constexpr double ln2 = 0.69314718055994530942, q29 = 536870912.0;
+  constexpr float c1 = (float)(ln2 * q29), c2 = (float)(ln2 * ln2 / 2 * q29), c3 = (float)(ln2 * ln2 * ln2 / 6 * q29);
+  const f32x2 q = f2_mul(g, f2_fma(g, f2_fma(g, f2_pack(c3, c3), f2_pack(c2, c2)), f2_pack(c1, c1)), nz);  // 2^29 (2^g - 1)
+  float s0, s1;
+  f2_unpack(s, s0, s1);
+  i0 = __float_as_uint(s0);  // 128 times the rounded exponent, and the bits of kRound
+  i1 = __float_as_uint(s1);
+  const Entry t0 = table[i0 & 127], t1 = table[i1 & 127];
+  float m0, m1;
+  f2_unpack(f2_fma(f2_pack(t0.t, t1.t), q, f2_pack(kMagic, kMagic)), m0, m1);
+  v0 = __float_as_uint(m0) + t0.i;  // 2^(29 + fraction of y)
+  v1 = __float_as_uint(m1) + t1.i;
 }
-// 2^43 e^((l - max) / T) truncated; 0 below `low` (and for NaN).  `table`: 2^(31 - j / 128).
-__device__ __forceinline__ u64 weight_of(const RowScale& r, const uint32_t* table, float l) {
-  const uint32_t d = distance(r, l);
-  const u64 y = (u64)d * (uint32_t)(r.c >> 32) + __umulhi(d, (uint32_t)r.c);  // exponent, 32 + shift fraction bits
-  const uint32_t n = (uint32_t)(y >> 32) >> r.shift, f = __funnelshift_r((uint32_t)y, (uint32_t)(y >> 32), r.shift);
-  const uint32_t t = table[f >> 25], x = f & 0x1ffffffu;  // 2^-f = 2^-(j / 128) 2^-x, x < 1/128 in units of 2^-32
-  constexpr double ln2 = 0.69314718055994530942, one = 4294967296.0;
-  constexpr uint32_t c1 = (uint32_t)(ln2 * one), c2 = (uint32_t)(ln2 * ln2 / 2 * one), c3 = (uint32_t)(ln2 * ln2 * ln2 / 6 * one);
-  // 1 - 2^-x = x ln2 - (x ln2)^2 / 2 + (x ln2)^3 / 6 - .. (the next term is below 2^-34)
-  const uint32_t q = __umulhi(x, c1 - __umulhi(x, c2 - __umulhi(x, c3)));
-  const uint32_t v = t - __umulhi(t, q);
-  return l >= r.low && n <= kFrac ? ((u64)v << 32) >> (63 - kFrac + n) : 0ull;
+// 2^43 e^((l - mx) / T) of two logits, truncated; 0 below `low` (and for NaN)
+__device__ __forceinline__ void weights_of(const RowScale& r, const Entry* table, f32x2 nz, float l0, float l1, u64& w0, u64& w1) {
+  uint32_t v0, v1, i0, i1;
+  parts_of(r, table, nz, l0, l1, v0, v1, i0, i1);
+  constexpr uint32_t n = 61 - kFrac + (kRoundBits >> 7);
+  w0 = l0 >= r.low ? ((u64)v0 << 32) >> min(n - (i0 >> 7), 63u) : 0ull;
+  w1 = l1 >= r.low ? ((u64)v1 << 32) >> min(n - (i1 >> 7), 63u) : 0ull;
 }
+// bins: two of the 128 steps an exponent has, both of one n
+__device__ __forceinline__ uint32_t bin_of_steps(uint32_t steps) { return (steps + 1) >> 1; }
+__device__ __forceinline__ int bin_exponent(int bin) { return (2 * bin + 127) >> 7; }
+
+struct Table {
+  Entry e[128];
+  // 2^(j / 128) by repeated multiplication with 2^(1/128), whose series to the sixth power is exact to 2^-52 here
+  constexpr Table() : e() {
+    constexpr double h = 0.69314718055994530942 / 128;
+    constexpr double step = 1 + h * (1 + h / 2 * (1 + h / 3 * (1 + h / 4 * (1 + h / 5 * (1 + h / 6)))));
+    double v = 1.0;
+    for (int j = 0; j < 128; ++j, v *= step) {
+      e[j].t = (float)v;
+      e[j].i = (uint32_t)(v * 536870912.0 + 0.5) - 0x4b400000u;  // the bits of kMagic
+    }
+  }
+};
+__constant__ constexpr Table kTable{};
 
 // ceil(f x) and floor(f x) for 0 <= f < 1: f = m 2^-s exactly
 __device__ __forceinline__ u64 scaled(float f, u64 x, bool up) {
@@ -133,27 +173,76 @@ __device__ __forceinline__ float order_value(uint32_t key) {
 }
 
 struct Shared {
-  uint32_t count[kBins], lo[kBins], hi[kBins];  // the histogram; at other times the list of candidates
-  uint32_t table[128];
+  // the histogram: counts, and the sums of the low 16 and the high bits of the weights' significands
+  uint32_t count[kBins], lo[kBins], hi[kBins];
+  u64 mine[kSmall], list[kSmall];               // candidates: this CTA's, all (rank 0)
+  Entry table[128];
   u64 ex[2][kMaxCluster][2];                    // what the CTAs tell one another: a pair of numbers each
-  u64 res[6];                                   // and what one of them found
+  u64 res[6];
   u64 red[kWarps][2];
-  uint32_t listed;
+  uint32_t listed, n_mine, n_before;
 };
 
 // What the tokens kept so far are: those above `value`, and its equals up to index `last`.
 struct Cut {
   float value;
   uint32_t last;
-  __device__ __forceinline__ bool has(float x, uint32_t i) const { return x > value || (x == value && i <= last); }
+  __device__ __forceinline__ bool has(float x, uint32_t i) const { return x >= value && !(x == value && i > last); }
 };
 
+template <int kType, bool kHeld>
 struct Row {
   Shared* sh;
-  const float* x;      // this CTA's slice
-  int slice;
+  const char* src;     // this CTA's logits in global memory ..
+  const float* x;      // .. and, where they are held, in shared memory
+  int slice, n;        // their number, rounded up to whole steps, and as it is
   uint32_t base, rank, size;
-  int buf = 0;
+  RowScale rs;
+  f32x2 nz;
+  bool infinite;       // the row's maximum is infinite: it is read as 0, all else as -inf
+  int buf;
+
+  static constexpr int kElem = kType == W8A8_TYPE_F32 ? 4 : 2;
+  // logits i .. i + 3 of the slice, -inf behind the row's end (no comparison below takes a NaN, and -0 is equal to 0 in all of
+  // them)
+  __device__ __forceinline__ float4 raw4(int i) const {
+    float f[4];
+    if (i + 4 <= n) {
+      if constexpr (kType == W8A8_TYPE_F32) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(src) + i / 4);
+        f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+      } else {
+        const uint2 w = __ldg(reinterpret_cast<const uint2*>(src) + i / 4);
+        const float2 a = unpack2<kType == W8A8_TYPE_BF16>(w.x), b = unpack2<kType == W8A8_TYPE_BF16>(w.y);
+        f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = -INFINITY;
+        if (i + e < n) {
+          if constexpr (kType == W8A8_TYPE_F32)
+            f[e] = __ldg(reinterpret_cast<const float*>(src) + i + e);
+          else
+            f[e] = unpack2<kType == W8A8_TYPE_BF16>(__ldg(reinterpret_cast<const uint16_t*>(src) + i + e)).x;
+        }
+      }
+    }
+    return make_float4(f[0], f[1], f[2], f[3]);
+  }
+  __device__ __forceinline__ float4 at4(int i) const {
+    if constexpr (kHeld) return *reinterpret_cast<const float4*>(x + i);
+    float4 v = raw4(i);
+    if (infinite)
+      v = make_float4(v.x == INFINITY ? 0.0f : -INFINITY, v.y == INFINITY ? 0.0f : -INFINITY,
+                      v.z == INFINITY ? 0.0f : -INFINITY, v.w == INFINITY ? 0.0f : -INFINITY);
+    return v;
+  }
+
+  __device__ __forceinline__ float at(int i) const {
+    const float4 v = at4(i & ~3);
+    return (i & 2) ? (i & 1) ? v.w : v.z : (i & 1) ? v.y : v.x;
+  }
 
   // (a, b) of every CTA, given by thread 0 .. size - 1 of each; one cluster barrier
   __device__ __forceinline__ const u64 (*tell(u64 a, u64 b))[2] {
@@ -167,222 +256,355 @@ struct Row {
     cluster_sync_all();
     return slot;
   }
-  // the block's sums of a and b, for every thread
-  __device__ __forceinline__ void block_sum(u64& a, u64& b) {
+  // the block's sum, for every thread
+  __device__ __forceinline__ u64 block_sum(u64 a) {
     a = warp_sum(a);
-    b = warp_sum(b);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) {
-      sh->red[threadIdx.x >> 5][0] = a;
-      sh->red[threadIdx.x >> 5][1] = b;
-    }
+    if ((threadIdx.x & 31) == 0) sh->red[threadIdx.x >> 5][0] = a;
     __syncthreads();
-    a = b = 0;
+    a = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      a += sh->red[w][0];
-      b += sh->red[w][1];
-    }
+    for (int w = 0; w < kWarps; ++w) a += sh->red[w][0];
+    return a;
   }
   // f(value, index) over the slice, each warp over a stretch of its own
   template <class F>
   __device__ __forceinline__ void each(F f) const {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = slice / kWarps;
+#pragma unroll 4
     for (int i = warp * part + 4 * lane; i < (warp + 1) * part; i += 128) {
-      const float4 v = *reinterpret_cast<const float4*>(x + i);
+      const float4 v = at4(i);
       f(v.x, base + i);
       f(v.y, base + i + 1);
       f(v.z, base + i + 2);
       f(v.w, base + i + 3);
     }
   }
+  // f(value, index, weight) for those that pred(value, index) takes and that weigh anything
+  template <class P, class F>
+  __device__ __forceinline__ void each_weight(P pred, F f) const {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = slice / kWarps;
+#pragma unroll 2
+    for (int i = warp * part + 4 * lane; i < (warp + 1) * part; i += 128) {
+      const float4 v = at4(i);
+      const float l[4] = {v.x, v.y, v.z, v.w};
+      bool in[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) in[e] = l[e] >= rs.low && pred(l[e], base + i + e);
+      if (!(in[0] || in[1] || in[2] || in[3])) continue;
+      u64 w[4];
+      weights_of(rs, sh->table, nz, l[0], l[1], w[0], w[1]);
+      weights_of(rs, sh->table, nz, l[2], l[3], w[2], w[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (in[e]) f(l[e], base + i + e, w[e]);
+    }
+  }
+  __device__ __forceinline__ u64 weight(float l) const {
+    u64 a, b;
+    weights_of(rs, sh->table, nz, l, l, a, b);
+    return a;
+  }
+  __device__ __forceinline__ u64 significand(float l) const {
+    uint32_t v, v1, i0, i1;
+    parts_of(rs, sh->table, nz, l, l, v, v1, i0, i1);
+    return v;
+  }
   __device__ __forceinline__ void clear() {
     for (int i = threadIdx.x; i < kBins; i += kT) sh->count[i] = sh->lo[i] = sh->hi[i] = 0;
     __syncthreads();
   }
-  __device__ __forceinline__ void add(uint32_t bin, u64 w) {
-    atomicAdd(&sh->count[bin], 1u);
-    const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh->lo[bin], lo);
-    const uint32_t up = (uint32_t)(w >> 32) + (old + lo < lo ? 1u : 0u);
-    if (up) atomicAdd(&sh->hi[bin], up);
+  __device__ __forceinline__ uint32_t bin_of(float x) const { return bin_of_steps((uint32_t)steps_of(rs, x)); }
+  // the logits that pred takes, and that may weigh anything, with their weights into the histogram
+  template <class P>
+  __device__ __forceinline__ void add_weights(P pred) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = slice / kWarps;
+#pragma unroll 2
+    for (int i = warp * part + 4 * lane; i < (warp + 1) * part; i += 128) {
+      const float4 v = at4(i);
+      const float l[4] = {v.x, v.y, v.z, v.w};
+      uint32_t s[4], b[4];
+      parts_of(rs, sh->table, nz, l[0], l[1], s[0], s[1], b[0], b[1]);
+      parts_of(rs, sh->table, nz, l[2], l[3], s[2], s[3], b[2], b[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!(l[e] >= rs.low) || !pred(l[e], base + i + e)) continue;
+        const uint32_t bin = bin_of_steps(kRoundBits - b[e]);
+        atomicAdd(&sh->count[bin], 1u);
+        atomicAdd(&sh->lo[bin], s[e] & 0xffffu);
+        atomicAdd(&sh->hi[bin], s[e] >> 16);
+      }
+    }
   }
-
-  // The bin of the cluster's histogram at which counts (or weights) above it, `c0` and `w0` before the first bin, reach the
-  // goal.  goal(total count, total weight) gives it.  Three cluster barriers.
+  // a bin of the divided range
+  __device__ __forceinline__ void add_fine(uint32_t bin, uint32_t v) {
+    atomicAdd(&sh->count[bin], 1u);
+    atomicAdd(&sh->lo[bin], v & 0xffffu);
+    atomicAdd(&sh->hi[bin], v >> 16);
+  }
+  // significands of a bin's weights, summed, as a weight
+  __device__ __forceinline__ u64 significant(u64 v, int bin) const {
+    const int up = kFrac - 29 - bin_exponent(bin);
+    return up >= 0 ? v << up : v >> -up;
+  }
+  // The bin of the cluster's histogram at which counts (or weights), c0 and w0 before the first bin, reach goal(all of the
+  // weight), or what there is.  The CTAs add up a share of the bins each.  Three cluster barriers; then the histogram may be changed.
   struct Cross {
     uint32_t bin;
-    u64 c_above, w_above, c_in, w_in, c_all, w_all;
+    u64 c_above, w_above, c_in, c_all;
   };
-  template <class Goal>
+  template <bool kFineBins, class Goal>
   __device__ __forceinline__ Cross cross(bool by_weight, u64 c0, u64 w0, Goal goal) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int seg = kBins / (int)size, per = (seg + kT - 1) / kT, first = (int)rank * seg;
-    cluster_sync_all();  // every CTA's histogram is complete
-    u64 c[4], w[4], cs = 0, ws = 0;  // this thread's bins (up to 4 where one CTA has them all)
+    const int seg = (kFineBins ? kFine : kBins) / (int)size, first = (int)rank * seg;
+    const int parts = 4 * seg <= kT ? 4 : 2 * seg <= kT ? 2 : 1, per = parts > 1 ? 1 : (seg + kT - 1) / kT;  // threads a bin, bins a thread
+    auto load = [&](int bin, int part, int n_parts, u64& c, u64& w) {
+      u64 lo = 0, hi = 0;
+      c = 0;
+      for (int r0 = part; r0 < (int)size; r0 += 8 * n_parts) {  // eight CTAs' loads ahead of their first use
+        uint32_t got[8][3];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      c[i] = w[i] = 0;
-      const int b = tid * per + i;
-      if (i < per && b < seg)
-        for (uint32_t r = 0; r < size; ++r) {
-          const uint32_t at = map_to_rank(smem_u32(sh->count) + 4u * (uint32_t)(first + b), r);
-          c[i] += ld_remote(at);
-          w[i] += ((u64)ld_remote(at + 8 * kBins) << 32) + ld_remote(at + 4 * kBins);
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t r = min((uint32_t)(r0 + k * n_parts), size - 1);
+          got[k][0] = ld_remote(map_to_rank(smem_u32(&sh->count[bin]), r));
+          got[k][1] = by_weight ? ld_remote(map_to_rank(smem_u32(&sh->lo[bin]), r)) : 0u;
+          got[k][2] = by_weight ? ld_remote(map_to_rank(smem_u32(&sh->hi[bin]), r)) : 0u;
         }
-      cs += c[i];
-      ws += w[i];
-    }
-    u64 cb = warp_scan(cs, lane), wb = warp_scan(ws, lane);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (r0 + k * n_parts < (int)size) {
+            c += got[k][0];
+            lo += got[k][1];
+            hi += got[k][2];
+          }
+      }
+      w = (hi << 16) + lo;
+    };
+    cluster_sync_all();  // every CTA's histogram is complete
+    const int mine = tid / parts * per;
+    u64 cs = 0, ws = 0;
+    if (mine < seg)
+      for (int i = 0; i < per && mine + i < seg; ++i) {
+        u64 c, w;
+        load(first + mine + i, tid % parts, parts, c, w);
+        for (int o = 1; o < parts; o <<= 1) {
+          c += __shfl_xor_sync(__activemask(), c, o);
+          w += __shfl_xor_sync(__activemask(), w, o);
+        }
+        if (tid % parts) continue;
+        cs += c;
+        ws += kFineBins ? w : significant(w, first + mine + i);
+      }
+    u64 cu = warp_scan(cs, lane), wu = warp_scan(ws, lane), ct = 0, wt = 0;
     __syncthreads();
     if (lane == 31) {
-      sh->red[warp][0] = cb;
-      sh->red[warp][1] = wb;
+      sh->red[warp][0] = cu;
+      sh->red[warp][1] = wu;
     }
     __syncthreads();
-    cb -= cs;
-    wb -= ws;
-    u64 cseg = 0, wseg = 0;
+    cu -= cs;
+    wu -= ws;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) {
       if (i < warp) {
-        cb += sh->red[i][0];
-        wb += sh->red[i][1];
+        cu += sh->red[i][0];
+        wu += sh->red[i][1];
       }
-      cseg += sh->red[i][0];
-      wseg += sh->red[i][1];
+      ct += sh->red[i][0];
+      wt += sh->red[i][1];
     }
-    const u64(*all)[2] = tell(cseg, wseg);
-    u64 ct = c0, wt = w0;
-    cb += c0;
-    wb += w0;
+    const u64(*all)[2] = tell(ct, wt);
+    cu += c0;
+    wu += w0;
+    ct = c0;
+    wt = w0;
     for (uint32_t r = 0; r < size; ++r) {
       if (r < rank) {
-        cb += all[r][0];
-        wb += all[r][1];
+        cu += all[r][0];
+        wu += all[r][1];
       }
       ct += all[r][0];
       wt += all[r][1];
     }
-    const u64 g = goal(ct, wt);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (by_weight ? wb < g && wb + w[i] >= g : cb < g && cb + c[i] >= g) {
-        const u64 v[5] = {(u64)(first + tid * per + i), cb, wb, c[i], w[i]};
-        for (uint32_t r = 0; r < size; ++r)
-#pragma unroll
-          for (int k = 0; k < 5; ++k) st_remote(map_to_rank(smem_u32(&sh->res[k]), r), v[k]);
+    const u64 g = min(goal(wt), by_weight ? wt : ct);
+    if (by_weight ? wu < g && wu + ws >= g : cu < g && cu + cs >= g) {  // within this thread's bins
+      u64 c = 0, w = 0;
+      int bin = first + mine;
+      for (;; ++bin) {
+        load(bin, 0, 1, c, w);
+        if (!kFineBins) w = significant(w, bin);
+        if (by_weight ? wu + w >= g : cu + c >= g) break;
+        cu += c;
+        wu += w;
       }
-      cb += c[i];
-      wb += w[i];
+      const u64 v[4] = {(u64)bin, cu, wu, c};
+      for (uint32_t r = 0; r < size; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) st_remote(map_to_rank(smem_u32(&sh->res[k]), r), v[k]);
     }
     cluster_sync_all();
-    return Cross{(uint32_t)sh->res[0], sh->res[1], sh->res[2], sh->res[3], sh->res[4], ct, wt};
+    return Cross{(uint32_t)sh->res[0], sh->res[1], sh->res[2], sh->res[3], ct};
   }
+
+  // The index of the slice at which the sum of f(value, index), `before` ahead of the slice and red[w][0] over warp w's stretch,
+  // passes `target`, and f there; for the CTA that has it.  The warps divide the stretch once more, then a warp's lanes.
+  template <class F>
+  __device__ __forceinline__ void find(u64 before, u64 target, F f, int& index, u64& value) const {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = slice / kWarps, sub = part / kWarps;
+    int w = 0;
+    for (; w < kWarps - 1 && before + sh->red[w][0] <= target; ++w) before += sh->red[w][0];
+    u64 sum = 0;
+    const int start = w * part + warp * sub;
+    for (int i = lane; i < sub; i += 32) sum += f(at(start + i), base + start + i);
+    sum = warp_sum(sum);
+    if (lane == 0) sh->red[warp][1] = sum;
+    __syncthreads();
+    int v = 0;
+    for (; v < kWarps - 1 && before + sh->red[v][1] <= target; ++v) before += sh->red[v][1];
+    if (warp != v) return;
+    const int per = (sub + 31) / 32;
+    sum = 0;
+    for (int i = lane * per; i < min(sub, lane * per + per); ++i) sum += f(at(start + i), base + start + i);
+    u64 upto = before + warp_scan(sum, lane);
+    if (upto <= target || upto - sum > target) return;
+    upto -= sum;
+    for (int i = lane * per; i < min(sub, lane * per + per); ++i) {
+      value = f(at(start + i), base + start + i);
+      upto += value;
+      if (upto > target) {
+        index = start + i;
+        return;
+      }
+    }
+  }
+
 };
 
 struct Found {
   Cut cut;
-  u64 weight;  // of the kept tokens
+  bool done;  // the cut by weight is in it
 };
 
-// Where the kept tokens end, among those of `in`: the first top_k (by_weight false: goal tokens), or the shortest prefix that
-// weighs share of the weight of `in` (`all`, or with all == 0 what the first histogram finds).  With `both`, a cut by count is
-// followed by the one by weight where the candidates are few.
-struct Filters {
-  int k;
-  float p;
-};
-
-template <class Weight>
-__device__ Found find_cut(Row& row, const RowScale& rs, const Weight& weight, const Cut in, bool by_weight, u64 known_all,
-                          const Filters fl, bool& done) {
+// Where the kept tokens end, among those of `in`: the first k (by_weight false), or the shortest prefix that weighs p of them.
+// Where the candidates of a cut by count are few, the cut by weight is made with it.
+template <int kType, bool kHeld>
+__device__ __forceinline__ Found find_cut(Row<kType, kHeld>& row, const Cut in, bool by_weight, int k, float p) {
   Shared* sh = row.sh;
+  const RowScale& rs = row.rs;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t far = distance(rs, rs.low);
-  const int sh1 = max(0, 32 - __clz((int)(far | 1u)) - 11);  // far >> sh1 < 2048; the last bin is for what weighs nothing
-  auto bin_of = [&](float x) { return x >= rs.low ? min(distance(rs, x) >> sh1, (uint32_t)kBins - 2) : (uint32_t)kBins - 1; };
-  auto goal = [&](u64, u64 w_all) {
-    return by_weight ? max(scaled(fl.p, known_all ? known_all : w_all, true), 1ull) : (u64)fl.k;
-  };
+  u64 want = 0;
   row.clear();
-  row.each([&](float x, uint32_t i) {
-    if (in.has(x, i) && (!by_weight || x >= rs.low)) row.add(bin_of(x), weight(x));
-  });
-  Row::Cross c = row.cross(by_weight, 0, 0, goal);
-  const u64 all = known_all ? known_all : c.w_all, want = goal(0, all);
-  if (!by_weight && c.bin == kBins - 1) return Found{in, c.w_all};  // all that weighs anything is among the first k
-  const uint32_t bin = c.bin;
-
-  if (c.c_above + c.c_in <= kSmall) {
-    // ---- few: one CTA sorts them (largest logit first, then lowest index) and cuts exactly
-    u64* list = reinterpret_cast<u64*>(sh->count);  // free since the last barrier
-    static_assert(sizeof(u64) * kSmall <= sizeof(uint32_t) * kBins, "the list fits over the counts");
-    if (tid == 0) sh->listed = 0;
-    cluster_sync_all();
-    const uint32_t list0 = map_to_rank(smem_u32(list), 0), n0 = map_to_rank(smem_u32(&sh->listed), 0);
-    row.each([&](float x, uint32_t i) {
-      if (in.has(x, i) && (!by_weight || x >= rs.low) && bin_of(x) <= bin)
-        st_remote(list0 + 8 * add_remote(n0, 1), ((u64)float_order_key(x) << 32) | (uint32_t)~i);
+  if (by_weight)
+    row.add_weights([&](float x, uint32_t i) { return in.has(x, i); });
+  else
+    row.each([&](float x, uint32_t) {
+      if (x >= rs.low) atomicAdd(&sh->count[row.bin_of(x)], 1u);
     });
+  typename Row<kType, kHeld>::Cross c = row.template cross<false>(
+      by_weight, 0, 0, [&](u64 w_all) { return want = by_weight ? max(scaled(p, w_all, true), 1ull) : (u64)k; });
+  if (!by_weight && c.c_all <= want) return Found{in, false};  // no more than k weigh anything
+  const uint32_t bin = c.bin;
+  u64 c_above = c.c_above, v_above = 0;
+  if (by_weight) {  // from here on in sums of the bin's significands: the least whose weight reaches the rest
+    const int up = kFrac - 29 - bin_exponent((int)bin);
+    const u64 rest = want - c.w_above;
+    want = up >= 0 ? (rest + (1ull << up) - 1) >> up : rest << -up;
+  }
+
+  // with few tokens down to the bin's end, all of them are sorted, and both cuts made
+  const bool both = !by_weight && c_above + c.c_in <= kSmall;
+  if (both || c.c_in <= kSmall) {
+    // ---- few: one CTA sorts them (largest logit first, then lowest index) and cuts exactly.  Each CTA's in its own shared
+    // memory first, then in one go behind the others'
+    const float from = __uint_as_float(kRoundBits - 2 * bin);  // the bin's two steps
+    const float to = both || bin == 0 ? kRound : __uint_as_float(kRoundBits - 2 * bin + 1);
+    row.each([&](float x, uint32_t i) {
+      const float s = rounded(rs, x);
+      if (s >= from && s <= to && x >= rs.low && in.has(x, i))
+        sh->mine[atomicAdd(&sh->n_mine, 1u)] = ((u64)float_order_key(x) << 32) | (uint32_t)~i;
+    });
+    __syncthreads();
+    const uint32_t n_mine = sh->n_mine;
+    if (tid == 0 && n_mine) sh->n_before = add_remote(map_to_rank(smem_u32(&sh->listed), 0), n_mine);
+    __syncthreads();
+    const uint32_t list0 = map_to_rank(smem_u32(sh->list), 0) + 8 * sh->n_before;
+    for (uint32_t i = tid; i < n_mine; i += kT) st_remote(list0 + 8 * i, sh->mine[i]);
+    if (tid == 0) sh->n_mine = 0;
     cluster_sync_all();
     if (row.rank == 0) {
-      const int n = (int)(c.c_above + c.c_in);
-      int n2 = 32;
-      while (n2 < n) n2 <<= 1;
-      for (int i = n + tid; i < n2; i += kT) list[i] = 0;
-      __syncthreads();
-      for (int k = 2; k <= n2; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-          for (int i = tid; i < n2 / 2; i += kT) {
-            const int a = 2 * i - (i & (j - 1)), b = a + j;
-            const u64 u = list[a], v = list[b];
-            if ((u < v) == ((a & k) == 0)) {
-              list[a] = v;
-              list[b] = u;
+      u64* list = sh->list;
+      const int n = (int)sh->listed;
+      if (n <= kT / 2) {  // each token's place is the number of greater ones: two threads a token
+        const int i = tid >> 1;
+        const u64 v = i < n ? list[i] : 0;
+        int place = 0;
+        for (int j = tid & 1; j < n; j += 2) place += list[j] > v;
+        place += __shfl_xor_sync(0xffffffffu, place, 1);
+        if (i < n && (tid & 1) == 0) sh->mine[place] = v;
+        list = sh->mine;
+        __syncthreads();
+      } else {
+        int n2 = kT;
+        while (n2 < n) n2 <<= 1;
+        for (int i = n + tid; i < n2; i += kT) list[i] = 0;
+        __syncthreads();
+        for (int len = 2; len <= n2; len <<= 1)
+          for (int j = len >> 1; j > 0; j >>= 1) {
+            for (int i = tid; i < n2 / 2; i += kT) {
+              const int a = 2 * i - (i & (j - 1)), b = a + j;
+              const u64 u = list[a], v = list[b];
+              if ((u < v) == ((a & len) == 0)) {
+                list[a] = v;
+                list[b] = u;
+              }
             }
+            __syncthreads();
           }
-          __syncthreads();
-        }
-      const int m = by_weight || fl.k > n ? n : fl.k;
-      u64 w[2], mine = 0;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        w[i] = 2 * tid + i < m ? weight(order_value((uint32_t)(list[2 * tid + i] >> 32))) : 0ull;
-        mine += w[i];
       }
-      u64 before = warp_scan(mine, lane);
-      if (lane == 31) sh->red[warp][0] = before;
-      __syncthreads();
-      before -= mine;
-      u64 total = 0;
+      if (tid == 0) sh->listed = 0;
+      if (!by_weight && !both) {
+        if (tid == 0) sh->res[0] = list[want - c_above - 1];
+      } else {
+        // by weight: the significands of the one bin; else weights
+        const int m = by_weight || k > n ? n : k;
+        u64 w[2], mine = 0;
 #pragma unroll
-      for (int i = 0; i < kWarps; ++i) {
-        if (i < warp) before += sh->red[i][0];
-        total += sh->red[i][0];
-      }
-      const bool cut_weight = by_weight || fl.p < 1.0f;
-      const u64 target = !cut_weight ? ~0ull : by_weight ? want : max(scaled(fl.p, total, true), 1ull);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int at = 2 * tid + i;
-        // the last one kept: the first at which the sum reaches the target, or the last of the m
-        if (at < m && before < target && (before + w[i] >= target || at == m - 1)) {
-          sh->res[0] = list[at];
-          sh->res[1] = before + w[i];
+        for (int i = 0; i < 2; ++i) {
+          w[i] = 0;
+          if (2 * tid + i < m) {
+            const float l = order_value((uint32_t)(list[2 * tid + i] >> 32));
+            w[i] = by_weight ? row.significand(l) : row.weight(l);
+          }
+          mine += w[i];
         }
-        before += w[i];
+        u64 before = warp_scan(mine, lane);
+        if (lane == 31) sh->red[warp][0] = before;
+        __syncthreads();
+        before -= mine;
+        u64 total = 0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+          if (i < warp) before += sh->red[i][0];
+          total += sh->red[i][0];
+        }
+        const u64 target = by_weight ? want : p < 1.0f ? max(scaled(p, total, true), 1ull) : ~0ull;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {  // the last one kept: where the sum reaches the target, or the last of the m
+          const int at = 2 * tid + i;
+          if (at < m && before < target && (before + w[i] >= target || at == m - 1)) sh->res[0] = list[at];
+          before += w[i];
+        }
       }
       __syncthreads();
     }
-    const u64(*told)[2] = row.tell(sh->res[0], sh->res[1]);
-    done = true;
-    return Found{Cut{order_value((uint32_t)(told[0][0] >> 32)), ~(uint32_t)told[0][0]}, told[0][1]};
+    const u64(*told)[2] = row.tell(sh->res[0], 0);
+    return Found{Cut{order_value((uint32_t)(told[0][0] >> 32)), ~(uint32_t)told[0][0]}, by_weight || both};
   }
 
-  // ---- many: divide the bin by the order of its floats
+  // ---- many: divide the range by the order of its floats
   uint32_t kmin = 0xffffffffu, kmax = 0;
   row.each([&](float x, uint32_t i) {
-    if (in.has(x, i) && bin_of(x) == bin) {
+    if (x >= rs.low && row.bin_of(x) == bin && in.has(x, i)) {
       kmin = min(kmin, float_order_key(x));
       kmax = max(kmax, float_order_key(x));
     }
@@ -390,66 +612,54 @@ __device__ Found find_cut(Row& row, const RowScale& rs, const Weight& weight, co
   kmin = __reduce_min_sync(0xffffffffu, kmin);
   kmax = __reduce_max_sync(0xffffffffu, kmax);
   __syncthreads();
-  if (lane == 0) sh->red[warp][0] = ((u64)kmin << 32) | kmax;
+  if (lane == 0) sh->red[warp][1] = ((u64)kmin << 32) | kmax;
   __syncthreads();
   auto fold = [&](u64 v) {
     kmin = min(kmin, (uint32_t)(v >> 32));
     kmax = max(kmax, (uint32_t)v);
   };
-  for (int i = 0; i < kWarps; ++i) fold(sh->red[i][0]);
+  for (int i = 0; i < kWarps; ++i) fold(sh->red[i][1]);
   const u64(*ends)[2] = row.tell(((u64)kmin << 32) | kmax, 0);
   for (uint32_t r = 0; r < row.size; ++r) fold(ends[r][0]);
-  u64 c_above = c.c_above, w_above = c.w_above, c_in = c.c_in;
-  while (kmin < kmax) {
+  do {
     const int s = max(0, 32 - __clz((int)(kmax - kmin)) - 11);
     row.clear();
     row.each([&](float x, uint32_t i) {
       const uint32_t key = float_order_key(x);
-      if (key >= kmin && key <= kmax && in.has(x, i)) row.add((kmax - key) >> s, weight(x));
+      if (x >= rs.low && key >= kmin && key <= kmax && in.has(x, i)) row.add_fine((kmax - key) >> s, by_weight ? (uint32_t)row.significand(x) : 0u);
     });
-    c = row.cross(by_weight, c_above, w_above, [&](u64, u64) { return want; });
+    c = row.template cross<true>(by_weight, c_above, v_above, [&](u64) { return want; });
     c_above = c.c_above;
-    w_above = c.w_above;
-    c_in = c.c_in;
+    v_above = c.w_above;
     const uint32_t top = kmax - (c.bin << s);
     kmin = (1u << s) - 1u >= top - kmin ? kmin : top - ((1u << s) - 1u);
     kmax = top;
-  }
+  } while (kmin < kmax);
   // ---- one value is left: as many of its equals as it takes, the lower indices first
   const float value = order_value(kmax);
-  const u64 each_w = weight(value);
-  const u64 ties = min(by_weight ? (want - w_above + each_w - 1) / each_w : want - c_above, c_in);
-  Found f{Cut{value, in.value == value ? in.last : 0xffffffffu}, w_above + ties * each_w};
-  if (ties == c_in) return f;
-  u64 eq = 0, none = 0;
+  const u64 one = row.significand(value);
+  const u64 ties = min(by_weight ? (want - v_above + one - 1) / one : want - c_above, c.c_in);
+  Found f{Cut{value, in.value == value ? in.last : 0xffffffffu}, by_weight};
+  if (ties == c.c_in) return f;
+  u64 eq = 0;
   row.each([&](float x, uint32_t) { eq += x == value; });
-  const u64 wsum = warp_sum(eq);
-  u64 csum = eq;
-  row.block_sum(csum, none);
+  const u64 csum = row.block_sum(eq);
   const u64(*counts)[2] = row.tell(csum, 0);
   u64 before = 0;
   for (uint32_t r = 0; r < row.rank; ++r) before += counts[r][0];
-  __syncthreads();
-  if (lane == 0) sh->red[warp][0] = wsum;
-  __syncthreads();
-  for (int i = 0; i < warp; ++i) before += sh->red[i][0];
-  if (before < ties && before + wsum >= ties) {  // this warp holds the last of them
-    const int part = row.slice / kWarps;
-    for (int i = warp * part; i < (warp + 1) * part; i += 32) {
-      const bool hit = row.x[i + lane] == value;
-      const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-      if (hit && before + __popc(hits & ((2u << lane) - 1u)) == ties) {
-        for (uint32_t r = 0; r < row.size; ++r) st_remote(map_to_rank(smem_u32(&sh->res[0]), r), row.base + i + lane);
-      }
-      before += __popc(hits);
-    }
+  if (before < ties && before + csum >= ties) {  // this CTA holds the last of them
+    int index = -1;
+    u64 v;
+    row.find(before, ties - 1, [&](float x, uint32_t) -> u64 { return x == value; }, index, v);
+    if (index >= 0)
+      for (uint32_t r = 0; r < row.size; ++r) st_remote(map_to_rank(smem_u32(&sh->res[5]), r), row.base + index);
   }
   cluster_sync_all();
-  f.cut.last = (uint32_t)sh->res[0];
+  f.cut.last = (uint32_t)sh->res[5];
   return f;
 }
 
-template <int kType>
+template <int kType, bool kHeld>
 __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64_t row_stride, int V, int slice, w8a8_sampling sp,
                                                        const float* __restrict__ u, int32_t* __restrict__ tokens,
                                                        float* __restrict__ probs) {
@@ -460,79 +670,33 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
   asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(size));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row = blockIdx.x / size;
-  if (tid < 128) sh.table[tid] = (uint32_t)rint(exp2(31.0 - tid / 128.0));
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");  // waited for after the load
+  if (tid < 128) sh.table[tid] = kTable.e[tid];
+  if (tid == 0) sh.listed = sh.n_mine = 0;
   pdl_wait();
   pdl_trigger();
-  Row rw{&sh, xs, slice, rank * (uint32_t)slice, rank, size};
+  const uint32_t base = rank * (uint32_t)slice;
+  Row<kType, kHeld> rw{&sh, static_cast<const char*>(logits) + ((int64_t)row * row_stride + base) * Row<kType, kHeld>::kElem, xs,
+                       slice, min(slice, max(0, V - (int)base)), base, rank, size, {}, f2_neg_zero(), false, 0};
   const float temp = sp.temperature ? sp.temperature[row] : 1.0f;
   const int k = sp.top_k ? sp.top_k[row] : 0;
   const float top_p = sp.top_p ? sp.top_p[row] : 1.0f, min_p = sp.min_p ? sp.min_p[row] : 0.0f;
 
-  // ---- the slice into shared memory (NaN as -inf, -0 as 0), its maximum and least finite value
+  // ---- the slice's maximum and least finite value
   float mx = -INFINITY, mn = INFINITY;
   uint32_t at = 0;
-  auto take = [&](float l, uint32_t i) {
-    l = isnan(l) ? -INFINITY : l + 0.0f;
-    if (l > mx) {  // indices ascend: the first of equals stays
-      mx = l;
-      at = i;
-    }
-    if (l > -INFINITY) mn = fminf(mn, l);
-    return l;
-  };
-  {
-    constexpr int kEach = kType == W8A8_TYPE_F32 ? 4 : 8, kAhead = kType == W8A8_TYPE_F32 ? 8 : 4;
-    constexpr int kElem = kType == W8A8_TYPE_F32 ? 4 : 2;
-    const char* src = static_cast<const char*>(logits) + (int64_t)row * row_stride * kElem;
-    const int n = min(slice, max(0, V - (int)rw.base));  // logits of this CTA
-    for (int i0 = 0; i0 < slice; i0 += kT * kEach * kAhead) {
-      uint4 v[kAhead];
+#pragma unroll 8
+  for (int i = 4 * tid; i < slice; i += 4 * kT) {
+    const float4 v = rw.raw4(i);
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    if constexpr (kHeld) *reinterpret_cast<float4*>(xs + i) = v;
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + (j * kT + tid) * kEach;
-        if (i + kEach <= n) v[j] = ldg_stream(src + (int64_t)(rw.base + i) * kElem);
+    for (int e = 0; e < 4; ++e) {
+      if (f[e] > mx) {  // indices ascend: the first of equals stays
+        mx = f[e];
+        at = base + i + e;
       }
-#pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const int i = i0 + (j * kT + tid) * kEach;
-        if (i >= slice) continue;
-        float f[kEach];
-        if (i + kEach <= n) {
-          const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-          if constexpr (kType == W8A8_TYPE_F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(w[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if constexpr (kType == W8A8_TYPE_BF16) {
-                f[2 * e] = bf16_lo(w[e]);
-                f[2 * e + 1] = bf16_hi(w[e]);
-              } else {
-                const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[e]));
-                f[2 * e] = h.x;
-                f[2 * e + 1] = h.y;
-              }
-            }
-          }
-        } else {  // the row's ragged end
-#pragma unroll
-          for (int e = 0; e < kEach; ++e) {
-            f[e] = -INFINITY;
-            if (i + e < n) {
-              const char* p = src + (int64_t)(rw.base + i + e) * kElem;
-              if constexpr (kType == W8A8_TYPE_F32) f[e] = *reinterpret_cast<const float*>(p);
-              if constexpr (kType == W8A8_TYPE_BF16) f[e] = bf16_bits_to_f32(*reinterpret_cast<const uint16_t*>(p));
-              if constexpr (kType == W8A8_TYPE_F16) f[e] = __half2float(*reinterpret_cast<const __half*>(p));
-            }
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) f[e] = take(f[e], rw.base + i + e);
-#pragma unroll
-        for (int e = 0; e < kEach; e += 4)
-          *reinterpret_cast<float4*>(xs + i + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
-      }
+      if (f[e] > -INFINITY) mn = fminf(mn, f[e]);
     }
   }
   u64 best = ((u64)float_order_key(mx) << 32) | (uint32_t)~at;
@@ -550,13 +714,14 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
     least_key = min(least_key, (uint32_t)sh.red[i][1]);
   }
   // the peers run: their shared memory may be written
-  cluster_sync_all();
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
   const u64(*tops)[2] = rw.tell(best, least_key);
   for (uint32_t r = 0; r < size; ++r) {
     best = max(best, tops[r][0]);
     least_key = min(least_key, (uint32_t)tops[r][1]);
   }
   mx = order_value((uint32_t)(best >> 32));
+  mn = order_value(least_key);
   if (mx == -INFINITY || !(temp > 0.0f)) {
     if (rank == 0 && tid == 0) {
       tokens[row] = mx == -INFINITY ? -1 : (int32_t)~(uint32_t)best;
@@ -564,31 +729,32 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
     }
     return;
   }
-
-  const RowScale rs = row_scale(mx, order_value(least_key), temp);
-  auto weight = [&](float l) { return weight_of(rs, sh.table, l); };
+  if (mx == INFINITY) {  // infinities share the weight: a row of zeros in their places
+    rw.infinite = true;
+    if constexpr (kHeld) {
+      for (int i = tid; i < slice; i += kT) xs[i] = xs[i] == INFINITY ? 0.0f : -INFINITY;
+      __syncthreads();
+    }
+    mx = mn = 0.0f;
+  }
+  rw.rs = row_scale(mx, mn, temp);
   Cut cut{-INFINITY, 0xffffffffu};
-  const Filters fl{k, top_p};
-  bool done = false;
-  if (k > 0 && k < V) {
-    const Found f = find_cut(rw, rs, weight, cut, false, 0, fl, done);
+  // by count, then by weight (one call in a loop, so that it is compiled once, in place)
+  for (int by_weight = k > 0 && k < V ? 0 : 1; by_weight < (top_p < 1.0f ? 2 : 1); ++by_weight) {
+    const Found f = find_cut(rw, cut, by_weight != 0, k, top_p);
     cut = f.cut;
-    if (!done && top_p < 1.0f) cut = find_cut(rw, rs, weight, cut, true, f.weight, fl, done).cut;
-  } else if (top_p < 1.0f) {
-    cut = find_cut(rw, rs, weight, cut, true, 0, fl, done).cut;
+    if (f.done) break;
   }
 
   // ---- the kept weights, and the token
   const u64 least = !(min_p > 0.0f) ? 0ull : min_p >= 1.0f ? 1ull << kFrac : scaled(min_p, 1ull << kFrac, true);
-  auto kept = [&](float x, uint32_t i) -> u64 {
-    if (!cut.has(x, i)) return 0ull;
-    const u64 w = weight(x);
-    return w >= least || x == mx ? w : 0ull;
-  };
-  u64 mine = 0, none = 0;
-  rw.each([&](float x, uint32_t i) { mine += kept(x, i); });
-  const u64 wsum = warp_sum(mine);
-  rw.block_sum(mine, none);
+  u64 mine = 0;
+  if (least)
+    rw.each_weight([&](float x, uint32_t i) { return cut.has(x, i); },
+                   [&](float x, uint32_t, u64 w) { mine += w >= least || x == mx ? w : 0ull; });
+  else
+    rw.each_weight([&](float x, uint32_t i) { return cut.has(x, i); }, [&](float, uint32_t, u64 w) { mine += w; });
+  mine = rw.block_sum(mine);
   const u64(*sums)[2] = rw.tell(mine, 0);
   u64 total = 0, before = 0;
   for (uint32_t r = 0; r < size; ++r) {
@@ -599,47 +765,37 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
   uu = uu >= 0.0f ? fminf(uu, 0x1.fffffep-1f) : 0.0f;
   const u64 target = scaled(uu, total, false);
   if (!(target >= before && target < before + mine)) return;  // another CTA's
-  __syncthreads();
-  if (lane == 0) sh.red[warp][0] = wsum;
-  __syncthreads();
-  for (int i = 0; i < warp; ++i) before += sh.red[i][0];
-  if (!(target >= before && target < before + wsum)) return;  // another warp's
-  const int part = slice / kWarps;
-  for (int i = warp * part; i < (warp + 1) * part; i += 32) {
-    const u64 w = kept(xs[i + lane], rw.base + i + lane);
-    const u64 upto = before + warp_scan(w, lane);
-    if (upto > target && upto - w <= target) {
-      tokens[row] = (int32_t)(rw.base + i + lane);
-      if (probs) probs[row] = (float)((double)w / (double)total);
-    }
-    before = __shfl_sync(0xffffffffu, upto, 31);
-    if (before > target) break;
+  int index = -1;
+  u64 w;
+  rw.find(before, target,
+          [&](float x, uint32_t i) -> u64 {
+            if (!(x >= rw.rs.low) || !cut.has(x, i)) return 0;
+            const u64 v = rw.weight(x);
+            return v >= least || x == mx ? v : 0;
+          },
+          index, w);
+  if (index >= 0) {
+    tokens[row] = (int32_t)(base + index);
+    if (probs) probs[row] = (float)((double)w / (double)total);
   }
 }
 
-template <int kType>
-w8a8_status launch(const void* logits, int64_t row_stride, int M, int V, const w8a8_sampling& sp, const float* u, int32_t* tokens,
-                   float* probs, int sms, cudaStream_t st) {
-  // CTAs a row: enough that a slice is 16384 logits at most (64 KB, two CTAs an SM), more for few rows, whose latency is
-  // that of a pass over a slice
-  int size = 1;
-  auto slice_of = [&](int n) { return (((V + n - 1) / n) + kUnit - 1) / kUnit * kUnit; };
-  while (size < kMaxCluster &&
-         (slice_of(size) > 16384 || (slice_of(size) > kUnit && (long long)M * size * 2 <= 2 * sms)))
-    size *= 2;
-  const int slice = slice_of(size);
+template <int kType, bool kHeld>
+w8a8_status launch(int size, int slice, const void* logits, int64_t row_stride, int M, int V, const w8a8_sampling& sp,
+                   const float* u, int32_t* tokens, float* probs, cudaStream_t st) {
   static bool attr_set[64] = {};
   int dev = 0;
   W8A8_CUDA(cudaGetDevice(&dev));
   if (dev >= 0 && dev < 64 && !attr_set[dev]) {
-    W8A8_CUDA(cudaFuncSetAttribute(sample_kernel<kType>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSlice * 4));
-    W8A8_CUDA(cudaFuncSetAttribute(sample_kernel<kType>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    if (kHeld)
+      W8A8_CUDA(cudaFuncSetAttribute(sample_kernel<kType, kHeld>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldSlice * 4));
+    W8A8_CUDA(cudaFuncSetAttribute(sample_kernel<kType, kHeld>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     attr_set[dev] = true;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(M * size));
   cfg.blockDim = dim3(kT);
-  cfg.dynamicSmemBytes = (size_t)slice * 4;
+  cfg.dynamicSmemBytes = kHeld ? (size_t)slice * 4 : 0;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -649,7 +805,7 @@ w8a8_status launch(const void* logits, int64_t row_stride, int M, int V, const w
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  W8A8_CUDA(cudaLaunchKernelEx(&cfg, sample_kernel<kType>, logits, row_stride, V, slice, sp, u, tokens, probs));
+  W8A8_CUDA(cudaLaunchKernelEx(&cfg, sample_kernel<kType, kHeld>, logits, row_stride, V, slice, sp, u, tokens, probs));
   return W8A8_OK;
 }
 
@@ -657,9 +813,24 @@ w8a8_status launch(const void* logits, int64_t row_stride, int M, int V, const w
 
 w8a8_status launch_sample(int dtype, const void* logits, int64_t row_stride, int M, int V, const w8a8_sampling& sp,
                           const float* u, int32_t* tokens, float* probs, int sms, cudaStream_t st) {
-  return dtype == W8A8_TYPE_F32    ? launch<W8A8_TYPE_F32>(logits, row_stride, M, V, sp, u, tokens, probs, sms, st)
-         : dtype == W8A8_TYPE_BF16 ? launch<W8A8_TYPE_BF16>(logits, row_stride, M, V, sp, u, tokens, probs, sms, st)
-                                   : launch<W8A8_TYPE_F16>(logits, row_stride, M, V, sp, u, tokens, probs, sms, st);
+  // CTAs a row: as many as all rows' clusters can run at once (two CTAs an SM; clusters of 16 and 8 leave some SMs of a GPC
+  // unused, and with a slice in shared memory one CTA fills an SM), down to one step a warp and up to the longest slice
+  int size = kMaxCluster;
+  auto slice_of = [&](int n) { return (((V + n - 1) / n) + kUnit - 1) / kUnit * kUnit; };
+  auto room = [&](int n) { return n == 16 ? 3 * sms / 4 : n == 8 ? 15 * sms / 8 : 2 * sms; };
+  while (size > 1 && ((long long)M * size > room(size) || slice_of(size) == slice_of(size / 2)) &&
+         slice_of(size / 2) <= kMostSlice)
+    size /= 2;
+  const int slice = slice_of(size);
+  auto go = [&](auto type) {
+    constexpr int kType = decltype(type)::value;
+    const bool held = slice <= kHeldSlice && (4 * slice <= 3 * kHeldSlice || (long long)M * size <= room(16));
+    return held ? launch<kType, true>(size, slice, logits, row_stride, M, V, sp, u, tokens, probs, st)
+                               : launch<kType, false>(size, slice, logits, row_stride, M, V, sp, u, tokens, probs, st);
+  };
+  return dtype == W8A8_TYPE_F32    ? go(std::integral_constant<int, W8A8_TYPE_F32>())
+         : dtype == W8A8_TYPE_BF16 ? go(std::integral_constant<int, W8A8_TYPE_BF16>())
+                                   : go(std::integral_constant<int, W8A8_TYPE_F16>());
 }
 
 }  // namespace w8a8
