@@ -47,6 +47,7 @@ struct LineStart {
   long long head_cost;          // key tiles of one head of sequence s
   long long rest;               // key tiles of sequence s before `begin`
   int s, ctas;
+  SeqShape q;                   // of sequence s
 };
 
 // Key tiles of one head of each lane's sequence (0 rows: none).  Sequences of many row tiles are summed by the whole warp, so
@@ -74,22 +75,27 @@ __device__ __forceinline__ long long head_cost(const SeqShape& q, int window, in
   return cost;
 }
 
-// All of the block's kT threads; `out` and `scan` (kT / 32 words) in shared memory.  Each thread takes `per` neighbouring sequences.
+// All of the block's kT threads; `out` and `scan` (kT / 32 words) in shared memory.  Each thread takes `per` neighbouring sequences; up
+// to 32 of them are one warp's alone.  A stretch has at least `least` key tiles (but the line's last).
 template <int kT>
 __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, int n_kv, int window, int tt, int bk_shift,
-                                           LineStart* out, long long* scan) {
+                                           int least, LineStart* out, long long* scan) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (b.n_seqs + kT - 1) / kT;
+  const bool one_warp = b.n_seqs <= 32;
+  if (one_warp && warp > 0) {
+    __syncthreads();
+    return;
+  }
+  const int per = one_warp ? 1 : (b.n_seqs + kT - 1) / kT;
+  SeqShape q{0, 0, 0, 0};
   auto cost_of = [&](int s) {
-    SeqShape q{0, 0, 0, 0};
+    q = SeqShape{0, 0, 0, 0};
     if (s < b.n_seqs) q = seq_shape(b, s, page_shift);
     return head_cost(q, window, tt, bk_shift, lane);
   };
-  long long mine = 0, one = 0;
-  for (int i = 0; i < per; ++i) {
-    one = cost_of(tid * per + i);
-    mine += one;
-  }
+  long long mine = 0;
+  for (int i = 0; i < per; ++i) mine += cost_of(tid * per + i);
+  const long long one = mine;
   mine *= n_kv;
   long long upto = mine;
 #pragma unroll
@@ -97,28 +103,32 @@ __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, 
     const long long x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
-  if (lane == 31) scan[warp] = upto;
-  __syncthreads();
   long long total = 0;
-  for (int w = 0; w < kT / 32; ++w) {
-    if (w < warp) upto += scan[w];
-    total += scan[w];
+  if (one_warp) {
+    total = __shfl_sync(0xffffffffu, upto, 31);
+  } else {
+    if (lane == 31) scan[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < kT / 32; ++w) {
+      if (w < warp) upto += scan[w];
+      total += scan[w];
+    }
   }
-  const int ctas = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
+  const int ctas = (int)min((long long)gridDim.x, (total + least - 1) / least), cta = blockIdx.x;
   if (cta >= ctas) {
-    if (tid == 0) *out = LineStart{total, 0, 0, 1, 0, 0, ctas};
+    if (tid == 0) *out = LineStart{total, 0, 0, 1, 0, 0, ctas, q};
     __syncthreads();
     return;
   }
   const long long begin = total * cta / ctas, end = total * (cta + 1) / ctas;
   const bool owner = begin >= upto - mine && begin < upto;
   if (per == 1) {
-    if (owner) *out = LineStart{total, begin, end, one, begin - (upto - mine), tid, ctas};
+    if (owner) *out = LineStart{total, begin, end, one, begin - (upto - mine), tid, ctas, q};
   } else if (__any_sync(0xffffffffu, owner)) {  // the owner's warp walks its sequences again
     long long at = upto - mine;
     for (int i = 0; i < per; ++i) {
       const long long c = cost_of(tid * per + i);
-      if (begin >= at && begin < at + c * n_kv) *out = LineStart{total, begin, end, c, begin - at, tid * per + i, ctas};
+      if (begin >= at && begin < at + c * n_kv) *out = LineStart{total, begin, end, c, begin - at, tid * per + i, ctas, q};
       at += c * n_kv;
     }
   }
@@ -141,9 +151,11 @@ struct Walk {
   __device__ __forceinline__ void start(const LineStart& ls, const PagedBatch& b, int page_shift, int window, int tt,
                                         int bk_shift, int lane) {
     s = ls.s;
-    q = seq_shape(b, s, page_shift);
+    q = ls.q;
     row_tiles = (q.rows + tt - 1) / tt;
-    h = (int)(ls.rest / ls.head_cost);
+    h = ls.rest < ls.head_cost ? 0
+        : ((ls.rest | ls.head_cost) >> 31) == 0 ? (int)((uint32_t)ls.rest / (uint32_t)ls.head_cost)
+                                                 : (int)(ls.rest / ls.head_cost);
     long long left = ls.rest - h * ls.head_cost;  // key tiles of this head before the stretch
     at = ls.begin;
     end = ls.end;
@@ -203,6 +215,15 @@ struct Walk {
   }
   __device__ __forceinline__ int hi(int tt) const { return q.pos0 + min(q.rows, (t + 1) * tt) - 1; }
 };
+
+// The pages of 32 consecutive 16-key groups, one a lane (-1: none, or none of its box of `box` keys in lo .. hi), beginning with
+// position p0 of sequence s.
+__device__ __forceinline__ int group_page(const PagedBatch& b, const PagedCache& c, int s, int p0, int lo, int hi, int box, int lane) {
+  const int p = p0 + 16 * lane, col = p >> c.page_shift;
+  int page = -1;
+  if (p <= hi && (p | (box - 1)) >= lo && col < b.max_pages) page = b.pages[(int64_t)s * b.max_pages + col];
+  return page < 0 || page >= c.n_pages ? -1 : page;
+}
 
 // The CTA whose stretch holds line offset x: the last i with floor(total i / ctas) <= x.
 __device__ __forceinline__ int cta_of(long long x, const LineStart& ls) {

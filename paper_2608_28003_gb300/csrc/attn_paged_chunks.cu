@@ -1,17 +1,21 @@
-// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 128 rows (tokens times
-// the query heads of a group, one row per TMEM lane).
+// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows (head dims 64 and
+// 128) or 128 rows (256), tokens times the query heads of a group, in tiles of 128 rows with one row per TMEM lane.
 //
 // One CTA per SM walks its stretch of the line of key tiles (attn_paged.cuh), 128 keys at a time:
-//  * warp 4 copies by TMA: an item's queries, and K and V tiles page by page;
-//  * warp 5 allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) into one of two 128-column slots, and
-//    O += P V (128 x dim x 128).  V lies as the cache has it, keys by dims, so it is the product's MN-major operand and needs
-//    no transposition.  S of the next tile is issued before P of this one is awaited;
-//  * warps 0-3: thread = row.  It reads its 128 scores, masks them, p = 2^(s c - m) with c = scale log2 e, adds the rounded
-//    weights and writes them into the swizzled tile that the second product reads.  m moves when the maximum grew by more than
-//    2^8 only: O is then rescaled in tensor memory.
-// At head dim 256 one K and one V tile fill shared memory beside the queries and P, so tiles are copied and handed
-// back in quarters (K by 64 dims, V by 32 keys): the copies of the next tile follow the products through this one.  At
-// head dims 128 and 64 two and four tiles fit.
+//  * the load warp copies by TMA: an item's queries, and K and V tiles page by page;
+//  * the issue warp allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) for each row tile, and O += P V
+//    (128 x dim x 128), P read from tensor memory.  V lies as the cache has it, keys by dims, so it is the product's
+//    MN-major operand and needs no transposition;
+//  * four softmax warps for each row tile, thread = row: they take the row's maximum over the scores, then p = 2^(s c - m) with
+//    c = scale log2 e in chunks of 32 scores, and write P over the scores they have read, where the second product finds it.  m
+//    moves when the maximum grew by more than 2^8 only: O is then rescaled in tensor memory.
+// Tensor memory holds 512 columns: two slots of 128 for S and P, and O of 2 x 64, 2 x 128 or 256.  With two row tiles each has
+// a slot of its own, and the tensor cores work for one while the other's softmax runs; a K and a V tile read from L2
+// serve 256 rows (with 128, L2 bounded the kernel).  At head dim 256 the slots alternate: S of the next key tile is
+// issued before P of this one is awaited; one K and one V tile fill shared memory beside the queries, so tiles are copied and
+// handed back in quarters (K by 64 dims, V by 32 keys), and the copies of the next tile follow the products through this one.
+// The products of one thread run in the order of their issue, which is what frees a slot: S of a slot is issued after
+// the product that read the slot's P.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
 #include "attn_paged.cuh"
 #include "ops.cuh"
@@ -26,21 +30,25 @@ namespace {
 
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
-constexpr int kLoadWarp = 4, kIssueWarp = 5, kThreads = 192;
-constexpr uint32_t kOCol = 256;  // tensor memory: two S slots of 128 columns, then O
+constexpr int kLeast = 2;        // key tiles of a stretch, at least
 
 template <int kDim>
 struct Cfg {
+  static constexpr int kRt = kDim == 256 ? 1 : 2;  // row tiles of an item
   static constexpr int kChunks = kDim / 64;
   static constexpr int kStages = kDim == 256 ? 1 : kDim == 128 ? 2 : 4;
   static constexpr int kTile = kChunks * kSub;
-  static constexpr int kOffK = kTile, kOffV = kOffK + kStages * kTile, kOffP = kOffV + kStages * kTile;
-  static constexpr int kSmem = kOffP + 2 * kSub + 1024;
-  static constexpr int kKParts = kChunks, kVParts = 4;  // a K tile comes by 64 dims, a V tile by 32 keys
-  static constexpr int kPart = kBq * kDim + 2 * kBq;    // floats of a partial: [dim / 4][128 rows][4], m, l
+  static constexpr int kOffK = kRt * kTile, kOffV = kOffK + kStages * kTile;
+  static constexpr int kSmem = kOffV + kStages * kTile + 1024;
+  static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys, or whole
+  static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
+  static constexpr int kSoft = 4 * kRt, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kThreads = 32 * (kSoft + 2);
+  static constexpr int kRows = kBq * kRt;
+  static constexpr int kPart = kRows * kDim + 2 * kRows;  // floats of a partial: [dim / 4][rows][4], m, l
+  static constexpr uint32_t kOCol = 256;                  // O of row tile r: kOCol + r kDim
   // barriers
-  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, S_FREE = 4, P_FULL = 6, PV_DONE = 7, O_FREE = 8, ALL_DONE = 9,
-                       K_FULL = 10, K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
+  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 6, O_FREE = 8, ALL_DONE = 10, K_FULL = 11,
+                       K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
                        V_FREE = V_FULL + kStages * kVParts, kBars = V_FREE + kStages * kVParts;
 };
 
@@ -52,6 +60,14 @@ __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, uint32_t lead) {
 }
 constexpr uint32_t kIdescBMnMajor = 1u << 16;
 
+// A from tensor memory (two 16-bit elements a column)
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
@@ -62,13 +78,24 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15};\n" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
 template <bool kBf16, int kDim>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     attn_chunks_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                        const __grid_constant__ CUtensorMap tmV, PagedCache c, PagedBatch b, AttnCall a, int tt,
                        float* __restrict__ part, unsigned int* __restrict__ counters, unsigned int* __restrict__ err) {
   using C = Cfg<kDim>;
+  constexpr int kRt = C::kRt, kThreads = C::kThreads, kLoadWarp = C::kLoadWarp, kIssueWarp = C::kIssueWarp;
+  constexpr uint32_t kOCol = C::kOCol;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ uint64_t bars[C::kBars];
   __shared__ LineStart ls;
@@ -79,11 +106,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = a.n_q / c.n_kv;
+  const int group = a.n_q / c.n_kv, item_tt = kRt * tt;  // tokens of a row tile, of an item
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i)
-      mbar_init(bar(i), i == C::S_FREE || i == C::S_FREE + 1 || i == C::P_FULL || i == C::O_FREE ? kBq : 1);
+      mbar_init(bar(i), i == C::P_FULL || i == C::P_FULL + 1 || i == C::O_FREE || i == C::O_FREE + 1 ? kBq : 1);
     fence_mbar_init();
     prefetch_tmap(&tmQ);
     prefetch_tmap(&tmK);
@@ -95,24 +122,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   tc_fence_before();
-  pdl_wait();
-  pdl_trigger();
-  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, tt, kBkShift, &ls, scan);  // syncs the block
+  __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
+  pdl_wait();
+  pdl_trigger();
+  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, kLeast, &ls, scan);  // syncs the block
   bool ok = true;
 
   if (ls.begin < ls.end) {
     Walk w;
-    w.start(ls, b, c.page_shift, a.window, tt, kBkShift, lane);
+    w.start(ls, b, c.page_shift, a.window, item_tt, kBkShift, lane);
     int g = 0, item = 0;  // tiles and items of this CTA so far
     if (warp == kLoadWarp) {
       // ---------------------------------------------------------------------- TMA copies
       const int box = min(kBoxSlots, 1 << c.page_shift);
-      const uint32_t q_bytes = (uint32_t)(group * tt * 128 * C::kChunks);
-      int nk = 0, nv = 0;  // tiles whose copies have been issued
-      for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, tt, kBkShift), ++item) {
-        const int lo = w.lo(a.window, tt), hi = w.hi(tt);
+      const uint32_t q_bytes = (uint32_t)(kRt * group * tt * 128 * C::kChunks);
+      int nk = 0, nv = 0;  // parts whose copies have been issued
+      for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
+        const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
+        constexpr int kGroups = kBk / 16, kBatch = 32 / kGroups;  // tiles whose pages are read at once, ahead of their use
+        int page = group_page(b, c, w.s, (w.first + w.k0) << kBkShift, lo, hi, box, lane), ahead = -1;
         if (item > 0 && !mbar_wait_warp(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) {
           ok = false;
           break;
@@ -120,54 +150,46 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (elect_one()) {
           mbar_arrive_expect_tx(bar(C::Q_FULL), q_bytes);
 #pragma unroll
-          for (int ch = 0; ch < C::kChunks; ++ch)
-            tma_load_3d(base + (uint32_t)(ch * kSub), &tmQ, 64 * ch, w.h * group, w.q.row0 + w.t * tt, bar(C::Q_FULL));
+          for (int rt = 0; rt < kRt; ++rt)
+#pragma unroll
+            for (int ch = 0; ch < C::kChunks; ++ch)
+              tma_load_3d(base + (uint32_t)(rt * C::kTile + ch * kSub), &tmQ, 64 * ch, w.h * group,
+                          w.q.row0 + w.t * item_tt + rt * tt, bar(C::Q_FULL));
         }
         __syncwarp();
         for (int i = 0; ok && i < w.cnt; ++i, ++g) {
-          const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << kBkShift;
-          int page = -1;
-          if (lane < kBk / 16) {
-            const int p = tile0 + 16 * lane, col = p >> c.page_shift;
-            if (p <= hi && (p | (box - 1)) >= lo && col < b.max_pages) page = b.pages[(int64_t)w.s * b.max_pages + col];
-            if (page < 0 || page >= c.n_pages) page = -1;
+          const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << kBkShift, in_batch = i % kBatch;
+          if (in_batch == 0) {
+            if (i > 0) page = ahead;
+            if (i + kBatch < w.cnt) ahead = group_page(b, c, w.s, tile0 + (kBatch << kBkShift), lo, hi, box, lane);
           }
-          const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
-          // K by 64 dims, V by 32 keys: 128 / box boxes a column of K, 32 / box a column of a part of V
+          const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (in_batch * kGroups)) & ((1u << kGroups) - 1u);
           const uint32_t ph = (uint32_t)(g / C::kStages - 1) & 1u;
-          const int kbox = kBk / box;
-          for (int ch = 0; ch < C::kKParts; ++ch) {
-            const int bi = st * C::kKParts + ch;
-            if (g >= C::kStages && !mbar_wait_warp(bar(C::K_FREE + bi), ph, kWaitBudgetCycles)) {
-              ok = false;
-              break;
+          const int kbox = kBk / box, vbox = C::kVKeys / box;  // boxes of a part in a column
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {  // K, then V
+            const int full = kv ? C::V_FULL : C::K_FULL, free = kv ? C::V_FREE : C::K_FREE;
+            for (int pt = 0; ok && pt < C::kKParts; ++pt) {
+              const int bi = st * C::kKParts + pt;
+              if (g >= C::kStages && !mbar_wait_warp(bar(free + bi), ph, kWaitBudgetCycles)) {
+                ok = false;
+                break;
+              }
+              if (lane == 0) {
+                if (kv == 0 && pt == 0) held[g & 7] = there;
+                mbar_arrive_expect_tx(bar(full + bi), (uint32_t)(C::kTile / C::kKParts));
+              }
+              __syncwarp();
+              // lane = (column, box)
+              const int n_box = kv ? vbox : kbox;
+              const int bx = (kv ? pt * vbox : 0) + lane % n_box, ch = (kv ? 0 : pt * C::kKCols) + lane / n_box;
+              const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + bx * (box / 16)) & 31);
+              if (lane < n_box * (kv ? C::kChunks : C::kKCols))
+                tma_load_4d(base + (uint32_t)((kv ? C::kOffV : C::kOffK) + st * C::kTile + ch * kSub + bx * box * 128),
+                            kv ? &tmV : &tmK, 64 * ch, (tile0 + bx * box) & ((1 << c.page_shift) - 1), w.h,
+                            pg < 0 ? c.n_pages : pg, bar(full + bi));
+              (kv ? nv : nk) = g * C::kKParts + pt + 1;
             }
-            if (lane == 0) {
-              if (ch == 0) held[g & 7] = there;
-              mbar_arrive_expect_tx(bar(C::K_FULL + bi), kSub);
-            }
-            __syncwarp();
-            const int pg = __shfl_sync(0xffffffffu, page, lane * (box / 16) & 31);
-            if (lane < kbox)
-              tma_load_4d(base + (uint32_t)(C::kOffK + st * C::kTile + ch * kSub + lane * box * 128), &tmK, 64 * ch,
-                          (tile0 + lane * box) & ((1 << c.page_shift) - 1), w.h, pg < 0 ? c.n_pages : pg, bar(C::K_FULL + bi));
-            nk = g * C::kKParts + ch + 1;
-          }
-          const int vbox = 32 / box, v_ops = C::kChunks * vbox;
-          for (int vp = 0; ok && vp < C::kVParts; ++vp) {
-            const int bi = st * C::kVParts + vp;
-            if (g >= C::kStages && !mbar_wait_warp(bar(C::V_FREE + bi), ph, kWaitBudgetCycles)) {
-              ok = false;
-              break;
-            }
-            if (lane == 0) mbar_arrive_expect_tx(bar(C::V_FULL + bi), (uint32_t)(C::kChunks * 32 * 128));
-            __syncwarp();
-            const int bx = vp * vbox + lane % vbox, ch = lane / vbox;  // box of the tile, column
-            const int pg = __shfl_sync(0xffffffffu, page, bx * (box / 16) & 31);
-            if (lane < v_ops)
-              tma_load_4d(base + (uint32_t)(C::kOffV + st * C::kTile + ch * kSub + bx * box * 128), &tmV, 64 * ch,
-                          (tile0 + bx * box) & ((1 << c.page_shift) - 1), w.h, pg < 0 ? c.n_pages : pg, bar(C::V_FULL + bi));
-            nv = g * C::kVParts + vp + 1;
           }
         }
       }
@@ -185,64 +207,71 @@ __global__ void __launch_bounds__(kThreads, 1)
       // ---------------------------------------------------------------------- MMAs
       constexpr uint32_t fmt = kBf16 ? 1u : 0u;
       constexpr uint32_t idesc_s = idesc_f16(fmt, kBk, kBq), idesc_o = idesc_f16(fmt, kDim, kBq) | kIdescBMnMajor;
-      const uint64_t dq = sdesc_swz(base), dp = sdesc_swz(base + C::kOffP);
-      // S of tile i (this CTA's count) of an item whose last tile is `last`
-      auto issue_s = [&](int i, bool last) {
-        const int st = i % C::kStages;
-        const uint32_t ph = (uint32_t)(i / C::kStages) & 1u;
-        if (i >= 2 && !mbar_wait_warp(bar(C::S_FREE + (i & 1)), (uint32_t)((i >> 1) - 1) & 1u, kWaitBudgetCycles)) return false;
+      const uint64_t dq = sdesc_swz(base);
+      // S of key tile i (this CTA's count) for row tile rt, into its slot; hands K back after the last row tile, Q after `last`
+      auto issue_s = [&](int i, int rt, bool last) {
+        const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
         const uint64_t dk = sdesc_swz(base + (uint32_t)(C::kOffK + st * C::kTile));
-        for (int ch = 0; ch < C::kChunks; ++ch) {
-          if (!mbar_wait_warp(bar(C::K_FULL + st * C::kKParts + ch), ph, kWaitBudgetCycles)) return false;
+#pragma unroll 1
+        for (int pt = 0; pt < C::kKParts; ++pt) {
+          if (rt == 0 &&
+              !mbar_wait_warp(bar(C::K_FULL + st * C::kKParts + pt), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+            return false;
           tc_fence_after();
           if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t at = (uint32_t)(ch * (kSub >> 4) + 2 * k);
-              tc_mma(tmem + 128u * (uint32_t)(i & 1), dq + at, dk + at, idesc_s, ch > 0 || k > 0);
+            for (int k = 0; k < 4 * C::kKCols; ++k) {
+              const uint32_t at = (uint32_t)((pt * C::kKCols + (k >> 2)) * (kSub >> 4) + 2 * (k & 3));
+              tc_mma(tmem + 128u * (uint32_t)slot, dq + (uint32_t)(rt * (C::kTile >> 4)) + at, dk + at, idesc_s, pt > 0 || k > 0);
             }
-            tc_commit(bar(C::K_FREE + st * C::kKParts + ch));
+            if (rt == kRt - 1) tc_commit(bar(C::K_FREE + st * C::kKParts + pt));
           }
           __syncwarp();
         }
         if (elect_one()) {
-          tc_commit(bar(C::S_FULL + (i & 1)));
-          if (last) tc_commit(bar(C::Q_FREE));
+          tc_commit(bar(C::S_FULL + slot));
+          if (last && rt == kRt - 1) tc_commit(bar(C::Q_FREE));
         }
         __syncwarp();
         return true;
       };
-      for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, tt, kBkShift), ++item) {
-        ok = mbar_wait_warp(bar(C::Q_FULL), (uint32_t)item & 1u, kWaitBudgetCycles) && issue_s(g, w.cnt == 1);
-        for (int i = 0; ok && i < w.cnt; ++i, ++g) {
-          if (i + 1 < w.cnt && !issue_s(g + 1, i + 2 == w.cnt)) {
-            ok = false;
-            break;
-          }
-          if (!mbar_wait_warp(bar(C::P_FULL), (uint32_t)g & 1u, kWaitBudgetCycles) ||
-              (i == 0 && item > 0 && !mbar_wait_warp(bar(C::O_FREE), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles))) {
-            ok = false;
-            break;
-          }
-          const int st = g % C::kStages;
-          const uint64_t dv = sdesc_mn(base + (uint32_t)(C::kOffV + st * C::kTile), kSub);
-          for (int vp = 0; vp < C::kVParts; ++vp) {  // O += P V, 32 keys at a time
-            if (!mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(g / C::kStages) & 1u, kWaitBudgetCycles)) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
-            if (elect_one()) {
+      // O += P V of key tile i for row tile rt; hands V back after the last row tile
+      auto issue_pv = [&](int i, int rt, bool first) {
+        const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
+        if (!mbar_wait_warp(bar(C::P_FULL + rt), (uint32_t)i & 1u, kWaitBudgetCycles) ||
+            (first && item > 0 && !mbar_wait_warp(bar(C::O_FREE + rt), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)))
+          return false;
+        const uint64_t dv = sdesc_mn(base + (uint32_t)(C::kOffV + st * C::kTile), kSub);
+        const uint32_t p = tmem + 128u * (uint32_t)slot, o = tmem + kOCol + (uint32_t)(rt * kDim);
+#pragma unroll 1
+        for (int vp = 0; vp < C::kVParts; ++vp) {
+          if (rt == 0 && !mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+            return false;
+          tc_fence_after();
+          if (elect_one()) {
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int kk = 2 * vp + k;  // 16 keys
-                tc_mma(tmem + kOCol, dp + (uint32_t)((kk >> 2) * (kSub >> 4) + 2 * (kk & 3)), dv + (uint32_t)(kk * (16 * 128 >> 4)),
-                       idesc_o, i > 0 || kk > 0);
-              }
-              tc_commit(bar(C::V_FREE + st * C::kVParts + vp));
-              if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE));
+            for (int k = 0; k < C::kVKeys / 16; ++k) {
+              const int kk = vp * (C::kVKeys / 16) + k;  // 16 keys: 8 columns of P
+              tc_mma_ts(o, p + 8u * (uint32_t)kk, dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
             }
-            __syncwarp();
+            if (rt == kRt - 1) tc_commit(bar(C::V_FREE + st * C::kVParts + vp));
+            if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE + rt));
+          }
+          __syncwarp();
+        }
+        return true;
+      };
+      for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
+        ok = mbar_wait_warp(bar(C::Q_FULL), (uint32_t)item & 1u, kWaitBudgetCycles);
+#pragma unroll
+        for (int rt = 0; rt < kRt; ++rt) ok = ok && issue_s(g, rt, w.cnt == 1);
+        for (int i = 0; ok && i < w.cnt; ++i, ++g) {
+          const bool more = i + 1 < w.cnt, last = i + 2 == w.cnt;
+          if constexpr (kRt == 1) {
+            ok = (!more || issue_s(g + 1, 0, last)) && issue_pv(g, 0, i == 0);
+          } else {  // a slot's next S follows the product that has read its P
+            ok = issue_pv(g, 0, i == 0) && (!more || issue_s(g + 1, 0, last)) && issue_pv(g, 1, i == 0) &&
+                 (!more || issue_s(g + 1, 1, last));
           }
         }
       }
@@ -254,100 +283,96 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
     } else {
       // ---------------------------------------------------------------------- softmax, one row per thread
-      const int r = threadIdx.x;
-      const uint32_t lanes = tmem + ((uint32_t)(32 * warp) << 16);
-      const uint32_t prow = base + C::kOffP + (uint32_t)(r * 128);
+      const int rt = kRt == 2 ? warp >> 2 : 0, r = threadIdx.x & (kBq - 1);  // row tile, row of it
+      const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
+      const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim);
       const float sc = a.scale * kLog2e;
-      for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, tt, kBkShift), ++item) {
-        const int tok0 = w.t * tt, rows = min(w.q.rows - tok0, tt) * group;
-        const int lo = w.lo(a.window, tt), hi = w.hi(tt);
-        const bool live = r < rows, busy = 32 * warp < rows;  // this row's, and any of the warp's
+      for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
+        const int tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
+        const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
+        const bool live = r < rows, busy = 32 * (warp & 3) < rows;  // this row's, and any of the warp's
         const int tok = tok0 + (live ? r / group : 0), head = w.h * group + (live ? r % group : 0);
         const int pos = w.q.pos0 + tok, from = a.window > 0 ? max(0, pos - a.window + 1) : 0;
         float m = -INFINITY, l = 0.0f;
         for (int i = 0; i < w.cnt; ++i, ++g) {
-          const int j0 = (w.first + w.k0 + i) << kBkShift;
-          if (ok && !mbar_wait_warp(bar(C::S_FULL + (g & 1)), (uint32_t)(g >> 1) & 1u, kWaitBudgetCycles)) ok = false;
+          const int j0 = (w.first + w.k0 + i) << kBkShift, slot = kRt == 2 ? rt : g & 1;
+          const uint32_t stm = lanes + 128u * (uint32_t)slot;
+          if (ok && !mbar_wait_warp(bar(C::S_FULL + slot), (uint32_t)(kRt == 2 ? g : g >> 1) & 1u, kWaitBudgetCycles)) ok = false;
           if (!ok) continue;
           tc_fence_after();
-          uint32_t pk[kBk / 2];
-          bool grown = false;
-          float up = 1.0f;
           if (busy) {
-            float v[kBk];
+            const uint32_t there = held[g & 7];
+            const bool cut = j0 < from || j0 + kBk - 1 > pos || there != 0xffu;  // some key is not this row's
+            // the scores of 32 keys that are not this row's become -inf
+            auto mask = [&](int q4, uint32_t (&x)[32]) {
+              const int f = from - j0 - 32 * q4, t = pos - j0 - 32 * q4;  // keys f .. t of the 32
+              uint32_t keep = t < 0 || f > 31 ? 0u : 0xffffffffu;
+              if (f > 0 && f <= 31) keep &= 0xffffffffu << f;
+              if (t >= 0 && t < 31) keep &= (2u << t) - 1u;
+              if (!((there >> (2 * q4)) & 1u)) keep &= 0xffff0000u;
+              if (!((there >> (2 * q4 + 1)) & 1u)) keep &= 0x0000ffffu;
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (!((keep >> k) & 1u)) x[k] = 0xff800000u;
+            };
+            uint32_t x[32];
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
-              uint32_t x[32];
-              tmem_ld32(lanes + 128u * (uint32_t)(g & 1) + 32 * q4, x);
+              tmem_ld32(stm + 32 * q4, x);
+              if (cut) mask(q4, x);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) v[32 * q4 + k] = __uint_as_float(x[k]);
+              for (int k = 0; k < 32; k += 2)
+                mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(x[k])), __uint_as_float(x[k + 1]));
             }
-            tc_fence_before();
-            mbar_arrive(bar(C::S_FREE + (g & 1)));
-            const uint32_t there = held[g & 7];
-            if (j0 < from || j0 + kBk - 1 > pos) {
-#pragma unroll
-              for (int k = 0; k < kBk; ++k)
-                if (j0 + k < from || j0 + k > pos) v[k] = -INFINITY;
-            }
-            if (there != 0xffu) {  // groups of 16 keys in no page
-#pragma unroll
-              for (int k = 0; k < kBk; ++k)
-                if (!((there >> (k >> 4)) & 1u)) v[k] = -INFINITY;
-            }
-            float mx[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) mx[k] = v[k];
-#pragma unroll
-            for (int k = 8; k < kBk; ++k) mx[k & 7] = fmaxf(mx[k & 7], v[k]);
-            const float top = sc * fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])),
-                                         fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
-            grown = top > m + kGrowth;  // m = -inf: any visible key
+            const float top = sc * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            const bool grown = top > m + kGrowth;  // m = -inf: any visible key
+            float up = 1.0f;
             if (grown) {
               up = m == -INFINITY ? 0.0f : ex2(m - top);
               m = top;
               l *= up;
             }
             const float ref = m == -INFINITY ? 0.0f : m;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const f32x2 sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
+            f32x2 sum[2] = {0ull, 0ull};
 #pragma unroll
-            for (int k = 0; k < kBk; k += 2) {
-              pk[k >> 1] = pack2<kBf16>(ex2(fmaf(v[k], sc, -ref)), ex2(fmaf(v[k + 1], sc, -ref)));
-              const float2 as_used = unpack2<kBf16>(pk[k >> 1]);
-              sum[(k >> 1) & 3] += as_used.x + as_used.y;
+            for (int q4 = 0; q4 < 4; ++q4) {
+              tmem_ld32(stm + 32 * q4, x);
+              if (cut) mask(q4, x);
+              uint32_t pk[16];
+#pragma unroll
+              for (int k = 0; k < 32; k += 2) {
+                float e0, e1;
+                f2_unpack(f2_fma(f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, ref2), e0, e1);
+                e0 = ex2(e0);
+                e1 = ex2(e1);
+                sum[(k >> 1) & 1] = f2_add(sum[(k >> 1) & 1], f2_pack(e0, e1));
+                pk[k >> 1] = pack2<kBf16>(e0, e1);
+              }
+              tmem_st16(stm + 16 * q4, pk);  // over scores that have been read
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          } else {
-            tc_fence_before();
-            mbar_arrive(bar(C::S_FREE + (g & 1)));
-          }
-          // the P tile and O are free once the previous tile's product has completed
-          if (g > 0 && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) {
-            ok = false;
-            continue;
-          }
-          if (i > 0 && __any_sync(0xffffffffu, grown)) {
-            tc_fence_after();
+            float s0, s1;
+            f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
+            l += s0 + s1;
+            if (i > 0 && __any_sync(0xffffffffu, grown)) {
+              // O is the previous products' (with two row tiles their order ahead of this S says so already)
+              if (kRt == 1 && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) {
+                ok = false;
+                continue;
+              }
+              tc_fence_after();
 #pragma unroll 1
-            for (int ch = 0; ch < kDim / 32; ++ch) {
-              uint32_t x[32];
-              tmem_ld32(lanes + kOCol + 32 * ch, x);
+              for (int ch = 0; ch < kDim / 32; ++ch) {
+                tmem_ld32(otm + 32 * ch, x);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * up);
-              tmem_st32(lanes + kOCol + 32 * ch, x);
+                for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * up);
+                tmem_st32(otm + 32 * ch, x);
+              }
             }
-            asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
-            tc_fence_before();
+            tmem_wait_st();
           }
-          if (busy) {
-#pragma unroll
-            for (int k = 0; k < kBk / 8; ++k)
-              asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(prow + (uint32_t)((k >> 3) * kSub) +
-                                                                              (uint32_t)(((k & 7) ^ (r & 7)) << 4)),
-                           "r"(pk[4 * k]), "r"(pk[4 * k + 1]), "r"(pk[4 * k + 2]), "r"(pk[4 * k + 3])
-                           : "memory");
-          }
-          if (j0 < lo || j0 + kBk - 1 > hi) {
+          if (rt == 0 && (j0 < lo || j0 + kBk - 1 > hi)) {
             // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero: row r
             // of the tile, once its copies have landed
             const int st = g % C::kStages;
@@ -370,11 +395,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                                "r"(0u)
                                : "memory");
             }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
           }
-          asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-          mbar_arrive(bar(C::P_FULL));
+          tc_fence_before();
+          mbar_arrive(bar(C::P_FULL + rt));
         }
-        if (ok && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) ok = false;
+        // the last product; with one row tile the one before it may not be known to be complete, and a wait tells only the
+        // current phase from the one before
+        if (kRt == 1 && ok && w.cnt > 1 && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 2) & 1u, kWaitBudgetCycles)) ok = false;
+        if (ok && !mbar_wait_warp(bar(C::PV_DONE + rt), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) ok = false;
         if (!ok && lane == 0) atomicOr(err, DEVERR_CONSUMER_WAIT);
         __syncwarp();
         tc_fence_after();
@@ -412,60 +441,63 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int ch = 0; ch < kDim / 32; ++ch) {
               uint32_t x[32];
               float f[32];
-              tmem_ld32(lanes + kOCol + 32 * ch, x);
+              tmem_ld32(otm + 32 * ch, x);
 #pragma unroll
               for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(x[k]);
               store(ch, f, inv, nan);
             }
             tc_fence_before();
-            mbar_arrive(bar(C::O_FREE));
+            mbar_arrive(bar(C::O_FREE + rt));
             exactly(nan != 0.0f || !(l > 0.0f));
           } else {
             tc_fence_before();
-            mbar_arrive(bar(C::O_FREE));
+            mbar_arrive(bar(C::O_FREE + rt));
           }
           continue;
         }
         // ---- a piece: into the workspace, joined by the last one to arrive
         const Pieces ps = pieces_of(w, ls);
+        const int pr = rt * kBq + r;  // row of the partial
         float* mine = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
         if (busy) {
 #pragma unroll 1
           for (int ch = 0; ch < kDim / 32; ++ch) {
             uint32_t x[32];
-            tmem_ld32(lanes + kOCol + 32 * ch, x);
+            tmem_ld32(otm + 32 * ch, x);
             if (live) {
 #pragma unroll
               for (int k = 0; k < 8; ++k)
-                __stcg(reinterpret_cast<float4*>(mine) + (size_t)(8 * ch + k) * kBq + r,
+                __stcg(reinterpret_cast<float4*>(mine) + (size_t)(8 * ch + k) * C::kRows + pr,
                        make_float4(__uint_as_float(x[4 * k]), __uint_as_float(x[4 * k + 1]), __uint_as_float(x[4 * k + 2]),
                                    __uint_as_float(x[4 * k + 3])));
             }
           }
           if (live) {
-            __stcg(mine + kBq * kDim + r, m);
-            __stcg(mine + kBq * kDim + kBq + r, l);
+            __stcg(mine + C::kRows * kDim + pr, m);
+            __stcg(mine + C::kRows * kDim + C::kRows + pr, l);
           }
         }
         tc_fence_before();
-        mbar_arrive(bar(C::O_FREE));
-        __threadfence();
-        named_bar_sync(1, kBq);
-        if (r == 0) {
+        mbar_arrive(bar(C::O_FREE + rt));
+        named_bar_sync(1, C::kRows);
+        if (threadIdx.x == 0) {
+          __threadfence();  // the block's partials, ordered before this thread by the barrier, ahead of the count
           const unsigned int before = atomicAdd(counters + ps.first, 1u);
           s_last = before + 1 == (unsigned int)ps.count;
           if (s_last) counters[ps.first] = 0;
           __threadfence();
         }
-        named_bar_sync(1, kBq);
+        named_bar_sync(1, C::kRows);
         if (s_last && busy) {
           auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
           float M = -INFINITY, L = 0.0f, nan = 0.0f;
           if (live) {
-            for (int i = 0; i < ps.count; ++i) M = fmaxf(M, __ldcg(slot(i) + kBq * kDim + r));
+#pragma unroll 4
+            for (int i = 0; i < ps.count; ++i) M = fmaxf(M, __ldcg(slot(i) + C::kRows * kDim + pr));
+#pragma unroll 4
             for (int i = 0; i < ps.count; ++i) {
-              const float mi = __ldcg(slot(i) + kBq * kDim + r);
-              L = fmaf(__ldcg(slot(i) + kBq * kDim + kBq + r), mi == -INFINITY ? 0.0f : ex2(mi - M), L);
+              const float mi = __ldcg(slot(i) + C::kRows * kDim + pr);
+              L = fmaf(__ldcg(slot(i) + C::kRows * kDim + C::kRows + pr), mi == -INFINITY ? 0.0f : ex2(mi - M), L);
             }
           }
           const float inv = 1.0f / L;
@@ -475,17 +507,20 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int k = 0; k < 32; ++k) f[k] = 0.0f;
             if (live) {
-#pragma unroll 1
+#pragma unroll 2
               for (int i = 0; i < ps.count; ++i) {
-                const float mi = __ldcg(slot(i) + kBq * kDim + r), e = mi == -INFINITY ? 0.0f : ex2(mi - M);
-                const float4* src = reinterpret_cast<const float4*>(slot(i)) + (size_t)(8 * ch) * kBq + r;
+                const float mi = __ldcg(slot(i) + C::kRows * kDim + pr);
+                const float4* src = reinterpret_cast<const float4*>(slot(i)) + (size_t)(8 * ch) * C::kRows + pr;
+                float4 x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = __ldcg(src + k * C::kRows);
+                const float e = mi == -INFINITY ? 0.0f : ex2(mi - M);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                  const float4 x = __ldcg(src + k * kBq);
-                  f[4 * k] = fmaf(x.x, e, f[4 * k]);
-                  f[4 * k + 1] = fmaf(x.y, e, f[4 * k + 1]);
-                  f[4 * k + 2] = fmaf(x.z, e, f[4 * k + 2]);
-                  f[4 * k + 3] = fmaf(x.w, e, f[4 * k + 3]);
+                  f[4 * k] = fmaf(x[k].x, e, f[4 * k]);
+                  f[4 * k + 1] = fmaf(x[k].y, e, f[4 * k + 1]);
+                  f[4 * k + 2] = fmaf(x[k].z, e, f[4 * k + 2]);
+                  f[4 * k + 3] = fmaf(x[k].w, e, f[4 * k + 3]);
                 }
               }
             }
@@ -493,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           exactly(nan != 0.0f || !(L > 0.0f));
         }
-        named_bar_sync(1, kBq);  // s_last is free again
+        named_bar_sync(1, C::kRows);  // s_last is free again
       }
     }
   }
@@ -523,7 +558,7 @@ w8a8_status launch(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a
   W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
   W8A8_TRY(make_kv_maps(pc, kDim, &tk, &tv));
   char* base = static_cast<char*>(ws);
-  W8A8_CUDA(launch_pdl(attn_chunks_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(kThreads), (size_t)C::kSmem, st, tq, tk, tv,
+  W8A8_CUDA(launch_pdl(attn_chunks_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
                        pc, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
                        reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
   return W8A8_OK;
@@ -531,7 +566,10 @@ w8a8_status launch(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a
 
 }  // namespace
 
-size_t attn_chunks_ws(int dim, int sms) { return (size_t)2 * sms * (kBq * dim + 2 * kBq) * sizeof(float); }
+size_t attn_chunks_ws(int dim, int sms) {
+  const int part = dim == 256 ? Cfg<256>::kPart : dim == 128 ? Cfg<128>::kPart : Cfg<64>::kPart;
+  return (size_t)2 * sms * part * sizeof(float);
+}
 
 w8a8_status launch_attn_chunks(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                cudaStream_t st) {

@@ -26,10 +26,11 @@ struct Cfg {
   static constexpr int kChunks = kDim / 64;                   // 128-byte columns of a tile
   static constexpr int kSub = kBk * 128, kTile = kChunks * kSub, kStage = 2 * kTile;
   static constexpr int kStages = 196608 / kStage;             // 3, 3, 6
-  static constexpr int kJoin = kWarps / 2 * kRows * kDim * 4; // outputs of half of the warps
+  static constexpr int kJoin = kWarps * 8 * kDim * 4;         // 8 rows' outputs of every warp
+  static constexpr int kPer = kDim / 8 / kWarps;              // groups of 8 dims that a warp joins
   static constexpr int kSmem = kStages * kStage + kJoin + 1024;
   static constexpr int kThreads = 32 * (kWarps + 1);
-  // a partial: [8 dims of 4 lanes.. as fragments: dim / 8][32 lanes][4] outputs, then m and l of the 16 rows
+  // floats of a partial: [row half][dim / 8][32 lanes][2] outputs, then m and l of the 16 rows
   static constexpr int kPart = kRows * kDim + 2 * kRows;
 };
 
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   __shared__ float s_m[C::kWarps][kRows], s_l[C::kWarps][kRows];
   __shared__ uint32_t s_last, s_bad;
   const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
-  float4* join = reinterpret_cast<float4*>(smem_raw + (ring - raw) + C::kStages * C::kStage);
+  float2* join = reinterpret_cast<float2*>(smem_raw + (ring - raw) + C::kStages * C::kStage);
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   auto empty = [&](int i) { return bar0 + 8u * (uint32_t)(C::kStages + i); };
@@ -84,7 +85,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
   pdl_wait();
   pdl_trigger();
-  find_start<C::kThreads>(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift, &ls, scan);
+  find_start<C::kThreads>(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift, 1, &ls, scan);
   if (ls.begin >= ls.end) return;
   Walk w;
   w.start(ls, b, c.page_shift, a.window, tt, C::kBkShift, lane);
@@ -97,16 +98,15 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     const int n_ops = 2 * C::kChunks * boxes;
     for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift)) {
       const int lo = w.lo(a.window, tt), hi = w.hi(tt);
+      constexpr int kGroups = C::kBk / 16, kBatch = 32 / kGroups;  // tiles whose pages are read at once, ahead of their use
+      int page = group_page(b, c, w.s, (w.first + w.k0) << C::kBkShift, lo, hi, box, lane), ahead = -1;
       for (int i = 0; i < w.cnt; ++i, ++g) {
-        const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << C::kBkShift;
-        // the pages of the tile's 16-key groups (all boxes begin at multiples of 16)
-        int page = -1;
-        if (lane < C::kBk / 16) {
-          const int p = tile0 + 16 * lane, col = p >> c.page_shift;
-          if (p <= hi && (p | (box - 1)) >= lo && col < b.max_pages) page = b.pages[(int64_t)w.s * b.max_pages + col];
-          if (page < 0 || page >= c.n_pages) page = -1;
+        const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << C::kBkShift, in_batch = i % kBatch;
+        if (in_batch == 0) {
+          if (i > 0) page = ahead;
+          if (i + kBatch < w.cnt) ahead = group_page(b, c, w.s, tile0 + (kBatch << C::kBkShift), lo, hi, box, lane);
         }
-        const uint32_t there = __ballot_sync(0xffffffffu, page >= 0);
+        const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (in_batch * kGroups)) & ((1u << kGroups) - 1u);
         if (g >= C::kStages && !mbar_wait_warp(empty(st), (uint32_t)(g / C::kStages - 1) & 1u, kWaitBudgetCycles)) {
           ok = false;
           break;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         const uint32_t dst = ring + (uint32_t)(st * C::kStage);
         for (int o0 = 0; o0 < n_ops; o0 += 32) {
           const int o = o0 + lane, bx = o % boxes, ch = o / boxes % C::kChunks, kv = o / boxes / C::kChunks;
-          const int pg = __shfl_sync(0xffffffffu, page, bx * (box / 16) & 31);
+          const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + bx * (box / 16)) & 31);
           if (o < n_ops) {
             const int slot = (tile0 + bx * box) & ((1 << c.page_shift) - 1);
             // a page that holds nothing: a coordinate outside the tensor, which fills zeros
@@ -293,81 +293,86 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         acc[d][2 * r + 1] *= f;
       }
     }
-#pragma unroll 1
-    for (int half = C::kWarps / 2; half > 0; half >>= 1) {
-      if (warp >= half && warp < 2 * half) {
-        float4* to = join + (warp - half) * (kRows * kDim / 4) + lane;
+    // each warp adds up its share of the dims over the warps, in their order, 8 rows at a time
+    constexpr int kPer = C::kPer;
+    float y[kPer][4];
 #pragma unroll
-        for (int d = 0; d < kDim / 8; ++d) to[32 * d] = make_float4(acc[d][0], acc[d][1], acc[d][2], acc[d][3]);
-      }
+    for (int r = 0; r < 2; ++r) {
+      if (r == 1 && rows <= 8) break;
+      if (r == 1) named_bar_sync(kBar, kConsumers);  // the first rows have been read
+      float2* to = join + warp * (kDim * 4) + lane;
+#pragma unroll
+      for (int d = 0; d < kDim / 8; ++d) to[32 * d] = make_float2(acc[d][2 * r], acc[d][2 * r + 1]);
       named_bar_sync(kBar, kConsumers);
-      if (warp < half) {
-        const float4* add = join + warp * (kRows * kDim / 4) + lane;
 #pragma unroll
-        for (int d = 0; d < kDim / 8; ++d) {
-          const float4 x = add[32 * d];
-          acc[d][0] += x.x;
-          acc[d][1] += x.y;
-          acc[d][2] += x.z;
-          acc[d][3] += x.w;
+      for (int d = 0; d < kPer; ++d) {
+        float2 sum = join[32 * (warp * kPer + d) + lane];
+#pragma unroll
+        for (int i = 1; i < C::kWarps; ++i) {
+          const float2 x = join[i * (kDim * 4) + 32 * (warp * kPer + d) + lane];
+          sum.x += x.x;
+          sum.y += x.y;
         }
+        y[d][2 * r] = sum.x;
+        y[d][2 * r + 1] = sum.y;
       }
-      named_bar_sync(kBar, kConsumers);
     }
 
     auto out_at = [&](int r) {
       return a.o + (int64_t)(w.q.row0 + tok0 + r / group) * a.o_row + (int64_t)(w.h * group + r % group) * a.o_head;
     };
-    auto exactly = [&](uint32_t bad) {  // rows whose result is not finite, or without weight, by one warp
-      for (; bad; bad &= bad - 1) {
-        const int r = __ffs(bad) - 1, tok = tok0 + r / group;
+    // this warp's dims of the output: y over the rows' sums; rows whose result is not finite, or without weight, are marked
+    auto put = [&](const float (&sums)[2]) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int row = r0 + 8 * r;
+        if (row >= rows) continue;
+        const float inv = 1.0f / sums[r];
+        float nan = 0.0f;
+        uint16_t* o = out_at(row) + 2 * quad + 8 * warp * kPer;
+#pragma unroll
+        for (int d = 0; d < kPer; ++d) {
+          const float x = y[d][2 * r] * inv, z = y[d][2 * r + 1] * inv;
+          nan = fmaf(x, 0.0f, fmaf(z, 0.0f, nan));
+          *reinterpret_cast<uint32_t*>(o + 8 * d) = pack2<kBf16>(x, z);
+        }
+        if (nan != 0.0f || !(sums[r] > 0.0f)) atomicOr(&s_bad, 1u << row);
+      }
+      named_bar_sync(kBar, kConsumers);
+      const uint32_t bad = s_bad;
+      if (bad == 0) return;
+      named_bar_sync(kBar, kConsumers);
+      if (threadIdx.x == 0) s_bad = 0;
+      for (int r = warp; r < rows; r += C::kWarps) {  // a warp a row, exactly
+        if (!((bad >> r) & 1u)) continue;
+        const int tok = tok0 + r / group;
         attend_row<kBf16, kDim>(c, b, a, w.s, w.q.pos0 + tok, w.q.row0 + tok, w.h * group + r % group, lane);
       }
+      named_bar_sync(kBar, kConsumers);
     };
     if (w.whole()) {
-      if (warp == 0) {
-        uint32_t bad = 0;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const int row = r0 + 8 * r;
-          const float inv = 1.0f / L[r];
-          float nan = 0.0f;
-          uint16_t* o = out_at(min(row, rows - 1)) + 2 * quad;
-#pragma unroll
-          for (int d = 0; d < kDim / 8; ++d) {
-            const float x = acc[d][2 * r] * inv, y = acc[d][2 * r + 1] * inv;
-            nan = fmaf(x, 0.0f, fmaf(y, 0.0f, nan));
-            if (row < rows) *reinterpret_cast<uint32_t*>(o + 8 * d) = pack2<kBf16>(x, y);
-          }
-          const uint32_t hit = __ballot_sync(0xffffffffu, row < rows && (nan != 0.0f || !(L[r] > 0.0f)));
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if ((hit >> (4 * i)) & 0xfu) bad |= 1u << (i + 8 * r);
-        }
-        __syncwarp();
-        if (bad) exactly(bad);
-      }
+      put(L);
       continue;
     }
     // ---- a piece: into the workspace, joined by the last one to arrive
     const Pieces ps = pieces_of(w, ls);
-    if (warp == 0) {
+    {
       float* to = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
 #pragma unroll
-      for (int d = 0; d < kDim / 8; ++d) {
-        if (r0 < rows) __stcg(reinterpret_cast<float2*>(to + (size_t)(d * 32 + lane) * 2), make_float2(acc[d][0], acc[d][1]));
-        if (r0 + 8 < rows)
-          __stcg(reinterpret_cast<float2*>(to + 8 * kDim + (size_t)(d * 32 + lane) * 2), make_float2(acc[d][2], acc[d][3]));
-      }
-      if (quad == 0)
+      for (int r = 0; r < 2; ++r) {
+        if (r0 + 8 * r >= rows) continue;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int d = 0; d < kPer; ++d)
+          __stcg(reinterpret_cast<float2*>(to + 8 * kDim * r + (size_t)((warp * kPer + d) * 32 + lane) * 2),
+                 make_float2(y[d][2 * r], y[d][2 * r + 1]));
+        if (warp == 0 && quad == 0) {
           __stcg(to + kRows * kDim + r0 + 8 * r, M[r]);
           __stcg(to + kRows * kDim + kRows + r0 + 8 * r, L[r]);
         }
-      __threadfence();
-      __syncwarp();
-      if (lane == 0) {
+      }
+      named_bar_sync(kBar, kConsumers);
+      if (threadIdx.x == 0) {
+        __threadfence();  // the block's partials, ordered before this thread by the barrier, ahead of the count
         const unsigned int before = atomicAdd(counters + ps.first, 1u);
         s_last = before + 1 == (unsigned int)ps.count;
         if (s_last) counters[ps.first] = 0;
@@ -376,15 +381,28 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     }
     named_bar_sync(kBar, kConsumers);
     if (s_last) {
-      constexpr int kPer = kDim / 8 / C::kWarps;  // this warp's groups of 8 dims
       auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
-      float Mj[2] = {-INFINITY, -INFINITY}, Lj[2] = {0.0f, 0.0f}, y[kPer][4];
+      float Mj[2] = {-INFINITY, -INFINITY}, Lj[2] = {0.0f, 0.0f};
+      // lane = piece: every row's maximum by the whole warp, all loads ahead of the first use
+      {
+        float top[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) top[r] = r < rows && lane < ps.count ? __ldcg(slot(lane) + kRows * kDim + r) : -INFINITY;
+        for (int i = lane + 32; i < ps.count; i += 32)
+#pragma unroll
+          for (int r = 0; r < kRows; ++r)
+            if (r < rows) top[r] = fmaxf(top[r], __ldcg(slot(i) + kRows * kDim + r));
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          if (r >= rows) break;
+          const float x = warp_max_f(top[r]);
+          if (r == r0) Mj[0] = x;
+          if (r == r0 + 8) Mj[1] = x;
+        }
+      }
 #pragma unroll
       for (int d = 0; d < kPer; ++d) y[d][0] = y[d][1] = y[d][2] = y[d][3] = 0.0f;
-      for (int i = 0; i < ps.count; ++i)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) Mj[r] = fmaxf(Mj[r], __ldcg(slot(i) + kRows * kDim + r0 + 8 * r));
-#pragma unroll 2
+#pragma unroll 4
       for (int i = 0; i < ps.count; ++i) {
         const float* from_piece = slot(i);
 #pragma unroll
@@ -402,27 +420,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
         }
       }
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int row = r0 + 8 * r;
-        const float inv = 1.0f / Lj[r];
-        float nan = 0.0f;
-        uint16_t* o = out_at(min(row, rows - 1)) + 2 * quad + 8 * warp * kPer;
-#pragma unroll
-        for (int d = 0; d < kPer; ++d) {
-          const float x = y[d][2 * r] * inv, z = y[d][2 * r + 1] * inv;
-          nan = fmaf(x, 0.0f, fmaf(z, 0.0f, nan));
-          if (row < rows) *reinterpret_cast<uint32_t*>(o + 8 * d) = pack2<kBf16>(x, z);
-        }
-        if (row < rows && (nan != 0.0f || !(Lj[r] > 0.0f))) atomicOr(&s_bad, 1u << row);
-      }
-      named_bar_sync(kBar, kConsumers);
-      if (warp == 0) {
-        const uint32_t bad = s_bad;
-        __syncwarp();
-        if (lane == 0) s_bad = 0;
-        if (bad) exactly(bad);
-      }
+      put(Lj);
     }
     named_bar_sync(kBar, kConsumers);  // s_last, s_bad and the statistics are free again
   }
