@@ -6,7 +6,8 @@
 //  * the issue warp allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) for each row tile, and O += P V
 //    (128 x dim x 128), P read from tensor memory.  V lies as the cache has it, keys by dims, so it is the product's
 //    MN-major operand and needs no transposition;
-//  * four softmax warps for each row tile, thread = row: they take the row's maximum over the scores, then p = 2^(s c - m) with
+//  * eight softmax warps, four for each row tile (thread = row), or two threads a row, each with half of the keys and of the
+//    dims, where there is one: they take the row's maximum over the scores, then p = 2^(s c - m) with
 //    c = scale log2 e in chunks of 32 scores, and write P over the scores they have read, where the second product finds it.  m
 //    moves when the maximum grew by more than 2^8 only: O is then rescaled in tensor memory.
 // Tensor memory holds 512 columns: two slots of 128 for S and P, and O of 2 x 64, 2 x 128 or 256.  With two row tiles each has
@@ -42,12 +43,14 @@ struct Cfg {
   static constexpr int kSmem = kOffV + kStages * kTile + 1024;
   static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys, or whole
   static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
-  static constexpr int kSoft = 4 * kRt, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kThreads = 32 * (kSoft + 2);
+  static constexpr int kSplit = 2 / kRt;           // threads a row
+  static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kThreads = 32 * (kSoft + 2);
   static constexpr int kRows = kBq * kRt;
   static constexpr int kPart = kRows * kDim + 2 * kRows;  // floats of a partial: [dim / 4][rows][4], m, l
   static constexpr uint32_t kOCol = 256;                  // O of row tile r: kOCol + r kDim
+  static constexpr int kArrive = kSplit * kBq;            // threads of a row tile
   // barriers
-  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 6, O_FREE = 8, ALL_DONE = 10, K_FULL = 11,
+  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 6, O_FREE = 8, ALL_DONE = 10, X_FULL = 11, K_FULL = 12,
                        K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
                        V_FREE = V_FULL + kStages * kVParts, kBars = V_FREE + kStages * kVParts;
 };
@@ -101,16 +104,19 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   __shared__ LineStart ls;
   __shared__ long long scan[kThreads / 32];
   __shared__ uint32_t held[8];  // 16-key groups of a tile that lie in a page
-  __shared__ uint32_t tmem_slot, s_last;
+  __shared__ uint32_t tmem_slot, s_last, s_bad[4];
+  __shared__ float s_max[C::kSplit][C::kSplit][kBq], s_sum[C::kSplit][kBq];  // two threads a row: what they tell each other
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int group = a.n_q / c.n_kv, item_tt = kRt * tt;  // tokens of a row tile, of an item
 
+  if (threadIdx.x < 4) s_bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i)
-      mbar_init(bar(i), i == C::P_FULL || i == C::P_FULL + 1 || i == C::O_FREE || i == C::O_FREE + 1 ? kBq : 1);
+      mbar_init(bar(i), i == C::P_FULL || i == C::P_FULL + 1 || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive
+                                                                                                                       : 1);
     fence_mbar_init();
     prefetch_tmap(&tmQ);
     prefetch_tmap(&tmK);
@@ -252,7 +258,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll
             for (int k = 0; k < C::kVKeys / 16; ++k) {
               const int kk = vp * (C::kVKeys / 16) + k;  // 16 keys: 8 columns of P
-              tc_mma_ts(o, p + 8u * (uint32_t)kk, dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
+              // (over the scores that were read: with two threads a row, the second half over its own)
+              tc_mma_ts(o, p + 8u * (uint32_t)kk + (C::kSplit == 2 && kk >= 4 ? 32u : 0u), dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
             }
             if (rt == kRt - 1) tc_commit(bar(C::V_FREE + st * C::kVParts + vp));
             if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE + rt));
@@ -283,9 +290,11 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       __syncwarp();
     } else {
       // ---------------------------------------------------------------------- softmax, one row per thread
+      constexpr int kSplit = C::kSplit, kQ = 4 / kSplit, kCh = kDim / 32 / kSplit;  // chunks of 32 keys, of 32 dims a thread
       const int rt = kRt == 2 ? warp >> 2 : 0, r = threadIdx.x & (kBq - 1);  // row tile, row of it
+      const int hf = kRt == 2 ? 0 : warp >> 2;                               // which half
       const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
-      const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim);
+      const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
       const float sc = a.scale * kLog2e;
       for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
         const int tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
@@ -300,32 +309,45 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           if (ok && !mbar_wait_warp(bar(C::S_FULL + slot), (uint32_t)(kRt == 2 ? g : g >> 1) & 1u, kWaitBudgetCycles)) ok = false;
           if (!ok) continue;
           tc_fence_after();
-          if (busy) {
-            const uint32_t there = held[g & 7];
-            const bool cut = j0 < from || j0 + kBk - 1 > pos || there != 0xffu;  // some key is not this row's
-            // the scores of 32 keys that are not this row's become -inf
-            auto mask = [&](int q4, uint32_t (&x)[32]) {
-              const int f = from - j0 - 32 * q4, t = pos - j0 - 32 * q4;  // keys f .. t of the 32
-              uint32_t keep = t < 0 || f > 31 ? 0u : 0xffffffffu;
-              if (f > 0 && f <= 31) keep &= 0xffffffffu << f;
-              if (t >= 0 && t < 31) keep &= (2u << t) - 1u;
-              if (!((there >> (2 * q4)) & 1u)) keep &= 0xffff0000u;
-              if (!((there >> (2 * q4 + 1)) & 1u)) keep &= 0x0000ffffu;
+          uint32_t x[32];
+          float top = -INFINITY;
+          const uint32_t there = held[g & 7];
+          const bool cut = j0 < from || j0 + kBk - 1 > pos || there != 0xffu;  // some key is not this row's
+          // the scores of 32 keys that are not this row's become -inf
+          auto mask = [&](int q4) {
+            const int f = from - j0 - 32 * q4, t = pos - j0 - 32 * q4;  // keys f .. t of the 32
+            uint32_t keep = t < 0 || f > 31 ? 0u : 0xffffffffu;
+            if (f > 0 && f <= 31) keep &= 0xffffffffu << f;
+            if (t >= 0 && t < 31) keep &= (2u << t) - 1u;
+            if (!((there >> (2 * q4)) & 1u)) keep &= 0xffff0000u;
+            if (!((there >> (2 * q4 + 1)) & 1u)) keep &= 0x0000ffffu;
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (!((keep >> k) & 1u)) x[k] = 0xff800000u;
-            };
-            uint32_t x[32];
+            for (int k = 0; k < 32; ++k)
+              if (!((keep >> k) & 1u)) x[k] = 0xff800000u;
+          };
+          if (busy) {
             float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-              tmem_ld32(stm + 32 * q4, x);
-              if (cut) mask(q4, x);
+            for (int q = 0; q < kQ; ++q) {
+              tmem_ld32(stm + 32 * (hf * kQ + q), x);
+              if (cut) mask(hf * kQ + q);
 #pragma unroll
               for (int k = 0; k < 32; k += 2)
                 mx[(k >> 1) & 3] = fmaxf(fmaxf(mx[(k >> 1) & 3], __uint_as_float(x[k])), __uint_as_float(x[k + 1]));
             }
-            const float top = sc * fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          }
+          if constexpr (kSplit == 2) {  // the row's other thread
+            s_max[g & 1][hf][r] = top;
+            mbar_arrive(bar(C::X_FULL));
+            if (!mbar_wait_warp(bar(C::X_FULL), (uint32_t)g & 1u, kWaitBudgetCycles)) {
+              ok = false;
+              continue;
+            }
+            top = fmaxf(top, s_max[g & 1][hf ^ 1][r]);
+          }
+          if (busy) {
+            top *= sc;
             const bool grown = top > m + kGrowth;  // m = -inf: any visible key
             float up = 1.0f;
             if (grown) {
@@ -337,9 +359,9 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             const f32x2 sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
             f32x2 sum[2] = {0ull, 0ull};
 #pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-              tmem_ld32(stm + 32 * q4, x);
-              if (cut) mask(q4, x);
+            for (int q = 0; q < kQ; ++q) {
+              tmem_ld32(stm + 32 * (hf * kQ + q), x);
+              if (cut) mask(hf * kQ + q);
               uint32_t pk[16];
 #pragma unroll
               for (int k = 0; k < 32; k += 2) {
@@ -350,7 +372,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                 sum[(k >> 1) & 1] = f2_add(sum[(k >> 1) & 1], f2_pack(e0, e1));
                 pk[k >> 1] = pack2<kBf16>(e0, e1);
               }
-              tmem_st16(stm + 16 * q4, pk);  // over scores that have been read
+              tmem_st16(stm + 64 * hf + 16 * q, pk);  // over scores that have been read
             }
             float s0, s1;
             f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
@@ -363,7 +385,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               }
               tc_fence_after();
 #pragma unroll 1
-              for (int ch = 0; ch < kDim / 32; ++ch) {
+              for (int ch = 0; ch < kCh; ++ch) {
                 tmem_ld32(otm + 32 * ch, x);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[k] = __float_as_uint(__uint_as_float(x[k]) * up);
@@ -372,7 +394,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             }
             tmem_wait_st();
           }
-          if (rt == 0 && (j0 < lo || j0 + kBk - 1 > hi)) {
+          if (rt == 0 && hf == 0 && (j0 < lo || j0 + kBk - 1 > hi)) {
             // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero: row r
             // of the tile, once its copies have landed
             const int st = g % C::kStages;
@@ -410,7 +432,12 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 
         // ---- the item's output
         const int64_t row = w.q.row0 + tok;
-        uint16_t* orow = a.o + row * a.o_row + (int64_t)head * a.o_head;
+        uint16_t* orow = a.o + row * a.o_row + (int64_t)head * a.o_head + hf * (kDim / 2);
+        if constexpr (kSplit == 2) {
+          s_sum[hf][r] = l;
+          named_bar_sync(1, 32 * C::kSoft);
+          l = s_sum[0][r] + s_sum[1][r];
+        }
         auto store = [&](int ch, const float (&x)[32], float inv, float& nan) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -424,9 +451,17 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             if (live) *reinterpret_cast<uint4*>(orow + 32 * ch + 8 * k) = make_uint4(p[0], p[1], p[2], p[3]);
           }
         };
-        auto exactly = [&](bool bad) {  // rows whose result is not finite, or without weight
-          __syncwarp();
-          for (uint32_t rest = __ballot_sync(0xffffffffu, live && bad); rest; rest &= rest - 1) {
+        auto exactly = [&](bool bad) {  // rows whose result is not finite, or without weight; all softmax warps
+          uint32_t rest = __ballot_sync(0xffffffffu, live && bad);
+          if constexpr (kSplit == 2) {  // in either half
+            if (rest && lane == 0) atomicOr(&s_bad[warp & 3], rest);
+            named_bar_sync(1, 32 * C::kSoft);
+            if (hf == 1) return;
+            rest = s_bad[warp & 3];
+            __syncwarp();
+            if (lane == 0) s_bad[warp & 3] = 0;
+          }
+          for (; rest; rest &= rest - 1) {
             const int src = __ffs(rest) - 1;
             attend_row<kBf16, kDim>(c, b, a, w.s, __shfl_sync(0xffffffffu, pos, src),
                                     (int64_t)w.q.row0 + __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src),
@@ -434,11 +469,11 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
         };
         if (w.whole()) {
+          float nan = 0.0f;
           if (busy) {
-            float nan = 0.0f;
             const float inv = 1.0f / l;
 #pragma unroll 1
-            for (int ch = 0; ch < kDim / 32; ++ch) {
+            for (int ch = 0; ch < kCh; ++ch) {
               uint32_t x[32];
               float f[32];
               tmem_ld32(otm + 32 * ch, x);
@@ -446,13 +481,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(x[k]);
               store(ch, f, inv, nan);
             }
-            tc_fence_before();
-            mbar_arrive(bar(C::O_FREE + rt));
-            exactly(nan != 0.0f || !(l > 0.0f));
-          } else {
-            tc_fence_before();
-            mbar_arrive(bar(C::O_FREE + rt));
           }
+          tc_fence_before();
+          mbar_arrive(bar(C::O_FREE + rt));
+          exactly(nan != 0.0f || !(l > 0.0f));
           continue;
         }
         // ---- a piece: into the workspace, joined by the last one to arrive
@@ -461,25 +493,25 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         float* mine = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
         if (busy) {
 #pragma unroll 1
-          for (int ch = 0; ch < kDim / 32; ++ch) {
+          for (int ch = 0; ch < kCh; ++ch) {
             uint32_t x[32];
             tmem_ld32(otm + 32 * ch, x);
             if (live) {
 #pragma unroll
               for (int k = 0; k < 8; ++k)
-                __stcg(reinterpret_cast<float4*>(mine) + (size_t)(8 * ch + k) * C::kRows + pr,
+                __stcg(reinterpret_cast<float4*>(mine) + (size_t)(8 * (hf * kCh + ch) + k) * C::kRows + pr,
                        make_float4(__uint_as_float(x[4 * k]), __uint_as_float(x[4 * k + 1]), __uint_as_float(x[4 * k + 2]),
                                    __uint_as_float(x[4 * k + 3])));
             }
           }
-          if (live) {
+          if (live && hf == 0) {
             __stcg(mine + C::kRows * kDim + pr, m);
             __stcg(mine + C::kRows * kDim + C::kRows + pr, l);
           }
         }
         tc_fence_before();
         mbar_arrive(bar(C::O_FREE + rt));
-        named_bar_sync(1, C::kRows);
+        named_bar_sync(1, 32 * C::kSoft);
         if (threadIdx.x == 0) {
           __threadfence();  // the block's partials, ordered before this thread by the barrier, ahead of the count
           const unsigned int before = atomicAdd(counters + ps.first, 1u);
@@ -487,8 +519,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           if (s_last) counters[ps.first] = 0;
           __threadfence();
         }
-        named_bar_sync(1, C::kRows);
-        if (s_last && busy) {
+        named_bar_sync(1, 32 * C::kSoft);
+        if (s_last) {
           auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
           float M = -INFINITY, L = 0.0f, nan = 0.0f;
           if (live) {
@@ -502,7 +534,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
           const float inv = 1.0f / L;
 #pragma unroll 1
-          for (int ch = 0; ch < kDim / 32; ++ch) {
+          for (int ch = 0; ch < kCh; ++ch) {
             float f[32];
 #pragma unroll
             for (int k = 0; k < 32; ++k) f[k] = 0.0f;
@@ -510,7 +542,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll 2
               for (int i = 0; i < ps.count; ++i) {
                 const float mi = __ldcg(slot(i) + C::kRows * kDim + pr);
-                const float4* src = reinterpret_cast<const float4*>(slot(i)) + (size_t)(8 * ch) * C::kRows + pr;
+                const float4* src = reinterpret_cast<const float4*>(slot(i)) + (size_t)(8 * (hf * kCh + ch)) * C::kRows + pr;
                 float4 x[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) x[k] = __ldcg(src + k * C::kRows);
@@ -528,7 +560,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
           exactly(nan != 0.0f || !(L > 0.0f));
         }
-        named_bar_sync(1, C::kRows);  // s_last is free again
+        named_bar_sync(1, 32 * C::kSoft);  // s_last is free again
       }
     }
   }
