@@ -2,11 +2,13 @@
 //
 // Work.  An item is (sequence, key/value head, tile of rows); its rows are the tokens of the tile times the query
 // heads of the group, so that a group reads its keys once.  Its cost is the number of key tiles any of its
-// rows sees.  All items, one after the other, make a line of key tiles, which the CTAs of the grid divide into equal
-// stretches: whatever the lengths, the CTAs finish together.  An item that a stretch border cuts leaves fp32
+// rows sees.  All items, one after the other, make a line of key tiles, which the workers of the grid (CTAs or pairs of them) divide
+// into equal stretches: whatever the lengths, they finish together.  An item that a stretch border cuts leaves fp32
 // partials (output, reference, sum) in the workspace, and the last of its pieces to arrive joins them in the order of the
-// pieces: a fixed order, so results do not depend on who was last.  Lengths are read on the device, so a captured call follows
-// them.
+// pieces: a fixed order, so results do not depend on who was last.  Where stretches are short (kShort tiles), two cut items
+// a worker would cost more than the balance gains: if items cut into pieces of at most `unit` tiles, for a unit of up to twice the
+// even share, make no more pieces than there are workers, each worker takes one piece.  Lengths are read on the device, so a
+// captured call follows them.
 #pragma once
 
 #include "attn_common.cuh"
@@ -41,23 +43,27 @@ __device__ __forceinline__ int tiles_seen(const SeqShape& q, int window, int tt,
   return hi < 0 ? 1 : (hi >> bk_shift) - first + 1;
 }
 
-// A CTA's place on the line.
+constexpr int kShort = 12;
+
+// A worker's place on the line, in its units: key tiles, or pieces of up to `unit` of them.
 struct LineStart {
-  long long total, begin, end;  // key tiles in all; this CTA's stretch
-  long long head_cost;          // key tiles of one head of sequence s
-  long long rest;               // key tiles of sequence s before `begin`
-  int s, ctas;
+  long long total, begin, end;  // units in all; this worker's stretch
+  long long head_cost;          // units of one head of sequence s
+  long long rest;               // units of sequence s before `begin`
+  int s, workers, unit;         // unit 0: key tiles
   SeqShape q;                   // of sequence s
 };
+__device__ __forceinline__ int units_of(int n, int unit) { return unit ? (n + unit - 1) / unit : n; }
 
-// Key tiles of one head of each lane's sequence (0 rows: none).  Sequences of many row tiles are summed by the whole warp, so
-// that one long prompt does not leave a single thread counting.
-__device__ __forceinline__ long long head_cost(const SeqShape& q, int window, int tt, int bk_shift, int lane) {
+// The sum of f(key tiles) over the row tiles of each lane's sequence, for one head (0 rows: 0).  Sequences of many row tiles are
+// summed by the whole warp, so that one long prompt does not leave a single thread counting.
+template <class F>
+__device__ __forceinline__ long long sum_tiles(const SeqShape& q, int window, int tt, int bk_shift, int lane, F f) {
   const int tiles = (q.rows + tt - 1) / tt;
   long long cost = 0;
   int first;
   if (tiles <= 4)
-    for (int t = 0; t < tiles; ++t) cost += tiles_seen(q, window, tt, bk_shift, t, first);
+    for (int t = 0; t < tiles; ++t) cost += f(tiles_seen(q, window, tt, bk_shift, t, first));
   for (uint32_t many = __ballot_sync(0xffffffffu, tiles > 4); many; many &= many - 1) {
     const int src = __ffs(many) - 1;
     SeqShape p;
@@ -66,20 +72,22 @@ __device__ __forceinline__ long long head_cost(const SeqShape& q, int window, in
     p.keys = 0;
     p.pos0 = __shfl_sync(0xffffffffu, q.pos0, src);
     const int n = (p.rows + tt - 1) / tt;
-    long long sum = 0;
-    for (int t = lane; t < n; t += 32) sum += tiles_seen(p, window, tt, bk_shift, t, first);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == src) cost = sum;
+    unsigned long long sum = 0;
+    for (int t = lane; t < n; t += 32) sum += (unsigned long long)f(tiles_seen(p, window, tt, bk_shift, t, first));
+    // the warp's sum in three digits of 24 bits
+    const uint32_t a = __reduce_add_sync(0xffffffffu, (uint32_t)(sum & 0xffffffu)),
+                   b = __reduce_add_sync(0xffffffffu, (uint32_t)((sum >> 24) & 0xffffffu)),
+                   c = __reduce_add_sync(0xffffffffu, (uint32_t)(sum >> 48));
+    if (lane == src) cost = (long long)(a + ((unsigned long long)b << 24) + ((unsigned long long)c << 48));
   }
   return cost;
 }
 
 // All of the block's kT threads; `out` and `scan` (kT / 32 words) in shared memory.  Each thread takes `per` neighbouring sequences; up
-// to 32 of them are one warp's alone.  A stretch has at least `least` key tiles (but the line's last).
+// to 32 of them are one warp's alone.
 template <int kT>
 __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, int n_kv, int window, int tt, int bk_shift,
-                                           int least, LineStart* out, long long* scan) {
+                                           int worker, int workers, LineStart* out, long long* scan) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool one_warp = b.n_seqs <= 32;
   if (one_warp && warp > 0) {
@@ -88,80 +96,124 @@ __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, 
   }
   const int per = one_warp ? 1 : (b.n_seqs + kT - 1) / kT;
   SeqShape q{0, 0, 0, 0};
-  auto cost_of = [&](int s) {
-    q = SeqShape{0, 0, 0, 0};
-    if (s < b.n_seqs) q = seq_shape(b, s, page_shift);
-    return head_cost(q, window, tt, bk_shift, lane);
+  auto sum_of = [&](int s, auto f) {
+    if (per > 1 || s < 0) {
+      s = s < 0 ? ~s : s;
+      q = SeqShape{0, 0, 0, 0};
+      if (s < b.n_seqs) q = seq_shape(b, s, page_shift);
+    }
+    return sum_tiles(q, window, tt, bk_shift, lane, f);
   };
-  long long mine = 0;
-  for (int i = 0; i < per; ++i) mine += cost_of(tid * per + i);
-  const long long one = mine;
-  mine *= n_kv;
-  long long upto = mine;
+  // the running sum over the block's threads, and its total
+  auto run = [&](long long mine, long long& total) {
+    if (b.n_seqs == 1) {
+      total = __shfl_sync(0xffffffffu, mine, 0);
+      return total;
+    }
+    long long upto = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long x = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += x;
-  }
-  long long total = 0;
-  if (one_warp) {
-    total = __shfl_sync(0xffffffffu, upto, 31);
-  } else {
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (one_warp) {
+      total = __shfl_sync(0xffffffffu, upto, 31);
+      return upto;
+    }
+    __syncthreads();
     if (lane == 31) scan[warp] = upto;
     __syncthreads();
+    total = 0;
     for (int w = 0; w < kT / 32; ++w) {
       if (w < warp) upto += scan[w];
       total += scan[w];
     }
+    return upto;
+  };
+  long long one = 0, total = 0;
+  for (int i = 0; i < per; ++i) one += sum_of(~(tid * per + i), [](int n) { return (long long)n; });
+  long long upto = run(one * n_kv, total);
+  int unit = 0;
+  if (total > workers && total <= (long long)kShort * workers) {
+    // pieces for four units, 16 bits each (no more of them than tiles, 12 x 152)
+    const int least = (int)((total + workers - 1) / workers), step = max(1, (least + 2) / 4);
+    uint32_t inv[4];  // quotients by a product: exact for the 12 x 152 tiles and units up to 21 there are
+#pragma unroll
+    for (int j = 0; j < 4; ++j) inv[j] = (uint32_t)ceilf(__fdividef(65536.0f, (float)(least + j * step)) + 0.001f);
+    auto pieces = [&](int n) {
+      uint32_t p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = (uint32_t)(n + least + j * step - 1) * inv[j] >> 16;
+      return (long long)(((unsigned long long)(p[3] << 16 | p[2]) << 32) | (p[1] << 16 | p[0]));
+    };
+    long long some = 0, sums = 0;
+    for (int i = 0; i < per; ++i) some += sum_of(tid * per + i, pieces);
+    const long long upto4 = run(some * n_kv, sums);
+#pragma unroll
+    for (int j = 3; j >= 0; --j)
+      if ((int)((sums >> (16 * j)) & 0xffff) <= workers) {
+        unit = least + j * step;
+        total = (sums >> (16 * j)) & 0xffff;
+        upto = (upto4 >> (16 * j)) & 0xffff;
+        one = (some >> (16 * j)) & 0xffff;
+      }
   }
-  const int ctas = (int)min((long long)gridDim.x, (total + least - 1) / least), cta = blockIdx.x;
-  if (cta >= ctas) {
-    if (tid == 0) *out = LineStart{total, 0, 0, 1, 0, 0, ctas, q};
+  const long long mine = one * n_kv;
+  const int used = (int)min((long long)workers, total);
+  if (worker >= used) {
+    if (tid == 0) *out = LineStart{total, 0, 0, 1, 0, 0, used, unit, q};
     __syncthreads();
     return;
   }
-  const long long begin = total * cta / ctas, end = total * (cta + 1) / ctas;
+  const long long begin = total * worker / used, end = total * (worker + 1) / used;
   const bool owner = begin >= upto - mine && begin < upto;
   if (per == 1) {
-    if (owner) *out = LineStart{total, begin, end, one, begin - (upto - mine), tid, ctas, q};
+    if (owner) *out = LineStart{total, begin, end, one, begin - (upto - mine), tid, used, unit, q};
   } else if (__any_sync(0xffffffffu, owner)) {  // the owner's warp walks its sequences again
     long long at = upto - mine;
     for (int i = 0; i < per; ++i) {
-      const long long c = cost_of(tid * per + i);
-      if (begin >= at && begin < at + c * n_kv) *out = LineStart{total, begin, end, c, begin - at, tid * per + i, ctas, q};
+      const long long c = sum_of(tid * per + i, [&](int n) { return (long long)units_of(n, unit); });
+      if (begin >= at && begin < at + c * n_kv) *out = LineStart{total, begin, end, c, begin - at, tid * per + i, used, unit, q};
       at += c * n_kv;
     }
   }
   __syncthreads();
 }
 
-// One item of a CTA's stretch and this CTA's piece of it; a warp walks the same items as the others.
+// One item of a worker's stretch and this worker's piece of it; a warp walks the same items as the others.
 struct Walk {
-  long long off, at, end;   // line offsets: the item's first key tile, the piece's, the stretch's end
+  long long off, at, end;   // line offsets: the item's first unit, the piece's, the stretch's end
   SeqShape q;
-  int s, h, t, row_tiles;
+  int s, h, t, row_tiles, unit;
   int first, n;             // the item's key tiles: first, first + 1, ..
   int k0, cnt;              // the piece: tiles k0 .. k0 + cnt - 1 of them
 
   __device__ __forceinline__ void piece() {
-    k0 = (int)(at - off);
-    cnt = (int)min((long long)(n - k0), end - at);
+    if (unit) {  // one unit: as even a share of the tiles as it goes
+      const int of = units_of(n, unit), j = (int)(at - off);
+      k0 = n * j / of;
+      cnt = n * (j + 1) / of - k0;
+    } else {
+      k0 = (int)(at - off);
+      cnt = (int)min((long long)(n - k0), end - at);
+    }
   }
   // the whole warp
   __device__ __forceinline__ void start(const LineStart& ls, const PagedBatch& b, int page_shift, int window, int tt,
                                         int bk_shift, int lane) {
     s = ls.s;
     q = ls.q;
+    unit = ls.unit;
     row_tiles = (q.rows + tt - 1) / tt;
     h = ls.rest < ls.head_cost ? 0
         : ((ls.rest | ls.head_cost) >> 31) == 0 ? (int)((uint32_t)ls.rest / (uint32_t)ls.head_cost)
                                                  : (int)(ls.rest / ls.head_cost);
-    long long left = ls.rest - h * ls.head_cost;  // key tiles of this head before the stretch
+    long long left = ls.rest - h * ls.head_cost;  // units of this head before the stretch
     at = ls.begin;
     end = ls.end;
     for (int t0 = 0;; t0 += 32) {
       int f;
-      const int c = t0 + lane < row_tiles ? tiles_seen(q, window, tt, bk_shift, t0 + lane, f) : 0;
+      const int c = t0 + lane < row_tiles ? units_of(tiles_seen(q, window, tt, bk_shift, t0 + lane, f), unit) : 0;
       int upto = c;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -188,9 +240,9 @@ struct Walk {
   }
   __device__ __forceinline__ bool more() const { return at < end; }
   __device__ __forceinline__ void next(const PagedBatch& b, int page_shift, int n_kv, int window, int tt, int bk_shift) {
-    at += cnt;
+    at += unit ? 1 : cnt;
     if (at >= end) return;
-    off += n;
+    off += units_of(n, unit);
     if (++t == row_tiles) {
       t = 0;
       if (++h == n_kv) {
@@ -225,21 +277,30 @@ __device__ __forceinline__ int group_page(const PagedBatch& b, const PagedCache&
   return page < 0 || page >= c.n_pages ? -1 : page;
 }
 
-// The CTA whose stretch holds line offset x: the last i with floor(total i / ctas) <= x.
-__device__ __forceinline__ int cta_of(long long x, const LineStart& ls) {
-  return (int)(((x + 1) * ls.ctas - 1) / ls.total);
+// The worker whose stretch holds line offset x: the last i with floor(total i / workers) <= x.
+__device__ __forceinline__ int worker_of(long long x, const LineStart& ls) {
+  return (int)(((x + 1) * ls.workers - 1) / ls.total);
 }
 
-// Partials.  A CTA cuts at most two items: the one its stretch begins within (slot 0) and the one it ends within and began
-// itself (slot 1); an item's pieces lie in slot 1 of its first CTA and slot 0 of the following ones.  Arrivals are counted
-// at the first CTA's index in the workspace's counters.
+// Partials.  A worker cuts at most two items: the one its stretch begins within (slot 0) and the one it ends within and began
+// itself (slot 1); an item's pieces lie in slot 1 of its first worker and slot 0 of the following ones.  Arrivals are counted
+// at the first worker's index in the workspace's counters.
 struct Pieces {
-  int first, count;  // CTAs
+  int first, count;  // workers
 };
+// One thread, after a barrier of the block: counts the block's piece in, its writes ahead of the count; what other blocks
+// wrote ahead of theirs is visible to the block after its next barrier.  Returns whether it is the last of `of`.
+__device__ __forceinline__ bool last_piece(unsigned int* counter, int of) {
+  unsigned int before;
+  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;\n" : "=r"(before) : "l"(counter) : "memory");
+  const bool last = before + 1 == (unsigned int)of;
+  if (last) *counter = 0;
+  return last;
+}
 __device__ __forceinline__ Pieces pieces_of(const Walk& w, const LineStart& ls) {
   Pieces p;
-  p.first = cta_of(w.off, ls);
-  p.count = cta_of(w.off + w.n - 1, ls) - p.first + 1;
+  p.first = worker_of(w.off, ls);
+  p.count = worker_of(w.off + units_of(w.n, w.unit) - 1, ls) - p.first + 1;
   return p;
 }
 

@@ -1,8 +1,11 @@
-// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows (head dims 64 and
-// 128) or 128 rows (256), tokens times the query heads of a group, in tiles of 128 rows with one row per TMEM lane.
+// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows, tokens times
+// the query heads of a group, in two tiles of 128 rows with one row per TMEM lane.  At head dims 64 and 128 one CTA has both tiles,
+// at 256 (whose output fills tensor memory) each CTA of a pair has one, and either copies half of every K and V part to both:
+// read from L2 once for 256 rows either way (with 128, L2 bounded the kernel: 23 bytes a clock and SM).
 //
-// One CTA per SM walks its stretch of the line of key tiles (attn_paged.cuh), 128 keys at a time:
-//  * the load warp copies by TMA: an item's queries, and K and V tiles page by page;
+// A worker (CTA or pair), one CTA per SM, walks its stretch of the line of key tiles (attn_paged.cuh), 128 keys at a time:
+//  * two warps copy by TMA, page by page: one an item's queries and the K tiles, one the V tiles (either as its tiles are handed
+//    back, which one warp's order would tie together);
 //  * the issue warp allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) for each row tile, and O += P V
 //    (128 x dim x 128), P read from tensor memory.  V lies as the cache has it, keys by dims, so it is the product's
 //    MN-major operand and needs no transposition;
@@ -11,8 +14,7 @@
 //    c = scale log2 e in chunks of 32 scores, and write P over the scores they have read, where the second product finds it.  m
 //    moves when the maximum grew by more than 2^8 only: O is then rescaled in tensor memory.
 // Tensor memory holds 512 columns: two slots of 128 for S and P, and O of 2 x 64, 2 x 128 or 256.  With two row tiles each has
-// a slot of its own, and the tensor cores work for one while the other's softmax runs; a K and a V tile read from L2
-// serve 256 rows (with 128, L2 bounded the kernel).  At head dim 256 the slots alternate: S of the next key tile is
+// a slot of its own, and the tensor cores work for one while the other's softmax runs.  At head dim 256 the slots alternate: S of the next key tile is
 // issued before P of this one is awaited; one K and one V tile fill shared memory beside the queries, so tiles are copied and
 // handed back in quarters (K by 64 dims, V by 32 keys), and the copies of the next tile follow the products through this one.
 // The products of one thread run in the order of their issue, which is what frees a slot: S of a slot is issued after
@@ -31,11 +33,11 @@ namespace {
 
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
-constexpr int kLeast = 2;        // key tiles of a stretch, at least
 
 template <int kDim>
 struct Cfg {
-  static constexpr int kRt = kDim == 256 ? 1 : 2;  // row tiles of an item
+  static constexpr int kRt = kDim == 256 ? 1 : 2;  // row tiles of a CTA
+  static constexpr int kCl = 2 / kRt;              // CTAs of a worker
   static constexpr int kChunks = kDim / 64;
   static constexpr int kStages = kDim == 256 ? 1 : kDim == 128 ? 2 : 4;
   static constexpr int kTile = kChunks * kSub;
@@ -44,7 +46,7 @@ struct Cfg {
   static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys, or whole
   static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
   static constexpr int kSplit = 2 / kRt;           // threads a row
-  static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kThreads = 32 * (kSoft + 2);
+  static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kLoadV = kSoft + 2, kThreads = 32 * (kSoft + 3);
   static constexpr int kRows = kBq * kRt;
   static constexpr int kPart = kRows * kDim + 2 * kRows;  // floats of a partial: [dim / 4][rows][4], m, l
   static constexpr uint32_t kOCol = 256;                  // O of row tile r: kOCol + r kDim
@@ -63,6 +65,25 @@ __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, uint32_t lead) {
 }
 constexpr uint32_t kIdescBMnMajor = 1u << 16;
 
+// Arrives, once the MMAs issued so far have completed, at the barrier in every CTA of a pair.
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
+}
+// A box into both CTAs of a pair, at the same offsets, counted at the same barrier of each.
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const void* tmap, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3, "
+      "%4, %5}], [%6], %7;\n" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar), "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
 // A from tensor memory (two 16-bit elements a column)
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -97,7 +118,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                        const __grid_constant__ CUtensorMap tmV, PagedCache c, PagedBatch b, AttnCall a, int tt,
                        float* __restrict__ part, unsigned int* __restrict__ counters, unsigned int* __restrict__ err) {
   using C = Cfg<kDim>;
-  constexpr int kRt = C::kRt, kThreads = C::kThreads, kLoadWarp = C::kLoadWarp, kIssueWarp = C::kIssueWarp;
+  constexpr int kRt = C::kRt, kThreads = C::kThreads, kIssueWarp = C::kIssueWarp;
   constexpr uint32_t kOCol = C::kOCol;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ uint64_t bars[C::kBars];
@@ -110,12 +131,15 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = a.n_q / c.n_kv, item_tt = kRt * tt;  // tokens of a row tile, of an item
+  const int group = a.n_q / c.n_kv, item_tt = 2 * tt;  // tokens of a row tile, of an item
+  constexpr int kCl = C::kCl;
+  const int rank = kCl == 2 ? (int)(blockIdx.x & 1) : 0, worker = (int)blockIdx.x / kCl;  // clusters are neighbouring CTAs
 
   if (threadIdx.x < 4) s_bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i)
       mbar_init(bar(i), i == C::P_FULL || i == C::P_FULL + 1 || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive
+                        : (i >= C::K_FREE && i < C::V_FULL) || i >= C::V_FREE                                          ? kCl
                                                                                                                        : 1);
     fence_mbar_init();
     prefetch_tmap(&tmQ);
@@ -129,40 +153,47 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if constexpr (kCl == 2) pair_sync();  // the peer's barriers are there to be arrived at
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   pdl_wait();
   pdl_trigger();
-  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, kLeast, &ls, scan);  // syncs the block
+  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, worker, (int)gridDim.x / kCl, &ls, scan);  // syncs the block
   bool ok = true;
 
   if (ls.begin < ls.end) {
     Walk w;
     w.start(ls, b, c.page_shift, a.window, item_tt, kBkShift, lane);
     int g = 0, item = 0;  // tiles and items of this CTA so far
-    if (warp == kLoadWarp) {
+    if (warp == C::kLoadWarp || warp == C::kLoadV) {
       // ---------------------------------------------------------------------- TMA copies
-      const int box = min(kBoxSlots, 1 << c.page_shift);
+      const bool kv = warp == C::kLoadV;
+      const CUtensorMap* map = kv ? &tmV : &tmK;
+      const int full = kv ? C::V_FULL : C::K_FULL, free = kv ? C::V_FREE : C::K_FREE;
+      const int box = min(kBoxSlots, 1 << c.page_shift), n_box = (kv ? C::kVKeys : kBk) / box;  // boxes of a part in a column
+      const int n_ops = n_box * (kv ? C::kChunks : C::kKCols);
       const uint32_t q_bytes = (uint32_t)(kRt * group * tt * 128 * C::kChunks);
-      int nk = 0, nv = 0;  // parts whose copies have been issued
+      int issued = 0;  // parts whose copies have been issued
       for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
         const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
         constexpr int kGroups = kBk / 16, kBatch = 32 / kGroups;  // tiles whose pages are read at once, ahead of their use
         int page = group_page(b, c, w.s, (w.first + w.k0) << kBkShift, lo, hi, box, lane), ahead = -1;
-        if (item > 0 && !mbar_wait_warp(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) {
-          ok = false;
-          break;
-        }
-        if (elect_one()) {
-          mbar_arrive_expect_tx(bar(C::Q_FULL), q_bytes);
+        if (!kv) {
+          if (item > 0 && !mbar_wait_warp(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) {
+            ok = false;
+            break;
+          }
+          if (elect_one()) {
+            mbar_arrive_expect_tx(bar(C::Q_FULL), q_bytes);
 #pragma unroll
-          for (int rt = 0; rt < kRt; ++rt)
+            for (int rt = 0; rt < kRt; ++rt)
 #pragma unroll
-            for (int ch = 0; ch < C::kChunks; ++ch)
-              tma_load_3d(base + (uint32_t)(rt * C::kTile + ch * kSub), &tmQ, 64 * ch, w.h * group,
-                          w.q.row0 + w.t * item_tt + rt * tt, bar(C::Q_FULL));
+              for (int ch = 0; ch < C::kChunks; ++ch)
+                tma_load_3d(base + (uint32_t)(rt * C::kTile + ch * kSub), &tmQ, 64 * ch, w.h * group,
+                            w.q.row0 + w.t * item_tt + (rank + rt) * tt, bar(C::Q_FULL));
+          }
+          __syncwarp();
         }
-        __syncwarp();
         for (int i = 0; ok && i < w.cnt; ++i, ++g) {
           const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << kBkShift, in_batch = i % kBatch;
           if (in_batch == 0) {
@@ -170,50 +201,50 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             if (i + kBatch < w.cnt) ahead = group_page(b, c, w.s, tile0 + (kBatch << kBkShift), lo, hi, box, lane);
           }
           const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (in_batch * kGroups)) & ((1u << kGroups) - 1u);
-          const uint32_t ph = (uint32_t)(g / C::kStages - 1) & 1u;
-          const int kbox = kBk / box, vbox = C::kVKeys / box;  // boxes of a part in a column
-#pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {  // K, then V
-            const int full = kv ? C::V_FULL : C::K_FULL, free = kv ? C::V_FREE : C::K_FREE;
-            for (int pt = 0; ok && pt < C::kKParts; ++pt) {
-              const int bi = st * C::kKParts + pt;
-              if (g >= C::kStages && !mbar_wait_warp(bar(free + bi), ph, kWaitBudgetCycles)) {
-                ok = false;
-                break;
-              }
-              if (lane == 0) {
-                if (kv == 0 && pt == 0) held[g & 7] = there;
-                mbar_arrive_expect_tx(bar(full + bi), (uint32_t)(C::kTile / C::kKParts));
-              }
-              __syncwarp();
-              // lane = (column, box)
-              const int n_box = kv ? vbox : kbox;
-              const int bx = (kv ? pt * vbox : 0) + lane % n_box, ch = (kv ? 0 : pt * C::kKCols) + lane / n_box;
-              const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + bx * (box / 16)) & 31);
-              if (lane < n_box * (kv ? C::kChunks : C::kKCols))
-                tma_load_4d(base + (uint32_t)((kv ? C::kOffV : C::kOffK) + st * C::kTile + ch * kSub + bx * box * 128),
-                            kv ? &tmV : &tmK, 64 * ch, (tile0 + bx * box) & ((1 << c.page_shift) - 1), w.h,
-                            pg < 0 ? c.n_pages : pg, bar(full + bi));
-              (kv ? nv : nk) = g * C::kKParts + pt + 1;
+          for (int pt = 0; pt < C::kKParts; ++pt) {
+            const int bi = st * C::kKParts + pt;
+            if (g >= C::kStages && !mbar_wait_warp(bar(free + bi), (uint32_t)(g / C::kStages - 1) & 1u, kWaitBudgetCycles)) {
+              ok = false;
+              break;
             }
+            if (lane == 0) {
+              if (!kv && pt == 0) held[g & 7] = there;
+              mbar_arrive_expect_tx(bar(full + bi), (uint32_t)(C::kTile / C::kKParts));
+            }
+            __syncwarp();
+            // lane = (column, box); of a pair each CTA copies every other one
+            const int o = lane * kCl + rank, bx = (kv ? pt * n_box : 0) + o % n_box, ch = (kv ? 0 : pt * C::kKCols) + o / n_box;
+            const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + bx * (box / 16)) & 31);
+            if (o < n_ops) {
+              const uint32_t dst = base + (uint32_t)((kv ? C::kOffV : C::kOffK) + st * C::kTile + ch * kSub + bx * box * 128);
+              const int slot = (tile0 + bx * box) & ((1 << c.page_shift) - 1), at = pg < 0 ? c.n_pages : pg;
+              if constexpr (kCl == 2)
+                tma_load_4d_pair(dst, map, 64 * ch, slot, w.h, at, bar(full + bi));
+              else
+                tma_load_4d(dst, map, 64 * ch, slot, w.h, at, bar(full + bi));
+            }
+            issued = g * C::kKParts + pt + 1;
           }
         }
       }
       // the last copies land before the CTA may end
       if (!ok && lane == 0) atomicOr(err, DEVERR_PRODUCER_WAIT);
-      bool drained = item == 0 || mbar_wait_warp(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles);
-      for (int k = max(0, nk - C::kStages * C::kKParts); k < nk; ++k)
-        drained &= mbar_wait_warp(bar(C::K_FULL + k % (C::kStages * C::kKParts)), (uint32_t)(k / (C::kStages * C::kKParts)) & 1u,
-                                  kWaitBudgetCycles);
-      for (int k = max(0, nv - C::kStages * C::kVParts); k < nv; ++k)
-        drained &= mbar_wait_warp(bar(C::V_FULL + k % (C::kStages * C::kVParts)), (uint32_t)(k / (C::kStages * C::kVParts)) & 1u,
-                                  kWaitBudgetCycles);
+      constexpr int kRing = C::kStages * C::kKParts;
+      bool drained = kv || item == 0 || mbar_wait_warp(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles);
+      for (int k = max(0, issued - kRing); k < issued; ++k)
+        drained &= mbar_wait_warp(bar(full + k % kRing), (uint32_t)(k / kRing) & 1u, kWaitBudgetCycles);
       if (!drained && lane == 0) atomicOr(err, DEVERR_DRAIN_WAIT);
     } else if (warp == kIssueWarp) {
       // ---------------------------------------------------------------------- MMAs
       constexpr uint32_t fmt = kBf16 ? 1u : 0u;
       constexpr uint32_t idesc_s = idesc_f16(fmt, kBk, kBq), idesc_o = idesc_f16(fmt, kDim, kBq) | kIdescBMnMajor;
       const uint64_t dq = sdesc_swz(base);
+      auto hand_back = [&](uint32_t b0) {  // either CTA of a pair writes to both
+        if constexpr (kCl == 2)
+          tc_commit_pair(b0);
+        else
+          tc_commit(b0);
+      };
       // S of key tile i (this CTA's count) for row tile rt, into its slot; hands K back after the last row tile, Q after `last`
       auto issue_s = [&](int i, int rt, bool last) {
         const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
@@ -230,7 +261,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               const uint32_t at = (uint32_t)((pt * C::kKCols + (k >> 2)) * (kSub >> 4) + 2 * (k & 3));
               tc_mma(tmem + 128u * (uint32_t)slot, dq + (uint32_t)(rt * (C::kTile >> 4)) + at, dk + at, idesc_s, pt > 0 || k > 0);
             }
-            if (rt == kRt - 1) tc_commit(bar(C::K_FREE + st * C::kKParts + pt));
+            if (rt == kRt - 1) hand_back(bar(C::K_FREE + st * C::kKParts + pt));
           }
           __syncwarp();
         }
@@ -261,7 +292,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               // (over the scores that were read: with two threads a row, the second half over its own)
               tc_mma_ts(o, p + 8u * (uint32_t)kk + (C::kSplit == 2 && kk >= 4 ? 32u : 0u), dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
             }
-            if (rt == kRt - 1) tc_commit(bar(C::V_FREE + st * C::kVParts + vp));
+            if (rt == kRt - 1) hand_back(bar(C::V_FREE + st * C::kVParts + vp));
             if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE + rt));
           }
           __syncwarp();
@@ -297,7 +328,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
       const float sc = a.scale * kLog2e;
       for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
-        const int tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
+        const int tok0 = w.t * item_tt + (rank + rt) * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
         const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
         const bool live = r < rows, busy = 32 * (warp & 3) < rows;  // this row's, and any of the warp's
         const int tok = tok0 + (live ? r / group : 0), head = w.h * group + (live ? r % group : 0);
@@ -490,7 +521,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         // ---- a piece: into the workspace, joined by the last one to arrive
         const Pieces ps = pieces_of(w, ls);
         const int pr = rt * kBq + r;  // row of the partial
-        float* mine = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
+        float* mine = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;  // pieces of one rank are joined
         if (busy) {
 #pragma unroll 1
           for (int ch = 0; ch < kCh; ++ch) {
@@ -512,16 +543,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         tc_fence_before();
         mbar_arrive(bar(C::O_FREE + rt));
         named_bar_sync(1, 32 * C::kSoft);
-        if (threadIdx.x == 0) {
-          __threadfence();  // the block's partials, ordered before this thread by the barrier, ahead of the count
-          const unsigned int before = atomicAdd(counters + ps.first, 1u);
-          s_last = before + 1 == (unsigned int)ps.count;
-          if (s_last) counters[ps.first] = 0;
-          __threadfence();
-        }
+        if (threadIdx.x == 0) s_last = last_piece(counters + ps.first * kCl + rank, ps.count);
         named_bar_sync(1, 32 * C::kSoft);
         if (s_last) {
-          auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
+          auto slot = [&](int i) { return part + (size_t)(2 * ((ps.first + i) * kCl + rank) + (i == 0 ? 1 : 0)) * C::kPart; };
           float M = -INFINITY, L = 0.0f, nan = 0.0f;
           if (live) {
 #pragma unroll 4
@@ -566,6 +591,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if constexpr (kCl == 2) pair_sync();  // the peer writes and arrives here no more
   if (warp == kIssueWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
@@ -590,9 +616,22 @@ w8a8_status launch(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a
   W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
   W8A8_TRY(make_kv_maps(pc, kDim, &tk, &tv));
   char* base = static_cast<char*>(ws);
-  W8A8_CUDA(launch_pdl(attn_chunks_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
-                       pc, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
-                       reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(sms / C::kCl * C::kCl));
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = C::kCl;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  W8A8_CUDA(cudaLaunchKernelEx(&cfg, attn_chunks_kernel<kBf16, kDim>, tq, tk, tv, pc, pb, a, tt,
+                               reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
+                               reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
   return W8A8_OK;
 }
 

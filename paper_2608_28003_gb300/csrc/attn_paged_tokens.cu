@@ -18,6 +18,7 @@ namespace w8a8 {
 namespace {
 
 constexpr int kRows = 16;
+constexpr int kMaxPieces = 192;  // of an item: no more than CTAs
 
 template <int kDim>
 struct Cfg {
@@ -30,7 +31,7 @@ struct Cfg {
   static constexpr int kPer = kDim / 8 / kWarps;              // groups of 8 dims that a warp joins
   static constexpr int kSmem = kStages * kStage + kJoin + 1024;
   static constexpr int kThreads = 32 * (kWarps + 1);
-  // floats of a partial: [row half][dim / 8][32 lanes][2] outputs, then m and l of the 16 rows
+  // floats of a partial: [16 rows][dim] outputs, then m and l of the rows
   static constexpr int kPart = kRows * kDim + 2 * kRows;
 };
 
@@ -52,6 +53,66 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uin
     mma_bf16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
   else
     mma_f16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
+}
+
+// The pieces of an item, joined in their order, by the consumer warps: outputs to o (row r at (r / group) o_row + (r % group) o_head).
+// What another SM has just written takes a microsecond to read, so few loads follow one another: the statistics of all
+// pieces (a warp a row, lane = piece), then every thread's part of the output with up to kAhead pieces in flight.  Rows whose
+// result is not finite, or without weight, are marked in *bad.  Not inline: its registers are not the main loop's.
+template <bool kBf16, int kDim>
+__device__ __noinline__ void join_pieces(const float* part, int first, int count, int rows, int group, uint16_t* o, int64_t o_row,
+                                         int64_t o_head, float* fac, uint32_t* bad) {
+  using C = Cfg<kDim>;
+  constexpr int kConsumers = 32 * C::kWarps, kAhead = 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto slot = [&](int i) { return part + (size_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
+  float* sums = fac + kMaxPieces * kRows;  // fac: [piece][row] 2^(m - max)
+  static_assert(C::kJoin >= (kMaxPieces + 1) * kRows * (int)sizeof(float), "the factors fit over the join buffer");
+  for (int r = warp; r < rows; r += C::kWarps) {
+    float mi[kMaxPieces / 32], li[kMaxPieces / 32], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kMaxPieces / 32; ++j) {
+      const bool there = lane + 32 * j < count;
+      mi[j] = there ? __ldcg(slot(lane + 32 * j) + kRows * kDim + r) : -INFINITY;
+      li[j] = there ? __ldcg(slot(lane + 32 * j) + kRows * kDim + kRows + r) : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kMaxPieces / 32; ++j) top = fmaxf(top, mi[j]);
+    top = warp_max_f(top);
+#pragma unroll
+    for (int j = 0; j < kMaxPieces / 32; ++j) {
+      const float f = mi[j] == -INFINITY ? 0.0f : ex2(mi[j] - top);
+      sum = fmaf(li[j], f, sum);
+      fac[(lane + 32 * j) * kRows + r] = f;
+    }
+    sum = warp_sum_f(sum);
+    if (lane == 0) sums[r] = sum;
+  }
+  named_bar_sync(1, kConsumers);
+  for (int e = threadIdx.x; e < rows * (kDim / 4); e += kConsumers) {  // four dims of a row
+    const int r = e / (kDim / 4);
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+      float4 x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i0 + i < count) x[i] = __ldcg(reinterpret_cast<const float4*>(slot(i0 + i)) + e);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i0 + i < count) {
+          const float f = fac[(i0 + i) * kRows + r];
+          y.x = fmaf(x[i].x, f, y.x);
+          y.y = fmaf(x[i].y, f, y.y);
+          y.z = fmaf(x[i].z, f, y.z);
+          y.w = fmaf(x[i].w, f, y.w);
+        }
+    }
+    const float sum = sums[r], inv = 1.0f / sum;
+    y.x *= inv, y.y *= inv, y.z *= inv, y.w *= inv;
+    *reinterpret_cast<uint2*>(o + (r / group) * o_row + (r % group) * o_head + 4 * (e % (kDim / 4))) =
+        make_uint2(pack2<kBf16>(y.x, y.y), pack2<kBf16>(y.z, y.w));
+    if (y.x * 0.0f + y.y * 0.0f + y.z * 0.0f + y.w * 0.0f != 0.0f || !(sum > 0.0f)) atomicOr(bad, 1u << r);
+  }
 }
 
 template <bool kBf16, int kDim>
@@ -85,7 +146,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
   pdl_wait();
   pdl_trigger();
-  find_start<C::kThreads>(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift, 1, &ls, scan);
+  find_start<C::kThreads>(b, c.page_shift, c.n_kv, a.window, tt, C::kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan);
   if (ls.begin >= ls.end) return;
   Walk w;
   w.start(ls, b, c.page_shift, a.window, tt, C::kBkShift, lane);
@@ -147,21 +208,31 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     const int lo = w.lo(a.window, tt), hi = w.hi(tt);
     // where every row of the item sees everything: between the last row's first key and the first row's position
     const int all_lo = a.window > 0 ? max(0, hi - a.window + 1) : 0, all_hi = w.q.pos0 + tok0;
-    uint32_t qf[kDim / 16][4];
+    // the queries as the first product's left operand, a lane's four words a k step, over this warp's part of the join buffer
+    // (as registers they would crowd the outputs out)
+    uint4* qf = reinterpret_cast<uint4*>(join + warp * (kDim * 4)) + lane;
     int pos[2], from[2];
+    {
+      const uint16_t* qp[2];
+      bool live[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = r0 + 8 * i;
-      const bool live = r < rows;
-      const int tok = live ? tok0 + r / group : tok0;
-      pos[i] = w.q.pos0 + tok;
-      from[i] = a.window > 0 ? pos[i] - a.window + 1 : 0;
-      const uint16_t* qp =
-          a.q + (int64_t)(w.q.row0 + tok) * a.q_row + (int64_t)(w.h * group + (live ? r % group : 0)) * a.q_head + 2 * quad;
+      for (int i = 0; i < 2; ++i) {
+        const int r = r0 + 8 * i;
+        live[i] = r < rows;
+        const int tok = live[i] ? tok0 + r / group : tok0;
+        pos[i] = w.q.pos0 + tok;
+        from[i] = a.window > 0 ? pos[i] - a.window + 1 : 0;
+        qp[i] = a.q + (int64_t)(w.q.row0 + tok) * a.q_row + (int64_t)(w.h * group + (live[i] ? r % group : 0)) * a.q_head + 2 * quad;
+      }
 #pragma unroll
       for (int k = 0; k < kDim / 16; ++k) {
-        qf[k][i] = live ? *reinterpret_cast<const uint32_t*>(qp + 16 * k) : 0u;
-        qf[k][2 + i] = live ? *reinterpret_cast<const uint32_t*>(qp + 16 * k + 8) : 0u;
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          v[i] = live[i] ? *reinterpret_cast<const uint32_t*>(qp[i] + 16 * k) : 0u;
+          v[2 + i] = live[i] ? *reinterpret_cast<const uint32_t*>(qp[i] + 16 * k + 8) : 0u;
+        }
+        qf[32 * k] = make_uint4(v[0], v[1], v[2], v[3]);
       }
     }
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, acc[kDim / 8][4];
@@ -182,8 +253,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             uint32_t kb[4];
             const int col = 2 * (k & 3) + half;
             ldsm4(kt + (uint32_t)((k >> 2) * C::kSub + row * 128 + ((col ^ (row & 7)) << 4)), kb);
-            mma16<kBf16>(s[0][k & 1], qf[k], kb[0], kb[1]);
-            mma16<kBf16>(s[1][k & 1], qf[k], kb[2], kb[3]);
+            const uint4 q4 = qf[32 * k];
+            const uint32_t qa[4] = {q4.x, q4.y, q4.z, q4.w};
+            mma16<kBf16>(s[0][k & 1], qa, kb[0], kb[1]);
+            mma16<kBf16>(s[1][k & 1], qa, kb[2], kb[3]);
           }
         }
 #pragma unroll
@@ -321,6 +394,19 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     auto out_at = [&](int r) {
       return a.o + (int64_t)(w.q.row0 + tok0 + r / group) * a.o_row + (int64_t)(w.h * group + r % group) * a.o_head;
     };
+    auto mend = [&]() {  // the marked rows, a warp each, exactly
+      named_bar_sync(kBar, kConsumers);
+      const uint32_t bad = s_bad;
+      if (bad == 0) return;
+      named_bar_sync(kBar, kConsumers);
+      if (threadIdx.x == 0) s_bad = 0;
+      for (int r = warp; r < rows; r += C::kWarps) {
+        if (!((bad >> r) & 1u)) continue;
+        const int tok = tok0 + r / group;
+        attend_row<kBf16, kDim>(c, b, a, w.s, w.q.pos0 + tok, w.q.row0 + tok, w.h * group + r % group, lane);
+      }
+      named_bar_sync(kBar, kConsumers);
+    };
     // this warp's dims of the output: y over the rows' sums; rows whose result is not finite, or without weight, are marked
     auto put = [&](const float (&sums)[2]) {
 #pragma unroll
@@ -338,17 +424,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         }
         if (nan != 0.0f || !(sums[r] > 0.0f)) atomicOr(&s_bad, 1u << row);
       }
-      named_bar_sync(kBar, kConsumers);
-      const uint32_t bad = s_bad;
-      if (bad == 0) return;
-      named_bar_sync(kBar, kConsumers);
-      if (threadIdx.x == 0) s_bad = 0;
-      for (int r = warp; r < rows; r += C::kWarps) {  // a warp a row, exactly
-        if (!((bad >> r) & 1u)) continue;
-        const int tok = tok0 + r / group;
-        attend_row<kBf16, kDim>(c, b, a, w.s, w.q.pos0 + tok, w.q.row0 + tok, w.h * group + r % group, lane);
-      }
-      named_bar_sync(kBar, kConsumers);
+      mend();
     };
     if (w.whole()) {
       put(L);
@@ -360,67 +436,23 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       float* to = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        if (r0 + 8 * r >= rows) continue;
+        const int row = r0 + 8 * r;
+        if (row >= rows) continue;
 #pragma unroll
         for (int d = 0; d < kPer; ++d)
-          __stcg(reinterpret_cast<float2*>(to + 8 * kDim * r + (size_t)((warp * kPer + d) * 32 + lane) * 2),
-                 make_float2(y[d][2 * r], y[d][2 * r + 1]));
+          __stcg(reinterpret_cast<float2*>(to + row * kDim + 8 * (warp * kPer + d) + 2 * quad), make_float2(y[d][2 * r], y[d][2 * r + 1]));
         if (warp == 0 && quad == 0) {
-          __stcg(to + kRows * kDim + r0 + 8 * r, M[r]);
-          __stcg(to + kRows * kDim + kRows + r0 + 8 * r, L[r]);
+          __stcg(to + kRows * kDim + row, M[r]);
+          __stcg(to + kRows * kDim + kRows + row, L[r]);
         }
       }
       named_bar_sync(kBar, kConsumers);
-      if (threadIdx.x == 0) {
-        __threadfence();  // the block's partials, ordered before this thread by the barrier, ahead of the count
-        const unsigned int before = atomicAdd(counters + ps.first, 1u);
-        s_last = before + 1 == (unsigned int)ps.count;
-        if (s_last) counters[ps.first] = 0;
-        __threadfence();
-      }
+      if (threadIdx.x == 0) s_last = last_piece(counters + ps.first, ps.count);
     }
     named_bar_sync(kBar, kConsumers);
     if (s_last) {
-      auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
-      float Mj[2] = {-INFINITY, -INFINITY}, Lj[2] = {0.0f, 0.0f};
-      // lane = piece: every row's maximum by the whole warp, all loads ahead of the first use
-      {
-        float top[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) top[r] = r < rows && lane < ps.count ? __ldcg(slot(lane) + kRows * kDim + r) : -INFINITY;
-        for (int i = lane + 32; i < ps.count; i += 32)
-#pragma unroll
-          for (int r = 0; r < kRows; ++r)
-            if (r < rows) top[r] = fmaxf(top[r], __ldcg(slot(i) + kRows * kDim + r));
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-          if (r >= rows) break;
-          const float x = warp_max_f(top[r]);
-          if (r == r0) Mj[0] = x;
-          if (r == r0 + 8) Mj[1] = x;
-        }
-      }
-#pragma unroll
-      for (int d = 0; d < kPer; ++d) y[d][0] = y[d][1] = y[d][2] = y[d][3] = 0.0f;
-#pragma unroll 4
-      for (int i = 0; i < ps.count; ++i) {
-        const float* from_piece = slot(i);
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          if (r0 + 8 * r >= rows) continue;
-          const float mi = __ldcg(from_piece + kRows * kDim + r0 + 8 * r);
-          const float f = mi == -INFINITY ? 0.0f : ex2(mi - Mj[r]);
-          Lj[r] = fmaf(__ldcg(from_piece + kRows * kDim + kRows + r0 + 8 * r), f, Lj[r]);
-#pragma unroll
-          for (int d = 0; d < kPer; ++d) {
-            const float2 x =
-                __ldcg(reinterpret_cast<const float2*>(from_piece + 8 * kDim * r + (size_t)((warp * kPer + d) * 32 + lane) * 2));
-            y[d][2 * r] = fmaf(x.x, f, y[d][2 * r]);
-            y[d][2 * r + 1] = fmaf(x.y, f, y[d][2 * r + 1]);
-          }
-        }
-      }
-      put(Lj);
+      join_pieces<kBf16, kDim>(part, ps.first, ps.count, rows, group, out_at(0), a.o_row, a.o_head, reinterpret_cast<float*>(join), &s_bad);
+      mend();
     }
     named_bar_sync(kBar, kConsumers);  // s_last, s_bad and the statistics are free again
   }
@@ -439,7 +471,7 @@ w8a8_status launch(const CUtensorMap& tk, const CUtensorMap& tv, const PagedCach
   }
   const int tt = kRows / (a.n_q / pc.n_kv);
   char* base = static_cast<char*>(ws);
-  W8A8_CUDA(launch_pdl(attn_tokens_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tk, tv, pc,
+  W8A8_CUDA(launch_pdl(attn_tokens_kernel<kBf16, kDim>, dim3((unsigned)(sms < kMaxPieces ? sms : kMaxPieces)), dim3(C::kThreads), (size_t)C::kSmem, st, tk, tv, pc,
                        pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
                        reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
   return W8A8_OK;
