@@ -534,8 +534,8 @@ w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache
  *   j <= p), p the row's position; query head h reads key/value head h / (n_q / n_kv).
  * A row without keys gets zeros.  A key outside a row's range, and slots that hold none, never reach it, whatever
  * their values; keys within it propagate NaN and infinities as the formula does.  Scores, softmax and sums
- * in fp32; a weight (at most e^5.5) is rounded once to the type before it meets v, and the sum that divides the
- * output is that of the rounded weights; the output is rounded once.  Deterministic.
+ * in fp32; a weight (at most 2^8) is rounded once to the type before it meets v; the output is rounded once.
+ * Deterministic: the same call gives the same bits, whatever runs beside it.
  * q and o [n_rows, n_q, head_dim] of the cache's type, strides in elements (multiples of 8); n_q a multiple of n_kv,
  * at most 128 query heads per key/value head; o overlaps no input. */
 w8a8_status w8a8_paged_attention_workspace_size(const w8a8_paged_cache* cache, int n_q, size_t* bytes);
@@ -567,6 +567,18 @@ typedef struct {
 /* tokens [M] int32; probs [M] fp32 (nullable): the token's share of the kept weight. */
 w8a8_status w8a8_sample(int dtype, const void* logits, int64_t row_stride, int M, int V, const w8a8_sampling* sampling,
                         const float* u, int32_t* tokens, float* probs, void* stream);
+
+/* A serving step of the decoder: the new tokens [n_rows] of a ragged batch through every layer under the model's mask,
+ * their keys and values appended to the caller's pages (layer l's lie layer_stride elements behind layer l - 1's; the
+ * model's own cache is not touched), and one token a sequence from its last row: by w8a8_sample from u [n_seqs]
+ * (sampling nullable: all defaults), or, with u NULL (then sampling and probs too), the largest logit's.
+ * logits [n_seqs, vocab] fp32: nullable; may be left out with u for up to max_batch sequences.  next [n_seqs], probs
+ * [n_seqs] nullable.  A sequence without rows gets the logits of a zero input; with n_rows 0 nothing is
+ * written.  n_rows and n_seqs at most max_tokens.
+ * Calls of one model that can run concurrently share its buffers: serialise them. */
+w8a8_status w8a8_decoder_step_paged(w8a8_model* m, const int32_t* tokens, const w8a8_paged_batch* batch,
+                                    const w8a8_paged_cache* cache, int64_t layer_stride, const w8a8_sampling* sampling,
+                                    const float* u, float* logits, int32_t* next, float* probs, void* stream);
 
 /* Negative log-likelihood of targets under softmax(logits) per row (LM Head section's
  * perplexity): nll[i] = logsumexp(logits[i, :]) - logits[i, targets[i]], fp32. */

@@ -197,6 +197,8 @@ SIGNATURES = {
     "w8a8_paged_attention": (_i32, [ctypes.POINTER(PagedCacheC), ctypes.POINTER(PagedBatchC), _vp, _i64, _i64, _i32, _f32,
                                     _i32, _vp, _i64, _i64, _vp, _sz, _vp]),
     "w8a8_sample": (_i32, [_i32, _vp, _i64, _i32, _i32, ctypes.POINTER(SamplingC), _vp, _vp, _vp, _vp]),
+    "w8a8_decoder_step_paged": (_i32, [_vp, _vp, ctypes.POINTER(PagedBatchC), ctypes.POINTER(PagedCacheC), _i64,
+                                       ctypes.POINTER(SamplingC), _vp, _vp, _vp, _vp, _vp]),
     "w8a8_token_nll": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp]),
     "w8a8_choose_mask": (_i32, [_fp, _fp, _fp, ctypes.POINTER(ctypes.c_int32), _i32, _f32, _f32]),
     "w8a8_allocate_mask": (_i32, [_vp, ctypes.POINTER(AllocOptsC), ctypes.POINTER(AllocReportC), _vp]),
@@ -905,6 +907,40 @@ class Decoder:
         _check("w8a8_decoder_decode_step", lib().w8a8_decoder_decode_step(self.h, _p(_bits(tokens)), B, int(pos),
                                                                           _p(logits), _p(top1), _stream(stream)))
         return logits, top1
+
+    def step_paged(self, tokens: torch.Tensor, k: torch.Tensor, v: torch.Tensor, batch: PagedBatch,
+                   u: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                   top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                   min_p: Optional[torch.Tensor] = None, want_logits: bool = False, want_probs: bool = False, stream=None):
+        """A serving step: the new tokens [n_rows] int32 of a ragged batch, their keys and values into the pages of k and v
+        [layers, n_pages, page_size, n_kv, head_dim] bf16, and the next token of every sequence: sampled from u
+        [n_seqs] with the given parameters (sample), or the largest logit's where u is None.  Returns (next
+        [n_seqs], logits [n_seqs, vocab] or None, probabilities or None); a call without rows gives -1 and zeros."""
+        dev = self._keep[0]["embed"].device
+        _need(k.dim() == 5 and k.shape[0] == self.cfg.layers and k.stride() == v.stride() and k.shape == v.shape,
+              "k and v must be [layers, n_pages, page_size, n_kv, head_dim] of equal strides")
+        n, rows = batch.kv_len.shape[0], tokens.shape[0]
+        _need(tokens.dim() == 1, "tokens [n_rows]")
+        _ints(tokens, "tokens")
+        params = ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32),
+                  (min_p, torch.float32))
+        for t, kind in params:
+            _need(t is None or (t.dtype == kind and t.shape == (n,) and t.is_contiguous()), f"a {kind} tensor [{n}] expected")
+        for t in (tokens, k, v, batch.row_start, batch.kv_len, batch.pages, *(t for t, _ in params)):
+            _need(t is None or t.device == dev, f"all tensors must be on the model's device {dev}")
+        _need(u is not None or (not want_probs and all(t is None for t, _ in params)), "sampling needs u")
+        cc, bc = PagedCache(k[0], v[0]).c(), batch.c(rows)
+        new = torch.empty if rows else torch.zeros  # without rows the library writes nothing
+        nxt = torch.empty(n, dtype=torch.int32, device=dev) if rows else torch.full((n,), -1, dtype=torch.int32, device=dev)
+        probs = new(n, dtype=torch.float32, device=dev) if want_probs else None
+        logits = None
+        if want_logits or (u is not None and n > self.cfg.max_batch):
+            logits = new(n, self.cfg.vocab, dtype=torch.float32, device=dev)
+        sp = SamplingC(*(None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)))
+        _check("w8a8_decoder_step_paged", lib().w8a8_decoder_step_paged(
+            self.h, _p(tokens), ctypes.byref(bc), ctypes.byref(cc), k.stride(0), ctypes.byref(sp) if u is not None else None,
+            _p(u), _p(logits), _p(nxt), _p(probs), _stream(stream)))
+        return nxt, logits if want_logits else None, probs
 
     TRACE_FIELDS = ("a_in", "qkv", "attn", "y_o", "a_ffn", "h", "y_f", "r", "a_fin")
 

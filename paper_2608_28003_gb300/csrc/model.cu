@@ -11,6 +11,7 @@
 
 #include "decoder_kernels.cuh"
 #include "ops.cuh"
+#include "paged.cuh"
 #include "stream_gemm.cuh"
 
 using namespace w8a8;
@@ -55,6 +56,7 @@ struct w8a8_model {
   uint16_t *kc = nullptr, *vc = nullptr;
   uint16_t *pf_k = nullptr, *pf_vt = nullptr;  // one layer's prefill attention operands (PrefillOperands)
   float *cos_l = nullptr, *sin_l = nullptr, *cos_g = nullptr, *sin_g = nullptr;
+  w8a8_rope_table rope_l{}, rope_g{};  // the same rotations for any position (w8a8_decoder_step_paged)
   int* d_pos = nullptr;
   int32_t* d_tokens = nullptr;
   float* d_logits = nullptr;
@@ -63,6 +65,7 @@ struct w8a8_model {
   size_t ws_bytes = 0;
   void* attn_ws = nullptr;
   size_t attn_ws_bytes = 0;
+  void* paged_ws = nullptr;
   // the next W8A8 linear's quantised input written by the norm kernels at 9+ tokens ([max_tokens,
   // hidden] fp16 codes, [max_tokens] scales and sums of |codes|), so that its GEMM needs no
   // quantiser launch
@@ -147,11 +150,31 @@ bool fuse_residual(const w8a8_model* m, int M, bool calib) {
   return true;
 }
 
+// A ragged batch over a paged cache, in place of the model's own cache (w8a8_decoder_step_paged): layer l's pages at
+// l layer_stride elements from layer 0's.  Logits are those of each sequence's last row.
+struct PagedStep {
+  PagedBatch batch;
+  PagedCache cache;
+  int64_t layer_stride;
+  int max_new;
+};
+
+// x[s] = the last row of sequence s (zeros where it has none); a row of H bf16 a block
+__global__ void __launch_bounds__(128) last_rows_kernel(const uint16_t* __restrict__ a, PagedBatch b, int page_shift, int H,
+                                                        uint16_t* __restrict__ x) {
+  pdl_trigger();
+  pdl_wait();
+  const SeqShape q = seq_shape(b, blockIdx.x, page_shift);
+  const uint4* src = reinterpret_cast<const uint4*>(a + (size_t)(q.row0 + max(q.rows, 1) - 1) * H);
+  uint4* dst = reinterpret_cast<uint4*>(x + (size_t)blockIdx.x * H);
+  for (int i = threadIdx.x; i < H / 8; i += 128) dst[i] = q.rows > 0 ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+}
+
 // The decoder over M = B * T rows whose positions start at *m->d_pos (set by the caller; T > 1: the
 // same as start_pos, which a decode step, T = 1, does not read).  The caller's launch before this one
 // (set_int, or the start of a graph) allows no overlap, so every launch here is settled (common.cuh).
 w8a8_status forward_core(w8a8_model* m, const int32_t* tokens, int B, int T, int start_pos, float* logits, int32_t* top1,
-                         bool calib, cudaStream_t st) {
+                         bool calib, cudaStream_t st, const PagedStep* paged = nullptr) {
   const w8a8_model_cfg& c = m->cfg;
   const int M = B * T, H = c.hidden, F = c.inter;
   const bool fuse = fuse_residual(m, M, calib);
@@ -200,7 +223,18 @@ w8a8_status forward_core(w8a8_model* m, const int32_t* tokens, int B, int T, int
       W8A8_TRY(linear(m, att8, qq, W.wqkv, m->qkv_dim, H, m->a, M, m->qkv, st, nullptr, pre_qkv ? &pc : nullptr));
       if (tr) W8A8_TRY(trace_copy(tr->qkv, l, m->qkv, m->qkv_dim, 2));
     }
-    if (attn_decode_supported(s)) {
+    if (paged) {
+      PagedCache pc = paged->cache;
+      pc.k += l * paged->layer_stride;
+      pc.v += l * paged->layer_stride;
+      uint16_t* q16 = reinterpret_cast<uint16_t*>(m->q);
+      W8A8_TRY(launch_rope_append(glob ? m->rope_g : m->rope_l, pc, paged->batch, c.head_dim, true, m->qkv, m->qkv_dim, c.n_q,
+                                  m->qkv + m->q_dim, m->qkv_dim, m->qkv + m->q_dim + m->kv_dim, m->qkv_dim, qn, kn, c.eps, q16,
+                                  m->q_dim, m->sms, st));
+      const AttnCall call{q16, m->q_dim, c.head_dim, m->o, m->q_dim, c.head_dim, c.n_q, c.head_dim, s.window, paged->max_new,
+                          s.scale, true};
+      W8A8_TRY(launch_paged_attention(pc, paged->batch, call, m->paged_ws, m->sms, st));
+    } else if (attn_decode_supported(s)) {
       W8A8_TRY(launch_attn_decode(m->qkv, s, m->d_pos, qn, kn, c.eps, cs, sn, kc, vc, m->o, st));
     } else if (attention_prefill_supported(s)) {
       const PrefillOperands w{reinterpret_cast<uint16_t*>(m->q), m->pf_k, m->pf_vt};
@@ -251,9 +285,17 @@ w8a8_status forward_core(w8a8_model* m, const int32_t* tokens, int B, int T, int
   if (tr) W8A8_TRY(trace_copy(tr->a_fin, 0, m->a, H, 2));
   if (calib) return launch_act_absmax(m->a, M, H, m->stat_lm(), st);
   const bool lm8 = m->prepared && m->lm;
-  for (int r0 = 0; r0 < M; r0 += kHeadChunk) {
-    const int rows = std::min(kHeadChunk, M - r0);
-    const uint16_t* X = m->a + (size_t)r0 * H;
+  const uint16_t* head_in = m->a;
+  int head_rows = M;
+  if (paged) {  // the residual step's input is free by now
+    head_in = m->y;
+    head_rows = paged->batch.n_seqs;
+    W8A8_CUDA(launch_pdl(last_rows_kernel, dim3((unsigned)head_rows), dim3(128), 0, st, m->a, paged->batch,
+                         paged->cache.page_shift, H, m->y));
+  }
+  for (int r0 = 0; r0 < head_rows; r0 += kHeadChunk) {
+    const int rows = std::min(kHeadChunk, head_rows - r0);
+    const uint16_t* X = head_in + (size_t)r0 * H;
     float* lg = logits ? logits + (size_t)r0 * c.vocab : nullptr;
     int32_t* tp = top1 + r0;
     if (lm8) {
@@ -423,6 +465,21 @@ extern "C" w8a8_status w8a8_model_create(const w8a8_model_cfg* cfg, const w8a8_l
   W8A8_MTRY(dalloc(m, &m->sin_l, rope));
   W8A8_MTRY(dalloc(m, &m->cos_g, rope));
   W8A8_MTRY(dalloc(m, &m->sin_g, rope));
+  for (int g = 0; g < 2; ++g) {  // the two rotations for positions of any size
+    w8a8_rope_table& rt = g ? m->rope_g : m->rope_l;
+    const w8a8_rope_cfg rc{c.head_dim, W8A8_ROPE_NONE, (double)(g ? c.rope_global : c.rope_local), 1.0, 1.0, 4.0, 1.0, 0};
+    std::vector<uint64_t> turns((size_t)c.head_dim / 2);
+    uint64_t* dev = nullptr;
+    if (rc.base <= 1.0) continue;  // (a base without rotations to speak of: the paged step refuses it)
+    W8A8_MTRY(w8a8_rope_frequencies(&rc, turns.data(), &rt.scale));
+    W8A8_MTRY(dalloc(m, &dev, turns.size()));
+    W8A8_MTRY(cudaMemcpy(dev, turns.data(), turns.size() * sizeof(uint64_t), cudaMemcpyHostToDevice) == cudaSuccess
+                  ? W8A8_OK
+                  : W8A8_ERR_CUDA);
+    rt.rotary_dim = c.head_dim;
+    rt.interleaved = 0;
+    rt.turns = dev;
+  }
   W8A8_MTRY(dalloc(m, &m->d_pos, 4));
   W8A8_MTRY(dalloc(m, &m->d_tokens, (size_t)c.max_batch));
   W8A8_MTRY(dalloc(m, &m->d_logits, (size_t)c.max_batch * c.vocab));
@@ -447,12 +504,14 @@ extern "C" w8a8_status w8a8_model_create(const w8a8_model_cfg* cfg, const w8a8_l
   }
   m->attn_ws_bytes = aws;
   W8A8_MTRY(dalloc(m, reinterpret_cast<char**>(&m->attn_ws), aws));
+  W8A8_MTRY(dalloc(m, reinterpret_cast<char**>(&m->paged_ws), paged_attention_ws(c.head_dim, c.n_q, c.n_kv, d.sms)));
   W8A8_MTRY(dalloc(m, &m->pcodes, (size_t)c.max_tokens * H));
   W8A8_MTRY(dalloc(m, &m->psx, (size_t)c.max_tokens + 4));
   W8A8_MTRY(dalloc(m, &m->psum, (size_t)c.max_tokens + 4));
   cudaStream_t st = m->st;
   W8A8_MTRY(cudaMemsetAsync(m->ws, 0, W8A8_WS_RESERVED, st) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA);
   W8A8_MTRY(cudaMemsetAsync(m->attn_ws, 0, aws, st) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA);
+  W8A8_MTRY(cudaMemsetAsync(m->paged_ws, 0, W8A8_WS_RESERVED, st) == cudaSuccess ? W8A8_OK : W8A8_ERR_CUDA);
   W8A8_MTRY(cudaMemsetAsync(m->stats, 0, ((size_t)c.layers * m->stats_stride() + H) * 4, st) == cudaSuccess
                 ? W8A8_OK
                 : W8A8_ERR_CUDA);
@@ -659,6 +718,50 @@ extern "C" w8a8_status w8a8_decoder_decode_step(w8a8_model* m, const int32_t* to
   W8A8_CUDA(cudaEventRecord(m->ev_out, st));
   W8A8_CUDA(cudaStreamWaitEvent(user, m->ev_out, 0));
   return W8A8_OK;
+}
+
+extern "C" w8a8_status w8a8_decoder_step_paged(w8a8_model* m, const int32_t* tokens, const w8a8_paged_batch* batch,
+                                               const w8a8_paged_cache* cache, int64_t layer_stride,
+                                               const w8a8_sampling* sampling, const float* u, float* logits, int32_t* next,
+                                               float* probs, void* stream) {
+  const char* who = "w8a8_decoder_step_paged";
+  W8A8_CHECK_ARG(m != nullptr, W8A8_ERR_INVALID_ARG, "%s: null model", who);
+  const w8a8_model_cfg& c = m->cfg;
+  PagedStep ps;
+  W8A8_TRY(check_paged(who, cache, batch, &ps.cache, &ps.batch));
+  W8A8_CHECK_ARG(cache->dtype == W8A8_TYPE_BF16 && cache->head_dim == c.head_dim && cache->n_kv == c.n_kv, W8A8_ERR_SHAPE,
+                 "%s: the cache must be bf16 of %d heads of %d", who, c.n_kv, c.head_dim);
+  W8A8_CHECK_ARG(layer_stride >= 0 && layer_stride % 8 == 0 && layer_stride <= (1ll << 40) && (c.layers == 1 || layer_stride > 0),
+                 W8A8_ERR_SHAPE, "%s: layer stride %lld", who, (long long)layer_stride);
+  W8A8_CHECK_ARG(ps.batch.n_rows <= c.max_tokens && ps.batch.n_seqs <= c.max_tokens, W8A8_ERR_SHAPE,
+                 "%s: %d rows of %d sequences exceed max_tokens %d", who, ps.batch.n_rows, ps.batch.n_seqs, c.max_tokens);
+  W8A8_CHECK_ARG(m->rope_l.turns && m->rope_g.turns, W8A8_ERR_UNSUPPORTED, "%s: rope bases must exceed 1", who);
+  W8A8_CHECK_ARG(u != nullptr || (sampling == nullptr && probs == nullptr), W8A8_ERR_INVALID_ARG,
+                 "%s: sampling needs uniform numbers", who);
+  if (ps.batch.n_seqs == 0 || ps.batch.n_rows == 0) return W8A8_OK;
+  W8A8_CHECK_ARG(tokens && next, W8A8_ERR_INVALID_ARG, "%s: null tokens or next", who);
+  W8A8_CHECK_ARG(aligned16(tokens) && aligned16(next) && aligned16(logits), W8A8_ERR_ALIGN,
+                 "%s: pointers must be 16-byte aligned", who);
+  if (u) {
+    W8A8_CHECK_ARG(logits != nullptr || ps.batch.n_seqs <= c.max_batch, W8A8_ERR_SHAPE,
+                   "%s: sampling for more than max_batch %d sequences needs logits", who, c.max_batch);
+    W8A8_CHECK_ARG(c.vocab <= W8A8_MAX_SAMPLE_VOCAB && c.vocab % 4 == 0, W8A8_ERR_SHAPE,
+                   "%s: sampling needs a vocabulary of a multiple of 4, up to %d", who, W8A8_MAX_SAMPLE_VOCAB);
+    const w8a8_sampling none{};
+    const w8a8_sampling& sp = sampling ? *sampling : none;
+    const void* words[] = {sp.temperature, sp.top_k, sp.top_p, sp.min_p, u, probs};
+    for (const void* p : words)
+      W8A8_CHECK_ARG((reinterpret_cast<uintptr_t>(p) & 3u) == 0, W8A8_ERR_ALIGN, "%s: arrays must be 4-byte aligned", who);
+  }
+  ps.layer_stride = layer_stride;
+  ps.max_new = batch->max_new;
+  cudaStream_t st = as_stream(stream);
+  float* lg = u && !logits ? m->d_logits : logits;
+  W8A8_TRY(launch_set_int(m->d_pos, 0, st));  // the call's first launch, which allows no overlap
+  W8A8_TRY(forward_core(m, tokens, 1, ps.batch.n_rows, 0, lg, next, false, st, &ps));
+  if (!u) return W8A8_OK;
+  return launch_sample(W8A8_TYPE_F32, lg, c.vocab, ps.batch.n_seqs, c.vocab, sampling ? *sampling : w8a8_sampling{}, u, next, probs,
+                       m->sms, st);
 }
 
 extern "C" w8a8_status w8a8_model_set_trace(w8a8_model* m, const w8a8_trace* t) {
