@@ -19,6 +19,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxDim = 256;
+constexpr int kAhead = 4;  // heads whose loads are in flight
 
 struct RopeArgs {
   const uint64_t* turns;
@@ -49,10 +50,15 @@ __device__ __forceinline__ void unit_angles(const RopeArgs& r, int unit, int pos
   }
 }
 
+struct Unit {
+  uint4 a, b;
+};
+__device__ __forceinline__ Unit unit_load(const uint16_t* p, int at0, int at1) {
+  return Unit{*reinterpret_cast<const uint4*>(p + at0), *reinterpret_cast<const uint4*>(p + at1)};
+}
 template <bool kBf16>
-__device__ __forceinline__ void unit_load(const uint16_t* p, int at0, int at1, float (&x)[16]) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p + at0), b = *reinterpret_cast<const uint4*>(p + at1);
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+__device__ __forceinline__ void unit_values(const Unit& u, float (&x)[16]) {
+  const uint32_t w[8] = {u.a.x, u.a.y, u.a.z, u.a.w, u.b.x, u.b.y, u.b.z, u.b.w};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float2 f = unpack2<kBf16>(w[i]);
@@ -105,11 +111,19 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs r, const uint16
   int at0, at1;
   unit_place(r, unit, rotated, at0, at1);
   float c[8], s[8], v[16];
-  if (rotated) unit_angles(r, unit, positions[row], c, s);
-  for (int h = h0; h < heads; h += step) {
-    unit_load<kBf16>(x + row * x_row + h * x_head, at0, at1, v);
-    if (rotated) unit_rotate(r.inter, c, s, v);
-    unit_store<kBf16>(y + row * y_row + h * y_head, at0, at1, v);
+  for (int h = h0, first = 1; h < heads; h += kAhead * step, first = 0) {
+    Unit u[kAhead];  // the loads of a few heads ahead of the first use, and of the angles
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (h + j * step < heads) u[j] = unit_load(x + row * x_row + (h + j * step) * x_head, at0, at1);
+    if (rotated && first) unit_angles(r, unit, positions[row], c, s);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (h + j * step >= heads) break;
+      unit_values<kBf16>(u[j], v);
+      if (rotated) unit_rotate(r.inter, c, s, v);
+      unit_store<kBf16>(y + row * y_row + (h + j * step) * y_head, at0, at1, v);
+    }
   }
 }
 
@@ -138,45 +152,51 @@ __global__ void __launch_bounds__(kThreads)
   int at0, at1;
   unit_place(r, unit, rotated, at0, at1);
   float c[8], sn[8], x[16];
-  if (rotated && live) unit_angles(r, unit, pos, c, sn);
   const int heads = n_q + 2 * cache.n_kv, trips = (heads + step - 1) / step;
-  for (int t = 0; t < trips; ++t) {
-    const int h = h0 + t * step;
-    const bool is_q = h < n_q, is_k = !is_q && h < n_q + cache.n_kv;
-    const bool here = live && h < heads;
-    const int kvh = is_k ? h - n_q : h - n_q - cache.n_kv;
-    if (here && !is_q && !is_k) {  // v: its bits as they are
-      if (slot >= 0) {
-        const uint16_t* src = v + (int64_t)row * v_row + (int64_t)kvh * kDim;
-        uint16_t* dst = cache.v + slot + (int64_t)kvh * cache.head_stride;
-        const uint4 a = *reinterpret_cast<const uint4*>(src + 16 * unit), b = *reinterpret_cast<const uint4*>(src + 16 * unit + 8);
-        *reinterpret_cast<uint4*>(dst + 16 * unit) = a;
-        *reinterpret_cast<uint4*>(dst + 16 * unit + 8) = b;
-      }
+  for (int t0 = 0; t0 < trips; t0 += kAhead) {
+    Unit u[kAhead];  // the loads of a few heads ahead of the first use, and of the angles
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = h0 + (t0 + j) * step;
+      if (!live || h >= heads) continue;
+      const uint16_t* src = h < n_q                ? q + (int64_t)row * q_row + (int64_t)h * kDim
+                            : h < n_q + cache.n_kv ? k + (int64_t)row * k_row + (int64_t)(h - n_q) * kDim
+                                                   : v + (int64_t)row * v_row + (int64_t)(h - n_q - cache.n_kv) * kDim;
+      u[j] = unit_load(src, at0, at1);
     }
-    const bool work = here && (is_q || is_k);
-    if (work)
-      unit_load<kBf16>(is_q ? q + (int64_t)row * q_row + (int64_t)h * kDim : k + (int64_t)row * k_row + (int64_t)kvh * kDim,
-                       at0, at1, x);
-    const float* nw = is_q ? q_norm : k_norm;
-    float ss = 0.0f;
-    if (work) {
+    if (t0 == 0 && rotated && live) unit_angles(r, unit, pos, c, sn);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
-    }
-#pragma unroll
-    for (int o = kUnits / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (work) {
-      if (nw) {
-        const float inv = 1.0f / sqrtf(ss / (float)kDim + eps);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = x[e] * inv * nw[e < 8 ? at0 + e : at1 + e - 8];
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = h0 + (t0 + j) * step;
+      if (t0 + j >= trips) break;
+      const bool is_q = h < n_q, is_k = !is_q && h < n_q + cache.n_kv, here = live && h < heads;
+      const bool work = here && (is_q || is_k);
+      if (here && !work && slot >= 0) {  // v: its bits as they are
+        uint16_t* dst = cache.v + slot + (int64_t)(h - n_q - cache.n_kv) * cache.head_stride;
+        *reinterpret_cast<uint4*>(dst + at0) = u[j].a;
+        *reinterpret_cast<uint4*>(dst + at1) = u[j].b;
       }
-      if (rotated) unit_rotate(r.inter, c, sn, x);
-      if (is_q)
-        unit_store<kBf16>(q_out + (int64_t)row * q_out_row + (int64_t)h * kDim, at0, at1, x);
-      else if (slot >= 0)
-        unit_store<kBf16>(cache.k + slot + (int64_t)kvh * cache.head_stride, at0, at1, x);
+      if (work) unit_values<kBf16>(u[j], x);
+      const float* nw = is_q ? q_norm : k_norm;
+      float ss = 0.0f;
+      if (work) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+      }
+#pragma unroll
+      for (int o = kUnits / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (work) {
+        if (nw) {
+          const float inv = 1.0f / sqrtf(ss / (float)kDim + eps);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[e] = x[e] * inv * nw[e < 8 ? at0 + e : at1 + e - 8];
+        }
+        if (rotated) unit_rotate(r.inter, c, sn, x);
+        if (is_q)
+          unit_store<kBf16>(q_out + (int64_t)row * q_out_row + (int64_t)h * kDim, at0, at1, x);
+        else if (slot >= 0)
+          unit_store<kBf16>(cache.k + slot + (int64_t)(h - n_q) * cache.head_stride, at0, at1, x);
+      }
     }
   }
 }
