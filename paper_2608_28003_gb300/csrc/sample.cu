@@ -29,7 +29,7 @@ typedef unsigned long long u64;
 
 constexpr int kT = 512, kWarps = kT / 32;
 constexpr int kFrac = 43;     // weights are multiples of 2^-43 of the largest
-constexpr int kBins = 3072;    // one per 1/64 of the exponent, 44.5 of which weigh anything
+constexpr int kBins = 2880;    // one per 1/64 of the exponent, 44.5 of which weigh anything (0 .. 2849); a multiple of 16 CTAs
 constexpr int kFine = 2048;    // and of the divisions of a crowded range
 constexpr int kMostSlice = 65536;  // 16-bit digits of that many weights add up in 32 bits
 constexpr int kSmall = 1024;
