@@ -52,7 +52,7 @@ struct Cfg {
   static constexpr uint32_t kOCol = 256;                  // O of row tile r: kOCol + r kDim
   static constexpr int kArrive = kSplit * kBq;            // threads of a row tile
   // barriers
-  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 6, O_FREE = 8, ALL_DONE = 10, X_FULL = 11, K_FULL = 12,
+  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 8, O_FREE = 10, ALL_DONE = 12, X_FULL = 13, K_FULL = 14,
                        K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
                        V_FREE = V_FULL + kStages * kVParts, kBars = V_FREE + kStages * kVParts;
 };
@@ -112,6 +112,27 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
+// 2^y of two numbers up to 8, to 2^-17 of each (below 2^-127: zero; NaN stays NaN), without the special function unit: the 128
+// exponentials of a row and tile keep its quarter rate busy, so a quarter of them go this way.  y = n + f, n its nearest integer,
+// taken from the sum with 1.5 2^23; 2^f, |f| <= 1/2, by the quartic through it at cos((2 i + 1) pi / 10) / 2, i = 0 .. 4.
+__device__ __forceinline__ void exp2_pair(f32x2 y, float& e0, float& e1) {
+  float y0, y1;
+  f2_unpack(y, y0, y1);
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-127.0f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-127.0f));
+  y = f2_pack(y0, y1);
+  const f32x2 magic = f2_both(0x4b400000u), r = f2_add(y, magic);
+  const f32x2 n = f2_add(r, f2_both(0xcb400000u)), f = f2_fma(n, f2_both(0xbf800000u), y);
+  constexpr float c1 = 0.693121045f, c2 = 0.24022349f, c3 = 0.0559219758f, c4 = 0.00966636852f;
+  const f32x2 p = f2_fma(f, f2_fma(f, f2_fma(f, f2_fma(f, f2_pack(c4, c4), f2_pack(c3, c3)), f2_pack(c2, c2)), f2_pack(c1, c1)),
+                         f2_both(0x3f800000u));
+  float r0, r1;
+  f2_unpack(r, r0, r1);
+  f2_unpack(f2_fma(p, f2_pack(__uint_as_float((__float_as_uint(r0) << 23) + 0x3f800000u),
+                              __uint_as_float((__float_as_uint(r1) << 23) + 0x3f800000u)), 0ull),
+            e0, e1);
+}
+
 template <bool kBf16, int kDim>
 __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     attn_chunks_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -138,7 +159,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   if (threadIdx.x < 4) s_bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i)
-      mbar_init(bar(i), i == C::P_FULL || i == C::P_FULL + 1 || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive
+      mbar_init(bar(i), (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive
                         : (i >= C::K_FREE && i < C::V_FULL) || i >= C::V_FREE                                          ? kCl
                                                                                                                        : 1);
     fence_mbar_init();
@@ -272,30 +293,49 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         __syncwarp();
         return true;
       };
-      // O += P V of key tile i for row tile rt; hands V back after the last row tile
+      // O += P V of key tile i for row tile rt, in two halves as P comes; hands V back after the last row tile
       auto issue_pv = [&](int i, int rt, bool first) {
         const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
-        if (!mbar_wait_warp(bar(C::P_FULL + rt), (uint32_t)i & 1u, kWaitBudgetCycles) ||
-            (first && item > 0 && !mbar_wait_warp(bar(C::O_FREE + rt), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)))
-          return false;
+        if (first && item > 0 && !mbar_wait_warp(bar(C::O_FREE + rt), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) return false;
         const uint64_t dv = sdesc_mn(base + (uint32_t)(C::kOffV + st * C::kTile), kSub);
         const uint32_t p = tmem + 128u * (uint32_t)slot, o = tmem + kOCol + (uint32_t)(rt * kDim);
-#pragma unroll 1
-        for (int vp = 0; vp < C::kVParts; ++vp) {
-          if (rt == 0 && !mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
-            return false;
-          tc_fence_after();
-          if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < C::kVKeys / 16; ++k) {
-              const int kk = vp * (C::kVKeys / 16) + k;  // 16 keys: 8 columns of P
-              // (over the scores that were read: with two threads a row, the second half over its own)
-              tc_mma_ts(o, p + 8u * (uint32_t)kk + (C::kSplit == 2 && kk >= 4 ? 32u : 0u), dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
+        for (int half = 0; half < 2; ++half) {
+          if (!mbar_wait_warp(bar(C::P_FULL + 2 * rt + half), (uint32_t)i & 1u, kWaitBudgetCycles)) return false;
+          if constexpr (C::kVParts == 1) {
+            if (rt == 0 && half == 0 && !mbar_wait_warp(bar(C::V_FULL + st), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+              return false;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int kk = 4 * half + k;  // 16 keys: 8 columns of P
+                tc_mma_ts(o, p + 8u * (uint32_t)kk, dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
+              }
+              if (half == 1 && rt == kRt - 1) hand_back(bar(C::V_FREE + st));
+              if (half == 1) tc_commit(bar(C::PV_DONE + rt));
             }
-            if (rt == kRt - 1) hand_back(bar(C::V_FREE + st * C::kVParts + vp));
-            if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE + rt));
+            __syncwarp();
+          } else {  // two threads a row: the halves are keys 0-31 and 64-95, then the others
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const int vp = half + 2 * j;  // 32 keys
+              if (!mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+                return false;
+              tc_fence_after();
+              if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const int kk = 2 * vp + k;  // (P over the scores that were read: the second thread's over its own)
+                  tc_mma_ts(o, p + 8u * (uint32_t)kk + (kk >= 4 ? 32u : 0u), dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o,
+                            !first || kk > 0);
+                }
+                hand_back(bar(C::V_FREE + st * C::kVParts + vp));
+                if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE + rt));
+              }
+              __syncwarp();
+            }
           }
-          __syncwarp();
         }
         return true;
       };
@@ -386,28 +426,6 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               m = top;
               l *= up;
             }
-            const float ref = m == -INFINITY ? 0.0f : m;
-            const f32x2 sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
-            f32x2 sum[2] = {0ull, 0ull};
-#pragma unroll
-            for (int q = 0; q < kQ; ++q) {
-              tmem_ld32(stm + 32 * (hf * kQ + q), x);
-              if (cut) mask(hf * kQ + q);
-              uint32_t pk[16];
-#pragma unroll
-              for (int k = 0; k < 32; k += 2) {
-                float e0, e1;
-                f2_unpack(f2_fma(f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, ref2), e0, e1);
-                e0 = ex2(e0);
-                e1 = ex2(e1);
-                sum[(k >> 1) & 1] = f2_add(sum[(k >> 1) & 1], f2_pack(e0, e1));
-                pk[k >> 1] = pack2<kBf16>(e0, e1);
-              }
-              tmem_st16(stm + 64 * hf + 16 * q, pk);  // over scores that have been read
-            }
-            float s0, s1;
-            f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
-            l += s0 + s1;
             if (i > 0 && __any_sync(0xffffffffu, grown)) {
               // O is the previous products' (with two row tiles their order ahead of this S says so already)
               if (kRt == 1 && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) {
@@ -423,7 +441,6 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                 tmem_st32(otm + 32 * ch, x);
               }
             }
-            tmem_wait_st();
           }
           if (rt == 0 && hf == 0 && (j0 < lo || j0 + kBk - 1 > hi)) {
             // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero: row r
@@ -450,8 +467,40 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             }
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
           }
-          tc_fence_before();
-          mbar_arrive(bar(C::P_FULL + rt));
+          const float ref = m == -INFINITY ? 0.0f : m;
+          const f32x2 sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
+          f32x2 sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int q = 0; q < kQ; ++q) {
+            if (busy) {
+              tmem_ld32(stm + 32 * (hf * kQ + q), x);
+              if (cut) mask(hf * kQ + q);
+              uint32_t pk[16];
+#pragma unroll
+              for (int k = 0; k < 32; k += 2) {
+                const f32x2 y = f2_fma(f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, ref2);
+                float e0, e1;
+                if (k % 8 == 6) {
+                  exp2_pair(y, e0, e1);
+                } else {
+                  f2_unpack(y, e0, e1);
+                  e0 = ex2(e0);
+                  e1 = ex2(e1);
+                }
+                sum[(k >> 1) & 1] = f2_add(sum[(k >> 1) & 1], f2_pack(e0, e1));
+                pk[k >> 1] = pack2<kBf16>(e0, e1);
+              }
+              tmem_st16(stm + 64 * hf + 16 * q, pk);  // over scores that have been read
+            }
+            if ((q + 1) % (kQ / 2) == 0) {  // half of P is there
+              if (busy) tmem_wait_st();
+              tc_fence_before();
+              mbar_arrive(bar(C::P_FULL + 2 * rt + (q + 1) / (kQ / 2) - 1));
+            }
+          }
+          float s0, s1;
+          f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
+          l += s0 + s1;
         }
         // the last product; with one row tile the one before it may not be known to be complete, and a wait tells only the
         // current phase from the one before
