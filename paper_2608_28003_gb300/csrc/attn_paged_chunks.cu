@@ -112,27 +112,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
-// 2^y of two numbers up to 8, to 2^-17 of each (below 2^-127: zero; NaN stays NaN), without the special function unit: the 128
-// exponentials of a row and tile keep its quarter rate busy, so a quarter of them go this way.  y = n + f, n its nearest integer,
-// taken from the sum with 1.5 2^23; 2^f, |f| <= 1/2, by the quartic through it at cos((2 i + 1) pi / 10) / 2, i = 0 .. 4.
-__device__ __forceinline__ void exp2_pair(f32x2 y, float& e0, float& e1) {
-  float y0, y1;
-  f2_unpack(y, y0, y1);
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y0) : "f"(-127.0f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(y1) : "f"(-127.0f));
-  y = f2_pack(y0, y1);
-  const f32x2 magic = f2_both(0x4b400000u), r = f2_add(y, magic);
-  const f32x2 n = f2_add(r, f2_both(0xcb400000u)), f = f2_fma(n, f2_both(0xbf800000u), y);
-  constexpr float c1 = 0.693121045f, c2 = 0.24022349f, c3 = 0.0559219758f, c4 = 0.00966636852f;
-  const f32x2 p = f2_fma(f, f2_fma(f, f2_fma(f, f2_fma(f, f2_pack(c4, c4), f2_pack(c3, c3)), f2_pack(c2, c2)), f2_pack(c1, c1)),
-                         f2_both(0x3f800000u));
-  float r0, r1;
-  f2_unpack(r, r0, r1);
-  f2_unpack(f2_fma(p, f2_pack(__uint_as_float((__float_as_uint(r0) << 23) + 0x3f800000u),
-                              __uint_as_float((__float_as_uint(r1) << 23) + 0x3f800000u)), 0ull),
-            e0, e1);
-}
-
 template <bool kBf16, int kDim>
 __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     attn_chunks_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -480,13 +459,9 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               for (int k = 0; k < 32; k += 2) {
                 const f32x2 y = f2_fma(f2_pack(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), sc2, ref2);
                 float e0, e1;
-                if (k % 8 == 6) {
-                  exp2_pair(y, e0, e1);
-                } else {
-                  f2_unpack(y, e0, e1);
-                  e0 = ex2(e0);
-                  e1 = ex2(e1);
-                }
+                f2_unpack(y, e0, e1);
+                e0 = ex2(e0);
+                e1 = ex2(e1);
                 sum[(k >> 1) & 1] = f2_add(sum[(k >> 1) & 1], f2_pack(e0, e1));
                 pk[k >> 1] = pack2<kBf16>(e0, e1);
               }
