@@ -23,10 +23,11 @@ constexpr int kMaxPieces = 192;  // of an item: no more than CTAs
 template <int kDim>
 struct Cfg {
   static constexpr int kWarps = kDim == 256 ? 4 : 8;          // consumers
-  static constexpr int kBk = 16 * kWarps, kBkShift = kDim == 256 ? 6 : 7;
+  static constexpr int kBlocks = kDim == 64 ? 2 : 1;          // of 16 keys, that a warp has of a tile
+  static constexpr int kBk = 16 * kBlocks * kWarps, kBkShift = kDim == 256 ? 6 : kDim == 128 ? 7 : 8;
   static constexpr int kChunks = kDim / 64;                   // 128-byte columns of a tile
   static constexpr int kSub = kBk * 128, kTile = kChunks * kSub, kStage = 2 * kTile;
-  static constexpr int kStages = 196608 / kStage;             // 3, 3, 6
+  static constexpr int kStages = 196608 / kStage;             // 3
   static constexpr int kJoin = kWarps * 8 * kDim * 4;         // 8 rows' outputs of every warp
   static constexpr int kPer = kDim / 8 / kWarps;              // groups of 8 dims that a warp joins
   static constexpr int kSmem = kStages * kStage + kJoin + 1024;
@@ -240,43 +241,56 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     for (int i = 0; i < kDim / 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
 
     for (int i = 0; i < w.cnt; ++i, ++g) {
-      const int st = g % C::kStages, j0 = ((w.first + w.k0 + i) << C::kBkShift) + 16 * warp;
+      constexpr int kBlocks = C::kBlocks;
+      const int st = g % C::kStages, j0 = ((w.first + w.k0 + i) << C::kBkShift) + 16 * kBlocks * warp;
       if (ok && !mbar_wait_warp(full(st), (uint32_t)(g / C::kStages) & 1u, kWaitBudgetCycles)) ok = false;
       if (!ok) continue;
-      if (((held[st] >> warp) & 1u) && j0 <= hi && j0 + 15 >= lo) {
+      const uint32_t there = held[st] >> (kBlocks * warp) & ((1u << kBlocks) - 1u);
+      if (there != 0 && j0 <= hi && j0 + 16 * kBlocks - 1 >= lo) {
         const uint32_t kt = ring + (uint32_t)(st * C::kStage), vt = kt + C::kTile;
-        float s[2][2][4] = {};  // [keys 0-7, 8-15][even, odd k steps]
+        float s[kBlocks][2][4];  // [block][keys 0-7, 8-15]
         {
-          const int row = 16 * warp + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
+          float z[kBlocks][2][2][4] = {};  // [even, odd k steps]
+          const int row = 16 * kBlocks * warp + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
 #pragma unroll
           for (int k = 0; k < kDim / 16; ++k) {
-            uint32_t kb[4];
             const int col = 2 * (k & 3) + half;
-            ldsm4(kt + (uint32_t)((k >> 2) * C::kSub + row * 128 + ((col ^ (row & 7)) << 4)), kb);
             const uint4 q4 = qf[32 * k];
             const uint32_t qa[4] = {q4.x, q4.y, q4.z, q4.w};
-            mma16<kBf16>(s[0][k & 1], qa, kb[0], kb[1]);
-            mma16<kBf16>(s[1][k & 1], qa, kb[2], kb[3]);
-          }
-        }
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][0][e] += s[n][1][e];
-        if (j0 < all_lo || j0 + 15 > all_hi) {
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = j0 + 8 * n + 2 * quad + (e & 1);
-              if (j > pos[e >> 1] || j < from[e >> 1]) s[n][0][e] = -INFINITY;
+            for (int u = 0; u < kBlocks; ++u) {
+              uint32_t kb[4];
+              ldsm4(kt + (uint32_t)((k >> 2) * C::kSub + (row + 16 * u) * 128 + ((col ^ (row & 7)) << 4)), kb);
+              mma16<kBf16>(z[u][k & 1][0], qa, kb[0], kb[1]);
+              mma16<kBf16>(z[u][k & 1][1], qa, kb[2], kb[3]);
             }
+          }
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[u][n][e] = z[u][0][n][e] + z[u][1][n][e];
+        }
+        if (j0 < all_lo || j0 + 16 * kBlocks - 1 > all_hi || there != (1u << kBlocks) - 1u) {
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int j = j0 + 16 * u + 8 * n + 2 * quad + (e & 1);
+                if (j > pos[e >> 1] || j < from[e >> 1] || !((there >> u) & 1u)) s[u][n][e] = -INFINITY;
+              }
         }
         float up[2], ref[2];
         bool grown = false;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          float top = fmaxf(fmaxf(s[0][0][2 * r], s[0][0][2 * r + 1]), fmaxf(s[1][0][2 * r], s[1][0][2 * r + 1]));
+          float top = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u)
+            top = fmaxf(top, fmaxf(fmaxf(s[u][0][2 * r], s[u][0][2 * r + 1]), fmaxf(s[u][1][2 * r], s[u][1][2 * r + 1])));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * sc;
           up[r] = 1.0f;
@@ -298,39 +312,40 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             acc[d][3] *= up[1];
           }
         }
-        uint32_t p[4];  // the weights as the second product's left operand: rows r0 / r0 + 8, keys 0-7 then 8-15
+        // the weights as the second product's left operand: rows r0 / r0 + 8, keys 0-7 then 8-15
+        uint32_t p[kBlocks][4];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            p[2 * n + r] = pack2<kBf16>(ex2(fmaf(s[n][0][2 * r], sc, -ref[r])), ex2(fmaf(s[n][0][2 * r + 1], sc, -ref[r])));
-            const float2 as_used = unpack2<kBf16>(p[2 * n + r]);
-            l[r] += as_used.x + as_used.y;
-          }
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              p[u][2 * n + r] = pack2<kBf16>(ex2(fmaf(s[u][n][2 * r], sc, -ref[r])), ex2(fmaf(s[u][n][2 * r + 1], sc, -ref[r])));
+              const float2 as_used = unpack2<kBf16>(p[u][2 * n + r]);
+              l[r] += as_used.x + as_used.y;
+            }
         // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero
-        uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
-        const bool cut = j0 < lo || j0 + 15 > hi;
-        if (cut) {
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const int j = j0 + 8 * n + 2 * quad;
-            keep[n] = (j >= lo && j <= hi ? 0xffffu : 0u) | (j + 1 >= lo && j + 1 <= hi ? 0xffff0000u : 0u);
-          }
-        }
-        const int key = 16 * warp + (((lane >> 3) & 1) << 3) + (lane & 7);
+        const bool cut = j0 < lo || j0 + 16 * kBlocks - 1 > hi;
+        const int key = 16 * kBlocks * warp + (((lane >> 3) & 1) << 3) + (lane & 7);
 #pragma unroll
         for (int d = 0; d < kDim / 16; ++d) {
-          uint32_t vb[4];
           const int col = 2 * (d & 3) + (lane >> 4);
-          ldsm4t(vt + (uint32_t)((d >> 2) * C::kSub + key * 128 + ((col ^ (key & 7)) << 4)), vb);
-          if (cut) {
-            vb[0] &= keep[0];
-            vb[1] &= keep[1];
-            vb[2] &= keep[0];
-            vb[3] &= keep[1];
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u) {
+            uint32_t vb[4];
+            ldsm4t(vt + (uint32_t)((d >> 2) * C::kSub + (key + 16 * u) * 128 + ((col ^ (key & 7)) << 4)), vb);
+            if (cut) {
+#pragma unroll
+              for (int n = 0; n < 2; ++n) {
+                const int j = j0 + 16 * u + 8 * n + 2 * quad;
+                const uint32_t keep = (j >= lo && j <= hi ? 0xffffu : 0u) | (j + 1 >= lo && j + 1 <= hi ? 0xffff0000u : 0u);
+                vb[n] &= keep;
+                vb[2 + n] &= keep;
+              }
+            }
+            mma16<kBf16>(acc[2 * d], p[u], vb[0], vb[1]);
+            mma16<kBf16>(acc[2 * d + 1], p[u], vb[2], vb[3]);
           }
-          mma16<kBf16>(acc[2 * d], p, vb[0], vb[1]);
-          mma16<kBf16>(acc[2 * d + 1], p, vb[2], vb[3]);
         }
       }
       __syncwarp();
