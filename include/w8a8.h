@@ -508,7 +508,8 @@ typedef struct {
  * slot p % page_size of page pages[s, p / page_size].  All three arrays are DEVICE memory and may be written by
  * earlier work on the stream; the host needs bounds only.  Checked on the device: rows outside
  * [row_start[0], row_start[n_seqs]) belong to no sequence, and their outputs are left as they were; a page id outside
- * [0, n_pages) (or past max_pages) holds no keys and takes none; a row at a negative position has no keys. */
+ * [0, n_pages) holds no keys and takes none; a row at a negative position has no keys; kv_len counts from 0 to max_pages
+ * page_size at most. */
 typedef struct {
   int32_t n_seqs, n_rows;
   int32_t max_new;   /* the most rows any sequence has, at least 1 (a longer one costs time only) */

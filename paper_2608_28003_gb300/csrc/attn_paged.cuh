@@ -307,7 +307,8 @@ __device__ __forceinline__ Pieces pieces_of(const Walk& w, const LineStart& ls) 
 // ------------------------------------------------------------------------------- one row exactly
 // One row's attention by one warp, key by key in the order of the formula: NaN and infinities travel as they do
 // in it, and nothing outside the row's range is read.  The kernels run it for rows whose result is not finite (a value
-// that only other rows of the tile may see can make it so).  Lane l scores key j0 + l, then holds dims l, l + 32, ...
+// that only other rows of the tile may see can make it so, or sums of weights times values beyond fp32's range: here the
+// output so far is kept as an average, which stays within the values).  Lane l scores key j0 + l, then holds dims l, l + 32, ...
 template <bool kBf16, int kDim>
 __device__ __noinline__ void attend_row(const PagedCache& c, const PagedBatch& b, const AttnCall& a, int s, int pos,
                                         int64_t row, int head, int lane) {
@@ -342,10 +343,13 @@ __device__ __noinline__ void attend_row(const PagedCache& c, const PagedBatch& b
     const float m_new = fmaxf(m, warp_max_f(sc));
     const float ref = m_new == -INFINITY ? 0.0f : m_new;
     const float corr = m == -INFINITY ? 0.0f : expf(m - ref);
-    const float p = at >= 0 ? expf(sc - ref) : 0.0f;
-    l = l * corr + warp_sum_f(p);
+    float p = at >= 0 ? expf(sc - ref) : 0.0f;
+    const float before = l * corr;
+    l = before + warp_sum_f(p);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // nothing but scores of -inf so far
+    p *= inv;
 #pragma unroll
-    for (int i = 0; i < kDim / 32; ++i) acc[i] *= corr;
+    for (int i = 0; i < kDim / 32; ++i) acc[i] *= before * inv;
     for (int u = 0; u < 32; ++u) {
       if (!((there >> u) & 1u)) continue;
       const float pu = __shfl_sync(0xffffffffu, p, u);
@@ -360,7 +364,7 @@ __device__ __noinline__ void attend_row(const PagedCache& c, const PagedBatch& b
   }
   uint16_t* o = a.o + row * a.o_row + head * a.o_head;
 #pragma unroll
-  for (int i = 0; i < kDim / 32; ++i) o[lane + 32 * i] = (uint16_t)pack2<kBf16>(any ? acc[i] / l : 0.0f, 0.0f);
+  for (int i = 0; i < kDim / 32; ++i) o[lane + 32 * i] = (uint16_t)pack2<kBf16>(!any ? 0.0f : l == 0.0f ? NAN : acc[i], 0.0f);
 }
 
 }  // namespace w8a8

@@ -536,3 +536,71 @@ def test_calls_of_nothing(B):
     q = torch.ones(3, 4, 256, device="cuda", dtype=torch.bfloat16)
     assert torch.equal(B.paged_attention(cache, none, q, out=q.clone()), q)
     assert B.sample(torch.empty(0, 8, device="cuda"), torch.empty(0, device="cuda")).shape == (0,)
+
+
+# ------------------------------------------------------------------- calls at the edge of what is allowed
+@pytest.mark.parametrize("new,n_q,n_kv,dim", [([1, 2, 1], 8, 2, 64), ([1, 1, 1], 4, 1, 256), ([40, 3, 130], 8, 2, 128),
+                                              ([20, 90, 1], 4, 1, 256)])
+def test_attention_pages_in_common(B, new, n_q, n_kv, dim):
+    """Sequences that share their first pages, and one that holds the same page twice."""
+    keys = [n + 150 for n in new]
+    b = make_batch(new, keys, 32, n_kv, dim, torch.bfloat16, 12)
+    b["pages"][1, :3] = b["pages"][0, :3]
+    b["pages"][2, 1] = b["pages"][2, 0]
+    cache, batch = objects(B, b)
+    q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 1.5).bfloat16()
+    attn_check(B.paged_attention(cache, batch, q), q, b, dim ** -0.5, 0)
+
+
+@pytest.mark.parametrize("new,n_q,n_kv,dim", [([1, 2], 8, 2, 64), ([1, 1], 4, 1, 256), ([40, 130], 8, 2, 128), ([50, 90], 4, 1, 256)])
+def test_attention_values_near_the_types_end(B, new, n_q, n_kv, dim):
+    """Values of 2^126 meet weights of up to 2^8: sums on the way overflow fp32, the result does not."""
+    b = make_batch(new, [n + 200 for n in new], 16, n_kv, dim, torch.bfloat16, 13)
+    b["v"].copy_(torch.where(b["v"] > 0, 2.0 ** 126, 2.0 ** 125))
+    b["k"].copy_(b["k"] * torch.linspace(0.1, 3, b["k"].shape[1], device="cuda")[None, :, None, None])  # the maximum grows on the way
+    cache, batch = objects(B, b)
+    q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 1.5).bfloat16()
+    got = B.paged_attention(cache, batch, q)
+    assert torch.isfinite(got).all()
+    attn_check(got, q, b, dim ** -0.5, 0)
+
+
+@pytest.mark.parametrize("new,n_q,dim", [([1, 1, 2, 1], 4, 256), ([30, 1, 50, 2], 4, 128)])
+def test_lengths_beyond_the_pages(B, new, n_q, dim):
+    """kv_len past the page table's columns counts as all of them; a negative one as none."""
+    b = make_batch(new, [60, 64, 64, 30], 16, 1, dim, torch.bfloat16, 14)
+    b["kv_len"] = np.array([60, 2 ** 31 - 1, 65, -2 ** 31], np.int32)
+    cache, batch = objects(B, b)
+    q = torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)).bfloat16()
+    got = B.paged_attention(cache, batch, q)
+    attn_check(got, q, b, dim ** -0.5, 0)
+    assert (got[int(b["row_start"][3]):] == 0).all()
+    x = torch.randn(b["n_rows"], 1, dim, device="cuda", generator=_gen(9)).bfloat16()
+    B.rope_append(B.rope_table(B.RopeConfig(dim)), cache, batch, q, x, x)
+    assert torch.equal(b["v"][int(b["pages"][1, 3]), 15, 0], x[int(b["row_start"][2]) - 1, 0])
+
+
+@pytest.mark.parametrize("n_q,n_kv,dim,most", [(4, 2, 64, 1), (4, 1, 256, 40), (8, 2, 128, 20)])
+def test_attention_many_sequences(B, n_q, n_kv, dim, most):
+    """More sequences than a block has threads, most of them without rows."""
+    rng = random.Random(3)
+    new = [rng.choice([0, 0, 0, 1, 1, most]) if i else 1 for i in range(1500)]
+    keys = [n + rng.randint(0, 40) for n in new]
+    b = make_batch(new, keys, 16, n_kv, dim, torch.float16, 15)
+    cache, batch = objects(B, b)
+    q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 1.5).half()
+    rows = set(rng.sample(range(b["n_rows"]), 200)) | {0, b["n_rows"] - 1}
+    got = B.paged_attention(cache, batch, q)
+    attn_check(got, q, b, dim ** -0.5, 0, rows)
+    low = dict(b, max_new=1)  # the hint too small: slower, the same
+    cache, batch = objects(B, low)
+    attn_check(B.paged_attention(cache, batch, q), q, b, dim ** -0.5, 0, rows)
+
+
+def test_sample_widest(B):
+    """The largest vocabulary, rows of the type's smallest alignment."""
+    V = 1048576
+    for dt, unit in ((torch.float32, 4), (torch.bfloat16, 8)):
+        x = torch.empty(2, V + unit, device="cuda", dtype=dt)
+        x.copy_((torch.randn(2, V + unit, device="cuda", generator=_gen(7)) * 2).to(dt))
+        sample_check(B, x[:, :V], torch.tensor([0.3, 0.999], device="cuda"), temperature=[0.8], top_k=[200, 3], top_p=[0.9])
