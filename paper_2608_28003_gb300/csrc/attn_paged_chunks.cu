@@ -51,7 +51,9 @@ struct Cfg {
   static constexpr int kPart = kRows * kDim + 2 * kRows;  // floats of a partial: [dim / 4][rows][4], m, l
   static constexpr uint32_t kOCol = 256;                  // O of row tile r: kOCol + r kDim
   static constexpr int kArrive = kSplit * kBq;            // threads of a row tile
-  // barriers
+  // barriers.  A wait tells a phase from the one before it only, so none may complete twice before a waiter looks: P_FULL counts by
+  // slot and half (with one row tile, whose softmax may be a tile ahead of the products; by row tile and half with two, the same);
+  // PV_DONE by row tile, its second one with one row tile for an item's last product
   static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 8, O_FREE = 10, ALL_DONE = 12, X_FULL = 13, K_FULL = 14,
                        K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
                        V_FREE = V_FULL + kStages * kVParts, kBars = V_FREE + kStages * kVParts;
@@ -273,14 +275,14 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         return true;
       };
       // O += P V of key tile i for row tile rt, in two halves as P comes; hands V back after the last row tile
-      auto issue_pv = [&](int i, int rt, bool first) {
+      auto issue_pv = [&](int i, int rt, bool first, bool last) {
         const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
         if (first && item > 0 && !mbar_wait_warp(bar(C::O_FREE + rt), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) return false;
         const uint64_t dv = sdesc_mn(base + (uint32_t)(C::kOffV + st * C::kTile), kSub);
         const uint32_t p = tmem + 128u * (uint32_t)slot, o = tmem + kOCol + (uint32_t)(rt * kDim);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          if (!mbar_wait_warp(bar(C::P_FULL + 2 * rt + half), (uint32_t)i & 1u, kWaitBudgetCycles)) return false;
+          if (!mbar_wait_warp(bar(C::P_FULL + 2 * slot + half), (uint32_t)(kRt == 2 ? i : i >> 1) & 1u, kWaitBudgetCycles)) return false;
           if constexpr (C::kVParts == 1) {
             if (rt == 0 && half == 0 && !mbar_wait_warp(bar(C::V_FULL + st), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
               return false;
@@ -310,7 +312,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                             !first || kk > 0);
                 }
                 hand_back(bar(C::V_FREE + st * C::kVParts + vp));
-                if (vp == C::kVParts - 1) tc_commit(bar(C::PV_DONE + rt));
+                if (vp == C::kVParts - 1) {
+                  tc_commit(bar(C::PV_DONE));
+                  if (last) tc_commit(bar(C::PV_DONE + 1));
+                }
               }
               __syncwarp();
             }
@@ -325,9 +330,9 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         for (int i = 0; ok && i < w.cnt; ++i, ++g) {
           const bool more = i + 1 < w.cnt, last = i + 2 == w.cnt;
           if constexpr (kRt == 1) {
-            ok = (!more || issue_s(g + 1, 0, last)) && issue_pv(g, 0, i == 0);
+            ok = (!more || issue_s(g + 1, 0, last)) && issue_pv(g, 0, i == 0, !more);
           } else {  // a slot's next S follows the product that has read its P
-            ok = issue_pv(g, 0, i == 0) && (!more || issue_s(g + 1, 0, last)) && issue_pv(g, 1, i == 0) &&
+            ok = issue_pv(g, 0, i == 0, !more) && (!more || issue_s(g + 1, 0, last)) && issue_pv(g, 1, i == 0, !more) &&
                  (!more || issue_s(g + 1, 1, last));
           }
         }
@@ -425,7 +430,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero: row r
             // of the tile, once its copies have landed
             const int st = g % C::kStages;
-            bool landed = true;
+            // with one row tile and stage, the values of the tile before may not have landed yet: its product has them
+            bool landed = kRt == 2 || i == 0 || mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles);
 #pragma unroll
             for (int vp = 0; vp < C::kVParts; ++vp)
               landed = landed && mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(g / C::kStages) & 1u,
@@ -470,17 +476,17 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             if ((q + 1) % (kQ / 2) == 0) {  // half of P is there
               if (busy) tmem_wait_st();
               tc_fence_before();
-              mbar_arrive(bar(C::P_FULL + 2 * rt + (q + 1) / (kQ / 2) - 1));
+              mbar_arrive(bar(C::P_FULL + 2 * slot + (q + 1) / (kQ / 2) - 1));
             }
           }
           float s0, s1;
           f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
           l += s0 + s1;
         }
-        // the last product; with one row tile the one before it may not be known to be complete, and a wait tells only the
-        // current phase from the one before
-        if (kRt == 1 && ok && w.cnt > 1 && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 2) & 1u, kWaitBudgetCycles)) ok = false;
-        if (ok && !mbar_wait_warp(bar(C::PV_DONE + rt), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) ok = false;
+        // the item's last product
+        if (ok && !mbar_wait_warp(bar(kRt == 2 ? C::PV_DONE + rt : C::PV_DONE + 1), (uint32_t)(kRt == 2 ? g - 1 : item) & 1u,
+                                  kWaitBudgetCycles))
+          ok = false;
         if (!ok && lane == 0) atomicOr(err, DEVERR_CONSUMER_WAIT);
         __syncwarp();
         tc_fence_after();

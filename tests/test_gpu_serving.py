@@ -604,3 +604,19 @@ def test_sample_widest(B):
         x = torch.empty(2, V + unit, device="cuda", dtype=dt)
         x.copy_((torch.randn(2, V + unit, device="cuda", generator=_gen(7)) * 2).to(dt))
         sample_check(B, x[:, :V], torch.tensor([0.3, 0.999], device="cuda"), temperature=[0.8], top_k=[200, 3], top_p=[0.9])
+
+
+@pytest.mark.parametrize("n_q,n_kv,dim,seqs,new,ctx,window", [
+    (4, 1, 256, 32, 8, 4000, 1024), (4, 1, 256, 64, 8, 4000, 0), (16, 1, 256, 20, 2, 3000, 0), (8, 2, 256, 30, 25, 2500, 700),
+    (28, 4, 128, 30, 3, 4000, 0), (24, 8, 64, 20, 10, 4000, 0), (4, 1, 256, 3, 70, 30000, 0)])
+def test_attention_few_rows_over_many_keys(B, n_q, n_kv, dim, seqs, new, ctx, window):
+    """Chunks that leave most of a row tile empty, or one of an item's two: its warps do nothing and are far ahead."""
+    rng = random.Random(seqs + dim)
+    b = make_batch([new] * seqs, [rng.randint(ctx // 2, ctx) for _ in range(seqs)], 64, n_kv, dim, torch.bfloat16, 16)
+    cache, batch = objects(B, b)
+    q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 1.5).bfloat16()
+    got = B.paged_attention(cache, batch, q, window=window)
+    rows = set(rng.sample(range(b["n_rows"]), 24)) | {0, b["n_rows"] - 1}
+    attn_check(got, q, b, dim ** -0.5, window, rows)
+    for _ in range(10):
+        assert torch.equal(B.paged_attention(cache, batch, q, window=window), got)
