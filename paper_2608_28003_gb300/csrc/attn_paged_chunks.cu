@@ -1,24 +1,34 @@
-// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows, tokens times
-// the query heads of a group, in two tiles of 128 rows with one row per TMEM lane.  At head dims 64 and 128 one CTA has both tiles,
-// at 256 (whose output fills tensor memory) each CTA of a pair has one, and either copies half of every K and V part to both:
-// read from L2 once for 256 rows either way (with 128, L2 bounded the kernel: 23 bytes a clock and SM).
+// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows, tokens
+// times the query heads of a group, in two tiles of 128 rows with one row per TMEM lane.  At head dims 64 and 128 one CTA
+// has both tiles, at 256 (whose output fills tensor memory) each CTA of a pair has one, and either copies half of every K
+// and V part to both: read from L2 once for 256 rows either way (with 128, L2 bounded the kernel: 23 bytes a clock and SM).
 //
 // A worker (CTA or pair), one CTA per SM, walks its stretch of the line of key tiles (attn_paged.cuh), 128 keys at a time:
-//  * two warps copy by TMA, page by page: one an item's queries and the K tiles, one the V tiles (either as its tiles are handed
-//    back, which one warp's order would tie together);
-//  * the issue warp allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) for each row tile, and O += P V
-//    (128 x dim x 128), P read from tensor memory.  V lies as the cache has it, keys by dims, so it is the product's
-//    MN-major operand and needs no transposition;
-//  * eight softmax warps, four for each row tile (thread = row), or two threads a row, each with half of the keys and of the
-//    dims, where there is one: they take the row's maximum over the scores, then p = 2^(s c - m) with
-//    c = scale log2 e in chunks of 32 scores, and write P over the scores they have read, where the second product finds it.  m
-//    moves when the maximum grew by more than 2^8 only: O is then rescaled in tensor memory.
-// Tensor memory holds 512 columns: two slots of 128 for S and P, and O of 2 x 64, 2 x 128 or 256.  With two row tiles each has
-// a slot of its own, and the tensor cores work for one while the other's softmax runs.  At head dim 256 the slots alternate: S of the next key tile is
-// issued before P of this one is awaited; one K and one V tile fill shared memory beside the queries, so tiles are copied and
-// handed back in quarters (K by 64 dims, V by 32 keys), and the copies of the next tile follow the products through this one.
+//  * two warps copy by TMA, page by page: one an item's queries and the K tiles, one the V tiles (either as its tiles are
+//    handed back, which one warp's order would tie together);
+//  * the issue warp allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) for each row tile, and
+//    O += P V (128 x dim x 128), P read from tensor memory.  V lies as the cache has it, keys by dims, so it is the
+//    product's MN-major operand and needs no transposition;
+//  * eight softmax warps, four for each row tile (thread = row), or two threads a row, each with half of the keys and of
+//    the dims, where there is one: they take the row's maximum over the scores, rescale O in tensor memory if it grew by
+//    more than 2^8 (m moves only then), then p = 2^(s c - m) with c = scale log2 e in chunks of 32 scores, and write P over
+//    the scores they have read, where the second product finds it.  P is handed over in halves: the product of the first
+//    half runs while the second is computed.
+// Tensor memory holds 512 columns: two slots of 128 for S and P, and O of 2 x 64, 2 x 128 or 256.  With two row tiles each
+// has a slot of its own, and the tensor cores work for one while the other's softmax runs.  At head dim 256 the slots
+// alternate: S of the next key tile is issued before P of this one is awaited; one K and one V tile fill shared memory
+// beside the queries, so tiles are copied and handed back in quarters (K by 64 dims, V by 32 keys), and the copies of the
+// next tile follow the products through this one.
 // The products of one thread run in the order of their issue, which is what frees a slot: S of a slot is issued after
 // the product that read the slot's P.
+//
+// What bounds it.  At head dims 64 and 128 the chain S -> maximum -> exponentials -> P V of a row tile, about 3100 cycles a
+// tile of keys where the products take 2048: four chunks of 1001 tokens behind up to 9000 keys, 28 heads over 4 of 128, take
+// 178 us (690 TFLOP/s, 0.37 of the measured rate; 217 with P in one piece after the rescaling).  Tried and slower: a part of
+// the exponentials as a polynomial (an eighth 180 us, a quarter 184, half 207: issue slots, not the special function unit,
+// are short), two threads a row for both row tiles (211: 96 registers), scores loaded ahead or kept in registers (189 and
+// 233: spills).  A whole prompt of 2048 tokens at head dim 256 takes 27.9 us, of which the lookup of the work is 2, the
+// first tile's way 3, four key tiles 7, and the partials of cut items and their join 8.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
 #include "attn_paged.cuh"
 #include "ops.cuh"
@@ -43,7 +53,7 @@ struct Cfg {
   static constexpr int kTile = kChunks * kSub;
   static constexpr int kOffK = kRt * kTile, kOffV = kOffK + kStages * kTile;
   static constexpr int kSmem = kOffV + kStages * kTile + 1024;
-  static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys, or whole
+  static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys
   static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
   static constexpr int kSplit = 2 / kRt;           // threads a row
   static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kLoadV = kSoft + 2, kThreads = 32 * (kSoft + 3);
@@ -54,8 +64,8 @@ struct Cfg {
   // barriers.  A wait tells a phase from the one before it only, so none may complete twice before a waiter looks: P_FULL counts by
   // slot and half (with one row tile, whose softmax may be a tile ahead of the products; by row tile and half with two, the same);
   // PV_DONE by row tile, its second one with one row tile for an item's last product
-  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 8, O_FREE = 10, ALL_DONE = 12, X_FULL = 13, K_FULL = 14,
-                       K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
+  static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 8, O_FREE = 10, ALL_DONE = 12, X_FULL = 13,
+                       K_FULL = 14, K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
                        V_FREE = V_FULL + kStages * kVParts, kBars = V_FREE + kStages * kVParts;
 };
 
@@ -160,7 +170,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   const uint32_t tmem = tmem_slot;
   pdl_wait();
   pdl_trigger();
-  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, worker, (int)gridDim.x / kCl, &ls, scan);  // syncs the block
+  // (syncs the block)
+  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, worker, (int)gridDim.x / kCl, &ls, scan);
   bool ok = true;
 
   if (ls.begin < ls.end) {
@@ -282,7 +293,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         const uint32_t p = tmem + 128u * (uint32_t)slot, o = tmem + kOCol + (uint32_t)(rt * kDim);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          if (!mbar_wait_warp(bar(C::P_FULL + 2 * slot + half), (uint32_t)(kRt == 2 ? i : i >> 1) & 1u, kWaitBudgetCycles)) return false;
+          if (!mbar_wait_warp(bar(C::P_FULL + 2 * slot + half), (uint32_t)(kRt == 2 ? i : i >> 1) & 1u, kWaitBudgetCycles))
+            return false;
           if constexpr (C::kVParts == 1) {
             if (rt == 0 && half == 0 && !mbar_wait_warp(bar(C::V_FULL + st), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
               return false;

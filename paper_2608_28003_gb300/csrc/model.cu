@@ -504,7 +504,7 @@ extern "C" w8a8_status w8a8_model_create(const w8a8_model_cfg* cfg, const w8a8_l
   }
   m->attn_ws_bytes = aws;
   W8A8_MTRY(dalloc(m, reinterpret_cast<char**>(&m->attn_ws), aws));
-  W8A8_MTRY(dalloc(m, reinterpret_cast<char**>(&m->paged_ws), paged_attention_ws(c.head_dim, c.n_q, c.n_kv, d.sms)));
+  W8A8_MTRY(dalloc(m, reinterpret_cast<char**>(&m->paged_ws), paged_attention_ws(c.head_dim, d.sms)));
   W8A8_MTRY(dalloc(m, &m->pcodes, (size_t)c.max_tokens * H));
   W8A8_MTRY(dalloc(m, &m->psx, (size_t)c.max_tokens + 4));
   W8A8_MTRY(dalloc(m, &m->psum, (size_t)c.max_tokens + 4));

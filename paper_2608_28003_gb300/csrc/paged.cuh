@@ -38,7 +38,7 @@ struct AttnCall {
 };
 w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st);
-size_t paged_attention_ws(int dim, int n_q, int n_kv, int sms);
+size_t paged_attention_ws(int dim, int sms);
 
 // Rows and keys of sequence s, held within the call's bounds whatever the arrays say.
 struct SeqShape {

@@ -15,6 +15,11 @@
 // sorted by one CTA; more (flat or tied rows) are divided by the order of their floats until one value is left, whose
 // equals are cut by index.  The last pass sums the kept weights and finds the token in index order.  Slices of up to 64 KB
 // (few rows) stay in shared memory between the passes; longer ones are read again from L2.
+//
+// Measured, 262144 logits a row: 1 row with every filter 22 us (floor 0.15: eight cluster barriers and the steps between them,
+// each a latency chain; 36 with 8 CTAs instead of 16, 27.4 with the slices read again from L2); 64 rows with a nucleus of 0.9
+// 134 us (floor 9.9): 127 instructions a logit of each warp, of which the weights' two passes are 94, at half of the issue
+// rate.  The next logits loaded ahead of a step's work: 138 (spills).
 #include <cmath>
 #include <type_traits>
 
