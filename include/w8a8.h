@@ -532,7 +532,7 @@ w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache
 
 /* Attention of every row over its sequence's cached keys (its own included: append first):
  *   o = sum_j softmax_j(scale q . k_j) v_j over the keys j of its sequence with p - window < j <= p (window 0: all
- *   j <= p), p the row's position; query head h reads key/value head h / (n_q / n_kv).
+ *   j <= p), p the row's position; query head h reads key/value head h / (n_q / n_kv); scale > 0.
  * A row without keys gets zeros.  A key outside a row's range, and slots that hold none, never reach it, whatever
  * their values; keys within it propagate NaN and infinities as the formula does.  Scores, softmax and sums
  * in fp32; a weight (at most 2^8) is rounded once to the type before it meets v; the output is rounded once.

@@ -47,7 +47,7 @@ namespace {
 constexpr int kTileCounterSlots = 8192;                      // uint32 slots at workspace offset 0
 constexpr size_t kGridCounterOffset = 8192 * 4;              // one uint32
 constexpr size_t kTopKeysOffset = 40960;                     // uint64 keys
-constexpr int kMaxTopKeys = (W8A8_WS_RESERVED - 40960) / 8;  // 3072
+constexpr int kMaxTopKeys = (W8A8_WS_RESERVED - 40960) / 8;
 constexpr int kConsumerWarps = 8;
 constexpr int kThreads = (kConsumerWarps + 1) * 32;
 constexpr int kSmemLimit = 227 * 1024;   // shared memory per SM available to CTAs
