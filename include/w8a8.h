@@ -545,7 +545,8 @@ w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged
                                  int64_t o_row, int64_t o_head, void* workspace, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------ sampling
- * One token a row from logits [M, V] (fp32, bf16 or fp16; row stride in elements) and one uniform number u in
+ * One token a row from logits [M, V] (fp32, bf16 or fp16; any row stride, in elements; V up to
+ * W8A8_MAX_SAMPLE_VOCAB, 3 less where a row does not begin at a multiple of four elements) and one uniform number u in
  * [0, 1) a row.  Weights w_i = e^((l_i - max l) / temperature), in multiples of 2^-43 and accurate to 2^-27 of each;
  * NaN and -inf weigh nothing.  Tokens in descending order of logits, the lower index first among equals:
  *   top_k  keeps the first top_k (all where top_k <= 0);

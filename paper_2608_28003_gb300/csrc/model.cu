@@ -745,8 +745,8 @@ extern "C" w8a8_status w8a8_decoder_step_paged(w8a8_model* m, const int32_t* tok
   if (u) {
     W8A8_CHECK_ARG(logits != nullptr || ps.batch.n_seqs <= c.max_batch, W8A8_ERR_SHAPE,
                    "%s: sampling for more than max_batch %d sequences needs logits", who, c.max_batch);
-    W8A8_CHECK_ARG(c.vocab <= W8A8_MAX_SAMPLE_VOCAB && c.vocab % 4 == 0, W8A8_ERR_SHAPE,
-                   "%s: sampling needs a vocabulary of a multiple of 4, up to %d", who, W8A8_MAX_SAMPLE_VOCAB);
+    W8A8_CHECK_ARG(c.vocab <= W8A8_MAX_SAMPLE_VOCAB - (c.vocab % 4 ? 3 : 0), W8A8_ERR_SHAPE,
+                   "%s: sampling takes vocabularies up to %d (3 less where not a multiple of 4)", who, W8A8_MAX_SAMPLE_VOCAB);
     const w8a8_sampling none{};
     const w8a8_sampling& sp = sampling ? *sampling : none;
     const void* words[] = {sp.temperature, sp.top_k, sp.top_p, sp.min_p, u, probs};

@@ -206,13 +206,14 @@ struct Row {
   f32x2 nz;
   bool infinite;       // the row's maximum is infinite: it is read as 0, all else as -inf
   int buf;
+  int lo;              // elements of the first four that lie before the row (see sample_kernel)
 
   static constexpr int kElem = kType == W8A8_TYPE_F32 ? 4 : 2;
-  // logits i .. i + 3 of the slice, -inf behind the row's end (no comparison below takes a NaN, and -0 is equal to 0 in all of
+  // logits i .. i + 3 of the slice, -inf before the row and behind its end (no comparison below takes a NaN, and -0 is equal to 0 in all of
   // them)
   __device__ __forceinline__ float4 raw4(int i) const {
     float f[4];
-    if (i + 4 <= n) {
+    if (i >= lo && i + 4 <= n) {
       if constexpr (kType == W8A8_TYPE_F32) {
         const float4 v = __ldg(reinterpret_cast<const float4*>(src) + i / 4);
         f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
@@ -225,7 +226,7 @@ struct Row {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         f[e] = -INFINITY;
-        if (i + e < n) {
+        if (i + e >= lo && i + e < n) {
           if constexpr (kType == W8A8_TYPE_F32)
             f[e] = __ldg(reinterpret_cast<const float*>(src) + i + e);
           else
@@ -681,8 +682,13 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
   pdl_wait();
   pdl_trigger();
   const uint32_t base = rank * (uint32_t)slice;
-  Row<kType, kHeld> rw{&sh, static_cast<const char*>(logits) + ((int64_t)row * row_stride + base) * Row<kType, kHeld>::kElem, xs,
-                       slice, min(slice, max(0, V - (int)base)), base, rank, size, {}, f2_neg_zero(), false, 0};
+  // A row may begin anywhere: its logits are counted from the four-element boundary at or before it, `skew` elements on (whose
+  // values are not read), so that all loads but those at the ends are of four.
+  constexpr int kElem = Row<kType, kHeld>::kElem;
+  const char* from = static_cast<const char*>(logits) + (int64_t)row * row_stride * kElem;
+  const int skew = (int)(reinterpret_cast<uintptr_t>(from) / kElem & 3u);
+  Row<kType, kHeld> rw{&sh, from + ((int64_t)base - skew) * kElem, xs, slice, min(slice, max(0, V + skew - (int)base)), base, rank,
+                       size, {}, f2_neg_zero(), false, 0, rank == 0 ? skew : 0};
   const float temp = sp.temperature ? sp.temperature[row] : 1.0f;
   const int k = sp.top_k ? sp.top_k[row] : 0;
   const float top_p = sp.top_p ? sp.top_p[row] : 1.0f, min_p = sp.min_p ? sp.min_p[row] : 0.0f;
@@ -729,7 +735,7 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
   mn = order_value(least_key);
   if (mx == -INFINITY || !(temp > 0.0f)) {
     if (rank == 0 && tid == 0) {
-      tokens[row] = mx == -INFINITY ? -1 : (int32_t)~(uint32_t)best;
+      tokens[row] = mx == -INFINITY ? -1 : (int32_t)(~(uint32_t)best - (uint32_t)skew);
       if (probs) probs[row] = mx == -INFINITY ? 0.0f : 1.0f;
     }
     return;
@@ -780,7 +786,7 @@ __global__ void __launch_bounds__(kT, 2) sample_kernel(const void* logits, int64
           },
           index, w);
   if (index >= 0) {
-    tokens[row] = (int32_t)(base + index);
+    tokens[row] = (int32_t)(base + index) - skew;
     if (probs) probs[row] = (float)((double)w / (double)total);
   }
 }
@@ -821,7 +827,9 @@ w8a8_status launch_sample(int dtype, const void* logits, int64_t row_stride, int
   // CTAs a row: as many as all rows' clusters can run at once (two CTAs an SM; clusters of 16 and 8 leave some SMs of a GPC
   // unused, and with a slice in shared memory one CTA fills an SM), down to one step a warp and up to the longest slice
   int size = kMaxCluster;
-  auto slice_of = [&](int n) { return (((V + n - 1) / n) + kUnit - 1) / kUnit * kUnit; };
+  const int elem = dtype == W8A8_TYPE_F32 ? 4 : 2;
+  const int all = V + (reinterpret_cast<uintptr_t>(logits) / elem % 4 || (M > 1 && row_stride % 4) ? 3 : 0);  // rows that begin anywhere
+  auto slice_of = [&](int n) { return (((all + n - 1) / n) + kUnit - 1) / kUnit * kUnit; };
   auto room = [&](int n) { return n == 16 ? 3 * sms / 4 : n == 8 ? 15 * sms / 8 : 2 * sms; };
   while (size > 1 && ((long long)M * size > room(size) || slice_of(size) == slice_of(size / 2)) &&
          slice_of(size / 2) <= kMostSlice)
@@ -852,10 +860,12 @@ extern "C" w8a8_status w8a8_sample(int dtype, const void* logits, int64_t row_st
   W8A8_CHECK_ARG(sampling != nullptr, W8A8_ERR_INVALID_ARG, "%s: null parameters", who);
   if (M == 0) return W8A8_OK;
   W8A8_CHECK_ARG(logits && u && tokens, W8A8_ERR_INVALID_ARG, "%s: null pointer", who);
-  const int64_t unit = dtype == W8A8_TYPE_F32 ? 4 : 8;
-  W8A8_CHECK_ARG(row_stride >= 0 && row_stride <= (1ll << 40) && (M == 1 || row_stride % unit == 0), W8A8_ERR_SHAPE,
-                 "%s: row stride %lld must be a multiple of 16 bytes", who, (long long)row_stride);
-  W8A8_CHECK_ARG(aligned16(logits), W8A8_ERR_ALIGN, "%s: logits must be 16-byte aligned", who);
+  const uintptr_t elem = dtype == W8A8_TYPE_F32 ? 4 : 2, at = reinterpret_cast<uintptr_t>(logits);
+  W8A8_CHECK_ARG(row_stride >= 0 && row_stride <= (1ll << 40), W8A8_ERR_SHAPE, "%s: row stride %lld", who, (long long)row_stride);
+  W8A8_CHECK_ARG(at % elem == 0, W8A8_ERR_ALIGN, "%s: logits must be aligned to their type", who);
+  W8A8_CHECK_ARG(V <= W8A8_MAX_SAMPLE_VOCAB - 3 || (at / elem % 4 == 0 && (M == 1 || row_stride % 4 == 0)), W8A8_ERR_SHAPE,
+                 "%s: V=%d exceeds %d, the most where rows do not begin at multiples of four elements", who, V,
+                 W8A8_MAX_SAMPLE_VOCAB - 3);
   const void* words[] = {sampling->temperature, sampling->top_k, sampling->top_p, sampling->min_p, u, tokens, probs};
   for (const void* p : words)
     W8A8_CHECK_ARG((reinterpret_cast<uintptr_t>(p) & 3u) == 0, W8A8_ERR_ALIGN, "%s: arrays must be 4-byte aligned", who);

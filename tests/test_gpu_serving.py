@@ -620,3 +620,19 @@ def test_attention_few_rows_over_many_keys(B, n_q, n_kv, dim, seqs, new, ctx, wi
     attn_check(got, q, b, dim ** -0.5, window, rows)
     for _ in range(10):
         assert torch.equal(B.paged_attention(cache, batch, q, window=window), got)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(temperature=[0.7, 0.0], top_k=[50, 3], top_p=[0.95], min_p=[0.02])])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("M,V,first", [(5, 1, 1), (6, 3, 0), (5, 1001, 0), (4, 5002, 3), (3, 33001, 2), (70, 8207, 1)])
+def test_sample_rows_that_begin_anywhere(B, dt, M, V, first, kw):
+    """Contiguous rows of an odd length, at any offset; what lies before the first and behind the last is larger than any
+    logit of theirs, and so is each row's neighbour."""
+    x = torch.full((M * V + 16,), float("inf"), device="cuda", dtype=dt)
+    rows = x[first:first + M * V].view(M, V)
+    rows.copy_(((torch.randn(M, V, device="cuda", generator=_gen(V)) * 3) + 8 * torch.arange(M, device="cuda")[:, None]).to(dt))
+    sample_check(B, rows, torch.rand(M, device="cuda", generator=_gen(2)), **kw)
+    if M > 2:  # infinities within a row of the same kind
+        rows[1, V // 2] = float("inf")
+        rows[2].fill_(float("-inf"))
+        sample_check(B, rows, torch.rand(M, device="cuda", generator=_gen(5)), **kw)

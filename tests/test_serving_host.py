@@ -178,8 +178,8 @@ def test_sample_refusals(B):
     def sample(dtype=2, x=P, row=1024, M=2, V=1000, sp=(None, None, None, None), u=P, tok=P, prob=None):
         return L.w8a8_sample(dtype, x, row, M, V, ctypes.byref(B.SamplingC(*sp)) if sp else None, u, tok, prob, None)
     for kw, want in [(dict(dtype=3), 1), (dict(dtype=-1), 1), (dict(M=-1), 1), (dict(V=0), 1), (dict(V=1 << 21), 2),
-                     (dict(sp=None), 1), (dict(x=None), 1), (dict(u=None), 1), (dict(tok=None), 1), (dict(x=P + 4), 3),
-                     (dict(row=1002), 2), (dict(row=-4), 2), (dict(u=P + 2), 3), (dict(sp=(None, P + 1, None, None)), 3)]:
+                     (dict(sp=None), 1), (dict(x=None), 1), (dict(u=None), 1), (dict(tok=None), 1), (dict(x=P + 2), 3),
+                     (dict(V=1 << 20, row=(1 << 20) + 2), 2), (dict(V=1 << 20, x=P + 4, M=1), 2), (dict(row=-4), 2), (dict(u=P + 2), 3), (dict(sp=(None, P + 1, None, None)), 3)]:
         assert sample(**kw) == want, kw
     assert sample(M=0, x=None, u=None, tok=None) == 0
 
