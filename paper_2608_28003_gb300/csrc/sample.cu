@@ -35,6 +35,7 @@ typedef unsigned long long u64;
 constexpr int kT = 512, kWarps = kT / 32;
 constexpr int kFrac = 43;     // weights are multiples of 2^-43 of the largest
 constexpr int kBins = 2880;    // one per 1/64 of the exponent, 44.5 of which weigh anything (0 .. 2849); a multiple of 16 CTAs
+constexpr int kMostSteps = 2 * 2849;  // of 1 / 128 of the exponent, that a logit with a bin lies below the maximum
 constexpr int kFine = 2048;    // and of the divisions of a crowded range
 constexpr int kMostSlice = 65536;  // 16-bit digits of that many weights add up in 32 bits
 constexpr int kSmall = 1024;
@@ -64,6 +65,9 @@ __device__ __forceinline__ RowScale row_scale(float mx, float least, float tempe
   r.c_hi = k_hi / t;
   r.c_lo = (fmaf(-r.c_hi, t, k_hi) + k_lo) / t;
   r.low = fmaxf(fmaxf(mx - (kFrac + 1.5f) / r.c_hi, least), mx - 3e38f);
+  // At a temperature of a few of mx's last places the difference rounds to a logit up to twice as far below, whose bin
+  // would lie beyond the last: a place or two up is one within them, which still weighs nothing.
+  while (steps_of(r, r.low) > kMostSteps) r.low = nextafterf(r.low, mx);
   return r;
 }
 // `table`: 2^(j / 128) as a float, and 2^(29 + j / 128) as an integer less the bits of kMagic.
