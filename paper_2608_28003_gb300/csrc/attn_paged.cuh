@@ -2,7 +2,7 @@
 //
 // Work.  An item is (sequence, key/value head, tile of rows); its rows are the tokens of the tile times the query
 // heads of the group, so that a group reads its keys once.  Its cost is the number of key tiles any of its rows sees.  All
-// items, one after the other, make a line of key tiles, which the workers of the grid (CTAs or pairs of them) divide into
+// items, one after the other, make a line of key tiles, which the workers of the grid (its CTAs) divide into
 // equal stretches: whatever the lengths, they finish together.  An item that a stretch border cuts leaves fp32
 // partials (output, reference, sum) in the workspace, and the last of its pieces to arrive joins them in the order of the
 // pieces: a fixed order, so results do not depend on who was last.  Where stretches are short (kShort tiles), two cut items

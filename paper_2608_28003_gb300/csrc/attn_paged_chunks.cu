@@ -1,9 +1,8 @@
-// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows, tokens
-// times the query heads of a group, in two tiles of 128 rows with one row per TMEM lane.  At head dims 64 and 128 one CTA
-// has both tiles, at 256 (whose output fills tensor memory) each CTA of a pair has one, and either copies half of every K
-// and V part to both: read from L2 once for 256 rows either way (with 128, L2 bounded the kernel: 23 bytes a clock and SM).
+// Attention over a paged cache for chunks of tokens, on the 5th-generation tensor cores: items of up to 256 rows (128 at head
+// dim 256, whose output fills tensor memory), tokens times the query heads of a group, in two tiles (one) of 128 rows with
+// one row per TMEM lane.
 //
-// A worker (CTA or pair), one CTA per SM, walks its stretch of the line of key tiles (attn_paged.cuh), 128 keys at a time:
+// One CTA per SM walks its stretch of the line of key tiles (attn_paged.cuh), 128 keys at a time:
 //  * two warps copy by TMA, page by page: one an item's queries and the K tiles, one the V tiles (either as its tiles are
 //    handed back, which one warp's order would tie together);
 //  * the issue warp allocates tensor memory and issues tcgen05.mma: S = Q K^T (128 x 128 x dim) for each row tile, and
@@ -27,8 +26,9 @@
 // 178 us (690 TFLOP/s, 0.37 of the measured rate; 217 with P in one piece after the rescaling).  Tried and slower: a part of
 // the exponentials as a polynomial (an eighth 180 us, a quarter 184, half 207: issue slots, not the special function unit,
 // are short), two threads a row for both row tiles (211: 96 registers), scores loaded ahead or kept in registers (189 and
-// 233: spills).  A whole prompt of 2048 tokens at head dim 256 takes 27.9 us, of which the lookup of the work is 2, the
-// first tile's way 3, four key tiles 7, and the partials of cut items and their join 8.
+// 233: spills).  A whole prompt of 2048 tokens at head dim 256 takes 28.4 us.  There every CTA copies all of its K and V from L2;
+// a pair of CTAs, each copying half for both, took 27.9, and 67.2 us instead of 71.9 for a larger chunk, but a copy to several
+// CTAs has no place in a library that also runs on several GPUs.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
 #include "attn_paged.cuh"
 #include "ops.cuh"
@@ -47,7 +47,6 @@ constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
 template <int kDim>
 struct Cfg {
   static constexpr int kRt = kDim == 256 ? 1 : 2;  // row tiles of a CTA
-  static constexpr int kCl = 2 / kRt;              // CTAs of a worker
   static constexpr int kChunks = kDim / 64;
   static constexpr int kStages = kDim == 256 ? 1 : kDim == 128 ? 2 : 4;
   static constexpr int kTile = kChunks * kSub;
@@ -77,25 +76,6 @@ __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, uint32_t lead) {
 }
 constexpr uint32_t kIdescBMnMajor = 1u << 16;
 
-// Arrives, once the MMAs issued so far have completed, at the barrier in every CTA of a pair.
-__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(bar),
-      "h"((uint16_t)3)
-      : "memory");
-}
-// A box into both CTAs of a pair, at the same offsets, counted at the same barrier of each.
-__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const void* tmap, int c0, int c1, int c2, int c3, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster [%0], [%1, {%2, %3, "
-      "%4, %5}], [%6], %7;\n" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar), "h"((uint16_t)3)
-      : "memory");
-}
-__device__ __forceinline__ void pair_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-}
 // A from tensor memory (two 16-bit elements a column)
 __device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -143,16 +123,12 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   const uint32_t bar0 = smem_u32(bars);
   auto bar = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = a.n_q / c.n_kv, item_tt = 2 * tt;  // tokens of a row tile, of an item
-  constexpr int kCl = C::kCl;
-  const int rank = kCl == 2 ? (int)(blockIdx.x & 1) : 0, worker = (int)blockIdx.x / kCl;  // clusters are neighbouring CTAs
+  const int group = a.n_q / c.n_kv, item_tt = kRt * tt;  // tokens of a row tile, of an item
 
   if (threadIdx.x < 4) s_bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kBars; ++i)
-      mbar_init(bar(i), (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive
-                        : (i >= C::K_FREE && i < C::V_FULL) || i >= C::V_FREE                                          ? kCl
-                                                                                                                       : 1);
+      mbar_init(bar(i), (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive : 1);
     fence_mbar_init();
     prefetch_tmap(&tmQ);
     prefetch_tmap(&tmK);
@@ -165,13 +141,12 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if constexpr (kCl == 2) pair_sync();  // the peer's barriers are there to be arrived at
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   pdl_wait();
   pdl_trigger();
   // (syncs the block)
-  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, worker, (int)gridDim.x / kCl, &ls, scan);
+  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan);
   bool ok = true;
 
   if (ls.begin < ls.end) {
@@ -203,7 +178,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll
               for (int ch = 0; ch < C::kChunks; ++ch)
                 tma_load_3d(base + (uint32_t)(rt * C::kTile + ch * kSub), &tmQ, 64 * ch, w.h * group,
-                            w.q.row0 + w.t * item_tt + (rank + rt) * tt, bar(C::Q_FULL));
+                            w.q.row0 + w.t * item_tt + rt * tt, bar(C::Q_FULL));
           }
           __syncwarp();
         }
@@ -225,16 +200,13 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               mbar_arrive_expect_tx(bar(full + bi), (uint32_t)(C::kTile / C::kKParts));
             }
             __syncwarp();
-            // lane = (column, box); of a pair each CTA copies every other one
-            const int o = lane * kCl + rank, bx = (kv ? pt * n_box : 0) + o % n_box, ch = (kv ? 0 : pt * C::kKCols) + o / n_box;
+            // lane = (column, box)
+            const int bx = (kv ? pt * n_box : 0) + lane % n_box, ch = (kv ? 0 : pt * C::kKCols) + lane / n_box;
             const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + bx * (box / 16)) & 31);
-            if (o < n_ops) {
+            if (lane < n_ops) {
               const uint32_t dst = base + (uint32_t)((kv ? C::kOffV : C::kOffK) + st * C::kTile + ch * kSub + bx * box * 128);
               const int slot = (tile0 + bx * box) & ((1 << c.page_shift) - 1), at = pg < 0 ? c.n_pages : pg;
-              if constexpr (kCl == 2)
-                tma_load_4d_pair(dst, map, 64 * ch, slot, w.h, at, bar(full + bi));
-              else
-                tma_load_4d(dst, map, 64 * ch, slot, w.h, at, bar(full + bi));
+              tma_load_4d(dst, map, 64 * ch, slot, w.h, at, bar(full + bi));
             }
             issued = g * C::kKParts + pt + 1;
           }
@@ -252,12 +224,6 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       constexpr uint32_t fmt = kBf16 ? 1u : 0u;
       constexpr uint32_t idesc_s = idesc_f16(fmt, kBk, kBq), idesc_o = idesc_f16(fmt, kDim, kBq) | kIdescBMnMajor;
       const uint64_t dq = sdesc_swz(base);
-      auto hand_back = [&](uint32_t b0) {  // either CTA of a pair writes to both
-        if constexpr (kCl == 2)
-          tc_commit_pair(b0);
-        else
-          tc_commit(b0);
-      };
       // S of key tile i (this CTA's count) for row tile rt, into its slot; hands K back after the last row tile, Q after `last`
       auto issue_s = [&](int i, int rt, bool last) {
         const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
@@ -274,7 +240,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               const uint32_t at = (uint32_t)((pt * C::kKCols + (k >> 2)) * (kSub >> 4) + 2 * (k & 3));
               tc_mma(tmem + 128u * (uint32_t)slot, dq + (uint32_t)(rt * (C::kTile >> 4)) + at, dk + at, idesc_s, pt > 0 || k > 0);
             }
-            if (rt == kRt - 1) hand_back(bar(C::K_FREE + st * C::kKParts + pt));
+            if (rt == kRt - 1) tc_commit(bar(C::K_FREE + st * C::kKParts + pt));
           }
           __syncwarp();
         }
@@ -305,7 +271,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                 const int kk = 4 * half + k;  // 16 keys: 8 columns of P
                 tc_mma_ts(o, p + 8u * (uint32_t)kk, dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o, !first || kk > 0);
               }
-              if (half == 1 && rt == kRt - 1) hand_back(bar(C::V_FREE + st));
+              if (half == 1 && rt == kRt - 1) tc_commit(bar(C::V_FREE + st));
               if (half == 1) tc_commit(bar(C::PV_DONE + rt));
             }
             __syncwarp();
@@ -323,7 +289,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                   tc_mma_ts(o, p + 8u * (uint32_t)kk + (kk >= 4 ? 32u : 0u), dv + (uint32_t)(kk * (16 * 128 >> 4)), idesc_o,
                             !first || kk > 0);
                 }
-                hand_back(bar(C::V_FREE + st * C::kVParts + vp));
+                tc_commit(bar(C::V_FREE + st * C::kVParts + vp));
                 if (vp == C::kVParts - 1) {
                   tc_commit(bar(C::PV_DONE));
                   if (last) tc_commit(bar(C::PV_DONE + 1));
@@ -364,7 +330,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
       const float sc = a.scale * kLog2e;
       for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
-        const int tok0 = w.t * item_tt + (rank + rt) * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
+        const int tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
         const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
         const bool live = r < rows, busy = 32 * (warp & 3) < rows;  // this row's, and any of the warp's
         const int tok = tok0 + (live ? r / group : 0), head = w.h * group + (live ? r % group : 0);
@@ -563,7 +529,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         // ---- a piece: into the workspace, joined by the last one to arrive
         const Pieces ps = pieces_of(w, ls);
         const int pr = rt * kBq + r;  // row of the partial
-        float* mine = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;  // pieces of one rank are joined
+        float* mine = part + (size_t)(2 * blockIdx.x + (w.k0 > 0 ? 0 : 1)) * C::kPart;
         if (busy) {
 #pragma unroll 1
           for (int ch = 0; ch < kCh; ++ch) {
@@ -585,10 +551,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         tc_fence_before();
         mbar_arrive(bar(C::O_FREE + rt));
         named_bar_sync(1, 32 * C::kSoft);
-        if (threadIdx.x == 0) s_last = last_piece(counters + ps.first * kCl + rank, ps.count);
+        if (threadIdx.x == 0) s_last = last_piece(counters + ps.first, ps.count);
         named_bar_sync(1, 32 * C::kSoft);
         if (s_last) {
-          auto slot = [&](int i) { return part + (size_t)(2 * ((ps.first + i) * kCl + rank) + (i == 0 ? 1 : 0)) * C::kPart; };
+          auto slot = [&](int i) { return part + (size_t)(2 * (ps.first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
           float M = -INFINITY, L = 0.0f, nan = 0.0f;
           if (live) {
 #pragma unroll 4
@@ -633,7 +599,6 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if constexpr (kCl == 2) pair_sync();  // the peer writes and arrives here no more
   if (warp == kIssueWarp) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem) : "memory");
@@ -658,22 +623,9 @@ w8a8_status launch(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a
   W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
   W8A8_TRY(make_kv_maps(pc, kDim, &tk, &tv));
   char* base = static_cast<char*>(ws);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(sms / C::kCl * C::kCl));
-  cfg.blockDim = dim3(C::kThreads);
-  cfg.dynamicSmemBytes = C::kSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = C::kCl;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  W8A8_CUDA(cudaLaunchKernelEx(&cfg, attn_chunks_kernel<kBf16, kDim>, tq, tk, tv, pc, pb, a, tt,
-                               reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
-                               reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
+  W8A8_CUDA(launch_pdl(attn_chunks_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
+                       pc, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
+                       reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
   return W8A8_OK;
 }
 
