@@ -398,6 +398,9 @@ typedef struct {
 } w8a8_trace;
 w8a8_status w8a8_model_set_trace(w8a8_model* m, const w8a8_trace* t);
 
+/* w8a8_workspace_check for the model's own workspaces, those of its steps over a paged cache included. */
+w8a8_status w8a8_model_check(w8a8_model* m, void* stream);
+
 /* Measurement aid with no counterpart in the paper: *kernels = the number of kernel launches
  * one w8a8_decoder_decode_step of B sequences makes under the current mask (the kernel nodes of
  * its CUDA graph plus the position update launched beside it; copies are not counted).  The
@@ -543,6 +546,14 @@ w8a8_status w8a8_paged_attention_workspace_size(const w8a8_paged_cache* cache, i
 w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged_batch* batch, const uint16_t* q,
                                  int64_t q_row, int64_t q_head, int n_q, float scale, int window, uint16_t* o,
                                  int64_t o_row, int64_t o_head, void* workspace, size_t ws_bytes, void* stream);
+
+/* Whether a wait in a call of paged attention on the current device gave up since the last check, whichever workspace the
+ * call had (its own error word says so too): a step of the decoder and a captured call included.  Waits for `stream`, then
+ * reads and clears the device's word: W8A8_ERR_TIMEOUT if any bit was set (the outputs of the calls in between are then
+ * undefined).  Synchronous.  w8a8_paged_attention_error_word gives the word's device address, for a program that fetches it
+ * with its results, within a graph of its own, say. */
+w8a8_status w8a8_paged_attention_check(void* stream);
+w8a8_status w8a8_paged_attention_error_word(uint32_t** word);
 
 /* ------------------------------------------------------------------------------ sampling
  * One token a row from logits [M, V] (fp32, bf16 or fp16; any row stride, in elements; V up to

@@ -189,6 +189,9 @@ SIGNATURES = {
     "w8a8_stream_gemm_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_int32)]),
     "w8a8_tc_gemm_plan": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(ctypes.c_int32)]),
     "w8a8_model_set_trace": (_i32, [_vp, ctypes.POINTER(TraceC)]),
+    "w8a8_model_check": (_i32, [_vp, _vp]),
+    "w8a8_paged_attention_check": (_i32, [_vp]),
+    "w8a8_paged_attention_error_word": (_i32, [ctypes.POINTER(_vp)]),
     "w8a8_rope_frequencies": (_i32, [ctypes.POINTER(RopeCfgC), ctypes.POINTER(ctypes.c_uint64), _fp]),
     "w8a8_rope": (_i32, [ctypes.POINTER(RopeTableC), _i32, _vp, _i64, _i64, _i32, _i32, _i32, _vp, _vp, _i64, _i64, _vp]),
     "w8a8_rope_append": (_i32, [ctypes.POINTER(RopeTableC), ctypes.POINTER(PagedCacheC), ctypes.POINTER(PagedBatchC), _vp,
@@ -689,6 +692,12 @@ def paged_attention(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale
     return (_CALLS or _calls()).paged_attention(cache, batch, q, scale, window, out, ws, stream)
 
 
+def paged_attention_check(stream=None) -> None:
+    """Raise W8A8Error(ERR_TIMEOUT) if a wait in a call of paged attention on the current device gave up since the last
+    check, with any workspace, in a step of a decoder or in a captured graph."""
+    _check("w8a8_paged_attention_check", lib().w8a8_paged_attention_check(_stream(stream)))
+
+
 def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
            top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
            want_probs: bool = False, tokens: Optional[torch.Tensor] = None, stream=None):
@@ -941,6 +950,10 @@ class Decoder:
             self.h, _p(tokens), ctypes.byref(bc), ctypes.byref(cc), k.stride(0), ctypes.byref(sp) if u is not None else None,
             _p(u), _p(logits), _p(nxt), _p(probs), _stream(stream)))
         return nxt, logits if want_logits else None, probs
+
+    def check(self, stream=None) -> None:
+        """Raise W8A8Error(ERR_TIMEOUT) if a wait in a call of this model gave up since the last check."""
+        _check("w8a8_model_check", lib().w8a8_model_check(self.h, _stream(stream)))
 
     TRACE_FIELDS = ("a_in", "qkv", "attn", "y_o", "a_ffn", "h", "y_f", "r", "a_fin")
 

@@ -405,8 +405,11 @@ extern "C" w8a8_status w8a8_set_kernel_events(void* start_event, void* stop_even
 
 extern "C" w8a8_status w8a8_workspace_check(void* workspace, void* stream) {
   W8A8_CHECK_ARG(workspace != nullptr, W8A8_ERR_INVALID_ARG, "w8a8_workspace_check: null workspace");
-  cudaStream_t st = as_stream(stream);
-  unsigned int* err = reinterpret_cast<unsigned int*>(reinterpret_cast<char*>(workspace) + kErrWordOffset);
+  return take_error_word(reinterpret_cast<unsigned int*>(reinterpret_cast<char*>(workspace) + kErrWordOffset),
+                         as_stream(stream));
+}
+
+w8a8_status w8a8::take_error_word(unsigned int* err, cudaStream_t st) {
   unsigned int host = 0;
   W8A8_CUDA(cudaMemcpyAsync(&host, err, sizeof(host), cudaMemcpyDeviceToHost, st));
   W8A8_CUDA(cudaStreamSynchronize(st));

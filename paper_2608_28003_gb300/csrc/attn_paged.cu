@@ -12,13 +12,36 @@ size_t paged_attention_ws(int dim, int sms) {
   return W8A8_WS_RESERVED + std::max(attn_tokens_ws(dim, sms), attn_chunks_ws(dim, sms));
 }
 
+namespace {
+
+__device__ unsigned int g_gave_up;  // DevErr bits of any call on this device since the last check
+
+w8a8_status gave_up_word(unsigned int** word) {
+  static unsigned int* at[64] = {};
+  int dev = 0;
+  W8A8_CUDA(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64 && at[dev]) {
+    *word = at[dev];
+    return W8A8_OK;
+  }
+  void* p = nullptr;
+  W8A8_CUDA(cudaGetSymbolAddress(&p, g_gave_up));
+  *word = static_cast<unsigned int*>(p);
+  if (dev >= 0 && dev < 64) at[dev] = *word;
+  return W8A8_OK;
+}
+
+}  // namespace
+
 // Up to 16 rows a sequence and key/value head go to the kernel for tokens, more to the one for chunks (a longer sequence in
 // the batch is right in either): 64 sequences of 4000 keys, 1 head of 256, take 55.7, 64.9 and 96.9 us for 4, 16 and 32 rows
 // there and 68.3 here; 40 sequences of 4 heads of 128 70.3 and 124 us for 16 and 32 rows there, 72.9 and 73.5 here; of 8
 // heads of 64 67.3 and 120 us for 15 and 30 rows there, 109 and 108 here.
-w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
+w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& call, void* ws, int sms,
                                    cudaStream_t st) {
-  const int group = a.n_q / pc.n_kv;
+  const int group = call.n_q / pc.n_kv;
+  AttnCall a = call;
+  W8A8_TRY(gave_up_word(&a.gave_up));
   return (long long)a.max_new * group <= 16 ? launch_attn_tokens(pc, pb, a, ws, sms, st)
                                             : launch_attn_chunks(pc, pb, a, ws, sms, st);
 }
@@ -77,4 +100,16 @@ extern "C" w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const
   const AttnCall a{q, q_row, q_head, o, o_row, o_head, n_q, dim, window, batch->max_new, scale,
                    cache->dtype == W8A8_TYPE_BF16};
   return launch_paged_attention(pc, pb, a, workspace, d.sms, as_stream(stream));
+}
+
+extern "C" w8a8_status w8a8_paged_attention_error_word(uint32_t** word) {
+  W8A8_CHECK_ARG(word != nullptr, W8A8_ERR_INVALID_ARG, "w8a8_paged_attention_error_word: null argument");
+  W8A8_TRY(check_device());
+  return gave_up_word(word);
+}
+
+extern "C" w8a8_status w8a8_paged_attention_check(void* stream) {
+  unsigned int* word = nullptr;
+  W8A8_TRY(w8a8_paged_attention_error_word(&word));
+  return take_error_word(word, as_stream(stream));
 }

@@ -27,6 +27,13 @@ w8a8_status launch_attn_chunks(const PagedCache& pc, const PagedBatch& pb, const
 size_t attn_tokens_ws(int dim, int sms);
 size_t attn_chunks_ws(int dim, int sms);
 
+// A wait that gave up, in the workspace's error word and in the device's: a decoder's workspace and a captured call's are out of
+// the caller's reach.
+__device__ __forceinline__ void give_up(unsigned int* err, const AttnCall& a, unsigned int bits) {
+  atomicOr(err, bits);
+  atomicOr(a.gave_up, bits);
+}
+
 constexpr float kGrowth = 8.0f;  // a row's reference moves when its maximum grew by 2^8: weights stay within 2^8
 constexpr float kLog2e = 1.4426950408889634f;
 

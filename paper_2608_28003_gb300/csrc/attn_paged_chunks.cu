@@ -213,12 +213,12 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         }
       }
       // the last copies land before the CTA may end
-      if (!ok && lane == 0) atomicOr(err, DEVERR_PRODUCER_WAIT);
+      if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
       constexpr int kRing = C::kStages * C::kKParts;
       bool drained = kv || item == 0 || mbar_wait_warp(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles);
       for (int k = max(0, issued - kRing); k < issued; ++k)
         drained &= mbar_wait_warp(bar(full + k % kRing), (uint32_t)(k / kRing) & 1u, kWaitBudgetCycles);
-      if (!drained && lane == 0) atomicOr(err, DEVERR_DRAIN_WAIT);
+      if (!drained && lane == 0) give_up(err, a, DEVERR_DRAIN_WAIT);
     } else if (warp == kIssueWarp) {
       // ---------------------------------------------------------------------- MMAs
       constexpr uint32_t fmt = kBf16 ? 1u : 0u;
@@ -316,9 +316,9 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         }
       }
       if (elect_one()) {
-        if (!ok) atomicOr(err, DEVERR_PRODUCER_WAIT);
+        if (!ok) give_up(err, a, DEVERR_PRODUCER_WAIT);
         tc_commit(bar(C::ALL_DONE));  // completes once every MMA issued above has
-        if (!mbar_wait_bounded(bar(C::ALL_DONE), 0u, kWaitBudgetCycles)) atomicOr(err, DEVERR_DRAIN_WAIT);
+        if (!mbar_wait_bounded(bar(C::ALL_DONE), 0u, kWaitBudgetCycles)) give_up(err, a, DEVERR_DRAIN_WAIT);
       }
       __syncwarp();
     } else {
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         if (ok && !mbar_wait_warp(bar(kRt == 2 ? C::PV_DONE + rt : C::PV_DONE + 1), (uint32_t)(kRt == 2 ? g - 1 : item) & 1u,
                                   kWaitBudgetCycles))
           ok = false;
-        if (!ok && lane == 0) atomicOr(err, DEVERR_CONSUMER_WAIT);
+        if (!ok && lane == 0) give_up(err, a, DEVERR_CONSUMER_WAIT);
         __syncwarp();
         tc_fence_after();
 

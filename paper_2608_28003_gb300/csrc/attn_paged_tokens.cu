@@ -198,10 +198,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       }
     }
     // the last copies land before the CTA may end
-    if (!ok && lane == 0) atomicOr(err, DEVERR_PRODUCER_WAIT);
+    if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
     for (int k = max(0, g - C::kStages); k < g; ++k)
       if (!mbar_wait_warp(full(k % C::kStages), (uint32_t)(k / C::kStages) & 1u, kWaitBudgetCycles) && lane == 0)
-        atomicOr(err, DEVERR_DRAIN_WAIT);
+        give_up(err, a, DEVERR_DRAIN_WAIT);
     return;
   }
 
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(empty(st));
     }
-    if (!ok && lane == 0) atomicOr(err, DEVERR_CONSUMER_WAIT);
+    if (!ok && lane == 0) give_up(err, a, DEVERR_CONSUMER_WAIT);
 
     // ---- the warps' outputs of the item, on a common reference
 #pragma unroll

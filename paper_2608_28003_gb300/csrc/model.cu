@@ -764,6 +764,12 @@ extern "C" w8a8_status w8a8_decoder_step_paged(w8a8_model* m, const int32_t* tok
                        m->sms, st);
 }
 
+extern "C" w8a8_status w8a8_model_check(w8a8_model* m, void* stream) {
+  W8A8_CHECK_ARG(m != nullptr, W8A8_ERR_INVALID_ARG, "w8a8_model_check: null model");
+  const w8a8_status a = w8a8_workspace_check(m->ws, stream), b = w8a8_workspace_check(m->paged_ws, stream);
+  return a != W8A8_OK ? a : b;
+}
+
 extern "C" w8a8_status w8a8_model_set_trace(w8a8_model* m, const w8a8_trace* t) {
   W8A8_CHECK_ARG(m, W8A8_ERR_INVALID_ARG, "w8a8_model_set_trace: null model");
   if (!t) {

@@ -12,6 +12,8 @@ struct DevInfo {
 };
 w8a8_status dev_info(DevInfo* out);
 int device_sms();
+// waits for the stream, reads and clears a word of DevErr bits: W8A8_ERR_TIMEOUT if any was set
+w8a8_status take_error_word(unsigned int* err, cudaStream_t st);
 
 struct LinearWs {
   size_t xf16, sx, part, total;

@@ -35,6 +35,7 @@ struct AttnCall {
   int n_q, dim, window, max_new;
   float scale;
   bool bf16;
+  unsigned int* gave_up = nullptr;  // the device's word of waits that gave up, beside the workspace's (launch_paged_attention's)
 };
 w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st);
