@@ -538,7 +538,10 @@ w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache
  *   j <= p), p the row's position; query head h reads key/value head h / (n_q / n_kv); scale > 0.
  * A row without keys gets zeros.  A key outside a row's range, and slots that hold none, never reach it, whatever
  * their values; keys within it propagate NaN and infinities as the formula does.  Scores, softmax and sums
- * in fp32; a weight (at most 2^8) is rounded once to the type before it meets v; the output is rounded once.
+ * in fp32; a weight is rounded once to the type before it meets v (in fp16 those down to 2^-26 of a reference within 2^3 of the
+ * row's largest keep all of its bits, and those down to 2^-37 count); the output is rounded once.  The sum of the weights is
+ * of the rounded ones with up to 16 rows (max_new times query heads per key/value head), of the unrounded ones with more, so
+ * outputs of the same row can differ by the weights' rounding.
  * Deterministic: the same call gives the same bits, whatever runs beside it.
  * q and o [n_rows, n_q, head_dim] of the cache's type, strides in elements (multiples of 8); n_q a multiple of n_kv,
  * at most 128 query heads per key/value head; o overlaps no input. */

@@ -34,7 +34,14 @@ __device__ __forceinline__ void give_up(unsigned int* err, const AttnCall& a, un
   atomicOr(a.gave_up, bits);
 }
 
-constexpr float kGrowth = 8.0f;  // a row's reference moves when its maximum grew by 2^8: weights stay within 2^8
+// A row's reference moves when its maximum grew by 2^kGrowth, and weights are 2^kLift times what they are against it, so that they
+// stay within 2^8 in bf16 and 2^15 in fp16, where the largest are put near the type's end: weights down to 2^-26 of the
+// reference are normal numbers and those down to 2^-37 are counted (unlifted, 2^-14 and 2^-25: a tail of 40000 keys at
+// 2^-25.5 vanished, which is 8e-4 of the output).
+template <bool kBf16>
+constexpr float kGrowth = kBf16 ? 8.0f : 3.0f;
+template <bool kBf16>
+constexpr float kLift = kBf16 ? 0.0f : 12.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float ex2(float x) {

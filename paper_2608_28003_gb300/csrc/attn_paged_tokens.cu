@@ -300,12 +300,12 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * sc;
           up[r] = 1.0f;
-          if (top > m[r] + kGrowth) {  // m = -inf: any visible key
+          if (top > m[r] + kGrowth<kBf16>) {  // m = -inf: any visible key
             up[r] = m[r] == -INFINITY ? 0.0f : ex2(m[r] - top);
             m[r] = top;
             grown = true;
           }
-          ref[r] = m[r] == -INFINITY ? 0.0f : m[r];
+          ref[r] = m[r] == -INFINITY ? 0.0f : m[r] - kLift<kBf16>;
         }
         if (__any_sync(0xffffffffu, grown)) {
           l[0] *= up[0];
