@@ -473,7 +473,8 @@ typedef struct {
 } w8a8_rope_cfg;
 
 /* Host only: turns[i] (HOST array, rotary_dim / 2 values) = f_i / (2 pi) as a fraction of 2^64, so that the
- * angle of any 32-bit position is one wrapping 64-bit product, reduced without error; *scale = the factor on
+ * angle of any 32-bit position is one wrapping 64-bit product, whose reduction loses nothing (the fractions are a double's, off by
+ * 2^-50 of themselves or so, and an angle by as many of its turns); *scale = the factor on
  * cos and sin.  W8A8_ERR_SHAPE for a rotary_dim that is not a multiple of 16 in [16, 256], W8A8_ERR_INVALID_ARG
  * for a null pointer or parameters outside their domain (base <= 1, factor <= 0, high <= low where they are used,
  * original_len <= 0 where it is). */
