@@ -462,7 +462,8 @@ enum { W8A8_TYPE_BF16 = 0, W8A8_TYPE_F16 = 1, W8A8_TYPE_F32 = 2 };
  *   PARTS       f ((1 - r) + r / factor), r = clamp((i - a) / max(b - a, 0.001), 0, 1) between the pair indices
  *               a = max(0, floor(at(high))) and b = min(rotary_dim - 1, ceil(at(low))) of
  *               at(x) = rotary_dim ln(original_len / (2 pi x)) / (2 ln base)
- * attn_factor multiplies cos and sin; 0 stands for 1, and for 0.1 ln(factor) + 1 under PARTS. */
+ * attn_factor multiplies cos and sin; 0 stands for 1, and for 0.1 ln(factor) + 1 under PARTS with a
+ * factor above 1. */
 enum { W8A8_ROPE_NONE = 0, W8A8_ROPE_LINEAR = 1, W8A8_ROPE_WAVELENGTH = 2, W8A8_ROPE_PARTS = 3 };
 typedef struct {
   int32_t rotary_dim; /* rotated dims of a head: a multiple of 16, at most 256 */

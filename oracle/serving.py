@@ -27,7 +27,7 @@ def rope_frequencies(rot, base, scaling="none", factor=1.0, low=1.0, high=4.0, o
             r = min(1.0, max(0.0, (i - a) / max(b - a, 0.001)))
             f = f * (1 - r) + f / factor * r
         out.append(f)
-    s = attn_factor if attn_factor > 0 else (0.1 * math.log(factor) + 1.0 if scaling == "parts" else 1.0)
+    s = attn_factor if attn_factor > 0 else (0.1 * math.log(factor) + 1.0 if scaling == "parts" and factor > 1 else 1.0)
     return np.array(out), s
 
 

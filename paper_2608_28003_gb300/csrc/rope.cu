@@ -319,7 +319,7 @@ extern "C" w8a8_status w8a8_rope_frequencies(const w8a8_rope_cfg* c, uint64_t* t
     const double turn = f / two_pi - std::floor(f / two_pi);  // whole turns a position change nothing
     turns[i] = turn >= 1.0 ? 0ull : (uint64_t)std::ldexp(turn, 64);
   }
-  const double def = c->scaling == W8A8_ROPE_PARTS ? 0.1 * std::log(c->factor) + 1.0 : 1.0;
+  const double def = c->scaling == W8A8_ROPE_PARTS && c->factor > 1.0 ? 0.1 * std::log(c->factor) + 1.0 : 1.0;
   *scale = (float)(c->attn_factor > 0.0 ? c->attn_factor : def);
   return W8A8_OK;
 }

@@ -31,3 +31,17 @@ def test_fractions_of_a_turn(B, rot, base, scaling, factor):
         off = abs(got - want)
         bound = f / (2 * PI) * (Decimal(2) ** -52 + ln * Decimal(2) ** -54 + 3 * Decimal(2) ** -53) + Decimal(2) ** -64
         assert min(off, 1 - off) <= bound, (i, float(off / bound))
+
+
+@pytest.mark.parametrize("factor", [1e-6, 4.5e-5, 0.25, 0.9999, 1.0, 1.0001, 16.0])
+def test_parts_by_a_factor_of_one_or_less(B, factor):
+    """The factor on cos and sin that PARTS brings with it is 1 where positions are not compressed: never below, let alone
+    zero or negative (0.1 ln(factor) + 1 is at factors of e^-10 and less)."""
+    import math
+    from oracle import serving as OS
+    kw = dict(factor=factor, low=1.0, high=32.0, original_len=4096)
+    _, scale = B.rope_frequencies(B.RopeConfig(64, scaling="parts", **kw))
+    want = 1.0 + max(0.0, 0.1 * math.log(factor))
+    assert abs(scale - want) <= 2.0 ** -24 * want
+    assert OS.rope_frequencies(64, 1e4, "parts", **kw)[1] == pytest.approx(want, abs=0, rel=2.0 ** -52)
+    assert B.rope_frequencies(B.RopeConfig(64, scaling="parts", attn_factor=0.5, **kw))[1] == 0.5  # given, it is taken
