@@ -392,14 +392,15 @@ struct Row {
     };
     cluster_sync_all();  // every CTA's histogram is complete
     const int mine = tid / parts * per;
+    const uint32_t lanes = __ballot_sync(0xffffffffu, mine < seg);  // that share bins below (one bin a thread where they do)
     u64 cs = 0, ws = 0;
     if (mine < seg)
       for (int i = 0; i < per && mine + i < seg; ++i) {
         u64 c, w;
         load(first + mine + i, tid % parts, parts, c, w);
         for (int o = 1; o < parts; o <<= 1) {
-          c += __shfl_xor_sync(__activemask(), c, o);
-          w += __shfl_xor_sync(__activemask(), w, o);
+          c += __shfl_xor_sync(lanes, c, o);
+          w += __shfl_xor_sync(lanes, w, o);
         }
         if (tid % parts) continue;
         cs += c;

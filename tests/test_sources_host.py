@@ -17,3 +17,9 @@ def test_no_bulk_copy_to_several_ctas(path):
     tensor cores' work may arrive at several CTAs)."""
     text = re.sub(r'"\s*"', "", open(path).read())  # adjacent string literals are one
     assert not re.search(r'cp\.async\.bulk[^"]*\.multicast', text)
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=os.path.basename)
+def test_no_shuffle_among_whoever_is_active(path):
+    """The lanes of a warp's exchange follow from a condition, never from which of them happen to run together."""
+    assert "__activemask" not in open(path).read()
