@@ -431,9 +431,11 @@ struct Tensor {
   int type = -1;  // W8A8_TYPE_*, 3 for int32, 4 for int64
   bool given() const { return o != nullptr; }
   bool contiguous() const {
+    for (int i = 0; i < dims; ++i)
+      if (size[i] == 0) return true;  // of nothing
     long long s = 1;
     for (int i = dims - 1; i >= 0; --i) {
-      if (size[i] != 1 && stride[i] != s) return size[0] == 0;
+      if (size[i] != 1 && stride[i] != s) return false;
       s *= size[i];
     }
     return true;
