@@ -546,7 +546,7 @@ w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache
  * outputs of the same row can differ by the weights' rounding.
  * Deterministic: the same call gives the same bits, whatever runs beside it.
  * q and o [n_rows, n_q, head_dim] of the cache's type, strides in elements (multiples of 8); n_q a multiple of n_kv,
- * at most 128 query heads per key/value head; o overlaps no input. */
+ * at most 128 query heads per key/value head; o overlaps no input (o == q is refused). */
 w8a8_status w8a8_paged_attention_workspace_size(const w8a8_paged_cache* cache, int n_q, size_t* bytes);
 w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const w8a8_paged_batch* batch, const uint16_t* q,
                                  int64_t q_row, int64_t q_head, int n_q, float scale, int window, uint16_t* o,

@@ -687,8 +687,8 @@ def stream_workspace(nbytes: int, dev: torch.device, stream=None) -> torch.Tenso
 def paged_attention(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: Optional[float] = None, window: int = 0,
                     out: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
     """Attention of every row over its sequence's cached keys, its own included (append first).  scale defaults to
-    1 / sqrt(head_dim); window 0 sees all earlier keys.  Rows of no sequence: left as they were in `out`.  Without
-    `ws`, scratch of the stream's own (stream_workspace)."""
+    1 / sqrt(head_dim); window 0 sees all earlier keys.  Rows of no sequence: left as they were in `out`, which
+    shares no memory with q or the cache.  Without `ws`, scratch of the stream's own (stream_workspace)."""
     return (_CALLS or _calls()).paged_attention(cache, batch, q, scale, window, out, ws, stream)
 
 

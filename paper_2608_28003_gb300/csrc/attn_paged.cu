@@ -91,6 +91,7 @@ extern "C" w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const
                    who);
   W8A8_CHECK_ARG(o_row >= (n_q - 1) * o_head + dim || o_head >= (pb.n_rows - 1) * o_row + dim, W8A8_ERR_SHAPE,
                  "%s: o's rows overlap (strides %lld, %lld)", who, (long long)o_row, (long long)o_head);
+  W8A8_CHECK_ARG(o != q, W8A8_ERR_INVALID_ARG, "%s: o must not be q: other rows' pieces still read it", who);
   DevInfo d;
   W8A8_TRY(dev_info(&d));
   const size_t need = paged_attention_ws(dim, d.sms);

@@ -13,3 +13,15 @@ def B():
 def test_null_arguments(B):
     assert B.lib().w8a8_model_check(None, None) == 1
     assert B.lib().w8a8_paged_attention_error_word(None) == 1
+
+
+def test_attention_in_place_is_refused(B):
+    import ctypes
+    P = 0x10000  # an aligned address nothing reads
+    c = B.PagedCacheC(0, 4, 16, 2, 128, 4096, 256, 128, P, P)
+    b = B.PagedBatchC(2, 3, 2, 4, P, P, P)
+
+    def attn(o, ws):
+        return B.lib().w8a8_paged_attention(ctypes.byref(c), ctypes.byref(b), P, 1024, 128, 8, 0.1, 0, o, 1024, 128, ws, 0, None)
+    assert attn(P, P) == 1 and b"must not be q" in B.lib().w8a8_last_error()
+    assert attn(2 * P, P) != 1
