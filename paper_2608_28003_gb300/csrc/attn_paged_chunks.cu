@@ -492,6 +492,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         };
         auto exactly = [&](bool bad) {  // rows whose result is not finite, or without weight; all softmax warps
           uint32_t rest = __ballot_sync(0xffffffffu, live && bad);
+          __syncwarp();  // the lanes' stores of their rows come before the warp's below
           if constexpr (kSplit == 2) {  // in either half
             if (rest && lane == 0) atomicOr(&s_bad[warp & 3], rest);
             named_bar_sync(1, 32 * C::kSoft);
