@@ -34,6 +34,24 @@ __device__ __forceinline__ void give_up(unsigned int* err, const AttnCall& a, un
   atomicOr(a.gave_up, bits);
 }
 
+// mbar_wait_warp, whose limit begins again whenever `beat`, in shared memory, has moved: while a warp computes rows again exactly
+// (11 us a key for a warp's 32 rows at head dim 256, 3 s at 260000 keys), the others' copies and products wait for it.
+__device__ __forceinline__ bool wait_beat(uint32_t bar, uint32_t parity, const uint32_t* beat) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  long long t0 = clock64();
+  uint32_t seen = *reinterpret_cast<const volatile uint32_t*>(beat);
+  while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+    const uint32_t now = *reinterpret_cast<const volatile uint32_t*>(beat);
+    if (__any_sync(0xffffffffu, now != seen)) {
+      seen = now;
+      t0 = clock64();
+    } else if (__any_sync(0xffffffffu, clock64() - t0 > kWaitBudgetCycles)) {
+      return false;
+    }
+  }
+  return true;
+}
+
 // A row's reference moves when its maximum grew by 2^kGrowth, and weights are 2^kLift times what they are against it, so that they
 // stay within 2^8 in bf16 and 2^15 in fp16, where the largest are put near the type's end: weights down to 2^-26 of the
 // reference are normal numbers and those down to 2^-37 are counted (unlifted, 2^-14 and 2^-25: a tail of 40000 keys at
@@ -325,9 +343,10 @@ __device__ __forceinline__ Pieces pieces_of(const Walk& w, const LineStart& ls) 
 // in it, and nothing outside the row's range is read.  The kernels run it for rows whose result is not finite (a value
 // that only other rows of the tile may see can make it so, or sums of weights times values beyond fp32's range: here the
 // output so far is kept as an average, which stays within the values).  Lane l scores key j0 + l, then holds dims l, l + 32, ...
+// It counts `beat` up as it goes (see wait_beat).
 template <bool kBf16, int kDim>
 __device__ __noinline__ void attend_row(const PagedCache& c, const PagedBatch& b, const AttnCall& a, int s, int pos,
-                                        int64_t row, int head, int lane) {
+                                        int64_t row, int head, int lane, uint32_t* beat) {
   const uint16_t* q = a.q + row * a.q_row + head * a.q_head;
   const int kvh = head / (a.n_q / c.n_kv);
   const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
@@ -336,6 +355,7 @@ __device__ __noinline__ void attend_row(const PagedCache& c, const PagedBatch& b
 #pragma unroll
   for (int i = 0; i < kDim / 32; ++i) acc[i] = 0.0f;
   for (int j0 = lo; j0 <= pos; j0 += 32) {
+    if (lane == 0 && ((j0 - lo) & 8191) == 0) atomicAdd(beat, 1u);
     const int j = j0 + lane;
     const int64_t at = j <= pos ? key_offset(b, c, s, j, kvh) : -1;
     float sc = -INFINITY;

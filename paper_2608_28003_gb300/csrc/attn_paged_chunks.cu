@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   __shared__ LineStart ls;
   __shared__ long long scan[kThreads / 32];
   __shared__ uint32_t held[8];  // 16-key groups of a tile that lie in a page
-  __shared__ uint32_t tmem_slot, s_last, s_bad[4];
+  __shared__ uint32_t tmem_slot, s_last, s_bad[4], s_beat;
   __shared__ float s_max[C::kSplit][C::kSplit][kBq], s_sum[C::kSplit][kBq];  // two threads a row: what they tell each other
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t bar0 = smem_u32(bars);
@@ -127,6 +127,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 
   if (threadIdx.x < 4) s_bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
+    s_beat = 0;
     for (int i = 0; i < C::kBars; ++i)
       mbar_init(bar(i), (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive : 1);
     fence_mbar_init();
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         constexpr int kGroups = kBk / 16, kBatch = 32 / kGroups;  // tiles whose pages are read at once, ahead of their use
         int page = group_page(b, c, w.s, (w.first + w.k0) << kBkShift, lo, hi, box, lane), ahead = -1;
         if (!kv) {
-          if (item > 0 && !mbar_wait_warp(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) {
+          if (item > 0 && !wait_beat(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, &s_beat)) {
             ok = false;
             break;
           }
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (in_batch * kGroups)) & ((1u << kGroups) - 1u);
           for (int pt = 0; pt < C::kKParts; ++pt) {
             const int bi = st * C::kKParts + pt;
-            if (g >= C::kStages && !mbar_wait_warp(bar(free + bi), (uint32_t)(g / C::kStages - 1) & 1u, kWaitBudgetCycles)) {
+            if (g >= C::kStages && !wait_beat(bar(free + bi), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat)) {
               ok = false;
               break;
             }
@@ -215,9 +216,9 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       // the last copies land before the CTA may end
       if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
       constexpr int kRing = C::kStages * C::kKParts;
-      bool drained = kv || item == 0 || mbar_wait_warp(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles);
+      bool drained = kv || item == 0 || wait_beat(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, &s_beat);
       for (int k = max(0, issued - kRing); k < issued; ++k)
-        drained &= mbar_wait_warp(bar(full + k % kRing), (uint32_t)(k / kRing) & 1u, kWaitBudgetCycles);
+        drained &= wait_beat(bar(full + k % kRing), (uint32_t)(k / kRing) & 1u, &s_beat);
       if (!drained && lane == 0) give_up(err, a, DEVERR_DRAIN_WAIT);
     } else if (warp == kIssueWarp) {
       // ---------------------------------------------------------------------- MMAs
@@ -231,7 +232,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll 1
         for (int pt = 0; pt < C::kKParts; ++pt) {
           if (rt == 0 &&
-              !mbar_wait_warp(bar(C::K_FULL + st * C::kKParts + pt), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+              !wait_beat(bar(C::K_FULL + st * C::kKParts + pt), (uint32_t)(i / C::kStages) & 1u, &s_beat))
             return false;
           tc_fence_after();
           if (elect_one()) {
@@ -254,15 +255,15 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       // O += P V of key tile i for row tile rt, in two halves as P comes; hands V back after the last row tile
       auto issue_pv = [&](int i, int rt, bool first, bool last) {
         const int st = i % C::kStages, slot = kRt == 2 ? rt : i & 1;
-        if (first && item > 0 && !mbar_wait_warp(bar(C::O_FREE + rt), (uint32_t)(item - 1) & 1u, kWaitBudgetCycles)) return false;
+        if (first && item > 0 && !wait_beat(bar(C::O_FREE + rt), (uint32_t)(item - 1) & 1u, &s_beat)) return false;
         const uint64_t dv = sdesc_mn(base + (uint32_t)(C::kOffV + st * C::kTile), kSub);
         const uint32_t p = tmem + 128u * (uint32_t)slot, o = tmem + kOCol + (uint32_t)(rt * kDim);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          if (!mbar_wait_warp(bar(C::P_FULL + 2 * slot + half), (uint32_t)(kRt == 2 ? i : i >> 1) & 1u, kWaitBudgetCycles))
+          if (!wait_beat(bar(C::P_FULL + 2 * slot + half), (uint32_t)(kRt == 2 ? i : i >> 1) & 1u, &s_beat))
             return false;
           if constexpr (C::kVParts == 1) {
-            if (rt == 0 && half == 0 && !mbar_wait_warp(bar(C::V_FULL + st), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+            if (rt == 0 && half == 0 && !wait_beat(bar(C::V_FULL + st), (uint32_t)(i / C::kStages) & 1u, &s_beat))
               return false;
             tc_fence_after();
             if (elect_one()) {
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const int vp = half + 2 * j;  // 32 keys
-              if (!mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles))
+              if (!wait_beat(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(i / C::kStages) & 1u, &s_beat))
                 return false;
               tc_fence_after();
               if (elect_one()) {
@@ -302,7 +303,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         return true;
       };
       for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
-        ok = mbar_wait_warp(bar(C::Q_FULL), (uint32_t)item & 1u, kWaitBudgetCycles);
+        ok = wait_beat(bar(C::Q_FULL), (uint32_t)item & 1u, &s_beat);
 #pragma unroll
         for (int rt = 0; rt < kRt; ++rt) ok = ok && issue_s(g, rt, w.cnt == 1);
         for (int i = 0; ok && i < w.cnt; ++i, ++g) {
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         for (int i = 0; i < w.cnt; ++i, ++g) {
           const int j0 = (w.first + w.k0 + i) << kBkShift, slot = kRt == 2 ? rt : g & 1;
           const uint32_t stm = lanes + 128u * (uint32_t)slot;
-          if (ok && !mbar_wait_warp(bar(C::S_FULL + slot), (uint32_t)(kRt == 2 ? g : g >> 1) & 1u, kWaitBudgetCycles)) ok = false;
+          if (ok && !wait_beat(bar(C::S_FULL + slot), (uint32_t)(kRt == 2 ? g : g >> 1) & 1u, &s_beat)) ok = false;
           if (!ok) continue;
           tc_fence_after();
           uint32_t x[32];
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           if constexpr (kSplit == 2) {  // the row's other thread
             s_max[g & 1][hf][r] = top;
             mbar_arrive(bar(C::X_FULL));
-            if (!mbar_wait_warp(bar(C::X_FULL), (uint32_t)g & 1u, kWaitBudgetCycles)) {
+            if (!wait_beat(bar(C::X_FULL), (uint32_t)g & 1u, &s_beat)) {
               ok = false;
               continue;
             }
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             }
             if (i > 0 && __any_sync(0xffffffffu, grown)) {
               // O is the previous products' (with two row tiles their order ahead of this S says so already)
-              if (kRt == 1 && !mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles)) {
+              if (kRt == 1 && !wait_beat(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, &s_beat)) {
                 ok = false;
                 continue;
               }
@@ -409,11 +410,10 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             // of the tile, once its copies have landed
             const int st = g % C::kStages;
             // with one row tile and stage, the values of the tile before may not have landed yet: its product has them
-            bool landed = kRt == 2 || i == 0 || mbar_wait_warp(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, kWaitBudgetCycles);
+            bool landed = kRt == 2 || i == 0 || wait_beat(bar(C::PV_DONE), (uint32_t)(g - 1) & 1u, &s_beat);
 #pragma unroll
             for (int vp = 0; vp < C::kVParts; ++vp)
-              landed = landed && mbar_wait_warp(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(g / C::kStages) & 1u,
-                                                kWaitBudgetCycles);
+              landed = landed && wait_beat(bar(C::V_FULL + st * C::kVParts + vp), (uint32_t)(g / C::kStages) & 1u, &s_beat);
             if (!landed) {
               ok = false;
               continue;
@@ -462,8 +462,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           l += s0 + s1;
         }
         // the item's last product
-        if (ok && !mbar_wait_warp(bar(kRt == 2 ? C::PV_DONE + rt : C::PV_DONE + 1), (uint32_t)(kRt == 2 ? g - 1 : item) & 1u,
-                                  kWaitBudgetCycles))
+        if (ok && !wait_beat(bar(kRt == 2 ? C::PV_DONE + rt : C::PV_DONE + 1), (uint32_t)(kRt == 2 ? g - 1 : item) & 1u, &s_beat))
           ok = false;
         if (!ok && lane == 0) give_up(err, a, DEVERR_CONSUMER_WAIT);
         __syncwarp();
@@ -505,7 +504,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             const int src = __ffs(rest) - 1;
             attend_row<kBf16, kDim>(c, b, a, w.s, __shfl_sync(0xffffffffu, pos, src),
                                     (int64_t)w.q.row0 + __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src),
-                                    lane);
+                                    lane, &s_beat);
           }
         };
         if (w.whole()) {

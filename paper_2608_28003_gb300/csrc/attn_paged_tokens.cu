@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   __shared__ long long scan[C::kThreads / 32];
   __shared__ uint32_t held[C::kStages];                    // 16-key groups of a stage's tile that lie in a page
   __shared__ float s_m[C::kWarps][kRows], s_l[C::kWarps][kRows];
-  __shared__ uint32_t s_last, s_bad;
+  __shared__ uint32_t s_last, s_bad, s_beat;
   const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
   float2* join = reinterpret_cast<float2*>(smem_raw + (ring - raw) + C::kStages * C::kStage);
   const uint32_t bar0 = smem_u32(bars);
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     fence_mbar_init();
     prefetch_tmap(&tmK);
     prefetch_tmap(&tmV);
-    s_bad = 0;
+    s_bad = s_beat = 0;
   }
   pdl_wait();
   pdl_trigger();
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           if (i + kBatch < w.cnt) ahead = group_page(b, c, w.s, tile0 + (kBatch << C::kBkShift), lo, hi, box, lane);
         }
         const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (in_batch * kGroups)) & ((1u << kGroups) - 1u);
-        if (g >= C::kStages && !mbar_wait_warp(empty(st), (uint32_t)(g / C::kStages - 1) & 1u, kWaitBudgetCycles)) {
+        if (g >= C::kStages && !wait_beat(empty(st), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat)) {
           ok = false;
           break;
         }
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     // the last copies land before the CTA may end
     if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
     for (int k = max(0, g - C::kStages); k < g; ++k)
-      if (!mbar_wait_warp(full(k % C::kStages), (uint32_t)(k / C::kStages) & 1u, kWaitBudgetCycles) && lane == 0)
+      if (!wait_beat(full(k % C::kStages), (uint32_t)(k / C::kStages) & 1u, &s_beat) && lane == 0)
         give_up(err, a, DEVERR_DRAIN_WAIT);
     return;
   }
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     for (int i = 0; i < w.cnt; ++i, ++g) {
       constexpr int kBlocks = C::kBlocks;
       const int st = g % C::kStages, j0 = ((w.first + w.k0 + i) << C::kBkShift) + 16 * kBlocks * warp;
-      if (ok && !mbar_wait_warp(full(st), (uint32_t)(g / C::kStages) & 1u, kWaitBudgetCycles)) ok = false;
+      if (ok && !wait_beat(full(st), (uint32_t)(g / C::kStages) & 1u, &s_beat)) ok = false;
       if (!ok) continue;
       const uint32_t there = held[st] >> (kBlocks * warp) & ((1u << kBlocks) - 1u);
       if (there != 0 && j0 <= hi && j0 + 16 * kBlocks - 1 >= lo) {
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       for (int r = warp; r < rows; r += C::kWarps) {
         if (!((bad >> r) & 1u)) continue;
         const int tok = tok0 + r / group;
-        attend_row<kBf16, kDim>(c, b, a, w.s, w.q.pos0 + tok, w.q.row0 + tok, w.h * group + r % group, lane);
+        attend_row<kBf16, kDim>(c, b, a, w.s, w.q.pos0 + tok, w.q.row0 + tok, w.h * group + r % group, lane, &s_beat);
       }
       named_bar_sync(kBar, kConsumers);
     };
