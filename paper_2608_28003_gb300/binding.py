@@ -278,6 +278,8 @@ class Workspace:
 
     def get(self, nbytes: int) -> torch.Tensor:
         if self.buf.numel() < nbytes:
+            if self.buf.is_cuda:  # calls of this stream may still use it
+                self.buf.record_stream(torch.cuda.current_stream(self.buf.device))
             self.buf = torch.zeros(int(nbytes * 1.25) + 256, dtype=torch.uint8, device=self.device)
         return self.buf
 
@@ -572,6 +574,12 @@ def _need(cond, msg):
         raise ValueError(msg)
 
 
+def _on(stream):
+    """A call on `stream`: outputs and scratch that it makes belong to that stream, so that work still queued on another
+    one that had their memory before cannot reach it."""
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
 def _ints(t, name):
     _need(t.dtype == torch.int32 and t.is_contiguous(), f"{name} must be a contiguous int32 tensor")
 
@@ -621,7 +629,10 @@ def rope_table(cfg: RopeConfig, device=None) -> RopeTable:
 def rope(table: RopeTable, x: torch.Tensor, positions: torch.Tensor, out: Optional[torch.Tensor] = None,
          stream=None) -> torch.Tensor:
     """x [T, heads, dim] (bf16 or fp16) rotated at positions [T] int32; out=x rotates in place."""
-    return (_CALLS or _calls()).rope(table, x, positions, out, stream)
+    if stream is not None:
+        with _on(stream):
+            return rope(table, x, positions, out)
+    return (_CALLS or _calls()).rope(table, x, positions, out, None)
 
 
 @dataclass
@@ -665,7 +676,10 @@ def rope_append(table: RopeTable, cache: PagedCache, batch: PagedBatch, q: torch
                 q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Rotated (and, with the norms, RMS-normalised) q heads, returned; k heads likewise and v heads into the
     cache's pages.  q [rows, n_q, dim], k and v [rows, n_kv, dim]: views of one projection are fine; q_out=q is too."""
-    return (_CALLS or _calls()).rope_append(table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out, stream)
+    if stream is not None:
+        with _on(stream):
+            return rope_append(table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out)
+    return (_CALLS or _calls()).rope_append(table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out, None)
 
 
 _STREAM_WS = {}
@@ -689,7 +703,10 @@ def paged_attention(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale
     """Attention of every row over its sequence's cached keys, its own included (append first).  scale defaults to
     1 / sqrt(head_dim); window 0 sees all earlier keys.  Rows of no sequence: left as they were in `out`, which
     shares no memory with q or the cache.  Without `ws`, scratch of the stream's own (stream_workspace)."""
-    return (_CALLS or _calls()).paged_attention(cache, batch, q, scale, window, out, ws, stream)
+    if stream is not None:
+        with _on(stream):
+            return paged_attention(cache, batch, q, scale, window, out, ws)
+    return (_CALLS or _calls()).paged_attention(cache, batch, q, scale, window, out, ws, None)
 
 
 def paged_attention_check(stream=None) -> None:
@@ -704,7 +721,10 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     """One token a row of logits [M, V] (fp32, bf16, fp16) from uniform numbers u [M] fp32; per-row parameters [M]
     (temperature, top_p, min_p fp32, top_k int32; None: 1 and off).  Returns tokens int32 [M], or (tokens, their
     probabilities among the kept ones) with want_probs."""
-    return (_CALLS or _calls()).sample(logits, u, temperature, top_k, top_p, min_p, want_probs, tokens, stream)
+    if stream is not None:
+        with _on(stream):
+            return sample(logits, u, temperature, top_k, top_p, min_p, want_probs, tokens)
+    return (_CALLS or _calls()).sample(logits, u, temperature, top_k, top_p, min_p, want_probs, tokens, None)
 
 
 # ------------------------------------------------------------------------------- decoder
@@ -925,6 +945,9 @@ class Decoder:
         [layers, n_pages, page_size, n_kv, head_dim] bf16, and the next token of every sequence: sampled from u
         [n_seqs] with the given parameters (sample), or the largest logit's where u is None.  Returns (next
         [n_seqs], logits [n_seqs, vocab] or None, probabilities or None); a call without rows gives -1 and zeros."""
+        if stream is not None:
+            with _on(stream):
+                return self.step_paged(tokens, k, v, batch, u, temperature, top_k, top_p, min_p, want_logits, want_probs)
         dev = self._keep[0]["embed"].device
         _need(k.dim() == 5 and k.shape[0] == self.cfg.layers and k.stride() == v.stride() and k.shape == v.shape,
               "k and v must be [layers, n_pages, page_size, n_kv, head_dim] of equal strides")
@@ -948,7 +971,7 @@ class Decoder:
         sp = SamplingC(*(None if t is None else t.data_ptr() for t in (temperature, top_k, top_p, min_p)))
         _check("w8a8_decoder_step_paged", lib().w8a8_decoder_step_paged(
             self.h, _p(tokens), ctypes.byref(bc), ctypes.byref(cc), k.stride(0), ctypes.byref(sp) if u is not None else None,
-            _p(u), _p(logits), _p(nxt), _p(probs), _stream(stream)))
+            _p(u), _p(logits), _p(nxt), _p(probs), _stream()))
         return nxt, logits if want_logits else None, probs
 
     def check(self, stream=None) -> None:
