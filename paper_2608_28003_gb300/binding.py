@@ -270,7 +270,9 @@ def _bits(t: torch.Tensor) -> torch.Tensor:
 
 # ------------------------------------------------------------------------------ workspace
 class Workspace:
-    """A zero-initialised device byte buffer, grown on demand (re-zeroed when regrown)."""
+    """A zero-initialised device byte buffer, grown on demand (re-zeroed when regrown).  While a stream is captured it does
+    not grow: a call that needs more gets scratch of the graph's own, zeroed at each replay (grow it before, with get, where
+    workspace_check is to see the graph's calls)."""
 
     def __init__(self, device=None):
         self.device = device or torch.device("cuda")
@@ -278,6 +280,8 @@ class Workspace:
 
     def get(self, nbytes: int) -> torch.Tensor:
         if self.buf.numel() < nbytes:
+            if self.buf.is_cuda and torch.cuda.is_current_stream_capturing():
+                return torch.zeros(nbytes, dtype=torch.uint8, device=self.device)
             if self.buf.is_cuda:  # calls of this stream may still use it
                 self.buf.record_stream(torch.cuda.current_stream(self.buf.device))
             self.buf = torch.zeros(int(nbytes * 1.25) + 256, dtype=torch.uint8, device=self.device)
@@ -290,7 +294,10 @@ _DEFAULT_WS = {}
 def default_workspace() -> Workspace:
     dev = torch.cuda.current_device()
     if dev not in _DEFAULT_WS:
-        _DEFAULT_WS[dev] = Workspace(torch.device("cuda", dev))
+        ws = Workspace(torch.device("cuda", dev))
+        if torch.cuda.is_current_stream_capturing():
+            return ws  # the graph's own
+        _DEFAULT_WS[dev] = ws
     return _DEFAULT_WS[dev]
 
 
