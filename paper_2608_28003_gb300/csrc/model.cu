@@ -470,7 +470,7 @@ extern "C" w8a8_status w8a8_model_create(const w8a8_model_cfg* cfg, const w8a8_l
     const w8a8_rope_cfg rc{c.head_dim, W8A8_ROPE_NONE, (double)(g ? c.rope_global : c.rope_local), 1.0, 1.0, 4.0, 1.0, 0};
     std::vector<uint64_t> turns((size_t)c.head_dim / 2);
     uint64_t* dev = nullptr;
-    if (rc.base <= 1.0) continue;  // (a base without rotations to speak of: the paged step refuses it)
+    if (!(rc.base > 1.0 && std::isfinite(rc.base))) continue;  // (a base without rotations to speak of: the paged step refuses it)
     W8A8_MTRY(w8a8_rope_frequencies(&rc, turns.data(), &rt.scale));
     W8A8_MTRY(dalloc(m, &dev, turns.size()));
     W8A8_MTRY(cudaMemcpy(dev, turns.data(), turns.size() * sizeof(uint64_t), cudaMemcpyHostToDevice) == cudaSuccess

@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+import synth
+
 pytestmark = pytest.mark.gpu
 
 
@@ -31,3 +33,20 @@ def test_a_page_table_without_columns(B, dim, new):
     assert torch.equal(q, B.rope(table, x[:, :4], pos))
     assert bool((cache.k == 3).all()) and bool((cache.v == 3).all())
     assert bool((B.paged_attention(cache, batch, q) == 0).all())
+
+
+@pytest.mark.parametrize("base", [float("inf"), 1.0, 0.5])
+def test_a_decoder_whose_rope_base_the_paged_step_refuses(B, base):
+    """Such a model is made, and its own cache's calls run, as they did before there was a paged step."""
+    _, bf, norms = synth.decoder_weights(1, 1152, 256, 512, n_q=4, n_kv=1, seed=2)
+    w = {k: [t.cuda() for t in v] if isinstance(v, list) else v.cuda() for k, v in bf.items()}
+    n = {k: [torch.from_numpy(a).cuda() for a in v] if isinstance(v, list) else torch.from_numpy(v).cuda()
+         for k, v in norms.items()}
+    dec = B.Decoder(B.DecoderConfig(max_batch=1, max_seq=64, max_tokens=64, layers=1, inter=256, vocab=512, window=64,
+                                    global_layers=(), rope_local=base), w, n)
+    toks = torch.arange(12, dtype=torch.int32, device="cuda").view(1, 12)
+    assert bool(torch.isfinite(dec.forward(toks, 0)[0]).all())
+    k = torch.zeros(1, 1, 16, 1, 256, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(B.W8A8Error) as e:
+        dec.step_paged(toks[0], k, k.clone(), B.PagedBatch(_i32([0, 12]), _i32([12]), _i32([[0]]), max_new=12))
+    assert e.value.status == 5
