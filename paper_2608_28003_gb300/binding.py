@@ -674,6 +674,7 @@ class PagedBatch:
               "row_start [n_seqs + 1], kv_len [n_seqs], pages [n_seqs, max_pages]")
         for name in ("row_start", "kv_len", "pages"):
             _ints(getattr(self, name), name)
+        _need(-1 << 31 <= self.max_new < 1 << 31, "max_new does not fit in 32 bits")
         return PagedBatchC(n, rows, self.max_new, self.pages.shape[1], self.row_start.data_ptr(), self.kv_len.data_ptr(),
                            self.pages.data_ptr())
 

@@ -90,6 +90,10 @@ bool ptr_attr(PyObject* o, PyObject* name, T** out) {
 bool int_attr(PyObject* o, PyObject* name, int32_t* out) {
   long long v;
   if (!as_int(PyObject_GetAttr(o, name), &v)) return false;
+  if (v < INT32_MIN || v > INT32_MAX) {
+    PyErr_Format(PyExc_ValueError, "%U does not fit in 32 bits", name);
+    return false;
+  }
   *out = (int32_t)v;
   return true;
 }
@@ -481,6 +485,8 @@ bool tensor(PyObject* o, long long* dev, Tensor* t) {
   if (!need(d == *dev, "all tensors must be on one device") || !tuple_of(PyObject_GetAttr(o, s_shape), &t->dims, t->size) ||
       !tuple_of(call0(o, s_stride), &n, t->stride) || !ptr_of(o, &t->ptr))
     return false;
+  for (int i = 0; i < t->dims; ++i)
+    if (!need(t->size[i] <= INT32_MAX, "a tensor's extent does not fit in 32 bits")) return false;
   Ref dt(PyObject_GetAttr(o, s_dtype));
   if (!dt) return false;
   t->type = dt.p == g_bf16  ? W8A8_TYPE_BF16
@@ -706,7 +712,7 @@ PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const long long M = x.size[0], V = x.size[1];
   if (!vector(u, M, W8A8_TYPE_F32, "u must be fp32 [M]") || !vector(temp, M, W8A8_TYPE_F32, "temperature must be fp32 [M]") ||
       !vector(k, M, kInt32, "top_k must be int32 [M]") || !vector(p, M, W8A8_TYPE_F32, "top_p must be fp32 [M]") ||
-      !vector(mp, M, W8A8_TYPE_F32, "min_p must be fp32 [M]") || !need(V <= 0x7fffffffLL, "V out of range") ||
+      !vector(mp, M, W8A8_TYPE_F32, "min_p must be fp32 [M]") ||
       !output(a[7], a[1], g_i32, &y) || !tensor(y.p, &dev, &tok) || !vector(tok, M, kInt32, "tokens must be int32 [M]"))
     return nullptr;
   if (want && (!output(Py_None, a[1], nullptr, &z) || !tensor(z.p, &dev, &prob))) return nullptr;

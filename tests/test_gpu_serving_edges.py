@@ -50,3 +50,19 @@ def test_a_decoder_whose_rope_base_the_paged_step_refuses(B, base):
     with pytest.raises(B.W8A8Error) as e:
         dec.step_paged(toks[0], k, k.clone(), B.PagedBatch(_i32([0, 12]), _i32([12]), _i32([[0]]), max_new=12))
     assert e.value.status == 5
+
+
+def test_numbers_beyond_32_bits_are_refused(B):
+    """They were cut to their lower half: one row of 2^32 + 1 was sampled, and the other tokens left unwritten."""
+    n = (1 << 32) + 1
+    logits, u = torch.zeros(1, 8, device="cuda").expand(n, 8), torch.empty(n, device="cuda")
+    with pytest.raises(ValueError, match="32 bits"):
+        B.sample(logits, u)
+    del u
+    k = torch.zeros(1, 16, 1, 64, device="cuda", dtype=torch.bfloat16)
+    batch = B.PagedBatch(_i32([0, 2]), _i32([2]), _i32([[0]]), max_new=n)
+    q = torch.zeros(2, 4, 64, device="cuda", dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="32 bits"):
+        B.paged_attention(B.PagedCache(k, k), batch, q)
+    with pytest.raises(ValueError, match="32 bits"):
+        batch.c(2)
