@@ -529,7 +529,7 @@ typedef struct {
  * position, rounded once; v heads to the cache as they are.  q [n_rows, n_q, head_dim], k and v
  * [n_rows, n_kv, head_dim], heads contiguous, row strides in elements (multiples of 8); q_out [n_rows, n_q, head_dim]
  * with its row stride, q itself allowed.  Everything has the cache's type.  Rows that share a slot (a page id twice in
- * one batch) leave either one's values there. */
+ * one batch) leave some row's values in each 16 bytes of it. */
 w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache* cache, const w8a8_paged_batch* batch,
                              const uint16_t* q, int64_t q_row, int n_q, const uint16_t* k, int64_t k_row,
                              const uint16_t* v, int64_t v_row, const float* q_norm, const float* k_norm, float eps,

@@ -34,9 +34,9 @@ w8a8_status gave_up_word(unsigned int** word) {
 }  // namespace
 
 // Up to 16 rows a sequence and key/value head go to the kernel for tokens, more to the one for chunks (a longer sequence in
-// the batch is right in either): 64 sequences of 4000 keys, 1 head of 256, take 55.7, 64.9 and 96.9 us for 4, 16 and 32 rows
-// there and 68.3 here; 40 sequences of 4 heads of 128 70.3 and 124 us for 16 and 32 rows there, 72.9 and 73.5 here; of 8
-// heads of 64 67.3 and 120 us for 15 and 30 rows there, 109 and 108 here.
+// the batch is right in either): 64 sequences of 4000 keys, 1 head of 256, take 54.5, 63.6 and 95.4 us for 4, 16 and 32 rows
+// there and 60 here; 40 sequences of 4 heads of 128 69.5 and 121 us for 16 and 32 rows there, 71 here; of 8
+// heads of 64 67.4 and 121 us for 15 and 30 rows there, 115 here.
 w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, const AttnCall& call, void* ws, int sms,
                                    cudaStream_t st) {
   const int group = call.n_q / pc.n_kv;

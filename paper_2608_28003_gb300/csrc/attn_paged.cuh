@@ -8,8 +8,8 @@
 // pieces: a fixed order, so results do not depend on who was last.  Where stretches are short (kShort tiles), two cut items
 // a worker would cost more than the balance gains: if items cut into pieces of at most `unit` tiles, for a unit of up to twice the
 // even share, make no more pieces than there are workers, each worker takes one piece.  A prompt of 2048 tokens at head
-// dim 256 (4 tiles a worker) takes 27.9 us so, and 35.4 in equal stretches; 32 single tokens in a window of 1024 (4) 16.7
-// and 19.6; 160 items of 10 tiles (11) 40.3 and 39.5, which is where kShort comes from.  Lengths are read on the device, so
+// dim 256 (4 tiles a worker) takes 28.5 us so, and 37.7 in equal stretches; 32 single tokens in a window of 1024 (4) 16.6
+// and 19.6; 160 items of 10 tiles (11) 40.2 and 39.9, which is where kShort comes from.  Lengths are read on the device, so
 // a captured call follows them.
 #pragma once
 

@@ -23,10 +23,12 @@
 //
 // What bounds it.  At head dims 64 and 128 the chain S -> maximum -> exponentials -> P V of a row tile, about 3100 cycles a
 // tile of keys where the products take 2048: four chunks of 1001 tokens behind up to 9000 keys, 28 heads over 4 of 128, take
-// 178 us (690 TFLOP/s, 0.37 of the measured rate; 217 with P in one piece after the rescaling).  Tried and slower: a part of
+// 180 to 183 us (680 TFLOP/s, 0.36 of the measured rate; 217 with P in one piece after the rescaling).  Tried and slower: a part of
 // the exponentials as a polynomial (an eighth 180 us, a quarter 184, half 207: issue slots, not the special function unit,
 // are short), two threads a row for both row tiles (211: 96 registers), scores loaded ahead or kept in registers (189 and
-// 233: spills).  A whole prompt of 2048 tokens at head dim 256 takes 28.4 us.  There every CTA copies all of its K and V from L2;
+// 233: spills, at the 168 registers that all of the block's threads have; not tried with shares of different size).  A whole
+// prompt of 2048 tokens at head dim 256 takes 28.5 us, four key tiles a CTA: latency from step to step, of which the parts
+// that were timed (lookup 2, first tile 3, key tiles 7, partials and their join 8) make two thirds.  There every CTA copies all of its K and V from L2;
 // a pair of CTAs, each copying half for both, took 27.9, and 67.2 us instead of 71.9 for a larger chunk, but a copy to several
 // CTAs has no place in a library that also runs on several GPUs.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.

@@ -13,8 +13,9 @@
 //
 // Measured: 64 sequences of up to 30000 keys at head dim 256 (934 MB) 147-151 us, 6.2-6.4 TB/s (0.91-0.94 of the measured
 // copy); 20 sequences of 4 drafted tokens behind up to 5000 keys, 8 heads of 64 in pages of 16 (98 MB, 160 items of about 10
-// tiles) 40.3 us: 5 until the first tile is there, and an item's end costs 2 to 3 (the warps' join, and for a cut item the
-// partial, its arrival and the join of the pieces); one sequence of 700 keys 10.9 us, latency alone.
+// tiles) 40.3 us: 5 until the first tile is there, 15 of copies, and an item's end costs 2 to 3 (the warps' join, and for a cut
+// item the partial, its arrival and the join of the pieces), twice a CTA; the rest, a third, is not accounted for.  One
+// sequence of 700 keys 11 to 12 us, latency alone.
 #include "attn_paged.cuh"
 #include "ops.cuh"
 #include "tmap.cuh"

@@ -60,8 +60,9 @@ w8a8_status run_ffn(const w8a8_ffn_weights* f, int precision, const uint16_t* X,
                     const PreCodes* pre_gate_up = nullptr);
 // rn (decode only): the call's input is computed from the decoder's residual step inside the
 // decode GEMV (X is ignored); W8A8_ERR_SHAPE when the decode GEMV does not take the call.
+bool decode_gemv_takes(bool int8, int M, int N, int K, bool geglu, int sms);
+
 w8a8_status launch_sample(int dtype, const void* logits, int64_t row_stride, int M, int V, const w8a8_sampling& sp,
                           const float* u, int32_t* tokens, float* probs, int sms, cudaStream_t st);
-bool decode_gemv_takes(bool int8, int M, int N, int K, bool geglu, int sms);
 
 }  // namespace w8a8

@@ -10,8 +10,9 @@
 // holds one unit of 16 dims (8 pairs: two 16-byte loads) and walks the heads of one row with a fixed step, so
 // that the 8 sines and cosines are computed once for all of its heads; the loads of four heads fly over the sines.
 // Measured: 8192 rows, half of every head rotated (134 MB) 23.9 us, 5.6 TB/s (0.83 of the measured copy; floor 19.8); the
-// append of 2400 rows of 16 + 8 heads of 128 (30 MB, floor 4.4) 11.4 us: one wave of threads, of which the wait for a row's
-// sequence, length and page, one after the other, is a third; 16 and 48 rows 7.1 and 10.5 us, the launch and its arguments.
+// append of 2400 rows of 16 + 8 heads of 128 (30 MB, floor 4.4) 11.4 to 14 us from one machine to the next: one wave of threads, of which
+// the wait for a row's sequence, length and page, one after the other, is a third (the rows' loads, which need none of them, come
+// after it); 16 and 48 rows 7 to 9 and 10.5 to 12 us, the launch and its arguments.
 #include <cmath>
 
 #include "ops.cuh"

@@ -5,7 +5,7 @@
 // exponential would not do: a flat row of 262144 logits has steps of 2^-18 in the sum, and weights off by 2^-24
 // or, far from the maximum, by 2^-19 would move the token in a noticeable share of draws.  So the exponent is kept with its
 // rounding errors (two-term difference and product) and 2^y comes from a table of 128 values and a cubic whose small part alone is
-// rounded in fp32: 2^-29 of the weight, in about 25 instructions (two logits at a time in packed fp32; the same
+// rounded in fp32: off by one to two steps of 2^-29 of the weight, within the 2^-27 that is promised, in about 25 instructions (two logits at a time in packed fp32; the same
 // in 32-bit integer products took three times as long).
 //
 // The work.  A cluster of up to 16 CTAs takes a row: the maximum; then, where a filter needs it, a histogram with a bin per 1/64
