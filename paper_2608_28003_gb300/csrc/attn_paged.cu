@@ -41,6 +41,7 @@ w8a8_status launch_paged_attention(const PagedCache& pc, const PagedBatch& pb, c
                                    cudaStream_t st) {
   const int group = call.n_q / pc.n_kv;
   AttnCall a = call;
+  if (a.window >= 1 << 30) a.window = 0;  // beyond every position, and negative ones less it would not fit in 32 bits
   W8A8_TRY(gave_up_word(&a.gave_up));
   return (long long)a.max_new * group <= 16 ? launch_attn_tokens(pc, pb, a, ws, sms, st)
                                             : launch_attn_chunks(pc, pb, a, ws, sms, st);
@@ -82,7 +83,6 @@ extern "C" w8a8_status w8a8_paged_attention(const w8a8_paged_cache* cache, const
   W8A8_CHECK_ARG(window >= 0 && std::isfinite(scale) && scale > 0.0f, W8A8_ERR_INVALID_ARG, "%s: window %d, scale %g", who,
                  window, (double)scale);
   if (pb.n_seqs == 0 || pb.n_rows == 0) return W8A8_OK;
-  if (window >= (1 << 30)) window = 0;  // beyond every position
   W8A8_CHECK_ARG(q && o, W8A8_ERR_INVALID_ARG, "%s: null pointer", who);
   W8A8_CHECK_ARG(aligned16(q) && aligned16(o), W8A8_ERR_ALIGN, "%s: q and o must be 16-byte aligned", who);
   const int64_t big = 1ll << 38, str[4] = {q_row, q_head, o_row, o_head};

@@ -66,3 +66,24 @@ def test_numbers_beyond_32_bits_are_refused(B):
         B.paged_attention(B.PagedCache(k, k), batch, q)
     with pytest.raises(ValueError, match="32 bits"):
         batch.c(2)
+
+
+@pytest.mark.parametrize("hint", [1, 40])  # either kernel
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_a_decoder_without_a_window_and_rows_at_negative_positions(B, new, hint):
+    """A window of 2^31 - 1 is none, also for sequences that have more rows than keys."""
+    _, bf, norms = synth.decoder_weights(1, 1152, 256, 512, n_q=4, n_kv=1, seed=2)
+    w = {k: [t.cuda() for t in v] if isinstance(v, list) else v.cuda() for k, v in bf.items()}
+    n = {k: [torch.from_numpy(a).cuda() for a in v] if isinstance(v, list) else torch.from_numpy(v).cuda()
+         for k, v in norms.items()}
+    toks = torch.arange(2 * new + 20, dtype=torch.int32, device="cuda")
+    got = []
+    for window in (64, (1 << 31) - 1, 0):
+        dec = B.Decoder(B.DecoderConfig(max_batch=4, max_seq=64, max_tokens=256, layers=1, inter=256, vocab=512, window=window,
+                                        global_layers=()), w, n)
+        k = torch.zeros(1, 4, 16, 1, 256, device="cuda", dtype=torch.bfloat16)
+        batch = B.PagedBatch(_i32([0, new, 2 * new, 2 * new + 20]), _i32([0, new // 2, 21]), _i32([[-1, -1], [2, 0], [1, 3]]),
+                             max_new=hint)
+        got.append(dec.step_paged(toks, k, k.clone(), batch, want_logits=True)[1])
+        B.paged_attention_check()
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
