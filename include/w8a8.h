@@ -491,8 +491,8 @@ typedef struct {
 /* y = x with every head's first rotary_dim dims rotated by its row's position, the others copied:
  *   (a, b) -> (a c - b s, b c + a s) with c, s = scale cos, scale sin of 2 pi frac(position turns / 2^64)
  * in fp32, rounded once to the type (bf16 or fp16).  x and y [T, heads, dim] with strides in elements
- * (multiples of 8); dim a multiple of 16 in [rotary_dim, 256].  y may be x itself (the same pointer and strides); any other overlap,
- * of the two or of y's own rows, is not allowed.  positions [T] int32, any value. */
+ * (multiples of 8); dim a multiple of 16 in [rotary_dim, 256]; at most 2^30 heads.  y may be x itself (the same pointer
+ * and strides); any other overlap, of the two or of y's own rows, is not allowed.  positions [T] int32, any value. */
 w8a8_status w8a8_rope(const w8a8_rope_table* rope, int dtype, const uint16_t* x, int64_t x_row, int64_t x_head, int T,
                       int heads, int dim, const int32_t* positions, uint16_t* y, int64_t y_row, int64_t y_head,
                       void* stream);

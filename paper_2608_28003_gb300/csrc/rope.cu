@@ -336,6 +336,7 @@ extern "C" w8a8_status w8a8_rope(const w8a8_rope_table* rope, int dtype, const u
                  who, dim, kMaxDim);
   W8A8_TRY(check_rope(who, rope, dim));
   if (T == 0 || heads == 0) return W8A8_OK;
+  W8A8_CHECK_ARG(heads <= 1 << 30, W8A8_ERR_SHAPE, "%s: more than 2^30 heads", who);  // a thread's steps over them fit in 32 bits
   W8A8_CHECK_ARG(x && y && positions, W8A8_ERR_INVALID_ARG, "%s: null pointer", who);
   W8A8_CHECK_ARG(aligned16(x) && aligned16(y) && (reinterpret_cast<uintptr_t>(positions) & 3u) == 0, W8A8_ERR_ALIGN,
                  "%s: x and y must be 16-byte aligned, positions 4-byte", who);
