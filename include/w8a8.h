@@ -598,6 +598,86 @@ w8a8_status w8a8_decoder_step_paged(w8a8_model* m, const int32_t* tokens, const 
                                     const w8a8_paged_cache* cache, int64_t layer_stride, const w8a8_sampling* sampling,
                                     const float* u, float* logits, int32_t* next, float* probs, void* stream);
 
+/* ======================================================================================
+ * Floating point of 4 bits (no counterpart in the paper, whose Future Work stops at FP8): linears with weights and
+ * activations, and a paged cache with keys and values, in e2m1 codes with a scale for every block of 16 or 32 values.
+ *
+ * A code is a sign (bit 3) and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0-2, in this order); two a byte, the even column
+ * in the low half.  A value is code * unit, unit the block's:
+ *   block 32  unit = 2^(b - 127), b the scale's byte (e8m0); 255 is NaN
+ *   block 16  unit = e4m3(scale byte) * row_scale[row]; 127 is NaN
+ * Quantisation of a row x[0 .. k), m the largest magnitude of a block:
+ *   block 32  unit = 2^max(floor(log2 m) - 2, -127), scale byte 0 where m = 0
+ *   block 16  row_scale = 2^p, p the smallest integer >= -126 with max |x| <= 2688 * 2^p (2688 = 6 * 448; 1 where every
+ *             block is 0), scale = e4m3(m / 6 / row_scale)
+ *   code = e2m1(x / unit), to the nearest, the even code at a tie, at most 6 in magnitude; 0 where the unit is 0
+ * All of it decided as in exact arithmetic.  A block that holds a NaN or an infinity is NaN as a whole (its codes are 0), and
+ * does not count for row_scale.
+ * ====================================================================================== */
+typedef struct {
+  int32_t rows, k;  /* k a multiple of 32, at most W8A8_MAX_K */
+  int32_t block;    /* 16 or 32 */
+  uint8_t* codes;   /* [rows, k / 2] */
+  uint8_t* scales;  /* w8a8_fp4_scale_bytes: block j of row r at byte ((r / 128) * G + j / 4) * 512 + (r % 32) * 16 +
+                       (r / 32) % 4 * 4 + j % 4, G = ceil(k / block / 4), the order the tensor cores read them in; bytes of no
+                       row or block are 0 */
+  float* row_scale; /* [rows] (block 16; NULL at block 32).  A weight's may hold any finite value */
+} w8a8_fp4;
+
+/* Bytes of scales of a [rows, k] matrix: ceil(rows / 128) * ceil(k / block / 4) * 512. */
+w8a8_status w8a8_fp4_scale_bytes(int rows, int k, int block, size_t* bytes);
+
+/* x [q->rows, q->k] (bf16, fp16 or fp32; the row stride in elements, a multiple of 16 bytes) into q. */
+w8a8_status w8a8_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4* q, void* stream);
+
+/* y = the values of q, rounded once to the type (exact in fp32 and in bf16 where row_scale is a power of two and the value
+ * within the type's range).  y's row stride in elements, a multiple of 16 bytes, at least k. */
+w8a8_status w8a8_fp4_dequantize(const w8a8_fp4* q, int dtype, void* y, int64_t y_row, void* stream);
+
+/* Y [M, N] = X W^T (+ bias): X [M, K] (bf16, fp16 or fp32) is quantised as w8a8_fp4_quantize does with the weight's block,
+ * then y_ti = sx_t * (sw_i * sum over the blocks of their units times the sum of code products), sx and sw the row scales,
+ * the sum in fp32; bias fp32 [N] is added in fp32 and the result rounded once to out_dtype (bf16, fp16 or fp32).  Row strides in
+ * elements: X's a multiple of 16 bytes, Y's at least N.  Y, 16-byte aligned, overlaps no input.  A NaN block of a row makes the
+ * row's (for a weight: the channel's) results NaN. */
+w8a8_status w8a8_fp4_linear_workspace_size(int M, int N, int K, int block, size_t* bytes);
+w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void* X, int64_t x_row, int M, const float* bias,
+                            int out_dtype, void* Y, int64_t y_row, void* workspace, size_t ws_bytes, void* stream);
+
+/* A paged cache in 4 bits: k and v codes [n_pages, page_size, n_kv, head_dim / 2] with common strides in bytes (multiples of 16,
+ * codes of a head contiguous), k_scales and v_scales e4m3 [n_pages, page_size, n_kv, head_dim / 16] with theirs (multiples of
+ * head_dim / 16 bytes): either order of slots and heads.  A value is code * scale * 2^k_exp (v_exp): the exponents, within
+ * [-100, 100], are the cache's and stay what they are while it holds anything.  page_size and head_dim as in
+ * w8a8_paged_cache. */
+typedef struct {
+  int32_t n_pages, page_size, n_kv, head_dim;
+  int32_t k_exp, v_exp;
+  int64_t page_stride, slot_stride, head_stride;
+  int64_t s_page_stride, s_slot_stride, s_head_stride;
+  uint8_t *k, *v, *k_scales, *v_scales;
+} w8a8_paged_cache_fp4;
+
+/* w8a8_rope_append into a 4-bit cache: the keys after norm and rotation and the values as they come are quantised by blocks of
+ * 16 dims with row_scale = 2^k_exp (2^v_exp); a block above 2688 times that is cut off at it.  The keys' codes are those of the
+ * formula in exact arithmetic, not of a rounded key.  dtype: of q, k, v and q_out, bf16 or fp16; q as in w8a8_rope_append. */
+w8a8_status w8a8_fp4_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache_fp4* cache,
+                                 const w8a8_paged_batch* batch, int dtype, const uint16_t* q, int64_t q_row, int n_q,
+                                 const uint16_t* k, int64_t k_row, const uint16_t* v, int64_t v_row, const float* q_norm,
+                                 const float* k_norm, float eps, uint16_t* q_out, int64_t q_out_row, void* stream);
+
+/* w8a8_paged_attention over a 4-bit cache: the same formula, row's ranges, checks, strides and guarantees, with the values the
+ * cache stands for as keys and values.  dtype: of q and o, bf16 or fp16. */
+w8a8_status w8a8_fp4_paged_attention_workspace_size(const w8a8_paged_cache_fp4* cache, int n_q, size_t* bytes);
+w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cache, const w8a8_paged_batch* batch, int dtype,
+                                     const uint16_t* q, int64_t q_row, int64_t q_head, int n_q, float scale, int window,
+                                     uint16_t* o, int64_t o_row, int64_t o_head, void* workspace, size_t ws_bytes,
+                                     void* stream);
+
+/* The values of the pages pages[0 .. n) (device int32; NULL: of all n = n_pages pages in order), keys to k_out and values to
+ * v_out, each contiguous [n, page_size, n_kv, head_dim] of the type (bf16, fp16 or fp32), rounded once; zeros for an id
+ * outside [0, n_pages).  Either output may be NULL. */
+w8a8_status w8a8_fp4_paged_values(const w8a8_paged_cache_fp4* cache, const int32_t* pages, int n, int dtype, void* k_out,
+                                  void* v_out, void* stream);
+
 /* Negative log-likelihood of targets under softmax(logits) per row (LM Head section's
  * perplexity): nll[i] = logsumexp(logits[i, :]) - logits[i, targets[i]], fp32. */
 w8a8_status w8a8_token_nll(const float* logits, const int32_t* targets, int M, int V, float* nll, void* stream);

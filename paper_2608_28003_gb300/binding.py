@@ -138,6 +138,19 @@ class SamplingC(ctypes.Structure):
     _fields_ = [("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp)]
 
 
+class Fp4C(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("k", ctypes.c_int32), ("block", ctypes.c_int32), ("codes", _vp), ("scales", _vp),
+                ("row_scale", _vp)]
+
+
+class PagedCacheFp4C(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("k_exp", ctypes.c_int32), ("v_exp", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("s_page_stride", ctypes.c_int64), ("s_slot_stride", ctypes.c_int64), ("s_head_stride", ctypes.c_int64),
+                ("k", _vp), ("v", _vp), ("k_scales", _vp), ("v_scales", _vp)]
+
+
 _fp = ctypes.POINTER(ctypes.c_float)
 _i64 = ctypes.c_int64
 
@@ -202,6 +215,17 @@ SIGNATURES = {
     "w8a8_sample": (_i32, [_i32, _vp, _i64, _i32, _i32, ctypes.POINTER(SamplingC), _vp, _vp, _vp, _vp]),
     "w8a8_decoder_step_paged": (_i32, [_vp, _vp, ctypes.POINTER(PagedBatchC), ctypes.POINTER(PagedCacheC), _i64,
                                        ctypes.POINTER(SamplingC), _vp, _vp, _vp, _vp, _vp]),
+    "w8a8_fp4_scale_bytes": (_i32, [_i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "w8a8_fp4_quantize": (_i32, [_i32, _vp, _i64, ctypes.POINTER(Fp4C), _vp]),
+    "w8a8_fp4_dequantize": (_i32, [ctypes.POINTER(Fp4C), _i32, _vp, _i64, _vp]),
+    "w8a8_fp4_linear_workspace_size": (_i32, [_i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "w8a8_fp4_linear": (_i32, [ctypes.POINTER(Fp4C), _i32, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _vp, _sz, _vp]),
+    "w8a8_fp4_rope_append": (_i32, [ctypes.POINTER(RopeTableC), ctypes.POINTER(PagedCacheFp4C), ctypes.POINTER(PagedBatchC),
+                                    _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]),
+    "w8a8_fp4_paged_attention_workspace_size": (_i32, [ctypes.POINTER(PagedCacheFp4C), _i32, ctypes.POINTER(_sz)]),
+    "w8a8_fp4_paged_attention": (_i32, [ctypes.POINTER(PagedCacheFp4C), ctypes.POINTER(PagedBatchC), _i32, _vp, _i64, _i64,
+                                        _i32, _f32, _i32, _vp, _i64, _i64, _vp, _sz, _vp]),
+    "w8a8_fp4_paged_values": (_i32, [ctypes.POINTER(PagedCacheFp4C), _vp, _i32, _i32, _vp, _vp, _vp]),
     "w8a8_token_nll": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp]),
     "w8a8_choose_mask": (_i32, [_fp, _fp, _fp, ctypes.POINTER(ctypes.c_int32), _i32, _f32, _f32]),
     "w8a8_allocate_mask": (_i32, [_vp, ctypes.POINTER(AllocOptsC), ctypes.POINTER(AllocReportC), _vp]),
@@ -733,6 +757,144 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
         with _on(stream):
             return sample(logits, u, temperature, top_k, top_p, min_p, want_probs, tokens)
     return (_CALLS or _calls()).sample(logits, u, temperature, top_k, top_p, min_p, want_probs, tokens, None)
+
+
+# ------------------------------------------------------------------------------- 4 bits
+@dataclass
+class Fp4Tensor:
+    """A matrix [rows, k] in floating point of 4 bits (w8a8_fp4): codes uint8 [rows, k / 2], the scales' bytes in the order the
+    tensor cores read them in, and for blocks of 16 the rows' scales fp32 [rows]."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    row_scale: Optional[torch.Tensor]
+    block: int
+
+    @property
+    def rows(self):
+        return self.codes.shape[0]
+
+    @property
+    def k(self):
+        return 2 * self.codes.shape[1]
+
+    def block_scales(self) -> torch.Tensor:
+        """The blocks' scale bytes as a plain uint8 matrix [rows, k / block]."""
+        n, g = self.rows, -(-self.k // self.block // 4)
+        t = self.scales.view(-(-n // 128), g, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(-1, 4 * g)
+        return t[:n, :self.k // self.block]
+
+    def c(self) -> Fp4C:
+        return Fp4C(self.rows, self.k, self.block, self.codes.data_ptr(), self.scales.data_ptr(),
+                    self.row_scale.data_ptr() if self.row_scale is not None else None)
+
+
+def fp4_tensor(codes: torch.Tensor, block_scales: torch.Tensor, row_scale: Optional[torch.Tensor] = None) -> Fp4Tensor:
+    """An Fp4Tensor of a matrix quantised elsewhere: codes uint8 [rows, k / 2], scale bytes uint8 [rows, k / 16] (e4m3) or
+    [rows, k / 32] (e8m0); row_scale fp32 [rows], 1 where it is not given (one scale for all rows: expanded)."""
+    _need(codes.dim() == 2 and block_scales.dim() == 2 and codes.shape[0] == block_scales.shape[0] and
+          codes.dtype == block_scales.dtype == torch.uint8, "codes [rows, k / 2] and block_scales [rows, k / block], uint8")
+    n, half = codes.shape
+    cols = block_scales.shape[1]
+    _need(half % 16 == 0 and (8 * cols == half or 16 * cols == half), "k must be a multiple of 32, blocks of 16 or 32")
+    block, g = 2 * half // cols, -(-cols // 4)
+    t = torch.zeros(-(-n // 128) * 128, 4 * g, dtype=torch.uint8, device=codes.device)
+    t[:n, :cols] = block_scales
+    t = t.view(-1, 4, 32, g, 4).permute(0, 3, 2, 1, 4).reshape(-1)
+    _need(block == 16 or row_scale is None, "blocks of 32 have no row_scale")
+    if block == 16:
+        row_scale = torch.ones(n, device=codes.device) if row_scale is None else row_scale.float().expand(n).contiguous()
+    return Fp4Tensor(codes.contiguous(), t.contiguous(), row_scale, block)
+
+
+def fp4_quantize(x: torch.Tensor, block: int = 16, stream=None) -> Fp4Tensor:
+    """x [rows, k] (bf16, fp16 or fp32) in floating point of 4 bits, by blocks of 16 (e4m3 scales under a power of two a row)
+    or 32 (scales that are powers of two): w8a8_fp4_quantize."""
+    if stream is not None:
+        with _on(stream):
+            return fp4_quantize(x, block)
+    return Fp4Tensor(*(_CALLS or _calls()).fp4_quantize(x, block, None), block)
+
+
+def fp4_dequantize(q: Fp4Tensor, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """The values of q [rows, k], rounded once to the type."""
+    if stream is not None:
+        with _on(stream):
+            return fp4_dequantize(q, dtype, out)
+    return (_CALLS or _calls()).fp4_dequantize(q, dtype, out, None)
+
+
+def fp4_linear(w: Fp4Tensor, X: torch.Tensor, bias: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None,
+               out: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None, stream=None) -> torch.Tensor:
+    """X W^T (+ bias fp32 [N]) with X [M, K] (bf16, fp16 or fp32) quantised as the weight is; the result's type defaults to
+    out's, or X's.  Without `ws`, scratch of the stream's own (stream_workspace)."""
+    if stream is not None:
+        with _on(stream):
+            return fp4_linear(w, X, bias, dtype, out, ws)
+    if dtype is None:
+        dtype = X.dtype if out is None else out.dtype
+    return (_CALLS or _calls()).fp4_linear(w, X, bias, dtype, out, ws, None)
+
+
+@dataclass
+class PagedCacheFp4:
+    """A paged cache in 4 bits (w8a8_paged_cache_fp4): k and v uint8 [n_pages, page_size, n_kv, head_dim / 2], k_scales and
+    v_scales uint8 (e4m3 bytes) [n_pages, page_size, n_kv, head_dim / 16]; either order of slots and heads as a view.  Values
+    are code * scale * 2^k_exp (v_exp): 2688 * 2^exp is the largest magnitude, 2^exp / 1024 the smallest."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+    k_exp: int = 0
+    v_exp: int = 0
+
+    def c(self) -> PagedCacheFp4C:
+        k, s = self.k, self.k_scales
+        n, page, heads, half = k.shape
+        st = [max(-(-x // 16) * 16, half) if e <= 1 else x for x, e in zip(k.stride(), k.shape)]
+        sb = half // 8
+        ss = [max(-(-x // sb) * sb, sb) if e <= 1 else x for x, e in zip(s.stride(), s.shape)]
+        return PagedCacheFp4C(n, page, heads, 2 * half, self.k_exp, self.v_exp, st[0], st[1], st[2], ss[0], ss[1], ss[2],
+                              k.data_ptr(), self.v.data_ptr(), s.data_ptr(), self.v_scales.data_ptr())
+
+
+def paged_cache_fp4(n_pages: int, page_size: int, n_kv: int, head_dim: int, device=None, k_exp: int = 0,
+                    v_exp: int = 0) -> PagedCacheFp4:
+    """An empty 4-bit cache, heads before slots: a head's page is contiguous, codes and scales."""
+    dev = device or torch.device("cuda")
+    k, v, ks, vs = (torch.zeros(n_pages, n_kv, page_size, head_dim // d, dtype=torch.uint8, device=dev).transpose(1, 2)
+                    for d in (2, 2, 16, 16))
+    return PagedCacheFp4(k, v, ks, vs, k_exp, v_exp)
+
+
+def fp4_rope_append(table: RopeTable, cache: PagedCacheFp4, batch: PagedBatch, q: torch.Tensor, k: torch.Tensor,
+                    v: torch.Tensor, q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None,
+                    eps: float = 1e-6, q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """rope_append into a 4-bit cache: q (bf16 or fp16) rotated, returned; k and v quantised into the cache's pages."""
+    if stream is not None:
+        with _on(stream):
+            return fp4_rope_append(table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out)
+    return (_CALLS or _calls()).fp4_rope_append(table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out, None)
+
+
+def fp4_paged_attention(cache: PagedCacheFp4, batch: PagedBatch, q: torch.Tensor, scale: Optional[float] = None,
+                        window: int = 0, out: Optional[torch.Tensor] = None, ws: Optional[Workspace] = None,
+                        stream=None) -> torch.Tensor:
+    """paged_attention over a 4-bit cache; q bf16 or fp16.  paged_attention_check speaks for these calls too."""
+    if stream is not None:
+        with _on(stream):
+            return fp4_paged_attention(cache, batch, q, scale, window, out, ws)
+    return (_CALLS or _calls()).fp4_paged_attention(cache, batch, q, scale, window, out, ws, None)
+
+
+def fp4_paged_values(cache: PagedCacheFp4, dtype: torch.dtype = torch.bfloat16, pages: Optional[torch.Tensor] = None,
+                     stream=None):
+    """The keys and the values of the pages (int32 [n]; None: all), each [n, page_size, n_kv, head_dim] of the type; zeros for
+    an id that is no page's."""
+    if stream is not None:
+        with _on(stream):
+            return fp4_paged_values(cache, dtype, pages)
+    return (_CALLS or _calls()).fp4_paged_values(cache, dtype, pages, None)
 
 
 # ------------------------------------------------------------------------------- decoder

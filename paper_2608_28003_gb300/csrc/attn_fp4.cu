@@ -1,0 +1,71 @@
+// Attention of a ragged batch over a paged cache in 4 bits, in its simplest form: a warp takes a row and head, key by key.
+#include <cmath>
+
+#include "attn_fp4.cuh"
+#include "ops.cuh"
+
+namespace w8a8 {
+
+namespace {
+
+template <bool kBf16, int kDim>
+__global__ void __launch_bounds__(128) attn_fp4_kernel(Fp4Pages c, PagedBatch b, AttnCall a) {
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const int64_t items = (int64_t)b.n_rows * a.n_q, warps = (int64_t)gridDim.x * 4;
+  for (int64_t i = ((int64_t)blockIdx.x * 128 + threadIdx.x) >> 5; i < items; i += warps) {
+    const int row = (int)(i / a.n_q), head = (int)(i % a.n_q), s = seq_of_row(b, row);
+    const SeqShape q = seq_shape(b, s, c.p.page_shift);
+    if (row < q.row0 || row >= q.row0 + q.rows) continue;
+    attend_row_fp4<kBf16, kDim>(c, b, a, s, q.pos0 + row - q.row0, row, head, lane, nullptr);
+  }
+}
+
+}  // namespace
+
+}  // namespace w8a8
+
+using namespace w8a8;
+
+extern "C" w8a8_status w8a8_fp4_paged_attention_workspace_size(const w8a8_paged_cache_fp4* cache, int n_q, size_t* bytes) {
+  const char* who = "w8a8_fp4_paged_attention_workspace_size";
+  W8A8_CHECK_ARG(cache && bytes, W8A8_ERR_INVALID_ARG, "%s: null argument", who);
+  W8A8_CHECK_ARG(cache->n_kv > 0 && (cache->head_dim == 64 || cache->head_dim == 128 || cache->head_dim == 256),
+                 W8A8_ERR_SHAPE, "%s: n_kv %d, head_dim %d", who, cache->n_kv, cache->head_dim);
+  W8A8_TRY(check_heads(who, cache->n_kv, cache->head_dim, n_q));
+  *bytes = paged_attention_ws(cache->head_dim, device_sms());
+  return W8A8_OK;
+}
+
+extern "C" w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cache, const w8a8_paged_batch* batch, int dtype,
+                                                const uint16_t* q, int64_t q_row, int64_t q_head, int n_q, float scale,
+                                                int window, uint16_t* o, int64_t o_row, int64_t o_head, void* workspace,
+                                                size_t ws_bytes, void* stream) {
+  const char* who = "w8a8_fp4_paged_attention";
+  Fp4Pages pc;
+  PagedBatch pb;
+  W8A8_TRY(check_fp4_paged(who, cache, batch, &pc, &pb));
+  W8A8_CHECK_ARG(dtype == W8A8_TYPE_BF16 || dtype == W8A8_TYPE_F16, W8A8_ERR_INVALID_ARG, "%s: type %d must be bf16 or fp16",
+                 who, dtype);
+  const int dim = cache->head_dim;
+  W8A8_TRY(check_heads(who, cache->n_kv, dim, n_q));
+  W8A8_TRY(check_attention(who, pb, q, q_row, q_head, n_q, dim, scale, window, o, o_row, o_head));
+  if (pb.n_seqs == 0 || pb.n_rows == 0) return W8A8_OK;
+  DevInfo d;
+  W8A8_TRY(dev_info(&d));
+  W8A8_TRY(check_attention_ws(who, dim, d.sms, workspace, ws_bytes));
+  AttnCall a{q, q_row, q_head, o, o_row, o_head, n_q, dim, window, batch->max_new, scale, dtype == W8A8_TYPE_BF16};
+  if (a.window >= 1 << 30) a.window = 0;  // beyond every position
+  W8A8_TRY(gave_up_word(&a.gave_up));
+  const int64_t items = (int64_t)pb.n_rows * n_q;
+  const dim3 grid((unsigned)(items / 4 + 1 < 152 * 64 ? items / 4 + 1 : 152 * 64));
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, as_stream(stream), pc, pb, a); };
+  W8A8_CUDA(a.bf16 ? (dim == 256   ? go(attn_fp4_kernel<true, 256>)
+                      : dim == 128 ? go(attn_fp4_kernel<true, 128>)
+                                   : go(attn_fp4_kernel<true, 64>))
+                   : (dim == 256   ? go(attn_fp4_kernel<false, 256>)
+                      : dim == 128 ? go(attn_fp4_kernel<false, 128>)
+                                   : go(attn_fp4_kernel<false, 64>)));
+  return W8A8_OK;
+}

@@ -1,0 +1,82 @@
+// Attention over a paged cache in 4 bits: one row exactly, and what its two kernels offer.  Work is divided as in attn_paged.cuh.
+#pragma once
+
+#include "attn_paged.cuh"
+#include "fp4.cuh"
+
+namespace w8a8 {
+
+// attend_row (attn_paged.cuh) with the values a 4-bit cache stands for: one row by one warp, key by key in the order of the formula.
+template <bool kBf16, int kDim>
+__device__ __noinline__ void attend_row_fp4(const Fp4Pages& c, const PagedBatch& b, const AttnCall& a, int s, int pos,
+                                            int64_t row, int head, int lane, uint32_t* beat) {
+  const uint16_t* q = a.q + row * a.q_row + head * a.q_head;
+  const int kvh = head / (a.n_q / c.p.n_kv);
+  const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+  const float scale = a.scale * two_to(c.k_exp);
+  float m = -INFINITY, l = 0.0f, acc[kDim / 32];
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < kDim / 32; ++i) acc[i] = 0.0f;
+  for (int j0 = lo; j0 <= pos; j0 += 32) {
+    if (beat && lane == 0 && ((j0 - lo) & 8191) == 0) atomicAdd(beat, 1u);
+    const int j = j0 + lane;
+    int64_t sat = 0;
+    const int64_t at = j <= pos ? fp4_key_offset(b, c, s, j, kvh, sat) : -1;
+    float sc = -INFINITY;
+    if (at >= 0) {
+      float d = 0.0f;
+      for (int i = 0; i < kDim / 16; ++i) {
+        const uint2 kw = *reinterpret_cast<const uint2*>(c.k + at + 8 * i);
+        const float unit = e4m3_value(c.ks[sat + i]);
+        const uint4 q0 = *reinterpret_cast<const uint4*>(q + 16 * i), q1 = *reinterpret_cast<const uint4*>(q + 16 * i + 8);
+        const uint32_t qa[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
+        uint32_t h[8];
+        e2m1x8_to_f16(kw.x, *reinterpret_cast<uint32_t(*)[4]>(h));
+        e2m1x8_to_f16(kw.y, *reinterpret_cast<uint32_t(*)[4]>(h + 4));
+        float part = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 x = unpack2<false>(h[e]), y = unpack2<kBf16>(qa[e]);
+          part = fmaf(x.x, y.x, part);
+          part = fmaf(x.y, y.y, part);
+        }
+        d = fmaf(part, unit, d);
+      }
+      sc = d * scale;
+    }
+    const uint32_t there = __ballot_sync(0xffffffffu, at >= 0);
+    if (!there) continue;
+    any = true;
+    const float m_new = fmaxf(m, warp_max_f(sc));
+    const float ref = m_new == -INFINITY ? 0.0f : m_new;
+    const float corr = m == -INFINITY ? 0.0f : expf(m - ref);
+    float p = at >= 0 ? expf(sc - ref) : 0.0f;
+    const float before = l * corr;
+    l = before + warp_sum_f(p);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // nothing but scores of -inf so far
+    p *= inv;
+#pragma unroll
+    for (int i = 0; i < kDim / 32; ++i) acc[i] *= before * inv;
+    for (int u = 0; u < 32; ++u) {
+      if (!((there >> u) & 1u)) continue;
+      const float pu = __shfl_sync(0xffffffffu, p, u);
+      const int64_t au = __shfl_sync(0xffffffffu, (long long)at, u), su = __shfl_sync(0xffffffffu, (long long)sat, u);
+#pragma unroll
+      for (int i = 0; i < kDim / 32; ++i) {
+        const int dim = lane + 32 * i;
+        uint32_t h[4];
+        e2m1x8_to_f16((uint32_t)c.v[au + (dim >> 1)] >> (4 * (dim & 1)), h);
+        acc[i] = fmaf(pu, unpack2<false>(h[0]).x * e4m3_value(c.vs[su + (dim >> 4)]), acc[i]);
+      }
+    }
+    m = m_new;
+  }
+  uint16_t* o = a.o + row * a.o_row + head * a.o_head;
+  const float back = two_to(c.v_exp);
+#pragma unroll
+  for (int i = 0; i < kDim / 32; ++i)
+    o[lane + 32 * i] = (uint16_t)pack2<kBf16>(!any ? 0.0f : l == 0.0f ? NAN : acc[i] * back, 0.0f);
+}
+
+}  // namespace w8a8

@@ -26,6 +26,13 @@ w8a8_status launch_attn_chunks(const PagedCache& pc, const PagedBatch& pb, const
 // bytes of the partials behind the workspace's reserved part
 size_t attn_tokens_ws(int dim, int sms);
 size_t attn_chunks_ws(int dim, int sms);
+// the device's word of waits that gave up
+w8a8_status gave_up_word(unsigned int** word);
+// what a call's heads, rows, strides and workspace have to be
+w8a8_status check_heads(const char* who, int n_kv, int dim, int n_q);
+w8a8_status check_attention(const char* who, const PagedBatch& pb, const uint16_t* q, int64_t q_row, int64_t q_head, int n_q,
+                            int dim, float scale, int window, const uint16_t* o, int64_t o_row, int64_t o_head);
+w8a8_status check_attention_ws(const char* who, int dim, int sms, const void* workspace, size_t ws_bytes);
 
 // A wait that gave up, in the workspace's error word and in the device's: a decoder's workspace and a captured call's are out of
 // the caller's reach.

@@ -35,6 +35,15 @@ struct Api {
   decltype(&w8a8_paged_attention_workspace_size) paged_ws;
   decltype(&w8a8_paged_attention) paged;
   decltype(&w8a8_sample) sample;
+  decltype(&w8a8_fp4_scale_bytes) fp4_scale_bytes;
+  decltype(&w8a8_fp4_quantize) fp4_quantize;
+  decltype(&w8a8_fp4_dequantize) fp4_dequantize;
+  decltype(&w8a8_fp4_linear_workspace_size) fp4_linear_ws;
+  decltype(&w8a8_fp4_linear) fp4_linear;
+  decltype(&w8a8_fp4_rope_append) fp4_append;
+  decltype(&w8a8_fp4_paged_attention_workspace_size) fp4_paged_ws;
+  decltype(&w8a8_fp4_paged_attention) fp4_paged;
+  decltype(&w8a8_fp4_paged_values) fp4_values;
 } g_api;
 
 // Python objects used by every call (owned by the module for the process's life).
@@ -44,7 +53,7 @@ PyObject *g_empty, *g_bf16, *g_f32, *g_i32, *g_raw_stream, *g_device, *g_check, 
 PyObject *s_data_ptr, *s_shape, *s_is_cuda, *s_is_contiguous, *s_numel, *s_device, *s_wq, *s_s_w, *s_inv_delta, *s_wq_f16,
     *s_buf, *s_get, *s_cuda_stream, *s_hidden, *s_inter, *s_vocab, *s_gate_up, *s_down, *s_gate_up_bf16, *s_down_bf16,
     *s_q, *s_bf16, *s_stride, *s_dtype, *s_get_device, *s_rotary_dim, *s_interleaved, *s_scale, *s_turns, *s_k, *s_v, *s_row_start,
-    *s_kv_len, *s_pages, *s_max_new;
+    *s_kv_len, *s_pages, *s_max_new, *s_codes, *s_scales, *s_row_scale, *s_block, *s_k_scales, *s_v_scales, *s_k_exp, *s_v_exp;
 PyObject* g_kw_empty;  // ("dtype", "device")
 
 // An owned reference.
@@ -432,7 +441,7 @@ struct Tensor {
   void* ptr = nullptr;
   int dims = 0;
   long long size[kMaxDims] = {}, stride[kMaxDims] = {};
-  int type = -1;  // W8A8_TYPE_*, 3 for int32, 4 for int64
+  int type = -1;  // W8A8_TYPE_*, 3 for int32, 4 for int64, 5 for uint8
   bool given() const { return o != nullptr; }
   bool contiguous() const {
     for (int i = 0; i < dims; ++i)
@@ -445,8 +454,8 @@ struct Tensor {
     return true;
   }
 };
-constexpr int kInt32 = 3, kInt64 = 4;
-PyObject* g_i64;
+constexpr int kInt32 = 3, kInt64 = 4, kUint8 = 5;
+PyObject *g_i64, *g_u8;
 
 bool need(bool ok, const char* msg) {
   if (!ok && !PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, msg);
@@ -494,6 +503,7 @@ bool tensor(PyObject* o, long long* dev, Tensor* t) {
             : dt.p == g_f32 ? W8A8_TYPE_F32
             : dt.p == g_i32 ? kInt32
             : dt.p == g_i64 ? kInt64
+            : dt.p == g_u8  ? kUint8
                             : -1;
   return true;
 }
@@ -545,6 +555,21 @@ struct Paged {
   w8a8_paged_batch b;
   Ref k, v, start, len, pages;
 };
+bool batch_of(const Tensor& start, const Tensor& len, const Tensor& pages, long long rows, w8a8_paged_batch* b) {
+  if (!need(len.dims == 1 && start.dims == 1 && start.size[0] == len.size[0] + 1 && pages.dims == 2 && pages.size[0] == len.size[0],
+            "row_start [n_seqs + 1], kv_len [n_seqs], pages [n_seqs, max_pages]") ||
+      !need(start.type == kInt32 && len.type == kInt32 && pages.type == kInt32 && start.contiguous() && len.contiguous() &&
+                pages.contiguous(),
+            "row_start, kv_len and pages must be contiguous int32 tensors"))
+    return false;
+  b->n_seqs = (int32_t)len.size[0];
+  b->n_rows = (int32_t)rows;
+  b->max_pages = (int32_t)pages.size[1];
+  b->row_start = static_cast<const int32_t*>(start.ptr);
+  b->kv_len = static_cast<const int32_t*>(len.ptr);
+  b->pages = static_cast<const int32_t*>(pages.ptr);
+  return true;
+}
 bool paged_of(PyObject* cache, PyObject* batch, long long rows, long long* dev, Paged* p) {
   Tensor k, v, start, len, pages;
   if (!tensor_attr(cache, s_k, dev, &k, &p->k) || !tensor_attr(cache, s_v, dev, &v, &p->v) ||
@@ -553,23 +578,12 @@ bool paged_of(PyObject* cache, PyObject* batch, long long rows, long long* dev, 
     return false;
   bool same = k.dims == 4 && same_shape(k, v) && k.type == v.type && k.stride[3] == 1;
   for (int i = 0; same && i < 4; ++i) same = k.stride[i] == v.stride[i];
-  if (!need(same, "k and v [n_pages, page_size, n_kv, head_dim] of equal shape, strides and type, dims contiguous") ||
-      !need(len.dims == 1 && start.dims == 1 && start.size[0] == len.size[0] + 1 && pages.dims == 2 && pages.size[0] == len.size[0],
-            "row_start [n_seqs + 1], kv_len [n_seqs], pages [n_seqs, max_pages]") ||
-      !need(start.type == kInt32 && len.type == kInt32 && pages.type == kInt32 && start.contiguous() && len.contiguous() &&
-                pages.contiguous(),
-            "row_start, kv_len and pages must be contiguous int32 tensors"))
+  if (!need(same, "k and v [n_pages, page_size, n_kv, head_dim] of equal shape, strides and type, dims contiguous"))
     return false;
   p->c = w8a8_paged_cache{k.type, (int32_t)k.size[0], (int32_t)k.size[1], (int32_t)k.size[2], (int32_t)k.size[3],
                           stride_or(k, 0, k.size[3]), stride_or(k, 1, k.size[3]), stride_or(k, 2, k.size[3]),
                           static_cast<uint16_t*>(k.ptr), static_cast<uint16_t*>(v.ptr)};
-  p->b.n_seqs = (int32_t)len.size[0];
-  p->b.n_rows = (int32_t)rows;
-  p->b.max_pages = (int32_t)pages.size[1];
-  p->b.row_start = static_cast<const int32_t*>(start.ptr);
-  p->b.kv_len = static_cast<const int32_t*>(len.ptr);
-  p->b.pages = static_cast<const int32_t*>(pages.ptr);
-  return true;
+  return batch_of(start, len, pages, rows, &p->b);
 }
 // [rows, heads, dim] with contiguous heads
 bool head_rows(const Tensor& t, long long rows, long long heads, long long dim, int type) {
@@ -728,6 +742,260 @@ PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyTuple_Pack(2, y.p, z.p);
 }
 
+// ------------------------------------------------------------------------------- 4 bits
+// W8A8_TYPE_* of a torch dtype; -1 with an error for another
+int type_of(PyObject* dtype) {
+  const int t = dtype == g_bf16 ? W8A8_TYPE_BF16 : dtype == g_f16 ? W8A8_TYPE_F16 : dtype == g_f32 ? W8A8_TYPE_F32 : -1;
+  need(t >= 0, "dtype must be torch.bfloat16, torch.float16 or torch.float32");
+  return t;
+}
+bool float_type(const Tensor& t) { return t.type >= W8A8_TYPE_BF16 && t.type <= W8A8_TYPE_F32; }
+// [rows, cols] of a floating type with contiguous rows
+bool float_matrix(const Tensor& t, const char* msg) {
+  return need(t.given() && t.dims == 2 && float_type(t) && (t.stride[1] == 1 || t.size[1] <= 1), msg);
+}
+// A matrix in 4 bits (its tensors stay alive in `keep`).
+struct Fp4 {
+  w8a8_fp4 d;
+  Ref codes, scales, row_scale;
+};
+bool fp4_of(PyObject* o, long long* dev, Fp4* f) {
+  Tensor c, s, r;
+  if (!tensor_attr(o, s_codes, dev, &c, &f->codes) || !tensor_attr(o, s_scales, dev, &s, &f->scales) ||
+      !tensor_attr(o, s_row_scale, dev, &r, &f->row_scale) || !int_attr(o, s_block, &f->d.block) ||
+      !need(c.given() && s.given() && c.dims == 2 && c.type == kUint8 && c.contiguous() && s.type == kUint8 && s.contiguous() &&
+                c.size[1] <= W8A8_MAX_K / 2,
+            "codes must be a contiguous uint8 tensor [rows, k / 2], scales a contiguous uint8 tensor"))
+    return false;
+  f->d.rows = (int32_t)c.size[0];
+  f->d.k = (int32_t)(2 * c.size[1]);
+  size_t bytes = 0;
+  if (!check("w8a8_fp4_scale_bytes", g_api.fp4_scale_bytes(f->d.rows, f->d.k, f->d.block, &bytes))) return false;
+  long long have = 1;
+  for (int i = 0; i < s.dims; ++i) have *= s.size[i];
+  if (!need(have == (long long)bytes, "scales must have as many bytes as w8a8_fp4_scale_bytes says") ||
+      !need(f->d.block == 32 || r.given(), "blocks of 16 need a row_scale") ||
+      !vector(r, c.size[0], W8A8_TYPE_F32, "row_scale must be fp32 [rows]"))
+    return false;
+  f->d.codes = static_cast<uint8_t*>(c.ptr);
+  f->d.scales = static_cast<uint8_t*>(s.ptr);
+  f->d.row_scale = f->d.block == 16 ? static_cast<float*>(r.ptr) : nullptr;
+  return true;
+}
+
+// (x, block, stream) -> (codes, scales, row_scale or None)
+PyObject* py_fp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 3, "fp4_quantize")) return nullptr;
+  long long dev = -1, block;
+  Tensor x, tc, ts, tr;
+  void* st;
+  size_t bytes = 0;
+  if (!tensor(a[0], &dev, &x) || !float_matrix(x, "x must be [rows, k] bf16, fp16 or fp32 with contiguous rows") ||
+      !as_int(PyNumber_Long(a[1]), &block) || !need(block == 16 || block == 32, "block must be 16 or 32") ||
+      !check("w8a8_fp4_scale_bytes", g_api.fp4_scale_bytes((int)x.size[0], (int)x.size[1], (int)block, &bytes)))
+    return nullptr;
+  Ref codes(new_empty(a[0], x.size[0], x.size[1] / 2, g_u8)), scales(new_empty(a[0], (long long)bytes, -1, g_u8));
+  Ref rows(block == 16 ? new_empty(a[0], x.size[0], -1, g_f32) : Py_NewRef(Py_None));
+  if (!codes || !scales || !rows || !tensor(codes.p, &dev, &tc) || !tensor(scales.p, &dev, &ts) || !tensor(rows.p, &dev, &tr) ||
+      !stream_of(a[2], &st))
+    return nullptr;
+  const w8a8_fp4 q{(int32_t)x.size[0], (int32_t)x.size[1], (int32_t)block, static_cast<uint8_t*>(tc.ptr),
+                   static_cast<uint8_t*>(ts.ptr), static_cast<float*>(tr.ptr)};
+  if (!check("w8a8_fp4_quantize",
+             unlocked([&] { return g_api.fp4_quantize(x.type, x.ptr, stride_or(x, 0, x.size[1]), &q, st); })))
+    return nullptr;
+  return PyTuple_Pack(3, codes.p, scales.p, rows.p);
+}
+
+// (q, dtype, out, stream) -> out
+PyObject* py_fp4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 4, "fp4_dequantize")) return nullptr;
+  long long dev = -1;
+  Fp4 q;
+  Tensor y;
+  Ref out;
+  void* st;
+  const int type = type_of(a[1]);
+  if (type < 0 || !fp4_of(a[0], &dev, &q)) return nullptr;
+  out.p = a[2] == Py_None ? new_empty(q.codes.p, q.d.rows, q.d.k, a[1]) : Py_NewRef(a[2]);
+  if (!out || !tensor(out.p, &dev, &y) || !float_matrix(y, "out must be [rows, k] with contiguous rows") ||
+      !need(y.type == type && y.size[0] == q.d.rows && y.size[1] == q.d.k, "out must be [rows, k] of the dtype") ||
+      !stream_of(a[3], &st))
+    return nullptr;
+  if (!check("w8a8_fp4_dequantize",
+             unlocked([&] { return g_api.fp4_dequantize(&q.d, type, y.ptr, stride_or(y, 0, y.size[1]), st); })))
+    return nullptr;
+  return out.give();
+}
+
+// (w, X, bias, dtype, out, ws, stream) -> out
+PyObject* py_fp4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 7, "fp4_linear")) return nullptr;
+  long long dev = -1;
+  Fp4 w;
+  Tensor x, bias, y;
+  Ref out;
+  void* st;
+  const int type = type_of(a[3]);
+  if (type < 0 || !tensor(a[1], &dev, &x) || !float_matrix(x, "X must be [M, K] bf16, fp16 or fp32 with contiguous rows") ||
+      !fp4_of(a[0], &dev, &w) || !need(x.size[1] == w.d.k, "X and the weight differ in K") || !tensor(a[2], &dev, &bias) ||
+      !vector(bias, w.d.rows, W8A8_TYPE_F32, "bias must be fp32 [N]"))
+    return nullptr;
+  out.p = a[4] == Py_None ? new_empty(a[1], x.size[0], w.d.rows, a[3]) : Py_NewRef(a[4]);
+  if (!out || !tensor(out.p, &dev, &y) || !float_matrix(y, "out must be [M, N] with contiguous rows") ||
+      !need(y.type == type && y.size[0] == x.size[0] && y.size[1] == w.d.rows, "out must be [M, N] of the dtype") ||
+      !stream_of(a[6], &st))
+    return nullptr;
+  const int M = (int)x.size[0];
+  size_t bytes = 0;
+  Buf b;
+  if (!check("w8a8_fp4_linear_workspace_size", g_api.fp4_linear_ws(M, w.d.rows, w.d.k, w.d.block, &bytes)) ||
+      !(a[5] == Py_None ? stream_workspace(a[1], a[6], dev, st, bytes, &b) : workspace(a[5], bytes, &b)))
+    return nullptr;
+  if (!check("w8a8_fp4_linear", unlocked([&] {
+               return g_api.fp4_linear(&w.d, x.type, x.ptr, stride_or(x, 0, x.size[1]), M, static_cast<float*>(bias.ptr), type,
+                                       y.ptr, M > 1 ? y.stride[0] : y.size[1], b.ptr, b.bytes, st);
+             })))
+    return nullptr;
+  return out.give();
+}
+
+struct PagedFp4 {
+  w8a8_paged_cache_fp4 c;
+  w8a8_paged_batch b;
+  Ref k, v, ks, vs, start, len, pages;
+};
+bool fp4_cache_of(PyObject* cache, long long* dev, PagedFp4* p) {
+  Tensor k, v, ks, vs;
+  if (!tensor_attr(cache, s_k, dev, &k, &p->k) || !tensor_attr(cache, s_v, dev, &v, &p->v) ||
+      !tensor_attr(cache, s_k_scales, dev, &ks, &p->ks) || !tensor_attr(cache, s_v_scales, dev, &vs, &p->vs) ||
+      !int_attr(cache, s_k_exp, &p->c.k_exp) || !int_attr(cache, s_v_exp, &p->c.v_exp))
+    return false;
+  auto alike = [](const Tensor& a, const Tensor& b) {
+    bool same = a.dims == 4 && same_shape(a, b) && a.type == kUint8 && b.type == kUint8 && a.stride[3] == 1;
+    for (int i = 0; same && i < 4; ++i) same = a.stride[i] == b.stride[i];
+    return same;
+  };
+  if (!need(alike(k, v), "k and v must be uint8 [n_pages, page_size, n_kv, head_dim / 2] of equal shape and strides, codes "
+                         "contiguous") ||
+      !need(alike(ks, vs) && ks.size[0] == k.size[0] && ks.size[1] == k.size[1] && ks.size[2] == k.size[2] &&
+                8 * ks.size[3] == k.size[3],
+            "k_scales and v_scales must be uint8 [n_pages, page_size, n_kv, head_dim / 16] of equal strides, scales contiguous"))
+    return false;
+  // the stride of an extent of one says nothing: any that the library takes
+  auto stride = [](const Tensor& t, int i, long long unit, long long least) {
+    if (t.size[i] > 1) return t.stride[i];
+    const long long s = (t.stride[i] + unit - 1) / unit * unit;
+    return s > least ? s : least;
+  };
+  const long long cb = k.size[3], sb = ks.size[3] > 0 ? ks.size[3] : 1;
+  p->c = w8a8_paged_cache_fp4{(int32_t)k.size[0], (int32_t)k.size[1], (int32_t)k.size[2], (int32_t)(2 * cb), p->c.k_exp,
+                              p->c.v_exp, stride(k, 0, 16, cb), stride(k, 1, 16, cb), stride(k, 2, 16, cb),
+                              stride(ks, 0, sb, sb), stride(ks, 1, sb, sb), stride(ks, 2, sb, sb),
+                              static_cast<uint8_t*>(k.ptr), static_cast<uint8_t*>(v.ptr), static_cast<uint8_t*>(ks.ptr),
+                              static_cast<uint8_t*>(vs.ptr)};
+  return need(cb <= 1 << 20, "head_dim too large");
+}
+bool fp4_batch_of(PyObject* batch, long long rows, long long* dev, PagedFp4* p) {
+  Tensor start, len, pages;
+  if (!tensor_attr(batch, s_row_start, dev, &start, &p->start) || !tensor_attr(batch, s_kv_len, dev, &len, &p->len) ||
+      !tensor_attr(batch, s_pages, dev, &pages, &p->pages) || !int_attr(batch, s_max_new, &p->b.max_new))
+    return false;
+  return batch_of(start, len, pages, rows, &p->b);
+}
+
+// (table, cache, batch, q, k, v, q_norm, k_norm, eps, q_out, stream) -> q_out
+PyObject* py_fp4_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 11, "fp4_rope_append")) return nullptr;
+  long long dev = -1;
+  w8a8_rope_table r;
+  PagedFp4 p;
+  Ref turns, y;
+  Tensor q, k, v, qn, kn, out;
+  void* st;
+  if (!tensor(a[3], &dev, &q) || !need(q.given() && q.dims == 3, "q must be [rows, n_q, head_dim]") ||
+      !need(q.type == W8A8_TYPE_BF16 || q.type == W8A8_TYPE_F16, "q, k and v must be bf16 or fp16") ||
+      !fp4_cache_of(a[1], &dev, &p) || !fp4_batch_of(a[2], q.size[0], &dev, &p) || !rope_of(a[0], &dev, &r, &turns) ||
+      !tensor(a[4], &dev, &k) || !tensor(a[5], &dev, &v) || !need(k.given() && v.given(), "k and v expected") ||
+      !tensor(a[6], &dev, &qn) || !tensor(a[7], &dev, &kn))
+    return nullptr;
+  const double eps = PyFloat_AsDouble(a[8]);
+  if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+  const long long rows = q.size[0], n_q = q.size[1], dim = p.c.head_dim;
+  if (!head_rows(q, rows, n_q, dim, q.type) || !head_rows(k, rows, p.c.n_kv, dim, q.type) ||
+      !head_rows(v, rows, p.c.n_kv, dim, q.type) || !vector(qn, dim, W8A8_TYPE_F32, "norms must be fp32 [head_dim]") ||
+      !vector(kn, dim, W8A8_TYPE_F32, "norms must be fp32 [head_dim]") || !output(a[9], a[3], nullptr, &y) ||
+      !tensor(y.p, &dev, &out) || !head_rows(out, rows, n_q, dim, q.type) || !stream_of(a[10], &st))
+    return nullptr;
+  if (!check("w8a8_fp4_rope_append", unlocked([&] {
+               return g_api.fp4_append(&r, &p.c, &p.b, q.type, static_cast<uint16_t*>(q.ptr), stride_or(q, 0, 0), (int)n_q,
+                                       static_cast<uint16_t*>(k.ptr), stride_or(k, 0, 0), static_cast<uint16_t*>(v.ptr),
+                                       stride_or(v, 0, 0), static_cast<float*>(qn.ptr), static_cast<float*>(kn.ptr), (float)eps,
+                                       static_cast<uint16_t*>(out.ptr), stride_or(out, 0, 0), st);
+             })))
+    return nullptr;
+  return y.give();
+}
+
+// (cache, batch, q, scale, window, out, ws, stream) -> out
+PyObject* py_fp4_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 8, "fp4_paged_attention")) return nullptr;
+  long long dev = -1, window;
+  PagedFp4 p;
+  Ref y;
+  Tensor q, out;
+  void* st;
+  if (!tensor(a[2], &dev, &q) || !need(q.given() && q.dims == 3 && q.stride[2] == 1, "q must be [rows, n_q, head_dim]") ||
+      !need(q.type == W8A8_TYPE_BF16 || q.type == W8A8_TYPE_F16, "q must be bf16 or fp16") || !fp4_cache_of(a[0], &dev, &p) ||
+      !fp4_batch_of(a[1], q.size[0], &dev, &p) || !output(a[5], a[2], nullptr, &y) || !tensor(y.p, &dev, &out) ||
+      !need(q.size[2] == p.c.head_dim && same_shape(q, out) && out.stride[2] == 1 && out.type == q.type,
+            "q and out must be [rows, n_q, head_dim] of one type") ||
+      !as_int(PyNumber_Long(a[4]), &window) || !stream_of(a[7], &st))
+    return nullptr;
+  double scale = a[3] == Py_None ? 1.0 / std::sqrt((double)q.size[2]) : PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred() || !need(window >= -2147483647LL && window <= 2147483647LL, "window out of range")) return nullptr;
+  const int n_q = (int)q.size[1];
+  const long long dim = q.size[2];
+  size_t bytes = 0;
+  Buf b;
+  if (!check("w8a8_fp4_paged_attention_workspace_size", g_api.fp4_paged_ws(&p.c, n_q, &bytes)) ||
+      !(a[6] == Py_None ? stream_workspace(a[2], a[7], dev, st, bytes, &b) : workspace(a[6], bytes, &b)))
+    return nullptr;
+  if (!check("w8a8_fp4_paged_attention", unlocked([&] {
+               return g_api.fp4_paged(&p.c, &p.b, q.type, static_cast<uint16_t*>(q.ptr), stride_or(q, 0, dim),
+                                      stride_or(q, 1, dim), n_q, (float)scale, (int)window, static_cast<uint16_t*>(out.ptr),
+                                      stride_or(out, 0, dim), stride_or(out, 1, dim), b.ptr, b.bytes, st);
+             })))
+    return nullptr;
+  return y.give();
+}
+
+// (cache, dtype, pages or None, stream) -> (k, v)
+PyObject* py_fp4_paged_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!nargs_are(n, 4, "fp4_paged_values")) return nullptr;
+  long long dev = -1;
+  PagedFp4 p;
+  Tensor pages, tk, tv;
+  void* st;
+  const int type = type_of(a[1]);
+  if (type < 0 || !fp4_cache_of(a[0], &dev, &p) || !tensor(a[2], &dev, &pages) ||
+      !need(!pages.given() || (pages.dims == 1 && pages.type == kInt32 && pages.contiguous()),
+            "pages must be a contiguous int32 tensor [n]"))
+    return nullptr;
+  const long long count = pages.given() ? pages.size[0] : p.c.n_pages;
+  Ref at(PyObject_GetAttr(p.k.p, s_device));
+  Ref shape(Py_BuildValue("(LLLL)", count, (long long)p.c.page_size, (long long)p.c.n_kv, (long long)p.c.head_dim));
+  if (!at || !shape) return nullptr;
+  PyObject* args[3] = {shape.p, a[1], at.p};
+  Ref k(PyObject_Vectorcall(g_empty, args, 1, g_kw_empty)), v(k ? PyObject_Vectorcall(g_empty, args, 1, g_kw_empty) : nullptr);
+  if (!k || !v || !tensor(k.p, &dev, &tk) || !tensor(v.p, &dev, &tv) || !stream_of(a[3], &st)) return nullptr;
+  if (!check("w8a8_fp4_paged_values", unlocked([&] {
+               return g_api.fp4_values(&p.c, static_cast<int32_t*>(pages.ptr), (int)count, type, tk.ptr, tv.ptr, st);
+             })))
+    return nullptr;
+  return PyTuple_Pack(2, k.p, v.p);
+}
+
 // (addresses: dict name -> int, check, default_workspace, workspace table, Workspace, stream_workspace, its table)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!nargs_are(n, 7, "init")) return nullptr;
@@ -750,7 +1018,13 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !address("w8a8_fp8_ffn_block", &g_api.fp8_ffn) || !address("w8a8_lm_head", &g_api.head) ||
       !address("w8a8_rope", &g_api.rope) || !address("w8a8_rope_append", &g_api.append) ||
       !address("w8a8_paged_attention_workspace_size", &g_api.paged_ws) ||
-      !address("w8a8_paged_attention", &g_api.paged) || !address("w8a8_sample", &g_api.sample))
+      !address("w8a8_paged_attention", &g_api.paged) || !address("w8a8_sample", &g_api.sample) ||
+      !address("w8a8_fp4_scale_bytes", &g_api.fp4_scale_bytes) || !address("w8a8_fp4_quantize", &g_api.fp4_quantize) ||
+      !address("w8a8_fp4_dequantize", &g_api.fp4_dequantize) ||
+      !address("w8a8_fp4_linear_workspace_size", &g_api.fp4_linear_ws) || !address("w8a8_fp4_linear", &g_api.fp4_linear) ||
+      !address("w8a8_fp4_rope_append", &g_api.fp4_append) ||
+      !address("w8a8_fp4_paged_attention_workspace_size", &g_api.fp4_paged_ws) ||
+      !address("w8a8_fp4_paged_attention", &g_api.fp4_paged) || !address("w8a8_fp4_paged_values", &g_api.fp4_values))
     return nullptr;
   Ref torch(PyImport_ImportModule("torch")), c(PyImport_ImportModule("torch._C"));
   if (!torch || !c) return nullptr;
@@ -763,6 +1037,7 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
                {&g_f32, torch.p, "float32"},
                {&g_i32, torch.p, "int32"},
                {&g_i64, torch.p, "int64"},
+               {&g_u8, torch.p, "uint8"},
                {&g_f16, torch.p, "float16"},
                {&g_capturing, c.p, "_cuda_isCurrentStreamCapturing"},
                {&g_raw_stream, c.p, "_cuda_getCurrentRawStream"},
@@ -786,7 +1061,9 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
                {&s_down_bf16, "down_bf16"}, {&s_q, "q"}, {&s_bf16, "bf16"},
                {&s_stride, "stride"}, {&s_dtype, "dtype"}, {&s_get_device, "get_device"}, {&s_rotary_dim, "rotary_dim"},
                {&s_interleaved, "interleaved"}, {&s_scale, "scale"}, {&s_turns, "turns"}, {&s_k, "k"}, {&s_v, "v"},
-               {&s_row_start, "row_start"}, {&s_kv_len, "kv_len"}, {&s_pages, "pages"}, {&s_max_new, "max_new"}};
+               {&s_row_start, "row_start"}, {&s_kv_len, "kv_len"}, {&s_pages, "pages"}, {&s_max_new, "max_new"}, {&s_codes, "codes"}, {&s_scales, "scales"},
+               {&s_row_scale, "row_scale"}, {&s_block, "block"}, {&s_k_scales, "k_scales"}, {&s_v_scales, "v_scales"},
+               {&s_k_exp, "k_exp"}, {&s_v_exp, "v_exp"}};
   for (auto& it : names)
     if (!(*it.to = PyUnicode_InternFromString(it.name))) return nullptr;
   if (!(g_kw_empty = Py_BuildValue("(ss)", "dtype", "device"))) return nullptr;
@@ -805,6 +1082,12 @@ PyMethodDef g_methods[] = {{"init", FAST(py_init), "Set the library's addresses 
                            {"rope_append", FAST(py_rope_append), "w8a8_rope_append"},
                            {"paged_attention", FAST(py_paged_attention), "w8a8_paged_attention"},
                            {"sample", FAST(py_sample), "w8a8_sample"},
+                           {"fp4_quantize", FAST(py_fp4_quantize), "w8a8_fp4_quantize"},
+                           {"fp4_dequantize", FAST(py_fp4_dequantize), "w8a8_fp4_dequantize"},
+                           {"fp4_linear", FAST(py_fp4_linear), "w8a8_fp4_linear"},
+                           {"fp4_rope_append", FAST(py_fp4_rope_append), "w8a8_fp4_rope_append"},
+                           {"fp4_paged_attention", FAST(py_fp4_paged_attention), "w8a8_fp4_paged_attention"},
+                           {"fp4_paged_values", FAST(py_fp4_paged_values), "w8a8_fp4_paged_values"},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", "Compute calls of the binding.", -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

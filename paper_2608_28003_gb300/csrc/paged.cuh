@@ -19,6 +19,11 @@ struct PagedCache {
 
 w8a8_status check_paged(const char* who, const w8a8_paged_cache* c, const w8a8_paged_batch* b, PagedCache* pc,
                         PagedBatch* pb);
+w8a8_status check_rope(const char* who, const w8a8_rope_table* r, int dim);
+// what an append's rows, norms and strides have to be
+w8a8_status check_append(const char* who, const PagedBatch& pb, int dim, const uint16_t* q, int64_t q_row, int n_q,
+                         const uint16_t* k, int64_t k_row, const uint16_t* v, int64_t v_row, const float* q_norm,
+                         const float* k_norm, float eps, const uint16_t* q_out, int64_t q_out_row);
 
 // (no argument checks; n_rows and n_seqs at least 1)
 w8a8_status launch_rope_append(const w8a8_rope_table& rt, const PagedCache& pc, const PagedBatch& pb, int dim, bool bf16,

@@ -206,14 +206,6 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-w8a8_status check_rope(const char* who, const w8a8_rope_table* r, int dim) {
-  W8A8_CHECK_ARG(r != nullptr && r->turns != nullptr, W8A8_ERR_INVALID_ARG, "%s: null rope table", who);
-  W8A8_CHECK_ARG(r->rotary_dim >= 16 && r->rotary_dim % 16 == 0 && r->rotary_dim <= dim, W8A8_ERR_SHAPE,
-                 "%s: rotary_dim %d must be a multiple of 16 in [16, %d]", who, r->rotary_dim, dim);
-  W8A8_CHECK_ARG(aligned16(r->turns), W8A8_ERR_ALIGN, "%s: turns must be 16-byte aligned", who);
-  return W8A8_OK;
-}
-
 // The threads a row's heads are spread over: as many as fill the SMs once (their registers hold 512 of a thread's 16 values, angles
 // and loads ahead), so that few rows spread over the heads, and many compute their angles once for all heads.  2400 rows of
 // 24 heads of 128: 11.5 us with one such wave, 16.4 with four (a thread a head, its angles for that head alone); 8192 rows of
@@ -225,6 +217,32 @@ int head_step(int64_t rows, int units, int heads, int sms) {
 }
 
 }  // namespace
+
+w8a8_status check_rope(const char* who, const w8a8_rope_table* r, int dim) {
+  W8A8_CHECK_ARG(r != nullptr && r->turns != nullptr, W8A8_ERR_INVALID_ARG, "%s: null rope table", who);
+  W8A8_CHECK_ARG(r->rotary_dim >= 16 && r->rotary_dim % 16 == 0 && r->rotary_dim <= dim, W8A8_ERR_SHAPE,
+                 "%s: rotary_dim %d must be a multiple of 16 in [16, %d]", who, r->rotary_dim, dim);
+  W8A8_CHECK_ARG(aligned16(r->turns), W8A8_ERR_ALIGN, "%s: turns must be 16-byte aligned", who);
+  return W8A8_OK;
+}
+
+w8a8_status check_append(const char* who, const PagedBatch& pb, int dim, const uint16_t* q, int64_t q_row, int n_q,
+                         const uint16_t* k, int64_t k_row, const uint16_t* v, int64_t v_row, const float* q_norm,
+                         const float* k_norm, float eps, const uint16_t* q_out, int64_t q_out_row) {
+  W8A8_CHECK_ARG(n_q > 0 && n_q <= 65536 / dim, W8A8_ERR_SHAPE, "%s: n_q=%d", who, n_q);
+  W8A8_CHECK_ARG(q_norm == nullptr && k_norm == nullptr || (eps >= 0.0f && std::isfinite(eps)), W8A8_ERR_INVALID_ARG,
+                 "%s: eps %g", who, (double)eps);
+  if (pb.n_seqs == 0 || pb.n_rows == 0) return W8A8_OK;
+  W8A8_CHECK_ARG(q && k && v && q_out, W8A8_ERR_INVALID_ARG, "%s: null pointer", who);
+  W8A8_CHECK_ARG(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(q_out) && aligned16(q_norm) && aligned16(k_norm),
+                 W8A8_ERR_ALIGN, "%s: pointers must be 16-byte aligned", who);
+  const int64_t big = 1ll << 40, rows[4] = {q_row, k_row, v_row, q_out_row};
+  for (int64_t s : rows) W8A8_CHECK_ARG(s >= 0 && s % 8 == 0 && s <= big, W8A8_ERR_SHAPE, "%s: row strides must be multiples of 8", who);
+  W8A8_CHECK_ARG(pb.n_rows == 1 || q_out_row >= (int64_t)n_q * dim, W8A8_ERR_SHAPE, "%s: q_out's rows overlap", who);
+  W8A8_CHECK_ARG(q != q_out || q_row == q_out_row || pb.n_rows == 1, W8A8_ERR_SHAPE, "%s: in place needs the same row stride",
+                 who);
+  return W8A8_OK;
+}
 
 w8a8_status launch_rope_append(const w8a8_rope_table& rt, const PagedCache& pc, const PagedBatch& pb, int dim, bool bf16,
                                const uint16_t* q, int64_t q_row, int n_q, const uint16_t* k, int64_t k_row,
@@ -375,18 +393,8 @@ extern "C" w8a8_status w8a8_rope_append(const w8a8_rope_table* rope, const w8a8_
   W8A8_TRY(check_paged(who, cache, batch, &pc, &pb));
   W8A8_TRY(check_rope(who, rope, cache->head_dim));
   const int dim = cache->head_dim;
-  W8A8_CHECK_ARG(n_q > 0 && n_q <= 65536 / dim, W8A8_ERR_SHAPE, "%s: n_q=%d", who, n_q);
-  W8A8_CHECK_ARG(q_norm == nullptr && k_norm == nullptr || (eps >= 0.0f && std::isfinite(eps)), W8A8_ERR_INVALID_ARG,
-                 "%s: eps %g", who, (double)eps);
+  W8A8_TRY(check_append(who, pb, dim, q, q_row, n_q, k, k_row, v, v_row, q_norm, k_norm, eps, q_out, q_out_row));
   if (pb.n_seqs == 0 || pb.n_rows == 0) return W8A8_OK;
-  W8A8_CHECK_ARG(q && k && v && q_out, W8A8_ERR_INVALID_ARG, "%s: null pointer", who);
-  W8A8_CHECK_ARG(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(q_out) && aligned16(q_norm) && aligned16(k_norm),
-                 W8A8_ERR_ALIGN, "%s: pointers must be 16-byte aligned", who);
-  const int64_t big = 1ll << 40, rows[4] = {q_row, k_row, v_row, q_out_row};
-  for (int64_t s : rows) W8A8_CHECK_ARG(s >= 0 && s % 8 == 0 && s <= big, W8A8_ERR_SHAPE, "%s: row strides must be multiples of 8", who);
-  W8A8_CHECK_ARG(pb.n_rows == 1 || q_out_row >= (int64_t)n_q * dim, W8A8_ERR_SHAPE, "%s: q_out's rows overlap", who);
-  W8A8_CHECK_ARG(q != q_out || q_row == q_out_row || pb.n_rows == 1, W8A8_ERR_SHAPE, "%s: in place needs the same row stride",
-                 who);
   DevInfo d;
   W8A8_TRY(dev_info(&d));
   return launch_rope_append(*rope, pc, pb, dim, cache->dtype == W8A8_TYPE_BF16, q, q_row, n_q, k, k_row, v, v_row, q_norm,
