@@ -1,74 +1,517 @@
-// The linear in floating point of 4 bits, in its simplest form: a block takes 16 x 64 outputs and walks k 32 columns at a time.
+// The linear in floating point of 4 bits, on the 5th-generation tensor cores' block-scaled products.
+//
+// y_ti = sx_t sw_i sum_b ux_tb uw_ib sum_j x_tj w_ij: tcgen05.mma kind::mxf4nvf4 takes 64 columns of codes of both operands and the
+// units of their blocks (four bytes a row with blocks of 16, two with blocks of 32) and adds the scaled sums into fp32 accumulators in
+// tensor memory; the row scales are applied to the accumulators.  One kernel computes D [A's rows, B's rows] = A B^T:
+//  * up to 128 tokens (kSwap): A are 128 output channels, B the tokens, so that few tokens do not pad 128 lanes.  The weights
+//    are read once, which HBM bounds (or, for a single layer's few megabytes, latency);
+//  * more tokens: A are 128 or 256 tokens, B 128 or 192 channels.
+// Codes come by TMA, 256 columns (128 bytes, swizzled) a stage; a stage's scales are one contiguous copy per 128 rows in the order
+// that they have in memory (w8a8_fp4), from where tcgen05.cp spreads them over tensor memory, 32 rows a column, ahead of the
+// products on the same pipe.
+// A warp copies, a warp issues, 4 or 8 epilogue warps (a thread per lane of tensor memory) turn accumulators into outputs: through
+// swizzled shared memory and TMA stores where D's lanes are tokens, directly where they are channels, which neighbouring lanes
+// hold.  Units are walked by one CTA an SM, copies running ahead over unit borders, accumulators in two slots where they fit.
+// Long rows of few tiles are split over a cluster of up to 8 CTAs, which add up their accumulators through distributed shared memory in
+// the order of their ranks: the same bits every time.
+//
+// Every wait is bounded: on timeout a bit of the workspace's error word is set and the CTA passes its units without waiting.
+#include <algorithm>
+
 #include "fp4.cuh"
 #include "ops.cuh"
+#include "tc_common.cuh"
+#include "tmap.cuh"
 
 namespace w8a8 {
 
 namespace {
 
-struct Side {
-  const uint8_t *codes, *scales;
-  const float* row_scale;
+constexpr int kKStage = 256;  // columns of a stage
+
+template <int kMT, int kBN, bool kSwap, int kBlock>
+struct Cfg {
+  static constexpr int kChunks = kKStage / (4 * kBlock);         // 512-byte pieces of scales a stage and 128 rows
+  static constexpr int kBBlocks = kBN > 128 ? 2 : 1;             // 128-row blocks of scales that B's rows touch
+  static constexpr int kARows = 128 * kMT;
+  static constexpr int kCodes = (kARows + kBN) * 128, kScales = (kMT + kBBlocks) * kChunks * 512;
+  static constexpr int kStage = (kCodes + kScales + 1023) / 1024 * 1024;
+  static constexpr int kEpi = 4 * kMT;                           // epilogue warps
+  static constexpr int kStaging = kSwap ? 0 : kEpi * 4096;       // 32 rows of 128 bytes a warp
+  static constexpr int kRoom = 227 * 1024 - 3072 - kStaging;
+  static constexpr int kStages = kRoom / kStage < 8 ? kRoom / kStage : 8;
+  static constexpr int kSmem = kStages * kStage + kStaging + 1024;
+  static constexpr int kThreads = 64 + 32 * kEpi;
+  static constexpr int kAccCols = kMT * kBN, kSfCols = (kMT + kBBlocks) * kChunks * 4;
+  static constexpr int kAccs = 2 * kAccCols + 2 * kSfCols <= 512 ? 2 : 1;
+  static constexpr int kCols = kAccs * kAccCols + 2 * kSfCols;
+  static constexpr int kTmem = kCols <= 32 ? 32 : kCols <= 64 ? 64 : kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+  static_assert(kCols <= 512 && kStages >= 3, "tensor memory and a ring");
+  static_assert(128 * kBN * 4 <= kStages * kStage || kMT == 2, "a cluster's accumulators fit over the ring");
 };
 
-__device__ __forceinline__ float unit_of(const Side& s, int64_t row, int col, int block, int groups) {
-  const uint32_t byte = s.scales[fp4_scale_at(row, col / block, groups)];
-  if (block == 16) return e4m3_value(byte);
-  return byte == kE8m0NaN ? NAN : byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
+struct Fp4Args {
+  const uint8_t *a_scales, *b_scales;
+  const float *x_scale, *w_scale, *bias;  // row scales: tokens', channels'
+  char* y;
+  int64_t y_row;  // elements
+  unsigned int* err;
+  int M, N, K;              // tokens, channels
+  int a_tiles, b_tiles;     // of A's and B's rows
+  int a_blocks, b_blocks;   // 128-row blocks of their scales
+  int groups;               // 512-byte pieces a block
+  int split;                // CTAs of a cluster, parts of k
+  int out;                  // W8A8_TYPE_*
+  int tma_out;              // y by TMA stores
+};
+
+// Instruction descriptor of kind::mxf4nvf4: both operands e2m1 (1 at bits 7 and 10), N >> 3 at bit 17, scales e4m3 (0) or
+// e8m0 (1) at bit 23, M >> 7 at bit 27; with blocks of 32, which half of a row's word holds the units (0 or 2) at bits 4 (B) and
+// 29 (A).  64 columns (bit 31 clear).
+template <int kBlock>
+__device__ constexpr uint32_t idesc_fp4(int n, int half) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (kBlock == 32 ? 1u << 23 : 0u) | (1u << 27) |
+         (kBlock == 32 ? (uint32_t)half << 5 | (uint32_t)half << 30 : 0u);
+}
+template <int kBlock>
+__device__ __forceinline__ void tc_mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                           uint32_t accumulate) {
+  if constexpr (kBlock == 16)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
+        : "memory");
+}
+// 512 bytes of scales, 32 rows of 16 bytes as they lie, to 4 columns of tensor memory, the same in all four lane quarters.
+__device__ __forceinline__ void tc_copy_scales(uint32_t tmem, uint32_t smem) {
+  // no swizzle: 8-row groups of 128 bytes (stride byte offset), descriptor version 1
+  const uint64_t d = (uint64_t)((smem & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n" ::"r"(tmem), "l"(d) : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int c0, int c1) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];\n" ::"l"(
+                   reinterpret_cast<uint64_t>(tmap)),
+               "r"(src), "r"(c0), "r"(c1)
+               : "memory");
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ float ld_peer(uint32_t addr, uint32_t rank) {
+  uint32_t at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void put_one(const Fp4Args& a, int64_t at, float v) {
+  if (a.out == W8A8_TYPE_F32)
+    reinterpret_cast<float*>(a.y)[at] = v;
+  else
+    reinterpret_cast<uint16_t*>(a.y)[at] = (uint16_t)(a.out == W8A8_TYPE_BF16 ? pack2<true>(v, 0.0f) : pack2<false>(v, 0.0f));
 }
 
-__global__ void __launch_bounds__(256) fp4_linear_kernel(Side w, Side x, int M, int N, int k, int block, const float* bias,
-                                                         int out, void* y, int64_t y_row) {
-  __shared__ float sx[16][33], sw[64][33];
-  pdl_wait();
+template <int kMT, int kBN, bool kSwap, int kBlock>
+__global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
+    fp4_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                    const __grid_constant__ CUtensorMap tmY, Fp4Args a) {
+  using C = Cfg<kMT, kBN, kSwap, kBlock>;
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  __shared__ uint64_t bars[2 * C::kStages + 4];
+  __shared__ uint32_t tmem_slot;
+  __shared__ float s_scale[kBN], s_bias[kBN];  // of B's rows
+  const uint32_t ring = (smem_u32(smem_raw) + 1023u) & ~1023u, staging = ring + C::kStages * C::kStage;
+  const uint32_t bar0 = smem_u32(bars);
+  auto full = [&](int i) { return bar0 + 8u * (uint32_t)i; };
+  auto empty = [&](int i) { return bar0 + 8u * (uint32_t)(C::kStages + i); };
+  auto acc_full = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::kStages + i); };
+  auto acc_free = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::kStages + 2 + i); };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
-  const int n0 = blockIdx.x * 64, groups = fp4_groups(k, block);
-  for (int m0 = blockIdx.y * 16; m0 < M; m0 += gridDim.y * 16) {
-    float acc[4] = {};
-    const int tm = threadIdx.x >> 4, tn = threadIdx.x & 15;
-    for (int k0 = 0; k0 < k; k0 += 32) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < 80 * 4; i += 256) {  // eight columns of a row
-        const int r = i >> 2, c = k0 + 8 * (i & 3);
-        const bool is_x = r < 16;
-        const int64_t row = is_x ? m0 + r : n0 + r - 16;
-        const Side& s = is_x ? x : w;
-        uint32_t codes = 0;
-        float u = 0.0f;
-        if (row < (is_x ? M : N)) {
-          codes = *reinterpret_cast<const uint32_t*>(s.codes + (row * k + c) / 2);
-          u = unit_of(s, row, c, block, groups);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(full(i), 1);
+      mbar_init(empty(i), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(acc_full(i), 1);
+      mbar_init(acc_free(i), 32 * C::kEpi);
+    }
+    fence_mbar_init();
+    prefetch_tmap(&tmA);
+    prefetch_tmap(&tmB);
+    if (!kSwap) prefetch_tmap(&tmY);
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(&tmem_slot)),
+                 "n"(C::kTmem)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  const int split = a.split, rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
+  const int tiles = a.a_tiles * a.b_tiles, first = (int)(blockIdx.x / (unsigned)split), step = (int)(gridDim.x / (unsigned)split);
+  const int all = (a.K + kKStage - 1) / kKStage;
+  const int s0 = all * rank / split, s1 = all * (rank + 1) / split;  // this CTA's stages of k
+  bool ok = true;
+
+  if (warp == 0) {
+    // -------------------------------------------------------------------------- copies
+    int g = 0;
+    // codes and scales of one operand's rows for a stage
+    auto bytes_of = [&](int s, int block0, int blocks, int of) {
+      const int pieces = min(C::kChunks, a.groups - s * C::kChunks);
+      return (uint32_t)(min(blocks, of - block0) * pieces * 512);
+    };
+    auto load = [&](bool is_b, int tile, int s, int st) {
+      const uint32_t at = ring + (uint32_t)(st * C::kStage);
+      const int rows = is_b ? kBN : C::kARows, r0 = tile * rows, block0 = r0 >> 7;
+      const int blocks = is_b ? C::kBBlocks : kMT, of = is_b ? a.b_blocks : a.a_blocks;
+      const int pieces = min(C::kChunks, a.groups - s * C::kChunks);
+      tma_load_2d(at + (is_b ? C::kARows * 128 : 0), is_b ? &tmB : &tmA, s * 128, r0, full(st));
+      for (int i = 0; i < blocks && block0 + i < of; ++i)
+        bulk_g2s(at + (uint32_t)(C::kCodes + ((is_b ? kMT : 0) + i) * C::kChunks * 512),
+                 (is_b ? a.b_scales : a.a_scales) + ((size_t)(block0 + i) * a.groups + (size_t)s * C::kChunks) * 512,
+                 (uint32_t)pieces * 512u, full(st));
+    };
+    // The weights do not wait for the launch before this one, the tokens' codes do: the first stages' weights are on their way.
+    constexpr bool kWeightsA = kSwap;
+    int ahead = 0;
+    if (first < tiles) {
+      const int at = first % a.a_tiles, bt = first / a.a_tiles;
+      ahead = min(C::kStages, s1 - s0);
+      if (elect_one())
+        for (int i = 0; i < ahead; ++i) {
+          const int s = s0 + i;
+          mbar_arrive_expect_tx(full(i), (uint32_t)C::kCodes + bytes_of(s, at * C::kARows >> 7, kMT, a.a_blocks) +
+                                             bytes_of(s, bt * kBN >> 7, C::kBBlocks, a.b_blocks));
+          load(!kWeightsA, kWeightsA ? at : bt, s, i);
         }
-        uint32_t h[4];
-        e2m1x8_to_f16(codes, h);
-        float* to = is_x ? &sx[r][8 * (i & 3)] : &sw[r - 16][8 * (i & 3)];
+      __syncwarp();
+    }
+    pdl_wait();
+    for (int u = first; ok && u < tiles; u += step) {
+      const int at = u % a.a_tiles, bt = u / a.a_tiles;
+      for (int s = s0; s < s1; ++s, ++g) {
+        const int st = g % C::kStages;
+        if (g >= C::kStages && !mbar_wait_warp(empty(st), (uint32_t)(g / C::kStages - 1) & 1u, kWaitBudgetCycles)) {
+          ok = false;
+          break;
+        }
+        if (elect_one()) {
+          if (g >= ahead) {
+            mbar_arrive_expect_tx(full(st), (uint32_t)C::kCodes + bytes_of(s, at * C::kARows >> 7, kMT, a.a_blocks) +
+                                                bytes_of(s, bt * kBN >> 7, C::kBBlocks, a.b_blocks));
+            load(!kWeightsA, kWeightsA ? at : bt, s, st);
+          }
+          load(kWeightsA, kWeightsA ? bt : at, s, st);
+        }
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) atomicOr(a.err, DEVERR_PRODUCER_WAIT);
+    for (int i = max(0, g - C::kStages); i < g; ++i)  // the last copies land before the CTA may end
+      if (!mbar_wait_warp(full(i % C::kStages), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles) && lane == 0)
+        atomicOr(a.err, DEVERR_DRAIN_WAIT);
+  } else if (warp == 1) {
+    // -------------------------------------------------------------------------- products
+    int g = 0, n = 0;
+    for (int u = first; ok && u < tiles; u += step, ++n) {
+      const int slot = n % C::kAccs, bt = u / a.a_tiles;
+      const uint32_t shift = (uint32_t)((bt * kBN & 127) >> 5);  // B's first row within its block of scales
+      if (n >= C::kAccs && !mbar_wait_warp(acc_free(slot), (uint32_t)(n / C::kAccs - 1) & 1u, kWaitBudgetCycles)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      for (int s = s0; s < s1; ++s, ++g) {
+        const int st = g % C::kStages;
+        if (!mbar_wait_warp(full(st), (uint32_t)(g / C::kStages) & 1u, kWaitBudgetCycles)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t at = ring + (uint32_t)(st * C::kStage);
+          const uint32_t sf = tmem + (uint32_t)(C::kAccs * C::kAccCols + (g & 1) * C::kSfCols);
+          const int pieces = min(C::kChunks, a.groups - s * C::kChunks);
+          for (int j = 0; j < pieces; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = unpack2<false>(h[e]);
-          to[2 * e] = f.x * u;
-          to[2 * e + 1] = f.y * u;
+            for (int i = 0; i < kMT + C::kBBlocks; ++i)
+              tc_copy_scales(sf + 4u * (uint32_t)(i < kMT ? i * C::kChunks + j : kMT * C::kChunks + j * C::kBBlocks + i - kMT),
+                             at + (uint32_t)(C::kCodes + (i * C::kChunks + j) * 512));
+          const uint64_t da = sdesc_swz(at), db = sdesc_swz(at + C::kARows * 128);
+          const int steps = min(kKStage / 64, (a.K - s * kKStage + 63) / 64);
+          for (int k = 0; k < steps; ++k) {
+            const int piece = kBlock == 16 ? k : k >> 1, half = kBlock == 16 ? 0 : k & 1;
+            const uint32_t idesc = half ? idesc_fp4<kBlock>(kBN, 1) : idesc_fp4<kBlock>(kBN, 0);
+            const uint32_t sfb = sf + (uint32_t)(4 * (kMT * C::kChunks + piece * C::kBBlocks)) + shift;
+#pragma unroll
+            for (int i = 0; i < kMT; ++i)
+              tc_mma_fp4<kBlock>(tmem + (uint32_t)(slot * C::kAccCols + i * kBN), da + (uint64_t)(i * (128 * 128 >> 4) + 2 * k),
+                                 db + (uint64_t)(2 * k), idesc, sf + (uint32_t)(4 * (i * C::kChunks + piece)), sfb,
+                                 s > s0 || k > 0);
+          }
+          tc_commit(empty(st));
+          if (s == s1 - 1) tc_commit(acc_full(slot));
+        }
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) atomicOr(a.err, DEVERR_PRODUCER_WAIT);
+    // every product issued ends before the accumulators go: the last stage's commit says so
+    if (g > 0 && !mbar_wait_warp(empty((g - 1) % C::kStages), (uint32_t)((g - 1) / C::kStages) & 1u, kWaitBudgetCycles) &&
+        lane == 0)
+      atomicOr(a.err, DEVERR_DRAIN_WAIT);
+  } else {
+    // -------------------------------------------------------------------------- outputs
+    pdl_wait();
+    const int e = warp - 2, quarter = warp & 3, mt = e >> 2, tid = threadIdx.x - 64;
+    const uint32_t lanes = tmem + ((uint32_t)(32 * quarter) << 16);
+    constexpr int kT = 32 * C::kEpi;
+    int n = 0;
+    for (int u = first; u < tiles; u += step, ++n) {
+      const int slot = n % C::kAccs, at = u % a.a_tiles, bt = u / a.a_tiles;
+      const int arow = at * C::kARows + 128 * mt + 32 * quarter + lane, b0 = bt * kBN;  // this thread's row of A
+      // scales and bias of B's rows in shared memory, of A's row here
+      const float* bs = kSwap ? a.x_scale : a.w_scale;
+      const int b_end = kSwap ? a.M : a.N, a_end = kSwap ? a.N : a.M;
+      named_bar_sync(1, kT);  // the tile before has read them
+      for (int i = tid; i < kBN; i += kT) {
+        s_scale[i] = kBlock == 16 && b0 + i < b_end ? bs[b0 + i] : 1.0f;
+        s_bias[i] = !kSwap && a.bias && b0 + i < b_end ? a.bias[b0 + i] : 0.0f;
+      }
+      const float mine = kBlock == 16 && arow < a_end ? (kSwap ? a.w_scale : a.x_scale)[arow] : 1.0f;
+      const float mine_bias = kSwap && a.bias && arow < a_end ? a.bias[arow] : 0.0f;
+      named_bar_sync(1, kT);
+      // the channel's scale first: the token's is a power of two
+      auto value = [&](float acc, int c) {
+        float v = acc;
+        if constexpr (kBlock == 16) v = kSwap ? v * mine * s_scale[c] : v * s_scale[c] * mine;
+        return v + (kSwap ? mine_bias : s_bias[c]);
+      };
+      if (ok && !mbar_wait_warp(acc_full(slot), (uint32_t)(n / C::kAccs) & 1u, kWaitBudgetCycles)) ok = false;
+      tc_fence_after();
+      const uint32_t acc = lanes + (uint32_t)(slot * C::kAccCols + mt * kBN);
+      if (split > 1) {  // (one unit a CTA; the accumulators leave over the ring, which every product has read)
+        if constexpr (kMT == 1) {
+          if (ok)
+            for (int c = 0; c < kBN; c += 8) {
+              uint32_t r[8];
+              tmem_ld8(acc + c, r);
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                asm volatile("st.shared.u32 [%0], %1;\n" ::"r"(ring + (uint32_t)(((c + j) * 128 + 32 * quarter + lane) * 4)),
+                             "r"(r[j])
+                             : "memory");
+            }
+        }
+      } else if constexpr (kSwap) {
+        for (int c = 0; ok && c < kBN && b0 + c < b_end; c += 8) {
+          uint32_t r[8];
+          tmem_ld8(acc + c, r);
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (b0 + c + j < b_end && arow < a_end)
+              put_one(a, (int64_t)(b0 + c + j) * a.y_row + arow, value(__uint_as_float(r[j]), c + j));
+        }
+        tc_fence_before();
+        mbar_arrive(acc_free(slot));
+      } else {
+        // groups of 128 bytes of a row: 64 columns of 16 bits or 32 of fp32
+        const uint32_t stage = staging + (uint32_t)(e * 4096);
+        const bool f32 = a.out == W8A8_TYPE_F32;
+        const int row0 = at * C::kARows + 128 * mt + 32 * quarter;
+        const int cols = f32 ? 32 : 64;
+        for (int c = 0; ok && c < kBN; c += cols) {
+          if (b0 + c >= b_end || row0 >= a_end) break;
+          if (a.tma_out) {
+            if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
+            __syncwarp();
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h == 1 && f32) break;
+            uint32_t r[32];
+            tmem_ld32(acc + c + 32 * h, r);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(value(__uint_as_float(r[j]), c + 32 * h + j));
+            if (f32) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                sts128(stage + (uint32_t)(lane * 128 + ((j ^ (lane & 7)) << 4)), r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint32_t w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                  const float lo = __uint_as_float(r[8 * j + 2 * q]), hi = __uint_as_float(r[8 * j + 2 * q + 1]);
+                  w[q] = a.out == W8A8_TYPE_BF16 ? pack2<true>(lo, hi) : pack2<false>(lo, hi);
+                }
+                sts128(stage + (uint32_t)(lane * 128 + (((4 * h + j) ^ (lane & 7)) << 4)), w[0], w[1], w[2], w[3]);
+              }
+            }
+          }
+          if (a.tma_out) {
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (elect_one()) {
+              tma_store_2d(&tmY, stage, b0 + c, row0);
+              asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
+            }
+            __syncwarp();
+          } else {  // rows that begin anywhere: a row at a time
+            __syncwarp();
+            const int rows = min(32, a_end - row0), here = min(cols, b_end - b0 - c);
+            for (int r = 0; r < rows; ++r)
+              for (int j = lane; j < here; j += 32) {
+                const uint32_t byte = (uint32_t)(j * (f32 ? 4 : 2));
+                const uint32_t from = stage + (uint32_t)(r * 128) + ((((byte >> 4) ^ (uint32_t)(r & 7)) << 4) | (byte & 15u));
+                const int64_t to = (int64_t)(row0 + r) * a.y_row + b0 + c + j;
+                if (f32) {
+                  float v;
+                  asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(from) : "memory");
+                  reinterpret_cast<float*>(a.y)[to] = v;
+                } else {
+                  uint16_t v;
+                  asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(from) : "memory");
+                  reinterpret_cast<uint16_t*>(a.y)[to] = v;
+                }
+              }
+            __syncwarp();
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(acc_free(slot));
+      }
+    }
+    if (!kSwap && a.tma_out && elect_one()) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
+    if (!ok && lane == 0) atomicOr(a.err, DEVERR_CONSUMER_WAIT);
+    __syncwarp();
+  }
+  if constexpr (kMT == 1) {
+    if (split > 1) {  // each CTA adds up a share of the columns of all of its cluster's accumulators
+      cluster_sync_all();
+      if (warp >= 2 && first < tiles) {
+        const int quarter = warp & 3, at = first % a.a_tiles, bt = first / a.a_tiles;
+        const int arow = at * 128 + 32 * quarter + lane, b0 = bt * kBN;
+        const int b_end = kSwap ? a.M : a.N, a_end = kSwap ? a.N : a.M;
+        const float* as = kSwap ? a.w_scale : a.x_scale;
+        const float mine = kBlock == 16 && arow < a_end ? as[arow] : 1.0f;
+        const float mine_bias = kSwap && a.bias && arow < a_end ? a.bias[arow] : 0.0f;
+        for (int c = kBN * rank / split; c < kBN * (rank + 1) / split && b0 + c < b_end; ++c) {
+          const uint32_t from = ring + (uint32_t)((c * 128 + 32 * quarter + lane) * 4);
+          float v = 0.0f;
+#pragma unroll 8
+          for (int r = 0; r < split; ++r) v += ld_peer(from, (uint32_t)r);
+          if constexpr (kBlock == 16) v = kSwap ? v * mine * s_scale[c] : v * s_scale[c] * mine;
+          v += kSwap ? mine_bias : s_bias[c];
+          if (arow < a_end) put_one(a, kSwap ? (int64_t)(b0 + c) * a.y_row + arow : (int64_t)arow * a.y_row + b0 + c, v);
         }
       }
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < 32; ++c)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = fmaf(sx[tm][c], sw[tn + 16 * j][c], acc[j]);
-    }
-    const int m = m0 + tm;
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + tn + 16 * j;
-      if (m >= M || n >= N) continue;
-      float v = acc[j];
-      if (block == 16) v = v * w.row_scale[n] * x.row_scale[m];
-      if (bias) v += bias[n];
-      if (out == W8A8_TYPE_F32)
-        static_cast<float*>(y)[m * y_row + n] = v;
-      else
-        static_cast<uint16_t*>(y)[m * y_row + n] =
-            (uint16_t)(out == W8A8_TYPE_BF16 ? pack2<true>(v, 0.0f) : pack2<false>(v, 0.0f));
+      cluster_sync_all();
     }
   }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "n"(C::kTmem) : "memory");
+  }
+}
+
+template <int kMT, int kBN, bool kSwap, int kBlock>
+w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int split, int sms, cudaStream_t st) {
+  using C = Cfg<kMT, kBN, kSwap, kBlock>;
+  static bool attr_set[64] = {};
+  int dev = 0;
+  W8A8_CUDA(cudaGetDevice(&dev));
+  auto kernel = fp4_gemm_kernel<kMT, kBN, kSwap, kBlock>;
+  if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+    W8A8_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    attr_set[dev] = true;
+  }
+  const w8a8_fp4 &fa = kSwap ? w : x, &fb = kSwap ? x : w;
+  a.a_scales = fa.scales;
+  a.b_scales = fb.scales;
+  a.a_tiles = (fa.rows + C::kARows - 1) / C::kARows;
+  a.b_tiles = (fb.rows + kBN - 1) / kBN;
+  a.a_blocks = (fa.rows + 127) / 128;
+  a.b_blocks = (fb.rows + 127) / 128;
+  a.split = split;
+  CUtensorMap ta, tb, ty;
+  const uint64_t bytes = (uint64_t)a.K / 2;
+  W8A8_TRY(make_tmap_2d(&ta, fa.codes, 1, bytes, (uint64_t)fa.rows, bytes, 128, C::kARows));
+  W8A8_TRY(make_tmap_2d(&tb, fb.codes, 1, bytes, (uint64_t)fb.rows, bytes, 128, kBN));
+  const int e = type_bytes(a.out);
+  a.tma_out = !kSwap && a.y_row * e % 16 == 0;
+  ty = ta;
+  if (a.tma_out)
+    W8A8_TRY(make_tmap_2d(&ty, a.y, e, (uint64_t)a.N, (uint64_t)a.M, (uint64_t)a.y_row * e, 128 / e, 32));
+  const int64_t tiles = (int64_t)a.a_tiles * a.b_tiles;
+  const unsigned grid = (unsigned)(split > 1 ? tiles * split : std::min<int64_t>(tiles, sms));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(C::kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = split > 1 ? 2 : 1;
+  W8A8_CUDA(cudaLaunchKernelEx(&cfg, kernel, ta, tb, ty, a));
+  return W8A8_OK;
+}
+
+// How a call is cut up.  Up to 128 tokens: as many columns of tokens as there are, 128 channels a tile.  More: 256 x 192 where such
+// tiles fill the SMs, else 128 x 128.  Parts of k: while they leave a CTA four stages, and the tiles do not fill the SMs.
+template <int kBlock>
+w8a8_status run_gemm(const w8a8_fp4& x, const w8a8_fp4& w, const Fp4Args& a, int sms, cudaStream_t st) {
+  const int stages = (a.K + kKStage - 1) / kKStage;
+  auto parts = [&](int64_t tiles) {
+    int s = 1;
+    while (s < 8 && tiles * 2 * s <= sms && stages >= 4 * 2 * s) s *= 2;
+    return s;
+  };
+  const int64_t channels = (a.N + 127) / 128;
+  if (a.M <= 128) {
+    const int s = parts(channels);
+    if (a.M <= 16) return launch<1, 16, true, kBlock>(x, w, a, s, sms, st);
+    if (a.M <= 32) return launch<1, 32, true, kBlock>(x, w, a, s, sms, st);
+    if (a.M <= 64) return launch<1, 64, true, kBlock>(x, w, a, s, sms, st);
+    return launch<1, 128, true, kBlock>(x, w, a, s, sms, st);
+  }
+  const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 191) / 192);
+  if (big >= sms) return launch<2, 192, false, kBlock>(x, w, a, 1, sms, st);
+  return launch<1, 128, false, kBlock>(x, w, a, parts((int64_t)((a.M + 127) / 128) * channels), sms, st);
 }
 
 struct LinearFp4Ws {
@@ -128,9 +571,17 @@ extern "C" w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void*
              reinterpret_cast<float*>(base + L.row_scale)};
   cudaStream_t st = as_stream(stream);
   W8A8_TRY(launch_fp4_quantize(dtype, X, x_row, x, false, false, st));
-  const Side ws{w->codes, w->scales, w->row_scale}, xs{x.codes, x.scales, x.row_scale};
-  const unsigned gy = (unsigned)((M + 15) / 16 < 65535 ? (M + 15) / 16 : 65535);
-  W8A8_CUDA(launch_pdl(fp4_linear_kernel, dim3((unsigned)((N + 63) / 64), gy), dim3(256), 0, st, ws, xs, M, N, K, (int)w->block,
-                       bias, out_dtype, Y, y_row));
-  return W8A8_OK;
+  Fp4Args a{};
+  a.x_scale = x.row_scale;
+  a.w_scale = w->row_scale;
+  a.bias = bias;
+  a.y = static_cast<char*>(Y);
+  a.y_row = M > 1 ? y_row : round_up((size_t)N, 8);  // one row has no stride
+  a.err = reinterpret_cast<unsigned int*>(base + kErrWordOffset);
+  a.M = M;
+  a.N = N;
+  a.K = K;
+  a.groups = fp4_groups(K, w->block);
+  a.out = out_dtype;
+  return w->block == 16 ? run_gemm<16>(x, *w, a, d.sms, st) : run_gemm<32>(x, *w, a, d.sms, st);
 }
