@@ -58,6 +58,8 @@ extern "C" w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cach
   AttnCall a{q, q_row, q_head, o, o_row, o_head, n_q, dim, window, batch->max_new, scale, dtype == W8A8_TYPE_BF16};
   if (a.window >= 1 << 30) a.window = 0;  // beyond every position
   W8A8_TRY(gave_up_word(&a.gave_up));
+  if ((long long)a.max_new * (n_q / pc.p.n_kv) <= 16)
+    return launch_attn_fp4_tokens(pc, pb, a, workspace, d.sms, as_stream(stream));
   const int64_t items = (int64_t)pb.n_rows * n_q;
   const dim3 grid((unsigned)(items / 4 + 1 < 152 * 64 ? items / 4 + 1 : 152 * 64));
   auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, as_stream(stream), pc, pb, a); };

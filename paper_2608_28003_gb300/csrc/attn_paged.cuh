@@ -345,6 +345,67 @@ __device__ __forceinline__ Pieces pieces_of(const Walk& w, const LineStart& ls) 
   return p;
 }
 
+constexpr int kTokenRows = 16;    // rows of a partial of the kernels for tokens: [row][dim] outputs, then the rows' m and l
+constexpr int kMaxPieces = 192;   // of an item: no more than CTAs
+
+// The pieces of an item of up to 16 rows, joined in their order, by the consumer warps (threads 0 .. 32 kWarps - 1; barrier 1): outputs, times `back`, to o (row r at (r / group) o_row + (r % group) o_head).
+// What another SM has just written takes a microsecond to read, so few loads follow one another: the statistics of all
+// pieces (a warp a row, lane = piece), then every thread's part of the output with up to kAhead pieces in flight.  Rows whose
+// result is not finite, or without weight, are marked in *bad.  Not inline: its registers are not the main loop's.
+template <bool kBf16, int kDim, int kWarps>
+__device__ __noinline__ void join_pieces(const float* part, int first, int count, int rows, int group, uint16_t* o, int64_t o_row,
+                                         int64_t o_head, float* fac, uint32_t* bad, float back = 1.0f) {
+  constexpr int kRows = kTokenRows, kPart = kRows * kDim + 2 * kRows, kConsumers = 32 * kWarps, kAhead = 8;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto slot = [&](int i) { return part + (size_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * kPart; };
+  float* sums = fac + kMaxPieces * kRows;  // fac: [piece][row] 2^(m - max)
+  for (int r = warp; r < rows; r += kWarps) {
+    float mi[kMaxPieces / 32], li[kMaxPieces / 32], top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kMaxPieces / 32; ++j) {
+      const bool there = lane + 32 * j < count;
+      mi[j] = there ? __ldcg(slot(lane + 32 * j) + kRows * kDim + r) : -INFINITY;
+      li[j] = there ? __ldcg(slot(lane + 32 * j) + kRows * kDim + kRows + r) : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < kMaxPieces / 32; ++j) top = fmaxf(top, mi[j]);
+    top = warp_max_f(top);
+#pragma unroll
+    for (int j = 0; j < kMaxPieces / 32; ++j) {
+      const float f = mi[j] == -INFINITY ? 0.0f : ex2(mi[j] - top);
+      sum = fmaf(li[j], f, sum);
+      fac[(lane + 32 * j) * kRows + r] = f;
+    }
+    sum = warp_sum_f(sum);
+    if (lane == 0) sums[r] = sum;
+  }
+  named_bar_sync(1, kConsumers);
+  for (int e = threadIdx.x; e < rows * (kDim / 4); e += kConsumers) {  // four dims of a row
+    const int r = e / (kDim / 4);
+    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+      float4 x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i0 + i < count) x[i] = __ldcg(reinterpret_cast<const float4*>(slot(i0 + i)) + e);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (i0 + i < count) {
+          const float f = fac[(i0 + i) * kRows + r];
+          y.x = fmaf(x[i].x, f, y.x);
+          y.y = fmaf(x[i].y, f, y.y);
+          y.z = fmaf(x[i].z, f, y.z);
+          y.w = fmaf(x[i].w, f, y.w);
+        }
+    }
+    const float sum = sums[r], inv = 1.0f / sum;
+    y.x = y.x * inv * back, y.y = y.y * inv * back, y.z = y.z * inv * back, y.w = y.w * inv * back;
+    *reinterpret_cast<uint2*>(o + (r / group) * o_row + (r % group) * o_head + 4 * (e % (kDim / 4))) =
+        make_uint2(pack2<kBf16>(y.x, y.y), pack2<kBf16>(y.z, y.w));
+    if (y.x * 0.0f + y.y * 0.0f + y.z * 0.0f + y.w * 0.0f != 0.0f || !(sum > 0.0f)) atomicOr(bad, 1u << r);
+  }
+}
+
 // ------------------------------------------------------------------------------- one row exactly
 // One row's attention by one warp, key by key in the order of the formula: NaN and infinities travel as they do
 // in it, and nothing outside the row's range is read.  The kernels run it for rows whose result is not finite (a value

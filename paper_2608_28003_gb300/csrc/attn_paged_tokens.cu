@@ -24,8 +24,7 @@ namespace w8a8 {
 
 namespace {
 
-constexpr int kRows = 16;
-constexpr int kMaxPieces = 192;  // of an item: no more than CTAs
+constexpr int kRows = kTokenRows;
 
 template <int kDim>
 struct Cfg {
@@ -41,6 +40,7 @@ struct Cfg {
   static constexpr int kThreads = 32 * (kWarps + 1);
   // floats of a partial: [16 rows][dim] outputs, then m and l of the rows
   static constexpr int kPart = kRows * kDim + 2 * kRows;
+  static_assert(kJoin >= (kMaxPieces + 1) * kRows * (int)sizeof(float), "the factors of a join fit over the join buffer");
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -61,66 +61,6 @@ __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uin
     mma_bf16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
   else
     mma_f16_16816(c, a[0], a[1], a[2], a[3], b0, b1);
-}
-
-// The pieces of an item, joined in their order, by the consumer warps: outputs to o (row r at (r / group) o_row + (r % group) o_head).
-// What another SM has just written takes a microsecond to read, so few loads follow one another: the statistics of all
-// pieces (a warp a row, lane = piece), then every thread's part of the output with up to kAhead pieces in flight.  Rows whose
-// result is not finite, or without weight, are marked in *bad.  Not inline: its registers are not the main loop's.
-template <bool kBf16, int kDim>
-__device__ __noinline__ void join_pieces(const float* part, int first, int count, int rows, int group, uint16_t* o, int64_t o_row,
-                                         int64_t o_head, float* fac, uint32_t* bad) {
-  using C = Cfg<kDim>;
-  constexpr int kConsumers = 32 * C::kWarps, kAhead = 8;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto slot = [&](int i) { return part + (size_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * C::kPart; };
-  float* sums = fac + kMaxPieces * kRows;  // fac: [piece][row] 2^(m - max)
-  static_assert(C::kJoin >= (kMaxPieces + 1) * kRows * (int)sizeof(float), "the factors fit over the join buffer");
-  for (int r = warp; r < rows; r += C::kWarps) {
-    float mi[kMaxPieces / 32], li[kMaxPieces / 32], top = -INFINITY, sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < kMaxPieces / 32; ++j) {
-      const bool there = lane + 32 * j < count;
-      mi[j] = there ? __ldcg(slot(lane + 32 * j) + kRows * kDim + r) : -INFINITY;
-      li[j] = there ? __ldcg(slot(lane + 32 * j) + kRows * kDim + kRows + r) : 0.0f;
-    }
-#pragma unroll
-    for (int j = 0; j < kMaxPieces / 32; ++j) top = fmaxf(top, mi[j]);
-    top = warp_max_f(top);
-#pragma unroll
-    for (int j = 0; j < kMaxPieces / 32; ++j) {
-      const float f = mi[j] == -INFINITY ? 0.0f : ex2(mi[j] - top);
-      sum = fmaf(li[j], f, sum);
-      fac[(lane + 32 * j) * kRows + r] = f;
-    }
-    sum = warp_sum_f(sum);
-    if (lane == 0) sums[r] = sum;
-  }
-  named_bar_sync(1, kConsumers);
-  for (int e = threadIdx.x; e < rows * (kDim / 4); e += kConsumers) {  // four dims of a row
-    const int r = e / (kDim / 4);
-    float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i0 = 0; i0 < count; i0 += kAhead) {
-      float4 x[kAhead];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (i0 + i < count) x[i] = __ldcg(reinterpret_cast<const float4*>(slot(i0 + i)) + e);
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i)
-        if (i0 + i < count) {
-          const float f = fac[(i0 + i) * kRows + r];
-          y.x = fmaf(x[i].x, f, y.x);
-          y.y = fmaf(x[i].y, f, y.y);
-          y.z = fmaf(x[i].z, f, y.z);
-          y.w = fmaf(x[i].w, f, y.w);
-        }
-    }
-    const float sum = sums[r], inv = 1.0f / sum;
-    y.x *= inv, y.y *= inv, y.z *= inv, y.w *= inv;
-    *reinterpret_cast<uint2*>(o + (r / group) * o_row + (r % group) * o_head + 4 * (e % (kDim / 4))) =
-        make_uint2(pack2<kBf16>(y.x, y.y), pack2<kBf16>(y.z, y.w));
-    if (y.x * 0.0f + y.y * 0.0f + y.z * 0.0f + y.w * 0.0f != 0.0f || !(sum > 0.0f)) atomicOr(bad, 1u << r);
-  }
 }
 
 template <bool kBf16, int kDim>
@@ -474,8 +414,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     }
     named_bar_sync(kBar, kConsumers);
     if (s_last) {
-      join_pieces<kBf16, kDim>(part, ps.first, ps.count, rows, group, out_at(0), a.o_row, a.o_head,
-                               reinterpret_cast<float*>(join), &s_bad);
+      join_pieces<kBf16, kDim, C::kWarps>(part, ps.first, ps.count, rows, group, out_at(0), a.o_row, a.o_head,
+                                          reinterpret_cast<float*>(join), &s_bad);
       mend();
     }
     named_bar_sync(kBar, kConsumers);  // s_last, s_bad and the statistics are free again

@@ -20,4 +20,8 @@ w8a8_status make_tmap_2d(CUtensorMap* map, const void* base, int elem_bytes, uin
 w8a8_status make_tmap_16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
                          const uint32_t* box);
 
+// The same of bytes; boxes of up to 128 bytes of the innermost dimension, swizzled over 128 or 64 bytes (0: not).
+w8a8_status make_tmap_8(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_bytes,
+                        const uint32_t* box, int swizzle_bytes);
+
 }  // namespace w8a8

@@ -31,9 +31,9 @@ def _np(t):
     return t.detach().double().cpu().numpy()
 
 
-def fp4_batch(new, keys, page, n_kv, dim, seed, heads_first=False, exps=(1, -2), fill=None, **kw):
-    """make_batch with its cache in 4 bits: codes and scales as views of one pool (with room between heads), and what they
-    stand for as k and v.  fill: scale bytes of the slots that hold no key of the batch."""
+def fp4_batch(new, keys, page, n_kv, dim, seed, heads_first=False, exps=(1, -2), fill=None, tight=False, **kw):
+    """make_batch with its cache in 4 bits: codes and scales as views of one pool (with room between heads, or tight), and what
+    they stand for as k and v.  fill: scale bytes of the slots that hold no key of the batch."""
     b = make_batch(new, keys, page, n_kv, dim, torch.float32, seed, **kw)
     n = b["k"].shape[0]
     live = torch.zeros(n, page, dtype=torch.bool, device="cuda")
@@ -57,7 +57,9 @@ def fp4_batch(new, keys, page, n_kv, dim, seed, heads_first=False, exps=(1, -2),
         pool = torch.randint(0, 256, (*shape, dim // 2 + 32), device="cuda", generator=_gen(seed + 7), dtype=torch.int32).to(torch.uint8)
         spool = torch.full((*shape, dim // 8), 127, device="cuda", dtype=torch.uint8)
         codes, scales = pool[..., :dim // 2], spool[..., dim // 16:]
-        if dim == 64:
+        if tight:
+            codes, scales = pool[..., :dim // 2].contiguous(), spool[..., :dim // 16].contiguous()
+        elif dim == 64:
             codes, scales = pool[..., 16:dim // 2 + 16], spool[..., :dim // 16]
         if heads_first:
             codes, scales = codes.transpose(1, 2), scales.transpose(1, 2)
@@ -181,10 +183,12 @@ def test_values_of_pages(B):
 
 
 # ----------------------------------------------------------------------------------- attention
+@pytest.mark.parametrize("tight", [False, True])
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 @pytest.mark.parametrize("new,keys,page,n_q,n_kv,dim,window", ATTN)
-def test_attention(B, dt, new, keys, page, n_q, n_kv, dim, window):
-    b = fp4_batch(new, keys, page, n_kv, dim, len(keys) + dim, heads_first=page != 16)
+def test_attention(B, dt, new, keys, page, n_q, n_kv, dim, window, tight):
+    """Pools with room between the heads and without (where a page's scales are one piece if its slots follow one another)."""
+    b = fp4_batch(new, keys, page, n_kv, dim, len(keys) + dim, heads_first=page != 16, tight=tight)
     cache, batch = objects(B, b)
     q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 1.5).to(DT[dt])
     attn_check(B.fp4_paged_attention(cache, batch, q, window=window), q, b, dim ** -0.5, window)
@@ -197,11 +201,11 @@ def test_attention_never_reads_what_is_masked(B, dim, n_q, n_kv, new, keys, bad)
     """Slots behind a sequence's end, before its window and in pages of nobody hold NaN or the largest scales; rows of no
     sequence stay as they were; strides of both kinds."""
     window = 150
-    b = fp4_batch(new, keys, 16, n_kv, dim, 5, heads_first=dim == 128, rows_after=3, fill=bad)
+    b = fp4_batch(new, keys, 32, n_kv, dim, 5, heads_first=dim == 128, rows_after=3, fill=bad, tight=n_q == 4 or n_q == 8)
     for s, (n, kk) in enumerate(zip(new, keys)):  # evicted: what no row of the sequence sees
         for p in range(0, max(0, kk - n - window + 1)):
             for t in (b["ks"], b["vs"]):
-                t[int(b["pages"][s, p // 16]), p % 16] = bad
+                t[int(b["pages"][s, p // 32]), p % 32] = bad
     refresh(b)
     cache, batch = objects(B, b)
     wide = torch.randn(b["n_rows"], n_q + 2, dim + 8, device="cuda", generator=_gen(8)).bfloat16()
@@ -305,7 +309,7 @@ def test_attention_split_over_the_gpu(B, n_q, n_kv, dim, seqs, new, ctx, window)
     """Enough keys that rows are divided between CTAs and joined again; the same bits every time."""
     rng = random.Random(seqs)
     keys = [rng.randint(new, ctx) for _ in range(seqs)]
-    b = fp4_batch([new] * seqs, keys, 64, n_kv, dim, 6)
+    b = fp4_batch([new] * seqs, keys, 64, n_kv, dim, 6, heads_first=True, tight=True)
     cache, batch = objects(B, b)
     q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 1.5).bfloat16()
     got = B.fp4_paged_attention(cache, batch, q, window=window)
