@@ -7,17 +7,18 @@
 // chosen so that codes need no shuffles:
 //  * scores: lane (g, q) = (lane / 4, lane % 4) has keys g and g + 8 and a quarter of their dims, whole blocks of them, 32, 16 or 8
 //    bytes as they lie; a product's k index is 4 dims of each of the quarters, the queries laid out alike;
-//  * values: lane (g, q) has an eighth of the dims of keys 2q, 2q + 1, 2q + 8, 2q + 9; two keys' pairs of dims become two dims' pairs of
-//    keys by two byte permutes.
+//  * values: lane (g, q) has an eighth of the dims of keys 2q, 2q + 1, 2q + 8, 2q + 9; the codes of two keys are
+//    interleaved by masks and a shift, so that a byte is a dim's two keys.
 // A code is converted (two an instruction) and multiplied by its block's scale in fp16, which is exact: six significant bits between
 // 2^-10 and 2688.  2^k_exp and 2^v_exp are applied to scores and outputs.
 // Queries are fp16 too: a row is brought to [2^14, 2^15) by a power of two, which is exact for fp16 and for all of a bf16 row's dims
 // down to 2^-29 of its largest (smaller ones are off by at most 2^-40 of it, less than fp32 sums are).  Weights are
 // fp16 lifted to 2^15 (attn_paged.cuh), whatever the type.
 //
-// One CTA per SM walks its stretch of the line of key tiles (attn_paged.cuh).  A loader warp copies the codes page by page by TMA and
-// the scales by bulk copies where a page's are contiguous, else key by key, into a ring of tiles of 36 KB (128, 256, 512 keys
-// at head dims 256, 128, 64); 8 consumer warps take 16, 32 or 64 keys of a tile each, on their own from scores to output.
+// One CTA per SM walks its stretch of the line of key tiles (attn_paged.cuh).  Four loader warps, one each for the codes and the
+// scales of keys and values, fill a ring of tiles of 36 KB (128, 256, 512 keys at head dims 256, 128, 64): codes page by page by
+// TMA (an operation costs its warp some 70 cycles, which one warp for all of them could not afford), scales 16 bytes a lane where a
+// page's follow one another, else key by key; 8 consumer warps take 16, 32 or 64 keys of a tile each, on their own from scores to output.
 // A warp's reference moves when one of its lanes sees a score that outgrew it, so a step has no reduction over lanes; sums stay
 // in the lanes until the item ends.
 #include "attn_fp4.cuh"
@@ -30,28 +31,31 @@ namespace {
 
 constexpr int kWarps = 8;  // consumers
 
-template <int kDim>
+template <int kDim, int kNt>
 struct Cfg {
-  static constexpr int kBlocks = 256 / kDim;                  // of 16 keys, that a warp has of a tile
-  static constexpr int kBk = 16 * kBlocks * kWarps, kBkShift = kDim == 256 ? 7 : kDim == 128 ? 8 : 9;
+  static constexpr int kTeams = kDim == 256 ? 2 : 1;          // of warps, that take tiles in turn
+  static constexpr int kTeam = kWarps / kTeams;               // warps of a team
+  static constexpr int kBlocks = kDim == 64 ? 4 : 2;          // of 16 keys, that a warp has of a tile, two at a time
+  static constexpr int kBk = 16 * kBlocks * kTeam, kBkShift = kDim == 256 ? 7 : kDim == 128 ? 8 : 9;
   static constexpr int kRow = kDim / 2, kSRow = kDim / 16;    // bytes of a key's codes, scales
   static constexpr int kCodes = kBk * kRow, kScales = kBk * kSRow;
   static constexpr int kStage = 2 * (kCodes + kScales);       // K codes, V codes, K scales, V scales
   static constexpr int kJoin = kWarps * 8 * kDim * 4;         // 8 rows' outputs of every warp
-  static constexpr int kQ = 32 * (kDim / 16) * 16;            // two tiles of queries, for items of more than 8 rows
-  static constexpr int kStages = kDim == 256 ? 4 : 5;
+  static constexpr int kQRow = 2 * kDim + 16;                 // bytes between the rows of an item's queries
+  static constexpr int kQ = 2 * 8 * kNt * kQRow;              // of two items
+  static constexpr int kStages = (kDim == 256 ? 5 : 6) - kNt;
   static constexpr int kSmem = kStages * kStage + kJoin + kQ + 1024;
-  static constexpr int kThreads = 32 * (kWarps + 1);
+  static constexpr int kThreads = 384;                        // consumers and four loaders
   static constexpr int kTiles = kDim / 16;                    // of 16 dims
   static constexpr int kPer = kTiles < kWarps ? 1 : kTiles / kWarps;  // tiles that a warp joins
-  static_assert(kSmem <= 227 * 1024 - 2048, "shared memory");
+  static_assert(kSmem + (kNt == 1 ? 0 : 32 * kDim) <= 227 * 1024 - 3072, "shared memory");
 };
 
 // Where byte `byte` of a key's codes lies in a tile: rows of 128 bytes swizzled over 128, of 64 over 64, of 32 as they are.
 template <int kDim>
 __device__ __forceinline__ uint32_t code_at(int key, int byte) {
   const int swz = kDim == 256 ? (key & 7) << 4 : kDim == 128 ? ((key >> 1) & 3) << 4 : 0;
-  return (uint32_t)(key * Cfg<kDim>::kRow + (byte ^ swz));
+  return (uint32_t)(key * (kDim / 2) + (byte ^ swz));
 }
 __device__ __forceinline__ uint32_t lds8(uint32_t a) {
   uint16_t v;
@@ -94,31 +98,39 @@ struct LoadPlan {
 };
 
 template <bool kBf16, int kDim, int kNt>
-__global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
+__global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
     attn_fp4_tokens_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, Fp4Pages c,
                            PagedBatch b, AttnCall a, LoadPlan plan, int tt, float* __restrict__ part,
                            unsigned int* __restrict__ counters, unsigned int* __restrict__ err) {
-  using C = Cfg<kDim>;
+  using C = Cfg<kDim, kNt>;
   constexpr int kRows = 8 * kNt, kPart = kTokenRows * kDim + 2 * kTokenRows;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
-  __shared__ uint64_t bars[2 * C::kStages];
+  __shared__ uint64_t bars[2 * C::kStages + 4];
   __shared__ LineStart ls;
   __shared__ long long scan[C::kThreads / 32];
   __shared__ uint32_t held[C::kStages];  // 16-key groups of a stage's tile that lie in a page
-  __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
+  __shared__ __align__(16) float s_m[kRows][kWarps], s_l[kRows][kWarps];
+  __shared__ uint4 qs[kNt == 1 ? 1 : kDim / 16 * 32];  // items of more than 8 rows: the right operand, [k step][lane]
   __shared__ uint32_t s_last, s_bad, s_beat;
   const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
   uint8_t* behind = smem_raw + (ring - raw) + C::kStages * C::kStage;
   float4* join = reinterpret_cast<float4*>(behind);
-  uint4* qs = reinterpret_cast<uint4*>(behind + C::kJoin);  // [k step][lane]
+  const uint32_t qring = ring + (uint32_t)(C::kStages * C::kStage + C::kJoin);  // the queries of two items as they come
   const uint32_t bar0 = smem_u32(bars);
   auto full = [&](int i) { return bar0 + 8u * (uint32_t)i; };
   auto empty = [&](int i) { return bar0 + 8u * (uint32_t)(C::kStages + i); };
+  auto q_full = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::kStages + i); };
+  auto q_free = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::kStages + 2 + i); };
+  const int group = a.n_q / c.p.n_kv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, shift = c.p.page_shift, n_kv = c.p.n_kv;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) {
-      mbar_init(full(i), plan.contiguous ? 1 : 33);
-      mbar_init(empty(i), kWarps);
+      mbar_init(full(i), 2 + 64);  // two counts of bytes, two warps of lanes
+      mbar_init(empty(i), C::kTeam);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full(i), 32);
+      mbar_init(q_free(i), kNt == 1 ? kWarps : 1);
     }
     fence_mbar_init();
     prefetch_tmap(&tmK);
@@ -131,14 +143,33 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   if (ls.begin >= ls.end) return;
   Walk w;
   w.start(ls, b, shift, a.window, tt, C::kBkShift, lane);
-  int g = 0;  // tiles of this CTA so far
+  int g = 0, item = 0;  // tiles and items of this CTA so far
   bool ok = true;
 
-  if (warp == kWarps) {
-    // -------------------------------------------------------------------------- loader
-    const int box = min(kBoxSlots, 1 << shift), boxes = C::kBk / box;  // per tile
-    for (; ok && w.more(); w.next(b, shift, n_kv, a.window, tt, C::kBkShift)) {
+  // registers: 384 threads of 168 are shared out as 256 of 216 and 128 of 72
+  if (warp >= kWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;\n");
+    // ------------------------------------------ loaders: K codes, V codes, K scales, V scales and queries
+    const int what = warp - kWarps, kv = what & 1;
+    const int box = min(1 << shift, C::kBk), boxes = C::kBk / box;  // per tile
+    const uint8_t* scales = kv ? c.vs : c.ks;
+    for (; ok && w.more(); w.next(b, shift, n_kv, a.window, tt, C::kBkShift), ++item) {
       const int lo = w.lo(a.window, tt), hi = w.hi(tt);
+      if (what == 3) {  // the item's queries
+        if (item >= 2 && !wait_beat(q_free(item & 1), (uint32_t)(item / 2 - 1) & 1u, &s_beat)) {
+          ok = false;
+          break;
+        }
+        const int tok0 = w.t * tt, rows = min(w.q.rows - tok0, tt) * group;
+        for (int e = lane; e < rows * (kDim / 8); e += 32) {
+          const int r = e / (kDim / 8), at = e % (kDim / 8);
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(
+                           qring + (uint32_t)(((item & 1) * kRows + r) * C::kQRow + 16 * at)),
+                       "l"(a.q + (int64_t)(w.q.row0 + tok0 + r / group) * a.q_row + (int64_t)(w.h * group + r % group) * a.q_head + 8 * at)
+                       : "memory");
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(q_full(item & 1)) : "memory");
+      }
       constexpr int kGroups = C::kBk / 16, kBatch = 32 / kGroups;  // tiles whose pages are read at once, ahead of their use
       int page = group_page(b, c.p, w.s, (w.first + w.k0) << C::kBkShift, lo, hi, box, lane), ahead = -1;
       for (int i = 0; i < w.cnt; ++i, ++g) {
@@ -153,38 +184,32 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           ok = false;
           break;
         }
-        const uint32_t dst = ring + (uint32_t)(st * C::kStage), sdst = dst + 2 * C::kCodes;
-        if (lane == 0) {
-          held[st] = there;
-          const int found = __popc(there & (box == 16 ? 0xffffffffu : 0x55555555u));  // boxes with a page
-          mbar_arrive_expect_tx(full(st), 2u * C::kCodes + (plan.contiguous ? (uint32_t)(found * 2 * box * C::kSRow) : 0u));
-        }
-        __syncwarp();
-        for (int o0 = 0; o0 < 2 * boxes; o0 += 32) {
-          const int o = o0 + lane, bx = o % boxes, kv = o / boxes;
-          const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + bx * (box / 16)) & 31);
-          if (o < 2 * boxes) {
-            const int slot = (tile0 + bx * box) & ((1 << shift) - 1);
-            // a page that holds nothing: a coordinate outside the tensor, which fills zeros
-            tma_load_4d(dst + (uint32_t)(kv * C::kCodes + bx * box * C::kRow), kv ? &tmV : &tmK, 0, slot, w.h,
-                        pg < 0 ? c.p.n_pages : pg, full(st));
-            if (plan.contiguous && pg >= 0)
-              bulk_g2s(sdst + (uint32_t)(kv * C::kScales + bx * box * C::kSRow),
-                       (kv ? c.vs : c.ks) + (int64_t)pg * c.s_page + (int64_t)slot * c.s_slot + (int64_t)w.h * c.s_head,
-                       (uint32_t)(box * C::kSRow), full(st));
+        const uint32_t dst = ring + (uint32_t)(st * C::kStage + kv * C::kCodes),
+                       sdst = ring + (uint32_t)(st * C::kStage + 2 * C::kCodes + kv * C::kScales);
+        if (what < 2) {
+          if (lane == 0) {
+            if (kv == 0) held[st] = there;
+            mbar_arrive_expect_tx(full(st), (uint32_t)C::kCodes);
           }
-        }
-        if (!plan.contiguous) {
-          for (int e0 = 0; e0 < C::kBk; e0 += 32) {
-            const int key = e0 + lane, pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + key / 16) & 31);
+          __syncwarp();
+          const int pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + lane * (box / 16)) & 31);
+          if (lane < boxes)  // a page that holds nothing: a coordinate outside the tensor, which fills zeros
+            tma_load_4d(dst + (uint32_t)(lane * box * C::kRow), kv ? &tmV : &tmK, 0, (tile0 + lane * box) & ((1 << shift) - 1), w.h,
+                        pg < 0 ? c.p.n_pages : pg, full(st));
+        } else {
+          // 16 bytes a lane where a page's scales follow one another, else a key's
+          const int per = plan.contiguous ? 16 / C::kSRow : 1;
+          for (int k0 = 0; k0 < C::kBk; k0 += 32 * per) {
+            const int key = k0 + lane * per, pg = __shfl_sync(0xffffffffu, page, (in_batch * kGroups + key / 16) & 31);
             if (pg >= 0) {
-              const int64_t from = (int64_t)pg * c.s_page + (int64_t)((tile0 + key) & ((1 << shift) - 1)) * c.s_slot +
-                                   (int64_t)w.h * c.s_head;
-#pragma unroll
-              for (int kv = 0; kv < 2; ++kv)
-                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(
-                                 sdst + (uint32_t)(kv * C::kScales + key * C::kSRow)),
-                             "l"((kv ? c.vs : c.ks) + from), "n"(C::kSRow)
+              const uint8_t* from = scales + (int64_t)pg * c.s_page + (int64_t)((tile0 + key) & ((1 << shift) - 1)) * c.s_slot +
+                                    (int64_t)w.h * c.s_head;
+              if (plan.contiguous)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(sdst + (uint32_t)(key * C::kSRow)), "l"(from)
+                             : "memory");
+              else
+                asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(sdst + (uint32_t)(key * C::kSRow)), "l"(from),
+                             "n"(C::kSRow)
                              : "memory");
             }
           }
@@ -194,18 +219,22 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     }
     // the last copies land before the CTA may end
     if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
-    for (int k = max(0, g - C::kStages); k < g; ++k)
-      if (!wait_beat(full(k % C::kStages), (uint32_t)(k / C::kStages) & 1u, &s_beat) && lane == 0)
-        give_up(err, a, DEVERR_DRAIN_WAIT);
+    if (what >= 2)
+      asm volatile("cp.async.wait_all;\n" ::: "memory");
+    else
+      for (int k = max(0, g - C::kStages); k < g; ++k)
+        if (!wait_beat(full(k % C::kStages), (uint32_t)(k / C::kStages) & 1u, &s_beat) && lane == 0)
+          give_up(err, a, DEVERR_DRAIN_WAIT);
     return;
   }
 
   // -------------------------------------------------------------------------- consumers
-  constexpr int kBar = 1, kConsumers = 32 * kWarps, kSteps = kDim / 16;
-  const int group = a.n_q / n_kv;
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 216;\n");
+  constexpr int kBar = 1, kConsumers = 32 * kWarps, kSteps = kDim / 16, kChains = kNt == 1 ? 4 : 2;
   const int gq = lane >> 2, quad = lane & 3;
   const float back = two_to(c.v_exp);
-  for (; w.more(); w.next(b, shift, n_kv, a.window, tt, C::kBkShift)) {
+  const int team = warp / C::kTeam, in_team = warp % C::kTeam;
+  for (; w.more(); w.next(b, shift, n_kv, a.window, tt, C::kBkShift), ++item) {
     const int tok0 = w.t * tt, n_tok = min(w.q.rows - tok0, tt), rows = n_tok * group;
     const int lo = w.lo(a.window, tt), hi = w.hi(tt);
     // where every row of the item sees everything: between the last row's first key and the first row's position
@@ -214,17 +243,16 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     uint32_t qf[kNt == 1 ? kSteps : 1][2];
     float fac[kNt][2];  // of rows 8 n + 2 quad + {0, 1}: scores in powers of two
     int pos[kNt][2], from[kNt][2];
+    if (ok && !wait_beat(q_full(item & 1), (uint32_t)(item / 2) & 1u, &s_beat)) ok = false;
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
       const int r = 8 * n + gq;
       uint4 x[kDim / 32];
       uint32_t top = 0;
       const bool live = r < rows;
-      const uint16_t* qp = a.q + (int64_t)(w.q.row0 + tok0 + (live ? r / group : 0)) * a.q_row +
-                           (int64_t)(w.h * group + (live ? r % group : 0)) * a.q_head + quad * (kDim / 4);
 #pragma unroll
       for (int i = 0; i < kDim / 32; ++i) {
-        x[i] = live ? *reinterpret_cast<const uint4*>(qp + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+        x[i] = live ? lds128(qring + (uint32_t)(((item & 1) * kRows + r) * C::kQRow + quad * (kDim / 2) + 16 * i)) : make_uint4(0u, 0u, 0u, 0u);
         const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -269,6 +297,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       }
     }
     if constexpr (kNt > 1) named_bar_sync(kBar, kConsumers);
+    __syncwarp();
+    if (lane == 0 && (kNt == 1 || warp == 0)) mbar_arrive(q_free(item & 1));
     float m[kNt][2], l[kNt][2], acc[kNt][C::kTiles][4];
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
@@ -279,19 +309,22 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
     }
 
     for (int it = 0; it < w.cnt; ++it, ++g) {
-      const int st = g % C::kStages, k0 = 16 * C::kBlocks * warp, j00 = ((w.first + w.k0 + it) << C::kBkShift) + k0;
+      if (C::kTeams > 1 && (g & 1) != team) continue;
+      const int st = g % C::kStages, k0 = 16 * C::kBlocks * in_team, j00 = ((w.first + w.k0 + it) << C::kBkShift) + k0;
       if (ok && !wait_beat(full(st), (uint32_t)(g / C::kStages) & 1u, &s_beat)) ok = false;
       if (!ok) continue;
-      const uint32_t mine = held[st] >> (C::kBlocks * warp);
+      const uint32_t mine = held[st] >> (C::kBlocks * in_team);
       const uint32_t kt = ring + (uint32_t)(st * C::kStage), vt = kt + C::kCodes, ksc = vt + C::kCodes, vsc = ksc + C::kScales;
 #pragma unroll 1
-      for (int u = 0; u < C::kBlocks; ++u) {
-        const int key0 = k0 + 16 * u, j0 = j00 + 16 * u;
-        if (!((mine >> u) & 1u) || j0 > hi || j0 + 15 < lo) continue;
-        // ---- scores of 16 keys
-        float s[kNt][4];
-        {
-          float z[kNt][2][4] = {};  // [even, odd k steps]
+      for (int u0 = 0; u0 < C::kBlocks; u0 += 2) {  // two blocks of 16 keys
+        const int jj = j00 + 16 * u0;
+        const uint32_t both = (mine >> u0) & 3u;
+        if (both == 0 || jj > hi || jj + 31 < lo) continue;
+        float s[2][kNt][4];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int key0 = k0 + 16 * (u0 + u);
+          float z[kNt][kChains][4] = {};  // k steps in turn
           uint32_t sp[2][kDim / 64];
 #pragma unroll
           for (int r = 0; r < 2; ++r) {
@@ -331,46 +364,56 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                   const uint4 v = qs[k * 32 + lane];
                   q0 = v.x, q1 = v.y, q2 = v.z, q3 = v.w;
                 }
-                mma_f16_16816(z[0][y], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1], q0, q1);
+                mma_f16_16816(z[0][k % kChains], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1], q0, q1);
                 if constexpr (kNt > 1)
-                  mma_f16_16816(z[kNt - 1][y], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1], q2, q3);
+                  mma_f16_16816(z[kNt - 1][k % kChains], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1], q2, q3);
               }
             }
           }
 #pragma unroll
           for (int n = 0; n < kNt; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][e] = (z[n][0][e] + z[n][1][e]) * fac[n][e & 1];
-        }
-        if (j0 < all_lo || j0 + 15 > all_hi) {
-#pragma unroll
-          for (int n = 0; n < kNt; ++n)
-#pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int j = j0 + gq + 8 * (e >> 1);
-              if (j > pos[n][e & 1] || j < from[n][e & 1]) s[n][e] = -INFINITY;
+              float x = z[n][0][e] + z[n][1][e];
+              if constexpr (kChains == 4) x += z[n][2][e] + z[n][3][e];
+              s[u][n][e] = x * fac[n][e & 1];
             }
+        }
+        if (jj < all_lo || jj + 31 > all_hi || both != 3u) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int n = 0; n < kNt; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int j = jj + 16 * u + gq + 8 * (e >> 1);
+                if (j > pos[n][e & 1] || j < from[n][e & 1] || !((both >> u) & 1u)) s[u][n][e] = -INFINITY;
+              }
         }
         // ---- the references
         bool grown = false;
+        float top[kNt][2];
 #pragma unroll
         for (int n = 0; n < kNt; ++n)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) grown = grown || fmaxf(s[n][i], s[n][2 + i]) > m[n][i] + kGrowth<false>;
+          for (int i = 0; i < 2; ++i) {
+            top[n][i] = fmaxf(fmaxf(s[0][n][i], s[0][n][2 + i]), fmaxf(s[1][n][i], s[1][n][2 + i]));
+            grown = grown || top[n][i] > m[n][i] + kGrowth<false>;
+          }
         if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
           for (int n = 0; n < kNt; ++n) {
             float up[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              float top = fmaxf(s[n][i], s[n][2 + i]);
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+              float t = top[n][i];
+              t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+              t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+              t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
               up[i] = 1.0f;
-              if (top > m[n][i] + kGrowth<false>) {  // m = -inf: any visible key
-                up[i] = m[n][i] == -INFINITY ? 0.0f : ex2(m[n][i] - top);
-                m[n][i] = top;
+              if (t > m[n][i] + kGrowth<false>) {  // m = -inf: any visible key
+                up[i] = m[n][i] == -INFINITY ? 0.0f : ex2(m[n][i] - t);
+                m[n][i] = t;
               }
               l[n][i] *= up[i];
             }
@@ -384,30 +427,35 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
         }
         // ---- the weights, keys by rows, turned into the second product's right operand, rows by keys
-        uint32_t p[kNt][2];
+        uint32_t p[2][kNt][2];
 #pragma unroll
         for (int n = 0; n < kNt; ++n) {
           const float r0 = m[n][0] == -INFINITY ? 0.0f : m[n][0] - kLift<false>, r1 = m[n][1] == -INFINITY ? 0.0f : m[n][1] - kLift<false>;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t x = pack2<false>(ex2(s[n][2 * h] - r0), ex2(s[n][2 * h + 1] - r1));
-            const float2 as_used = unpack2<false>(x);
-            l[n][0] += as_used.x;
-            l[n][1] += as_used.y;
-            p[n][h] = transposed(x);
-          }
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t x = pack2<false>(ex2(s[u][n][2 * h] - r0), ex2(s[u][n][2 * h + 1] - r1));
+              const float2 as_used = unpack2<false>(x);
+              l[n][0] += as_used.x;
+              l[n][1] += as_used.y;
+              p[u][n][h] = transposed(x);
+            }
         }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+        const int key0 = k0 + 16 * (u0 + u), j0 = jj + 16 * u;
         // ---- values: keys 2 quad + {0, 1, 8, 9}, an eighth of the dims
-        const bool cut = j0 < lo || j0 + 15 > hi;  // values of keys outside the item's range must not meet a weight of 0
-        uint32_t sv[4][kDim == 256 ? 2 : 1];
+        // values of keys outside the item's range, or in no page, must not meet a weight of 0
+        const bool none = !((both >> u) & 1u), cut = j0 < lo || j0 + 15 > hi || none;
+        uint32_t sv[2][kDim == 256 ? 2 : 1], sb[4];  // scales of the pairs of keys
         uint32_t vw[4][kDim / 64];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int key = key0 + 2 * quad + (x & 1) + 8 * (x >> 1), j = j0 + key - key0;
           const uint32_t at = vsc + (uint32_t)(key * C::kSRow);
-          uint32_t bytes = kDim == 256 ? lds16(at + 2 * gq) : kDim == 128 ? lds8(at + gq) : lds8(at + (gq >> 1));
-          if (cut && (j < lo || j > hi)) bytes = 0;
-          scale_pairs(bytes, sv[x]);
+          sb[x] = kDim == 256 ? lds16(at + 2 * gq) : kDim == 128 ? lds8(at + gq) : lds8(at + (gq >> 1));
+          if (cut && (j < lo || j > hi || none)) sb[x] = 0;
           const uint32_t from_at = vt + code_at<kDim>(key, gq * (kDim / 16));
           if constexpr (kDim == 256) {
             const uint4 v = lds128(from_at);
@@ -420,21 +468,27 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
         }
 #pragma unroll
-        for (int y = 0; y < kDim / 64; ++y) {  // 8 dims of the lane: four tiles
-          uint32_t h[4][4];
+        for (int x = 0; x < 2; ++x) {
+          sv[x][0] = e4m3x2_to_f16x2(__byte_perm(sb[2 * x], sb[2 * x + 1], 0x0040));
+          if constexpr (kDim == 256) sv[x][1] = e4m3x2_to_f16x2(__byte_perm(sb[2 * x], sb[2 * x + 1], 0x0051));
+        }
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            e2m1x8_to_f16(vw[x][y], h[x]);
+        for (int y = 0; y < kDim / 64; ++y) {  // 8 dims of the lane: four tiles of two dims
+          uint32_t h[2][2][4];                 // [pair of keys][even, odd dims][]: a dim's two keys
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[x][e] = hmul2_bits(h[x][e], sv[x][kDim == 256 ? y / 2 : 0]);
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t w0 = vw[2 * x][y], w1 = vw[2 * x + 1][y];
+            e2m1x8_to_f16((w0 & 0x0f0f0f0fu) | ((w1 << 4) & 0xf0f0f0f0u), h[x][0]);
+            e2m1x8_to_f16(((w0 >> 4) & 0x0f0f0f0fu) | (w1 & 0xf0f0f0f0u), h[x][1]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[x][e >> 2][e & 3] = hmul2_bits(h[x][e >> 2][e & 3], sv[x][kDim == 256 ? y / 2 : 0]);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t a0 = __byte_perm(h[0][e], h[1][e], 0x5410), a1 = __byte_perm(h[0][e], h[1][e], 0x7632),
-                           a2 = __byte_perm(h[2][e], h[3][e], 0x5410), a3 = __byte_perm(h[2][e], h[3][e], 0x7632);
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int n = 0; n < kNt; ++n) mma_f16_16816(acc[n][4 * y + e], a0, a1, a2, a3, p[n][0], p[n][1]);
-          }
+            for (int n = 0; n < kNt; ++n)
+              mma_f16_16816(acc[n][4 * y + e], h[0][0][e], h[0][1][e], h[1][0][e], h[1][1][e], p[u][n][0], p[u][n][1]);
+        }
         }
       }
       __syncwarp();
@@ -451,8 +505,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
         l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], 8);
         l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], 16);
         if (gq == 0) {
-          s_m[warp][8 * n + 2 * quad + i] = m[n][i];
-          s_l[warp][8 * n + 2 * quad + i] = l[n][i];
+          s_m[8 * n + 2 * quad + i][warp] = m[n][i];
+          s_l[8 * n + 2 * quad + i][warp] = l[n][i];
         }
       }
     named_bar_sync(kBar, kConsumers);
@@ -463,17 +517,22 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = 8 * n + 2 * quad + i;
-        M[n][i] = -INFINITY;
-        L[n][i] = 0.0f;
-        for (int k = 0; k < kWarps; ++k) M[n][i] = fmaxf(M[n][i], s_m[k][r]);
-        for (int k = 0; k < kWarps; ++k) {
-          const float mk = s_m[k][r];
-          L[n][i] += s_l[k][r] * (mk == -INFINITY ? 0.0f : ex2(mk - M[n][i]));
+        float mk[kWarps], lk[kWarps];
+#pragma unroll
+        for (int k = 0; k < kWarps; k += 4) {
+          *reinterpret_cast<float4*>(mk + k) = *reinterpret_cast<const float4*>(&s_m[r][k]);
+          *reinterpret_cast<float4*>(lk + k) = *reinterpret_cast<const float4*>(&s_l[r][k]);
         }
+        M[n][i] = fmaxf(fmaxf(fmaxf(mk[0], mk[1]), fmaxf(mk[2], mk[3])), fmaxf(fmaxf(mk[4], mk[5]), fmaxf(mk[6], mk[7])));
+        L[n][i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) L[n][i] += lk[k] * (mk[k] == -INFINITY ? 0.0f : ex2(mk[k] - M[n][i]));
         f[i] = m[n][i] == -INFINITY ? 0.0f : ex2(m[n][i] - M[n][i]);
       }
       // each warp adds up its tiles over the warps, in their order, 8 rows at a time
       if (n > 0) named_bar_sync(kBar, kConsumers);  // the first rows have been read
+      const bool used = 8 * n + 2 * quad < rows;  // any of the lane's two rows
+      if (used)
 #pragma unroll
       for (int i = 0; i < C::kTiles; ++i)
         join[(warp * C::kTiles + i) * 32 + lane] =
@@ -482,7 +541,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 #pragma unroll
       for (int i = 0; i < C::kPer; ++i) {
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (warp * C::kPer + i < C::kTiles) {
+        if (used && warp * C::kPer + i < C::kTiles) {
 #pragma unroll
           for (int k = 0; k < kWarps; ++k) {
             const float4 x = join[(k * C::kTiles + warp * C::kPer + i) * 32 + lane];
@@ -564,7 +623,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
 
 template <bool kBf16, int kDim, int kNt>
 w8a8_status launch(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms, cudaStream_t st) {
-  using C = Cfg<kDim>;
+  using C = Cfg<kDim, kNt>;
   static bool attr_set[64] = {};
   int dev = 0;
   W8A8_CUDA(cudaGetDevice(&dev));
@@ -577,7 +636,7 @@ w8a8_status launch(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, 
   const int page = 1 << pc.p.page_shift;
   const uint64_t dims[4] = {(uint64_t)C::kRow, (uint64_t)page, (uint64_t)pc.p.n_kv, (uint64_t)pc.p.n_pages};
   const uint64_t strides[3] = {(uint64_t)pc.p.slot_stride, (uint64_t)pc.p.head_stride, (uint64_t)pc.p.page_stride};
-  const uint32_t box[4] = {(uint32_t)C::kRow, (uint32_t)(page < kBoxSlots ? page : kBoxSlots), 1, 1};
+  const uint32_t box[4] = {(uint32_t)C::kRow, (uint32_t)(page < C::kBk ? page : C::kBk), 1, 1};
   const int swizzle = kDim == 256 ? 128 : kDim == 128 ? 64 : 0;
   W8A8_TRY(make_tmap_8(&tk, pc.k, 4, dims, strides, box, swizzle));
   W8A8_TRY(make_tmap_8(&tv, pc.v, 4, dims, strides, box, swizzle));

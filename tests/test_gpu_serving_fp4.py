@@ -8,7 +8,7 @@ import torch
 
 from oracle import fp4 as O4
 from oracle import serving as OS
-from test_gpu_serving import ATTN, attn_check, make_batch
+from test_gpu_serving import ATTN, make_batch
 
 pytestmark = pytest.mark.gpu
 
@@ -82,6 +82,25 @@ def objects(B, b):
     dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
     return (B.PagedCacheFp4(b["k4"], b["v4"], b["ks"], b["vs"], *b["exps"]),
             B.PagedBatch(dev(b["row_start"]), dev(b["kv_len"]), dev(b["pages"]), max_new=b["max_new"]))
+
+
+def attn_check(got, q, b, scale, window, rows=None):
+    """Per output: half a step of the result; weights rounded to the type and their sum (2 half-steps of the weighted |v|);
+    scores summed in fp32 (dim 2^-24 of the largest sum of |q k|, twice: numerator and sum) and exponentials and sums of 2^-20;
+    fp16 also half its smallest step.  Where weights are fp16, lifted by 2^12 against a reference that is at most the row's
+    largest, one below 2^-14 is off by up to 2^-25, 2^-37 of the largest, and vanishes below that: n 2^-37 of the largest |v|
+    over n keys (every weight's part of the sum is at most its share of the largest weight, which the sum holds)."""
+    want, mass, mag = OS.attention(_np(q), _np(b["k"]), _np(b["v"]), b, scale, window, rows)
+    dt = q.dtype
+    eps, dim = torch.finfo(dt).eps / 2, q.shape[2]
+    delta = scale * dim * 2.0 ** -24 * mag
+    vanish = float(np.max(b["kv_len"], initial=1)) if window == 0 else float(window)
+    vanish = min(vanish, b["pages"].shape[1] * b["k"].shape[1]) * 2.0 ** -37 * float(torch.nan_to_num(b["v"], 0, 0, 0).abs().max())
+    tol = eps * np.abs(want) + (2 * eps + 2 * delta[..., None] + 2.0 ** -20) * mass + (2.0 ** -25 if dt == torch.float16 else 1e-38)
+    got, some = _np(got), ~np.isnan(want).all(axis=(1, 2))
+    err = np.abs(got - want)[some] - tol[some] - vanish
+    assert err.max() <= 0, (float(err.max()), np.argwhere(err > 0)[:4].tolist())
+    return want
 
 
 # -------------------------------------------------------------------------------------- append
