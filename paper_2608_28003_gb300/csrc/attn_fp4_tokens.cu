@@ -48,7 +48,7 @@ struct Cfg {
   static constexpr int kThreads = 384;                        // consumers and four loaders
   static constexpr int kTiles = kDim / 16;                    // of 16 dims
   static constexpr int kPer = kTiles < kWarps ? 1 : kTiles / kWarps;  // tiles that a warp joins
-  static_assert(kSmem + (kNt == 1 ? 0 : 32 * kDim) <= 227 * 1024 - 3072, "shared memory");
+  static_assert(kSmem + 16 * kNt * kDim <= 227 * 1024 - 2048, "shared memory");
 };
 
 // Where byte `byte` of a key's codes lies in a tile: rows of 128 bytes swizzled over 128, of 64 over 64, of 32 as they are.
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
   __shared__ long long scan[C::kThreads / 32];
   __shared__ uint32_t held[C::kStages];  // 16-key groups of a stage's tile that lie in a page
   __shared__ __align__(16) float s_m[kRows][kWarps], s_l[kRows][kWarps];
-  __shared__ uint4 qs[kNt == 1 ? 1 : kDim / 16 * 32];  // items of more than 8 rows: the right operand, [k step][lane]
+  __shared__ uint2 qs[kNt][kDim / 16][32];  // the queries as the first product's right operand, a lane's words of a k step
   __shared__ uint32_t s_last, s_bad, s_beat;
   const uint32_t raw = smem_u32(smem_raw), ring = (raw + 1023u) & ~1023u;
   uint8_t* behind = smem_raw + (ring - raw) + C::kStages * C::kStage;
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full(i), 32);
-      mbar_init(q_free(i), kNt == 1 ? kWarps : 1);
+      mbar_init(q_free(i), kWarps);
     }
     fence_mbar_init();
     prefetch_tmap(&tmK);
@@ -146,9 +146,9 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
   int g = 0, item = 0;  // tiles and items of this CTA so far
   bool ok = true;
 
-  // registers: 384 threads of 168 are shared out as 256 of 216 and 128 of 72
+  // registers: 384 threads of 168 are shared out as 256 of 200 and 128 of 104
   if (warp >= kWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;\n");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;\n");
     // ------------------------------------------ loaders: K codes, V codes, K scales, V scales and queries
     const int what = warp - kWarps, kv = what & 1;
     const int box = min(1 << shift, C::kBk), boxes = C::kBk / box;  // per tile
@@ -229,8 +229,8 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
   }
 
   // -------------------------------------------------------------------------- consumers
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 216;\n");
-  constexpr int kBar = 1, kConsumers = 32 * kWarps, kSteps = kDim / 16, kChains = kNt == 1 ? 4 : 2;
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 200;\n");
+  constexpr int kBar = 1, kConsumers = 32 * kWarps, kChains = 2;
   const int gq = lane >> 2, quad = lane & 3;
   const float back = two_to(c.v_exp);
   const int team = warp / C::kTeam, in_team = warp % C::kTeam;
@@ -239,53 +239,42 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
     const int lo = w.lo(a.window, tt), hi = w.hi(tt);
     // where every row of the item sees everything: between the last row's first key and the first row's position
     const int all_lo = a.window > 0 ? max(0, hi - a.window + 1) : 0, all_hi = w.q.pos0 + tok0;
-    // the queries as the first product's right operand: row 8 n + gq, dims of quarter `quad`, four a k step
-    uint32_t qf[kNt == 1 ? kSteps : 1][2];
+    // the queries as the first product's right operand: row 8 n + gq, dims of quarter `quad`, four a k step; a warp turns the
+    // slices of 32 dims that are its own, after every warp has the rows' largest magnitudes
     float fac[kNt][2];  // of rows 8 n + 2 quad + {0, 1}: scores in powers of two
     int pos[kNt][2], from[kNt][2];
     if (ok && !wait_beat(q_full(item & 1), (uint32_t)(item / 2) & 1u, &s_beat)) ok = false;
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
       const int r = 8 * n + gq;
-      uint4 x[kDim / 32];
-      uint32_t top = 0;
       const bool live = r < rows;
+      const uint32_t qat = qring + (uint32_t)(((item & 1) * kRows + (live ? r : 0)) * C::kQRow + quad * (kDim / 2));
+      uint32_t tops = 0;  // of both halves, as integers
 #pragma unroll
       for (int i = 0; i < kDim / 32; ++i) {
-        x[i] = live ? lds128(qring + (uint32_t)(((item & 1) * kRows + r) * C::kQRow + quad * (kDim / 2) + 16 * i)) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = unpack2<kBf16>(v[e]);
-          top = max(top, max(__float_as_uint(f.x) & 0x7fffffffu, __float_as_uint(f.y) & 0x7fffffffu));
-        }
+        const uint4 x = lds128(qat + 16 * i);
+        tops = __vmaxu2(__vmaxu2(tops, __vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu)),
+                        __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
       }
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, 1));
+      tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, 2));
+      const uint32_t top16 = live ? max(tops & 0xffffu, tops >> 16) : 0u, top = __float_as_uint(unpack2<kBf16>(top16).x);
       // the row in units of 2^e: its largest in [2^14, 2^15) (a row that is not finite is NaN, and its result too)
       const int e = top == 0 ? 0 : max((int)(top >> 23) - 127, -126) - 14;
       const float up0 = top >= 0x7f800000u ? NAN : two_to(-e / 2), up1 = two_to(-e - (-e / 2));
 #pragma unroll
       for (int i = 0; i < kDim / 32; ++i) {
-        const uint32_t v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        if (i % kWarps != warp) continue;
+        const uint4 x = live ? lds128(qat + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
         uint32_t h[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float2 f = unpack2<kBf16>(v[k]);
           h[k] = pack2<false>(f.x * up0 * up1, f.y * up0 * up1);
         }
-        if constexpr (kNt == 1) {
-          qf[2 * i][0] = h[0];
-          qf[2 * i][1] = h[1];
-          qf[2 * i + 1][0] = h[2];
-          qf[2 * i + 1][1] = h[3];
-        } else if (warp == 0) {  // every warp has the same
-          uint32_t* to = reinterpret_cast<uint32_t*>(qs + (2 * i) * 32 + lane) + 2 * n;
-          to[0] = h[0];
-          to[1] = h[1];
-          to[4 * 32] = h[2];
-          to[4 * 32 + 1] = h[3];
-        }
+        qs[n][2 * i][lane] = make_uint2(h[0], h[1]);
+        qs[n][2 * i + 1][lane] = make_uint2(h[2], h[3]);
       }
       const float f = ldexpf(a.scale * kLog2e, e + c.k_exp);  // of row 8 n + gq, which lane 4 gq has
 #pragma unroll
@@ -296,9 +285,8 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
         from[n][i] = a.window > 0 ? pos[n][i] - a.window + 1 : 0;
       }
     }
-    if constexpr (kNt > 1) named_bar_sync(kBar, kConsumers);
-    __syncwarp();
-    if (lane == 0 && (kNt == 1 || warp == 0)) mbar_arrive(q_free(item & 1));
+    named_bar_sync(kBar, kConsumers);
+    if (lane == 0) mbar_arrive(q_free(item & 1));
     float m[kNt][2], l[kNt][2], acc[kNt][C::kTiles][4];
 #pragma unroll
     for (int n = 0; n < kNt; ++n) {
@@ -321,63 +309,63 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
         const uint32_t both = (mine >> u0) & 3u;
         if (both == 0 || jj > hi || jj + 31 < lo) continue;
         float s[2][kNt][4];
+        {
+          float z[2][kNt][kChains][4] = {};  // k steps in turn
+          uint32_t sp[2][2][kDim / 64];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int key0 = k0 + 16 * (u0 + u);
-          float z[kNt][kChains][4] = {};  // k steps in turn
-          uint32_t sp[2][kDim / 64];
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            const uint32_t at = ksc + (uint32_t)((key0 + gq + 8 * r) * C::kSRow + quad * (kDim / 64));
-            scale_pairs(kDim == 256 ? lds32(at) : kDim == 128 ? lds16(at) : lds8(at), sp[r]);
-          }
-#pragma unroll
-          for (int t4 = 0; t4 < (kDim == 256 ? 2 : 1); ++t4) {
-            uint32_t cw[2][4];
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-              const uint32_t at = kt + code_at<kDim>(key0 + gq + 8 * r, quad * (kDim / 8) + 16 * t4);
-              if constexpr (kDim == 64) {
-                const uint2 v = lds64(at);
-                cw[r][0] = v.x, cw[r][1] = v.y, cw[r][2] = cw[r][3] = 0;
-              } else {
-                const uint4 v = lds128(at);
-                cw[r][0] = v.x, cw[r][1] = v.y, cw[r][2] = v.z, cw[r][3] = v.w;
-              }
+              const uint32_t at = ksc + (uint32_t)((k0 + 16 * (u0 + u) + gq + 8 * r) * C::kSRow + quad * (kDim / 64));
+              scale_pairs(kDim == 256 ? lds32(at) : kDim == 128 ? lds16(at) : lds8(at), sp[u][r]);
             }
 #pragma unroll
-            for (int x = 0; x < (kDim == 64 ? 2 : 4); ++x) {  // 8 dims: two k steps
-              uint32_t h[2][4];
+          for (int t4 = 0; t4 < (kDim == 256 ? 2 : 1); ++t4) {
+            uint32_t cw[2][2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
               for (int r = 0; r < 2; ++r) {
-                e2m1x8_to_f16(cw[r][x], h[r]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[r][e] = hmul2_bits(h[r][e], sp[r][2 * t4 + x / 2]);
+                const uint32_t at = kt + code_at<kDim>(k0 + 16 * (u0 + u) + gq + 8 * r, quad * (kDim / 8) + 16 * t4);
+                if constexpr (kDim == 64) {
+                  const uint2 v = lds64(at);
+                  cw[u][r][0] = v.x, cw[u][r][1] = v.y, cw[u][r][2] = cw[u][r][3] = 0;
+                } else {
+                  const uint4 v = lds128(at);
+                  cw[u][r][0] = v.x, cw[u][r][1] = v.y, cw[u][r][2] = v.z, cw[u][r][3] = v.w;
+                }
               }
 #pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                const int k = 8 * t4 + 2 * x + y;
-                uint32_t q0, q1, q2 = 0, q3 = 0;
-                if constexpr (kNt == 1) {
-                  q0 = qf[k][0], q1 = qf[k][1];
-                } else {
-                  const uint4 v = qs[k * 32 + lane];
-                  q0 = v.x, q1 = v.y, q2 = v.z, q3 = v.w;
+            for (int x = 0; x < (kDim == 64 ? 2 : 4); ++x) {  // 8 dims: two k steps
+              uint2 qv[2][kNt];
+#pragma unroll
+              for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int n = 0; n < kNt; ++n) qv[y][n] = qs[n][8 * t4 + 2 * x + y][lane];
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                uint32_t h[2][4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                  e2m1x8_to_f16(cw[u][r][x], h[r]);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) h[r][e] = hmul2_bits(h[r][e], sp[u][r][2 * t4 + x / 2]);
                 }
-                mma_f16_16816(z[0][k % kChains], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1], q0, q1);
-                if constexpr (kNt > 1)
-                  mma_f16_16816(z[kNt - 1][k % kChains], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1], q2, q3);
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                  for (int n = 0; n < kNt; ++n)
+                    mma_f16_16816(z[u][n][(2 * x + y) % kChains], h[0][2 * y], h[1][2 * y], h[0][2 * y + 1], h[1][2 * y + 1],
+                                  qv[y][n].x, qv[y][n].y);
               }
             }
           }
 #pragma unroll
-          for (int n = 0; n < kNt; ++n)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float x = z[n][0][e] + z[n][1][e];
-              if constexpr (kChains == 4) x += z[n][2][e] + z[n][3][e];
-              s[u][n][e] = x * fac[n][e & 1];
-            }
+            for (int n = 0; n < kNt; ++n)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[u][n][e] = (z[u][n][0][e] + z[u][n][1][e]) * fac[n][e & 1];
         }
         if (jj < all_lo || jj + 31 > all_hi || both != 3u) {
 #pragma unroll
@@ -442,9 +430,15 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
               p[u][n][h] = transposed(x);
             }
         }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
+#pragma unroll 1
+        for (int u = 0; u < 2; ++u) {  // (rolled: the code of both stays in the instruction cache)
         const int key0 = k0 + 16 * (u0 + u), j0 = jj + 16 * u;
+        uint32_t pu[kNt][2];
+#pragma unroll
+        for (int n = 0; n < kNt; ++n) {
+          pu[n][0] = u ? p[1][n][0] : p[0][n][0];
+          pu[n][1] = u ? p[1][n][1] : p[0][n][1];
+        }
         // ---- values: keys 2 quad + {0, 1, 8, 9}, an eighth of the dims
         // values of keys outside the item's range, or in no page, must not meet a weight of 0
         const bool none = !((both >> u) & 1u), cut = j0 < lo || j0 + 15 > hi || none;
@@ -487,7 +481,7 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
           for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int n = 0; n < kNt; ++n)
-              mma_f16_16816(acc[n][4 * y + e], h[0][0][e], h[0][1][e], h[1][0][e], h[1][1][e], p[u][n][0], p[u][n][1]);
+              mma_f16_16816(acc[n][4 * y + e], h[0][0][e], h[0][1][e], h[1][0][e], h[1][1][e], pu[n][0], pu[n][1]);
         }
         }
       }
