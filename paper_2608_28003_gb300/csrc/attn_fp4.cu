@@ -1,30 +1,8 @@
-// Attention of a ragged batch over a paged cache in 4 bits, in its simplest form: a warp takes a row and head, key by key.
+// Attention of a ragged batch over a paged cache in 4 bits: checks and choice of the kernel.
 #include <cmath>
 
 #include "attn_fp4.cuh"
 #include "ops.cuh"
-
-namespace w8a8 {
-
-namespace {
-
-template <bool kBf16, int kDim>
-__global__ void __launch_bounds__(128) attn_fp4_kernel(Fp4Pages c, PagedBatch b, AttnCall a) {
-  pdl_wait();
-  pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const int64_t items = (int64_t)b.n_rows * a.n_q, warps = (int64_t)gridDim.x * 4;
-  for (int64_t i = ((int64_t)blockIdx.x * 128 + threadIdx.x) >> 5; i < items; i += warps) {
-    const int row = (int)(i / a.n_q), head = (int)(i % a.n_q), s = seq_of_row(b, row);
-    const SeqShape q = seq_shape(b, s, c.p.page_shift);
-    if (row < q.row0 || row >= q.row0 + q.rows) continue;
-    attend_row_fp4<kBf16, kDim>(c, b, a, s, q.pos0 + row - q.row0, row, head, lane, nullptr);
-  }
-}
-
-}  // namespace
-
-}  // namespace w8a8
 
 using namespace w8a8;
 
@@ -58,16 +36,6 @@ extern "C" w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cach
   AttnCall a{q, q_row, q_head, o, o_row, o_head, n_q, dim, window, batch->max_new, scale, dtype == W8A8_TYPE_BF16};
   if (a.window >= 1 << 30) a.window = 0;  // beyond every position
   W8A8_TRY(gave_up_word(&a.gave_up));
-  if ((long long)a.max_new * (n_q / pc.p.n_kv) <= 16)
-    return launch_attn_fp4_tokens(pc, pb, a, workspace, d.sms, as_stream(stream));
-  const int64_t items = (int64_t)pb.n_rows * n_q;
-  const dim3 grid((unsigned)(items / 4 + 1 < 152 * 64 ? items / 4 + 1 : 152 * 64));
-  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, dim3(128), 0, as_stream(stream), pc, pb, a); };
-  W8A8_CUDA(a.bf16 ? (dim == 256   ? go(attn_fp4_kernel<true, 256>)
-                      : dim == 128 ? go(attn_fp4_kernel<true, 128>)
-                                   : go(attn_fp4_kernel<true, 64>))
-                   : (dim == 256   ? go(attn_fp4_kernel<false, 256>)
-                      : dim == 128 ? go(attn_fp4_kernel<false, 128>)
-                                   : go(attn_fp4_kernel<false, 64>)));
-  return W8A8_OK;
+  return (long long)a.max_new * (n_q / pc.p.n_kv) <= 16 ? launch_attn_fp4_tokens(pc, pb, a, workspace, d.sms, as_stream(stream))
+                                                        : launch_attn_fp4_chunks(pc, pb, a, workspace, d.sms, as_stream(stream));
 }

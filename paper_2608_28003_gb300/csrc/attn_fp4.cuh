@@ -9,6 +9,9 @@ namespace w8a8 {
 w8a8_status launch_attn_fp4_tokens(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st);
 
+w8a8_status launch_attn_fp4_chunks(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
+                                   cudaStream_t st);
+
 // attend_row (attn_paged.cuh) with the values a 4-bit cache stands for: one row by one warp, key by key in the order of the formula.
 template <bool kBf16, int kDim>
 __device__ __noinline__ void attend_row_fp4(const Fp4Pages& c, const PagedBatch& b, const AttnCall& a, int s, int pos,

@@ -32,6 +32,7 @@
 // a pair of CTAs, each copying half for both, took 27.9, and 67.2 us instead of 71.9 for a larger chunk, but a copy to several
 // CTAs has no place in a library that also runs on several GPUs.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
+#include "attn_fp4.cuh"
 #include "attn_paged.cuh"
 #include "ops.cuh"
 #include "tc_common.cuh"
@@ -46,7 +47,7 @@ namespace {
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
 
-template <int kDim>
+template <int kDim, bool kFp4>
 struct Cfg {
   static constexpr int kRt = kDim == 256 ? 1 : 2;  // row tiles of a CTA
   static constexpr int kChunks = kDim / 64;
@@ -57,7 +58,11 @@ struct Cfg {
   static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys
   static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
   static constexpr int kSplit = 2 / kRt;           // threads a row
-  static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kSoft + 1, kLoadV = kSoft + 2, kThreads = 32 * (kSoft + 3);
+  // warps: softmax, then (16 bits) a copier of queries and K, the issuer, a copier of V, or (4 bits) the issuer and seven that
+  // turn codes into operands, three for K and four for V
+  static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kFp4 ? kSoft : kSoft + 1, kLoadV = kSoft + 2;
+  static constexpr int kMakeK = 3, kMakeV = 4, kMakers = kMakeK + kMakeV;
+  static constexpr int kThreads = kFp4 ? 512 : 32 * (kSoft + 3);
   static constexpr int kRows = kBq * kRt;
   static constexpr int kPart = kRows * kDim + 2 * kRows;  // floats of a partial: [dim / 4][rows][4], m, l
   static constexpr uint32_t kOCol = 256;                  // O of row tile r: kOCol + r kDim
@@ -106,12 +111,56 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
-template <bool kBf16, int kDim>
-__global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
+// The pages' shape of a cache of either kind.
+__device__ __forceinline__ const PagedCache& shape_of(const PagedCache& c) { return c; }
+__device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c) { return c.p; }
+
+// ------------------------------------------------------------------------------------ operands from 4 bits
+// Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  They are fp16, whatever the
+// call's type: a code times its scale has six significant bits, so the product is exact.
+struct Fp4Unit {
+  uint4 w;
+  uint32_t sc;
+};
+__device__ __forceinline__ Fp4Unit load_unit(const uint8_t* codes, const uint8_t* scales, const Fp4Pages& c, int page, int slot,
+                                             int head, int ch, int lane) {
+  Fp4Unit u;
+  u.w = make_uint4(0u, 0u, 0u, 0u);
+  u.sc = 0;
+  if (page >= 0) {
+    const int part = 2 * ch + (lane & 1);
+    u.w = __ldg(reinterpret_cast<const uint4*>(codes + (int64_t)page * c.p.page_stride + (int64_t)slot * c.p.slot_stride +
+                                               (int64_t)head * c.p.head_stride) + part);
+    u.sc = __ldg(reinterpret_cast<const uint16_t*>(scales + (int64_t)page * c.s_page + (int64_t)slot * c.s_slot +
+                                                   (int64_t)head * c.s_head) + part);
+  }
+  return u;
+}
+// Into row `key` of the 64-dim column at `at` (128-byte rows, swizzled).
+__device__ __forceinline__ void store_unit(const Fp4Unit& u, uint32_t at, int key, int lane) {
+  const uint32_t w[4] = {u.w.x, u.w.y, u.w.z, u.w.w}, h2 = e4m3x2_to_f16x2(u.sc);
+  const uint32_t s0 = __byte_perm(h2, h2, 0x1010), s1 = __byte_perm(h2, h2, 0x3232);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t h[4];
+    e2m1x8_to_f16(w[i], h);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = hmul2_bits(h[e], i < 2 ? s0 : s1);
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (uint32_t)(key * 128 + (((4 * (lane & 1) + i) ^ (key & 7)) << 4))),
+                 "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3])
+                 : "memory");
+  }
+}
+
+// kBf16: the type of queries and outputs; the operands' too with a 16-bit cache, fp16 with a 4-bit one.
+template <bool kBf16, int kDim, class Pages>
+__global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kThreads, 1)
     attn_chunks_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
-                       const __grid_constant__ CUtensorMap tmV, PagedCache c, PagedBatch b, AttnCall a, int tt,
+                       const __grid_constant__ CUtensorMap tmV, Pages pages, PagedBatch b, AttnCall a, int tt,
                        float* __restrict__ part, unsigned int* __restrict__ counters, unsigned int* __restrict__ err) {
-  using C = Cfg<kDim>;
+  constexpr bool kFp4 = std::is_same_v<Pages, Fp4Pages>, kOpBf16 = kBf16 && !kFp4;
+  const PagedCache& c = shape_of(pages);
+  using C = Cfg<kDim, kFp4>;
   constexpr int kRt = C::kRt, kThreads = C::kThreads, kIssueWarp = C::kIssueWarp;
   constexpr uint32_t kOCol = C::kOCol;
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -120,6 +169,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   __shared__ long long scan[kThreads / 32];
   __shared__ uint32_t held[8];  // 16-key groups of a tile that lie in a page
   __shared__ uint32_t tmem_slot, s_last, s_bad[4], s_beat;
+  __shared__ int s_exp[2][kFp4 ? C::kRows : 1];  // 4 bits: the powers of two that rows of queries are in units of, of two items
   __shared__ float s_max[C::kSplit][C::kSplit][kBq], s_sum[C::kSplit][kBq];  // two threads a row: what they tell each other
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t bar0 = smem_u32(bars);
@@ -130,12 +180,19 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   if (threadIdx.x < 4) s_bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     s_beat = 0;
-    for (int i = 0; i < C::kBars; ++i)
-      mbar_init(bar(i), (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive : 1);
+    for (int i = 0; i < C::kBars; ++i) {
+      int n = (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive : 1;
+      if (kFp4 && i == C::Q_FULL) n = C::kMakers;
+      if (kFp4 && i >= C::K_FULL && i < C::K_FREE) n = C::kMakeK;
+      if (kFp4 && i >= C::V_FULL && i < C::V_FREE) n = C::kMakeV;
+      mbar_init(bar(i), n);
+    }
     fence_mbar_init();
-    prefetch_tmap(&tmQ);
-    prefetch_tmap(&tmK);
-    prefetch_tmap(&tmV);
+    if constexpr (!kFp4) {
+      prefetch_tmap(&tmQ);
+      prefetch_tmap(&tmK);
+      prefetch_tmap(&tmV);
+    }
   }
   if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&tmem_slot))
@@ -151,12 +208,129 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   // (syncs the block)
   find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan);
   bool ok = true;
+  if constexpr (kFp4) {  // registers: 512 threads of 128 are shared out as 256 of 168 and 256 of 88
+    if (warp < C::kSoft)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 168;\n");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
+  }
 
   if (ls.begin < ls.end) {
     Walk w;
     w.start(ls, b, c.page_shift, a.window, item_tt, kBkShift, lane);
     int g = 0, item = 0;  // tiles and items of this CTA so far
-    if (warp == C::kLoadWarp || warp == C::kLoadV) {
+    if (kFp4 && warp > kIssueWarp) {
+      if constexpr (kFp4) {
+        // -------------------------------------------------------------------- operands from 4 bits
+        const int me = warp - kIssueWarp - 1;
+        const bool kv = me >= C::kMakeK;  // V
+        const int team = kv ? C::kMakeV : C::kMakeK, mine = kv ? me - C::kMakeK : me;
+        const int full = kv ? C::V_FULL : C::K_FULL, free = kv ? C::V_FREE : C::K_FREE, off = kv ? C::kOffV : C::kOffK;
+        const uint8_t *codes = kv ? pages.v : pages.k, *scales = kv ? pages.vs : pages.ks;
+        constexpr int kUnits = 8 * C::kChunks, kMost = (kUnits + C::kMakeK - 1) / C::kMakeK;  // of a tile; a warp's at most
+        // unit n of a tile: K by 64 dims, V by 16 keys, the order in which their parts are handed over
+        auto place = [&](int n, int& group, int& ch) {
+          group = kv ? n / C::kChunks : n & 7;
+          ch = kv ? n % C::kChunks : n >> 3;
+        };
+        for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
+          const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
+          // the pages of four tiles, a 16-key group a lane
+          int page = group_page(b, c, w.s, (w.first + w.k0) << kBkShift, lo, hi, 16, lane), ahead = -1;
+          Fp4Unit u[kMost];
+          auto load_tile = [&](int i) {
+            const int tile0 = (w.first + w.k0 + i) << kBkShift;
+#pragma unroll
+            for (int j = 0; j < kMost; ++j) {
+              const int n = mine + j * team;
+              int group, ch;
+              place(n, group, ch);
+              const int pg = __shfl_sync(0xffffffffu, page, ((i & 3) * 8 + group) & 31), key = tile0 + 16 * group + (lane >> 1);
+              // keys that no row of the item sees are zeros: nothing of theirs may meet a weight of 0
+              if (n < kUnits) u[j] = load_unit(codes, scales, pages, key >= lo && key <= hi ? pg : -1, key & ((1 << c.page_shift) - 1), w.h, ch, lane);
+            }
+          };
+          load_tile(0);
+          // ---- the item's queries: all of these warps, D / 8 lanes a row
+          if (item > 0 && !wait_beat(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, &s_beat)) {
+            ok = false;
+            break;
+          }
+          {
+            constexpr int kL = kDim / 8, kPer = 32 / kL;  // lanes a row, rows a step
+            const int sub = lane % kL;
+#pragma unroll 2
+            for (int r0 = me * kPer; r0 < C::kRows; r0 += C::kMakers * kPer) {
+              const int r = r0 + lane / kL;
+              const int rt = r / kBq, rr = r % kBq, tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
+              uint4 x = make_uint4(0u, 0u, 0u, 0u);
+              if (r < C::kRows && rr < rows)
+                x = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.q.row0 + tok0 + rr / group) * a.q_row +
+                                                    (int64_t)(w.h * group + rr % group) * a.q_head + 8 * sub);
+              uint32_t tops = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
+#pragma unroll
+              for (int o = kL / 2; o > 0; o >>= 1) tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, o));
+              const uint32_t top = __float_as_uint(unpack2<kBf16>(max(tops & 0xffffu, tops >> 16)).x);
+              // the row in units of 2^e: its largest in [2^14, 2^15) (a row that is not finite is NaN, and its result too)
+              const int e = top == 0 ? 0 : max((int)(top >> 23) - 127, -126) - 14;
+              const float up0 = top >= 0x7f800000u ? NAN : two_to(-e / 2), up1 = two_to(-e - (-e / 2));
+              const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+              uint32_t h[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float2 f = unpack2<kBf16>(v[k]);
+                h[k] = pack2<false>(f.x * up0 * up1, f.y * up0 * up1);
+              }
+              if (r < C::kRows) {
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(
+                                 base + (uint32_t)(rt * C::kTile + (sub >> 3) * kSub + rr * 128 + (((sub & 7) ^ (rr & 7)) << 4))),
+                             "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3])
+                             : "memory");
+                if (sub == 0) s_exp[item & 1][r] = e;
+              }
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(C::Q_FULL));
+          }
+          for (int i = 0; ok && i < w.cnt; ++i, ++g) {
+            const int st = g % C::kStages;
+            const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (8 * (i & 3))) & 0xffu;
+            constexpr int kParts = C::kKParts;
+            int at_part = -1;
+#pragma unroll
+            for (int j = 0; j < kMost; ++j) {
+              const int n = mine + j * team;
+              if (n >= kUnits) continue;
+              int group, ch;
+              place(n, group, ch);
+              const int pt = n / (kUnits / kParts);
+              if (pt != at_part) {  // the parts before are complete, this one's place has to be free
+                for (; at_part >= 0 && at_part < pt; ++at_part) {
+                  asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                  __syncwarp();
+                  if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
+                }
+                at_part = pt;
+                if (ok && g >= C::kStages && !wait_beat(bar(free + st * kParts + pt), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat))
+                  ok = false;
+                if (!kv && mine == 0 && pt == 0 && lane == 0) held[g & 7] = there;
+              }
+              if (ok) store_unit(u[j], base + (uint32_t)(off + st * C::kTile + ch * kSub), 16 * group + (lane >> 1), lane);
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
+            // the next tile's codes are on their way while this one's place in the ring is awaited
+            if (((i + 1) & 3) == 0 && i + 1 < w.cnt) page = ahead;
+            if ((i & 3) == 1 && i + 3 < w.cnt)
+              ahead = group_page(b, c, w.s, (w.first + w.k0 + (i | 3) + 1) << kBkShift, lo, hi, 16, lane);
+            if (i + 1 < w.cnt) load_tile(i + 1);
+          }
+        }
+        if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
+      }
+    } else if (!kFp4 && (warp == C::kLoadWarp || warp == C::kLoadV)) {
       // ---------------------------------------------------------------------- TMA copies
       const bool kv = warp == C::kLoadV;
       const CUtensorMap* map = kv ? &tmV : &tmK;
@@ -224,7 +398,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       if (!drained && lane == 0) give_up(err, a, DEVERR_DRAIN_WAIT);
     } else if (warp == kIssueWarp) {
       // ---------------------------------------------------------------------- MMAs
-      constexpr uint32_t fmt = kBf16 ? 1u : 0u;
+      constexpr uint32_t fmt = kOpBf16 ? 1u : 0u;
       constexpr uint32_t idesc_s = idesc_f16(fmt, kBk, kBq), idesc_o = idesc_f16(fmt, kDim, kBq) | kIdescBMnMajor;
       const uint64_t dq = sdesc_swz(base);
       // S of key tile i (this CTA's count) for row tile rt, into its slot; hands K back after the last row tile, Q after `last`
@@ -331,7 +505,11 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
       const int hf = kRt == 2 ? 0 : warp >> 2;                               // which half
       const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
       const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
-      const float sc = a.scale * kLog2e;
+      float sc = a.scale * kLog2e;
+      const float back = [&] {
+        if constexpr (kFp4) return two_to(pages.v_exp);
+        return 1.0f;
+      }();
       for (; w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
         const int tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
         const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
@@ -345,6 +523,9 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           if (ok && !wait_beat(bar(C::S_FULL + slot), (uint32_t)(kRt == 2 ? g : g >> 1) & 1u, &s_beat)) ok = false;
           if (!ok) continue;
           tc_fence_after();
+          if constexpr (kFp4) {  // (written ahead of the queries, which these scores are of)
+            if (i == 0) sc = ldexpf(a.scale * kLog2e, s_exp[item & 1][rt * kBq + r] + pages.k_exp);
+          }
           uint32_t x[32];
           float top = -INFINITY;
           const uint32_t there = held[g & 7];
@@ -384,7 +565,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
           if (busy) {
             top *= sc;
-            const bool grown = top > m + kGrowth<kBf16>;  // m = -inf: any visible key
+            const bool grown = top > m + kGrowth<kOpBf16>;  // m = -inf: any visible key
             float up = 1.0f;
             if (grown) {
               up = m == -INFINITY ? 0.0f : ex2(m - top);
@@ -407,7 +588,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
               }
             }
           }
-          if (rt == 0 && hf == 0 && (j0 < lo || j0 + kBk - 1 > hi)) {
+          if (!kFp4 && rt == 0 && hf == 0 && (j0 < lo || j0 + kBk - 1 > hi)) {
             // values of keys outside the item's range (another sequence's, or nobody's) must not meet a weight of zero: row r
             // of the tile, once its copies have landed
             const int st = g % C::kStages;
@@ -432,7 +613,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             }
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
           }
-          const float ref = m == -INFINITY ? 0.0f : m - kLift<kBf16>;
+          const float ref = m == -INFINITY ? 0.0f : m - kLift<kOpBf16>;
           const f32x2 sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
           f32x2 sum[2] = {0ull, 0ull};  // of weights before their rounding: summed as used, 188 us where it is 180 and no closer
 #pragma unroll
@@ -449,7 +630,7 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
                 e0 = ex2(e0);
                 e1 = ex2(e1);
                 sum[(k >> 1) & 1] = f2_add(sum[(k >> 1) & 1], f2_pack(e0, e1));
-                pk[k >> 1] = pack2<kBf16>(e0, e1);
+                pk[k >> 1] = pack2<kOpBf16>(e0, e1);
               }
               tmem_st16(stm + 64 * hf + 16 * q, pk);  // over scores that have been read
             }
@@ -484,7 +665,8 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
             uint32_t p[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float y = x[8 * k + 2 * e] * inv, z = x[8 * k + 2 * e + 1] * inv;
+              float y = x[8 * k + 2 * e] * inv, z = x[8 * k + 2 * e + 1] * inv;
+              if constexpr (kFp4) y *= back, z *= back;
               nan = fmaf(y, 0.0f, fmaf(z, 0.0f, nan));
               p[e] = pack2<kBf16>(y, z);
             }
@@ -504,9 +686,12 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
           }
           for (; rest; rest &= rest - 1) {
             const int src = __ffs(rest) - 1;
-            attend_row<kBf16, kDim>(c, b, a, w.s, __shfl_sync(0xffffffffu, pos, src),
-                                    (int64_t)w.q.row0 + __shfl_sync(0xffffffffu, tok, src), __shfl_sync(0xffffffffu, head, src),
-                                    lane, &s_beat);
+            const int at_pos = __shfl_sync(0xffffffffu, pos, src), at_head = __shfl_sync(0xffffffffu, head, src);
+            const int64_t at_row = (int64_t)w.q.row0 + __shfl_sync(0xffffffffu, tok, src);
+            if constexpr (kFp4)
+              attend_row_fp4<kBf16, kDim>(pages, b, a, w.s, at_pos, at_row, at_head, lane, &s_beat);
+            else
+              attend_row<kBf16, kDim>(c, b, a, w.s, at_pos, at_row, at_head, lane, &s_beat);
           }
         };
         if (w.whole()) {
@@ -607,26 +792,34 @@ __global__ void __launch_bounds__(Cfg<kDim>::kThreads, 1)
   }
 }
 
-template <bool kBf16, int kDim>
-w8a8_status launch(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms, cudaStream_t st) {
-  using C = Cfg<kDim>;
+template <bool kBf16, int kDim, class Pages>
+w8a8_status launch(const Pages& pages, const PagedBatch& pb, const AttnCall& a, void* ws, int sms, cudaStream_t st) {
+  constexpr bool kFp4 = std::is_same_v<Pages, Fp4Pages>;
+  using C = Cfg<kDim, kFp4>;
   static bool attr_set[64] = {};
   int dev = 0;
   W8A8_CUDA(cudaGetDevice(&dev));
+  auto kernel = attn_chunks_kernel<kBf16, kDim, Pages>;
   if (dev >= 0 && dev < 64 && !attr_set[dev]) {
-    W8A8_CUDA(cudaFuncSetAttribute(attn_chunks_kernel<kBf16, kDim>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    W8A8_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     attr_set[dev] = true;
   }
-  const int group = a.n_q / pc.n_kv, tt = kBq / group;
-  CUtensorMap tq, tk, tv;
-  const uint64_t dims[3] = {(uint64_t)kDim, (uint64_t)a.n_q, (uint64_t)pb.n_rows};
-  const uint64_t strides[2] = {(uint64_t)a.q_head * 2, (uint64_t)a.q_row * 2};
-  const uint32_t box[3] = {64, (uint32_t)group, (uint32_t)tt};
-  W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
-  W8A8_TRY(make_kv_maps(pc, kDim, &tk, &tv));
+  CUtensorMap tq{}, tk{}, tv{};
+  int tt;
+  if constexpr (kFp4) {  // (no copies by TMA)
+    tt = kBq / (a.n_q / pages.p.n_kv);
+  } else {
+    const int group = a.n_q / pages.n_kv;
+    tt = kBq / group;
+    const uint64_t dims[3] = {(uint64_t)kDim, (uint64_t)a.n_q, (uint64_t)pb.n_rows};
+    const uint64_t strides[2] = {(uint64_t)a.q_head * 2, (uint64_t)a.q_row * 2};
+    const uint32_t box[3] = {64, (uint32_t)group, (uint32_t)tt};
+    W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
+    W8A8_TRY(make_kv_maps(pages, kDim, &tk, &tv));
+  }
   char* base = static_cast<char*>(ws);
-  W8A8_CUDA(launch_pdl(attn_chunks_kernel<kBf16, kDim>, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
-                       pc, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
+  W8A8_CUDA(launch_pdl(kernel, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
+                       pages, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
                        reinterpret_cast<unsigned int*>(base + kErrWordOffset)));
   return W8A8_OK;
 }
@@ -634,12 +827,23 @@ w8a8_status launch(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a
 }  // namespace
 
 size_t attn_chunks_ws(int dim, int sms) {
-  const int part = dim == 256 ? Cfg<256>::kPart : dim == 128 ? Cfg<128>::kPart : Cfg<64>::kPart;
+  const int part = dim == 256 ? Cfg<256, false>::kPart : dim == 128 ? Cfg<128, false>::kPart : Cfg<64, false>::kPart;
   return (size_t)2 * sms * part * sizeof(float);
 }
 
 w8a8_status launch_attn_chunks(const PagedCache& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                cudaStream_t st) {
+  if (a.bf16)
+    return a.dim == 256   ? launch<true, 256>(pc, pb, a, ws, sms, st)
+           : a.dim == 128 ? launch<true, 128>(pc, pb, a, ws, sms, st)
+                          : launch<true, 64>(pc, pb, a, ws, sms, st);
+  return a.dim == 256   ? launch<false, 256>(pc, pb, a, ws, sms, st)
+         : a.dim == 128 ? launch<false, 128>(pc, pb, a, ws, sms, st)
+                        : launch<false, 64>(pc, pb, a, ws, sms, st);
+}
+
+w8a8_status launch_attn_fp4_chunks(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
+                                   cudaStream_t st) {
   if (a.bf16)
     return a.dim == 256   ? launch<true, 256>(pc, pb, a, ws, sms, st)
            : a.dim == 128 ? launch<true, 128>(pc, pb, a, ws, sms, st)
