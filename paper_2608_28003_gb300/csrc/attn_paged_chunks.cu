@@ -112,12 +112,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
 
 // The pages' shape of a cache of either kind.
-__device__ __forceinline__ const PagedCache& shape_of(const PagedCache& c) { return c; }
-__device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c) { return c.p; }
+__host__ __device__ __forceinline__ const PagedCache& shape_of(const PagedCache& c) { return c; }
+__host__ __device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c) { return c.p; }
 
 // ------------------------------------------------------------------------------------ operands from 4 bits
-// Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  They are fp16, whatever the
-// call's type: a code times its scale has six significant bits, so the product is exact.
+// Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  A code times its scale has six
+// significant bits and lies within fp16's range as within bf16's, so operands are exact in either type: K has the queries', V is fp16
+// whatever the type, as the weights are.
 struct Fp4Unit {
   uint4 w;
   uint32_t sc;
@@ -136,23 +137,40 @@ __device__ __forceinline__ Fp4Unit load_unit(const uint8_t* codes, const uint8_t
   }
   return u;
 }
-// Into row `key` of the 64-dim column at `at` (128-byte rows, swizzled).
-__device__ __forceinline__ void store_unit(const Fp4Unit& u, uint32_t at, int key, int lane) {
-  const uint32_t w[4] = {u.w.x, u.w.y, u.w.z, u.w.w}, h2 = e4m3x2_to_f16x2(u.sc);
+// Into row `key` of a 64-dim column (128-byte rows, swizzled): `at` is the row, `swz` its part and swizzle.  Not inline: the code
+// of a dozen copies would not stay in the instruction cache.
+// To bf16: fp16's bits shifted into place are the value times 2^-112 (nothing of a code is lost), the scale is taken times 2^112.
+template <bool kToBf16>
+__device__ __noinline__ void store_unit(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, uint32_t sc, uint32_t at, uint32_t swz) {
+  const uint32_t w[4] = {w0, w1, w2, w3};
+  uint32_t h2 = e4m3x2_to_f16x2(sc);
+  if constexpr (kToBf16) {
+    const uint32_t lo = h2 & 0xffffu, hi = h2 >> 16;
+    h2 = (lo ? (lo >> 3) + 0x7000u : 0u) | (hi ? (hi >> 3) + 0x7000u : 0u) << 16;
+  }
   const uint32_t s0 = __byte_perm(h2, h2, 0x1010), s1 = __byte_perm(h2, h2, 0x3232);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t h[4];
     e2m1x8_to_f16(w[i], h);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = hmul2_bits(h[e], i < 2 ? s0 : s1);
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (uint32_t)(key * 128 + (((4 * (lane & 1) + i) ^ (key & 7)) << 4))),
-                 "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3])
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t s = i < 2 ? s0 : s1;
+      if constexpr (kToBf16) {
+        const uint32_t t = ((h[e] & 0x7fff7fffu) >> 3) | (h[e] & 0x80008000u);
+        const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&t), *reinterpret_cast<const __nv_bfloat162*>(&s));
+        h[e] = *reinterpret_cast<const uint32_t*>(&y);
+      } else {
+        h[e] = hmul2_bits(h[e], s);
+      }
+    }
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (swz ^ (uint32_t)(i << 4))), "r"(h[0]), "r"(h[1]), "r"(h[2]),
+                 "r"(h[3])
                  : "memory");
   }
 }
 
-// kBf16: the type of queries and outputs; the operands' too with a 16-bit cache, fp16 with a 4-bit one.
+// kBf16: the type of queries, outputs and K; of weights and V too with a 16-bit cache, which are fp16 with a 4-bit one.
 template <bool kBf16, int kDim, class Pages>
 __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kThreads, 1)
     attn_chunks_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -169,7 +187,6 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
   __shared__ long long scan[kThreads / 32];
   __shared__ uint32_t held[8];  // 16-key groups of a tile that lie in a page
   __shared__ uint32_t tmem_slot, s_last, s_bad[4], s_beat;
-  __shared__ int s_exp[2][kFp4 ? C::kRows : 1];  // 4 bits: the powers of two that rows of queries are in units of, of two items
   __shared__ float s_max[C::kSplit][C::kSplit][kBq], s_sum[C::kSplit][kBq];  // two threads a row: what they tell each other
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t bar0 = smem_u32(bars);
@@ -182,14 +199,13 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
     s_beat = 0;
     for (int i = 0; i < C::kBars; ++i) {
       int n = (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive : 1;
-      if (kFp4 && i == C::Q_FULL) n = C::kMakers;
       if (kFp4 && i >= C::K_FULL && i < C::K_FREE) n = C::kMakeK;
       if (kFp4 && i >= C::V_FULL && i < C::V_FREE) n = C::kMakeV;
       mbar_init(bar(i), n);
     }
     fence_mbar_init();
+    prefetch_tmap(&tmQ);
     if constexpr (!kFp4) {
-      prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
       prefetch_tmap(&tmV);
     }
@@ -208,11 +224,11 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
   // (syncs the block)
   find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan);
   bool ok = true;
-  if constexpr (kFp4) {  // registers: 512 threads of 128 are shared out as 256 of 168 and 256 of 88
+  if constexpr (kFp4) {  // registers: 512 threads of 128 are shared out as 256 of 152 and 256 of 104
     if (warp < C::kSoft)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 168;\n");
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 152;\n");
     else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;\n");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 104;\n");
   }
 
   if (ls.begin < ls.end) {
@@ -229,8 +245,8 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
         const uint8_t *codes = kv ? pages.v : pages.k, *scales = kv ? pages.vs : pages.ks;
         constexpr int kUnits = 8 * C::kChunks, kMost = (kUnits + C::kMakeK - 1) / C::kMakeK;  // of a tile; a warp's at most
         // unit n of a tile: K by 64 dims, V by 16 keys, the order in which their parts are handed over
-        auto place = [&](int n, int& group, int& ch) {
-          group = kv ? n / C::kChunks : n & 7;
+        auto place = [&](int n, int& gr, int& ch) {
+          gr = kv ? n / C::kChunks : n & 7;
           ch = kv ? n % C::kChunks : n >> 3;
         };
         for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
@@ -243,92 +259,78 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
 #pragma unroll
             for (int j = 0; j < kMost; ++j) {
               const int n = mine + j * team;
-              int group, ch;
-              place(n, group, ch);
-              const int pg = __shfl_sync(0xffffffffu, page, ((i & 3) * 8 + group) & 31), key = tile0 + 16 * group + (lane >> 1);
+              int gr, ch;
+              place(n, gr, ch);
+              const int pg = __shfl_sync(0xffffffffu, page, ((i & 3) * 8 + gr) & 31), key = tile0 + 16 * gr + (lane >> 1);
               // keys that no row of the item sees are zeros: nothing of theirs may meet a weight of 0
               if (n < kUnits) u[j] = load_unit(codes, scales, pages, key >= lo && key <= hi ? pg : -1, key & ((1 << c.page_shift) - 1), w.h, ch, lane);
             }
           };
-          load_tile(0);
-          // ---- the item's queries: all of these warps, D / 8 lanes a row
-          if (item > 0 && !wait_beat(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, &s_beat)) {
-            ok = false;
-            break;
-          }
-          {
-            constexpr int kL = kDim / 8, kPer = 32 / kL;  // lanes a row, rows a step
-            const int sub = lane % kL;
-#pragma unroll 2
-            for (int r0 = me * kPer; r0 < C::kRows; r0 += C::kMakers * kPer) {
-              const int r = r0 + lane / kL;
-              const int rt = r / kBq, rr = r % kBq, tok0 = w.t * item_tt + rt * tt, rows = max(0, min(w.q.rows - tok0, tt)) * group;
-              uint4 x = make_uint4(0u, 0u, 0u, 0u);
-              if (r < C::kRows && rr < rows)
-                x = *reinterpret_cast<const uint4*>(a.q + (int64_t)(w.q.row0 + tok0 + rr / group) * a.q_row +
-                                                    (int64_t)(w.h * group + rr % group) * a.q_head + 8 * sub);
-              uint32_t tops = __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu));
-#pragma unroll
-              for (int o = kL / 2; o > 0; o >>= 1) tops = __vmaxu2(tops, __shfl_xor_sync(0xffffffffu, tops, o));
-              const uint32_t top = __float_as_uint(unpack2<kBf16>(max(tops & 0xffffu, tops >> 16)).x);
-              // the row in units of 2^e: its largest in [2^14, 2^15) (a row that is not finite is NaN, and its result too)
-              const int e = top == 0 ? 0 : max((int)(top >> 23) - 127, -126) - 14;
-              const float up0 = top >= 0x7f800000u ? NAN : two_to(-e / 2), up1 = two_to(-e - (-e / 2));
-              const uint32_t v[4] = {x.x, x.y, x.z, x.w};
-              uint32_t h[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float2 f = unpack2<kBf16>(v[k]);
-                h[k] = pack2<false>(f.x * up0 * up1, f.y * up0 * up1);
-              }
-              if (r < C::kRows) {
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(
-                                 base + (uint32_t)(rt * C::kTile + (sub >> 3) * kSub + rr * 128 + (((sub & 7) ^ (rr & 7)) << 4))),
-                             "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3])
-                             : "memory");
-                if (sub == 0) s_exp[item & 1][r] = e;
-              }
+          // ---- the item's queries
+          if (me == 0) {
+            if (item > 0 && !wait_beat(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, &s_beat)) {
+              ok = false;
+              break;
             }
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(C::Q_FULL));
-          }
-          for (int i = 0; ok && i < w.cnt; ++i, ++g) {
-            const int st = g % C::kStages;
-            const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (8 * (i & 3))) & 0xffu;
-            constexpr int kParts = C::kKParts;
-            int at_part = -1;
+            if (elect_one()) {
+              mbar_arrive_expect_tx(bar(C::Q_FULL), (uint32_t)(kRt * group * tt * 128 * C::kChunks));
 #pragma unroll
-            for (int j = 0; j < kMost; ++j) {
-              const int n = mine + j * team;
-              if (n >= kUnits) continue;
-              int group, ch;
-              place(n, group, ch);
-              const int pt = n / (kUnits / kParts);
-              if (pt != at_part) {  // the parts before are complete, this one's place has to be free
-                for (; at_part >= 0 && at_part < pt; ++at_part) {
-                  asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-                  __syncwarp();
-                  if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
+              for (int rt = 0; rt < kRt; ++rt)
+#pragma unroll
+                for (int ch = 0; ch < C::kChunks; ++ch)
+                  tma_load_3d(base + (uint32_t)(rt * C::kTile + ch * kSub), &tmQ, 64 * ch, w.h * group,
+                              w.q.row0 + w.t * item_tt + rt * tt, bar(C::Q_FULL));
+            }
+            __syncwarp();
+          }
+#pragma unroll 1
+          for (int i = -1; ok && i < w.cnt; ++i) {
+            if (i >= 0) {
+              const int st = g % C::kStages;
+              const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (8 * (i & 3))) & 0xffu;
+              constexpr int kParts = C::kKParts;
+              int at_part = -1;
+#pragma unroll
+              for (int j = 0; j < kMost; ++j) {
+                const int n = mine + j * team;
+                if (n >= kUnits) continue;
+                int gr, ch;
+                place(n, gr, ch);
+                const int pt = n / (kUnits / kParts);
+                if (pt != at_part) {  // the part before is complete, this one's place has to be free
+                  if (at_part >= 0) {
+                    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
+                  }
+                  at_part = pt;
+                  if (ok && g >= C::kStages && !wait_beat(bar(free + st * kParts + pt), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat))
+                    ok = false;
+                  if (!kv && mine == 0 && pt == 0 && lane == 0) held[g & 7] = there;
                 }
-                at_part = pt;
-                if (ok && g >= C::kStages && !wait_beat(bar(free + st * kParts + pt), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat))
-                  ok = false;
-                if (!kv && mine == 0 && pt == 0 && lane == 0) held[g & 7] = there;
+                const int key = 16 * gr + (lane >> 1);
+                const uint32_t at = base + (uint32_t)(off + st * C::kTile + ch * kSub + key * 128), swz = (uint32_t)((4 * (lane & 1)) ^ (key & 7)) << 4;
+                if (kv)
+                  store_unit<false>(u[j].w.x, u[j].w.y, u[j].w.z, u[j].w.w, u[j].sc, at, swz);
+                else
+                  store_unit<kBf16>(u[j].w.x, u[j].w.y, u[j].w.z, u[j].w.w, u[j].sc, at, swz);
               }
-              if (ok) store_unit(u[j], base + (uint32_t)(off + st * C::kTile + ch * kSub), 16 * group + (lane >> 1), lane);
+              asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
+              ++g;
+              if (((i + 1) & 3) == 0) page = ahead;
             }
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
             // the next tile's codes are on their way while this one's place in the ring is awaited
-            if (((i + 1) & 3) == 0 && i + 1 < w.cnt) page = ahead;
             if ((i & 3) == 1 && i + 3 < w.cnt)
               ahead = group_page(b, c, w.s, (w.first + w.k0 + (i | 3) + 1) << kBkShift, lo, hi, 16, lane);
             if (i + 1 < w.cnt) load_tile(i + 1);
           }
         }
         if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
+        // the queries' copies land before the CTA may end
+        if (me == 0 && item > 0 && !wait_beat(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, &s_beat) && lane == 0)
+          give_up(err, a, DEVERR_DRAIN_WAIT);
       }
     } else if (!kFp4 && (warp == C::kLoadWarp || warp == C::kLoadV)) {
       // ---------------------------------------------------------------------- TMA copies
@@ -398,8 +400,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
       if (!drained && lane == 0) give_up(err, a, DEVERR_DRAIN_WAIT);
     } else if (warp == kIssueWarp) {
       // ---------------------------------------------------------------------- MMAs
-      constexpr uint32_t fmt = kOpBf16 ? 1u : 0u;
-      constexpr uint32_t idesc_s = idesc_f16(fmt, kBk, kBq), idesc_o = idesc_f16(fmt, kDim, kBq) | kIdescBMnMajor;
+      constexpr uint32_t idesc_s = idesc_f16(kBf16 ? 1u : 0u, kBk, kBq), idesc_o = idesc_f16(kOpBf16 ? 1u : 0u, kDim, kBq) | kIdescBMnMajor;
       const uint64_t dq = sdesc_swz(base);
       // S of key tile i (this CTA's count) for row tile rt, into its slot; hands K back after the last row tile, Q after `last`
       auto issue_s = [&](int i, int rt, bool last) {
@@ -505,7 +506,10 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
       const int hf = kRt == 2 ? 0 : warp >> 2;                               // which half
       const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
       const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
-      float sc = a.scale * kLog2e;
+      const float sc = [&] {
+        if constexpr (kFp4) return ldexpf(a.scale * kLog2e, pages.k_exp);
+        return a.scale * kLog2e;
+      }();
       const float back = [&] {
         if constexpr (kFp4) return two_to(pages.v_exp);
         return 1.0f;
@@ -523,9 +527,6 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
           if (ok && !wait_beat(bar(C::S_FULL + slot), (uint32_t)(kRt == 2 ? g : g >> 1) & 1u, &s_beat)) ok = false;
           if (!ok) continue;
           tc_fence_after();
-          if constexpr (kFp4) {  // (written ahead of the queries, which these scores are of)
-            if (i == 0) sc = ldexpf(a.scale * kLog2e, s_exp[item & 1][rt * kBq + r] + pages.k_exp);
-          }
           uint32_t x[32];
           float top = -INFINITY;
           const uint32_t there = held[g & 7];
@@ -804,19 +805,16 @@ w8a8_status launch(const Pages& pages, const PagedBatch& pb, const AttnCall& a, 
     W8A8_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     attr_set[dev] = true;
   }
-  CUtensorMap tq{}, tk{}, tv{};
-  int tt;
-  if constexpr (kFp4) {  // (no copies by TMA)
-    tt = kBq / (a.n_q / pages.p.n_kv);
-  } else {
-    const int group = a.n_q / pages.n_kv;
-    tt = kBq / group;
-    const uint64_t dims[3] = {(uint64_t)kDim, (uint64_t)a.n_q, (uint64_t)pb.n_rows};
-    const uint64_t strides[2] = {(uint64_t)a.q_head * 2, (uint64_t)a.q_row * 2};
-    const uint32_t box[3] = {64, (uint32_t)group, (uint32_t)tt};
-    W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
+  const int group = a.n_q / shape_of(pages).n_kv, tt = kBq / group;
+  CUtensorMap tq, tk, tv;
+  const uint64_t dims[3] = {(uint64_t)kDim, (uint64_t)a.n_q, (uint64_t)pb.n_rows};
+  const uint64_t strides[2] = {(uint64_t)a.q_head * 2, (uint64_t)a.q_row * 2};
+  const uint32_t box[3] = {64, (uint32_t)group, (uint32_t)tt};
+  W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
+  if constexpr (kFp4)
+    tk = tv = tq;  // not used: the cache is not copied by TMA
+  else
     W8A8_TRY(make_kv_maps(pages, kDim, &tk, &tv));
-  }
   char* base = static_cast<char*>(ws);
   W8A8_CUDA(launch_pdl(kernel, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
                        pages, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
