@@ -54,14 +54,17 @@ struct Cfg {
   static constexpr int kStages = kDim == 256 ? 1 : kDim == 128 ? 2 : 4;
   static constexpr int kTile = kChunks * kSub;
   static constexpr int kOffK = kRt * kTile, kOffV = kOffK + kStages * kTile;
-  static constexpr int kSmem = kOffV + kStages * kTile + 1024;
+  static constexpr int kOffRaw = kOffV + kStages * kTile;  // (of K, then of V)
+  static constexpr int kSmem = kOffRaw + (kFp4 ? 2 * 3 * 4608 : 0) + 1024;
   static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys
   static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
   static constexpr int kSplit = 2 / kRt;           // threads a row
-  // warps: softmax, then (16 bits) a copier of queries and K, the issuer, a copier of V, or (4 bits) the issuer and seven that
-  // turn codes into operands, three for K and four for V
-  static constexpr int kSoft = 8, kLoadWarp = kSoft, kIssueWarp = kFp4 ? kSoft : kSoft + 1, kLoadV = kSoft + 2;
-  static constexpr int kMakeK = 3, kMakeV = 4, kMakers = kMakeK + kMakeV;
+  // warps: softmax, then (16 bits) a copier of queries and K, the issuer, a copier of V, or (4 bits) the issuer, a copier of queries
+  // and codes, and six that turn codes into operands, four for K (which takes more where it becomes bf16) and two for V
+  static constexpr int kSoft = 8, kLoadWarp = kFp4 ? kSoft + 1 : kSoft, kIssueWarp = kFp4 ? kSoft : kSoft + 1, kLoadV = kSoft + 2;
+  static constexpr int kMakeK = 4, kMakeV = 2;
+  // codes come by parts of 4 KB with 512 bytes of scales: 64 dims of a tile's keys (K), 32, 64 or 128 keys (V); rings of three
+  static constexpr int kRawParts = kChunks, kRawKeys = kBk / kRawParts, kRaw = 4096 + 512, kRawSlots = 3;
   static constexpr int kThreads = kFp4 ? 512 : 32 * (kSoft + 3);
   static constexpr int kRows = kBq * kRt;
   static constexpr int kPart = kRows * kDim + 2 * kRows;  // floats of a partial: [dim / 4][rows][4], m, l
@@ -72,7 +75,8 @@ struct Cfg {
   // PV_DONE by row tile, its second one with one row tile for an item's last product
   static constexpr int Q_FULL = 0, Q_FREE = 1, S_FULL = 2, P_FULL = 4, PV_DONE = 8, O_FREE = 10, ALL_DONE = 12, X_FULL = 13,
                        K_FULL = 14, K_FREE = K_FULL + kStages * kKParts, V_FULL = K_FREE + kStages * kKParts,
-                       V_FREE = V_FULL + kStages * kVParts, kBars = V_FREE + kStages * kVParts;
+                       V_FREE = V_FULL + kStages * kVParts, RAW_FULL = V_FREE + kStages * kVParts, RAW_FREE = RAW_FULL + 6,
+                       kBars = kFp4 ? RAW_FREE + 6 : RAW_FULL;
 };
 
 // Shared-memory descriptor of an MN-major tile, 128-byte swizzle: 64 elements of the MN dimension a row of 128 bytes, 8 rows
@@ -119,30 +123,11 @@ __host__ __device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c
 // Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  A code times its scale has six
 // significant bits and lies within fp16's range as within bf16's, so operands are exact in either type: K has the queries', V is fp16
 // whatever the type, as the weights are.
-struct Fp4Unit {
-  uint4 w;
-  uint32_t sc;
-};
-__device__ __forceinline__ Fp4Unit load_unit(const uint8_t* codes, const uint8_t* scales, const Fp4Pages& c, int page, int slot,
-                                             int head, int ch, int lane) {
-  Fp4Unit u;
-  u.w = make_uint4(0u, 0u, 0u, 0u);
-  u.sc = 0;
-  if (page >= 0) {
-    const int part = 2 * ch + (lane & 1);
-    u.w = __ldg(reinterpret_cast<const uint4*>(codes + (int64_t)page * c.p.page_stride + (int64_t)slot * c.p.slot_stride +
-                                               (int64_t)head * c.p.head_stride) + part);
-    u.sc = __ldg(reinterpret_cast<const uint16_t*>(scales + (int64_t)page * c.s_page + (int64_t)slot * c.s_slot +
-                                                   (int64_t)head * c.s_head) + part);
-  }
-  return u;
-}
-// Into row `key` of a 64-dim column (128-byte rows, swizzled): `at` is the row, `swz` its part and swizzle.  Not inline: the code
-// of a dozen copies would not stay in the instruction cache.
+// Into a row of a 64-dim column (128-byte rows, swizzled): `at` is the row, `swz` its part and swizzle.
 // To bf16: fp16's bits shifted into place are the value times 2^-112 (nothing of a code is lost), the scale is taken times 2^112.
 template <bool kToBf16>
-__device__ __noinline__ void store_unit(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, uint32_t sc, uint32_t at, uint32_t swz) {
-  const uint32_t w[4] = {w0, w1, w2, w3};
+__device__ __forceinline__ void store_unit(const uint4& codes, uint32_t sc, uint32_t at, uint32_t swz) {
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
   uint32_t h2 = e4m3x2_to_f16x2(sc);
   if constexpr (kToBf16) {
     const uint32_t lo = h2 & 0xffffu, hi = h2 >> 16;
@@ -186,6 +171,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
   __shared__ LineStart ls;
   __shared__ long long scan[kThreads / 32];
   __shared__ uint32_t held[8];  // 16-key groups of a tile that lie in a page
+  __shared__ uint32_t raw_held[2][kFp4 ? C::kRawSlots : 1];  // of the tile a part is of
   __shared__ uint32_t tmem_slot, s_last, s_bad[4], s_beat;
   __shared__ float s_max[C::kSplit][C::kSplit][kBq], s_sum[C::kSplit][kBq];  // two threads a row: what they tell each other
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -201,14 +187,13 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
       int n = (i >= C::P_FULL && i < C::PV_DONE) || i == C::O_FREE || i == C::O_FREE + 1 || i == C::X_FULL ? C::kArrive : 1;
       if (kFp4 && i >= C::K_FULL && i < C::K_FREE) n = C::kMakeK;
       if (kFp4 && i >= C::V_FULL && i < C::V_FREE) n = C::kMakeV;
+      if (kFp4 && i >= C::RAW_FULL) n = i < C::RAW_FREE ? 33 : i < C::RAW_FREE + 3 ? C::kMakeK : C::kMakeV;
       mbar_init(bar(i), n);
     }
     fence_mbar_init();
     prefetch_tmap(&tmQ);
-    if constexpr (!kFp4) {
-      prefetch_tmap(&tmK);
-      prefetch_tmap(&tmV);
-    }
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
   }
   if (warp == kIssueWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(smem_u32(&tmem_slot))
@@ -235,39 +220,125 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
     Walk w;
     w.start(ls, b, c.page_shift, a.window, item_tt, kBkShift, lane);
     int g = 0, item = 0;  // tiles and items of this CTA so far
-    if (kFp4 && warp > kIssueWarp) {
+    if (kFp4 && warp > C::kLoadWarp) {
       if constexpr (kFp4) {
         // -------------------------------------------------------------------- operands from 4 bits
-        const int me = warp - kIssueWarp - 1;
+        const int me = warp - C::kLoadWarp - 1;
         const bool kv = me >= C::kMakeK;  // V
         const int team = kv ? C::kMakeV : C::kMakeK, mine = kv ? me - C::kMakeK : me;
         const int full = kv ? C::V_FULL : C::K_FULL, free = kv ? C::V_FREE : C::K_FREE, off = kv ? C::kOffV : C::kOffK;
-        const uint8_t *codes = kv ? pages.v : pages.k, *scales = kv ? pages.vs : pages.ks;
-        constexpr int kUnits = 8 * C::kChunks, kMost = (kUnits + C::kMakeK - 1) / C::kMakeK;  // of a tile; a warp's at most
-        // unit n of a tile: K by 64 dims, V by 16 keys, the order in which their parts are handed over
-        auto place = [&](int n, int& gr, int& ch) {
-          gr = kv ? n / C::kChunks : n & 7;
-          ch = kv ? n % C::kChunks : n >> 3;
-        };
+        const int rfull = C::RAW_FULL + (kv ? 3 : 0), rfree = C::RAW_FREE + (kv ? 3 : 0);
+        const uint32_t raw0 = base + (uint32_t)(C::kOffRaw + (kv ? 3 * C::kRaw : 0));
+        const int key0 = lane >> 1, half = lane & 1;  // of a unit: 16 keys by 64 dims, 32 dims a lane
+        const uint32_t to0 = (uint32_t)(key0 * 128), swz = (uint32_t)((4 * half) ^ (key0 & 7)) << 4;
+        // bytes between keys in a part; K: 64 dims, V: all
+        const uint32_t row = kv ? kDim / 2 : 32, srow = kv ? kDim / 16 : 4;
+        int r = 0;  // parts so far
         for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
           const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
-          // the pages of four tiles, a 16-key group a lane
-          int page = group_page(b, c, w.s, (w.first + w.k0) << kBkShift, lo, hi, 16, lane), ahead = -1;
-          Fp4Unit u[kMost];
-          auto load_tile = [&](int i) {
-            const int tile0 = (w.first + w.k0 + i) << kBkShift;
-#pragma unroll
-            for (int j = 0; j < kMost; ++j) {
-              const int n = mine + j * team;
-              int gr, ch;
-              place(n, gr, ch);
-              const int pg = __shfl_sync(0xffffffffu, page, ((i & 3) * 8 + gr) & 31), key = tile0 + 16 * gr + (lane >> 1);
-              // keys that no row of the item sees are zeros: nothing of theirs may meet a weight of 0
-              if (n < kUnits) u[j] = load_unit(codes, scales, pages, key >= lo && key <= hi ? pg : -1, key & ((1 << c.page_shift) - 1), w.h, ch, lane);
+          for (int i = 0; ok && i < w.cnt; ++i, ++g) {
+            const int st = g % C::kStages, tile0 = (w.first + w.k0 + i) << kBkShift;
+            const bool edge = tile0 < lo || tile0 + kBk - 1 > hi;
+#pragma unroll 1
+            for (int pt = 0; pt < C::kRawParts; ++pt, ++r) {
+              const int slot = r % C::kRawSlots, op = C::kKParts == 1 ? 0 : pt;  // the operand's part
+              if (ok && !wait_beat(bar(rfull + slot), (uint32_t)(r / C::kRawSlots) & 1u, &s_beat)) ok = false;
+              if (ok && g >= C::kStages && (C::kKParts > 1 || pt == 0) &&
+                  !wait_beat(bar(free + st * C::kKParts + op), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat))
+                ok = false;
+              if (!ok) break;
+              const uint32_t there = raw_held[kv][slot];
+              if (!kv && me == 0 && pt == 0 && lane == 0) held[g & 7] = there;
+              const uint32_t src = raw0 + (uint32_t)(slot * C::kRaw);
+              // the part's eight units: by keys (K), by keys and 64 dims (V)
+#pragma unroll 1
+              for (int n = mine; n < 8; n += team) {
+                const int gr = kv ? n / C::kChunks : n, ch = kv ? n % C::kChunks : pt, in = 16 * gr + key0;  // group, column, key of the part
+                const int group16 = gr + (kv ? pt * (C::kRawKeys / 16) : 0), key = tile0 + 16 * group16 + key0;
+                uint4 x = lds128(src + (uint32_t)in * row + (kv ? 32u * ch : 0u) + 16u * half);
+                uint16_t sc;
+                asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(sc) : "r"(src + 4096u + (uint32_t)in * srow + (kv ? 4u * ch : 0u) + 2u * half) : "memory");
+                // keys that no row of the item sees, or in no page, are zeros: nothing of theirs may meet a weight of 0
+                if (!((there >> group16) & 1u) || (edge && (key < lo || key > hi))) {
+                  x = make_uint4(0u, 0u, 0u, 0u);
+                  sc = 0;
+                }
+                const uint32_t at = base + (uint32_t)(off + st * C::kTile + ch * kSub + group16 * 2048) + to0;
+                if (kv)
+                  store_unit<false>(x, sc, at, swz);
+                else
+                  store_unit<kBf16>(x, sc, at, swz);
+              }
+              asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+              __syncwarp();
+              if (lane == 0) {
+                mbar_arrive(bar(rfree + slot));
+                if (C::kKParts > 1 || pt == C::kRawParts - 1) mbar_arrive(bar(full + st * C::kKParts + op));
+              }
             }
-          };
-          // ---- the item's queries
-          if (me == 0) {
+          }
+        }
+        if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
+      }
+    } else if (kFp4 && warp == C::kLoadWarp) {
+      if constexpr (kFp4) {
+        // -------------------------------------------------------------------- copies of queries, codes and scales
+        int r = 0;  // parts of K, and of V, so far
+        for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
+          const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
+          constexpr int kBatch = 4;  // tiles whose pages are read at once, ahead of their use: a 16-key group a lane
+          const int box = min(1 << c.page_shift, C::kRawKeys);
+          int page = group_page(b, c, w.s, (w.first + w.k0) << kBkShift, lo, hi, box, lane), ahead = -1;
+          for (int i = 0; ok && i < w.cnt; ++i) {
+            const int tile0 = (w.first + w.k0 + i) << kBkShift, in_batch = i % kBatch;
+            if (in_batch == 0) {
+              if (i > 0) page = ahead;
+              if (i + kBatch < w.cnt) ahead = group_page(b, c, w.s, tile0 + (kBatch << kBkShift), lo, hi, box, lane);
+            }
+            const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (8 * in_batch)) & 0xffu;
+#pragma unroll 1
+            for (int pt = 0; ok && pt < C::kRawParts; ++pt, ++r) {
+              const int slot = r % C::kRawSlots;
+#pragma unroll 1
+              for (int kv = 0; kv < 2; ++kv) {
+                if (r >= C::kRawSlots && !wait_beat(bar(C::RAW_FREE + 3 * kv + slot), (uint32_t)(r / C::kRawSlots - 1) & 1u, &s_beat)) {
+                  ok = false;
+                  break;
+                }
+                const uint32_t fullbar = bar(C::RAW_FULL + 3 * kv + slot), dst = base + (uint32_t)(C::kOffRaw + (3 * kv + slot) * C::kRaw);
+                if (lane == 0) {
+                  raw_held[kv][slot] = there;
+                  mbar_arrive_expect_tx(fullbar, 4096u);
+                }
+                __syncwarp();
+                const int keys = kv ? C::kRawKeys : kBk, first = kv ? pt * C::kRawKeys : 0;  // of the tile
+                const int row = kv ? kDim / 2 : 32;
+                const int pg = __shfl_sync(0xffffffffu, page, (8 * in_batch + (first + lane * box) / 16) & 31);
+                if (lane * box < keys) {
+                  const int slot0 = (tile0 + first + lane * box) & ((1 << c.page_shift) - 1), at = pg < 0 ? c.n_pages : pg;
+                  tma_load_4d(dst + (uint32_t)(lane * box * row), kv ? &tmV : &tmK, kv ? 0 : 32 * pt, slot0, w.h, at, fullbar);
+                }
+                const uint8_t* scales = (kv ? pages.vs : pages.ks) + (int64_t)w.h * pages.s_head;
+#pragma unroll 1
+                for (int k0 = 0; k0 < keys; k0 += 32) {
+                  const int key = first + k0 + lane, kpg = __shfl_sync(0xffffffffu, page, (8 * in_batch + key / 16) & 31);
+                  if (k0 + lane < keys && kpg >= 0) {
+                    const uint8_t* from = scales + (int64_t)kpg * pages.s_page + (int64_t)((tile0 + key) & ((1 << c.page_shift) - 1)) * pages.s_slot;
+                    if (kv)
+                      asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(dst + 4096u + (uint32_t)((k0 + lane) * (kDim / 16))),
+                                   "l"(from), "n"(kDim / 16)
+                                   : "memory");
+                    else
+                      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst + 4096u + (uint32_t)((k0 + lane) * 4)),
+                                   "l"(from + 4 * pt)
+                                   : "memory");
+                  }
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(fullbar) : "memory");
+              }
+            }
+            // the queries, behind the first tile: that needs nothing of this item, and is on its way while the last item's products run
+            if (i > 0) continue;
             if (item > 0 && !wait_beat(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, &s_beat)) {
               ok = false;
               break;
@@ -283,54 +354,15 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
             }
             __syncwarp();
           }
-#pragma unroll 1
-          for (int i = -1; ok && i < w.cnt; ++i) {
-            if (i >= 0) {
-              const int st = g % C::kStages;
-              const uint32_t there = (__ballot_sync(0xffffffffu, page >= 0) >> (8 * (i & 3))) & 0xffu;
-              constexpr int kParts = C::kKParts;
-              int at_part = -1;
-#pragma unroll
-              for (int j = 0; j < kMost; ++j) {
-                const int n = mine + j * team;
-                if (n >= kUnits) continue;
-                int gr, ch;
-                place(n, gr, ch);
-                const int pt = n / (kUnits / kParts);
-                if (pt != at_part) {  // the part before is complete, this one's place has to be free
-                  if (at_part >= 0) {
-                    asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
-                  }
-                  at_part = pt;
-                  if (ok && g >= C::kStages && !wait_beat(bar(free + st * kParts + pt), (uint32_t)(g / C::kStages - 1) & 1u, &s_beat))
-                    ok = false;
-                  if (!kv && mine == 0 && pt == 0 && lane == 0) held[g & 7] = there;
-                }
-                const int key = 16 * gr + (lane >> 1);
-                const uint32_t at = base + (uint32_t)(off + st * C::kTile + ch * kSub + key * 128), swz = (uint32_t)((4 * (lane & 1)) ^ (key & 7)) << 4;
-                if (kv)
-                  store_unit<false>(u[j].w.x, u[j].w.y, u[j].w.z, u[j].w.w, u[j].sc, at, swz);
-                else
-                  store_unit<kBf16>(u[j].w.x, u[j].w.y, u[j].w.z, u[j].w.w, u[j].sc, at, swz);
-              }
-              asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-              __syncwarp();
-              if (lane == 0) mbar_arrive(bar(full + st * kParts + at_part));
-              ++g;
-              if (((i + 1) & 3) == 0) page = ahead;
-            }
-            // the next tile's codes are on their way while this one's place in the ring is awaited
-            if ((i & 3) == 1 && i + 3 < w.cnt)
-              ahead = group_page(b, c, w.s, (w.first + w.k0 + (i | 3) + 1) << kBkShift, lo, hi, 16, lane);
-            if (i + 1 < w.cnt) load_tile(i + 1);
-          }
         }
         if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
-        // the queries' copies land before the CTA may end
-        if (me == 0 && item > 0 && !wait_beat(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, &s_beat) && lane == 0)
-          give_up(err, a, DEVERR_DRAIN_WAIT);
+        // the last copies land before the CTA may end
+        asm volatile("cp.async.wait_all;\n" ::: "memory");
+        bool drained = item == 0 || wait_beat(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, &s_beat);
+        for (int k = max(0, r - C::kRawSlots); k < r; ++k)
+          for (int kv = 0; kv < 2; ++kv)
+            drained &= wait_beat(bar(C::RAW_FULL + 3 * kv + k % C::kRawSlots), (uint32_t)(k / C::kRawSlots) & 1u, &s_beat);
+        if (!drained && lane == 0) give_up(err, a, DEVERR_DRAIN_WAIT);
       }
     } else if (!kFp4 && (warp == C::kLoadWarp || warp == C::kLoadV)) {
       // ---------------------------------------------------------------------- TMA copies
@@ -811,10 +843,17 @@ w8a8_status launch(const Pages& pages, const PagedBatch& pb, const AttnCall& a, 
   const uint64_t strides[2] = {(uint64_t)a.q_head * 2, (uint64_t)a.q_row * 2};
   const uint32_t box[3] = {64, (uint32_t)group, (uint32_t)tt};
   W8A8_TRY(make_tmap_16(&tq, a.q, 3, dims, strides, box));
-  if constexpr (kFp4)
-    tk = tv = tq;  // not used: the cache is not copied by TMA
-  else
+  if constexpr (kFp4) {  // codes: 64 dims of K, all of V, of up to a part's keys
+    const int page = 1 << pages.p.page_shift;
+    const uint64_t cd[4] = {(uint64_t)kDim / 2, (uint64_t)page, (uint64_t)pages.p.n_kv, (uint64_t)pages.p.n_pages};
+    const uint64_t cs[3] = {(uint64_t)pages.p.slot_stride, (uint64_t)pages.p.head_stride, (uint64_t)pages.p.page_stride};
+    uint32_t cb[4] = {32, (uint32_t)(page < C::kRawKeys ? page : C::kRawKeys), 1, 1};
+    W8A8_TRY(make_tmap_8(&tk, pages.k, 4, cd, cs, cb, 0));
+    cb[0] = kDim / 2;
+    W8A8_TRY(make_tmap_8(&tv, pages.v, 4, cd, cs, cb, 0));
+  } else {
     W8A8_TRY(make_kv_maps(pages, kDim, &tk, &tv));
+  }
   char* base = static_cast<char*>(ws);
   W8A8_CUDA(launch_pdl(kernel, dim3((unsigned)sms), dim3(C::kThreads), (size_t)C::kSmem, st, tq, tk, tv,
                        pages, pb, a, tt, reinterpret_cast<float*>(base + W8A8_WS_RESERVED), reinterpret_cast<unsigned int*>(base),
