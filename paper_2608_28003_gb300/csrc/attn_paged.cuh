@@ -93,6 +93,7 @@ struct LineStart {
   long long rest;               // units of sequence s before `begin`
   int s, workers, unit;         // unit 0: key tiles
   SeqShape q;                   // of sequence s
+  int extra;                    // units ahead of an item's tiles that stand for what an item costs beside them; nobody's work
 };
 __device__ __forceinline__ int units_of(int n, int unit) { return unit ? (n + unit - 1) / unit : n; }
 
@@ -128,7 +129,7 @@ __device__ __forceinline__ long long sum_tiles(const SeqShape& q, int window, in
 // sequences; up to 32 of them are one warp's alone.
 template <int kT>
 __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, int n_kv, int window, int tt, int bk_shift,
-                                           int worker, int workers, LineStart* out, long long* scan) {
+                                           int worker, int workers, LineStart* out, long long* scan, int extra = 0) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool one_warp = b.n_seqs <= 32;
   if (one_warp && warp > 0) {
@@ -172,7 +173,7 @@ __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, 
     return upto;
   };
   long long one = 0, total = 0;
-  for (int i = 0; i < per; ++i) one += sum_of(~(tid * per + i), [](int n) { return (long long)n; });
+  for (int i = 0; i < per; ++i) one += sum_of(~(tid * per + i), [&](int n) { return (long long)(n + extra); });
   long long upto = run(one * n_kv, total);
   int unit = 0;
   if (total > workers && total <= (long long)kShort * workers) {
@@ -199,22 +200,23 @@ __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, 
         one = (some >> (16 * j)) & 0xffff;
       }
   }
+  if (unit) extra = 0;
   const long long mine = one * n_kv;
   const int used = (int)min((long long)workers, total);
   if (worker >= used) {
-    if (tid == 0) *out = LineStart{total, 0, 0, 1, 0, 0, used, unit, q};
+    if (tid == 0) *out = LineStart{total, 0, 0, 1, 0, 0, used, unit, q, 0};
     __syncthreads();
     return;
   }
   const long long begin = total * worker / used, end = total * (worker + 1) / used;
   const bool owner = begin >= upto - mine && begin < upto;
   if (per == 1) {
-    if (owner) *out = LineStart{total, begin, end, one, begin - (upto - mine), tid, used, unit, q};
+    if (owner) *out = LineStart{total, begin, end, one, begin - (upto - mine), tid, used, unit, q, extra};
   } else if (__any_sync(0xffffffffu, owner)) {  // the owner's warp walks its sequences again
     long long at = upto - mine;
     for (int i = 0; i < per; ++i) {
-      const long long c = sum_of(tid * per + i, [&](int n) { return (long long)units_of(n, unit); });
-      if (begin >= at && begin < at + c * n_kv) *out = LineStart{total, begin, end, c, begin - at, tid * per + i, used, unit, q};
+      const long long c = sum_of(tid * per + i, [&](int n) { return (long long)(units_of(n, unit) + extra); });
+      if (begin >= at && begin < at + c * n_kv) *out = LineStart{total, begin, end, c, begin - at, tid * per + i, used, unit, q, extra};
       at += c * n_kv;
     }
   }
@@ -225,7 +227,7 @@ __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, 
 struct Walk {
   long long off, at, end;   // line offsets: the item's first unit, the piece's, the stretch's end
   SeqShape q;
-  int s, h, t, row_tiles, unit;
+  int s, h, t, row_tiles, unit, extra;
   int first, n;             // the item's key tiles: first, first + 1, ..
   int k0, cnt;              // the piece: tiles k0 .. k0 + cnt - 1 of them
 
@@ -245,6 +247,7 @@ struct Walk {
     s = ls.s;
     q = ls.q;
     unit = ls.unit;
+    extra = ls.extra;
     row_tiles = (q.rows + tt - 1) / tt;
     h = ls.rest < ls.head_cost ? 0
         : ((ls.rest | ls.head_cost) >> 31) == 0 ? (int)((uint32_t)ls.rest / (uint32_t)ls.head_cost)
@@ -254,7 +257,7 @@ struct Walk {
     end = ls.end;
     for (int t0 = 0;; t0 += 32) {
       int f;
-      const int c = t0 + lane < row_tiles ? units_of(tiles_seen(q, window, tt, bk_shift, t0 + lane, f), unit) : 0;
+      const int c = t0 + lane < row_tiles ? units_of(tiles_seen(q, window, tt, bk_shift, t0 + lane, f), unit) + extra : 0;
       int upto = c;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -265,7 +268,8 @@ struct Walk {
       if (hit) {
         const int src = __ffs(hit) - 1;
         t = t0 + src;
-        off = at - (left - __shfl_sync(0xffffffffu, upto - c, src));
+        off = at - (left - __shfl_sync(0xffffffffu, upto - c, src)) + extra;  // the first tile's
+        if (at < off) at = off;
         break;
       }
       left -= __shfl_sync(0xffffffffu, upto, 31);
@@ -281,9 +285,9 @@ struct Walk {
   }
   __device__ __forceinline__ bool more() const { return at < end; }
   __device__ __forceinline__ void next(const PagedBatch& b, int page_shift, int n_kv, int window, int tt, int bk_shift) {
-    at += unit ? 1 : cnt;
+    at += (unit ? 1 : cnt) + extra;
     if (at >= end) return;
-    off += units_of(n, unit);
+    off += units_of(n, unit) + extra;
     if (++t == row_tiles) {
       t = 0;
       if (++h == n_kv) {

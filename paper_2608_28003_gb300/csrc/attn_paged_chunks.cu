@@ -46,6 +46,7 @@ namespace {
 
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
+constexpr int kItemCost = 2;     // 4 bits: what an item costs beside its key tiles, in key tiles
 
 template <int kDim, bool kFp4>
 struct Cfg {
@@ -59,10 +60,11 @@ struct Cfg {
   static constexpr int kKParts = kDim == 256 ? 4 : 1, kVParts = kKParts;  // a K tile comes by 64 dims, a V tile by 32 keys
   static constexpr int kKCols = kChunks / kKParts, kVKeys = kBk / kVParts;  // columns, keys a part
   static constexpr int kSplit = 2 / kRt;           // threads a row
-  // warps: softmax, then (16 bits) a copier of queries and K, the issuer, a copier of V, or (4 bits) the issuer, a copier of queries
-  // and codes, and six that turn codes into operands, four for K (which takes more where it becomes bf16) and two for V
+  // warps: softmax, then (16 bits) a copier of queries and K, the issuer, a copier of V, or (4 bits) the issuer,
+  // two for codes and scales of K, and the queries, and for V,
+  // and five that turn codes into operands, three for K (which takes more where it becomes bf16) and two for V
   static constexpr int kSoft = 8, kLoadWarp = kFp4 ? kSoft + 1 : kSoft, kIssueWarp = kFp4 ? kSoft : kSoft + 1, kLoadV = kSoft + 2;
-  static constexpr int kMakeK = 4, kMakeV = 2;
+  static constexpr int kMakeK = 3, kMakeV = 2;
   // codes come by parts of 4 KB with 512 bytes of scales: 64 dims of a tile's keys (K), 32, 64 or 128 keys (V); rings of three
   static constexpr int kRawParts = kChunks, kRawKeys = kBk / kRawParts, kRaw = 4096 + 512, kRawSlots = 3;
   static constexpr int kThreads = kFp4 ? 512 : 32 * (kSoft + 3);
@@ -207,25 +209,26 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
   pdl_wait();
   pdl_trigger();
   // (syncs the block)
-  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan);
+  find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan,
+                       kFp4 ? kItemCost : 0);
   bool ok = true;
-  if constexpr (kFp4) {  // registers: 512 threads of 128 are shared out as 256 of 152 and 256 of 104
+  if constexpr (kFp4) {  // registers: 512 threads of 128 are shared out as 256 of 144 and 256 of 112
     if (warp < C::kSoft)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 152;\n");
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 144;\n");
     else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 104;\n");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 112;\n");
   }
 
   if (ls.begin < ls.end) {
     Walk w;
     w.start(ls, b, c.page_shift, a.window, item_tt, kBkShift, lane);
     int g = 0, item = 0;  // tiles and items of this CTA so far
-    if (kFp4 && warp > C::kLoadWarp) {
+    if (kFp4 && warp > C::kLoadV) {
       if constexpr (kFp4) {
         // -------------------------------------------------------------------- operands from 4 bits
-        const int me = warp - C::kLoadWarp - 1;
+        const int me = warp - C::kLoadV - 1;
         const bool kv = me >= C::kMakeK;  // V
-        const int team = kv ? C::kMakeV : C::kMakeK, mine = kv ? me - C::kMakeK : me;
+        const int mine = kv ? me - C::kMakeK : me;
         const int full = kv ? C::V_FULL : C::K_FULL, free = kv ? C::V_FREE : C::K_FREE, off = kv ? C::kOffV : C::kOffK;
         const int rfull = C::RAW_FULL + (kv ? 3 : 0), rfree = C::RAW_FREE + (kv ? 3 : 0);
         const uint32_t raw0 = base + (uint32_t)(C::kOffRaw + (kv ? 3 * C::kRaw : 0));
@@ -252,7 +255,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
               const uint32_t src = raw0 + (uint32_t)(slot * C::kRaw);
               // the part's eight units: by keys (K), by keys and 64 dims (V)
 #pragma unroll 1
-              for (int n = mine; n < 8; n += team) {
+              for (int n = mine; n < 8; n += kv ? C::kMakeV : C::kMakeK) {
                 const int gr = kv ? n / C::kChunks : n, ch = kv ? n % C::kChunks : pt, in = 16 * gr + key0;  // group, column, key of the part
                 const int group16 = gr + (kv ? pt * (C::kRawKeys / 16) : 0), key = tile0 + 16 * group16 + key0;
                 uint4 x = lds128(src + (uint32_t)in * row + (kv ? 32u * ch : 0u) + 16u * half);
@@ -280,10 +283,11 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
         }
         if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
       }
-    } else if (kFp4 && warp == C::kLoadWarp) {
+    } else if (kFp4 && (warp == C::kLoadWarp || warp == C::kLoadV)) {
       if constexpr (kFp4) {
         // -------------------------------------------------------------------- copies of queries, codes and scales
-        int r = 0;  // parts of K, and of V, so far
+        const int kv = warp == C::kLoadV ? 1 : 0;  // V
+        int r = 0;                                 // parts so far
         for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
           const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
           constexpr int kBatch = 4;  // tiles whose pages are read at once, ahead of their use: a 16-key group a lane
@@ -299,8 +303,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
 #pragma unroll 1
             for (int pt = 0; ok && pt < C::kRawParts; ++pt, ++r) {
               const int slot = r % C::kRawSlots;
-#pragma unroll 1
-              for (int kv = 0; kv < 2; ++kv) {
+              {
                 if (r >= C::kRawSlots && !wait_beat(bar(C::RAW_FREE + 3 * kv + slot), (uint32_t)(r / C::kRawSlots - 1) & 1u, &s_beat)) {
                   ok = false;
                   break;
@@ -338,7 +341,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
               }
             }
             // the queries, behind the first tile: that needs nothing of this item, and is on its way while the last item's products run
-            if (i > 0) continue;
+            if (kv || i > 0) continue;
             if (item > 0 && !wait_beat(bar(C::Q_FREE), (uint32_t)(item - 1) & 1u, &s_beat)) {
               ok = false;
               break;
@@ -358,9 +361,8 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
         if (!ok && lane == 0) give_up(err, a, DEVERR_PRODUCER_WAIT);
         // the last copies land before the CTA may end
         asm volatile("cp.async.wait_all;\n" ::: "memory");
-        bool drained = item == 0 || wait_beat(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, &s_beat);
+        bool drained = kv || item == 0 || wait_beat(bar(C::Q_FULL), (uint32_t)(item - 1) & 1u, &s_beat);
         for (int k = max(0, r - C::kRawSlots); k < r; ++k)
-          for (int kv = 0; kv < 2; ++kv)
             drained &= wait_beat(bar(C::RAW_FULL + 3 * kv + k % C::kRawSlots), (uint32_t)(k / C::kRawSlots) & 1u, &s_beat);
         if (!drained && lane == 0) give_up(err, a, DEVERR_DRAIN_WAIT);
       }
