@@ -29,7 +29,8 @@ namespace w8a8 {
 
 namespace {
 
-constexpr int kWarps = 8;  // consumers
+constexpr int kWarps = 8;     // consumers
+constexpr int kItemCost = 4;  // what an item costs beside its key tiles, in key tiles
 
 template <int kDim, int kNt>
 struct Cfg {
@@ -139,7 +140,8 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
   }
   pdl_wait();
   pdl_trigger();
-  find_start<C::kThreads>(b, shift, n_kv, a.window, tt, C::kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan);
+  find_start<C::kThreads>(b, shift, n_kv, a.window, tt, C::kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan,
+                          kItemCost);
   if (ls.begin >= ls.end) return;
   Walk w;
   w.start(ls, b, shift, a.window, tt, C::kBkShift, lane);

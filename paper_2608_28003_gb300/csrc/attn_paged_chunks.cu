@@ -46,7 +46,7 @@ namespace {
 
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
-constexpr int kItemCost = 2;     // 4 bits: what an item costs beside its key tiles, in key tiles
+constexpr int kItemCost = 3;     // 4 bits: what an item costs beside its key tiles, in key tiles
 
 template <int kDim, bool kFp4>
 struct Cfg {
