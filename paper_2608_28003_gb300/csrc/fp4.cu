@@ -1,17 +1,17 @@
 // Quantisation of matrix rows to floating point of 4 bits, and back (w8a8_fp4).
 //
-// Both kernels only move data, so HBM bounds them, or for few rows the launch.  A thread holds a unit of 16 columns: 32 or 64
+// Both kernels only move data, so HBM bounds them, or for few rows the launch.  A thread holds units of 16 columns: 32 or 64
 // bytes in, 8 bytes of codes out; the scales of four neighbouring blocks meet in one lane, whose word is contiguous in the
 // tiled order.  With blocks of 16 a row's largest magnitude comes first: the row stays in registers over that reduction (up to
-// kHeld units a thread; longer rows are read again, from L2).
+// kHeld units a thread; what is beyond is read again, from L2).
+#include <algorithm>
+
 #include "fp4.cuh"
 #include "ops.cuh"
 
 namespace w8a8 {
 
 namespace {
-
-constexpr int kHeld = 2;  // units of a row that a thread keeps
 
 template <int kType>
 struct Unit16;  // 16 columns as loaded
@@ -53,50 +53,68 @@ __device__ __forceinline__ void unit_floats(const Unit16<kType>& u, float (&x)[1
     }
   }
 }
-// The bits of the largest magnitude: as integers, so that NaN and infinities are above everything.
-__device__ __forceinline__ uint32_t top_of(const float (&x)[16]) {
+// The bits of the largest magnitude, as an fp32 number's: compared as integers, so that NaN and infinities are above everything.
+template <int kType>
+__device__ __forceinline__ uint32_t top_of(const Unit16<kType>& u) {
   uint32_t t = 0;
 #pragma unroll
-  for (int e = 0; e < 16; ++e) t = max(t, __float_as_uint(x[e]) & 0x7fffffffu);
-  return t;
-}
-// Codes of 16 values in units already divided out.
-__device__ __forceinline__ uint2 codes16(const float (&q)[16]) {
-  uint32_t w[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    w[h] = e2m1x2_of(q[8 * h], q[8 * h + 1]) | e2m1x2_of(q[8 * h + 2], q[8 * h + 3]) << 8 |
-           e2m1x2_of(q[8 * h + 4], q[8 * h + 5]) << 16 | e2m1x2_of(q[8 * h + 6], q[8 * h + 7]) << 24;
-  return make_uint2(w[0], w[1]);
+  for (int i = 0; i < (int)(sizeof(u) / 16); ++i) {
+    if constexpr (kType == W8A8_TYPE_F32)
+      t = max(max(max(t, u.w[i].x & 0x7fffffffu), max(u.w[i].y & 0x7fffffffu, u.w[i].z & 0x7fffffffu)), u.w[i].w & 0x7fffffffu);
+    else
+      t = __vmaxu2(__vmaxu2(__vmaxu2(t, u.w[i].x & 0x7fff7fffu), __vmaxu2(u.w[i].y & 0x7fff7fffu, u.w[i].z & 0x7fff7fffu)),
+                   u.w[i].w & 0x7fff7fffu);
+  }
+  if constexpr (kType == W8A8_TYPE_F32) return t;
+  t = max(t & 0xffffu, t >> 16);
+  return kType == W8A8_TYPE_BF16 ? t << 16 : __float_as_uint(__half2float(__ushort_as_half((unsigned short)t)));
 }
 
 // One unit: its codes, and its block's scale byte (both lanes of a block of 32 have it).  `top` of this unit; s2 the reciprocal of
 // the row's scale (blocks of 16).  All lanes of a warp.
-template <int kBlock>
-__device__ __forceinline__ uint32_t quantise_unit(const float (&x)[16], uint32_t top, float s2, uint2& codes) {
-  float q[16];
+template <int kType, int kBlock>
+__device__ __forceinline__ uint32_t quantise_unit(const Unit16<kType>& u, uint32_t top, float s2, uint2& codes) {
+  float x[16];
+  unit_floats<kType>(u, x);
+  f32x2 q[8], hi, lo = 0ull;
+  uint32_t byte;
+  bool nan;
   if constexpr (kBlock == 16) {
     Block16 b;
     b.unit(top, s2);
+    byte = b.byte;
+    nan = byte == kE4m3NaN;
+    if (s2 > 0x1p60f || s2 < 0x1p-60f) {
+      // a row of numbers near the type's ends: brought towards 1 first (exactly, but for numbers whose codes are 0), so that the
+      // products below are normal numbers
+      const float near = s2 > 1.0f ? 0x1p60f : 0x1p-60f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) q[e] = b.byte == kE4m3NaN ? 0.0f : b.over(x[e] * s2);
-    codes = codes16(q);
-    return b.byte;
+      for (int e = 0; e < 16; ++e) x[e] *= near;
+      s2 *= s2 > 1.0f ? 0x1p-60f : 0x1p60f;
+    }
+    hi = f2_pack(b.hi * s2, b.hi * s2);  // (s2 is a power of two)
+    lo = f2_pack(b.lo * s2, b.lo * s2);
   } else {
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    const int e8 = top >= 0x7f800000u ? (int)kE8m0NaN : max((int)(top >> 23) - 2, 0);  // 2^(e8 - 127)
-    // 2^(127 - e8), a normal number but for e8 = 254, which no finite block has (253 - 2 at most); x times it is exact, or so
+    nan = top >= 0x7f800000u;
+    byte = nan ? kE8m0NaN : (uint32_t)max((int)(top >> 23) - 2, 0);  // 2^(byte - 127)
+    // 2^(127 - byte), a normal number but for 254, which no finite block has (252 at most); x times it is exact, or so
     // small that its code is 0
-    const float inv = __uint_as_float((uint32_t)(254 - e8) << 23);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) q[e] = top >= 0x7f800000u ? 0.0f : x[e] * inv;
-    codes = codes16(q);
-    return (uint32_t)e8;
+    const float inv = __uint_as_float((254u - min(byte, 253u)) << 23);
+    hi = f2_pack(inv, inv);
   }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const f32x2 v = f2_pack(x[2 * e], x[2 * e + 1]);
+    q[e] = f2_fma(v, hi, kBlock == 16 ? f2_fma(v, lo, 0ull) : 0ull);
+  }
+  codes = make_uint2(e2m1x8_of(q[0], q[1], q[2], q[3]), e2m1x8_of(q[4], q[5], q[6], q[7]));
+  if (nan) codes = make_uint2(0u, 0u);
+  return byte;
 }
 
 // kWarp: tpr (a power of two, kBlock / 4 to 32) neighbouring lanes take a row, else a block takes one.
-template <int kType, int kBlock, bool kWarp>
+template <int kType, int kBlock, bool kWarp, int kHeld>
 __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restrict__ x, int64_t x_row_bytes, int rows, int padded,
                                                            int k, int tpr, uint8_t* __restrict__ codes,
                                                            uint8_t* __restrict__ scales, float* __restrict__ row_scale,
@@ -113,25 +131,18 @@ __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restric
   const char* src = x + row * x_row_bytes;
   Unit16<kType> held[kHeld];
   uint32_t tops[kHeld];
-  float v[16], s2 = 1.0f;
+  float s2 = 1.0f;
 #pragma unroll
   for (int i = 0; i < kHeld; ++i)
     if (live && u0 + i * step < units) held[i] = load_unit<kType>(src, u0 + i * step);
 #pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    tops[i] = 0;
-    if (live && u0 + i * step < units) {
-      unit_floats<kType>(held[i], v);
-      tops[i] = top_of(v);
-    }
-  }
+  for (int i = 0; i < kHeld; ++i) tops[i] = live && u0 + i * step < units ? top_of<kType>(held[i]) : 0u;
   if constexpr (kBlock == 16) {
     uint32_t top = 0;  // of the blocks that are finite
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) top = max(top, tops[i] < 0x7f800000u ? tops[i] : 0u);
     for (int u = u0 + kHeld * step; live && u < units; u += step) {
-      unit_floats<kType>(load_unit<kType>(src, u), v);
-      const uint32_t t = top_of(v);
+      const uint32_t t = top_of<kType>(load_unit<kType>(src, u));
       top = max(top, t < 0x7f800000u ? t : 0u);
     }
     if constexpr (kWarp) {
@@ -146,84 +157,80 @@ __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restric
     s2 = two_to(-p);
     if (live && u0 == 0) row_scale[row] = two_to(p);
   }
-  // every lane makes the same trips: the scales' exchange is a whole warp's
-  for (int i = 0, first = kWarp ? 0 : (int)(threadIdx.x & ~31u); first < units; ++i, first += step) {
-    const int u = u0 + i * step;
+  auto put = [&](int u, const Unit16<kType>& x, uint32_t top) {
     const bool here = live && u < units;
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = 0.0f;
-    if (here) {
-      if (i < kHeld) {  // (unrolled, so that what is held stays in registers)
-#pragma unroll
-        for (int j = 0; j < kHeld; ++j)
-          if (i == j) {
-            unit_floats<kType>(held[j], v);
-            top = tops[j];
-          }
-      } else {
-        unit_floats<kType>(load_unit<kType>(src, u), v);
-        top = top_of(v);
-      }
-    }
     uint2 c;
-    uint32_t byte = quantise_unit<kBlock>(v, top, s2, c);
+    uint32_t byte = quantise_unit<kType, kBlock>(x, top, s2, c);
     if (here) *reinterpret_cast<uint2*>(codes + row * (int64_t)(k / 2) + 8 * u) = c;
     // the bytes of four blocks in their first lane
     constexpr int kStep = kBlock / 16;  // lanes a block
     const int j = u / kStep;
-    byte = here ? byte : 0u;
-    byte <<= 8 * (j & 3);
+    byte = here ? byte << (8 * (j & 3)) : 0u;
     byte |= __shfl_xor_sync(0xffffffffu, byte, kStep);
     byte |= __shfl_xor_sync(0xffffffffu, byte, 2 * kStep);
     if ((u & (4 * kStep - 1)) == 0 && u < units && row < padded)
       *reinterpret_cast<uint32_t*>(scales + fp4_scale_at(row, j, groups)) = byte;
+  };
+  // every lane makes the same trips: the scales' exchange is a whole warp's
+  const int first = kWarp ? 0 : (int)(threadIdx.x & ~31u);
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i)
+    if (first + i * step < units) {
+      if (!(live && u0 + i * step < units)) held[i] = Unit16<kType>{};
+      put(u0 + i * step, held[i], tops[i]);
+    }
+  for (int i = kHeld; first + i * step < units; ++i) {
+    Unit16<kType> x{};
+    if (live && u0 + i * step < units) x = load_unit<kType>(src, u0 + i * step);
+    put(u0 + i * step, x, top_of<kType>(x));
   }
 }
 
+// A thread has eight columns, so that a warp's loads and stores are contiguous, of kAhead places 256 threads apart.
+constexpr int kAhead = 4;
 template <int kType>
 __global__ void __launch_bounds__(256) fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
-                                                             const float* __restrict__ row_scale, int64_t total, int units,
+                                                             const float* __restrict__ row_scale, int64_t total, int eighths,
                                                              int block, int groups, char* __restrict__ y, int64_t y_row_bytes) {
   pdl_wait();
   pdl_trigger();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= total) return;
-  const int64_t row = i / units;
-  const int u = (int)(i - row * units);
-  const uint2 c = *reinterpret_cast<const uint2*>(codes + i * 8);
-  const uint32_t byte = scales[fp4_scale_at(row, block == 16 ? u : u >> 1, groups)];
-  float a, b = 1.0f;
-  if (block == 16) {
-    a = e4m3_value(byte);
-    b = row_scale[row];
-  } else {
-    a = byte == kE8m0NaN ? NAN : byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
+  const int64_t i0 = (int64_t)blockIdx.x * (256 * kAhead) + threadIdx.x;
+  uint32_t c[kAhead], byte[kAhead];
+  float b[kAhead];
+  int64_t row[kAhead];
+  int e8[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j) {
+    const int64_t i = i0 + 256 * j;
+    if (i >= total) continue;
+    row[j] = total < (1ll << 32) ? (int64_t)((uint32_t)i / (uint32_t)eighths) : i / eighths;
+    e8[j] = (int)(i - row[j] * eighths);
+    c[j] = *reinterpret_cast<const uint32_t*>(codes + i * 4);
+    byte[j] = scales[fp4_scale_at(row[j], block == 16 ? e8[j] >> 1 : e8[j] >> 2, groups)];
+    b[j] = block == 16 ? row_scale[row[j]] : 1.0f;
   }
-  float v[16];
-  uint32_t h[8];
-  uint32_t(&h0)[4] = *reinterpret_cast<uint32_t(*)[4]>(h), (&h1)[4] = *reinterpret_cast<uint32_t(*)[4]>(h + 4);
-  e2m1x8_to_f16(c.x, h0);
-  e2m1x8_to_f16(c.y, h1);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float2 f = unpack2<false>(h[e]);
-    v[2 * e] = f.x * a * b;
-    v[2 * e + 1] = f.y * a * b;
-  }
-  constexpr int kBytes = kType == W8A8_TYPE_F32 ? 64 : 32;
-  uint4* to = reinterpret_cast<uint4*>(y + row * y_row_bytes + (int64_t)u * kBytes);
-  if constexpr (kType == W8A8_TYPE_F32) {
+  for (int j = 0; j < kAhead; ++j) {
+    if (i0 + 256 * j >= total) break;
+    const float a = block == 16 ? e4m3_value(byte[j]) : byte[j] == kE8m0NaN ? NAN : byte[j] == 0 ? 0x1p-127f : __uint_as_float(byte[j] << 23);
+    uint32_t h[4];
+    float v[8];
+    e2m1x8_to_f16(c[j], h);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      to[e] = make_uint4(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), __float_as_uint(v[4 * e + 2]),
-                         __float_as_uint(v[4 * e + 3]));
-  } else {
-    constexpr bool kBf = kType == W8A8_TYPE_BF16;
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      to[e] = make_uint4(pack2<kBf>(v[8 * e], v[8 * e + 1]), pack2<kBf>(v[8 * e + 2], v[8 * e + 3]),
-                         pack2<kBf>(v[8 * e + 4], v[8 * e + 5]), pack2<kBf>(v[8 * e + 6], v[8 * e + 7]));
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = unpack2<false>(h[e]);
+      v[2 * e] = f.x * a * b[j];
+      v[2 * e + 1] = f.y * a * b[j];
+    }
+    constexpr int kBytes = kType == W8A8_TYPE_F32 ? 32 : 16;
+    uint4* to = reinterpret_cast<uint4*>(y + row[j] * y_row_bytes + (int64_t)e8[j] * kBytes);
+    if constexpr (kType == W8A8_TYPE_F32) {
+      to[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      to[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    } else {
+      constexpr bool kBf = kType == W8A8_TYPE_BF16;
+      to[0] = make_uint4(pack2<kBf>(v[0], v[1]), pack2<kBf>(v[2], v[3]), pack2<kBf>(v[4], v[5]), pack2<kBf>(v[6], v[7]));
+    }
   }
 }
 
@@ -248,14 +255,16 @@ w8a8_status check_fp4(const char* who, const w8a8_fp4* q) {
   return W8A8_OK;
 }
 
-// Lanes of a warp share its rows while a row's units fit; then a block a row, of as few threads as leave kHeld units to each.
+// Lanes of a warp share its rows while a row's units fit; then a block a row.  Many rows: threads of up to four units, whose loads fly
+// together (8191 rows of 6912: XX us, YY with one); few: of one, for the shortest chain.
 w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, bool settled,
                                 cudaStream_t st) {
   const int units = q.k / 16, padded = pad ? (int)round_up((size_t)q.rows, 128) : q.rows;
   int tpr = q.block / 4;  // four blocks' scales meet within a row's lanes
   while (tpr < units && tpr < 32) tpr *= 2;
-  const bool warp = units <= 32;
-  const int threads = warp ? 128 : units <= 512 ? (int)round_up((size_t)units, 32) : 512;
+  const bool warp = units <= 32, many = !warp && q.rows >= 1024;
+  const int held = dtype == W8A8_TYPE_F32 ? 2 : 4, each = many ? held : 1;
+  const int threads = warp ? 128 : std::min((int)round_up((size_t)(units + each - 1) / each, 32), 512);
   const int64_t blocks = warp ? ((int64_t)padded * tpr + 127) / 128 : padded;
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), 0, st, static_cast<const char*>(x),
@@ -263,8 +272,14 @@ w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w
   };
   auto of = [&](auto type) {
     constexpr int kT = decltype(type)::value;
-    if (q.block == 16) return warp ? go(fp4_quantise_kernel<kT, 16, true>) : go(fp4_quantise_kernel<kT, 16, false>);
-    return warp ? go(fp4_quantise_kernel<kT, 32, true>) : go(fp4_quantise_kernel<kT, 32, false>);
+    constexpr int kH = kT == W8A8_TYPE_F32 ? 2 : 4;
+    if (q.block == 16)
+      return warp   ? go(fp4_quantise_kernel<kT, 16, true, 1>)
+             : many ? go(fp4_quantise_kernel<kT, 16, false, kH>)
+                    : go(fp4_quantise_kernel<kT, 16, false, 2>);
+    return warp   ? go(fp4_quantise_kernel<kT, 32, true, 1>)
+           : many ? go(fp4_quantise_kernel<kT, 32, false, kH>)
+                  : go(fp4_quantise_kernel<kT, 32, false, 2>);
   };
   W8A8_CUDA(dtype == W8A8_TYPE_BF16  ? of(std::integral_constant<int, W8A8_TYPE_BF16>())
             : dtype == W8A8_TYPE_F16 ? of(std::integral_constant<int, W8A8_TYPE_F16>())
@@ -307,12 +322,12 @@ extern "C" w8a8_status w8a8_fp4_dequantize(const w8a8_fp4* q, int dtype, void* y
   W8A8_CHECK_ARG(aligned16(y), W8A8_ERR_ALIGN, "%s: y must be 16-byte aligned", who);
   W8A8_CHECK_ARG(q->rows == 1 || y_row >= q->k, W8A8_ERR_SHAPE, "%s: y's rows overlap", who);
   W8A8_TRY(check_device());
-  const int units = q->k / 16;
-  const int64_t total = (int64_t)q->rows * units, blocks = (total + 255) / 256;
+  const int eighths = q->k / 8;
+  const int64_t total = (int64_t)q->rows * eighths, blocks = (total + 256 * kAhead - 1) / (256 * kAhead);
   W8A8_CHECK_ARG(blocks <= 0x7fffffffll, W8A8_ERR_SHAPE, "%s: [%d, %d] is too large", who, q->rows, q->k);
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), (const uint8_t*)q->codes,
-                      (const uint8_t*)q->scales, (const float*)q->row_scale, total, units, q->block,
+                      (const uint8_t*)q->scales, (const float*)q->row_scale, total, eighths, q->block,
                       fp4_groups(q->k, q->block), static_cast<char*>(y), y_row * type_bytes(dtype));
   };
   W8A8_CUDA(dtype == W8A8_TYPE_BF16  ? go(fp4_dequantise_kernel<W8A8_TYPE_BF16>)

@@ -13,6 +13,16 @@ __device__ __forceinline__ uint32_t e2m1x2_of(float lo, float hi) {
   asm("{\n .reg .b8 t;\n cvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n cvt.u16.u8 %0, t;\n}\n" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// Four packed pairs -> eight codes, in order.
+__device__ __forceinline__ uint32_t e2m1x8_of(f32x2 a, f32x2 b, f32x2 c, f32x2 d) {
+  uint32_t r;
+  asm("{\n .reg .b8 p, q, r, s;\n .reg .f32 l, h;\n mov.b64 {l, h}, %1;\n cvt.rn.satfinite.e2m1x2.f32 p, h, l;\n"
+      " mov.b64 {l, h}, %2;\n cvt.rn.satfinite.e2m1x2.f32 q, h, l;\n mov.b64 {l, h}, %3;\n cvt.rn.satfinite.e2m1x2.f32 r, h, l;\n"
+      " mov.b64 {l, h}, %4;\n cvt.rn.satfinite.e2m1x2.f32 s, h, l;\n mov.b32 %0, {p, q, r, s};\n}\n"
+      : "=r"(r)
+      : "l"(a), "l"(b), "l"(c), "l"(d));
+  return r;
+}
 // Eight codes -> their values as four fp16 pairs, in order (exact).
 __device__ __forceinline__ void e2m1x8_to_f16(uint32_t w, uint32_t (&h)[4]) {
   asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
@@ -49,10 +59,10 @@ __device__ __forceinline__ int row_exponent(uint32_t top) {
 // one, and on a border only with it: a border b has few bits, and x (24 bits) over a scale of 4 bits, or m over 6, that
 // differs from b does so by more than half a unit in the last place of b (with f and g the significands of b and of
 // b times the divisor: by 2 g^-1 of that, relative to f^-1, and g < 2 f).
-// The quotient is a product with the reciprocal, corrected once by its exact residual (Markstein, Computation of elementary
-// functions on the IBM RISC System/6000, 1990): exact where the quotient is a border, within 2^-20 of a unit elsewhere.
+// The quotient is x hi + fl(x lo) with hi + lo the reciprocal to twice the bits: exact where the quotient is a border, within
+// 2^-20 of a unit in the last place of correctly rounded elsewhere.
 struct Block16 {
-  float scale, inv;
+  float scale, hi, lo;
   uint32_t byte;
   __device__ __forceinline__ void unit(uint32_t top_bits, float s2) {  // top_bits: of the block's largest magnitude
     if (top_bits >= 0x7f800000u) {
@@ -62,13 +72,12 @@ struct Block16 {
       byte = e4m3_of(__fdiv_rn(__uint_as_float(top_bits) * s2, 6.0f));
       scale = e4m3_value(byte);
     }
-    inv = scale > 0.0f ? __frcp_rn(scale) : 0.0f;
+    hi = scale > 0.0f ? __frcp_rn(scale) : 0.0f;
+    lo = fmaf(-scale, hi, 1.0f) * hi;
+    if (scale == 0.0f) lo = 0.0f;
   }
   // x s2 / scale (x already times s2)
-  __device__ __forceinline__ float over(float x) const {
-    const float q = x * inv;
-    return fmaf(fmaf(-q, scale, x), inv, q);
-  }
+  __device__ __forceinline__ float over(float x) const { return fmaf(x, hi, x * lo); }
 };
 
 // ------------------------------------------------------------------------------- matrices

@@ -18,6 +18,7 @@ namespace w8a8 {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 4;  // heads whose loads are in flight
 
 struct Turn {
   const uint64_t* turns;
@@ -113,7 +114,10 @@ __global__ void __launch_bounds__(kThreads)
            : h < n_q + cache.p.n_kv ? k + row64 * k_row + (int64_t)(h - n_q) * kDim
                                     : v + row64 * v_row + (int64_t)(h - n_q - cache.p.n_kv) * kDim;
   };
-  Raw<kE> next = *(reinterpret_cast<const Raw<kE>*>(source(h0)) + lane);  // (rows of no sequence are the caller's memory too)
+  Raw<kE> next[kAhead];  // the heads ahead (rows of no sequence are the caller's memory too)
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j)
+    if (h0 + j * step < heads) next[j] = *(reinterpret_cast<const Raw<kE>*>(source(h0 + j * step)) + lane);
   const int s = seq_of_row(batch, row);
   const SeqShape sq = seq_shape(batch, s, cache.p.page_shift);
   if (row < sq.row0 || row >= sq.row0 + sq.rows) return;
@@ -139,8 +143,10 @@ __global__ void __launch_bounds__(kThreads)
   }
 
   for (int h = h0; h < heads; h += step) {
-    const Raw<kE> raw = next;
-    if (h + step < heads) next = *(reinterpret_cast<const Raw<kE>*>(source(h + step)) + lane);
+    const Raw<kE> raw = next[0];
+#pragma unroll
+    for (int j = 0; j + 1 < kAhead; ++j) next[j] = next[j + 1];
+    if (h + kAhead * step < heads) next[kAhead - 1] = *(reinterpret_cast<const Raw<kE>*>(source(h + kAhead * step)) + lane);
     const bool is_q = h < n_q, is_v = h >= n_q + cache.p.n_kv;
     if (!is_q && code_at < 0) continue;
     float x[kE], y[kE], off[kE];  // as they come, turned, the bound on what y is off by
@@ -212,7 +218,7 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         g[e] = b.over(y[2 * i + e] * s2);
-        o[e] = off[2 * i + e] * s2 * b.inv;
+        o[e] = off[2 * i + e] * s2 * b.hi;
       }
       if (!nan) {
         w |= e2m1x2_of(g[0], g[1]) << (8 * i);
@@ -292,54 +298,47 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
-// A thread a block of 16 dims of (page, slot, head); blockIdx.y: keys or values.
+// A thread has eight dims of (page, slot, head), so that a warp's stores are contiguous; blockIdx.y: keys or values.
 template <int kType>
 __global__ void __launch_bounds__(kThreads) fp4_values_kernel(Fp4Pages c, const int32_t* __restrict__ pages, int64_t total,
-                                                              int blocks, void* k_out, void* v_out) {
+                                                              int eighths_shift, void* k_out, void* v_out) {
   pdl_wait();
   pdl_trigger();
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   const bool is_v = blockIdx.y == 1 || k_out == nullptr;
   char* out = static_cast<char*>(is_v ? v_out : k_out);
   if (i >= total) return;
-  const int d = (int)(i % blocks);
-  const int64_t r = i / blocks;
-  const int h = (int)(r % c.p.n_kv), slot = (int)((r / c.p.n_kv) & ((1 << c.p.page_shift) - 1));
-  const int64_t n = (r / c.p.n_kv) >> c.p.page_shift;
+  const int d = (int)i & ((1 << eighths_shift) - 1);
+  const int64_t r = i >> eighths_shift;
+  const int64_t rh = r < (1ll << 32) ? (int64_t)((uint32_t)r / (uint32_t)c.p.n_kv) : r / c.p.n_kv;  // page and slot
+  const int h = (int)(r - rh * c.p.n_kv), slot = (int)(rh & ((1 << c.p.page_shift) - 1));
+  const int64_t n = rh >> c.p.page_shift;
   const int64_t page = pages ? pages[n] : n;
-  uint2 w = make_uint2(0u, 0u);
+  uint32_t w = 0;
   float unit = 0.0f;
   if (page >= 0 && page < c.p.n_pages) {
-    w = *reinterpret_cast<const uint2*>((is_v ? c.v : c.k) + page * c.p.page_stride + slot * c.p.slot_stride +
-                                        h * c.p.head_stride + 8 * d);
-    unit = e4m3_value((is_v ? c.vs : c.ks)[page * c.s_page + slot * c.s_slot + h * c.s_head + d]) *
+    w = *reinterpret_cast<const uint32_t*>((is_v ? c.v : c.k) + page * c.p.page_stride + slot * c.p.slot_stride +
+                                           h * c.p.head_stride + 4 * d);
+    unit = e4m3_value((is_v ? c.vs : c.ks)[page * c.s_page + slot * c.s_slot + h * c.s_head + (d >> 1)]) *
            two_to(is_v ? c.v_exp : c.k_exp);
   }
-  uint32_t a[4], b[4];
-  e2m1x8_to_f16(w.x, a);
-  e2m1x8_to_f16(w.y, b);
-  float v[16];
+  uint32_t a[4];
+  e2m1x8_to_f16(w, a);
+  float v[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const float2 f = unpack2<false>(a[e]), g = unpack2<false>(b[e]);
+    const float2 f = unpack2<false>(a[e]);
     v[2 * e] = f.x * unit;
     v[2 * e + 1] = f.y * unit;
-    v[8 + 2 * e] = g.x * unit;
-    v[8 + 2 * e + 1] = g.y * unit;
   }
   if constexpr (kType == W8A8_TYPE_F32) {
-    uint4* to = reinterpret_cast<uint4*>(out + i * 64);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      to[e] = make_uint4(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), __float_as_uint(v[4 * e + 2]),
-                         __float_as_uint(v[4 * e + 3]));
+    uint4* to = reinterpret_cast<uint4*>(out + i * 32);
+    to[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    to[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
   } else {
     constexpr bool kBf = kType == W8A8_TYPE_BF16;
-    uint4* to = reinterpret_cast<uint4*>(out + i * 32);
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-      to[e] = make_uint4(pack2<kBf>(v[8 * e], v[8 * e + 1]), pack2<kBf>(v[8 * e + 2], v[8 * e + 3]),
-                         pack2<kBf>(v[8 * e + 4], v[8 * e + 5]), pack2<kBf>(v[8 * e + 6], v[8 * e + 7]));
+    *reinterpret_cast<uint4*>(out + i * 16) =
+        make_uint4(pack2<kBf>(v[0], v[1]), pack2<kBf>(v[2], v[3]), pack2<kBf>(v[4], v[5]), pack2<kBf>(v[6], v[7]));
   }
 }
 
@@ -403,7 +402,7 @@ extern "C" w8a8_status w8a8_fp4_rope_append(const w8a8_rope_table* rope, const w
   const Turn t{rope->turns, rope->scale, rope->rotary_dim, rope->interleaved};
   // few rows spread over their heads, many compute their angles once: about 16 warps an SM
   const int heads = n_q + 2 * pc.p.n_kv;
-  const int64_t want = (int64_t)d.sms * 16 / pb.n_rows;
+  const int64_t want = (int64_t)d.sms * 64 / pb.n_rows;
   const int step = (int)(want < 1 ? 1 : want > heads ? heads : want);
   const int64_t warps = (int64_t)pb.n_rows * step;
   const dim3 grid((unsigned)((warps * 32 + kThreads - 1) / kThreads));
@@ -435,12 +434,12 @@ extern "C" w8a8_status w8a8_fp4_paged_values(const w8a8_paged_cache_fp4* cache, 
   W8A8_CHECK_ARG(aligned16(k_out) && aligned16(v_out) && (reinterpret_cast<uintptr_t>(pages) & 3u) == 0, W8A8_ERR_ALIGN,
                  "%s: outputs must be 16-byte aligned, pages 4-byte", who);
   W8A8_TRY(check_device());
-  const int blocks = cache->head_dim / 16;
-  const int64_t total = ((int64_t)n << pc.p.page_shift) * pc.p.n_kv * blocks, grid = (total + kThreads - 1) / kThreads;
+  const int shift = cache->head_dim == 256 ? 5 : cache->head_dim == 128 ? 4 : 3;  // eight dims a thread
+  const int64_t total = (((int64_t)n << pc.p.page_shift) * pc.p.n_kv) << shift, grid = (total + kThreads - 1) / kThreads;
   W8A8_CHECK_ARG(grid <= 0x7fffffffll, W8A8_ERR_SHAPE, "%s: %d pages are too many for one call", who, n);
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)grid, k_out && v_out ? 2u : 1u), dim3(kThreads), 0, as_stream(stream), pc, pages,
-                      total, blocks, k_out, v_out);
+                      total, shift, k_out, v_out);
   };
   W8A8_CUDA(dtype == W8A8_TYPE_BF16  ? go(fp4_values_kernel<W8A8_TYPE_BF16>)
             : dtype == W8A8_TYPE_F16 ? go(fp4_values_kernel<W8A8_TYPE_F16>)
