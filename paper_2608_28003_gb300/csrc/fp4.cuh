@@ -65,13 +65,11 @@ struct Block16 {
   float scale, hi, lo;
   uint32_t byte;
   __device__ __forceinline__ void unit(uint32_t top_bits, float s2) {  // top_bits: of the block's largest magnitude
-    if (top_bits >= 0x7f800000u) {
-      byte = kE4m3NaN;
-      scale = 0.0f;
-    } else {
-      byte = e4m3_of(__fdiv_rn(__uint_as_float(top_bits) * s2, 6.0f));
-      scale = e4m3_value(byte);
-    }
+    byte = top_bits >= 0x7f800000u ? kE4m3NaN : e4m3_of(__fdiv_rn(__uint_as_float(top_bits) * s2, 6.0f));
+    of_byte();
+  }
+  __device__ __forceinline__ void of_byte() {
+    scale = byte == kE4m3NaN ? 0.0f : e4m3_value(byte);
     hi = scale > 0.0f ? __frcp_rn(scale) : 0.0f;
     lo = fmaf(-scale, hi, 1.0f) * hi;
     if (scale == 0.0f) lo = 0.0f;

@@ -1,9 +1,9 @@
 // A paged cache in 4 bits: the append of a projection's rows to it, and its pages' values.
 //
-// Append.  A warp takes a row and walks heads of it with a fixed step, so that the row's sines and cosines are computed once for all of
-// them; a lane holds 8, 4 or 2 neighbouring dims (head dim 256, 128, 64) and reaches the other dim of a pair by a shuffle.  A block of
-// 16 dims is 2, 4 or 8 lanes.  Little is moved (a key's 144 bytes at head dim 256), so latency bounds it: launch, sequence, length,
-// page, store.
+// Append.  Queries are turned by blocks of their own, as rope_append does it.  For keys and values a warp takes a row and walks its
+// heads with a fixed step, so that the row's sines and cosines are computed once for all of them; a lane holds 8, 4 or 2
+// neighbouring dims (head dim 256, 128, 64) and reaches the other dim of a pair by a shuffle.  A block of 16 dims is 2, 4 or 8
+// lanes.  Little is moved (a key's 144 bytes at head dim 256), so latency bounds it: launch, sequence, length, page, store.
 //
 // Codes are decided as in exact arithmetic: the rotation and the norm are computed in fp32 with a bound on what they are off by, and where
 // that leaves a code or a scale open (both ends of the bound are rounded and compared; a few heads in a thousand) the value is
@@ -12,19 +12,13 @@
 
 #include "fp4.cuh"
 #include "ops.cuh"
+#include "rope.cuh"
 
 namespace w8a8 {
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 4;  // heads whose loads are in flight
-
-struct Turn {
-  const uint64_t* turns;
-  float scale;
-  int rot, inter;
-};
 
 // What the fp32 values are off by, in units of 2^-24 of |x| + |its partner|: 3.6 for cos and sin (their argument to 2^-25 half
 // turns, 1 unit in the last place, the factor), 2 for the two products, and with a norm 11 (13 additions' halves, the square root, the
@@ -95,24 +89,78 @@ __device__ __forceinline__ void put_codes(uint8_t* codes, uint8_t* scales, uint3
   if (lane % (16 / kE) == 0) scales[lane / (16 / kE)] = (uint8_t)byte;
 }
 
+// A row's queries, by units of 16 dims as in rope_append: thread i of all.  Every lane of a warp makes the same number of trips, so
+// that the shuffles of the norm's sum are whole.
+template <bool kBf16, int kUnits>
+__device__ __forceinline__ void turn_queries(const RopeArgs& r, const PagedCache& c, const PagedBatch& batch, int64_t i,
+                                             const uint16_t* q, int64_t q_row, int n_q, const float* __restrict__ q_norm, float eps,
+                                             uint16_t* q_out, int64_t q_out_row, int step) {
+  const int unit = (int)(i % kUnits), h0 = (int)((i / kUnits) % step);
+  const int64_t row64 = i / kUnits / step;
+  const int row = (int)min(row64, (int64_t)batch.n_rows - 1), s = seq_of_row(batch, row);
+  const SeqShape q0 = seq_shape(batch, s, c.page_shift);
+  const bool live = row64 < batch.n_rows && row >= q0.row0 && row < q0.row0 + q0.rows;
+  bool rotated;
+  int at0, at1;
+  unit_place(r, unit, rotated, at0, at1);
+  float co[8], si[8], x[16];
+  const int trips = (n_q + step - 1) / step;
+  for (int t0 = 0; t0 < trips; t0 += kAhead) {
+    Unit u[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = h0 + (t0 + j) * step;
+      if (live && h < n_q) u[j] = unit_load(q + (int64_t)row * q_row + (int64_t)h * (16 * kUnits), at0, at1);
+    }
+    if (t0 == 0 && rotated && live) unit_angles(r, unit, q0.pos0 + (row - q0.row0), co, si);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int h = h0 + (t0 + j) * step;
+      if (t0 + j >= trips) break;
+      const bool work = live && h < n_q;
+      float ss = 0.0f;
+      if (work) {
+        unit_values<kBf16>(u[j], x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ss = fmaf(x[e], x[e], ss);
+      }
+      if (q_norm)
+#pragma unroll
+        for (int o = kUnits / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (!work) continue;
+      if (q_norm) {
+        const float inv = 1.0f / sqrtf(ss / (float)(16 * kUnits) + eps);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = x[e] * inv * q_norm[e < 8 ? at0 + e : at1 + e - 8];
+      }
+      if (rotated) unit_rotate(r.inter, co, si, x);
+      unit_store<kBf16>(q_out + (int64_t)row * q_out_row + (int64_t)h * (16 * kUnits), at0, at1, x);
+    }
+  }
+}
+
 template <bool kBf16, int kDim>
 __global__ void __launch_bounds__(kThreads)
-    fp4_append_kernel(Turn t, Fp4Pages cache, PagedBatch batch, const uint16_t* q, int64_t q_row, int n_q, const uint16_t* k,
+    fp4_append_kernel(RopeArgs t, Fp4Pages cache, PagedBatch batch, const uint16_t* q, int64_t q_row, int n_q, const uint16_t* k,
                       int64_t k_row, const uint16_t* v, int64_t v_row, const float* __restrict__ q_norm,
-                      const float* __restrict__ k_norm, float eps, uint16_t* q_out, int64_t q_out_row, int step) {
+                      const float* __restrict__ k_norm, float eps, uint16_t* q_out, int64_t q_out_row, int step, int q_step,
+                      unsigned kv_blocks) {
   constexpr int kE = kDim / 32, kLanes = 16 / kE;
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x >= kv_blocks) {
+    turn_queries<kBf16, kDim / 16>(t, cache.p, batch, (int64_t)(blockIdx.x - kv_blocks) * kThreads + threadIdx.x, q, q_row, n_q,
+                                   q_norm, eps, q_out, q_out_row, q_step);
+    return;
+  }
   const int lane = threadIdx.x & 31;
   const int64_t wid = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
   const int h0 = (int)(wid % step);
   const int64_t row64 = wid / step;
   if (row64 >= batch.n_rows) return;
-  const int row = (int)row64, heads = n_q + 2 * cache.p.n_kv;
+  const int row = (int)row64, n_kv = cache.p.n_kv, heads = 2 * n_kv;
   auto source = [&](int h) {
-    return h < n_q                  ? q + row64 * q_row + (int64_t)h * kDim
-           : h < n_q + cache.p.n_kv ? k + row64 * k_row + (int64_t)(h - n_q) * kDim
-                                    : v + row64 * v_row + (int64_t)(h - n_q - cache.p.n_kv) * kDim;
+    return h < n_kv ? k + row64 * k_row + (int64_t)h * kDim : v + row64 * v_row + (int64_t)(h - n_kv) * kDim;
   };
   Raw<kE> next[kAhead];  // the heads ahead (rows of no sequence are the caller's memory too)
 #pragma unroll
@@ -124,6 +172,7 @@ __global__ void __launch_bounds__(kThreads)
   const int pos = sq.pos0 + (row - sq.row0);
   int64_t scale_at = 0;
   const int64_t code_at = fp4_key_offset(batch, cache, s, pos, 0, scale_at);
+  if (code_at < 0) return;
 
   // this lane's angles: dim d of a pair with the other one `mate` lanes on (half layout) or beside it
   const int d0 = lane * kE, half = t.rot / 2;
@@ -147,11 +196,10 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int j = 0; j + 1 < kAhead; ++j) next[j] = next[j + 1];
     if (h + kAhead * step < heads) next[kAhead - 1] = *(reinterpret_cast<const Raw<kE>*>(source(h + kAhead * step)) + lane);
-    const bool is_q = h < n_q, is_v = h >= n_q + cache.p.n_kv;
-    if (!is_q && code_at < 0) continue;
+    const bool is_v = h >= n_kv;
     float x[kE], y[kE], off[kE];  // as they come, turned, the bound on what y is off by
     raw_floats<kBf16, kE>(raw, x);
-    const float* nw = is_v ? nullptr : is_q ? q_norm : k_norm;
+    const float* nw = is_v ? nullptr : k_norm;
     if (!is_v) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) y[e] = x[e];
@@ -183,16 +231,7 @@ __global__ void __launch_bounds__(kThreads)
         off[e] = 0.0f;
       }
     }
-    if (is_q) {
-      Raw<kE> out;
-      uint32_t* w = reinterpret_cast<uint32_t*>(&out);
-#pragma unroll
-      for (int i = 0; i < kE / 2; ++i) w[i] = pack2<kBf16>(y[2 * i], y[2 * i + 1]);
-      *(reinterpret_cast<Raw<kE>*>(q_out + row64 * q_out_row + (int64_t)h * kDim) + lane) = out;
-      continue;
-    }
-
-    const int kv_head = is_v ? h - n_q - cache.p.n_kv : h - n_q, exponent = is_v ? cache.v_exp : cache.k_exp;
+    const int kv_head = is_v ? h - n_kv : h, exponent = is_v ? cache.v_exp : cache.k_exp;
     const float s2 = two_to(-exponent);
     float top = 0.0f, wide = 0.0f;
     bool finite = true;
@@ -212,26 +251,30 @@ __global__ void __launch_bounds__(kThreads)
     if (!nan && wide > 0.0f)
       open_unit = e4m3_of(__fdiv_rn((top - wide) * s2, 6.0f)) != e4m3_of(__fdiv_rn((top + wide) * s2, 6.0f));
     uint32_t w = 0;
+    auto encode = [&] {
+      w = 0;
 #pragma unroll
-    for (int i = 0; i < kE / 2; ++i) {
-      float g[2], o[2];
+      for (int i = 0; i < kE / 2; ++i) {
+        float g[2], o[2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        g[e] = b.over(y[2 * i + e] * s2);
-        o[e] = off[2 * i + e] * s2 * b.hi;
+        for (int e = 0; e < 2; ++e) {
+          g[e] = b.over(y[2 * i + e] * s2);
+          o[e] = off[2 * i + e] * s2 * b.hi;
+        }
+        if (!nan) {
+          w |= e2m1x2_of(g[0], g[1]) << (8 * i);
+          const uint32_t apart = e2m1x2_of(g[0] - o[0], g[1] - o[1]) ^ e2m1x2_of(g[0] + o[0], g[1] + o[1]);
+          open[2 * i] = (apart & 15u) != 0;
+          open[2 * i + 1] = (apart >> 4) != 0;
+        }
       }
-      if (!nan) {
-        w |= e2m1x2_of(g[0], g[1]) << (8 * i);
-        const uint32_t apart = e2m1x2_of(g[0] - o[0], g[1] - o[1]) ^ e2m1x2_of(g[0] + o[0], g[1] + o[1]);
-        open[2 * i] = open_unit || (apart & 15u) != 0;
-        open[2 * i + 1] = open_unit || (apart >> 4) != 0;
-      }
-    }
-    bool any = false;
+    };
+    encode();
+    bool any = open_unit;
 #pragma unroll
     for (int e = 0; e < kE; ++e) any = any || open[e];
     if (__any_sync(0xffffffffu, any) && !is_v) {
-      // ---- 64 bits
+      // ---- 64 bits: a key's dim e of this lane (all lanes take part in the exchange; `mine`: those that want it)
       double inv = 1.0;
       if (nw) {
         double ss = 0.0;
@@ -241,12 +284,10 @@ __global__ void __launch_bounds__(kThreads)
         for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         inv = 1.0 / sqrt(ss / kDim + (double)eps);
       }
-      double top64 = 0.0;
-      const bool redo = __any_sync(0xffffffffu, open_unit);
-      double unit = (double)b.scale / (double)s2;
-      // first the blocks whose scale is open, then the codes
+      double top64 = 0.0, unit = (double)b.scale / (double)s2;
+      // first the scales that are open, for which the dims that can be their blocks' largest are looked at; then the codes that are
 #pragma unroll 1
-      for (int pass = redo ? 0 : 1; pass < 2; ++pass) {
+      for (int pass = __any_sync(0xffffffffu, open_unit) ? 0 : 1; pass < 2; ++pass) {
 #pragma unroll 1
         for (int e = 0; e < kE; ++e) {
           float xe = 0.0f, we = 1.0f, pe = 0.0f, wp = 1.0f;
@@ -256,11 +297,11 @@ __global__ void __launch_bounds__(kThreads)
             if (j == e) {
               xe = x[j];
               pe = t.inter ? x[j ^ 1] : 0.0f;
-              mine = open[j];
+              mine = pass == 0 ? open_unit && fabsf(y[j]) + off[j] >= top - wide : open[j];
             }
           const float other = __shfl_sync(0xffffffffu, xe, mate);
           if (!t.inter) pe = other;
-          if (pass == 0 ? !open_unit : !mine) continue;
+          if (!mine) continue;
           if (nw) {
             we = nw[d0 + e];
             wp = t.inter ? nw[d0 + (e ^ 1)] : nw[mate * kE + e];
@@ -286,9 +327,11 @@ __global__ void __launch_bounds__(kThreads)
           for (int o = kLanes / 2; o > 0; o >>= 1) top64 = fmax(top64, __shfl_xor_sync(0xffffffffu, top64, o));
           if (open_unit) {
             b.byte = e4m3_of_double(top64 * (double)s2 / 6.0);
-            b.scale = e4m3_value(b.byte);
+            b.of_byte();
             unit = (double)b.scale / (double)s2;
+            encode();
           }
+          __syncwarp();
         }
       }
     }
@@ -399,16 +442,18 @@ extern "C" w8a8_status w8a8_fp4_rope_append(const w8a8_rope_table* rope, const w
   if (pb.n_seqs == 0 || pb.n_rows == 0) return W8A8_OK;
   DevInfo d;
   W8A8_TRY(dev_info(&d));
-  const Turn t{rope->turns, rope->scale, rope->rotary_dim, rope->interleaved};
-  // few rows spread over their heads, many compute their angles once: about 16 warps an SM
-  const int heads = n_q + 2 * pc.p.n_kv;
-  const int64_t want = (int64_t)d.sms * 64 / pb.n_rows;
-  const int step = (int)(want < 1 ? 1 : want > heads ? heads : want);
-  const int64_t warps = (int64_t)pb.n_rows * step;
-  const dim3 grid((unsigned)((warps * 32 + kThreads - 1) / kThreads));
+  const RopeArgs t{rope->turns, rope->scale, rope->rotary_dim, rope->interleaved};
+  // few rows spread over their heads, many compute their angles once: up to 32 warps an SM
+  const int64_t want = (int64_t)d.sms * 32 / pb.n_rows;
+  const int step = (int)(want < 1 ? 1 : want > 2 * pc.p.n_kv ? 2 * pc.p.n_kv : want), units = dim / 16;
+  const int q_step = head_step(pb.n_rows, units, n_q, d.sms);
+  const int64_t kv_blocks = ((int64_t)pb.n_rows * step * 32 + kThreads - 1) / kThreads;
+  const int64_t q_blocks = ((int64_t)pb.n_rows * units * q_step + kThreads - 1) / kThreads;
+  W8A8_CHECK_ARG(kv_blocks + q_blocks <= 0x7fffffffll, W8A8_ERR_SHAPE, "%s: n_rows=%d is too large", who, pb.n_rows);
+  const dim3 grid((unsigned)(kv_blocks + q_blocks));
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, grid, dim3(kThreads), 0, as_stream(stream), t, pc, pb, q, q_row, n_q, k, k_row, v, v_row, q_norm,
-                      k_norm, eps, q_out, q_out_row, step);
+                      k_norm, eps, q_out, q_out_row, step, q_step, (unsigned)kv_blocks);
   };
   W8A8_CUDA(dtype == W8A8_TYPE_BF16 ? (dim == 256   ? go(fp4_append_kernel<true, 256>)
                                        : dim == 128 ? go(fp4_append_kernel<true, 128>)
