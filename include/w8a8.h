@@ -615,12 +615,12 @@ w8a8_status w8a8_decoder_step_paged(w8a8_model* m, const int32_t* tokens, const 
  * does not count for row_scale.
  * ====================================================================================== */
 typedef struct {
-  int32_t rows, k;  /* k a multiple of 32, at most W8A8_MAX_K */
+  int32_t rows, k;  /* rows at most 2^31 - 128; k a multiple of 32, at most W8A8_MAX_K */
   int32_t block;    /* 16 or 32 */
   uint8_t* codes;   /* [rows, k / 2] */
   uint8_t* scales;  /* w8a8_fp4_scale_bytes: block j of row r at byte ((r / 128) * G + j / 4) * 512 + (r % 32) * 16 +
                        (r / 32) % 4 * 4 + j % 4, G = ceil(k / block / 4), the order the tensor cores read them in; bytes of no
-                       row or block are 0 */
+                       row or block are 0, and so is a scale's bit 7 at block 16 */
   float* row_scale; /* [rows] (block 16; NULL at block 32).  A weight's may hold any finite value */
 } w8a8_fp4;
 
@@ -658,7 +658,8 @@ typedef struct {
 
 /* w8a8_rope_append into a 4-bit cache: the keys after norm and rotation and the values as they come are quantised by blocks of
  * 16 dims with row_scale = 2^k_exp (2^v_exp); a block above 2688 times that is cut off at it.  The keys' codes are those of the
- * formula in exact arithmetic, not of a rounded key.  dtype: of q, k, v and q_out, bf16 or fp16; q as in w8a8_rope_append. */
+ * formula in exact arithmetic, not of a rounded key.  dtype: of q, k, v and q_out, bf16 or fp16; q as in w8a8_rope_append.
+ * Rows that share a slot leave some row's codes in each 4 bytes of it (2 at head_dim 128, 1 at 64) and some row's scales. */
 w8a8_status w8a8_fp4_rope_append(const w8a8_rope_table* rope, const w8a8_paged_cache_fp4* cache,
                                  const w8a8_paged_batch* batch, int dtype, const uint16_t* q, int64_t q_row, int n_q,
                                  const uint16_t* k, int64_t k_row, const uint16_t* v, int64_t v_row, const float* q_norm,

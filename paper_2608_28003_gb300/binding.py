@@ -790,13 +790,15 @@ class Fp4Tensor:
 
 def fp4_tensor(codes: torch.Tensor, block_scales: torch.Tensor, row_scale: Optional[torch.Tensor] = None) -> Fp4Tensor:
     """An Fp4Tensor of a matrix quantised elsewhere: codes uint8 [rows, k / 2], scale bytes uint8 [rows, k / 16] (e4m3) or
-    [rows, k / 32] (e8m0); row_scale fp32 [rows], 1 where it is not given (one scale for all rows: expanded)."""
+    [rows, k / 32] (e8m0); row_scale fp32 [rows], 1 where it is not given (one scale for all rows: expanded).  An e4m3 scale has
+    no sign: the tensor cores read seven bits of it, so a byte above 127 is refused (which reads the bytes back)."""
     _need(codes.dim() == 2 and block_scales.dim() == 2 and codes.shape[0] == block_scales.shape[0] and
           codes.dtype == block_scales.dtype == torch.uint8, "codes [rows, k / 2] and block_scales [rows, k / block], uint8")
     n, half = codes.shape
     cols = block_scales.shape[1]
     _need(half % 16 == 0 and (8 * cols == half or 16 * cols == half), "k must be a multiple of 32, blocks of 16 or 32")
     block, g = 2 * half // cols, -(-cols // 4)
+    _need(block == 32 or not bool((block_scales > 127).any()), "a scale of a block of 16 has no sign")
     t = torch.zeros(-(-n // 128) * 128, 4 * g, dtype=torch.uint8, device=codes.device)
     t[:n, :cols] = block_scales
     t = t.view(-1, 4, 32, g, 4).permute(0, 3, 2, 1, 4).reshape(-1)

@@ -84,6 +84,7 @@ __host__ __device__ __forceinline__ size_t fp4_scale_at(int64_t r, int j, int gr
   return ((size_t)(r >> 7) * groups + (j >> 2)) * 512 + (size_t)(r & 31) * 16 + (size_t)((r >> 5) & 3) * 4 + (j & 3);
 }
 __host__ __device__ __forceinline__ int fp4_groups(int k, int block) { return (k / block + 3) / 4; }
+constexpr int kMaxFp4Rows = 0x7fffff80;  // whole 128-row blocks of scales stay within an int
 w8a8_status check_fp4(const char* who, const w8a8_fp4* q);
 // (no argument checks).  pad: rows beyond q.rows, up to a multiple of 128, get scales of 0 as well.
 w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, bool settled,

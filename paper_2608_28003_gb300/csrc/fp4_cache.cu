@@ -6,8 +6,8 @@
 // lanes.  Little is moved (a key's 144 bytes at head dim 256), so latency bounds it: launch, sequence, length, page, store.
 //
 // Codes are decided as in exact arithmetic: the rotation and the norm are computed in fp32 with a bound on what they are off by, and where
-// that leaves a code or a scale open (both ends of the bound are rounded and compared; a few heads in a thousand) the value is
-// computed again in 64 bits.
+// that leaves a code or a scale open (both ends of the bound are rounded and compared; a few heads in a thousand), or fp32's range does not
+// hold the norm or the rotation, the value is computed again in 64 bits.
 #include <cmath>
 
 #include "fp4.cuh"
@@ -71,12 +71,6 @@ __device__ __forceinline__ float block_max(float x) {
   for (int o = kLanes / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
   return x;
 }
-template <int kLanes>
-__device__ __forceinline__ bool block_any(bool x, int lane) {
-  const uint32_t all = __ballot_sync(0xffffffffu, x);
-  return (all >> (lane & ~(kLanes - 1)) & ((1u << kLanes) - 1u)) != 0;
-}
-
 // Codes to their place, kE / 2 bytes a lane, and the scale by the block's first lane.
 template <int kE>
 __device__ __forceinline__ void put_codes(uint8_t* codes, uint8_t* scales, uint32_t w, uint32_t byte, int lane) {
@@ -200,6 +194,7 @@ __global__ void __launch_bounds__(kThreads)
     float x[kE], y[kE], off[kE];  // as they come, turned, the bound on what y is off by
     raw_floats<kBf16, kE>(raw, x);
     const float* nw = is_v ? nullptr : k_norm;
+    bool far = false;  // the sum of squares left fp32's range
     if (!is_v) {
 #pragma unroll
       for (int e = 0; e < kE; ++e) y[e] = x[e];
@@ -209,6 +204,7 @@ __global__ void __launch_bounds__(kThreads)
         for (int e = 0; e < kE; ++e) ss = fmaf(x[e], x[e], ss);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        far = ss > 0x1p120f || (ss < 0x1p-80f && eps < 0x1p-60f);
         const float inv = 1.0f / sqrtf(ss / (float)kDim + eps);
 #pragma unroll
         for (int e = 0; e < kE; ++e) y[e] = x[e] * inv * nw[d0 + e];
@@ -231,19 +227,72 @@ __global__ void __launch_bounds__(kThreads)
         off[e] = 0.0f;
       }
     }
+    // A key's dim e of this lane in 64 bits (all lanes take part in the exchange; `mine`: those that want it).
+    auto exact_norm = [&] {
+      double ss = 0.0;
+#pragma unroll 1
+      for (int e = 0; e < kE; ++e) ss += (double)x[e] * (double)x[e];
+#pragma unroll 1
+      for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      return 1.0 / sqrt(ss / kDim + (double)eps);
+    };
+    auto exact = [&](int e, double inv, bool mine) {
+      float xe = 0.0f, we = 1.0f, pe = 0.0f, wp = 1.0f;
+#pragma unroll
+      for (int j = 0; j < kE; ++j)
+        if (j == e) {
+          xe = x[j];
+          pe = t.inter ? x[j ^ 1] : 0.0f;
+        }
+      const float other = __shfl_sync(0xffffffffu, xe, mate);
+      if (!t.inter) pe = other;
+      if (!mine) return 0.0;
+      if (nw) {
+        we = nw[d0 + e];
+        wp = t.inter ? nw[d0 + (e ^ 1)] : nw[mate * kE + e];
+      }
+      double z = (double)xe * inv * (double)we;
+      if (turned) {
+        const uint64_t turn = (uint64_t)(int64_t)pos * t.turns[pair_of(e)];
+        double cd, sd;
+        sincospi((double)(int64_t)turn * 0x1p-63, &sd, &cd);
+        const double zp = (double)pe * inv * (double)wp;
+        z = (z * cd + (minus(e) ? -zp : zp) * sd) * (double)t.scale;
+      }
+      return z;
+    };
     const int kv_head = is_v ? h - n_kv : h, exponent = is_v ? cache.v_exp : cache.k_exp;
     const float s2 = two_to(-exponent);
-    float top = 0.0f, wide = 0.0f;
     bool finite = true;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) finite = finite && fabsf(y[e]) < INFINITY;
+    uint32_t unsound = __ballot_sync(0xffffffffu, !finite || far);
+    if (unsound != 0 && !is_v) {  // fp32 left its range: the key in 64 bits, what is beyond fp32 at its end (far above the cut-off)
+      const double inv = nw ? exact_norm() : 1.0;
+      finite = true;
+#pragma unroll 1
+      for (int e = 0; e < kE; ++e) {
+        const double z = exact(e, inv, true);
+        finite = finite && fabs(z) < (double)INFINITY;
+        const float f = (float)fmax(fmin(z, 0x1.fffffep127), -0x1.fffffep127);
+#pragma unroll
+        for (int j = 0; j < kE; ++j)
+          if (j == e) {
+            y[j] = f;
+            off[j] = 0x1p-23f * fabsf(f);
+          }
+      }
+      unsound = __ballot_sync(0xffffffffu, !finite);
+    }
+    const bool nan = (unsound >> (lane & ~(kLanes - 1)) & ((1u << kLanes) - 1u)) != 0;
+    float top = 0.0f, wide = 0.0f;
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       top = fmaxf(top, fabsf(y[e]));
       wide = fmaxf(wide, off[e]);
-      finite = finite && fabsf(y[e]) < INFINITY;
     }
     top = block_max<kLanes>(top);
     wide = block_max<kLanes>(wide);
-    const bool nan = block_any<kLanes>(!finite, lane);
     Block16 b;
     b.unit(__float_as_uint(nan ? INFINITY : top), s2);
     // both ends of the bound
@@ -258,7 +307,8 @@ __global__ void __launch_bounds__(kThreads)
         float g[2], o[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          g[e] = b.over(y[2 * i + e] * s2);
+          // (what is beyond the cut-off is 6 of any unit, but an infinite product has no quotient)
+          g[e] = b.over(fminf(fmaxf(y[2 * i + e] * s2, -0x1p20f), 0x1p20f));
           o[e] = off[2 * i + e] * s2 * b.hi;
         }
         if (!nan) {
@@ -274,46 +324,19 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int e = 0; e < kE; ++e) any = any || open[e];
     if (__any_sync(0xffffffffu, any) && !is_v) {
-      // ---- 64 bits: a key's dim e of this lane (all lanes take part in the exchange; `mine`: those that want it)
-      double inv = 1.0;
-      if (nw) {
-        double ss = 0.0;
-#pragma unroll 1
-        for (int e = 0; e < kE; ++e) ss += (double)x[e] * (double)x[e];
-#pragma unroll 1
-        for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        inv = 1.0 / sqrt(ss / kDim + (double)eps);
-      }
+      const double inv = nw ? exact_norm() : 1.0;
       double top64 = 0.0, unit = (double)b.scale / (double)s2;
       // first the scales that are open, for which the dims that can be their blocks' largest are looked at; then the codes that are
 #pragma unroll 1
       for (int pass = __any_sync(0xffffffffu, open_unit) ? 0 : 1; pass < 2; ++pass) {
 #pragma unroll 1
         for (int e = 0; e < kE; ++e) {
-          float xe = 0.0f, we = 1.0f, pe = 0.0f, wp = 1.0f;
           bool mine = false;
 #pragma unroll
           for (int j = 0; j < kE; ++j)
-            if (j == e) {
-              xe = x[j];
-              pe = t.inter ? x[j ^ 1] : 0.0f;
-              mine = pass == 0 ? open_unit && fabsf(y[j]) + off[j] >= top - wide : open[j];
-            }
-          const float other = __shfl_sync(0xffffffffu, xe, mate);
-          if (!t.inter) pe = other;
+            if (j == e) mine = pass == 0 ? open_unit && fabsf(y[j]) + off[j] >= top - wide : open[j];
+          const double z = exact(e, inv, mine);
           if (!mine) continue;
-          if (nw) {
-            we = nw[d0 + e];
-            wp = t.inter ? nw[d0 + (e ^ 1)] : nw[mate * kE + e];
-          }
-          double z = (double)xe * inv * (double)we;
-          if (turned) {
-            const uint64_t turn = (uint64_t)(int64_t)pos * t.turns[pair_of(e)];
-            double cd, sd;
-            sincospi((double)(int64_t)turn * 0x1p-63, &sd, &cd);
-            const double zp = (double)pe * inv * (double)wp;
-            z = (z * cd + (minus(e) ? -zp : zp) * sd) * (double)t.scale;
-          }
           if (pass == 0) {
             top64 = fmax(top64, fabs(z));
           } else {

@@ -148,7 +148,6 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
   auto acc_full = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::kStages + i); };
   auto acc_free = [&](int i) { return bar0 + 8u * (uint32_t)(2 * C::kStages + 2 + i); };
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_trigger();
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kStages; ++i) {
       mbar_init(full(i), 1);
@@ -172,6 +171,7 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_trigger();  // after the allocation: a kernel behind this one that wants tensor memory too comes second
   const uint32_t tmem = tmem_slot;
 
   const int split = a.split, rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
@@ -566,7 +566,7 @@ extern "C" w8a8_status w8a8_fp4_linear_workspace_size(int M, int N, int K, int b
   const char* who = "w8a8_fp4_linear_workspace_size";
   W8A8_CHECK_ARG(bytes != nullptr && (block == 16 || block == 32), W8A8_ERR_INVALID_ARG, "%s: null pointer, or block %d", who,
                  block);
-  W8A8_CHECK_ARG(M >= 0 && N >= 0 && K > 0 && K % 32 == 0 && K <= W8A8_MAX_K, W8A8_ERR_SHAPE, "%s: M=%d N=%d K=%d", who, M, N,
+  W8A8_CHECK_ARG(M >= 0 && M <= kMaxFp4Rows && N >= 0 && N <= kMaxFp4Rows && K > 0 && K % 32 == 0 && K <= W8A8_MAX_K, W8A8_ERR_SHAPE, "%s: M=%d N=%d K=%d", who, M, N,
                  K);
   *bytes = linear_fp4_ws(M, K, block).total;
   return W8A8_OK;
@@ -577,6 +577,7 @@ extern "C" w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void*
   const char* who = "w8a8_fp4_linear";
   W8A8_TRY(check_fp4(who, w));
   W8A8_CHECK_ARG(M >= 0, W8A8_ERR_INVALID_ARG, "%s: M=%d is negative", who, M);
+  W8A8_CHECK_ARG(M <= kMaxFp4Rows, W8A8_ERR_SHAPE, "%s: M=%d is too large", who, M);
   W8A8_CHECK_ARG(dtype >= W8A8_TYPE_BF16 && dtype <= W8A8_TYPE_F32 && out_dtype >= W8A8_TYPE_BF16 &&
                      out_dtype <= W8A8_TYPE_F32,
                  W8A8_ERR_INVALID_ARG, "%s: types %d, %d", who, dtype, out_dtype);

@@ -95,7 +95,7 @@ def _q(B, rows=4, k=64, block=16, codes=0x1000, scales=0x2000, row_scale=0x3000)
 
 
 @pytest.mark.parametrize("kw,want", [
-    (dict(block=8), 1), (dict(k=48), 2), (dict(k=0), 2), (dict(k=65568), 2), (dict(rows=-1), 2), (dict(codes=None), 1),
+    (dict(block=8), 1), (dict(k=48), 2), (dict(k=0), 2), (dict(k=65568), 2), (dict(rows=-1), 2), (dict(rows=2 ** 31 - 1), 2), (dict(codes=None), 1),
     (dict(scales=None), 1), (dict(row_scale=None), 1), (dict(codes=0x1008), 3), (dict(scales=0x2004), 3),
     (dict(row_scale=0x3004), 3)])
 def test_matrix_refusals(B, kw, want):
@@ -104,6 +104,13 @@ def test_matrix_refusals(B, kw, want):
     assert L.w8a8_fp4_dequantize(ctypes.byref(q), 0, P, 65600, None) == want
     assert L.w8a8_fp4_linear(ctypes.byref(q), 0, P, 65600, 3, None, 0, P, 64, P, 1 << 30, None) == want
     assert L.w8a8_last_error()
+
+
+def test_signed_scales_are_refused(B):
+    codes, plain = torch.zeros(3, 32, dtype=torch.uint8), torch.full((3, 4), 130, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="no sign"):
+        B.fp4_tensor(codes, plain)
+    assert B.fp4_tensor(codes, plain[:, :2]).block == 32  # there all of the byte is the exponent
 
 
 def test_call_refusals(B):

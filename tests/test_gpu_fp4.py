@@ -219,6 +219,26 @@ def test_linear_weight_quantised_elsewhere(B):
         _check_linear(B.fp4_linear(w, x, dtype=torch.float32), xv, wv, None, k)
 
 
+@pytest.mark.parametrize("m", [4, 150])
+def test_linear_scales_at_their_ends(B, m):
+    """Powers of two from 2^-127 to 2^127 as scales: blocks of zeros under the largest add nothing, large ones meet small rows."""
+    n, k = 130, 160
+    codes = torch.randint(0, 256, (n, k // 2), device="cuda", generator=_gen(1), dtype=torch.int32).to(torch.uint8)
+    scales = torch.full((n, k // 32), 127, dtype=torch.uint8, device="cuda")
+    scales[:, 0], scales[:, 1], scales[:, 2], scales[:, 3] = 254, 254, 0, 1
+    codes[:, :16] = 0x80  # 0 and -0
+    x = torch.randn(m, k, device="cuda", generator=_gen(2))
+    x[:, 32:64] *= 2.0 ** -120   # under 2^127
+    x[:, 64:128] *= 2.0 ** 120   # under 2^-127 and 2^-126
+    xq = B.fp4_quantize(x.bfloat16(), 32)
+    w = B.fp4_tensor(codes, scales)
+    xv = _np(B.fp4_dequantize(xq, torch.float32))
+    wv = O4.dequantise(O4.unpack(codes.cpu().numpy()), scales.cpu().numpy(), None, 32)
+    with np.errstate(over="ignore"):  # 4 and 6 times 2^127 are beyond fp32: rounded, infinite
+        np.testing.assert_array_equal(_np(B.fp4_dequantize(w, torch.float32)), wv.astype(np.float32))
+    _check_linear(B.fp4_linear(w, x.bfloat16(), dtype=torch.float32), xv, wv, None, k)
+
+
 def test_linear_views_and_refusals(B):
     w = B.fp4_quantize(torch.randn(72, 64, device="cuda", generator=_gen(1)).bfloat16())
     wide = torch.randn(9, 3, 128, device="cuda", generator=_gen(2)).bfloat16()

@@ -167,6 +167,35 @@ def test_append_borders(B):
         np.testing.assert_array_equal(O4.values_of(got), O4.values_of(c))
 
 
+@pytest.mark.parametrize("dim,rot,inter", [(256, 256, False), (128, 64, True), (64, 32, False)])
+def test_append_beyond_the_range_of_fp32(B, dim, rot, inter):
+    """Norms whose sum of squares fp32 does not hold (above it, and below it without an eps), and rotations that leave it."""
+    table = B.rope_table(B.RopeConfig(rot, interleaved=inter))
+    f, s = OS.rope_frequencies(rot, 1e4)
+    qn = (1 + 0.3 * torch.randn(dim, device="cuda", generator=_gen(1)))
+    for scale, norm, eps, exps in ((1e30, qn, 1e-5, (0, 0)), (1e-30, qn, 0.0, (-1, 0)), (0.8e38, None, 1e-5, (100, 99)),
+                                   (0.8e38, None, 1e-5, (-100, -90)), (1e-30, qn, 1e-5, (-80, -90))):
+        b = fp4_batch([7, 1], [90, 60], 16, 2, dim, 5, exps=exps)
+        cache, batch = objects(B, b)
+        x = (torch.randn(8, 5, dim, device="cuda", generator=_gen(2)).clamp(-4, 4) * scale).bfloat16()
+        x[3, 1, 5], x[4, 2, 7], x[5, 2] = float("inf"), float("nan"), 0.0
+        want = {n: b[n].cpu().numpy().copy() for n in ("k4", "v4", "ks", "vs")}
+        B.fp4_rope_append(table, cache, batch, x[:, :1], x[:, 1:3], x[:, 3:], k_norm=norm, eps=eps)
+        eps = float(np.float32(eps))
+        for r, seq, pos, _ in OS.rows_of(b, 16):
+            at = OS.place(b, b["k"].shape[0], 16, seq, pos)
+            with np.errstate(all="ignore"):
+                k = _np(x[r:r + 1, 1:3])
+                k = OS.rope(k if norm is None else OS.rms_norm(k, _np(norm), eps), [pos], f, s, inter)[0]
+                for name, y, e in (("k", k, exps[0]), ("v", _np(x[r, 3:]), exps[1])):
+                    c, sc = O4.cache_quantise(y, e)
+                    want[name + "4"][at], want[name + "s"][at] = O4.pack(c), sc
+        for n in ("ks", "vs"):
+            np.testing.assert_array_equal(b[n].cpu().numpy(), want[n])
+        for n in ("k4", "v4"):
+            np.testing.assert_array_equal(O4.values_of(O4.unpack(b[n].cpu().numpy())), O4.values_of(O4.unpack(want[n])))
+
+
 def test_append_leaves_bad_pages_alone(B):
     b = fp4_batch([2, 3, 1], [40, 2, 9], 16, 2, 64, 3)
     b["pages"][0, 2] = b["k"].shape[0]
