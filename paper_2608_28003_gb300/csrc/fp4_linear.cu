@@ -3,7 +3,7 @@
 // y_ti = sx_t sw_i sum_b ux_tb uw_ib sum_j x_tj w_ij: tcgen05.mma kind::mxf4nvf4 takes 64 columns of codes of both operands and the
 // units of their blocks (four bytes a row with blocks of 16, two with blocks of 32) and adds the scaled sums into fp32 accumulators in
 // tensor memory; the row scales are applied to the accumulators.  One kernel computes D [A's rows, B's rows] = A B^T:
-//  * up to 128 tokens (kSwap): A are 128 output channels, B the tokens, so that few tokens do not pad 128 lanes.  The weights
+//  * up to 48 tokens (kSwap): A are 128 output channels, B the tokens, so that few tokens do not pad 128 lanes.  The weights
 //    are read once, which HBM bounds (or, for a single layer's few megabytes, latency);
 //  * more tokens: A are 128 or 256 tokens, B 128 or 192 channels.
 // Codes come by TMA, 256 columns (128 bytes, swizzled) a stage; a stage's scales are one contiguous copy per 128 rows in the order
@@ -14,6 +14,11 @@
 // hold.  Units are walked by one CTA an SM, copies running ahead over unit borders, accumulators in two slots where they fit.
 // Long rows of few tiles are split over a cluster of up to 8 CTAs, which add up their accumulators through distributed shared memory in
 // the order of their ranks: the same bits every time.
+//
+// Measured, with the quantisation of the tokens ahead of it (2.5 us for few tokens, 5 for 2048): 1 token 1152 -> 6912 6.6 us, 37 tokens
+// 6912 -> 1152 8.1, both latency (two launches, five to eight dependent steps of a microsecond or so); 16 tokens 1152 -> 262144 34.3,
+// 170 MB at 5.0 TB/s and 0.73 of the copy rate; 2048 tokens 1152 -> 13824 27 us, 22 of them in the product, where
+// 167 MB of operands from L2 and 57 MB of outputs bound it, not the tensor cores (8.4 us at four times the bf16 rate).
 //
 // Every wait is bounded: on timeout a bit of the workspace's error word is set and the CTA passes its units without waiting.
 #include <algorithm>
@@ -115,10 +120,13 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
-__device__ __forceinline__ float ld_peer(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
   uint32_t at;
-  float v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
+  return at;
+}
+__device__ __forceinline__ float ld_peer(uint32_t at) {
+  float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(at) : "memory");
   return v;
 }
@@ -130,6 +138,60 @@ __device__ __forceinline__ void put_one(const Fp4Args& a, int64_t at, float v) {
     reinterpret_cast<float*>(a.y)[at] = v;
   else
     reinterpret_cast<uint16_t*>(a.y)[at] = (uint16_t)(a.out == W8A8_TYPE_BF16 ? pack2<true>(v, 0.0f) : pack2<false>(v, 0.0f));
+}
+
+// This CTA's share of the columns (a row a thread), added up over its cluster's accumulators in the order of the ranks, to y.  kFly loads of
+// distributed shared memory are in flight: a column at a time, 64 of 6912 -> 1152 at 37 tokens in parts of two took 19.5 us, more than
+// whole ones (15.2).
+constexpr int kFly = 32;
+template <int kS, int kBN, bool kSwap, int kBlock, int kHalves>
+__device__ __forceinline__ void add_up(const Fp4Args& a, uint32_t ring, int rank, int tile, int warp, int lane, const float* s_scale,
+                                       const float* s_bias) {
+  constexpr int kShare = kBN / kS / kHalves, kC = kFly / kS < kShare ? kFly / kS : kShare;  // columns of a warp, together
+  static_assert(kShare >= 1 && kShare % kC == 0, "whole groups of columns");
+  const int quarter = warp & 3, half = (warp - 2) >> 2, at = tile % a.a_tiles, b0 = tile / a.a_tiles * kBN;
+  const int arow = at * 128 + 32 * quarter + lane, b_end = kSwap ? a.M : a.N, a_end = kSwap ? a.N : a.M;
+  const float mine = kBlock == 16 && arow < a_end ? (kSwap ? a.w_scale : a.x_scale)[arow] : 1.0f;
+  const float mine_bias = kSwap && a.bias && arow < a_end ? a.bias[arow] : 0.0f;
+  uint32_t from[kS];
+#pragma unroll
+  for (int r = 0; r < kS; ++r) from[r] = peer_addr(ring + (uint32_t)((32 * quarter + lane) * 4), (uint32_t)r);
+  const int c_end = (rank * kHalves + half + 1) * kShare;
+  for (int c = c_end - kShare; c < c_end && b0 + c < b_end; c += kC) {
+    float p[kS][kC];
+#pragma unroll
+    for (int r = 0; r < kS; ++r)
+#pragma unroll
+      for (int j = 0; j < kC; ++j) p[r][j] = ld_peer(from[r] + (uint32_t)((c + j) * 512));
+    float v[kC];
+#pragma unroll
+    for (int j = 0; j < kC; ++j) {
+      v[j] = p[0][j];
+#pragma unroll
+      for (int r = 1; r < kS; ++r) v[j] += p[r][j];
+      if constexpr (kBlock == 16) v[j] = kSwap ? v[j] * mine * s_scale[c + j] : v[j] * s_scale[c + j] * mine;
+      v[j] += kSwap ? mine_bias : s_bias[c + j];
+    }
+    if (arow >= a_end) continue;
+    if constexpr (!kSwap && kC % 4 == 0) {
+      if (a.tma_out && b0 + c + kC <= b_end) {  // rows 16-byte aligned, so are four columns
+        char* to = a.y + ((int64_t)arow * a.y_row + b0 + c) * (a.out == W8A8_TYPE_F32 ? 4 : 2);
+#pragma unroll
+        for (int j = 0; j < kC; j += 4) {
+          if (a.out == W8A8_TYPE_F32)
+            *reinterpret_cast<float4*>(to + 4 * j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          else if (a.out == W8A8_TYPE_BF16)
+            *reinterpret_cast<uint2*>(to + 2 * j) = make_uint2(pack2<true>(v[j], v[j + 1]), pack2<true>(v[j + 2], v[j + 3]));
+          else
+            *reinterpret_cast<uint2*>(to + 2 * j) = make_uint2(pack2<false>(v[j], v[j + 1]), pack2<false>(v[j + 2], v[j + 3]));
+        }
+        continue;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kC; ++j)
+      if (b0 + c + j < b_end) put_one(a, kSwap ? (int64_t)(b0 + c + j) * a.y_row + arow : (int64_t)arow * a.y_row + b0 + c + j, v[j]);
+  }
 }
 
 template <int kMT, int kBN, bool kSwap, int kBlock>
@@ -447,21 +509,12 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
     if (split > 1) {  // each CTA adds up a share of the columns of all of its cluster's accumulators
       cluster_sync_all();
       if (warp >= 2 && first < tiles) {
-        const int quarter = warp & 3, half = (warp - 2) >> 2, at = first % a.a_tiles, bt = first / a.a_tiles;
-        const int arow = at * 128 + 32 * quarter + lane, b0 = bt * kBN;
-        const int b_end = kSwap ? a.M : a.N, a_end = kSwap ? a.N : a.M;
-        const float* as = kSwap ? a.w_scale : a.x_scale;
-        const float mine = kBlock == 16 && arow < a_end ? as[arow] : 1.0f;
-        const float mine_bias = kSwap && a.bias && arow < a_end ? a.bias[arow] : 0.0f;
-        for (int c = kBN * rank / split + half; c < kBN * (rank + 1) / split && b0 + c < b_end; c += C::kHalves) {
-          const uint32_t from = ring + (uint32_t)((c * 128 + 32 * quarter + lane) * 4);
-          float v = 0.0f;
-#pragma unroll 8
-          for (int r = 0; r < split; ++r) v += ld_peer(from, (uint32_t)r);
-          if constexpr (kBlock == 16) v = kSwap ? v * mine * s_scale[c] : v * s_scale[c] * mine;
-          v += kSwap ? mine_bias : s_bias[c];
-          if (arow < a_end) put_one(a, kSwap ? (int64_t)(b0 + c) * a.y_row + arow : (int64_t)arow * a.y_row + b0 + c, v);
-        }
+        if (split == 2)
+          add_up<2, kBN, kSwap, kBlock, C::kHalves>(a, ring, rank, first, warp, lane, s_scale, s_bias);
+        else if (split == 4)
+          add_up<4, kBN, kSwap, kBlock, C::kHalves>(a, ring, rank, first, warp, lane, s_scale, s_bias);
+        else
+          add_up<8, kBN, kSwap, kBlock, C::kHalves>(a, ring, rank, first, warp, lane, s_scale, s_bias);
       }
       cluster_sync_all();
     }
@@ -521,27 +574,31 @@ w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int split, i
   return W8A8_OK;
 }
 
-// How a call is cut up.  Up to 128 tokens: as many columns of tokens as there are, 128 channels a tile.  More: 256 x 192 where such
-// tiles fill the SMs, else 128 x 128.  Parts of k: while they leave a CTA four stages, and the tiles do not fill the SMs.
+// How a call is cut up.
+// Up to 48 tokens: as many columns of tokens as there are, 128 channels a tile (1152 -> 262144 at 16 tokens: 34.3 us, 55 with the tiles
+// for more; at 37: 42.4 and 55.3).  From there on those (64 tokens: 50.2, 53.8 with channels as the lanes, whose stores are 16 bits each;
+// 128: 43.2 and 90.8).
+// More: 256 x 192, whose operands are read less often, or 128 x 128, whichever has its waves over the SMs done first, at 2.4 times
+// the time for a larger tile (2048 tokens 1152 -> 13824: 27.2 and 32.2; 8192 tokens 1152 -> 1152: 24.0 and 22.4).
+// Parts of k: while the tiles do not fill the SMs and a CTA has two stages (6912 -> 1152 at 1 token: 14.0, 10.5, 7.9, 7.0 us in 1, 2, 4, 8
+// parts; at 300, whose 27 tiles fill the SMs in 4, 16.2, 15.0, 12.2, 18.3; 2304 -> 1152 at 16: 8.4, 7.5, 6.8 in 1, 2, 4); tiles of 128
+// tokens, whose sums are 64 KB a part, from 16 stages on (1152 -> 6912, 5 stages, at 128 tokens: 7.7 whole, 9.9 in two).
 template <int kBlock>
 w8a8_status run_gemm(const w8a8_fp4& x, const w8a8_fp4& w, const Fp4Args& a, int sms, cudaStream_t st) {
   const int stages = (a.K + kKStage - 1) / kKStage;
-  auto parts = [&](int64_t tiles) {
+  auto parts = [&](int64_t tiles, int least) {
     int s = 1;
-    while (s < 8 && tiles * 2 * s <= sms && stages >= 4 * 2 * s) s *= 2;
+    while (s < 8 && tiles * 2 * s <= sms && stages >= std::max(4 * s, least)) s *= 2;
     return s;
   };
   const int64_t channels = (a.N + 127) / 128;
-  if (a.M <= 128) {
-    const int s = parts(channels);
-    if (a.M <= 16) return launch<1, 16, true, kBlock>(x, w, a, s, sms, st);
-    if (a.M <= 32) return launch<1, 32, true, kBlock>(x, w, a, s, sms, st);
-    if (a.M <= 64) return launch<1, 64, true, kBlock>(x, w, a, s, sms, st);
-    return launch<1, 128, true, kBlock>(x, w, a, s, sms, st);
-  }
-  const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 191) / 192);
-  if (big >= sms) return launch<2, 192, false, kBlock>(x, w, a, 1, sms, st);
-  return launch<1, 128, false, kBlock>(x, w, a, parts((int64_t)((a.M + 127) / 128) * channels), sms, st);
+  if (a.M <= 16) return launch<1, 16, true, kBlock>(x, w, a, parts(channels, 0), sms, st);
+  if (a.M <= 32) return launch<1, 32, true, kBlock>(x, w, a, parts(channels, 0), sms, st);
+  if (a.M <= 48) return launch<1, 64, true, kBlock>(x, w, a, parts(channels, 0), sms, st);
+  auto waves = [&](int64_t tiles) { return (tiles + sms - 1) / sms; };
+  const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 191) / 192), small = (int64_t)((a.M + 127) / 128) * channels;
+  if (12 * waves(big) <= 5 * waves(small)) return launch<2, 192, false, kBlock>(x, w, a, 1, sms, st);
+  return launch<1, 128, false, kBlock>(x, w, a, parts(small, 16), sms, st);
 }
 
 struct LinearFp4Ws {

@@ -145,7 +145,9 @@ def _check_linear(y, xq, wq, bias, k):
     (64, 1152, 1024, "bf16", "bf16", False), (100, 777, 2080, "f32", "f32", True), (128, 128, 256, "bf16", "bf16", False),
     (129, 1152, 6912, "f16", "f16", True), (255, 2304, 544, "bf16", "bf16", False), (300, 1000, 1152, "bf16", "bf16", True),
     (513, 6912, 320, "bf16", "bf16", False), (1030, 7000, 544, "bf16", "bf16", True), (771, 10007, 160, "f16", "f32", False),
-    (2048, 4800, 96, "bf16", "f16", True)])
+    (2048, 4800, 96, "bf16", "f16", True), (1030, 5500, 544, "bf16", "bf16", True), (771, 7001, 160, "f16", "f32", False),
+    (1793, 3900, 96, "bf16", "f16", True), (2047, 7000, 288, "bf16", "bf16", False), (49, 1152, 6912, "bf16", "bf16", True),
+    (30, 130, 2304, "bf16", "f32", False), (60, 1000, 1024, "f32", "f32", True), (90, 515, 2048, "f16", "f16", True)])
 def test_linear(B, m, n, k, dt, out, with_bias, block):
     x = torch.randn(m, k, device="cuda", generator=_gen(m + n)).to(DT[dt])
     x[:, ::29] *= 20
