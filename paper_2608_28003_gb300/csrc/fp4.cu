@@ -3,8 +3,8 @@
 // Both kernels only move data, so HBM bounds them, or for few rows the launch.  A thread holds units of 16 columns: 32 or 64
 // bytes in, 8 bytes of codes out; the scales of four neighbouring blocks meet in one lane, whose word is contiguous in the
 // tiled order.  With blocks of 16 a row's largest magnitude comes first: the row stays in registers over that reduction (up to
-// kHeld units a thread; what is beyond is read again, from L2).  At 8191 rows of 6912 bf16 numbers: quantised in 23.3 us with
-// blocks of 32 (6.2 TB/s), in 29.3 with blocks of 16 (5.0; a row's reduction stands between its loads and stores), back in 27.7
+// kHeld units a thread; what is beyond is read again, from L2).  At 8191 rows of 6912 bf16 numbers: quantised in 23.1 us with
+// blocks of 32 (6.2 TB/s), in 30.2 with blocks of 16 (4.8; a row's reduction stands between its loads and stores), back in 27.7
 // (5.2 TB/s); before the maxima and quotients were packed two to a register and four units flew together, 75 there and back.
 #include <algorithm>
 
@@ -115,7 +115,7 @@ __device__ __forceinline__ uint32_t quantise_unit(const Unit16<kType>& u, uint32
   return byte;
 }
 
-// kWarp: tpr (a power of two, kBlock / 4 to 32) neighbouring lanes take a row, else a block takes one.
+// kWarp: tpr (a power of two, kBlock / 4 to 32) neighbouring lanes take a row (all 32 where kHeld > 1), else a block takes one.
 template <int kType, int kBlock, bool kWarp, int kHeld>
 __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restrict__ x, int64_t x_row_bytes, int rows, int padded,
                                                            int k, int tpr, uint8_t* __restrict__ codes,
@@ -257,15 +257,21 @@ w8a8_status check_fp4(const char* who, const w8a8_fp4* q) {
   return W8A8_OK;
 }
 
-// Lanes of a warp share its rows while a row's units fit; then a block a row.  Many rows: threads of up to four units, whose loads fly
-// together (8191 rows of 6912: 23 us with blocks of 32, 29 with blocks of 16; with one 47 and 65); few: of one, for the shortest chain.
+// Lanes of a warp share its rows while a row's units fit; then a block a row.  What fills the SMs with a thread a unit more than once has
+// lanes of up to four units, whose loads fly together (8191 rows of 6912: 23 us with blocks of 32, 30 with blocks of 16; with one 30 and
+// 54), and rows of up to 128 units a warp each, four a block (262144 rows of 1152: 149 and 242 us; 263 and 264 with one; instructions
+// bound it there, half as many again for blocks of 16 as for 32).  The others have one, for the shortest chain (2048 rows of 1152: 2.6 and 3.4 us;
+// with up to four 2.8 and 4.0).
 w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, bool settled,
                                 cudaStream_t st) {
   const int units = q.k / 16, padded = pad ? (int)round_up((size_t)q.rows, 128) : q.rows;
   int tpr = q.block / 4;  // four blocks' scales meet within a row's lanes
   while (tpr < units && tpr < 32) tpr *= 2;
-  const bool warp = units <= 32, many = !warp && q.rows >= 1024;
-  const int held = dtype == W8A8_TYPE_F32 ? 2 : 4, each = many ? held : 1;
+  const int held = dtype == W8A8_TYPE_F32 ? 2 : 4;
+  DevInfo d;
+  W8A8_TRY(dev_info(&d));
+  const bool many = (int64_t)q.rows * units >= (int64_t)d.sms * 2048, warp = units <= 32 || (many && units <= 32 * held);
+  const int each = many ? held : 1;
   const int threads = warp ? 128 : std::min((int)round_up((size_t)(units + each - 1) / each, 32), 512);
   const int64_t blocks = warp ? ((int64_t)padded * tpr + 127) / 128 : padded;
   auto go = [&](auto kernel) {
@@ -276,10 +282,12 @@ w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w
     constexpr int kT = decltype(type)::value;
     constexpr int kH = kT == W8A8_TYPE_F32 ? 2 : 4;
     if (q.block == 16)
-      return warp   ? go(fp4_quantise_kernel<kT, 16, true, 1>)
+      return warp && units > 32 ? go(fp4_quantise_kernel<kT, 16, true, kH>)
+             : warp ? go(fp4_quantise_kernel<kT, 16, true, 1>)
              : many ? go(fp4_quantise_kernel<kT, 16, false, kH>)
                     : go(fp4_quantise_kernel<kT, 16, false, 2>);
-    return warp   ? go(fp4_quantise_kernel<kT, 32, true, 1>)
+    return warp && units > 32 ? go(fp4_quantise_kernel<kT, 32, true, kH>)
+           : warp ? go(fp4_quantise_kernel<kT, 32, true, 1>)
            : many ? go(fp4_quantise_kernel<kT, 32, false, kH>)
                   : go(fp4_quantise_kernel<kT, 32, false, 2>);
   };
