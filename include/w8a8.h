@@ -666,9 +666,9 @@ w8a8_status w8a8_fp4_rope_append(const w8a8_rope_table* rope, const w8a8_paged_c
                                  const float* k_norm, float eps, uint16_t* q_out, int64_t q_out_row, void* stream);
 
 /* w8a8_paged_attention over a 4-bit cache: the same formula, row's ranges, checks, strides and guarantees, with the values the
- * cache stands for as keys and values.  dtype: of q and o, bf16 or fp16.  With up to 16 rows (max_new times query heads per
- * key/value head) weights are fp16 whatever the type, as the fp16 call's there, and a query whose dims are more than 2^29 apart
- * is off by up to 2^-40 of its largest; a row whose query is not finite is NaN. */
+ * cache stands for as keys and values.  dtype: of q and o, bf16 or fp16.  Weights are fp16 whatever the type, as the fp16 call's
+ * there.  With up to 16 rows (max_new times query heads per key/value head) a query whose dims are more than 2^29 apart is off by
+ * up to 2^-40 of its largest, and a row whose query is not finite is NaN. */
 w8a8_status w8a8_fp4_paged_attention_workspace_size(const w8a8_paged_cache_fp4* cache, int n_q, size_t* bytes);
 w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cache, const w8a8_paged_batch* batch, int dtype,
                                      const uint16_t* q, int64_t q_row, int64_t q_head, int n_q, float scale, int window,

@@ -36,6 +36,8 @@ extern "C" w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cach
   AttnCall a{q, q_row, q_head, o, o_row, o_head, n_q, dim, window, batch->max_new, scale, dtype == W8A8_TYPE_BF16};
   if (a.window >= 1 << 30) a.window = 0;  // beyond every position
   W8A8_TRY(gave_up_word(&a.gave_up));
+  // up to 16 rows an item: 64 tokens of 4 rows behind 8000 keys at head dim 256 56 us, 149 by the chunk kernel, whose row tiles are 128;
+  // at 16 rows still 45 and 75 (8 x 8 tokens of 2 heads behind 5000 keys), 30 and 45 (4 x 16 behind 2000)
   return (long long)a.max_new * (n_q / pc.p.n_kv) <= 16 ? launch_attn_fp4_tokens(pc, pb, a, workspace, d.sms, as_stream(stream))
                                                         : launch_attn_fp4_chunks(pc, pb, a, workspace, d.sms, as_stream(stream));
 }

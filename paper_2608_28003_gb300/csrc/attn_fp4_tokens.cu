@@ -21,6 +21,12 @@
 // page's follow one another, else key by key; 8 consumer warps take 16, 32 or 64 keys of a tile each, on their own from scores to output.
 // A warp's reference moves when one of its lanes sees a score that outgrew it, so a step has no reduction over lanes; sums stay
 // in the lanes until the item ends.
+//
+// Measured: 64 sequences of up to 30000 keys at head dim 256 (263 MB) 63.5 us, 4.1 TB/s and 0.61 of the copy rate; the loaders alone
+// would take 41 (6.4 TB/s), then 6 until the first tile is there, 2.5 to 5 an item's end, and the consumers, of whose
+// issue slots 0.6 are taken, two warps a scheduler.  20 sequences with 4 drafted tokens, fp16, head dim 64 (28 MB) 30.5 us: latency from step to
+// step, a fifth of it waits for instructions that run for the first time.  With one loader warp, one block of keys at a time and the
+// queries read as they are needed the first took 105 us.
 #include "attn_fp4.cuh"
 #include "ops.cuh"
 #include "tmap.cuh"
@@ -30,7 +36,9 @@ namespace w8a8 {
 namespace {
 
 constexpr int kWarps = 8;     // consumers
-constexpr int kItemCost = 4;  // what an item costs beside its key tiles, in key tiles
+// What an item costs beside its key tiles, in key tiles (0, 2, 4, 6: 64 long sequences 73.0, 67.5, 65.3, 65.0 us, 20 with drafts 42.4,
+// 31.4, 31.2, 33.4).
+constexpr int kItemCost = 4;
 
 template <int kDim, int kNt>
 struct Cfg {

@@ -31,6 +31,15 @@
 // that were timed (lookup 2, first tile 3, key tiles 7, partials and their join 8) make two thirds.  There every CTA copies all of its K and V from L2;
 // a pair of CTAs, each copying half for both, took 27.9, and 67.2 us instead of 71.9 for a larger chunk, but a copy to several
 // CTAs has no place in a library that also runs on several GPUs.
+//
+// Over a cache in 4 bits (Fp4Pages) the products and the softmax are the same; operands are made in shared memory.  Two warps copy codes
+// and scales by TMA into rings of 4.5 KB parts (one for K and the queries, one for V: one for both could not keep up, 266 us against
+// 205), three more turn K's codes into rows of the queries' type, two V's into fp16, which P is
+// then too: a code times its scale has at most six significant bits, so operands are exact, and 2^k_exp and 2^v_exp are applied to
+// scores and outputs.  The same four chunks over 4 bits, 127 GFLOP: 203 to 207 us (0.87 of the 16-bit kernel's rate), from 516
+// with codes read straight from memory by seven warps; its makers write the 256 bytes of a key (K and V of a head) that TMA writes in
+// 16 bits, which costs the issue slots the softmax is short of.  Makers' loops are not unrolled: their code was larger than the
+// instruction caches, and slower.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
 #include "attn_fp4.cuh"
 #include "attn_paged.cuh"
@@ -46,7 +55,7 @@ namespace {
 
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
-constexpr int kItemCost = 3;     // 4 bits: what an item costs beside its key tiles, in key tiles
+constexpr int kItemCost = 3;     // 4 bits: what an item costs beside its key tiles, in key tiles (1, 2, 3, 4: 226, 207, 204, 203 us)
 
 template <int kDim, bool kFp4>
 struct Cfg {
