@@ -4,8 +4,9 @@
 // bytes in, 8 bytes of codes out; the scales of four neighbouring blocks meet in one lane, whose word is contiguous in the
 // tiled order.  With blocks of 16 a row's largest magnitude comes first: the row stays in registers over that reduction (up to
 // kHeld units a thread; what is beyond is read again, from L2).  At 8191 rows of 6912 bf16 numbers: quantised in 23.1 us with
-// blocks of 32 (6.2 TB/s), in 30.2 with blocks of 16 (4.8; a row's reduction stands between its loads and stores), back in 27.7
-// (5.2 TB/s); before the maxima and quotients were packed two to a register and four units flew together, 75 there and back.
+// blocks of 32 (6.2 TB/s), in 30.2 with blocks of 16 (4.8; a row's reduction stands between its loads and stores), back in 24.1
+// and 32.5 (5.9 and 4.5 TB/s; 27.7 with a division a place); before the maxima and quotients were packed two to a register and four
+// units flew together, 75 there and back with blocks of 32.
 #include <algorithm>
 
 #include "fp4.cuh"
@@ -188,12 +189,14 @@ __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restric
   }
 }
 
-// A thread has eight columns, so that a warp's loads and stores are contiguous, of kAhead places 256 threads apart.
+// A thread has eight columns, so that a warp's loads and stores are contiguous, of kAhead places 256 threads apart.  per_row =
+// ceil(2^64 / eighths): i per_row / 2^64 is less than i / 2^64 above i / eighths, and i < 2^44 and eighths <= 2^13.
 constexpr int kAhead = 4;
-template <int kType>
+template <int kType, int kBlock>
 __global__ void __launch_bounds__(256) fp4_dequantise_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                              const float* __restrict__ row_scale, int64_t total, int eighths,
-                                                             int block, int groups, char* __restrict__ y, int64_t y_row_bytes) {
+                                                             uint64_t per_row, int groups, char* __restrict__ y,
+                                                             int64_t y_row_bytes) {
   pdl_wait();
   pdl_trigger();
   const int64_t i0 = (int64_t)blockIdx.x * (256 * kAhead) + threadIdx.x;
@@ -205,24 +208,30 @@ __global__ void __launch_bounds__(256) fp4_dequantise_kernel(const uint8_t* __re
   for (int j = 0; j < kAhead; ++j) {
     const int64_t i = i0 + 256 * j;
     if (i >= total) continue;
-    row[j] = total < (1ll << 32) ? (int64_t)((uint32_t)i / (uint32_t)eighths) : i / eighths;
+    row[j] = (int64_t)__umul64hi((uint64_t)i, per_row);  // i / eighths
     e8[j] = (int)(i - row[j] * eighths);
     c[j] = *reinterpret_cast<const uint32_t*>(codes + i * 4);
-    byte[j] = scales[fp4_scale_at(row[j], block == 16 ? e8[j] >> 1 : e8[j] >> 2, groups)];
-    b[j] = block == 16 ? row_scale[row[j]] : 1.0f;
+    byte[j] = scales[fp4_scale_at(row[j], kBlock == 16 ? e8[j] >> 1 : e8[j] >> 2, groups)];
+    if (kBlock == 16) b[j] = row_scale[row[j]];
   }
 #pragma unroll
   for (int j = 0; j < kAhead; ++j) {
     if (i0 + 256 * j >= total) break;
-    const float a = block == 16 ? e4m3_value(byte[j]) : byte[j] == kE8m0NaN ? NAN : byte[j] == 0 ? 0x1p-127f : __uint_as_float(byte[j] << 23);
     uint32_t h[4];
     float v[8];
     e2m1x8_to_f16(c[j], h);
+    if constexpr (kBlock == 16) {
+      const uint32_t a = e4m3x2_to_f16x2(byte[j] * 0x101u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = hmul2_bits(h[e], a);  // exact: six significant bits between 2^-10 and 2688
+    } else {
+      b[j] = byte[j] == kE8m0NaN ? NAN : byte[j] == 0 ? 0x1p-127f : __uint_as_float(byte[j] << 23);
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float2 f = unpack2<false>(h[e]);
-      v[2 * e] = f.x * a * b[j];
-      v[2 * e + 1] = f.y * a * b[j];
+      v[2 * e] = f.x * b[j];
+      v[2 * e + 1] = f.y * b[j];
     }
     constexpr int kBytes = kType == W8A8_TYPE_F32 ? 32 : 16;
     uint4* to = reinterpret_cast<uint4*>(y + row[j] * y_row_bytes + (int64_t)e8[j] * kBytes);
@@ -336,11 +345,15 @@ extern "C" w8a8_status w8a8_fp4_dequantize(const w8a8_fp4* q, int dtype, void* y
   W8A8_CHECK_ARG(blocks <= 0x7fffffffll, W8A8_ERR_SHAPE, "%s: [%d, %d] is too large", who, q->rows, q->k);
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), 0, as_stream(stream), (const uint8_t*)q->codes,
-                      (const uint8_t*)q->scales, (const float*)q->row_scale, total, eighths, q->block,
+                      (const uint8_t*)q->scales, (const float*)q->row_scale, total, eighths, ~0ull / (uint64_t)eighths + 1,
                       fp4_groups(q->k, q->block), static_cast<char*>(y), y_row * type_bytes(dtype));
   };
-  W8A8_CUDA(dtype == W8A8_TYPE_BF16  ? go(fp4_dequantise_kernel<W8A8_TYPE_BF16>)
-            : dtype == W8A8_TYPE_F16 ? go(fp4_dequantise_kernel<W8A8_TYPE_F16>)
-                                     : go(fp4_dequantise_kernel<W8A8_TYPE_F32>));
+  auto of = [&](auto type) {
+    constexpr int kT = decltype(type)::value;
+    return q->block == 16 ? go(fp4_dequantise_kernel<kT, 16>) : go(fp4_dequantise_kernel<kT, 32>);
+  };
+  W8A8_CUDA(dtype == W8A8_TYPE_BF16  ? of(std::integral_constant<int, W8A8_TYPE_BF16>())
+            : dtype == W8A8_TYPE_F16 ? of(std::integral_constant<int, W8A8_TYPE_F16>())
+                                     : of(std::integral_constant<int, W8A8_TYPE_F32>()));
   return W8A8_OK;
 }
