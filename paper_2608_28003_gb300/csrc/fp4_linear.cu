@@ -45,7 +45,7 @@ struct Cfg {
   static constexpr int kEpi = 4 * kMT * kHalves;                 // epilogue warps
   static constexpr int kEpiCols = kBN / kHalves;
   static constexpr int kStaging = kSwap ? 0 : kEpi * 2048;       // 32 rows of 64 bytes a warp
-  static constexpr int kRoom = 227 * 1024 - 3072 - kStaging;
+  static constexpr int kRoom = 224 * 1024 - kStaging;
   static constexpr int kStages = kRoom / kStage < 8 ? kRoom / kStage : 8;
   static constexpr int kSmem = kStages * kStage + kStaging + 1024;
   static constexpr int kThreads = 64 + 32 * kEpi;
@@ -527,15 +527,39 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
   }
 }
 
+cudaLaunchConfig_t config(unsigned grid, int threads, int smem, int split, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = split > 1 ? 2 : 1;
+  return cfg;
+}
+
+// least: stages from which on k is divided.
 template <int kMT, int kBN, bool kSwap, int kBlock>
-w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int split, int sms, cudaStream_t st) {
+w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int least, int sms, cudaStream_t st) {
   using C = Cfg<kMT, kBN, kSwap, kBlock>;
   static bool attr_set[64] = {};
+  static int at_once[64][4] = {};  // clusters of 1, 2, 4, 8 that the GPU holds
   int dev = 0;
   W8A8_CUDA(cudaGetDevice(&dev));
+  W8A8_CHECK_ARG(dev >= 0 && dev < 64, W8A8_ERR_CUDA, "w8a8_fp4_linear: device %d", dev);
   auto kernel = fp4_gemm_kernel<kMT, kBN, kSwap, kBlock>;
-  if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+  cudaLaunchAttribute attr[2];
+  if (!attr_set[dev]) {
     W8A8_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
+    for (int i = 1; i < 4 && kMT == 1; ++i) {
+      const cudaLaunchConfig_t one = config(1u << i, C::kThreads, C::kSmem, 1 << i, st, attr);
+      W8A8_CUDA(cudaOccupancyMaxActiveClusters(&at_once[dev][i], kernel, &one));
+    }
     attr_set[dev] = true;
   }
   const w8a8_fp4 &fa = kSwap ? w : x, &fb = kSwap ? x : w;
@@ -545,6 +569,11 @@ w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int split, i
   a.b_tiles = (fb.rows + kBN - 1) / kBN;
   a.a_blocks = (fa.rows + 127) / 128;
   a.b_blocks = (fb.rows + 127) / 128;
+  const int64_t tiles = (int64_t)a.a_tiles * a.b_tiles;
+  const int stages = (a.K + kKStage - 1) / kKStage;
+  int split = 1;
+  for (int i = 1; i < 4 && kMT == 1; ++i)
+    if (tiles <= at_once[dev][i] && stages >= std::max(2 << i, least)) split = 1 << i;
   a.split = split;
   CUtensorMap ta, tb, ty;
   const uint64_t bytes = (uint64_t)a.K / 2;
@@ -555,21 +584,8 @@ w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int split, i
   ty = ta;
   if (a.tma_out)
     W8A8_TRY(make_tmap_2d(&ty, a.y, e, (uint64_t)a.N, (uint64_t)a.M, (uint64_t)a.y_row * e, 64 / e, 32, 64));
-  const int64_t tiles = (int64_t)a.a_tiles * a.b_tiles;
   const unsigned grid = (unsigned)(split > 1 ? tiles * split : std::min<int64_t>(tiles, sms));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(C::kThreads);
-  cfg.dynamicSmemBytes = C::kSmem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)split;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = split > 1 ? 2 : 1;
+  const cudaLaunchConfig_t cfg = config(grid, C::kThreads, C::kSmem, split, st, attr);
   W8A8_CUDA(cudaLaunchKernelEx(&cfg, kernel, ta, tb, ty, a));
   return W8A8_OK;
 }
@@ -580,25 +596,20 @@ w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int split, i
 // 128: 43.2 and 90.8).
 // More: 256 x 192, whose operands are read less often, or 128 x 128, whichever has its waves over the SMs done first, at 2.4 times
 // the time for a larger tile (2048 tokens 1152 -> 13824: 27.2 and 32.2; 8192 tokens 1152 -> 1152: 24.0 and 22.4).
-// Parts of k: while the tiles do not fill the SMs and a CTA has two stages (6912 -> 1152 at 1 token: 14.0, 10.5, 7.9, 7.0 us in 1, 2, 4, 8
-// parts; at 300, whose 27 tiles fill the SMs in 4, 16.2, 15.0, 12.2, 18.3; 2304 -> 1152 at 16: 8.4, 7.5, 6.8 in 1, 2, 4); tiles of 128
-// tokens, whose sums are 64 KB a part, from 16 stages on (1152 -> 6912, 5 stages, at 128 tokens: 7.7 whole, 9.9 in two).
+// Parts of k: while a CTA has two stages (6912 -> 1152 at 1 token: 14.0, 10.5, 7.9, 7.0 us in 1, 2, 4, 8 parts; 2304 -> 1152 at 16: 8.4, 7.5,
+// 6.8 in 1, 2, 4) and the GPU holds all clusters at once, which are as many as its groups of SMs have room for, not its SMs divided by
+// the parts (6912 -> 2048 at 16 tokens, 16 tiles, in 8 parts 12.4 us, 8.6 in 4; 4096 -> 4608 and 4736, 36 and 37 tiles, in 4: 8.6 and
+// 12.9); tiles of 128 tokens, whose sums are 64 KB a part, from 16 stages on (1152 -> 6912, 5 stages, at 128 tokens: 7.7 whole, 9.9 in two).
 template <int kBlock>
 w8a8_status run_gemm(const w8a8_fp4& x, const w8a8_fp4& w, const Fp4Args& a, int sms, cudaStream_t st) {
-  const int stages = (a.K + kKStage - 1) / kKStage;
-  auto parts = [&](int64_t tiles, int least) {
-    int s = 1;
-    while (s < 8 && tiles * 2 * s <= sms && stages >= std::max(4 * s, least)) s *= 2;
-    return s;
-  };
-  const int64_t channels = (a.N + 127) / 128;
-  if (a.M <= 16) return launch<1, 16, true, kBlock>(x, w, a, parts(channels, 0), sms, st);
-  if (a.M <= 32) return launch<1, 32, true, kBlock>(x, w, a, parts(channels, 0), sms, st);
-  if (a.M <= 48) return launch<1, 64, true, kBlock>(x, w, a, parts(channels, 0), sms, st);
+  if (a.M <= 16) return launch<1, 16, true, kBlock>(x, w, a, 0, sms, st);
+  if (a.M <= 32) return launch<1, 32, true, kBlock>(x, w, a, 0, sms, st);
+  if (a.M <= 48) return launch<1, 64, true, kBlock>(x, w, a, 0, sms, st);
   auto waves = [&](int64_t tiles) { return (tiles + sms - 1) / sms; };
-  const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 191) / 192), small = (int64_t)((a.M + 127) / 128) * channels;
-  if (12 * waves(big) <= 5 * waves(small)) return launch<2, 192, false, kBlock>(x, w, a, 1, sms, st);
-  return launch<1, 128, false, kBlock>(x, w, a, parts(small, 16), sms, st);
+  const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 191) / 192),
+                small = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
+  if (12 * waves(big) <= 5 * waves(small)) return launch<2, 192, false, kBlock>(x, w, a, 0, sms, st);
+  return launch<1, 128, false, kBlock>(x, w, a, 16, sms, st);
 }
 
 struct LinearFp4Ws {
