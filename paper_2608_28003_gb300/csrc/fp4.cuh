@@ -59,20 +59,25 @@ __device__ __forceinline__ int row_exponent(uint32_t top) {
 // one, and on a border only with it: a border b has few bits, and x (24 bits) over a scale of 4 bits, or m over 6, that
 // differs from b does so by more than half a unit in the last place of b (with f and g the significands of b and of
 // b times the divisor: by 2 g^-1 of that, relative to f^-1, and g < 2 f).
-// The quotient is x hi + fl(x lo) with hi + lo the reciprocal to twice the bits: exact where the quotient is a border, within
-// 2^-20 of a unit in the last place of correctly rounded elsewhere.
+// The quotient is x hi + fl(x lo) with hi + lo the reciprocal to 2^-43 (hi to 2^-22, lo from its exact remainder): exact where the
+// quotient is a border, within 2^-19 of a unit in the last place of correctly rounded elsewhere, where the nearest border is 2^-5 of
+// one further off than half of it (g is at most 1.875 where f is 1).
+__device__ __forceinline__ float sixth(float x) {  // x / 6; what is above every scale as the largest of them has it
+  x = fminf(x, 0x1p20f);
+  return fmaf(x, 0x1.555556p-3f, x * -0x1.555556p-28f);
+}
 struct Block16 {
   float scale, hi, lo;
   uint32_t byte;
   __device__ __forceinline__ void unit(uint32_t top_bits, float s2) {  // top_bits: of the block's largest magnitude
-    byte = top_bits >= 0x7f800000u ? kE4m3NaN : e4m3_of(__fdiv_rn(__uint_as_float(top_bits) * s2, 6.0f));
+    byte = top_bits >= 0x7f800000u ? kE4m3NaN : e4m3_of(sixth(__uint_as_float(top_bits) * s2));
     of_byte();
   }
   __device__ __forceinline__ void of_byte() {
     scale = byte == kE4m3NaN ? 0.0f : e4m3_value(byte);
-    hi = scale > 0.0f ? __frcp_rn(scale) : 0.0f;
+    asm("rcp.approx.f32 %0, %1;\n" : "=f"(hi) : "f"(scale));
     lo = fmaf(-scale, hi, 1.0f) * hi;
-    if (scale == 0.0f) lo = 0.0f;
+    if (scale == 0.0f) hi = lo = 0.0f;
   }
   // x s2 / scale (x already times s2)
   __device__ __forceinline__ float over(float x) const { return fmaf(x, hi, x * lo); }

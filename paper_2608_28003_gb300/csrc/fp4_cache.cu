@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads)
     // both ends of the bound
     bool open_unit = false, open[kE] = {};
     if (!nan && wide > 0.0f)
-      open_unit = e4m3_of(__fdiv_rn((top - wide) * s2, 6.0f)) != e4m3_of(__fdiv_rn((top + wide) * s2, 6.0f));
+      open_unit = e4m3_of(sixth((top - wide) * s2)) != e4m3_of(sixth((top + wide) * s2));
     uint32_t w = 0;
     auto encode = [&] {
       w = 0;

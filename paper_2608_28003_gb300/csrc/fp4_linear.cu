@@ -606,7 +606,7 @@ w8a8_status run_gemm(const w8a8_fp4& x, const w8a8_fp4& w, const Fp4Args& a, int
   if (a.M <= 32) return launch<1, 32, true, kBlock>(x, w, a, 0, sms, st);
   if (a.M <= 48) return launch<1, 64, true, kBlock>(x, w, a, 0, sms, st);
   auto waves = [&](int64_t tiles) { return (tiles + sms - 1) / sms; };
-  const int64_t big = (int64_t)((a.M + 255) / 256) * ((a.N + 191) / 192),
+  const int64_t big = (int64_t)((a.M + 255) / 256) * (((int64_t)a.N + 191) / 192),
                 small = (int64_t)((a.M + 127) / 128) * ((a.N + 127) / 128);
   if (12 * waves(big) <= 5 * waves(small)) return launch<2, 192, false, kBlock>(x, w, a, 0, sms, st);
   return launch<1, 128, false, kBlock>(x, w, a, 16, sms, st);
@@ -634,8 +634,8 @@ extern "C" w8a8_status w8a8_fp4_linear_workspace_size(int M, int N, int K, int b
   const char* who = "w8a8_fp4_linear_workspace_size";
   W8A8_CHECK_ARG(bytes != nullptr && (block == 16 || block == 32), W8A8_ERR_INVALID_ARG, "%s: null pointer, or block %d", who,
                  block);
-  W8A8_CHECK_ARG(M >= 0 && M <= kMaxFp4Rows && N >= 0 && N <= kMaxFp4Rows && K > 0 && K % 32 == 0 && K <= W8A8_MAX_K, W8A8_ERR_SHAPE, "%s: M=%d N=%d K=%d", who, M, N,
-                 K);
+  W8A8_CHECK_ARG(M >= 0 && M <= kMaxFp4Rows && N >= 0 && N <= kMaxFp4Rows && K > 0 && K % 32 == 0 && K <= W8A8_MAX_K,
+                 W8A8_ERR_SHAPE, "%s: M=%d N=%d K=%d", who, M, N, K);
   *bytes = linear_fp4_ws(M, K, block).total;
   return W8A8_OK;
 }

@@ -98,6 +98,30 @@ def test_every_bf16_is_decided_right(B):
         _check_matrix(B.fp4_quantize(x, block), x, block)
 
 
+@pytest.mark.parametrize("p", [0, -60, 37, 100])
+def test_borders_of_every_scale(B, p):
+    """fp32 rows with, for every e4m3 scale, the seven borders of its codes and the numbers next to them on both sides, and blocks whose
+    largest magnitude is on and beside every border of the scales."""
+    near = lambda x: [np.nextafter(np.float32(x), np.float32(0)), np.float32(x), np.nextafter(np.float32(x), np.float32(1e30))]  # noqa: E731
+    blocks = []
+    for s in O4.E4M3[1:]:
+        borders = [v for b in (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0) for v in near(b * s)]
+        for part in (borders[:11], borders[11:]):
+            blocks.append([6 * s] + part + [0.0] * (15 - len(part)))
+    for mid in (O4.E4M3[1:] + O4.E4M3[:-1]) / 2:
+        for top in near(6 * mid):
+            blocks.append([top, -top] + [top * f for f in np.linspace(0, 1, 14)])
+    x = np.array(blocks, np.float32)
+    x[1::2] *= -1
+    first = np.zeros_like(x)
+    first[:, 0] = 2000.0  # keeps the row's scale at 2^p
+    x = np.concatenate([first, x], 1) * np.float32(2.0 ** p)
+    x = torch.from_numpy(x).cuda()
+    q = B.fp4_quantize(x, 16)
+    assert (q.row_scale == 2.0 ** p).all()
+    _check_matrix(q, x, 16)
+
+
 def test_quantise_views_and_outputs(B):
     wide = torch.randn(9, 3, 128, device="cuda", generator=_gen(1)).bfloat16()
     x = wide[:, 1, :64]
