@@ -4,8 +4,9 @@
 // heads with a fixed step, so that the row's sines and cosines are computed once for all of them; a lane holds 8, 4 or 2
 // neighbouring dims (head dim 256, 128, 64) and reaches the other dim of a pair by a shuffle.  A block of 16 dims is 2, 4 or 8
 // lanes.  Little is moved (a key's 144 bytes at head dim 256), so latency bounds it: launch, sequence, length, page, store.
-// 5 chunks of up to 811 tokens, 16 query and 4 key/value heads of 128: the host's 14 us at most (23 with the queries by warps too and every
-// dim of an open block in 64 bits; 33 with a head's load behind the one before).
+// 5 chunks of up to 811 tokens, 16 query and 4 key/value heads of 128: 13.0 us, half of the issue slots used (the 16-bit append: 7.5); 23 with
+// the queries by warps too and every dim of an open block in 64 bits, 33 with a head's load behind the one before.  48 single
+// tokens 4.8.
 //
 // Codes are decided as in exact arithmetic: the rotation and the norm are computed in fp32 with a bound on what they are off by, and where
 // that leaves a code or a scale open (both ends of the bound are rounded and compared; a few heads in a thousand), or fp32's range does not
@@ -468,8 +469,9 @@ extern "C" w8a8_status w8a8_fp4_rope_append(const w8a8_rope_table* rope, const w
   DevInfo d;
   W8A8_TRY(dev_info(&d));
   const RopeArgs t{rope->turns, rope->scale, rope->rotary_dim, rope->interleaved};
-  // few rows spread over their heads, many compute their angles once: up to 32 warps an SM
-  const int64_t want = (int64_t)d.sms * 32 / pb.n_rows;
+  // few rows spread over their heads, many compute their angles once: up to 16 warps an SM, one wave (2400 rows, 4 key/value heads of 128:
+  // 13.0 us; 14.2 with 32 warps, 16.5 with 48)
+  const int64_t want = (int64_t)d.sms * 16 / pb.n_rows;
   const int step = (int)(want < 1 ? 1 : want > 2 * pc.p.n_kv ? 2 * pc.p.n_kv : want), units = dim / 16;
   const int q_step = head_step(pb.n_rows, units, n_q, d.sms);
   const int64_t kv_blocks = ((int64_t)pb.n_rows * step * 32 + kThreads - 1) / kThreads;
