@@ -24,8 +24,9 @@
 //
 // Measured: 64 sequences of up to 30000 keys at head dim 256 (263 MB) 63.5 us, 4.1 TB/s and 0.61 of the copy rate; the loaders alone
 // would take 41 (6.4 TB/s), then 6 until the first tile is there, 2.5 to 5 an item's end, and the consumers, of whose
-// issue slots 0.6 are taken, two warps a scheduler.  20 sequences with 4 drafted tokens, fp16, head dim 64 (28 MB) 30.5 us: latency from step to
-// step, a fifth of it waits for instructions that run for the first time.  With one loader warp, one block of keys at a time and the
+// issue slots half are taken, two warps a scheduler (three, with a block of keys each and fewer stages, spill: 97.7 us).  20 sequences
+// with 4 drafted tokens, fp16, head dim 64 (28 MB) 30.2 us: latency from step to step, a fifth of it waits for instructions that
+// run for the first time.  With one loader warp, one block of keys at a time and the
 // queries read as they are needed the first took 105 us.
 #include "attn_fp4.cuh"
 #include "ops.cuh"

@@ -352,7 +352,8 @@ __device__ __forceinline__ Pieces pieces_of(const Walk& w, const LineStart& ls) 
 constexpr int kTokenRows = 16;    // rows of a partial of the kernels for tokens: [row][dim] outputs, then the rows' m and l
 constexpr int kMaxPieces = 192;   // of an item: no more than CTAs
 
-// The pieces of an item of up to 16 rows, joined in their order, by the consumer warps (threads 0 .. 32 kWarps - 1; barrier 1): outputs, times `back`, to o (row r at (r / group) o_row + (r % group) o_head).
+// The pieces of an item of up to 16 rows, joined in their order, by the consumer warps (threads 0 .. 32 kWarps - 1; barrier 1):
+// outputs, times `back`, to o (row r at (r / group) o_row + (r % group) o_head).
 // What another SM has just written takes a microsecond to read, so few loads follow one another: the statistics of all
 // pieces (a warp a row, lane = piece), then every thread's part of the output with up to kAhead pieces in flight.  Rows whose
 // result is not finite, or without weight, are marked in *bad.  Not inline: its registers are not the main loop's.

@@ -4,9 +4,9 @@
 // heads with a fixed step, so that the row's sines and cosines are computed once for all of them; a lane holds 8, 4 or 2
 // neighbouring dims (head dim 256, 128, 64) and reaches the other dim of a pair by a shuffle.  A block of 16 dims is 2, 4 or 8
 // lanes.  Little is moved (a key's 144 bytes at head dim 256), so latency bounds it: launch, sequence, length, page, store.
-// 5 chunks of up to 811 tokens, 16 query and 4 key/value heads of 128: 13.0 us, half of the issue slots used (the 16-bit append: 7.5); 23 with
-// the queries by warps too and every dim of an open block in 64 bits, 33 with a head's load behind the one before.  48 single
-// tokens 4.8.
+// 5 chunks of up to 811 tokens, 16 query and 4 key/value heads of 128: 13.0 us, half of the issue slots used (the 16-bit append: 7.5);
+// 23 with the queries by warps too and every dim of an open block in 64 bits, 33 with a head's load behind the one before.  48
+// single tokens 4.8.
 //
 // Codes are decided as in exact arithmetic: the rotation and the norm are computed in fp32 with a bound on what they are off by, and where
 // that leaves a code or a scale open (both ends of the bound are rounded and compared; a few heads in a thousand), or fp32's range does not
