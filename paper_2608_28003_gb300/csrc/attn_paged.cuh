@@ -129,7 +129,8 @@ __device__ __forceinline__ long long sum_tiles(const SeqShape& q, int window, in
 // sequences; up to 32 of them are one warp's alone.
 template <int kT>
 __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, int n_kv, int window, int tt, int bk_shift,
-                                           int worker, int workers, LineStart* out, long long* scan, int extra = 0) {
+                                           int worker, int workers, LineStart* out, long long* scan, int extra = 0,
+                                           float per_unit = 0.0f) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool one_warp = b.n_seqs <= 32;
   if (one_warp && warp > 0) {
@@ -176,9 +177,12 @@ __device__ __forceinline__ void find_start(const PagedBatch& b, int page_shift, 
   for (int i = 0; i < per; ++i) one += sum_of(~(tid * per + i), [&](int n) { return (long long)(n + extra); });
   long long upto = run(one * n_kv, total);
   int unit = 0;
-  if (total > workers && total <= (long long)kShort * workers) {
+  // A piece costs its item's last one a join: of n tiles in pieces of u they take u tiles' time and n / u joins', least at the
+  // square root of n times a join over a tile.  per_unit: that quotient over the items there can be (0: pieces of any size).
+  const int few = (int)min((float)kShort, sqrtf(per_unit * (float)total));
+  if ((total > workers || few > 1) && total <= (long long)kShort * workers) {
     // pieces for four units, 16 bits each (no more of them than tiles, 12 x 152)
-    const int least = (int)((total + workers - 1) / workers), step = max(1, (least + 2) / 4);
+    const int least = max((int)((total + workers - 1) / workers), few), step = max(1, (least + 2) / 4);
     uint32_t inv[4];  // quotients by a product: exact for the 12 x 152 tiles and units up to 21 there are
 #pragma unroll
     for (int j = 0; j < 4; ++j) inv[j] = (uint32_t)ceilf(__fdividef(65536.0f, (float)(least + j * step)) + 0.001f);
