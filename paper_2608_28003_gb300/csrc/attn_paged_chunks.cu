@@ -56,8 +56,9 @@ namespace {
 constexpr int kBq = 128, kBk = 128, kBkShift = 7;
 constexpr int kSub = 128 * 128;  // bytes of 128 rows of 64 dims
 constexpr int kItemCost = 3;     // 4 bits: what an item costs beside its key tiles, in key tiles (1, 2, 3, 4: 226, 207, 204, 203 us)
-template <int kDim>
-constexpr float kJoinCost = kDim == 256 ? 0.6f : 1.2f;  // 4 bits: what a piece's join costs, in key tiles
+// 4 bits: what a piece's join costs, in key tiles (0, 0.6, 1.2, 2.4: 64 tokens of 4 heads of 256 behind 8000 keys 182, 65, 64, 67 us; 32
+// of 16 over 2 of 128 behind 16000 210, 89, 72, 71; 300 of 5 of 64 behind 3000 36, 32, 29, 28).
+constexpr float kJoinCost = 1.2f;
 
 template <int kDim, bool kFp4>
 struct Cfg {
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
   // (syncs the block)
   find_start<kThreads>(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift, (int)blockIdx.x, (int)gridDim.x, &ls, scan,
                        kFp4 ? kItemCost : 0,
-                       kFp4 ? kJoinCost<kDim> / ((float)c.n_kv * ((float)b.n_seqs + (float)b.n_rows / (float)item_tt)) : 0.0f);
+                       kFp4 ? kJoinCost / ((float)c.n_kv * ((float)b.n_seqs + (float)b.n_rows / (float)item_tt)) : 0.0f);
   bool ok = true;
   if constexpr (kFp4) {  // registers: 512 threads of 128 are shared out as 256 of 144 and 256 of 112
     if (warp < C::kSoft)
