@@ -352,7 +352,9 @@ def test_attention_rows_outside_the_batch(B):
 @pytest.mark.parametrize("n_q,n_kv,dim,seqs,new,ctx,window", [(4, 1, 256, 40, 1, 3000, 0), (4, 1, 256, 300, 1, 90, 0),
                                                               (8, 8, 64, 3, 400, 900, 0), (4, 1, 256, 2, 700, 2000, 512),
                                                               (16, 2, 128, 5, 7, 4000, 1000), (28, 4, 128, 1, 512, 3000, 0),
-                                                              (16, 2, 128, 12, 2, 3000, 0), (12, 4, 64, 20, 4, 2500, 0)])
+                                                              (16, 2, 128, 12, 2, 3000, 0), (12, 4, 64, 20, 4, 2500, 0),
+                                                              (4, 1, 256, 1, 64, 8000, 0), (16, 2, 128, 1, 32, 9000, 0),
+                                                              (5, 5, 64, 2, 40, 6000, 0), (4, 1, 256, 40, 20, 1500, 600)])
 def test_attention_split_over_the_gpu(B, n_q, n_kv, dim, seqs, new, ctx, window):
     """Enough keys that rows are divided between CTAs and joined again; the same bits every time."""
     rng = random.Random(seqs)
