@@ -36,10 +36,11 @@
 // and scales by TMA into rings of 4.5 KB parts (one for K and the queries, one for V: one for both could not keep up, 266 us against
 // 205), three more turn K's codes into rows of the queries' type, two V's into fp16, which P is
 // then too: a code times its scale has at most six significant bits, so operands are exact, and 2^k_exp and 2^v_exp are applied to
-// scores and outputs.  The same four chunks over 4 bits, 127 GFLOP: 203 to 207 us (0.87 of the 16-bit kernel's rate), from 516
-// with codes read straight from memory by seven warps; its makers write the 256 bytes of a key (K and V of a head) that TMA writes in
-// 16 bits, which costs the issue slots the softmax is short of.  Makers' loops are not unrolled: their code was larger than the
-// instruction caches, and slower.
+// scores and outputs.  The same four chunks over 4 bits, 127 GFLOP: 196 to 200 us (0.92 of the 16-bit kernel's rate; with fp16
+// queries 188), from 516 with codes read straight from memory by seven warps.  The makers, five warps beside eight of softmax, are what
+// is short where the softmax is not: a prompt of 2048 tokens at head dim 256 takes 43.7 us, 29 over 16 bits.  Their loops are not
+// unrolled, nor is a unit read ahead of the one before's making (199): their code was larger than the instruction caches, and slower;
+// nine makers leave the softmax 96 registers, which spill.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
 #include "attn_fp4.cuh"
 #include "attn_paged.cuh"
@@ -138,29 +139,22 @@ __host__ __device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c
 // significant bits and lies within fp16's range as within bf16's, so operands are exact in either type: K has the queries', V is fp16
 // whatever the type, as the weights are.
 // Into a row of a 64-dim column (128-byte rows, swizzled): `at` is the row, `swz` its part and swizzle.
-// To bf16: fp16's bits shifted into place are the value times 2^-112 (nothing of a code is lost), the scale is taken times 2^112.
+// To bf16 by way of fp32, on two pipes; fp16's bits shifted into a bf16's place took three operations a pair more of the one that
+// codes are converted on (203 us for the four chunks above, 196 so).
 template <bool kToBf16>
 __device__ __forceinline__ void store_unit(const uint4& codes, uint32_t sc, uint32_t at, uint32_t swz) {
   const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-  uint32_t h2 = e4m3x2_to_f16x2(sc);
-  if constexpr (kToBf16) {
-    const uint32_t lo = h2 & 0xffffu, hi = h2 >> 16;
-    h2 = (lo ? (lo >> 3) + 0x7000u : 0u) | (hi ? (hi >> 3) + 0x7000u : 0u) << 16;
-  }
-  const uint32_t s0 = __byte_perm(h2, h2, 0x1010), s1 = __byte_perm(h2, h2, 0x3232);
+  const uint32_t h2 = e4m3x2_to_f16x2(sc), s0 = __byte_perm(h2, h2, 0x1010), s1 = __byte_perm(h2, h2, 0x3232);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t h[4];
     e2m1x8_to_f16(w[i], h);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t s = i < 2 ? s0 : s1;
+      h[e] = hmul2_bits(h[e], i < 2 ? s0 : s1);
       if constexpr (kToBf16) {
-        const uint32_t t = ((h[e] & 0x7fff7fffu) >> 3) | (h[e] & 0x80008000u);
-        const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&t), *reinterpret_cast<const __nv_bfloat162*>(&s));
-        h[e] = *reinterpret_cast<const uint32_t*>(&y);
-      } else {
-        h[e] = hmul2_bits(h[e], s);
+        const float2 f = unpack2<false>(h[e]);
+        h[e] = pack2<true>(f.x, f.y);
       }
     }
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (swz ^ (uint32_t)(i << 4))), "r"(h[0]), "r"(h[1]), "r"(h[2]),
