@@ -5,7 +5,7 @@
 // tiled order.  With blocks of 16 a row's largest magnitude comes first: the row stays in registers over that reduction (up to
 // kHeld units a thread; what is beyond is read again, from L2).  At 8191 rows of 6912 bf16 numbers: quantised in 23.1 us with
 // blocks of 32 (6.2 TB/s), in 27.7 with blocks of 16 (5.2; a row's reduction stands between its loads and stores), back in 24.1
-// and 32.5 (5.9 and 4.5 TB/s; 27.7 with a division a place); before the maxima and quotients were packed two to a register and four
+// and 32.8 (5.9 and 4.4 TB/s; 27.7 with a division a place); before the maxima and quotients were packed two to a register and four
 // units flew together, 75 there and back with blocks of 32.
 #include <algorithm>
 
@@ -189,6 +189,15 @@ __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restric
   }
 }
 
+// f b rounded to odd: cut off, and its last bit set where that lost something.  fp32 has more than two bits beyond the 16-bit types', so what
+// is rounded from it to one of them is as if from f b itself.  The remainder is rounded away from zero: its last bits can lie below
+// fp32's smallest number.
+__device__ __forceinline__ float product_to_odd(float f, float b) {
+  const float x = fabsf(f), y = fabsf(b), p = __fmul_rz(x, y);
+  const uint32_t sign = (__float_as_uint(f) ^ __float_as_uint(b)) & 0x80000000u;
+  return __uint_as_float(__float_as_uint(p) | (__fmaf_ru(x, y, -p) > 0.0f ? 1u : 0u) | sign);
+}
+
 // A thread has eight columns, so that a warp's loads and stores are contiguous, of kAhead places 256 threads apart.  per_row =
 // ceil(2^64 / eighths): i per_row / 2^64 is less than i / 2^64 above i / eighths, and i < 2^44 and eighths <= 2^13.
 constexpr int kAhead = 4;
@@ -227,11 +236,22 @@ __global__ void __launch_bounds__(256) fp4_dequantise_kernel(const uint8_t* __re
     } else {
       b[j] = byte[j] == kE8m0NaN ? NAN : byte[j] == 0 ? 0x1p-127f : __uint_as_float(byte[j] << 23);
     }
+    // A row's scale that is a (normal) power of two, as the quantiser's are, costs the product no rounding; another would cost a 16-bit
+    // value two (to odd: 38.8 us at 8191 x 6912, 32.8 with powers of two).
+    if (kBlock == 16 && kType != W8A8_TYPE_F32 && (__float_as_uint(b[j]) << 9) != 0) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = unpack2<false>(h[e]);
-      v[2 * e] = f.x * b[j];
-      v[2 * e + 1] = f.y * b[j];
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack2<false>(h[e]);
+        v[2 * e] = product_to_odd(f.x, b[j]);
+        v[2 * e + 1] = product_to_odd(f.y, b[j]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = unpack2<false>(h[e]);
+        v[2 * e] = f.x * b[j];
+        v[2 * e + 1] = f.y * b[j];
+      }
     }
     constexpr int kBytes = kType == W8A8_TYPE_F32 ? 32 : 16;
     uint4* to = reinterpret_cast<uint4*>(y + row[j] * y_row_bytes + (int64_t)e8[j] * kBytes);
