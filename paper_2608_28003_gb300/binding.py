@@ -311,13 +311,14 @@ class Workspace:
         self.buf = torch.zeros(WS_RESERVED, dtype=torch.uint8, device=self.device)
 
     def get(self, nbytes: int) -> torch.Tensor:
-        if self.buf.numel() < nbytes:
-            if self.buf.is_cuda and torch.cuda.is_current_stream_capturing():
+        buf = self.buf  # another thread's call may put its own in place meanwhile
+        if buf.numel() < nbytes:
+            if buf.is_cuda and torch.cuda.is_current_stream_capturing():
                 return _graph_scratch(nbytes, self.device)
-            if self.buf.is_cuda:  # calls of this stream may still use it
-                self.buf.record_stream(torch.cuda.current_stream(self.buf.device))
-            self.buf = torch.zeros(int(nbytes * 1.25) + 256, dtype=torch.uint8, device=self.device)
-        return self.buf
+            if buf.is_cuda:  # calls of this stream may still use it
+                buf.record_stream(torch.cuda.current_stream(buf.device))
+            self.buf = buf = torch.zeros(int(nbytes * 1.25) + 256, dtype=torch.uint8, device=self.device)
+        return buf
 
 
 _DEFAULT_WS = {}
@@ -727,14 +728,15 @@ _STREAM_WS = {}
 
 def stream_workspace(nbytes: int, dev: torch.device, stream=None) -> torch.Tensor:
     """Scratch of calls without a workspace of their own, its counters zero: one per stream, so that calls on different
-    streams do not share one; while a stream is captured, a new one that lives as long as the graph's memory."""
+    streams do not share one (threads on one stream do, and a call's launches stay together); while a stream is captured, a new
+    one that lives as long as the graph's memory."""
     s = stream if stream is not None else torch.cuda.current_stream(dev)
     with torch.cuda.stream(s):
         if torch.cuda.is_current_stream_capturing():
             return _graph_scratch(nbytes, dev)
         key = (dev.index, s.cuda_stream)
         if key not in _STREAM_WS:
-            _STREAM_WS[key] = Workspace(dev)
+            _STREAM_WS.setdefault(key, Workspace(dev))
         return _STREAM_WS[key].get(nbytes)
 
 

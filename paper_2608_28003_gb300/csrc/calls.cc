@@ -21,6 +21,7 @@
 
 #include <cmath>
 #include <cstring>
+#include <mutex>
 
 #include "../../include/w8a8.h"
 
@@ -274,6 +275,18 @@ w8a8_status unlocked(F f) {
   Py_BEGIN_ALLOW_THREADS st = f();
   Py_END_ALLOW_THREADS return st;
 }
+// The same of a call over workspace `ws`, which threads that share a stream share too: a call's launches stay together in the stream, as
+// what one leaves in the workspace (codes, partial sums) the next one reads.  A lock stands for several workspaces, so that none is made or
+// kept for one.
+template <class F>
+w8a8_status unlocked(const void* ws, F f) {
+  static std::mutex locks[61];
+  std::mutex& mine = locks[(reinterpret_cast<uintptr_t>(ws) >> 9) % 61];
+  return unlocked([&] {
+    const std::lock_guard<std::mutex> held(mine);
+    return f();
+  });
+}
 
 // (w, X, bias, out, ws, stream) -> Y
 template <class W, class Fill, class Run>
@@ -299,7 +312,7 @@ PyObject* linear_call(PyObject* const* a, const char* name, Fill fill, Run run) 
   if (!workspace(a[4], need, &b) || !check_bits(a[1]) || !ptr_of(a[1], &X) || !ptr_of(a[2], &bias) || !ptr_of(y.p, &Y) ||
       !stream_of(a[5], &st))
     return nullptr;
-  if (!check(name, unlocked([&] { return run(&d, X, (int)M, bias, Y, b.ptr, b.bytes, st); }))) return nullptr;
+  if (!check(name, unlocked(b.ptr, [&] { return run(&d, X, (int)M, bias, Y, b.ptr, b.bytes, st); }))) return nullptr;
   return y.give();
 }
 
@@ -344,7 +357,7 @@ PyObject* py_linear_bf16(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!workspace(a[4], need, &b) || !check_bits(a[0]) || !ptr_of(a[0], &W) || !check_bits(a[1]) || !ptr_of(a[1], &X) ||
       !ptr_of(a[2], &bias) || !ptr_of(y.p, &Y) || !stream_of(a[5], &st))
     return nullptr;
-  if (!check("w8a8_linear_bf16", unlocked([&] { return g_api.bf16(W, N, K, X, (int)M, bias, Y, b.ptr, b.bytes, st); })))
+  if (!check("w8a8_linear_bf16", unlocked(b.ptr, [&] { return g_api.bf16(W, N, K, X, (int)M, bias, Y, b.ptr, b.bytes, st); })))
     return nullptr;
   return y.give();
 }
@@ -395,7 +408,7 @@ PyObject* py_ffn_block(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !ptr_attr(a[0], s_gate_up_bf16, &d.gate_up_bf16) || !ptr_attr(a[0], s_down_bf16, &d.down_bf16) ||
       !ffn_out(a[2], want_h, a[4], a[5], a[6], d.hidden, d.inter, &o))
     return nullptr;
-  if (!check("w8a8_ffn_block", unlocked([&] {
+  if (!check("w8a8_ffn_block", unlocked(o.b.ptr, [&] {
                return g_api.ffn(&d, (int)prec, o.X, (int)o.M, o.Y, o.H, o.b.ptr, o.b.bytes, o.st);
              })))
     return nullptr;
@@ -413,7 +426,7 @@ PyObject* py_fp8_ffn_block(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !weight_desc(gu.p, &d.gate_up) || !weight_desc(dn.p, &d.down) ||
       !ffn_out(a[1], want_h, a[3], a[4], a[5], d.hidden, d.inter, &o))
     return nullptr;
-  if (!check("w8a8_fp8_ffn_block", unlocked([&] {
+  if (!check("w8a8_fp8_ffn_block", unlocked(o.b.ptr, [&] {
                return g_api.fp8_ffn(&d, o.X, (int)o.M, o.Y, o.H, o.b.ptr, o.b.bytes, o.st);
              })))
     return nullptr;
@@ -462,7 +475,7 @@ PyObject* py_lm_head(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !check_bits(a[2]) || !ptr_of(a[2], &X) || !ptr_of(tp.p, &T) || !stream_of(a[7], &st))
     return nullptr;
   if (!check("w8a8_lm_head",
-             unlocked([&] { return g_api.head(&d, (int)prec, X, (int)M, L, T, b.ptr, b.bytes, st); })))
+             unlocked(b.ptr, [&] { return g_api.head(&d, (int)prec, X, (int)M, L, T, b.ptr, b.bytes, st); })))
     return nullptr;
   return PyTuple_Pack(2, lg.p, tp.p);
 }
@@ -774,7 +787,7 @@ PyObject* py_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!check("w8a8_paged_attention_workspace_size", g_api.paged_ws(&p.c, n_q, &bytes)) ||
       !(a[6] == Py_None ? stream_workspace(a[2], a[7], dev, st, bytes, &b) : workspace(a[6], bytes, &b)))
     return nullptr;
-  if (!check("w8a8_paged_attention", unlocked([&] {
+  if (!check("w8a8_paged_attention", unlocked(b.ptr, [&] {
                return g_api.paged(&p.c, &p.b, static_cast<uint16_t*>(q.ptr), stride_or(q, 0, dim), stride_or(q, 1, dim), n_q,
                                   (float)scale, (int)window, static_cast<uint16_t*>(out.ptr), stride_or(out, 0, dim),
                                   stride_or(out, 1, dim), b.ptr, b.bytes, st);
@@ -925,7 +938,7 @@ PyObject* py_fp4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!check("w8a8_fp4_linear_workspace_size", g_api.fp4_linear_ws(M, w.d.rows, w.d.k, w.d.block, &bytes)) ||
       !(a[5] == Py_None ? stream_workspace(a[1], a[6], dev, st, bytes, &b) : workspace(a[5], bytes, &b)))
     return nullptr;
-  if (!check("w8a8_fp4_linear", unlocked([&] {
+  if (!check("w8a8_fp4_linear", unlocked(b.ptr, [&] {
                return g_api.fp4_linear(&w.d, x.type, x.ptr, stride_or(x, 0, x.size[1]), M, static_cast<float*>(bias.ptr), type,
                                        y.ptr, M > 1 ? y.stride[0] : y.size[1], b.ptr, b.bytes, st);
              })))
@@ -1034,7 +1047,7 @@ PyObject* py_fp4_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!check("w8a8_fp4_paged_attention_workspace_size", g_api.fp4_paged_ws(&p.c, n_q, &bytes)) ||
       !(a[6] == Py_None ? stream_workspace(a[2], a[7], dev, st, bytes, &b) : workspace(a[6], bytes, &b)))
     return nullptr;
-  if (!check("w8a8_fp4_paged_attention", unlocked([&] {
+  if (!check("w8a8_fp4_paged_attention", unlocked(b.ptr, [&] {
                return g_api.fp4_paged(&p.c, &p.b, q.type, static_cast<uint16_t*>(q.ptr), stride_or(q, 0, dim),
                                       stride_or(q, 1, dim), n_q, (float)scale, (int)window, static_cast<uint16_t*>(out.ptr),
                                       stride_or(out, 0, dim), stride_or(out, 1, dim), b.ptr, b.bytes, st);
