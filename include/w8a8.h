@@ -643,6 +643,11 @@ w8a8_status w8a8_fp4_linear_workspace_size(int M, int N, int K, int block, size_
 w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void* X, int64_t x_row, int M, const float* bias,
                             int out_dtype, void* Y, int64_t y_row, void* workspace, size_t ws_bytes, void* stream);
 
+/* w8a8_paged_attention_check and w8a8_paged_attention_error_word for the calls of w8a8_fp4_linear: whether a wait of theirs on the
+ * current device gave up since the last check, whichever workspace they had. */
+w8a8_status w8a8_fp4_linear_check(void* stream);
+w8a8_status w8a8_fp4_linear_error_word(uint32_t** word);
+
 /* A paged cache in 4 bits: k and v codes [n_pages, page_size, n_kv, head_dim / 2] with common strides in bytes (multiples of 16,
  * codes of a head contiguous), k_scales and v_scales e4m3 [n_pages, page_size, n_kv, head_dim / 16] with theirs (multiples of
  * head_dim / 16 bytes): either order of slots and heads.  A value is code * scale * 2^k_exp (v_exp): the exponents, within

@@ -220,6 +220,8 @@ SIGNATURES = {
     "w8a8_fp4_dequantize": (_i32, [ctypes.POINTER(Fp4C), _i32, _vp, _i64, _vp]),
     "w8a8_fp4_linear_workspace_size": (_i32, [_i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
     "w8a8_fp4_linear": (_i32, [ctypes.POINTER(Fp4C), _i32, _vp, _i64, _i32, _vp, _i32, _vp, _i64, _vp, _sz, _vp]),
+    "w8a8_fp4_linear_check": (_i32, [_vp]),
+    "w8a8_fp4_linear_error_word": (_i32, [ctypes.POINTER(_vp)]),
     "w8a8_fp4_rope_append": (_i32, [ctypes.POINTER(RopeTableC), ctypes.POINTER(PagedCacheFp4C), ctypes.POINTER(PagedBatchC),
                                     _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]),
     "w8a8_fp4_paged_attention_workspace_size": (_i32, [ctypes.POINTER(PagedCacheFp4C), _i32, ctypes.POINTER(_sz)]),
@@ -846,6 +848,12 @@ def fp4_linear(w: Fp4Tensor, X: torch.Tensor, bias: Optional[torch.Tensor] = Non
     if dtype is None:
         dtype = X.dtype if out is None else out.dtype
     return (_CALLS or _calls()).fp4_linear(w, X, bias, dtype, out, ws, None)
+
+
+def fp4_linear_check(stream=None) -> None:
+    """Raise W8A8Error(ERR_TIMEOUT) if a wait in a call of fp4_linear on the current device gave up since the last check, with any
+    workspace or in a captured graph."""
+    _check("w8a8_fp4_linear_check", lib().w8a8_fp4_linear_check(_stream(stream)))
 
 
 @dataclass

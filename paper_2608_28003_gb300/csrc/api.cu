@@ -420,6 +420,19 @@ w8a8_status w8a8::take_error_word(unsigned int* err, cudaStream_t st) {
             "affected calls are undefined", host);
   return W8A8_ERR_TIMEOUT;
 }
+w8a8_status w8a8::device_word(const void* symbol, unsigned int* (&known)[64], unsigned int** word) {
+  int dev = 0;
+  W8A8_CUDA(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64 && known[dev]) {
+    *word = known[dev];
+    return W8A8_OK;
+  }
+  void* p = nullptr;
+  W8A8_CUDA(cudaGetSymbolAddress(&p, symbol));
+  *word = static_cast<unsigned int*>(p);
+  if (dev >= 0 && dev < 64) known[dev] = *word;
+  return W8A8_OK;
+}
 extern "C" const char* w8a8_last_error(void) { return get_error(); }
 
 // ---------------------------------------------------------------------------- linear

@@ -19,18 +19,8 @@ __device__ unsigned int g_gave_up;  // DevErr bits of any call on this device si
 }  // namespace
 
 w8a8_status gave_up_word(unsigned int** word) {
-  static unsigned int* at[64] = {};
-  int dev = 0;
-  W8A8_CUDA(cudaGetDevice(&dev));
-  if (dev >= 0 && dev < 64 && at[dev]) {
-    *word = at[dev];
-    return W8A8_OK;
-  }
-  void* p = nullptr;
-  W8A8_CUDA(cudaGetSymbolAddress(&p, g_gave_up));
-  *word = static_cast<unsigned int*>(p);
-  if (dev >= 0 && dev < 64) at[dev] = *word;
-  return W8A8_OK;
+  static unsigned int* known[64] = {};
+  return device_word(&g_gave_up, known, word);
 }
 
 // Up to 16 rows a sequence and key/value head go to the kernel for tokens, more to the one for chunks (a longer sequence in

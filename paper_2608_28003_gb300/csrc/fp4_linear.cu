@@ -20,7 +20,8 @@
 // 170 MB at 5.0 TB/s and 0.73 of the copy rate; 2048 tokens 1152 -> 13824 27 us, 22 of them in the product, where
 // 167 MB of operands from L2 and 57 MB of outputs bound it, not the tensor cores (8.4 us at four times the bf16 rate).
 //
-// Every wait is bounded: on timeout a bit of the workspace's error word is set and the CTA passes its units without waiting.
+// Every wait is bounded: on timeout a bit is set in the workspace's error word and in the device's, as the stream's own scratch and a
+// captured call's are out of the caller's reach, and the CTA passes its units without waiting.
 #include <algorithm>
 
 #include "fp4.cuh"
@@ -31,6 +32,8 @@
 namespace w8a8 {
 
 namespace {
+
+__device__ unsigned int g_gave_up;  // DevErr bits of any call on this device since the last check
 
 constexpr int kKStage = 256;  // columns of a stage
 
@@ -62,7 +65,7 @@ struct Fp4Args {
   const float *x_scale, *w_scale, *bias;  // row scales: tokens', channels'
   char* y;
   int64_t y_row;  // elements
-  unsigned int* err;
+  unsigned int *err, *gave_up;  // the workspace's word of waits that gave up, the device's
   int M, N, K;              // tokens, channels
   int a_tiles, b_tiles;     // of A's and B's rows
   int a_blocks, b_blocks;   // 128-row blocks of their scales
@@ -132,6 +135,10 @@ __device__ __forceinline__ float ld_peer(uint32_t at) {
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void give_up(const Fp4Args& a, unsigned int bits) {
+  atomicOr(a.err, bits);
+  atomicOr(a.gave_up, bits);
 }
 __device__ __forceinline__ void put_one(const Fp4Args& a, int64_t at, float v) {
   if (a.out == W8A8_TYPE_F32)
@@ -296,10 +303,10 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
         __syncwarp();
       }
     }
-    if (!ok && lane == 0) atomicOr(a.err, DEVERR_PRODUCER_WAIT);
+    if (!ok && lane == 0) give_up(a, DEVERR_PRODUCER_WAIT);
     for (int i = max(0, g - C::kStages); i < g; ++i)  // the last copies land before the CTA may end
       if (!mbar_wait_warp(full(i % C::kStages), (uint32_t)(i / C::kStages) & 1u, kWaitBudgetCycles) && lane == 0)
-        atomicOr(a.err, DEVERR_DRAIN_WAIT);
+        give_up(a, DEVERR_DRAIN_WAIT);
   } else if (warp == 1) {
     // -------------------------------------------------------------------------- products
     int g = 0, n = 0;
@@ -345,11 +352,11 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
         __syncwarp();
       }
     }
-    if (!ok && lane == 0) atomicOr(a.err, DEVERR_PRODUCER_WAIT);
+    if (!ok && lane == 0) give_up(a, DEVERR_PRODUCER_WAIT);
     // every product issued ends before the accumulators go: the last stage's commit says so
     if (g > 0 && !mbar_wait_warp(empty((g - 1) % C::kStages), (uint32_t)((g - 1) / C::kStages) & 1u, kWaitBudgetCycles) &&
         lane == 0)
-      atomicOr(a.err, DEVERR_DRAIN_WAIT);
+      give_up(a, DEVERR_DRAIN_WAIT);
   } else {
     // -------------------------------------------------------------------------- outputs
     pdl_wait();
@@ -502,7 +509,7 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
       }
     }
     if (!kSwap && a.tma_out && elect_one()) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
-    if (!ok && lane == 0) atomicOr(a.err, DEVERR_CONSUMER_WAIT);
+    if (!ok && lane == 0) give_up(a, DEVERR_CONSUMER_WAIT);
     __syncwarp();
   }
   if constexpr (kMT == 1) {
@@ -612,6 +619,11 @@ w8a8_status run_gemm(const w8a8_fp4& x, const w8a8_fp4& w, const Fp4Args& a, int
   return launch<1, 128, false, kBlock>(x, w, a, 16, sms, st);
 }
 
+w8a8_status gave_up_word(unsigned int** word) {
+  static unsigned int* known[64] = {};
+  return device_word(&g_gave_up, known, word);
+}
+
 struct LinearFp4Ws {
   size_t codes, scales, row_scale, total;
 };
@@ -669,7 +681,6 @@ extern "C" w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void*
   w8a8_fp4 x{M, K, w->block, reinterpret_cast<uint8_t*>(base + L.codes), reinterpret_cast<uint8_t*>(base + L.scales),
              reinterpret_cast<float*>(base + L.row_scale)};
   cudaStream_t st = as_stream(stream);
-  W8A8_TRY(launch_fp4_quantize(dtype, X, x_row, x, false, false, st));
   Fp4Args a{};
   a.x_scale = x.row_scale;
   a.w_scale = w->row_scale;
@@ -677,10 +688,24 @@ extern "C" w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void*
   a.y = static_cast<char*>(Y);
   a.y_row = M > 1 ? y_row : round_up((size_t)N, 8);  // one row has no stride
   a.err = reinterpret_cast<unsigned int*>(base + kErrWordOffset);
+  W8A8_TRY(gave_up_word(&a.gave_up));
+  W8A8_TRY(launch_fp4_quantize(dtype, X, x_row, x, false, false, st));
   a.M = M;
   a.N = N;
   a.K = K;
   a.groups = fp4_groups(K, w->block);
   a.out = out_dtype;
   return w->block == 16 ? run_gemm<16>(x, *w, a, d.sms, st) : run_gemm<32>(x, *w, a, d.sms, st);
+}
+
+extern "C" w8a8_status w8a8_fp4_linear_error_word(uint32_t** word) {
+  W8A8_CHECK_ARG(word != nullptr, W8A8_ERR_INVALID_ARG, "w8a8_fp4_linear_error_word: null argument");
+  W8A8_TRY(check_device());
+  return gave_up_word(word);
+}
+
+extern "C" w8a8_status w8a8_fp4_linear_check(void* stream) {
+  unsigned int* word = nullptr;
+  W8A8_TRY(w8a8_fp4_linear_error_word(&word));
+  return take_error_word(word, as_stream(stream));
 }

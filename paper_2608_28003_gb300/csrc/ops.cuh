@@ -14,6 +14,8 @@ w8a8_status dev_info(DevInfo* out);
 int device_sms();
 // waits for the stream, reads and clears a word of DevErr bits: W8A8_ERR_TIMEOUT if any was set
 w8a8_status take_error_word(unsigned int* err, cudaStream_t st);
+// The current device's address of a __device__ word (symbol: its address on the host), kept in `known` by device.
+w8a8_status device_word(const void* symbol, unsigned int* (&known)[64], unsigned int** word);
 
 struct LinearWs {
   size_t xf16, sx, part, total;
