@@ -16,6 +16,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/core/DimVector.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -172,8 +173,17 @@ bool qweight_attr(PyObject* o, PyObject* name, w8a8_qweight* d) {  // zeros wher
 // A tensor that is no subclass; else null.
 const at::Tensor* plain(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
 
+// The interpreter's lock, free while this lives.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  Unlocked() = default;
+  Unlocked(const Unlocked&) = delete;
+  Unlocked& operator=(const Unlocked&) = delete;
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 // torch.empty(size, dtype=dtype, device=like.device) of a plain tensor (null: its size, its type); null without an error for another, or
-// where that fails.
+// where that fails.  Other threads run meanwhile: the allocator may have to wait for the driver.
 PyObject* quick_empty(PyObject* like, const at::IntArrayRef* size, PyObject* dtype) {
   const at::Tensor* x = plain(like);
   if (!x) return nullptr;
@@ -185,7 +195,12 @@ PyObject* quick_empty(PyObject* like, const at::IntArrayRef* size, PyObject* dty
                                 : dtype == g_u8   ? at::kByte
                                                   : at::ScalarType::Undefined;
     if (type == at::ScalarType::Undefined || !x->is_cuda()) return nullptr;
-    return THPVariable_Wrap(at::empty(size ? *size : x->sizes(), at::TensorOptions().dtype(type).device(x->device())));
+    const at::TensorOptions options = at::TensorOptions().dtype(type).device(x->device());
+    const at::DimVector extents(size ? *size : x->sizes());
+    return THPVariable_Wrap([&] {
+      const Unlocked free;
+      return at::empty(extents, options);
+    }());
   } catch (...) {
     PyErr_Clear();
     return nullptr;

@@ -1,0 +1,71 @@
+"""While a call allocates its output, other threads of the program run: an allocation can wait for the driver."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+ALLOCATOR = """
+#include <cuda_runtime.h>
+#include <unistd.h>
+extern "C" int slow;
+int slow = 0;
+extern "C" void* get(ssize_t size, int device, cudaStream_t) {
+  if (slow) usleep(400000);
+  void* p = nullptr;
+  return cudaMalloc(&p, size > 0 ? size : 1) == cudaSuccess ? p : nullptr;
+}
+extern "C" void put(void* p, ssize_t, int, cudaStream_t) { cudaFree(p); }
+"""
+
+PROGRAM = """
+import ctypes, sys, threading, time
+import torch
+torch.cuda.memory.change_current_allocator(torch.cuda.memory.CUDAPluggableAllocator(sys.argv[1], "get", "put"))
+from paper_2608_28003_gb300 import binding as B
+slow = ctypes.c_int.in_dll(ctypes.CDLL(sys.argv[1]), "slow")
+x = torch.randn(4, 64, device="cuda").bfloat16()
+table, pos = B.rope_table(B.RopeConfig(64)), torch.zeros(4, device="cuda", dtype=torch.int32)
+calls = [lambda: B.fp4_quantize(x, 32), lambda: B.rope(table, x[:, None], pos)]
+for call in calls:
+    call()
+torch.cuda.synchronize()
+ticks, stop = [], False
+def tick():
+    while not stop:
+        ticks.append(time.perf_counter())
+        time.sleep(0.002)
+t = threading.Thread(target=tick)
+t.start()
+worst = []
+for call in calls:
+    time.sleep(0.1)
+    n = len(ticks)
+    slow.value = 1
+    t0 = time.perf_counter()
+    y = call()
+    took = time.perf_counter() - t0
+    slow.value = 0
+    time.sleep(0.05)
+    seen = ticks[n - 1:]
+    assert took > 0.3, took
+    worst.append(max(b - a for a, b in zip(seen, seen[1:])))
+stop = True
+t.join()
+print("longest silence", worst)
+assert max(worst) < 0.2, worst
+"""
+
+
+def test_other_threads_run_while_an_output_is_allocated(tmp_path):
+    from paper_2608_28003_gb300 import build
+    build.build()
+    src, so = tmp_path / "alloc.cu", tmp_path / "alloc.so"
+    src.write_text(ALLOCATOR)
+    subprocess.run([build.nvcc(), "-shared", "-Xcompiler", "-fPIC", "-cudart", "shared", str(src), "-o", str(so)], check=True)
+    r = subprocess.run([sys.executable, "-c", PROGRAM, str(so)], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-500:] + r.stderr[-2000:]
