@@ -267,7 +267,7 @@ def _calls():
         try:
             from . import _calls as mod
         except ImportError as e:
-            raise RuntimeError("paper_2608_28003_gb300/_calls.so is not built: run "
+            raise RuntimeError("paper_2608_28003_gb300/_calls.so is not built, or not for this PyTorch: run "
                                "paper_2608_28003_gb300.build.build()") from e
         mod.init({name: ctypes.cast(getattr(L, name), _vp).value for name in SIGNATURES}, _check, default_workspace,
                  _DEFAULT_WS, Workspace, stream_workspace, _STREAM_WS)

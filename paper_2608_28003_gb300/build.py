@@ -3,7 +3,8 @@
 Each ``csrc/*.cu`` compiles to an object under ``_build/`` (in parallel), and the objects link
 into ``paper_2608_28003_gb300/libw8a8.so``; ``csrc/calls.cc``, the binding's marshalling, compiles
 to the extension module ``_calls.so`` beside it.  A source newer than its object, or a header newer
-than the library, triggers a rebuild.  No fast-math: every rounding the header documents is an
+than the library, triggers a rebuild; ``_calls.so`` reads tensors where PyTorch's headers say they lie, so another PyTorch or
+interpreter than it was compiled for, or another command, does too.  No fast-math: every rounding the header documents is an
 IEEE operation.
 """
 from __future__ import annotations
@@ -13,6 +14,7 @@ import glob
 import os
 import shutil
 import subprocess
+import sys
 import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -21,6 +23,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libw8a8.so")
 CALLS = os.path.join(PKG, "_calls.so")
+CALLS_STAMP = os.path.join(BUILD, "calls.stamp")  # what _calls.so was compiled with
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
@@ -47,21 +50,49 @@ def _compile(src: str, obj: str, verbose: bool) -> None:
         print(r.stdout, r.stderr)
 
 
+def torch_id() -> str:
+    """The PyTorch that _calls.so is compiled for, which it compares with the one it is loaded beside."""
+    import torch
+    return f"{torch.__version__} {torch.version.git_version}"
+
+
+def _calls_flags() -> list:
+    import torch  # for its headers and libraries: the module reads tensors through them
+    at = os.path.dirname(torch.__file__)
+    return ["-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DW8A8_TORCH="{torch_id()}"',
+            "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(at, "include"),
+            "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+
+
+def _calls_stamp() -> str:
+    """What _calls.so depends on beside its sources."""
+    return "\n".join([*_calls_flags(), sysconfig.get_config_var("SOABI") or "", sys.version])
+
+
 def _compile_calls(src: str) -> None:
     cxx = shutil.which(os.environ.get("CXX", "g++")) or shutil.which("c++")
     if cxx is None:
         raise RuntimeError("g++ not found: it compiles the binding's calls")
-    import torch  # for its headers and libraries: the module reads tensors through them
-    at = os.path.dirname(torch.__file__)
     tmp = CALLS + ".tmp"
-    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(at, "include"),
-           "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"), src, "-o", tmp,
-           "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    flags = _calls_flags()
+    libs = flags.index("-L")
+    r = subprocess.run([cxx, *flags[:libs], src, "-o", tmp, *flags[libs:]], capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed for {os.path.basename(src)}:\n{r.stdout}\n{r.stderr}")
+    if os.path.exists(CALLS_STAMP):  # a module never lies beside another one's stamp
+        os.remove(CALLS_STAMP)
     os.replace(tmp, CALLS)
+    with open(CALLS_STAMP, "w") as f:
+        f.write(_calls_stamp())
+
+
+def _calls_stale(newest: float) -> bool:
+    if not os.path.exists(CALLS) or os.path.getmtime(CALLS) < newest or not os.path.exists(CALLS_STAMP):
+        return True
+    with open(CALLS_STAMP) as f:
+        return f.read() != _calls_stamp()
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -78,7 +109,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     with cf.ThreadPoolExecutor(max_workers=max(1, min(len(jobs), os.cpu_count() or 4))) as ex:
         futs = [ex.submit(_compile, s, o, verbose) for s, o, stale in jobs if stale]
         calls = os.path.join(CSRC, "calls.cc")
-        if force or not os.path.exists(CALLS) or os.path.getmtime(CALLS) < max(os.path.getmtime(calls), hdr_mtime):
+        if force or _calls_stale(max(os.path.getmtime(calls), hdr_mtime)):
             futs.append(ex.submit(_compile_calls, calls))
         for f in futs:
             f.result()

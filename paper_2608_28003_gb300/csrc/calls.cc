@@ -1097,9 +1097,24 @@ PyObject* py_fp4_paged_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return PyTuple_Pack(2, k.p, v.p);
 }
 
+// Whether this is the PyTorch whose headers this file was compiled with: tensors are read at the places those give them.
+bool same_torch(PyObject* torch) {
+  Ref version(PyObject_GetAttrString(torch, "__version__")), more(PyObject_GetAttrString(torch, "version"));
+  Ref git(more ? PyObject_GetAttrString(more.p, "git_version") : nullptr);
+  if (!version || !git) return false;
+  Ref id(PyUnicode_FromFormat("%S %S", version.p, git.p));
+  if (!id) return false;
+  if (PyUnicode_CompareWithASCIIString(id.p, W8A8_TORCH) == 0) return true;
+  PyErr_Format(PyExc_ImportError, "_calls.so is compiled for PyTorch %s, this is %U: run paper_2608_28003_gb300.build.build()",
+               W8A8_TORCH, id.p);
+  return false;
+}
+
 // (addresses: dict name -> int, check, default_workspace, workspace table, Workspace, stream_workspace, its table)
 PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!nargs_are(n, 7, "init")) return nullptr;
+  Ref torch(PyImport_ImportModule("torch")), c(PyImport_ImportModule("torch._C"));
+  if (!torch || !c || !same_torch(torch.p)) return nullptr;
   auto address = [&](const char* name, void* slot) {
     PyObject* v = PyDict_GetItemString(a[0], name);
     const unsigned long long p = v ? PyLong_AsUnsignedLongLong(v) : 0ull;
@@ -1127,8 +1142,6 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !address("w8a8_fp4_paged_attention_workspace_size", &g_api.fp4_paged_ws) ||
       !address("w8a8_fp4_paged_attention", &g_api.fp4_paged) || !address("w8a8_fp4_paged_values", &g_api.fp4_values))
     return nullptr;
-  Ref torch(PyImport_ImportModule("torch")), c(PyImport_ImportModule("torch._C"));
-  if (!torch || !c) return nullptr;
   struct {
     PyObject** to;
     PyObject* from;
