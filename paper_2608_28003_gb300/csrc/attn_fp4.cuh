@@ -19,7 +19,7 @@ __device__ __noinline__ void attend_row_fp4(const Fp4Pages& c, const PagedBatch&
   const uint16_t* q = a.q + row * a.q_row + head * a.q_head;
   const int kvh = head / (a.n_q / c.p.n_kv);
   const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-  const float scale = a.scale * two_to(c.k_exp);
+  const float k_unit = two_to(c.k_exp);
   float m = -INFINITY, l = 0.0f, acc[kDim / 32];
   bool any = false;
 #pragma unroll
@@ -34,22 +34,21 @@ __device__ __noinline__ void attend_row_fp4(const Fp4Pages& c, const PagedBatch&
       float d = 0.0f;
       for (int i = 0; i < kDim / 16; ++i) {
         const uint2 kw = *reinterpret_cast<const uint2*>(c.k + at + 8 * i);
-        const float unit = e4m3_value(c.ks[sat + i]);
+        const float unit = e4m3_value(c.ks[sat + i]) * k_unit;
         const uint4 q0 = *reinterpret_cast<const uint4*>(q + 16 * i), q1 = *reinterpret_cast<const uint4*>(q + 16 * i + 8);
         const uint32_t qa[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
         uint32_t h[8];
         e2m1x8_to_f16(kw.x, *reinterpret_cast<uint32_t(*)[4]>(h));
         e2m1x8_to_f16(kw.y, *reinterpret_cast<uint32_t(*)[4]>(h + 4));
-        float part = 0.0f;
+        // a code times its unit is the key's value, exactly: what fp32 holds of the formula it holds here, whatever the exponent
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float2 x = unpack2<false>(h[e]), y = unpack2<kBf16>(qa[e]);
-          part = fmaf(x.x, y.x, part);
-          part = fmaf(x.y, y.y, part);
+          d = fmaf(x.x * unit, y.x, d);
+          d = fmaf(x.y * unit, y.y, d);
         }
-        d = fmaf(part, unit, d);
       }
-      sc = d * scale;
+      sc = d * a.scale;
     }
     const uint32_t there = __ballot_sync(0xffffffffu, at >= 0);
     if (!there) continue;

@@ -35,10 +35,10 @@
 // Over a cache in 4 bits (Fp4Pages) the products and the softmax are the same; operands are made in shared memory.  Two warps copy codes
 // and scales by TMA into rings of 4.5 KB parts (one for K and the queries, one for V: one for both could not keep up, 266 us against
 // 205), three more turn K's codes into rows of the queries' type, two V's into fp16, which P is
-// then too: a code times its scale has at most six significant bits, so operands are exact, and 2^k_exp and 2^v_exp are applied to
-// scores and outputs.  The same four chunks over 4 bits, 127 GFLOP: 196 to 200 us (0.92 of the 16-bit kernel's rate; with fp16
+// then too: a code times its scale has at most six significant bits, so operands are exact; 2^v_exp is applied to outputs, 2^k_exp to
+// K in bf16 and to scores with fp16.  The same four chunks over 4 bits, 127 GFLOP: 195 us (0.93 of the 16-bit kernel's rate; with fp16
 // queries 188), from 516 with codes read straight from memory by seven warps.  The makers, five warps beside eight of softmax, are what
-// is short where the softmax is not: a prompt of 2048 tokens at head dim 256 takes 43.7 us, 29 over 16 bits.  Their loops are not
+// is short where the softmax is not: a prompt of 2048 tokens at head dim 256 takes 44 us, 29 over 16 bits.  Their loops are not
 // unrolled, nor is a unit read ahead of the one before's making (199): their code was larger than the instruction caches, and slower;
 // nine makers leave the softmax 96 registers, which spill.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
@@ -137,24 +137,31 @@ __host__ __device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c
 // ------------------------------------------------------------------------------------ operands from 4 bits
 // Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  A code times its scale has six
 // significant bits and lies within fp16's range as within bf16's, so operands are exact in either type: K has the queries', V is fp16
-// whatever the type, as the weights are.
+// whatever the type, as the weights are.  In bf16 K has 2^k_exp (`unit`) in its scales as well, between 2^-110 and 2^112 in all: fp32 then
+// holds the products with queries of any size that it holds in the formula (fp16 queries times codes are below 2^36).
 // Into a row of a 64-dim column (128-byte rows, swizzled): `at` is the row, `swz` its part and swizzle.
 // To bf16 by way of fp32, on two pipes; fp16's bits shifted into a bf16's place took three operations a pair more of the one that
 // codes are converted on (203 us for the four chunks above, 196 so).
 template <bool kToBf16>
-__device__ __forceinline__ void store_unit(const uint4& codes, uint32_t sc, uint32_t at, uint32_t swz) {
+__device__ __forceinline__ void store_unit(const uint4& codes, uint32_t sc, uint32_t at, uint32_t swz, float unit = 1.0f) {
   const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
-  const uint32_t h2 = e4m3x2_to_f16x2(sc), s0 = __byte_perm(h2, h2, 0x1010), s1 = __byte_perm(h2, h2, 0x3232);
+  uint32_t h2 = e4m3x2_to_f16x2(sc);
+  if constexpr (kToBf16) {
+    const float2 f = unpack2<false>(h2);
+    h2 = pack2<true>(f.x * unit, f.y * unit);
+  }
+  const uint32_t s0 = __byte_perm(h2, h2, 0x1010), s1 = __byte_perm(h2, h2, 0x3232);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     uint32_t h[4];
     e2m1x8_to_f16(w[i], h);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      h[e] = hmul2_bits(h[e], i < 2 ? s0 : s1);
       if constexpr (kToBf16) {
         const float2 f = unpack2<false>(h[e]);
-        h[e] = pack2<true>(f.x, f.y);
+        h[e] = bmul2_bits(pack2<true>(f.x, f.y), i < 2 ? s0 : s1);
+      } else {
+        h[e] = hmul2_bits(h[e], i < 2 ? s0 : s1);
       }
     }
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (swz ^ (uint32_t)(i << 4))), "r"(h[0]), "r"(h[1]), "r"(h[2]),
@@ -243,6 +250,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
         const uint32_t to0 = (uint32_t)(key0 * 128), swz = (uint32_t)((4 * half) ^ (key0 & 7)) << 4;
         // bytes between keys in a part; K: 64 dims, V: all
         const uint32_t row = kv ? kDim / 2 : 32, srow = kv ? kDim / 16 : 4;
+        const float k_unit = two_to(pages.k_exp);
         int r = 0;  // parts so far
         for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
           const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
@@ -277,7 +285,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
                 if (kv)
                   store_unit<false>(x, sc, at, swz);
                 else
-                  store_unit<kBf16>(x, sc, at, swz);
+                  store_unit<kBf16>(x, sc, at, swz, k_unit);
               }
               asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
               __syncwarp();
@@ -548,7 +556,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
       const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
       const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
       const float sc = [&] {
-        if constexpr (kFp4) return ldexpf(a.scale * kLog2e, pages.k_exp);
+        if constexpr (kFp4 && !kBf16) return ldexpf(a.scale * kLog2e, pages.k_exp);  // (in bf16 K has it)
         return a.scale * kLog2e;
       }();
       const float back = [&] {
