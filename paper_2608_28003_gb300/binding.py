@@ -795,10 +795,6 @@ class Fp4Tensor:
         t = self.scales.view(-(-n // 128), g, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(-1, 4 * g)
         return t[:n, :self.k // self.block]
 
-    def c(self) -> Fp4C:
-        return Fp4C(self.rows, self.k, self.block, self.codes.data_ptr(), self.scales.data_ptr(),
-                    self.row_scale.data_ptr() if self.row_scale is not None else None)
-
 
 def fp4_tensor(codes: torch.Tensor, block_scales: torch.Tensor, row_scale: Optional[torch.Tensor] = None) -> Fp4Tensor:
     """An Fp4Tensor of a matrix quantised elsewhere: codes uint8 [rows, k / 2], scale bytes uint8 [rows, k / 16] (e4m3) or
@@ -867,15 +863,6 @@ class PagedCacheFp4:
     v_scales: torch.Tensor
     k_exp: int = 0
     v_exp: int = 0
-
-    def c(self) -> PagedCacheFp4C:
-        k, s = self.k, self.k_scales
-        n, page, heads, half = k.shape
-        st = [max(-(-x // 16) * 16, half) if e <= 1 else x for x, e in zip(k.stride(), k.shape)]
-        sb = half // 8
-        ss = [max(-(-x // sb) * sb, sb) if e <= 1 else x for x, e in zip(s.stride(), s.shape)]
-        return PagedCacheFp4C(n, page, heads, 2 * half, self.k_exp, self.v_exp, st[0], st[1], st[2], ss[0], ss[1], ss[2],
-                              k.data_ptr(), self.v.data_ptr(), s.data_ptr(), self.v_scales.data_ptr())
 
 
 def paged_cache_fp4(n_pages: int, page_size: int, n_kv: int, head_dim: int, device=None, k_exp: int = 0,

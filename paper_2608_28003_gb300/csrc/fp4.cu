@@ -120,12 +120,10 @@ __device__ __forceinline__ uint32_t quantise_unit(const Unit16<kType>& u, uint32
 template <int kType, int kBlock, bool kWarp, int kHeld>
 __global__ void __launch_bounds__(512) fp4_quantise_kernel(const char* __restrict__ x, int64_t x_row_bytes, int rows, int padded,
                                                            int k, int tpr, uint8_t* __restrict__ codes,
-                                                           uint8_t* __restrict__ scales, float* __restrict__ row_scale,
-                                                           int settled) {
+                                                           uint8_t* __restrict__ scales, float* __restrict__ row_scale) {
   __shared__ uint32_t s_top[16];
-  if (settled) pdl_trigger();
   pdl_wait();
-  if (!settled) pdl_trigger();
+  pdl_trigger();  // (behind the wait: a product may read its weights ahead of its own)
   const int units = k / 16, groups = fp4_groups(k, kBlock), lane = threadIdx.x & 31;
   const int step = kWarp ? tpr : (int)blockDim.x;
   const int64_t row = kWarp ? ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / tpr : (int64_t)blockIdx.x;
@@ -291,8 +289,7 @@ w8a8_status check_fp4(const char* who, const w8a8_fp4* q) {
 // 54), and rows of up to 128 units a warp each, four a block (262144 rows of 1152: 149 and 242 us; 263 and 264 with one).  The others
 // have one, for the shortest chain (2048 rows of 1152: 2.6 and 3.4 us; with up to four 2.8 and 4.0).  Blocks of 16 are bound by
 // instructions: with a division by 6 and a reciprocal of two instructions each (Block16) 27.7, 208 and 3.0 us.
-w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, bool settled,
-                                cudaStream_t st) {
+w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, cudaStream_t st) {
   const int units = q.k / 16, padded = pad ? (int)round_up((size_t)q.rows, 128) : q.rows;
   int tpr = q.block / 4;  // four blocks' scales meet within a row's lanes
   while (tpr < units && tpr < 32) tpr *= 2;
@@ -305,7 +302,7 @@ w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w
   const int64_t blocks = warp ? ((int64_t)padded * tpr + 127) / 128 : padded;
   auto go = [&](auto kernel) {
     return launch_pdl(kernel, dim3((unsigned)blocks), dim3((unsigned)threads), 0, st, static_cast<const char*>(x),
-                      x_row * type_bytes(dtype), q.rows, padded, q.k, tpr, q.codes, q.scales, q.row_scale, (int)settled);
+                      x_row * type_bytes(dtype), q.rows, padded, q.k, tpr, q.codes, q.scales, q.row_scale);
   };
   auto of = [&](auto type) {
     constexpr int kT = decltype(type)::value;
@@ -348,7 +345,7 @@ extern "C" w8a8_status w8a8_fp4_quantize(int dtype, const void* x, int64_t x_row
   W8A8_CHECK_ARG(x != nullptr, W8A8_ERR_INVALID_ARG, "%s: null x", who);
   W8A8_CHECK_ARG(aligned16(x), W8A8_ERR_ALIGN, "%s: x must be 16-byte aligned", who);
   W8A8_TRY(check_device());
-  return launch_fp4_quantize(dtype, x, x_row, *q, true, false, as_stream(stream));
+  return launch_fp4_quantize(dtype, x, x_row, *q, true, as_stream(stream));
 }
 
 extern "C" w8a8_status w8a8_fp4_dequantize(const w8a8_fp4* q, int dtype, void* y, int64_t y_row, void* stream) {

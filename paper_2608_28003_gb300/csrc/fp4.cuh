@@ -96,8 +96,7 @@ __host__ __device__ __forceinline__ int fp4_groups(int k, int block) { return (k
 constexpr int kMaxFp4Rows = 0x7fffff80;  // whole 128-row blocks of scales stay within an int
 w8a8_status check_fp4(const char* who, const w8a8_fp4* q);
 // (no argument checks).  pad: rows beyond q.rows, up to a multiple of 128, get scales of 0 as well.
-w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, bool settled,
-                                cudaStream_t st);
+w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, cudaStream_t st);
 inline int type_bytes(int dtype) { return dtype == W8A8_TYPE_F32 ? 4 : 2; }
 
 // ------------------------------------------------------------------------------- cache

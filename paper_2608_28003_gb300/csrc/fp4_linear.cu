@@ -689,7 +689,7 @@ extern "C" w8a8_status w8a8_fp4_linear(const w8a8_fp4* w, int dtype, const void*
   a.y_row = M > 1 ? y_row : round_up((size_t)N, 8);  // one row has no stride
   a.err = reinterpret_cast<unsigned int*>(base + kErrWordOffset);
   W8A8_TRY(gave_up_word(&a.gave_up));
-  W8A8_TRY(launch_fp4_quantize(dtype, X, x_row, x, false, false, st));
+  W8A8_TRY(launch_fp4_quantize(dtype, X, x_row, x, false, st));
   a.M = M;
   a.N = N;
   a.K = K;
