@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kThreads)
       }
       if (turned)  // cos and sin are up to the table's factor
 #pragma unroll
-        for (int e = 0; e < kE; ++e) off[e] *= fmaxf(1.0f, t.scale);
+        for (int e = 0; e < kE; ++e) off[e] *= fmaxf(1.0f, fabsf(t.scale));
     } else {
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
