@@ -72,7 +72,7 @@ struct Fp4Args {
   int groups;               // 512-byte pieces a block
   int split;                // CTAs of a cluster, parts of k
   int out;                  // W8A8_TYPE_*
-  int tma_out;              // y by TMA stores
+  int tma_out;              // y by TMA stores: 1 but for a row's last columns, 2 those too
 };
 
 // Instruction descriptor of kind::mxf4nvf4: both operands e2m1 (1 at bits 7 and 10), N >> 3 at bit 17, scales e4m3 (0) or
@@ -444,13 +444,15 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
         // 64 bytes of each of the warp's rows, from column c0 on
         auto put_group = [&](int c0, uint32_t (&w)[16]) {
           if (c0 >= b_end || row0 >= a_end) return;
+          // a store is of whole 16 bytes, those that cross the row's end too: columns beside y are not its to write
+          const bool by_tma = a.tma_out > (c0 + (f32 ? 16 : 32) > b_end ? 1 : 0);
           if (a.tma_out) {
             if (elect_one()) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
             __syncwarp();
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) sts128(to + ((j ^ swz) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-          if (a.tma_out) {
+          if (by_tma) {
             asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             __syncwarp();
             if (elect_one()) {
@@ -460,7 +462,7 @@ __global__ void __launch_bounds__(Cfg<kMT, kBN, kSwap, kBlock>::kThreads, 1)
             __syncwarp();
             return;
           }
-          __syncwarp();  // rows that begin anywhere: a row at a time
+          __syncwarp();  // rows that begin or end anywhere: a row at a time
           const int rows = min(32, a_end - row0), here = min(f32 ? 16 : 32, b_end - c0);
           for (int q = 0; q < rows; ++q)
             if (lane < here) {
@@ -587,7 +589,7 @@ w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int least, i
   W8A8_TRY(make_tmap_2d(&ta, fa.codes, 1, bytes, (uint64_t)fa.rows, bytes, 128, C::kARows));
   W8A8_TRY(make_tmap_2d(&tb, fb.codes, 1, bytes, (uint64_t)fb.rows, bytes, 128, kBN));
   const int e = type_bytes(a.out);
-  a.tma_out = !kSwap && a.y_row * e % 16 == 0;
+  a.tma_out = kSwap || a.y_row * e % 16 != 0 ? 0 : (int64_t)a.N * e % 16 != 0 ? 1 : 2;
   ty = ta;
   if (a.tma_out)
     W8A8_TRY(make_tmap_2d(&ty, a.y, e, (uint64_t)a.N, (uint64_t)a.M, (uint64_t)a.y_row * e, 64 / e, 32, 64));
