@@ -12,14 +12,22 @@ w8a8_status launch_attn_fp4_tokens(const Fp4Pages& pc, const PagedBatch& pb, con
 w8a8_status launch_attn_fp4_chunks(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st);
 
-// attend_row (attn_paged.cuh) with the values a 4-bit cache stands for: one row by one warp, key by key in the order of the formula.
+// attend_row (attn_paged.cuh) with the values a 4-bit cache stands for: one row by one warp, key by key in the order of the formula.  The
+// query is brought to 1 first, and the powers of two are applied last, so that a score that fp32 holds is one whatever its factors are.
 template <bool kBf16, int kDim>
 __device__ __noinline__ void attend_row_fp4(const Fp4Pages& c, const PagedBatch& b, const AttnCall& a, int s, int pos,
                                             int64_t row, int head, int lane, uint32_t* beat) {
   const uint16_t* q = a.q + row * a.q_row + head * a.q_head;
   const int kvh = head / (a.n_q / c.p.n_kv);
   const int lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
-  const float k_unit = two_to(c.k_exp);
+  uint32_t top = 0;
+  for (int i = lane; i < kDim; i += 32) top = max(top, __float_as_uint(unpack2<kBf16>(q[i]).x) & 0x7fffffffu);
+  top = __reduce_max_sync(0xffffffffu, top);
+  const int e = top == 0 || top >= 0x7f800000u ? 0 : min((int)(top >> 23) - 127, 126);
+  const float up = e < -126 ? two_to(126) : two_to(-e);
+  const int se = ilogbf(a.scale), powers = se + max(e, -126) + c.k_exp;  // within 3 x 126
+  const float scale = ldexpf(a.scale, -se), p0 = two_to(powers / 3), p1 = two_to((powers - powers / 3) / 2),
+              p2 = two_to(powers - powers / 3 - (powers - powers / 3) / 2);
   float m = -INFINITY, l = 0.0f, acc[kDim / 32];
   bool any = false;
 #pragma unroll
@@ -34,21 +42,20 @@ __device__ __noinline__ void attend_row_fp4(const Fp4Pages& c, const PagedBatch&
       float d = 0.0f;
       for (int i = 0; i < kDim / 16; ++i) {
         const uint2 kw = *reinterpret_cast<const uint2*>(c.k + at + 8 * i);
-        const float unit = e4m3_value(c.ks[sat + i]) * k_unit;
+        const float unit = e4m3_value(c.ks[sat + i]);
         const uint4 q0 = *reinterpret_cast<const uint4*>(q + 16 * i), q1 = *reinterpret_cast<const uint4*>(q + 16 * i + 8);
         const uint32_t qa[8] = {q0.x, q0.y, q0.z, q0.w, q1.x, q1.y, q1.z, q1.w};
         uint32_t h[8];
         e2m1x8_to_f16(kw.x, *reinterpret_cast<uint32_t(*)[4]>(h));
         e2m1x8_to_f16(kw.y, *reinterpret_cast<uint32_t(*)[4]>(h + 4));
-        // a code times its unit is the key's value, exactly: what fp32 holds of the formula it holds here, whatever the exponent
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 x = unpack2<false>(h[e]), y = unpack2<kBf16>(qa[e]);
-          d = fmaf(x.x * unit, y.x, d);
-          d = fmaf(x.y * unit, y.y, d);
+        for (int j = 0; j < 8; ++j) {
+          const float2 x = unpack2<false>(h[j]), y = unpack2<kBf16>(qa[j]);
+          d = fmaf(x.x * unit, y.x * up, d);
+          d = fmaf(x.y * unit, y.y * up, d);
         }
       }
-      sc = d * a.scale;
+      sc = d * scale * p0 * p1 * p2;
     }
     const uint32_t there = __ballot_sync(0xffffffffu, at >= 0);
     if (!there) continue;

@@ -36,12 +36,15 @@
 // and scales by TMA into rings of 4.5 KB parts (one for K and the queries, one for V: one for both could not keep up, 266 us against
 // 205), three more turn K's codes into rows of the queries' type, two V's into fp16, which P is
 // then too: a code times its scale has at most six significant bits, so operands are exact; 2^v_exp is applied to outputs, 2^k_exp to
-// K in bf16 and to scores with fp16.  The same four chunks over 4 bits, 127 GFLOP: 195 us (0.93 of the 16-bit kernel's rate; with fp16
-// queries 188), from 516 with codes read straight from memory by seven warps.  The makers, five warps beside eight of softmax, are what
+// K or to the sums (score_units).  The same four chunks over 4 bits, 127 GFLOP: 198 us (0.92 of the 16-bit kernel's rate; with fp16
+// queries 186), from 516 with codes read straight from memory by seven warps.  The makers, five warps beside eight of softmax, are what
 // is short where the softmax is not: a prompt of 2048 tokens at head dim 256 takes 44 us, 29 over 16 bits.  Their loops are not
 // unrolled, nor is a unit read ahead of the one before's making (199): their code was larger than the instruction caches, and slower;
 // nine makers leave the softmax 96 registers, which spill.
 // Every wait is bounded: on timeout a bit of the error word is set, and the CTA passes its items without waiting.
+#include <algorithm>
+#include <cmath>
+
 #include "attn_fp4.cuh"
 #include "attn_paged.cuh"
 #include "ops.cuh"
@@ -135,10 +138,19 @@ __host__ __device__ __forceinline__ const PagedCache& shape_of(const PagedCache&
 __host__ __device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c) { return c.p; }
 
 // ------------------------------------------------------------------------------------ operands from 4 bits
+// 2^k_exp times the scale, in powers of two for the exponentials, as a part 2^t (k_unit) in K's operand and a factor (score) on the sums.  With bf16
+// queries the operand has all of the product's exponent that its type leaves room for: a sum of products then is the score but for a
+// factor in [1, 2), so that it lies beyond fp32 only where the score does, whatever the queries' size.  (fp16 queries times codes are
+// below 2^36, and no power of two has room in fp16 beside the codes and their scales.)
+void score_units(float scale, bool bf16, Fp4Pages* c) {
+  const int e = std::ilogb(scale), t = bf16 ? std::min(std::max(e + c->k_exp, -110), 110) : 0;  // codes times scales: [2^-10, 2^12)
+  c->k_unit = std::ldexp(1.0f, t);
+  c->score = std::ldexp(std::ldexp(scale, -e) * kLog2e, e + c->k_exp - t);
+}
+
 // Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  A code times its scale has six
 // significant bits and lies within fp16's range as within bf16's, so operands are exact in either type: K has the queries', V is fp16
-// whatever the type, as the weights are.  In bf16 K has 2^k_exp (`unit`) in its scales as well, between 2^-110 and 2^112 in all: fp32 then
-// holds the products with queries of any size that it holds in the formula (fp16 queries times codes are below 2^36).
+// whatever the type, as the weights are.  In bf16 K has a power of two (`unit`, score_units) in its scales as well.
 // Into a row of a 64-dim column (128-byte rows, swizzled): `at` is the row, `swz` its part and swizzle.
 // To bf16 by way of fp32, on two pipes; fp16's bits shifted into a bf16's place took three operations a pair more of the one that
 // codes are converted on (203 us for the four chunks above, 196 so).
@@ -250,7 +262,6 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
         const uint32_t to0 = (uint32_t)(key0 * 128), swz = (uint32_t)((4 * half) ^ (key0 & 7)) << 4;
         // bytes between keys in a part; K: 64 dims, V: all
         const uint32_t row = kv ? kDim / 2 : 32, srow = kv ? kDim / 16 : 4;
-        const float k_unit = two_to(pages.k_exp);
         int r = 0;  // parts so far
         for (; ok && w.more(); w.next(b, c.page_shift, c.n_kv, a.window, item_tt, kBkShift), ++item) {
           const int lo = w.lo(a.window, item_tt), hi = w.hi(item_tt);
@@ -285,7 +296,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
                 if (kv)
                   store_unit<false>(x, sc, at, swz);
                 else
-                  store_unit<kBf16>(x, sc, at, swz, k_unit);
+                  store_unit<kBf16>(x, sc, at, swz, pages.k_unit);
               }
               asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
               __syncwarp();
@@ -556,7 +567,7 @@ __global__ void __launch_bounds__(Cfg<kDim, std::is_same_v<Pages, Fp4Pages>>::kT
       const uint32_t lanes = tmem + ((uint32_t)(32 * (warp & 3)) << 16);
       const uint32_t otm = lanes + kOCol + (uint32_t)(rt * kDim + hf * (kDim / 2));
       const float sc = [&] {
-        if constexpr (kFp4 && !kBf16) return ldexpf(a.scale * kLog2e, pages.k_exp);  // (in bf16 K has it)
+        if constexpr (kFp4) return pages.score;
         return a.scale * kLog2e;
       }();
       const float back = [&] {
@@ -896,8 +907,10 @@ w8a8_status launch_attn_chunks(const PagedCache& pc, const PagedBatch& pb, const
                         : launch<false, 64>(pc, pb, a, ws, sms, st);
 }
 
-w8a8_status launch_attn_fp4_chunks(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
+w8a8_status launch_attn_fp4_chunks(const Fp4Pages& cache, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st) {
+  Fp4Pages pc = cache;
+  score_units(a.scale, a.bf16, &pc);
   if (a.bf16)
     return a.dim == 256   ? launch<true, 256>(pc, pb, a, ws, sms, st)
            : a.dim == 128 ? launch<true, 128>(pc, pb, a, ws, sms, st)

@@ -31,6 +31,21 @@ def test_far_exponents(B, new, n_q, n_kv, dim, k_exp, up):
     attn_check(B.fp4_paged_attention(cache, batch, q, scale=scale), q, b, scale, 0)
 
 
+@pytest.mark.parametrize("new,n_q,n_kv,dim", [([1, 2], 8, 2, 64), ([1, 1], 4, 1, 256), ([40, 130], 8, 2, 128), ([50, 90], 4, 1, 256),
+                                              ([30, 1, 60], 6, 3, 64)])
+@pytest.mark.parametrize("k_exp,up", [(100, 18), (100, 14), (80, 38), (10, 108), (0, 118), (-100, 118)])
+def test_products_beyond_the_type_that_the_scale_brings_back(B, new, n_q, n_kv, dim, k_exp, up):
+    """Queries times keys around 2^(k_exp + up + 12), up to 2^132, and scores around 64 of which few keys of a row are near the top."""
+    b = fp4_batch(new, [100, 190, 77][:len(new)], 16, n_kv, dim, 5, exps=(-8, 0))
+    b["exps"] = (k_exp, 0)
+    refresh(b)
+    q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 2.0 ** up).bfloat16()
+    cache, batch = objects(B, b)
+    scale = 4.0 * 2.0 ** -(up + k_exp + 8)
+    assert 2.0 ** -126 <= scale
+    attn_check(B.fp4_paged_attention(cache, batch, q, scale=scale), q, b, scale, 0)
+
+
 @pytest.mark.parametrize("new,n_q,n_kv,dim", [([1, 2], 8, 2, 64), ([40, 130], 8, 2, 128), ([50, 90], 4, 1, 256)])
 def test_a_scale_beyond_the_type_with_the_exponent(B, new, n_q, n_kv, dim):
     """scale 2^k_exp = 2^130 is no fp32 number, the scores are."""
