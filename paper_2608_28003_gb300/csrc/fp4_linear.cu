@@ -23,6 +23,7 @@
 // Every wait is bounded: on timeout a bit is set in the workspace's error word and in the device's, as the stream's own scratch and a
 // captured call's are out of the caller's reach, and the CTA passes its units without waiting.
 #include <algorithm>
+#include <atomic>
 
 #include "fp4.cuh"
 #include "ops.cuh"
@@ -556,20 +557,20 @@ cudaLaunchConfig_t config(unsigned grid, int threads, int smem, int split, cudaS
 template <int kMT, int kBN, bool kSwap, int kBlock>
 w8a8_status launch(const w8a8_fp4& x, const w8a8_fp4& w, Fp4Args a, int least, int sms, cudaStream_t st) {
   using C = Cfg<kMT, kBN, kSwap, kBlock>;
-  static bool attr_set[64] = {};
-  static int at_once[64][4] = {};  // clusters of 1, 2, 4, 8 that the GPU holds
+  static std::atomic<bool> known[64] = {};  // whether the attribute is set and at_once filled in, for threads to see in this order
+  static int at_once[64][4] = {};           // clusters of 1, 2, 4, 8 that the GPU holds: a call's sums are split by it
   int dev = 0;
   W8A8_CUDA(cudaGetDevice(&dev));
   W8A8_CHECK_ARG(dev >= 0 && dev < 64, W8A8_ERR_CUDA, "w8a8_fp4_linear: device %d", dev);
   auto kernel = fp4_gemm_kernel<kMT, kBN, kSwap, kBlock>;
   cudaLaunchAttribute attr[2];
-  if (!attr_set[dev]) {
+  if (!known[dev].load(std::memory_order_acquire)) {
     W8A8_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem));
     for (int i = 1; i < 4 && kMT == 1; ++i) {
       const cudaLaunchConfig_t one = config(1u << i, C::kThreads, C::kSmem, 1 << i, st, attr);
       W8A8_CUDA(cudaOccupancyMaxActiveClusters(&at_once[dev][i], kernel, &one));
     }
-    attr_set[dev] = true;
+    known[dev].store(true, std::memory_order_release);
   }
   const w8a8_fp4 &fa = kSwap ? w : x, &fb = kSwap ? x : w;
   a.a_scales = fa.scales;
