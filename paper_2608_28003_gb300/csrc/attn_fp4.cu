@@ -36,8 +36,9 @@ extern "C" w8a8_status w8a8_fp4_paged_attention(const w8a8_paged_cache_fp4* cach
   AttnCall a{q, q_row, q_head, o, o_row, o_head, n_q, dim, window, batch->max_new, scale, dtype == W8A8_TYPE_BF16};
   if (a.window >= 1 << 30) a.window = 0;  // beyond every position
   W8A8_TRY(gave_up_word(&a.gave_up));
-  // up to 16 rows an item: 64 tokens of 4 rows behind 8000 keys at head dim 256 56 us, 149 by the chunk kernel, whose row tiles are 128;
-  // at 16 rows still 45 and 75 (8 x 8 tokens of 2 heads behind 5000 keys), 30 and 45 (4 x 16 behind 2000)
+  // Up to 16 rows an item: 64 tokens of 4 rows behind 8000 keys at head dim 256 43.5 us, 130 by the chunk kernel, whose row tiles are 128.
+  // At 16 rows still 98 and 127 (the 64 with 4 drafted tokens), 66 and 143 (32 x 2 tokens of 8 heads on each of 4 of 128 behind 8000 keys), 47
+  // and 121 (64 x 4 of 4 heads on each of 2 of 64); nearest 24.1 and 26.4 (one sequence of 700 keys, 4 drafted tokens, head dim 256).
   return (long long)a.max_new * (n_q / pc.p.n_kv) <= 16 ? launch_attn_fp4_tokens(pc, pb, a, workspace, d.sms, as_stream(stream))
                                                         : launch_attn_fp4_chunks(pc, pb, a, workspace, d.sms, as_stream(stream));
 }

@@ -3,10 +3,10 @@
 // Both kernels only move data, so HBM bounds them, or for few rows the launch.  A thread holds units of 16 columns: 32 or 64
 // bytes in, 8 bytes of codes out; the scales of four neighbouring blocks meet in one lane, whose word is contiguous in the
 // tiled order.  With blocks of 16 a row's largest magnitude comes first: the row stays in registers over that reduction (up to
-// kHeld units a thread; what is beyond is read again, from L2).  At 8191 rows of 6912 bf16 numbers: quantised in 23.1 us with
-// blocks of 32 (6.2 TB/s), in 27.7 with blocks of 16 (5.2; a row's reduction stands between its loads and stores), back in 24.1
-// and 32.8 (5.9 and 4.4 TB/s; 27.7 with a division a place); before the maxima and quotients were packed two to a register and four
-// units flew together, 75 there and back with blocks of 32.
+// kHeld units a thread; what is beyond is read again, from L2).  At 8191 rows of 6912 bf16 numbers: quantised in 23.0 us with
+// blocks of 32 (6.2 TB/s), in 27.8 with blocks of 16 (5.2; a row's reduction stands between its loads and stores), back in 24.0
+// and 32.8 (6.0 and 4.4 TB/s; with a division a place blocks of 32 took 27.7); before the maxima and quotients were packed two to a
+// register and four units flew together, 75 there and back with blocks of 32.
 #include <algorithm>
 
 #include "fp4.cuh"
@@ -285,10 +285,10 @@ w8a8_status check_fp4(const char* who, const w8a8_fp4* q) {
 }
 
 // Lanes of a warp share its rows while a row's units fit; then a block a row.  What fills the SMs with a thread a unit more than once has
-// lanes of up to four units, whose loads fly together (8191 rows of 6912: 23 us with blocks of 32, 30 with blocks of 16; with one 30 and
-// 54), and rows of up to 128 units a warp each, four a block (262144 rows of 1152: 149 and 242 us; 263 and 264 with one).  The others
-// have one, for the shortest chain (2048 rows of 1152: 2.6 and 3.4 us; with up to four 2.8 and 4.0).  Blocks of 16 are bound by
-// instructions: with a division by 6 and a reciprocal of two instructions each (Block16) 27.7, 208 and 3.0 us.
+// lanes of up to four units, whose loads fly together (8191 rows of 6912: 23.0 us with blocks of 32, 27.8 with blocks of 16; with one 30.2
+// and 39.1), and rows of up to 128 units a warp each, four a block (262144 rows of 1152: 149 and 207 us; 264 and 265 with one).  The
+// others have one, for the shortest chain (2048 rows of 1152: 2.6 and 3.0 us; with up to four 2.8 and 3.5; 16 rows 1.4 and 1.7; 1.9 and
+// 2.5).  Blocks of 16 are bound by instructions.
 w8a8_status launch_fp4_quantize(int dtype, const void* x, int64_t x_row, const w8a8_fp4& q, bool pad, cudaStream_t st) {
   const int units = q.k / 16, padded = pad ? (int)round_up((size_t)q.rows, 128) : q.rows;
   int tpr = q.block / 4;  // four blocks' scales meet within a row's lanes

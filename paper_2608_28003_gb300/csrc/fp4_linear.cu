@@ -11,14 +11,17 @@
 // products on the same pipe.
 // A warp copies, a warp issues, 4 to 16 epilogue warps (a thread per lane of tensor memory) turn accumulators into outputs: through
 // swizzled shared memory and TMA stores where D's lanes are tokens, directly where they are channels, which neighbouring lanes
-// hold.  Units are walked by one CTA an SM, copies running ahead over unit borders, accumulators in two slots where they fit.
+// hold.  Units are walked by one CTA an SM, copies running ahead over unit borders, accumulators in two slots where they fit: not in the
+// 256 x 192 tile of long prompts (384 columns of 512, and three stages of copies), whose next products wait until its accumulators are
+// read.
 // Long rows of few tiles are split over a cluster of up to 8 CTAs, which add up their accumulators through distributed shared memory in
 // the order of their ranks: the same bits every time.
 //
 // Measured, with the quantisation of the tokens ahead of it (2.5 us for few tokens, 5 for 2048): 1 token 1152 -> 6912 6.6 us, 37 tokens
-// 6912 -> 1152 8.1, both latency (two launches, five to eight dependent steps of a microsecond or so); 16 tokens 1152 -> 262144 34.3,
-// 170 MB at 5.0 TB/s and 0.73 of the copy rate; 2048 tokens 1152 -> 13824 27 us, 22 of them in the product, where
-// 167 MB of operands from L2 and 57 MB of outputs bound it, not the tensor cores (8.4 us at four times the bf16 rate).
+// 6912 -> 1152 8.1 (5.4 and 7.0 in a chain of captured calls, whose starts and ends overlap), both latency (two launches, five to eight
+// dependent steps of a microsecond or so); 16 tokens 1152 -> 262144 34.3, 170 MB at 5.0 TB/s and 0.73 of the copy rate; 2048 tokens
+// 1152 -> 13824 27 us, 22 of them in the product, where 167 MB of operands from L2, 57 MB of outputs and the accumulators' one slot bound
+// it, not the tensor cores (8.4 us at four times the bf16 rate).
 //
 // Every wait is bounded: on timeout a bit is set in the workspace's error word and in the device's, as the stream's own scratch and a
 // captured call's are out of the caller's reach, and the CTA passes its units without waiting.
