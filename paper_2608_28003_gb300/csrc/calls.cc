@@ -545,6 +545,7 @@ bool on_device(long long d, long long* dev) {
   return need(d == *dev, "all tensors must be on one device");
 }
 bool extents_fit(const Tensor& t) {
+  if (t.dims == 1 && t.type == kUint8) return true;  // a matrix's scales, whose number is counted in 64 bits
   for (int i = 0; i < t.dims; ++i)
     if (!need(t.size[i] <= INT32_MAX, "a tensor's extent does not fit in 32 bits")) return false;
   return true;
@@ -594,7 +595,7 @@ bool tensor(PyObject* o, long long* dev, Tensor* t) {
   }
   int n;
   if (!on_device(d, dev) || !tuple_of(PyObject_GetAttr(o, s_shape), &t->dims, t->size) ||
-      !tuple_of(call0(o, s_stride), &n, t->stride) || !ptr_of(o, &t->ptr) || !extents_fit(*t))
+      !tuple_of(call0(o, s_stride), &n, t->stride) || !ptr_of(o, &t->ptr))
     return false;
   Ref dt(PyObject_GetAttr(o, s_dtype));
   if (!dt) return false;
@@ -605,7 +606,7 @@ bool tensor(PyObject* o, long long* dev, Tensor* t) {
             : dt.p == g_i64 ? kInt64
             : dt.p == g_u8  ? kUint8
                             : -1;
-  return true;
+  return extents_fit(*t);
 }
 bool tensor_attr(PyObject* o, PyObject* name, long long* dev, Tensor* t, Ref* keep) {
   keep->p = PyObject_GetAttr(o, name);

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_fp4 import DT, _check_matrix, _rows
+from test_gpu_fp4 import DT, _check_linear, _check_matrix, _np, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +30,24 @@ def test_quantise(B, rows, k, dt, block):
     assert same(B.fp4_dequantize(q, torch.float32).double(), want)
     if dt != "f32":
         assert same(B.fp4_dequantize(q, DT[dt]).double(), want)
+
+
+@pytest.mark.parametrize("block", [16, 32])
+def test_more_than_two_gigabytes_of_scales(B, block):
+    """Rows whose scales, or codes, 32 bits do not count (all rows of the matrix are the same memory)."""
+    k = 65536
+    rows = (524289 if block == 16 else 1048577) + 511
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GB")
+    x = torch.randn(1, k, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    q, one = B.fp4_quantize(x.expand(rows, k), block), B.fp4_quantize(x, block)
+    assert q.scales.numel() > 1 << 31
+    for r in (0, 127, 128, 65535, 65536, rows - 129, rows - 1):
+        at = B.Fp4Tensor(q.codes[r:r + 1], q.scales.view(-1, one.scales.numel())[r // 128].roll(-(r % 128 % 32 * 16 + r % 128 // 32 * 4)),
+                         None if block == 32 else q.row_scale[r:r + 1], block)
+        assert torch.equal(at.codes, one.codes) and torch.equal(at.block_scales(), one.block_scales())
+    t = torch.randn(3, k, device="cuda", generator=torch.Generator("cuda").manual_seed(2)).bfloat16()
+    got = B.fp4_linear(q, t)
+    assert got.shape == (3, rows) and bool((got == got[:, :1]).all())
+    tv, wv = (_np(B.fp4_dequantize(a, torch.float32)) for a in (B.fp4_quantize(t, block), one))
+    _check_linear(got[:, :1], tv, wv, None, k)
