@@ -1,6 +1,8 @@
 // Attention over a paged cache in 4 bits: one row exactly, and what its two kernels offer.  Work is divided as in attn_paged.cuh.
 #pragma once
 
+#include <cmath>
+
 #include "attn_paged.cuh"
 #include "fp4.cuh"
 
@@ -11,6 +13,10 @@ w8a8_status launch_attn_fp4_tokens(const Fp4Pages& pc, const PagedBatch& pb, con
 
 w8a8_status launch_attn_fp4_chunks(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st);
+
+// The scale in powers of two for the exponentials, without its own power of two, 2^ilogb(scale): times log2 e a scale need be no fp32 number,
+// or has fewer bits than it had.
+inline float score_significand(float scale) { return std::ldexp(scale, -std::ilogb(scale)) * kLog2e; }
 
 // attend_row (attn_paged.cuh) with the values a 4-bit cache stands for: one row by one warp, key by key in the order of the formula.  The
 // query is brought to 1 first, and the powers of two are applied last, so that a score that fp32 holds is one whatever its factors are.

@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(Cfg<kDim, kNt>::kThreads, 1)
         qs[n][2 * i][lane] = make_uint2(h[0], h[1]);
         qs[n][2 * i + 1][lane] = make_uint2(h[2], h[3]);
       }
-      const float f = ldexpf(a.scale * kLog2e, e + c.k_exp);  // of row 8 n + gq, which lane 4 gq has
+      const float f = ldexpf(c.score, e + c.k_exp + ilogbf(a.scale));  // of row 8 n + gq, which lane 4 gq has
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         fac[n][i] = __shfl_sync(0xffffffffu, f, 4 * (2 * quad + i));
@@ -658,8 +658,10 @@ w8a8_status launch(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, 
 
 }  // namespace
 
-w8a8_status launch_attn_fp4_tokens(const Fp4Pages& pc, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
+w8a8_status launch_attn_fp4_tokens(const Fp4Pages& cache, const PagedBatch& pb, const AttnCall& a, void* ws, int sms,
                                    cudaStream_t st) {
+  Fp4Pages pc = cache;
+  pc.score = score_significand(a.scale);
   const bool wide = (long long)a.max_new * (a.n_q / pc.p.n_kv) > 8;
   auto of = [&](auto bf) {
     constexpr bool kBf = decltype(bf)::value;

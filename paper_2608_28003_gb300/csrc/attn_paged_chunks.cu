@@ -143,9 +143,10 @@ __host__ __device__ __forceinline__ const PagedCache& shape_of(const Fp4Pages& c
 // factor in [1, 2), so that it lies beyond fp32 only where the score does, whatever the queries' size.  (fp16 queries times codes are
 // below 2^36, and no power of two has room in fp16 beside the codes and their scales.)
 void score_units(float scale, bool bf16, Fp4Pages* c) {
-  const int e = std::ilogb(scale), t = bf16 ? std::min(std::max(e + c->k_exp, -110), 110) : 0;  // codes times scales: [2^-10, 2^12)
+  const int power = std::ilogb(scale) + c->k_exp;
+  const int t = bf16 ? std::min(std::max(power, -110), 110) : 0;  // codes times scales lie in [2^-10, 2^12)
   c->k_unit = std::ldexp(1.0f, t);
-  c->score = std::ldexp(std::ldexp(scale, -e) * kLog2e, e + c->k_exp - t);
+  c->score = std::ldexp(score_significand(scale), power - t);
 }
 
 // Sixteen keys by 64 dims of a tile: a lane has 32 dims of a key, 16 bytes of codes and two scales.  A code times its scale has six

@@ -106,7 +106,7 @@ struct Fp4Pages {
   int64_t s_page, s_slot, s_head;
   uint8_t *k, *v, *ks, *vs;
   int k_exp, v_exp;
-  float k_unit = 1.0f, score = 0.0f;  // of attention over chunks (score_units): in K's operand, on sums of products
+  float k_unit = 1.0f, score = 0.0f;  // of attention: in K's operand (chunks), on sums of products
 };
 w8a8_status check_fp4_paged(const char* who, const w8a8_paged_cache_fp4* c, const w8a8_paged_batch* b, Fp4Pages* pc,
                             PagedBatch* pb);

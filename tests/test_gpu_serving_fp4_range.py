@@ -1,8 +1,10 @@
 """Attention over a 4-bit cache whose scores are ordinary numbers, of queries, exponents and scales that are not."""
+import math
+
 import pytest
 import torch
 
-from test_gpu_serving_fp4 import _gen, attn_check, fp4_batch, objects, refresh
+from test_gpu_serving_fp4 import DT, _gen, attn_check, fp4_batch, objects, refresh
 
 pytestmark = pytest.mark.gpu
 
@@ -43,6 +45,23 @@ def test_products_beyond_the_type_that_the_scale_brings_back(B, new, n_q, n_kv, 
     cache, batch = objects(B, b)
     scale = 4.0 * 2.0 ** -(up + k_exp + 8)
     assert 2.0 ** -126 <= scale
+    attn_check(B.fp4_paged_attention(cache, batch, q, scale=scale), q, b, scale, 0)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("new,n_q,n_kv,dim", [([1, 2], 8, 2, 64), ([1, 1], 4, 1, 256), ([40, 130], 8, 2, 128), ([50, 90], 4, 1, 256)])
+@pytest.mark.parametrize("scale", [5 * 2.0 ** -147, 2.0 ** -149, 3 * 2.0 ** -130, 1.5 * 2.0 ** 127])
+def test_scales_at_the_ends_of_the_type(B, dt, new, n_q, n_kv, dim, scale):
+    """A scale below fp32's normal numbers has few bits, which log2 e must not cost it any of; one at the other end times log2 e is none."""
+    b = fp4_batch(new, [100, 190], 16, n_kv, dim, 5, exps=(-8, 0))
+    k_exp = 100 if scale < 1 else -100
+    up = round(-math.log2(scale)) - k_exp - 8  # scores of a few units
+    if dt == "f16":
+        up = max(-10, min(up, 12))
+    b["exps"] = (k_exp, 0)
+    refresh(b)
+    q = (torch.randn(b["n_rows"], n_q, dim, device="cuda", generator=_gen(8)) * 2.0 ** up).to(DT[dt])
+    cache, batch = objects(B, b)
     attn_check(B.fp4_paged_attention(cache, batch, q, scale=scale), q, b, scale, 0)
 
 
