@@ -15,7 +15,7 @@ ALLOCATOR = """
 extern "C" int slow;
 int slow = 0;
 extern "C" void* get(ssize_t size, int device, cudaStream_t) {
-  if (slow) usleep(400000);
+  if (slow) usleep(800000);
   void* p = nullptr;
   return cudaMalloc(&p, size > 0 ? size : 1) == cudaSuccess ? p : nullptr;
 }
@@ -52,12 +52,12 @@ for call in calls:
     slow.value = 0
     time.sleep(0.05)
     seen = ticks[n - 1:]
-    assert took > 0.3, took
+    assert took > 0.7, took
     worst.append(max(b - a for a, b in zip(seen, seen[1:])))
 stop = True
 t.join()
 print("longest silence", worst)
-assert max(worst) < 0.2, worst
+assert max(worst) < 0.6, worst
 """
 
 
